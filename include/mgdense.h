@@ -21,6 +21,7 @@
 #ifndef MGDENSE_H
 #define MGDENSE_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -39,6 +40,7 @@ extern "C" {
 
 #define MG_DTYPE_F32 0
 #define MG_DTYPE_F16 1
+#define MG_DTYPE_BF16 2 /* rows of mg_dropout and mg_group_norm; feature tables are fp32 or fp16 */
 
 #define MG_BACKING_HBM 0  /* the whole feature table lives in device memory */
 #define MG_BACKING_HOST 1 /* the table stays in (preferably pinned) host memory; only the
@@ -501,6 +503,67 @@ int mg_gat_model_free(mg_gat_model* m);
 /* Attention forward pass for every batch of `d`; out_dev (DEVICE) receives one row of dims[k] floats per target, batch
  * after batch in the caller's target order.  Synchronous on the context's stream.  Errors as mg_forward. */
 int mg_gat_forward(mg_ctx* ctx, const mg_gat_model* m, mg_dense* d, float* out_dev);
+
+/* ---- between two layers: dropout, group norm with an activation ---------------------------- */
+
+/* Dropout whose mask comes from a counter-based generator and is never stored.  Element c of a row with key r is kept where the 16-bit
+ * half c % 8 (low half first) of the Philox4x32-10 block with counter (low word of r, high word of r, c / 8, 0x64720000 + site) and
+ * key (seed low, seed high) is at least t = round(65536 p) (to even); what is kept is scaled by 65536 / (65536 - t), what is dropped is
+ * zero, a NaN or an infinity too.  So p is met to 2^-17 and the mean exactly, and the gradient is the same call on the output's gradient.
+ * The mask goes by (seed, site, row key, channel) alone: not by the type, the strides, or how the rows are cut into calls. */
+typedef struct mg_dropout_spec {
+    double p;                /* share to drop, in [0, 1] */
+    uint64_t seed;           /* of the step, say */
+    uint32_t site;           /* which dropout of the program this is, below 65536 */
+    int64_t first_row;       /* row i of the call has the key first_row + i ... */
+    const int64_t* row_keys; /* ... or, where this is not null, row_keys[i]: DEVICE, 8-byte aligned (node ids make a mask that follows the nodes) */
+} mg_dropout_spec;
+
+/* y = dropout(x) for `rows` x `channels` values of `dtype`, rows x_stride / y_stride elements apart.  DEVICE pointers, aligned to their
+ * elements; x's rows may overlap, y's may not; y may be x with the same stride, or lie apart from it.  Rows of whole 16-byte pieces are fastest.  The gradient: x = d_y, y = d_x.
+ * One kernel, queued on `stream` (a cudaStream_t of the context's device; NULL = the default stream), not waited for; it may be captured
+ * into a graph.  Errors: MG_ERR_ARG (2^31 rows or more among them). */
+int mg_dropout(mg_ctx* ctx, const void* x, int64_t x_stride, void* y, int64_t y_stride, int dtype, int64_t rows, int32_t channels,
+               const mg_dropout_spec* spec, void* stream);
+
+#define MG_ACT_NONE 0
+#define MG_ACT_RELU 1
+#define MG_ACT_SILU 2 /* n / (1 + exp(-n)) */
+#define MG_ACT_GELU 3 /* n (1 + erf(n / sqrt 2)) / 2 */
+
+/* Group norm with an activation and a dropout behind it, channels last.  The channels are cut into `groups` equal blocks; the values of
+ * one block over all rows of a sample share their mean and (biased) variance:
+ *   hat = (x - mean) rstd,  rstd = 1 / sqrt(variance + eps),  y = dropout(act(hat weight + bias)).
+ * Samples lie one behind the other: rows_per_sample rows each (1: every row by itself), or, with sample_offsets (HOST, n_samples + 1
+ * entries from 0 on, not decreasing; read during the call), sample s = rows sample_offsets[s] .. sample_offsets[s + 1]: mini-batches of a
+ * packed layer.  A sample may be empty (its mean and rstd are zero); rows behind the last sample are neither read nor written. */
+typedef struct mg_norm_spec {
+    int64_t rows;
+    int32_t channels, groups;
+    int32_t dtype;                     /* of x, y and their gradients; statistics, weight and bias are fp32 */
+    int32_t activation;
+    float eps;
+    int32_t n_samples;                 /* with sample_offsets: 1 .. MG_MAX_BATCHES */
+    const int64_t* sample_offsets;     /* HOST, nullable */
+    int64_t rows_per_sample;           /* without: must divide rows */
+    const float* weight;               /* DEVICE [channels], nullable: ones */
+    const float* bias;                 /* DEVICE [channels], nullable: zeros */
+    const mg_dropout_spec* dropout;    /* HOST, nullable */
+} mg_norm_spec;
+
+/* Bytes of DEVICE memory (16-byte aligned) that the call wants beside its arguments; calls that may run at the same time each want
+ * their own. */
+int mg_group_norm_workspace(mg_ctx* ctx, const mg_norm_spec* spec, int backward, size_t* bytes);
+/* mean, rstd: DEVICE [samples, groups], written.  Strides, streams and capture as mg_dropout; y may be x.  Sums are fp32, in an order that
+ * does not change from run to run.  Errors: MG_ERR_ARG, MG_ERR_CAPACITY (workspace too small). */
+int mg_group_norm(mg_ctx* ctx, const mg_norm_spec* spec, const void* x, int64_t x_stride, void* y, int64_t y_stride, float* mean, float* rstd,
+                  void* workspace, size_t workspace_bytes, void* stream);
+/* Gradients of a scalar loss: d_y = dL/dy in, d_x = dL/dx out, d_weight and d_bias [channels] (DEVICE, nullable), from the forward call's x,
+ * mean and rstd under the same spec (eps is not used).  d_x may be d_y or x.  A ReLU's side of zero is the one that hat weight + bias has in
+ * 64 bits. */
+int mg_group_norm_backward(mg_ctx* ctx, const mg_norm_spec* spec, const void* x, int64_t x_stride, const void* d_y, int64_t d_y_stride,
+                           const float* mean, const float* rstd, void* d_x, int64_t d_x_stride, float* d_weight, float* d_bias,
+                           void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- COMET: partition replacement for link prediction out of core (Section 5.1, Section 6) ----
  * Host-side planning only; no context, no device work.  Partition ids are the physical partitions of

@@ -22,10 +22,12 @@ LIB_PATH = os.path.join(HERE, "libmgdense.so")
 MG_OK = 0
 ERR_NAMES = {-1: "MG_ERR_ARG", -2: "MG_ERR_STATE", -3: "MG_ERR_NONRESIDENT", -4: "MG_ERR_DUPLICATE",
              -5: "MG_ERR_CAPACITY", -6: "MG_ERR_OOM", -7: "MG_ERR_TIMEOUT", -8: "MG_ERR_CUDA"}
-DTYPE_F32, DTYPE_F16 = 0, 1
+DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
 BACKING_HBM, BACKING_HOST = 0, 1
 GEMM_TF32, GEMM_FP32 = 0, 1
 CORRUPT_DST, CORRUPT_SRC, CORRUPT_BOTH = 1, 2, 3
+ROW_TYPES = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}      # of dropout and group_norm
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 # every symbol include/mgdense.h declares
 EXPORTS = [
@@ -34,6 +36,7 @@ EXPORTS = [
     "mg_dense_counts", "mg_dense_view", "mg_dense_export_many", "mg_dense_export_view", "mg_dense_export_copy", "mg_dense_arrays_copy", "mg_dense_export_copy_aligned", "mg_dense_arrays_copy_aligned", "mg_dense_free", "mg_model_create", "mg_model_set_aggregator", "mg_model_set_intermediates", "mg_model_free",
     "mg_forward", "mg_set_layer_window", "mg_keep_layer_outputs", "mg_forward_host_async", "mg_wait_output", "mg_forward_noalloc", "mg_gather_h0", "mg_layer_output", "mg_lp_prepare", "mg_lp_view", "mg_lp_targets", "mg_lp_record_stream", "mg_lp_free",
     "mg_distmult_score", "mg_kernel_launches", "mg_profile", "mg_profile_read", "mg_comet_plan", "mg_comet_bias", "mg_comet_autotune", "mg_gat_model_create", "mg_gat_model_set_heads", "mg_gat_model_free", "mg_gat_forward", "mg_backward", "mg_backward_begin", "mg_backward_end", "mg_model_grads", "mg_model_sgd_step", "mg_model_adagrad_step", "mg_dense_packed_ids", "mg_apply_embedding_sgd",
+    "mg_dropout", "mg_group_norm_workspace", "mg_group_norm", "mg_group_norm_backward",
 ]
 
 
@@ -52,6 +55,16 @@ class DenseArrays(C.Structure):
     _fields_ = [("k", C.c_int32), ("n_nodes", C.c_int32), ("n_sampled", C.c_int32), ("n_entries", C.c_int32),
                 ("node_ids", C.c_void_p), ("node_id_offsets", C.c_void_p), ("nbrs", C.c_void_p),
                 ("nbr_offsets", C.c_void_p), ("repr_map", C.c_void_p)]
+
+
+class DropoutSpec(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("site", C.c_uint32), ("first_row", C.c_int64), ("row_keys", C.c_void_p)]
+
+
+class NormSpec(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("channels", C.c_int32), ("groups", C.c_int32), ("dtype", C.c_int32), ("activation", C.c_int32),
+                ("eps", C.c_float), ("n_samples", C.c_int32), ("sample_offsets", C.c_void_p), ("rows_per_sample", C.c_int64),
+                ("weight", C.c_void_p), ("bias", C.c_void_p), ("dropout", C.c_void_p)]
 
 
 _lib = None
@@ -181,6 +194,43 @@ def _from_dev(ptr, n: int, device) -> torch.Tensor:
     if n == 0 or not ptr:
         return torch.empty(0, dtype=torch.int32, device=device)
     return torch.as_tensor(_DeviceInts(ptr, n), device=device).clone()
+
+
+@dataclass(frozen=True)
+class Dropout:
+    """A dropout whose mask is computed, not stored: a share `p` of the elements, by the seed (of a step, say), the site (which dropout of
+    the program it is) and the key of an element's row -- first_row + its place, or its entry of row_keys (a CUDA tensor of int64: node
+    ids, say).  The same values give the same mask again, which is how the gradient finds it."""
+    p: float
+    seed: int
+    site: int = 0
+    first_row: int = 0
+    row_keys: torch.Tensor | None = None
+
+    def _spec(self, rows: int, device: torch.device) -> DropoutSpec:
+        keys = self.row_keys
+        if keys is not None:
+            assert keys.dtype == torch.int64 and keys.device == device and keys.is_contiguous() and keys.numel() == rows, "row_keys: a contiguous int64 key per row"
+        assert 0 <= self.site < 65536, "a dropout's site must be below 65536"
+        return DropoutSpec(self.p, int(self.seed) & 0xFFFFFFFFFFFFFFFF, self.site, self.first_row, keys.data_ptr() if keys is not None else None)
+
+
+def _matrix(t: torch.Tensor, device: torch.device, like: torch.Tensor | None = None):
+    """A [..., channels] tensor as the library takes it: itself or a copy with its channels one behind the other, and the rows' stride."""
+    assert t.device == device and t.dim() >= 2 and t.dtype in ROW_TYPES, "a CUDA tensor [..., channels] of float32, float16 or bfloat16, on the context's device"
+    assert like is None or (t.shape == like.shape and t.dtype == like.dtype), "tensors of one shape and type"
+    if t.shape[-1] > 1 and t.stride(-1) != 1 or t.dim() > 2 and not t.is_contiguous():
+        t = t.contiguous()
+    return t, t.stride(0) if t.dim() == 2 else t.shape[-1]
+
+
+def _result(out: torch.Tensor | None, like: torch.Tensor):
+    """The caller's tensor for a result, or a new one, and the rows' stride."""
+    if out is None:
+        out = torch.empty(like.shape, dtype=like.dtype, device=like.device)
+    assert out.device == like.device and out.shape == like.shape and out.dtype == like.dtype, "out: a tensor like the input"
+    assert (out.shape[-1] <= 1 or out.stride(-1) == 1) and (out.dim() == 2 or out.is_contiguous()), "out: channels one behind the other"
+    return out, out.stride(0) if out.dim() == 2 else out.shape[-1]
 
 
 @dataclass
@@ -630,3 +680,88 @@ class Context:
         self._check(self.lib.mg_distmult_score(self.handle, lp.handle, _ptr(h), C.c_int32(h.shape[1]), _ptr(rel_emb),
                                                C.c_int32(rel_emb.shape[0]), C.c_int(corrupt), C.c_int(precision), _ptr(pos), _ptr(nd), _ptr(ns)))
         return pos, nd, ns
+
+    # -- between two layers
+    def dropout(self, x: torch.Tensor, drop: Dropout, out: torch.Tensor | None = None) -> torch.Tensor:
+        """x [..., channels] with the elements that `drop` names zeroed and the others scaled up, queued on torch's current stream.  out:
+        where to (x itself, say), else a new tensor."""
+        x, x_stride = _matrix(x, self.device)
+        out, out_stride = _result(out, x)
+        channels = x.shape[-1]
+        rows = x.numel() // channels if channels else 0
+        spec = drop._spec(rows, self.device)
+        self._check(self.lib.mg_dropout(self.handle, _ptr(x), C.c_int64(x_stride), _ptr(out), C.c_int64(out_stride), C.c_int(ROW_TYPES[x.dtype]),
+                                        C.c_int64(rows), C.c_int32(channels), C.byref(spec), _raw_stream(self.device)))
+        return out
+
+    def dropout_backward(self, d_y: torch.Tensor, drop: Dropout, out: torch.Tensor | None = None) -> torch.Tensor:
+        """Gradient of dropout(x, drop) from its output's: the same elements zeroed, the others scaled."""
+        return self.dropout(d_y, drop, out)
+
+    def _norm_spec(self, x, groups, weight, bias, sample_offsets, eps, activation, dropout):
+        channels = x.shape[-1]
+        rows = x.numel() // channels if channels else 0
+        for p in (weight, bias):
+            assert p is None or (p.device == self.device and p.dtype == torch.float32 and p.is_contiguous() and p.numel() == channels), \
+                "weight, bias: a contiguous float32 value per channel"
+        offsets = None
+        if sample_offsets is not None:
+            assert x.dim() == 2, "sample_offsets cut the rows of a matrix"
+            offsets = _host(sample_offsets, torch.int64)
+            samples = offsets.numel() - 1
+        else:
+            per = 1
+            for n in x.shape[1:-1]:
+                per *= n
+            samples = x.shape[0] if per else 0
+        drop = dropout._spec(rows, self.device) if dropout is not None else None
+        spec = NormSpec(rows, channels, groups, ROW_TYPES[x.dtype], ACTIVATIONS[activation], eps, samples if offsets is not None else 0,
+                        offsets.data_ptr() if offsets is not None else None, 1 if offsets is not None or not samples else rows // samples,
+                        weight.data_ptr() if weight is not None else None, bias.data_ptr() if bias is not None else None,
+                        C.addressof(drop) if drop is not None else None)
+        return spec, samples, rows if offsets is None else offsets, drop
+
+    def _norm_workspace(self, spec, backward):
+        need = C.c_size_t(0)
+        self._check(self.lib.mg_group_norm_workspace(self.handle, C.byref(spec), C.c_int(backward), C.byref(need)))
+        return torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None, need
+
+    def group_norm(self, x: torch.Tensor, groups: int, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, sample_offsets=None,
+                   eps: float = 1e-5, activation: str = "none", dropout: Dropout | None = None, out: torch.Tensor | None = None):
+        """dropout(activation(norm(x) * weight + bias)), the mean and the reciprocal deviation [samples, groups].  x is [rows, channels]:
+        every row is a sample by itself or, with sample_offsets (host; first rows and the end of the last), samples lie one behind the
+        other, mini-batches of a packed layer, say; or x is [samples, ..., channels].  activation: "none", "relu", "silu" or "gelu".  Rows
+        behind the last sample stay as they are in `out`, and are zero in a new tensor."""
+        x, x_stride = _matrix(x, self.device)
+        spec, samples, rows, drop = self._norm_spec(x, groups, weight, bias, sample_offsets, eps, activation, dropout)
+        new = out is None
+        out, out_stride = _result(out, x)
+        mean = torch.empty((2, samples, groups), dtype=torch.float32, device=self.device)
+        mean, rstd = mean[0], mean[1]
+        work, need = self._norm_workspace(spec, 0)
+        self._check(self.lib.mg_group_norm(self.handle, C.byref(spec), _ptr(x), C.c_int64(x_stride), _ptr(out), C.c_int64(out_stride), _ptr(mean), _ptr(rstd),
+                                           _ptr(work), need, _raw_stream(self.device)))
+        if new and sample_offsets is not None and int(rows[-1]) < x.shape[0]:
+            out[int(rows[-1]):].zero_()
+        return out, mean, rstd
+
+    def group_norm_backward(self, d_y: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, groups: int, weight: torch.Tensor | None = None,
+                            bias: torch.Tensor | None = None, sample_offsets=None, activation: str = "none", dropout: Dropout | None = None,
+                            out: torch.Tensor | None = None):
+        """Gradients of group_norm from its output's: of x, and of weight and bias (as if they were ones and zeros where they are None).
+        x, mean, rstd and the rest as in the forward call; out may be d_y."""
+        x, x_stride = _matrix(x, self.device)
+        d_y, d_y_stride = _matrix(d_y, self.device, x)
+        spec, samples, rows, drop = self._norm_spec(x, groups, weight, bias, sample_offsets, 1.0, activation, dropout)
+        for s in (mean, rstd):
+            assert s.device == self.device and s.dtype == torch.float32 and s.is_contiguous() and s.shape == (samples, groups), "mean, rstd: as group_norm gave them"
+        new = out is None
+        out, out_stride = _result(out, x)
+        d_weight, d_bias = torch.empty((2, x.shape[-1]), dtype=torch.float32, device=self.device).unbind(0)
+        work, need = self._norm_workspace(spec, 1)
+        self._check(self.lib.mg_group_norm_backward(self.handle, C.byref(spec), _ptr(x), C.c_int64(x_stride), _ptr(d_y), C.c_int64(d_y_stride), _ptr(mean),
+                                                    _ptr(rstd), _ptr(out), C.c_int64(out_stride), _ptr(d_weight), _ptr(d_bias), _ptr(work), need,
+                                                    _raw_stream(self.device)))
+        if new and sample_offsets is not None and int(rows[-1]) < x.shape[0]:
+            out[int(rows[-1]):].zero_()
+        return out, d_weight, d_bias
