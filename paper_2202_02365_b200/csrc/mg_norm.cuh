@@ -4,52 +4,122 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "mg_device.cuh"
 
 constexpr uint32_t kDropTag = 0x64720000u;   // counter word 3 of a dropout's draws; the sampler's and the negatives' are far below or all ones
 
 struct DropArgs {
     int on = 0;
-    uint32_t limit = 0;      // kept: a 16-bit half at or above it
+    uint32_t below = 0;      // kept: a 16-bit half at or above the limit, that is, as the upper half of a word above limit * 65536 - 1
     float factor = 1.f;      // 65536 / (65536 - limit); 0 where all are dropped
     uint32_t k0 = 0, k1 = 0, tag = 0;
     int64_t first_row = 0;
     const int64_t* keys = nullptr;
 };
 
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-// (rounded once, to nearest: off by half a step of the type at most)
-__device__ __forceinline__ void from_float(float v, float* out) { *out = v; }
-__device__ __forceinline__ void from_float(float v, __half* out) { *out = __float2half_rn(v); }
-__device__ __forceinline__ void from_float(float v, __nv_bfloat16* out) { *out = __float2bfloat16_rn(v); }
-
-template <typename T, int VEC> struct alignas(sizeof(T) * VEC) Pack { T v[VEC]; };
+// VEC neighbouring elements of a row as they lie in memory: 2, 4, 8, 16 or 32 bytes in one access
+template <typename T, int VEC> struct Raw {
+    static constexpr int kBytes = (int)sizeof(T) * VEC, kWords = (kBytes + 3) / 4;
+    uint32_t w[kWords];
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) w[i] = 0;
+    }
+    // (volatile, and after what comes before: a row may be read again behind a wait, or be the output too)
+    __device__ __forceinline__ void load(const T* p) {
+        if constexpr (kBytes == 32)
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]) : "l"(p) : "memory");
+        else if constexpr (kBytes == 16) asm volatile("ld.global.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p) : "memory");
+        else if constexpr (kBytes == 8) asm volatile("ld.global.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p) : "memory");
+        else if constexpr (kBytes == 4) asm volatile("ld.global.b32 %0, [%1];" : "=r"(w[0]) : "l"(p) : "memory");
+        else {
+            uint16_t h;
+            asm volatile("ld.global.b16 %0, [%1];" : "=h"(h) : "l"(p) : "memory");
+            w[0] = h;
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const {
+        if constexpr (kBytes == 32)
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+        else if constexpr (kBytes == 16) asm volatile("st.global.v4.b32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+        else if constexpr (kBytes == 8) asm volatile("st.global.v2.b32 [%0], {%1, %2};" ::"l"(p), "r"(w[0]), "r"(w[1]) : "memory");
+        else if constexpr (kBytes == 4) asm volatile("st.global.b32 [%0], %1;" ::"l"(p), "r"(w[0]) : "memory");
+        else asm volatile("st.global.b16 [%0], %1;" ::"l"(p), "h"((uint16_t)w[0]) : "memory");
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else if constexpr (std::is_same<T, __nv_bfloat16>::value) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+        else return __half2float(__ushort_as_half((unsigned short)(w[i / 2] >> (i & 1) * 16)));
+    }
+    // (rounded once, to nearest: off by half a step of the type at most)
+    __device__ __forceinline__ void put(const float (&f)[VEC]) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[i] = __float_as_uint(f[i]);
+        } else if constexpr (VEC == 1) {
+            if constexpr (std::is_same<T, __half>::value) w[0] = __half_as_ushort(__float2half_rn(f[0]));
+            else w[0] = __bfloat16_as_ushort(__float2bfloat16_rn(f[0]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < VEC; i += 2) {
+                if constexpr (std::is_same<T, __half>::value) {
+                    const __half2 h = __floats2half2_rn(f[i], f[i + 1]);
+                    w[i / 2] = reinterpret_cast<const uint32_t&>(h);
+                } else {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(f[i], f[i + 1]);
+                    w[i / 2] = reinterpret_cast<const uint32_t&>(h);
+                }
+            }
+        }
+    }
+};
 
 __device__ __forceinline__ uint64_t drop_key(const DropArgs& d, int64_t row) { return (uint64_t)(d.keys ? d.keys[row] : d.first_row + row); }
 
-// bit i: element c + i of the row with this key is kept (c a multiple of VEC, VEC of 1, 2, 4 or 8): the halves of one Philox block per eight
-// elements.  16 bits an element, so that a block serves 16 or 32 bytes of a row: p is met to 2^-17, and the factor goes by the p that is met.
-template <int VEC>
-__device__ __forceinline__ uint32_t drop_bits(const DropArgs& d, uint64_t key, uint32_t c) {
-    uint32_t w[4];
-    philox4x32_10((uint32_t)key, (uint32_t)(key >> 32), c >> 3, d.tag, d.k0, d.k1, w);
-    uint32_t bits = 0;
+// Which of elements c .. c + VEC - 1 of the row with this key are kept (c a multiple of VEC; VEC of 1, 2, 4 or 8): the halves of one Philox
+// block per eight elements.  16 bits an element, so that a block serves 16 or 32 bytes of a row: p is met to 2^-17, and the factor goes by
+// the p that is met.
+template <int VEC> struct Keep {
+    uint32_t w[(VEC + 1) / 2];
+    __device__ __forceinline__ void draw(const DropArgs& d, uint64_t key, uint32_t c) {
+        uint32_t all[4];
+        philox4x32_10((uint32_t)key, (uint32_t)(key >> 32), c >> 3, d.tag, d.k0, d.k1, all);
+        if constexpr (VEC == 8) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        bits |= (uint32_t)((w[i] & 0xFFFFu) >= d.limit) << (2 * i);
-        bits |= (uint32_t)((w[i] >> 16) >= d.limit) << (2 * i + 1);
+            for (int i = 0; i < 4; ++i) w[i] = all[i];
+        } else if constexpr (VEC == 4) {
+            w[0] = c & 4 ? all[2] : all[0];
+            w[1] = c & 4 ? all[3] : all[1];
+        } else {
+            const uint32_t lo = c & 2 ? all[1] : all[0], hi = c & 2 ? all[3] : all[2];
+            w[0] = c & 4 ? hi : lo;
+            if (VEC == 1 && (c & 1)) w[0] >>= 16;
+        }
     }
-    return VEC == 8 ? bits : bits >> (c & 7u);
-}
+    __device__ __forceinline__ bool operator()(const DropArgs& d, int i) const { return (i & 1 ? w[i / 2] : w[i / 2] << 16) > d.below; }
+};
 
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2, ACT_GELU = 3 };   // MG_ACT_*
 
+// e^x to 2^-22 and |x| 2^-24 (the special function unit's power of two behind one product); 1 / x to 2^-22.  Where an activation uses them, either
+// enters times a factor below one: sums and statistics do without.
+__device__ __forceinline__ float fast_exp(float x) { return __expf(x); }
+
+// (1 + erf(n / sqrt 2)) / 2 to 4 * 2^-24, by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (1.5e-7 off in erf); `bell` =
+// e^(-n^2 / 2), which the slope wants too.  A third of erff's instructions.
+__device__ __forceinline__ float normal_cdf(float n, float* bell) {
+    const float z = fabsf(n) * 0.70710678118654752f, t = __fdividef(1.f, fmaf(0.3275911f, z, 1.f));
+    *bell = fast_exp(-0.5f * n * n);
+    const float tail = 0.5f * *bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    return n < 0.f ? tail : 1.f - tail;
+}
+
 __device__ __forceinline__ float act_value(int act, float n) {
     if (act == ACT_RELU) return n < 0.f ? 0.f : n;   // (NaN stays)
-    if (act == ACT_SILU) return n / (1.f + expf(-n));
-    if (act == ACT_GELU) return 0.5f * n * (1.f + erff(n * 0.70710678118654752f));
+    if (act == ACT_SILU) return __fdividef(n, 1.f + fast_exp(-n));
+    if (act == ACT_GELU) { float bell; return n * normal_cdf(n, &bell); }
     return n;
 }
 
@@ -64,9 +134,13 @@ __device__ __forceinline__ float act_slope(int act, float n, float x, float mean
         return at <= 0.0 ? 0.f : 1.f;
     }
     if (act == ACT_SILU) {
-        const float s = 1.f / (1.f + expf(-n));
+        const float s = __fdividef(1.f, 1.f + fast_exp(-n));
         return s * (1.f + n * (1.f - s));
     }
-    if (act == ACT_GELU) return 0.5f * (1.f + erff(n * 0.70710678118654752f)) + n * expf(-0.5f * n * n) * 0.39894228040143268f;
+    if (act == ACT_GELU) {
+        float bell;
+        const float cdf = normal_cdf(n, &bell);
+        return fmaf(n * 0.39894228040143268f, bell, cdf);
+    }
     return 1.f;
 }

@@ -1,0 +1,66 @@
+// Launches of dropout's and group norm's kernels, by vector width.
+#pragma once
+
+#include "mg_norm_tiles.cuh"
+
+namespace mgnorm {
+
+template <typename T>
+void launch_dropout(int vec, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t rows, int32_t channels, const DropArgs& d, int grid, cudaStream_t st) {
+    const T* from = static_cast<const T*>(x);
+    T* to = static_cast<T*>(y);
+    if (vec == 8) k_dropout<T, 8><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, rows, channels, d);
+    else if (vec == 4) k_dropout<T, 4><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, rows, channels, d);
+    else if (sizeof(T) == 2 && vec == 2) k_dropout<T, sizeof(T) == 2 ? 2 : 1><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, rows, channels, d);
+    else k_dropout<T, 1><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, rows, channels, d);
+}
+
+template <typename T, int VEC, int NV>
+void launch_rows_of(const RowLaunch& l, const NormArgs& a, cudaStream_t st) {
+    const size_t params = Params<VEC, NV>::kHeld ? 0 : 2 * sizeof(float) * (size_t)a.channels, sums = 2 * sizeof(float) * (size_t)a.channels;
+    if (l.backward) {
+        if (l.general) k_norm_rows_backward<T, VEC, NV, true><<<l.grid, kNormThreads, params + sums, st>>>(a, l.shape);
+        else k_norm_rows_backward<T, VEC, NV, false><<<l.grid, kNormThreads, params + sums, st>>>(a, l.shape);
+    } else {
+        if (l.general) k_norm_rows<T, VEC, NV, true><<<l.grid, kNormThreads, params, st>>>(a, l.shape);
+        else k_norm_rows<T, VEC, NV, false><<<l.grid, kNormThreads, params, st>>>(a, l.shape);
+    }
+}
+
+// (vectors per lane: the next number that there is a kernel for; lanes beyond the row's vectors do nothing)
+template <typename T>
+void launch_rows(const RowLaunch& l, const NormArgs& a, cudaStream_t st) {
+    constexpr int kTwo = sizeof(T) == 2 ? 2 : 1;
+    if (l.vec == 8) {
+        if (l.nv == 1) launch_rows_of<T, 8, 1>(l, a, st);
+        else if (l.nv == 2) launch_rows_of<T, 8, 2>(l, a, st);
+        else launch_rows_of<T, 8, 4>(l, a, st);
+    } else if (l.vec == 4) {
+        if (l.nv <= 2) launch_rows_of<T, 4, 2>(l, a, st);
+        else launch_rows_of<T, 4, 8>(l, a, st);
+    } else if (l.vec == kTwo && kTwo == 2) {
+        if (l.nv <= 4) launch_rows_of<T, kTwo, 4>(l, a, st);
+        else launch_rows_of<T, kTwo, 16>(l, a, st);
+    } else {
+        if (l.nv <= 4) launch_rows_of<T, 1, 4>(l, a, st);
+        else launch_rows_of<T, 1, 32>(l, a, st);
+    }
+}
+
+// K rows in flight for the sums, U for the results
+template <typename T, int VEC>
+void launch_tiles_of(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
+    constexpr bool wide = sizeof(T) * VEC == 32;
+    if (l.backward) k_norm_tiles<T, VEC, true, wide ? 2 : 4, 2, 3><<<l.grid, kNormThreads, 0, st>>>(a);
+    else k_norm_tiles<T, VEC, false, wide ? 4 : 8, 4, 3><<<l.grid, kNormThreads, 0, st>>>(a);
+}
+
+template <typename T>
+void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
+    if (l.vec == 8) launch_tiles_of<T, 8>(l, a, st);
+    else if (l.vec == 4) launch_tiles_of<T, 4>(l, a, st);
+    else if (sizeof(T) == 2 && l.vec == 2) launch_tiles_of<T, sizeof(T) == 2 ? 2 : 1>(l, a, st);
+    else launch_tiles_of<T, 1>(l, a, st);
+}
+
+}  // namespace mgnorm

@@ -6,9 +6,11 @@
 #include <algorithm>
 
 #include "mg_internal.cuh"
-#include "mg_norm.cuh"
+#include "mg_norm_tiles.cuh"
 
 namespace {
+
+using namespace mgnorm;
 
 int elem_size(int dtype) { return dtype == MG_DTYPE_F32 ? 4 : 2; }
 
@@ -18,9 +20,10 @@ int check_dropout(mg_ctx* ctx, const mg_dropout_spec* s, DropArgs* d) {
     if (!(s->p >= 0.0 && s->p <= 1.0)) return mg_fail(ctx, MG_ERR_ARG, "the share to drop must be in [0, 1]");
     if (s->site > 0xFFFFu) return mg_fail(ctx, MG_ERR_ARG, "a dropout's site must be below 65536");
     if (reinterpret_cast<uintptr_t>(s->row_keys) % 8) return mg_fail(ctx, MG_ERR_ARG, "row keys must be 8-byte aligned");
-    d->limit = (uint32_t)nearbyint(s->p * 65536.0);
-    d->on = d->limit > 0;
-    d->factor = d->limit < 65536u ? 65536.f / (float)(65536u - d->limit) : 0.f;
+    const uint32_t limit = (uint32_t)nearbyint(s->p * 65536.0);
+    d->on = limit > 0;
+    d->below = (uint32_t)((uint64_t)limit * 65536u - 1u);
+    d->factor = limit < 65536u ? 65536.f / (float)(65536u - limit) : 0.f;
     d->k0 = (uint32_t)s->seed; d->k1 = (uint32_t)(s->seed >> 32);
     d->tag = kDropTag + s->site;
     d->first_row = s->first_row; d->keys = s->row_keys;
@@ -76,8 +79,128 @@ int check_norm(mg_ctx* ctx, const mg_norm_spec* s) {
 
 int64_t sample_count(const mg_norm_spec* s) { return s->sample_offsets ? s->n_samples : s->rows / s->rows_per_sample; }
 
-size_t norm_workspace(const mg_norm_spec* s) { return s->sample_offsets ? sizeof(int64_t) * (size_t)(s->n_samples + 1) : 0; }
+// ---- how a call is cut ------------------------------------------------------------------
 
+enum { NORM_NOTHING = 0, NORM_ROWS = 1, NORM_TILES = 2 };
+
+struct NormPlan {
+    int mode = NORM_NOTHING, vec = 1;
+    int grid = 0;
+    // rows
+    int nv = 1;
+    bool general = false;
+    RowShape shape{0, 0};
+    // workspace: bytes that are cleared first, then where the others start
+    size_t cleared = 0, at_fan_count = 0, at_sample_count = 0, at_ready = 0, at_table = 0, at_tile_parts = 0, at_fan_parts = 0, at_group_parts = 0, at_parts = 0, bytes = 0;
+    int64_t n_parts = 0;   // backward: what k_norm_params adds up
+};
+
+int ceil_log2(int64_t v) { int l = 0; while ((1ll << l) < v) ++l; return l; }
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+constexpr int kRowsMaxChannels = 32 * kRowValues;
+constexpr int kRowBlocks = 8, kRowBlocksBackward = 4;   // blocks per SM
+constexpr int kTileBlocks = 4;
+
+// Rows that are samples by themselves, `vec` values to a vector.
+void plan_rows(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p) {
+    p->mode = NORM_ROWS; p->vec = vec;
+    const int64_t vecs = s->channels / vec;
+    const int64_t each = s->channels / s->groups;
+    p->shape.lanes = std::min(5, ceil_log2(vecs));
+    p->nv = 1 << ceil_log2((vecs + 31) / 32);
+    const int64_t width = each / vec;
+    p->general = s->groups > 1 && (each % vec || (width & (width - 1)));
+    p->shape.gshift = s->groups == 1 ? 31 : ceil_log2(std::max<int64_t>(width, 1));
+    const int64_t per_block = (int64_t)kNormWarps * (32 >> p->shape.lanes);
+    p->grid = (int)std::min<int64_t>((s->rows + per_block - 1) / per_block, (int64_t)n_sms * (backward ? kRowBlocksBackward : kRowBlocks));
+    p->n_parts = backward ? p->grid : 0;
+    p->bytes = backward ? sizeof(float) * 2 * (size_t)s->channels * p->grid : 0;
+}
+
+constexpr int64_t kTileBytes = 64 << 10, kWindowBytes = 16 << 20;
+
+// Samples of several rows.  a: the geometry's part of the arguments.
+void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p, TileArgs* a) {
+    p->mode = NORM_TILES; p->vec = vec;
+    const int64_t n = sample_count(s), vecs = s->channels / vec, elem = elem_size(s->dtype);
+    const bool equal = !s->sample_offsets;
+    const int64_t used = equal ? s->rows : s->sample_offsets[n];
+    int64_t longest = equal ? s->rows_per_sample : 0;
+    if (!equal) for (int64_t i = 0; i < n; ++i) longest = std::max(longest, s->sample_offsets[i + 1] - s->sample_offsets[i]);
+    a->tx = std::min(ceil_log2(kNormThreads), ceil_log2(vecs));
+    a->chunks = (int32_t)((vecs + (1 << a->tx) - 1) >> a->tx);
+    const int64_t n_ty = kNormThreads >> a->tx, row_bytes = std::min<int64_t>(s->channels, (int64_t)vec << a->tx) * elem;
+    // tiles of 64 KB, smaller ones where those would leave SMs idle, larger ones where a sample had more than kFan^2
+    const int64_t spread = (used * a->chunks + (int64_t)n_sms * kTileBlocks - 1) / ((int64_t)n_sms * kTileBlocks);
+    int64_t rows = std::min(std::max<int64_t>(kTileBytes / row_bytes, 1), std::max<int64_t>(spread, 1));
+    rows = std::max({round_up(rows, n_ty), round_up((longest + kFan * kFan - 1) / (kFan * kFan), n_ty), (int64_t)16});
+    a->tile_rows = (int32_t)std::min<int64_t>(rows, 1 << 30);
+    a->samples = (int32_t)n; a->equal = equal;
+    a->rows_per_sample = s->rows_per_sample;
+    a->tiles_per_sample = equal ? (int32_t)((s->rows_per_sample + a->tile_rows - 1) / a->tile_rows) : 0;
+    // windows: whole samples of at least 16 MB
+    const int64_t bytes_per_row = (int64_t)s->channels * elem * (backward ? 2 : 1);
+    const int64_t window = std::max(kWindowBytes, used * bytes_per_row / (kMaxWindows - 8));
+    int64_t tiles = 0, in_window = 0;
+    a->windows = 0;
+    a->window_tile[0] = 0;
+    const auto sample_tiles = [&](int64_t i) { return equal ? (int64_t)a->tiles_per_sample : (s->sample_offsets[i + 1] - s->sample_offsets[i] + a->tile_rows - 1) / a->tile_rows; };
+    if (equal) {
+        const int64_t sample_bytes = std::max<int64_t>(1, s->rows_per_sample * bytes_per_row), per = std::max<int64_t>(1, (window + sample_bytes - 1) / sample_bytes);
+        for (int64_t i = 0; i < n; i += per) { tiles += std::min(per, n - i) * a->tiles_per_sample; a->window_tile[++a->windows] = (int32_t)tiles; }
+    } else {
+        for (int64_t i = 0; i < n; ++i) {
+            tiles += sample_tiles(i);
+            in_window += (s->sample_offsets[i + 1] - s->sample_offsets[i]) * bytes_per_row;
+            if (in_window >= window || i + 1 == n) { a->window_tile[++a->windows] = (int32_t)tiles; in_window = 0; }
+        }
+    }
+    a->reversed = longest * bytes_per_row > 48 << 20;   // (a sample that L2 does not hold)
+    p->grid = (int)std::max<int64_t>(1, std::min<int64_t>(2 * tiles * a->chunks, (int64_t)n_sms * kTileBlocks));
+    p->n_parts = backward ? n : 0;
+    const int64_t fans = tiles / kFan + n + 1, pair = 2 * sizeof(float) * (int64_t)s->channels;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 15) / 16 * 16; return was; };
+    take(4);   // the ticket
+    p->at_fan_count = take(4 * (size_t)fans);
+    p->at_sample_count = take(4 * (size_t)n);
+    p->at_ready = take(4 * (size_t)n);
+    p->cleared = at;
+    p->at_table = take(!equal && n > kInlineSamples ? sizeof(int2) * (size_t)(n + 1) : 0);
+    p->at_tile_parts = take((size_t)(tiles * pair));
+    p->at_fan_parts = take((size_t)(fans * pair));
+    p->at_group_parts = take(backward ? 2 * sizeof(float) * (size_t)(n * s->groups) : 0);
+    p->at_parts = take(backward ? (size_t)(n * pair) : 0);
+    p->bytes = at;
+}
+
+// the vector widths that there are kernels for: 32, 16, 8 (16-bit types: 16, 8, 4) and one element
+const int* vec_widths(int dtype) {
+    static const int wide[] = {8, 4, 1, 0}, narrow[] = {8, 4, 2, 1, 0};
+    return dtype == MG_DTYPE_F32 ? wide : narrow;
+}
+
+int norm_mode(const mg_norm_spec* s) {
+    if (sample_count(s) == 0) return NORM_NOTHING;
+    if (!s->sample_offsets && s->rows_per_sample == 1 && s->channels <= kRowsMaxChannels) return NORM_ROWS;
+    return NORM_TILES;
+}
+
+// whatever the matrices' alignment makes of it
+size_t norm_workspace(const mg_norm_spec* s, int n_sms, bool backward) {
+    const int mode = norm_mode(s);
+    size_t most = 0;
+    for (const int* v = vec_widths(s->dtype); *v && mode != NORM_NOTHING; ++v) {
+        if (s->channels % *v) continue;
+        NormPlan p;
+        TileArgs a;
+        if (mode == NORM_ROWS) plan_rows(s, n_sms, backward, *v, &p);
+        else plan_tiles(s, n_sms, backward, *v, &p, &a);
+        most = std::max(most, p.bytes);
+    }
+    return most;
+}
 
 struct Matrix { const char* what; const void* p; int64_t stride; bool written; };
 
@@ -88,6 +211,24 @@ int check_matrices(mg_ctx* ctx, const Matrix* m, int n, int dtype, int64_t rows,
     for (int i = 0; i + 1 < n; ++i)
         if (int rc = check_apart(ctx, m[i].what, m[i].p, m[i].stride, m[n - 1].p, m[n - 1].stride, dtype, rows, channels)) return rc;
     return MG_OK;
+}
+
+// The widest vectors that all the matrices' rows are made of; whole groups of them, or whole rows where the groups do not matter.
+int vec_width(const Matrix* m, int n, int dtype, int64_t rows, int32_t of) {
+    const int64_t e = elem_size(dtype);
+    for (const int* v = vec_widths(dtype); *v; ++v) {
+        bool ok = of % *v == 0;
+        for (int i = 0; i < n; ++i) ok = ok && reinterpret_cast<uintptr_t>(m[i].p) % (uintptr_t)(*v * e) == 0 && (rows <= 1 || m[i].stride % *v == 0);
+        if (ok) return *v;
+    }
+    return 1;
+}
+
+// ... for rows that are samples by themselves: a group's vectors where they are a power of two in number, else the row's
+int rows_vec_width(const Matrix* m, int n, const mg_norm_spec* s) {
+    const int32_t each = s->channels / s->groups;
+    const int v = vec_width(m, n, s->dtype, s->rows, each), w = each / v;
+    return (w & (w - 1)) == 0 ? v : vec_width(m, n, s->dtype, s->rows, s->channels);
 }
 
 // every check of an entry point's arguments but the workspace's; `d`: the dropout as the kernels take it

@@ -1,0 +1,378 @@
+// Dropout, and group norm of rows that are samples by themselves: a warp, or a part of one, holds a row in registers.
+#pragma once
+
+#include "mg_norm.cuh"
+
+namespace mgnorm {
+
+constexpr int kNormThreads = 256, kNormWarps = kNormThreads / 32;
+constexpr int kRowValues = 32;   // values of a row that a lane holds at most
+
+struct NormArgs {
+    const void* x = nullptr; const void* d_y = nullptr; void* out = nullptr;
+    int64_t x_stride = 0, d_y_stride = 0, out_stride = 0;
+    const float* weight = nullptr; const float* bias = nullptr;   // null: ones, zeros
+    float* mean = nullptr; float* rstd = nullptr;                 // [samples, groups]
+    float* parts = nullptr;                                       // backward: sums of dz hat, then of dz, by channel: [parts][2][channels]
+    int64_t rows = 0;
+    int32_t channels = 0, groups = 0, act = 0;
+    int32_t each = 0;                                             // channels of a group
+    float eps = 0.f;
+    DropArgs drop;
+};
+
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kNormThreads) k_dropout(const T* x, int64_t x_stride, T* y, int64_t y_stride, int64_t rows, int32_t channels, DropArgs d) {
+    const int64_t vecs = channels / VEC, step = (int64_t)gridDim.x * kNormThreads;
+    int64_t i = blockIdx.x * (int64_t)kNormThreads + threadIdx.x;
+    int64_t row = i / vecs;
+    int32_t v = (int32_t)(i - row * vecs);
+    const int64_t step_rows = step / vecs;
+    const int32_t step_v = (int32_t)(step - step_rows * vecs);
+    constexpr int U = 4;   // accesses in flight per thread
+    while (row < rows) {
+        Raw<T, VEC> p[U];
+        int64_t at_row[U];
+        int32_t at_v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            at_row[u] = row; at_v[u] = v;
+            if (row < rows) p[u].load(x + row * x_stride + v * VEC);
+            row += step_rows; v += step_v;
+            if (v >= vecs) { v -= (int32_t)vecs; ++row; }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (at_row[u] >= rows) break;
+            if (d.on) {
+                Keep<VEC> keep;
+                keep.draw(d, drop_key(d, at_row[u]), (uint32_t)(at_v[u] * VEC));
+                float f[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f[e] = keep(d, e) ? p[u].get(e) * d.factor : 0.f;
+                p[u].put(f);
+            }
+            p[u].store(y + at_row[u] * y_stride + at_v[u] * VEC);
+        }
+    }
+}
+
+// ---- group norm of single rows ----------------------------------------------------------
+// A row's vectors lie on 2^lanes lanes (all 32 where it has more than 32 vectors, NV of them per lane then); a warp holds 32 >> lanes rows.
+// The groups are equal blocks of `1 << gshift` vectors (gshift 31: the whole row) or, GENERAL, of any width: then they are taken one after
+// the other under masks.
+
+struct RowShape { int32_t lanes, gshift; };
+
+template <int NV>
+__device__ __forceinline__ void group_sum(float (&s)[NV], const RowShape& r) {
+    if (r.gshift >= 31) {
+        float t = s[0];
+#pragma unroll
+        for (int i = 1; i < NV; ++i) t += s[i];
+        for (int o = 1; o < 1 << r.lanes; o <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) s[i] = t;
+        return;
+    }
+    const int width = 1 << min(r.gshift, r.lanes);
+    for (int o = 1; o < width; o <<= 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], o);
+    }
+    if (NV > 1 && r.gshift > 5) {   // (groups wider than a warp are of whole warps)
+#pragma unroll
+        for (int st = 1; st < NV; st <<= 1) {
+            if (32 * st < 1 << r.gshift) {
+                float t[NV];
+#pragma unroll
+                for (int i = 0; i < NV; ++i) t[i] = s[i] + s[i ^ st];
+#pragma unroll
+                for (int i = 0; i < NV; ++i) s[i] = t[i];
+            }
+        }
+    }
+}
+
+__device__ __forceinline__ float row_sum(float t, int lanes) {
+    for (int o = 1; o < 1 << lanes; o <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+    return t;
+}
+
+// Weight and bias of a lane's channels: held in registers where they are few, else read from shared memory again for every row.
+template <int VEC, int NV> struct Params {
+    static constexpr bool kHeld = VEC * NV <= 8;
+    float w[kHeld ? NV : 1][VEC], b[kHeld ? NV : 1][VEC];
+    const float* shared;
+    int32_t channels;
+    __device__ __forceinline__ Params(const NormArgs& a, float* smem, int sub, int32_t vecs) : shared(smem), channels(a.channels) {
+        if constexpr (kHeld) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int32_t c = (sub + 32 * i) * VEC + e;
+                    const bool in = sub + 32 * i < vecs;
+                    w[i][e] = in && a.weight ? a.weight[c] : 1.f;
+                    b[i][e] = in && a.bias ? a.bias[c] : 0.f;
+                }
+        } else {
+            for (int32_t c = threadIdx.x; c < a.channels; c += kNormThreads) {
+                smem[c] = a.weight ? a.weight[c] : 1.f;
+                smem[a.channels + c] = a.bias ? a.bias[c] : 0.f;
+            }
+            __syncthreads();
+        }
+    }
+    __device__ __forceinline__ static void read(const float* s, float (&o)[VEC]) {
+        if constexpr (VEC % 4 == 0) {
+#pragma unroll
+            for (int q = 0; q < VEC; q += 4) {
+                const float4 f = *reinterpret_cast<const float4*>(s + q);
+                o[q] = f.x; o[q + 1] = f.y; o[q + 2] = f.z; o[q + 3] = f.w;
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < VEC; ++q) o[q] = s[q];
+        }
+    }
+    __device__ __forceinline__ void get(int i, int32_t v, float (&wo)[VEC], float (&bo)[VEC]) const {
+        if constexpr (kHeld) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) { wo[e] = w[i][e]; bo[e] = b[i][e]; }
+        } else {
+            read(shared + v * VEC, wo);
+            read(shared + channels + v * VEC, bo);
+        }
+    }
+};
+
+template <typename T, int VEC, int NV, bool GENERAL>
+__global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape r) {
+    extern __shared__ __align__(16) float params[];   // [2][channels], where they are not held
+    const int lane = threadIdx.x & 31, sub = lane & ((1 << r.lanes) - 1), per_warp = 32 >> r.lanes;
+    const int32_t vecs = a.channels / VEC;
+    const float inv = 1.f / (float)a.each;
+    const T* x = static_cast<const T*>(a.x);
+    T* y = static_cast<T*>(a.out);
+    const Params<VEC, NV> par(a, params, sub, vecs);
+    const int64_t step = (int64_t)gridDim.x * kNormWarps * per_warp;
+    for (int64_t row0 = (blockIdx.x * (int64_t)kNormWarps + (threadIdx.x >> 5)) * per_warp; row0 < a.rows; row0 += step) {
+        const int64_t row = row0 + (lane >> r.lanes);
+        const bool here = row < a.rows;
+        Raw<T, VEC> raw[NV];
+        float f[NV][VEC];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            raw[i].zero();
+            if (here && sub + 32 * i < vecs) raw[i].load(x + row * a.x_stride + (sub + 32 * i) * VEC);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[i][e] = raw[i].get(e);
+        if constexpr (GENERAL) {   // f becomes the normalised value
+            for (int32_t g = 0, lo = 0; g < a.groups; ++g, lo += a.each) {
+                float s = 0.f, q = 0.f;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) if ((uint32_t)((sub + 32 * i) * VEC + e - lo) < (uint32_t)a.each) s += f[i][e];
+                const float mean = row_sum(s, r.lanes) * inv;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) if ((uint32_t)((sub + 32 * i) * VEC + e - lo) < (uint32_t)a.each) { f[i][e] -= mean; q = fmaf(f[i][e], f[i][e], q); }
+                const float rstd = rsqrtf(row_sum(q, r.lanes) * inv + a.eps);
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) if ((uint32_t)((sub + 32 * i) * VEC + e - lo) < (uint32_t)a.each) f[i][e] *= rstd;
+                if (here && sub == 0) { a.mean[row * a.groups + g] = mean; a.rstd[row * a.groups + g] = rstd; }
+            }
+        } else {
+            float s[NV], q[NV];
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                s[i] = 0.f;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) s[i] += f[i][e];
+            }
+            group_sum<NV>(s, r);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                s[i] *= inv; q[i] = 0.f;
+                const bool in = sub + 32 * i < vecs;   // (a lane without a vector would count the mean)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) { f[i][e] -= s[i]; q[i] = fmaf(f[i][e], f[i][e], q[i]); }
+                if (!in) q[i] = 0.f;
+            }
+            group_sum<NV>(q, r);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const float rstd = rsqrtf(q[i] * inv + a.eps);
+                const int32_t v = sub + 32 * i;
+                if (here && v < vecs && (r.gshift >= 31 ? v == 0 : (v & ((1 << r.gshift) - 1)) == 0)) {
+                    const int64_t at = row * a.groups + (r.gshift >= 31 ? 0 : v >> r.gshift);
+                    a.mean[at] = s[i]; a.rstd[at] = rstd;
+                }
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f[i][e] *= rstd;
+            }
+        }
+        const uint64_t key = here && a.drop.on ? drop_key(a.drop, row) : 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int32_t v = sub + 32 * i;
+            if (!here || v >= vecs) continue;
+            float w[VEC], b[VEC];
+            par.get(i, v, w, b);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[i][e] = act_value(a.act, fmaf(f[i][e], w[e], b[e]));
+            if (a.drop.on) {
+                Keep<VEC> keep;
+                keep.draw(a.drop, key, (uint32_t)(v * VEC));
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f[i][e] = keep(a.drop, e) ? f[i][e] * a.drop.factor : 0.f;
+            }
+            raw[i].put(f[i]);
+            raw[i].store(y + row * a.out_stride + v * VEC);
+        }
+    }
+}
+
+// Gradient: dz = dropout(dy) act', then dx = rstd (dz w - mean(dz w) - hat mean(dz w hat)); every lane adds up dz hat and dz of its channels over
+// its rows, every block its lanes', and k_norm_params the blocks'.
+template <typename T, int VEC, int NV, bool GENERAL>
+__global__ void __launch_bounds__(kNormThreads) k_norm_rows_backward(NormArgs a, RowShape r) {
+    extern __shared__ __align__(16) float params[];   // [2][channels], where they are not held; then the block's sums [2][channels]
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane & ((1 << r.lanes) - 1), per_warp = 32 >> r.lanes;
+    const int32_t vecs = a.channels / VEC;
+    const float inv = 1.f / (float)a.each;
+    const T* x = static_cast<const T*>(a.x);
+    const T* d_y = static_cast<const T*>(a.d_y);
+    T* d_x = static_cast<T*>(a.out);
+    const Params<VEC, NV> par(a, params, sub, vecs);
+    float* sums = params + (Params<VEC, NV>::kHeld ? 0 : 2 * a.channels);
+    float dw[NV][VEC], db[NV][VEC];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) dw[i][e] = db[i][e] = 0.f;
+    const int64_t step = (int64_t)gridDim.x * kNormWarps * per_warp;
+    for (int64_t row0 = (blockIdx.x * (int64_t)kNormWarps + warp) * per_warp; row0 < a.rows; row0 += step) {
+        const int64_t row = row0 + (lane >> r.lanes);
+        const bool here = row < a.rows;
+        Raw<T, VEC> rx[NV], rd[NV];
+        float h[NV][VEC], g[NV][VEC], rstd[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            rx[i].zero(); rd[i].zero();
+            if (here && sub + 32 * i < vecs) {
+                rx[i].load(x + row * a.x_stride + (sub + 32 * i) * VEC);
+                rd[i].load(d_y + row * a.d_y_stride + (sub + 32 * i) * VEC);
+            }
+        }
+        const uint64_t key = here && a.drop.on ? drop_key(a.drop, row) : 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int32_t v = sub + 32 * i;
+            const bool in = here && v < vecs;
+            float mean = 0.f;
+            rstd[i] = 0.f;
+            if (in && !GENERAL) {
+                const int64_t at = row * a.groups + (r.gshift >= 31 ? 0 : v >> r.gshift);
+                mean = a.mean[at]; rstd[i] = a.rstd[at];
+            }
+            Keep<VEC> keep;
+            if (a.drop.on) keep.draw(a.drop, key, (uint32_t)(v * VEC));
+            float w[VEC], b[VEC];
+            par.get(i, in ? v : 0, w, b);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const int32_t c = v * VEC + e;
+                float r_e = rstd[i], m_e = mean;
+                if (GENERAL && in) {
+                    const int64_t at = row * a.groups + c / a.each;
+                    m_e = a.mean[at]; r_e = a.rstd[at];
+                }
+                const float xv = rx[i].get(e);
+                float d = rd[i].get(e);
+                h[i][e] = (xv - m_e) * r_e;
+                d *= act_slope(a.act, fmaf(h[i][e], w[e], b[e]), xv, m_e, r_e, w[e], b[e]);
+                if (a.drop.on) d = keep(a.drop, e) ? d * a.drop.factor : 0.f;
+                if (!in) d = 0.f;
+                dw[i][e] = fmaf(d, h[i][e], dw[i][e]); db[i][e] += d;
+                g[i][e] = d * w[e];
+            }
+        }
+        if constexpr (GENERAL) {
+            for (int32_t q = 0, lo = 0; q < a.groups; ++q, lo += a.each) {
+                float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if ((uint32_t)((sub + 32 * i) * VEC + e - lo) < (uint32_t)a.each) { s1 += g[i][e]; s2 = fmaf(g[i][e], h[i][e], s2); }
+                s1 = row_sum(s1, r.lanes) * inv; s2 = row_sum(s2, r.lanes) * inv;
+                const float r_q = here ? a.rstd[row * a.groups + q] : 0.f;
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if ((uint32_t)((sub + 32 * i) * VEC + e - lo) < (uint32_t)a.each) g[i][e] = r_q * (g[i][e] - s1 - h[i][e] * s2);
+            }
+        } else {
+            float s1[NV], s2[NV];
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                s1[i] = s2[i] = 0.f;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) { s1[i] += g[i][e]; s2[i] = fmaf(g[i][e], h[i][e], s2[i]); }
+            }
+            group_sum<NV>(s1, r);
+            group_sum<NV>(s2, r);
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) g[i][e] = rstd[i] * (g[i][e] - s1[i] * inv - h[i][e] * (s2[i] * inv));
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int32_t v = sub + 32 * i;
+            if (!here || v >= vecs) continue;
+            rx[i].put(g[i]);
+            rx[i].store(d_x + row * a.out_stride + v * VEC);
+        }
+    }
+    if (!a.parts) return;
+    // the warp's rows, then the block's warps one after the other
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+            for (int o = 1 << r.lanes; o < 32; o <<= 1) {
+                dw[i][e] += __shfl_xor_sync(0xFFFFFFFFu, dw[i][e], o);
+                db[i][e] += __shfl_xor_sync(0xFFFFFFFFu, db[i][e], o);
+            }
+    for (int q = 0; q < kNormWarps; ++q) {
+        if (q == warp && lane == sub) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int32_t v = sub + 32 * i;
+                if (v >= vecs) continue;
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    float* at = sums + v * VEC + e;
+                    at[0] = q ? at[0] + dw[i][e] : dw[i][e];
+                    at[a.channels] = q ? at[a.channels] + db[i][e] : db[i][e];
+                }
+            }
+        }
+        __syncthreads();
+    }
+    float* part = a.parts + (int64_t)blockIdx.x * 2 * a.channels;
+    for (int32_t c = threadIdx.x; c < 2 * a.channels; c += kNormThreads) part[c] = sums[c];
+}
+
+}  // namespace mgnorm

@@ -1,0 +1,434 @@
+// Group norm of samples of many rows: tiles of rows are dealt out to persistent blocks, first for the sums of a sample's channels, then, once
+// all of the sample's are there, for the result.  Both come from one queue, so one launch does it, and a sample that fits L2 is read from
+// memory once.
+#pragma once
+
+#include "mg_norm_rows.cuh"
+
+namespace mgnorm {
+
+constexpr int kFan = 32;             // tiles whose sums one block brings together; then as many of those
+constexpr int kInlineSamples = 64;   // samples whose place is handed over in the kernel's parameters
+constexpr int kMaxWindows = 72;
+constexpr int kTilePolls = 1 << 22;  // (a poll is an L2 round trip: far beyond any legitimate wait)
+constexpr uint32_t kRoleNorm = 30u;  // what a wait that ran out leaves in the context's status word
+
+struct TileArgs : NormArgs {
+    // samples: equal ones, or a table of (first row, first tile), one entry more than samples
+    int32_t samples = 0, equal = 0;
+    int64_t rows_per_sample = 0;
+    int32_t tiles_per_sample = 0;
+    const int2* table = nullptr;     // null: `inl`
+    int2 inl[kInlineSamples + 1];
+    // tiles: tile_rows rows, each in `chunks` runs of (256 or fewer) vectors
+    int32_t tile_rows = 0, chunks = 0, tx = 0;   // tx: log2 of the threads along a row
+    // queue: the windows' first tiles; position p of the queue: sums of window 0, sums of window 1, results of window 0, sums of window 2, ...
+    int32_t windows = 0, reversed = 0;
+    int32_t window_tile[kMaxWindows + 1];
+    // workspace
+    uint32_t* ticket = nullptr;      // cleared: the queue's next position ...
+    uint32_t* fan_count = nullptr;   // ... sums that have arrived, by kFan tiles of a sample ...
+    uint32_t* sample_count = nullptr;   // ... and by sample ...
+    uint32_t* ready = nullptr;       // ... 1: the sample's statistics (backward: group sums) are there
+    float* tile_parts = nullptr;     // [tiles][2][channels]
+    float* fan_parts = nullptr;      // [tiles / kFan + samples][2][channels]
+    float* group_parts = nullptr;    // backward: mean of dz w, mean of dz w hat: [samples][2][groups]
+    uint32_t* status = nullptr;
+    int32_t polls = kTilePolls;
+};
+
+struct Tile {
+    int32_t kind;          // 0 sums, 1 result, 2 nothing left
+    int32_t tile, chunk;   // its number among all
+    int32_t sample, first, tiles;   // the sample's first tile and how many it has
+    int64_t row0, row1, sample_rows;
+};
+
+__device__ __forceinline__ int2 sample_entry(const TileArgs& a, int32_t s) { return a.table ? a.table[s] : a.inl[s]; }
+
+__device__ __forceinline__ int64_t queue_start(const TileArgs& a, int i) {   // of the sums of window i
+    return (int64_t)(a.window_tile[i] + (i ? a.window_tile[i - 1] : 0)) * a.chunks;
+}
+
+__device__ inline void next_tile(const TileArgs& a, Tile* t) {
+    const int64_t total = (int64_t)a.window_tile[a.windows] * a.chunks, p = atomicAdd(a.ticket, 1u);
+    if (p >= 2 * total) { t->kind = 2; return; }
+    int lo = 0, hi = a.windows;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (queue_start(a, mid) <= p) lo = mid; else hi = mid;
+    }
+    int64_t off = p - queue_start(a, lo);
+    int w = lo;
+    t->kind = 0;
+    const int64_t sums = (int64_t)(a.window_tile[lo + 1] - a.window_tile[lo]) * a.chunks;
+    if (off >= sums) {   // the results of the window before, and behind the last window's sums and those its own too
+        off -= sums;
+        t->kind = 1;
+        w = lo - 1;
+        const int64_t before = lo ? (int64_t)(a.window_tile[lo] - a.window_tile[lo - 1]) * a.chunks : 0;
+        if (lo == 0 || off >= before) { off -= before; w = lo; }
+    }
+    const int32_t n = a.window_tile[w + 1] - a.window_tile[w];
+    int32_t tile = (int32_t)(off / a.chunks);
+    t->chunk = (int32_t)(off - (int64_t)tile * a.chunks);
+    if (a.reversed && t->kind == 1) tile = n - 1 - tile;   // (what was read last is still in L2)
+    tile += a.window_tile[w];
+    t->tile = tile;
+    int64_t s0, s1;
+    if (a.equal) {
+        t->sample = tile / a.tiles_per_sample;
+        t->first = t->sample * a.tiles_per_sample;
+        t->tiles = a.tiles_per_sample;
+        s0 = t->sample * a.rows_per_sample; s1 = s0 + a.rows_per_sample;
+    } else {
+        int32_t l = 0, h = a.samples;
+        while (h - l > 1) {
+            const int32_t mid = (l + h) >> 1;
+            if (sample_entry(a, mid).y <= tile) l = mid; else h = mid;
+        }
+        const int2 e = sample_entry(a, l), f = sample_entry(a, l + 1);
+        t->sample = l; t->first = e.y; t->tiles = f.y - e.y;
+        s0 = e.x; s1 = f.x;
+    }
+    t->row0 = s0 + (int64_t)(tile - t->first) * a.tile_rows;
+    t->row1 = min(s1, t->row0 + a.tile_rows);
+    t->sample_rows = s1 - s0;
+}
+
+// Mean and sum of squares about it of two sets (Chan, Golub and LeVeque 1979)
+__device__ __forceinline__ void merge_moments(float& n, float& m, float& q, float nb, float mb, float qb) {
+    const float all = n + nb, f = all > 0.f ? nb / all : 0.f, d = mb - m;
+    m = fmaf(d, f, m);
+    q += fmaf(d * n * f, d, qb);   // (a first set, n = 0: no square of its mean)
+    n = all;
+}
+
+// What a thread has of its channels: forward the mean and the squares about it over n rows, backward two sums
+template <int VEC> struct Pair { float n; float u[VEC], v[VEC]; };
+
+template <int VEC, bool BACKWARD>
+__device__ __forceinline__ void merge(Pair<VEC>& a, float nb, const float (&u)[VEC], const float (&v)[VEC]) {
+    if (BACKWARD) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) { a.u[e] += u[e]; a.v[e] += v[e]; }
+    } else {
+        const float all = a.n + nb, f = all > 0.f ? nb / all : 0.f, g = a.n * f;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const float d = u[e] - a.u[e];
+            a.u[e] = fmaf(d, f, a.u[e]);
+            a.v[e] += fmaf(d * g, d, v[e]);   // (a first set, g = 0: no square of its mean)
+        }
+        a.n = all;
+    }
+}
+
+// Sums of a tile: every thread has one vector of the channels and every TY-th row, K rows in flight; then the block's threads are brought together.
+template <typename T, int VEC, bool BACKWARD, int K>
+__device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int32_t c, bool in, int ty, int n_ty, float mean, float rstd, const float (&w)[VEC],
+                                          const float (&b)[VEC], Pair<VEC>& p) {
+    const T* x = static_cast<const T*>(a.x) + c;
+    const T* d_y = static_cast<const T*>(a.d_y) + c;
+    p.n = 0.f;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) p.u[e] = p.v[e] = 0.f;
+    if (!in) return;
+    for (int64_t r = t.row0 + ty; r < t.row1; r += (int64_t)K * n_ty) {
+        Raw<T, VEC> raw[K], rd[BACKWARD ? K : 1];
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+            if (r + k * n_ty < t.row1) {
+                raw[k].load(x + (r + k * n_ty) * a.x_stride);
+                if (BACKWARD) rd[k].load(d_y + (r + k * n_ty) * a.d_y_stride);
+            }
+        if constexpr (BACKWARD) {
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const int64_t row = r + k * n_ty;
+                if (row >= t.row1) break;
+                Keep<VEC> keep;
+                if (a.drop.on) keep.draw(a.drop, drop_key(a.drop, row), (uint32_t)c);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const float xv = raw[k].get(e), h = (xv - mean) * rstd;
+                    float d = rd[k].get(e) * act_slope(a.act, fmaf(h, w[e], b[e]), xv, mean, rstd, w[e], b[e]);
+                    if (a.drop.on) d = keep(a.drop, e) ? d * a.drop.factor : 0.f;
+                    p.u[e] = fmaf(d, h, p.u[e]);
+                    p.v[e] += d;
+                }
+            }
+        } else {
+            const int64_t left = (t.row1 - r + n_ty - 1) / n_ty;
+            const int n = left < K ? (int)left : K;
+            const float inv = 1.f / (float)n;
+            float u[VEC], v[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                float s = 0.f, q = 0.f;
+#pragma unroll
+                for (int k = 0; k < K; ++k) if (k < n) s += raw[k].get(e);
+                s *= inv;
+#pragma unroll
+                for (int k = 0; k < K; ++k) if (k < n) { const float d = raw[k].get(e) - s; q = fmaf(d, d, q); }
+                u[e] = s; v[e] = q;
+            }
+            merge<VEC, false>(p, (float)n, u, v);
+        }
+    }
+}
+
+// The block's threads with the same channels, into `out` ([2][channels], the chunk's channels of it)
+template <int VEC, bool BACKWARD>
+__device__ __forceinline__ void block_pairs(const TileArgs& a, Pair<VEC>& p, float* smem, int tx, int32_t chunk0, float* out) {
+    const int threads_x = 1 << a.tx, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int o = threads_x; o < 32; o <<= 1) {
+        float u[VEC], v[VEC];
+        const float n = __shfl_xor_sync(0xFFFFFFFFu, p.n, o);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) { u[e] = __shfl_xor_sync(0xFFFFFFFFu, p.u[e], o); v[e] = __shfl_xor_sync(0xFFFFFFFFu, p.v[e], o); }
+        // (the lower lane's set first on both sides, so that both have the same)
+        if (!BACKWARD && (lane & o)) {
+            Pair<VEC> q;
+            q.n = n;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) { q.u[e] = u[e]; q.v[e] = v[e]; u[e] = p.u[e]; v[e] = p.v[e]; }
+            const float mine = p.n;
+            merge<VEC, BACKWARD>(q, mine, u, v);
+            p = q;
+        } else merge<VEC, BACKWARD>(p, n, u, v);
+    }
+    const int across = threads_x < 32 ? kNormWarps : kNormThreads / threads_x;   // sets of a channel that are left
+    const int set = threads_x < 32 ? warp : threadIdx.x >> a.tx, width = threads_x * VEC;
+    float* su = smem;                          // [across][width], across * width <= 256 * VEC
+    float* sv = smem + kNormThreads * VEC;
+    float* sn = smem + 2 * kNormThreads * VEC;   // [across]
+    __syncthreads();
+    if (threads_x >= 32 || lane < threads_x) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) { su[set * width + tx * VEC + e] = p.u[e]; sv[set * width + tx * VEC + e] = p.v[e]; }
+        if (tx == 0) sn[set] = p.n;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < width; i += kNormThreads) {
+        const int32_t c = chunk0 + i;
+        if (c >= a.channels) break;
+        float u = su[i], v = sv[i], n = sn[0];
+        for (int s = 1; s < across; ++s) {
+            if (BACKWARD) { u += su[s * width + i]; v += sv[s * width + i]; }
+            else merge_moments(n, u, v, sn[s], su[s * width + i], sv[s * width + i]);
+        }
+        __stcg(out + c, u);
+        __stcg(out + a.channels + c, v);
+    }
+}
+
+// sums of `n` sets that lie one behind the other, rows_of(i) rows each, into `out`
+template <bool BACKWARD, typename Rows>
+__device__ __forceinline__ void merge_parts(const TileArgs& a, const float* parts, int32_t n, Rows rows_of, float* out) {
+    const int64_t step = 2 * (int64_t)a.channels;
+    for (int32_t c = threadIdx.x; c < a.channels; c += kNormThreads) {
+        float u = 0.f, v = 0.f, m = 0.f;
+        for (int32_t i0 = 0; i0 < n; i0 += 8) {
+            float pu[8], pv[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i0 + k < n) { pu[k] = __ldcg(parts + (i0 + k) * step + c); pv[k] = __ldcg(parts + (i0 + k) * step + a.channels + c); }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i0 + k < n) {
+                    if (BACKWARD) { u += pu[k]; v += pv[k]; }
+                    else merge_moments(m, u, v, rows_of(i0 + k), pu[k], pv[k]);
+                }
+        }
+        __stcg(out + c, u);
+        __stcg(out + a.channels + c, v);
+    }
+}
+
+// the groups' values from the channels' of a whole sample: a warp per group
+template <bool BACKWARD>
+__device__ __forceinline__ void finish_sample(const TileArgs& a, int32_t sample, float rows, const float* part) {
+    const int lane = threadIdx.x & 31;
+    const float n = rows * (float)a.each;
+    for (int32_t g = threadIdx.x >> 5; g < a.groups; g += kNormWarps) {
+        float u = 0.f, v = 0.f;
+        for (int32_t c = g * a.each + lane; c < (g + 1) * a.each; c += 32) {
+            if (BACKWARD) {
+                const float w = a.weight ? a.weight[c] : 1.f;
+                u = fmaf(w, __ldcg(part + c), u); v = fmaf(w, __ldcg(part + a.channels + c), v);
+            } else u += __ldcg(part + c);
+        }
+        u = row_sum(u, 5); v = row_sum(v, 5);
+        if (BACKWARD) {
+            if (lane == 0) {
+                __stcg(a.group_parts + ((int64_t)sample * 2) * a.groups + g, v / n);        // mean of dz w
+                __stcg(a.group_parts + ((int64_t)sample * 2 + 1) * a.groups + g, u / n);    // mean of dz w hat
+            }
+            continue;
+        }
+        const float mean = u / (float)a.each;
+        for (int32_t c = g * a.each + lane; c < (g + 1) * a.each; c += 32) {
+            const float d = __ldcg(part + c) - mean;
+            v += fmaf(d * d, rows, __ldcg(part + a.channels + c));
+        }
+        v = row_sum(v, 5);
+        if (lane == 0) {
+            __stcg(a.mean + (int64_t)sample * a.groups + g, mean);
+            __stcg(a.rstd + (int64_t)sample * a.groups + g, rsqrtf(v / n + a.eps));
+        }
+    }
+}
+
+// A tile's sums are written: the last of kFan tiles brings theirs together, the last of those the sample's.
+template <bool BACKWARD>
+__device__ __forceinline__ void arrive(const TileArgs& a, const Tile& t, int32_t* sh_last) {
+    const int32_t in_sample = t.tile - t.first, fan = in_sample / kFan, fans = (t.tiles + kFan - 1) / kFan, fan_tiles = min(kFan, t.tiles - fan * kFan);
+    const int64_t fan_id = t.first / kFan + t.sample + fan;   // (blocks of kFan tiles of all samples before lie below)
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) *sh_last = atomicAdd(a.fan_count + fan_id, 1u) + 1u == (uint32_t)(fan_tiles * a.chunks);
+    __syncthreads();
+    if (!*sh_last) return;
+    __threadfence();
+    const int64_t step = 2 * (int64_t)a.channels;
+    float* fan_part = a.fan_parts + fan_id * step;
+    const auto tile_rows = [&](int32_t i) { return (float)min((int64_t)a.tile_rows, t.sample_rows - ((int64_t)fan * kFan + i) * a.tile_rows); };
+    float* whole = BACKWARD ? a.parts + t.sample * step : a.fan_parts + (t.first / kFan + t.sample) * step;   // the sample's channels
+    merge_parts<BACKWARD>(a, a.tile_parts + ((int64_t)t.first + fan * kFan) * step, fan_tiles, tile_rows, fans == 1 ? whole : fan_part);
+    __syncthreads();
+    if (fans > 1) {
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) *sh_last = atomicAdd(a.sample_count + t.sample, 1u) + 1u == (uint32_t)fans;
+        __syncthreads();
+        if (!*sh_last) return;
+        __threadfence();
+        const auto fan_rows = [&](int32_t i) { return (float)min((int64_t)kFan * a.tile_rows, t.sample_rows - (int64_t)i * kFan * a.tile_rows); };
+        merge_parts<BACKWARD>(a, a.fan_parts + (t.first / kFan + t.sample) * step, fans, fan_rows, whole);
+        __syncthreads();
+    }
+    finish_sample<BACKWARD>(a, t.sample, (float)t.sample_rows, whole);
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) *reinterpret_cast<volatile uint32_t*>(a.ready + t.sample) = 1u;
+}
+
+template <int VEC>
+__device__ __forceinline__ void load_params(const float* p, int32_t c, float without, float (&o)[VEC]) {
+    if constexpr (VEC >= 4) if (p && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+#pragma unroll
+        for (int q = 0; q < VEC; q += 4) {
+            const float4 f = *reinterpret_cast<const float4*>(p + c + q);
+            o[q] = f.x; o[q + 1] = f.y; o[q + 2] = f.z; o[q + 3] = f.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) o[e] = p ? p[c + e] : without;
+}
+
+// A block that waits for a sample's sums waits for positions of the queue before its own, which running blocks have; one that is taken ahead of
+// its time is held by a block whose present one lies before it.  So every wait ends; it is bounded all the same.
+template <typename T, int VEC, bool BACKWARD, int K, int U, int MINB>
+__global__ void __launch_bounds__(kNormThreads, MINB) k_norm_tiles(const __grid_constant__ TileArgs a) {
+    __shared__ __align__(16) float smem[2 * kNormThreads * VEC + kNormWarps];
+    __shared__ Tile sh_tile[2];
+    __shared__ int32_t sh_flag;
+    const int tx = threadIdx.x & ((1 << a.tx) - 1), ty = threadIdx.x >> a.tx, n_ty = kNormThreads >> a.tx;
+    if (!a.equal) {   // samples without rows have no tiles
+        for (int32_t s = blockIdx.x; s < a.samples; s += gridDim.x) {
+            if (sample_entry(a, s).x != sample_entry(a, s + 1).x) continue;
+            if (!BACKWARD) for (int32_t g = threadIdx.x; g < a.groups; g += kNormThreads) { a.mean[(int64_t)s * a.groups + g] = 0.f; a.rstd[(int64_t)s * a.groups + g] = 0.f; }
+            else for (int32_t c = threadIdx.x; c < 2 * a.channels; c += kNormThreads) a.parts[2 * (int64_t)s * a.channels + c] = 0.f;
+        }
+    }
+    if (threadIdx.x == 0) next_tile(a, &sh_tile[0]);
+    __syncthreads();
+    for (int at = 0;; at ^= 1) {
+        const Tile t = sh_tile[at];
+        if (t.kind == 2) break;
+        if (threadIdx.x == 0) next_tile(a, &sh_tile[at ^ 1]);
+        const int32_t chunk0 = t.chunk * (VEC << a.tx), c = chunk0 + tx * VEC;
+        const bool in = c < a.channels;
+        float w[VEC], b[VEC], mean = 0.f, rstd = 0.f;
+        if (BACKWARD || t.kind == 1) {
+            load_params<VEC>(in ? a.weight : nullptr, c, 1.f, w);
+            load_params<VEC>(in ? a.bias : nullptr, c, 0.f, b);
+        }
+        const int64_t stat = (int64_t)t.sample * a.groups + (in ? c / a.each : 0);
+        if (BACKWARD) { mean = a.mean[stat]; rstd = a.rstd[stat]; }
+        if (t.kind == 0) {
+            Pair<VEC> p;
+            tile_sums<T, VEC, BACKWARD, K>(a, t, c, in, ty, n_ty, mean, rstd, w, b, p);
+            block_pairs<VEC, BACKWARD>(a, p, smem, tx, chunk0, a.tile_parts + 2 * (int64_t)t.tile * a.channels);
+            arrive<BACKWARD>(a, t, &sh_flag);
+        } else {
+            if (threadIdx.x == 0) {
+                int polls = 0;
+                const volatile uint32_t* ready = a.ready + t.sample;
+                while (!*ready && ++polls < a.polls) {}
+                sh_flag = polls < a.polls;
+                if (!sh_flag) *reinterpret_cast<volatile uint32_t*>(a.status) = kRoleNorm;
+                __threadfence();
+            }
+            __syncthreads();
+            if (in && sh_flag) {
+                const T* x = static_cast<const T*>(a.x) + c;
+                const T* d_y = static_cast<const T*>(a.d_y) + c;
+                T* out = static_cast<T*>(a.out) + c;
+                float s1 = 0.f, s2 = 0.f;
+                if (BACKWARD) {
+                    const int64_t at_group = (int64_t)t.sample * 2 * a.groups + c / a.each;
+                    s1 = __ldcg(a.group_parts + at_group); s2 = __ldcg(a.group_parts + at_group + a.groups);
+                } else {
+                    mean = __ldcg(a.mean + stat); rstd = __ldcg(a.rstd + stat);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) w[e] *= rstd;
+                }
+                for (int64_t r = t.row0 + ty; r < t.row1; r += (int64_t)U * n_ty) {
+                    Raw<T, VEC> raw[U], rd[BACKWARD ? U : 1];
+#pragma unroll
+                    for (int k = 0; k < U; ++k)
+                        if (r + k * n_ty < t.row1) {
+                            raw[k].load(x + (r + k * n_ty) * a.x_stride);
+                            if (BACKWARD) rd[k].load(d_y + (r + k * n_ty) * a.d_y_stride);
+                        }
+#pragma unroll
+                    for (int k = 0; k < U; ++k) {
+                        const int64_t row = r + k * n_ty;
+                        if (row >= t.row1) break;
+                        Keep<VEC> keep;
+                        if (a.drop.on) keep.draw(a.drop, drop_key(a.drop, row), (uint32_t)c);
+                        float f[VEC];
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            const float xv = raw[k].get(e);
+                            if (BACKWARD) {
+                                const float h = (xv - mean) * rstd;
+                                float d = rd[k].get(e) * act_slope(a.act, fmaf(h, w[e], b[e]), xv, mean, rstd, w[e], b[e]);
+                                if (a.drop.on) d = keep(a.drop, e) ? d * a.drop.factor : 0.f;
+                                f[e] = rstd * fmaf(-h, s2, fmaf(d, w[e], -s1));
+                            } else {
+                                f[e] = act_value(a.act, fmaf(xv - mean, w[e], b[e]));
+                                if (a.drop.on) f[e] = keep(a.drop, e) ? f[e] * a.drop.factor : 0.f;
+                            }
+                        }
+                        raw[k].put(f);
+                        raw[k].store(out + row * a.out_stride);
+                    }
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// what a translation unit of its own per row type launches
+struct RowLaunch { int vec, nv; bool general, backward; int grid; RowShape shape; };
+struct TileLaunch { int vec; bool backward; int grid; };
+template <typename T> void launch_dropout(int vec, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t rows, int32_t channels, const DropArgs& d, int grid, cudaStream_t st);
+template <typename T> void launch_rows(const RowLaunch& l, const NormArgs& a, cudaStream_t st);
+template <typename T> void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st);
+
+}  // namespace mgnorm
