@@ -754,7 +754,8 @@ class Context:
         d_y, d_y_stride = _matrix(d_y, self.device, x)
         spec, samples, rows, drop = self._norm_spec(x, groups, weight, bias, sample_offsets, 1.0, activation, dropout)
         for s in (mean, rstd):
-            assert s.device == self.device and s.dtype == torch.float32 and s.is_contiguous() and s.shape == (samples, groups), "mean, rstd: as group_norm gave them"
+            assert s.device == self.device and s.dtype == torch.float32 and s.shape == (samples, groups), "mean, rstd: as group_norm gave them"
+        mean, rstd = mean.contiguous(), rstd.contiguous()
         new = out is None
         out, out_stride = _result(out, x)
         d_weight, d_bias = torch.empty((2, x.shape[-1]), dtype=torch.float32, device=self.device).unbind(0)

@@ -5,20 +5,31 @@
 
 namespace {
 
-// Weight and bias gradients from `n` blocks' or samples' sums: 32 channels a block, 8 threads to a channel.
-__global__ void __launch_bounds__(kNormThreads) k_norm_params(const float* parts, int64_t n, int32_t channels, float* d_weight, float* d_bias) {
+// Sums of `n` parts ([n][columns]) by column: 32 columns a block, 8 threads to a column; blockIdx.y: a slice of the parts.  In the last step the
+// columns are the weight's gradients, then the bias's.
+__global__ void __launch_bounds__(kNormThreads) k_norm_params(const float* parts, int64_t n, int64_t columns, float* out, float* d_weight, float* d_bias) {
     __shared__ float part[kNormWarps][32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane, lo = n * blockIdx.y / gridDim.y, hi = n * (blockIdx.y + 1) / gridDim.y;
     float s = 0.f;
-    if (c < 2 * (int64_t)channels)
-        for (int64_t i = warp; i < n; i += kNormWarps) s += parts[i * 2 * channels + c];
+    if (c < columns) {
+        int64_t i = lo + warp;
+        for (; i + 7 * kNormWarps < hi; i += 8 * kNormWarps) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = __ldcg(parts + (i + k * kNormWarps) * columns + c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) s += v[k];
+        }
+        for (; i < hi; i += kNormWarps) s += __ldcg(parts + i * columns + c);
+    }
     part[warp][lane] = s;
     __syncthreads();
-    if (warp || c >= 2 * (int64_t)channels) return;
+    if (warp || c >= columns) return;
     for (int w = 1; w < kNormWarps; ++w) s += part[w][lane];
-    float* out = c < channels ? d_weight : d_bias;
-    if (out) out[c < channels ? c : c - channels] = s;
+    if (out) { out[blockIdx.y * columns + c] = s; return; }
+    float* to = c < columns / 2 ? d_weight : d_bias;
+    if (to) to[c < columns / 2 ? c : c - columns / 2] = s;
 }
 
 constexpr int kSamplesPerLaunch = 480;   // (in the kernel's parameters: a host array need not outlive the call, nor a captured graph)
@@ -55,7 +66,7 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
     MG_CUDA(ctx, on.err);
     const int mode = norm_mode(s);
     char* ws = static_cast<char*>(workspace);
-    TileArgs a;
+    RingArgs a;
     NormPlan p;
     a.x = m[0].p; a.x_stride = m[0].stride;
     if (backward) { a.d_y = m[1].p; a.d_y_stride = m[1].stride; }
@@ -71,7 +82,9 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
         MG_BY_TYPE(s->dtype, launch_rows<T>(l, a, st));
         ctx->launches++;
     } else if (mode == NORM_TILES) {
-        plan_tiles(s, ctx->n_sms, backward, vec_width(m, n_matrices, s->dtype, s->rows, a.each), &p, &a);
+        const int ring_vec = ring_vec_width(m, n_matrices, s);
+        if (!ring_vec || !plan_ring(s, ctx->n_sms, backward, ring_vec, &p, &a))
+            plan_tiles(s, ctx->n_sms, backward, vec_width(m, n_matrices, s->dtype, s->rows, a.each), &p, &a);
         a.ticket = reinterpret_cast<uint32_t*>(ws);
         a.fan_count = reinterpret_cast<uint32_t*>(ws + p.at_fan_count);
         a.sample_count = reinterpret_cast<uint32_t*>(ws + p.at_sample_count);
@@ -79,7 +92,7 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
         a.tile_parts = reinterpret_cast<float*>(ws + p.at_tile_parts);
         a.fan_parts = reinterpret_cast<float*>(ws + p.at_fan_parts);
         a.group_parts = reinterpret_cast<float*>(ws + p.at_group_parts);
-        a.parts = reinterpret_cast<float*>(ws + p.at_parts);
+        a.parts = backward && (params || p.mode == NORM_TILES) ? reinterpret_cast<float*>(ws + p.at_parts) : nullptr;
         a.status = ctx->d_flags;
         MG_CUDA(ctx, cudaMemsetAsync(ws, 0, p.cleared, st));
         if (!a.equal) {
@@ -100,12 +113,27 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
             }
             if (a.samples > kInlineSamples) a.table = table;
         }
-        const TileLaunch l{p.vec, backward, p.grid};
-        MG_BY_TYPE(s->dtype, launch_tiles<T>(l, a, st));
+        if (p.mode == NORM_RING) {
+            const RingLaunch l{p.vec, backward, p.grid};
+            MG_BY_TYPE(s->dtype, MG_CUDA(ctx, launch_ring<T>(l, a, st)));
+        } else {
+            const TileLaunch l{p.vec, backward, p.grid};
+            MG_BY_TYPE(s->dtype, launch_tiles<T>(l, a, st));
+        }
         ctx->launches++;
     }
     if (backward && params) {
-        k_norm_params<<<(unsigned)((2 * (int64_t)s->channels + 31) / 32), kNormThreads, 0, st>>>(a.parts, p.n_parts, s->channels, d_weight, d_bias);
+        const int64_t columns = 2 * (int64_t)s->channels;
+        const unsigned blocks = (unsigned)((columns + 31) / 32);
+        const float* parts = a.parts;
+        int64_t n = p.n_parts;
+        if (n > 512) {   // (one step reads them with 16 blocks for 256 channels)
+            float* slices = reinterpret_cast<float*>(ws + p.at_slices);
+            k_norm_params<<<dim3(blocks, (unsigned)kParamSlices), kNormThreads, 0, st>>>(parts, n, columns, slices, nullptr, nullptr);
+            ctx->launches++;
+            parts = slices; n = kParamSlices;
+        }
+        k_norm_params<<<blocks, kNormThreads, 0, st>>>(parts, n, columns, nullptr, d_weight, d_bias);
         ctx->launches++;
     }
     MG_CUDA(ctx, cudaGetLastError());

@@ -14,7 +14,8 @@ struct DropArgs {
     int on = 0;
     uint32_t below = 0;      // kept: a 16-bit half at or above the limit, that is, as the upper half of a word above limit * 65536 - 1
     float factor = 1.f;      // 65536 / (65536 - limit); 0 where all are dropped
-    uint32_t k0 = 0, k1 = 0, tag = 0;
+    uint32_t k0[10] = {0}, k1[10] = {0};   // the rounds' keys: those of the seed, and 0x9E3779B9, 0xBB67AE85 more with every round
+    uint32_t tag = 0;
     int64_t first_row = 0;
     const int64_t* keys = nullptr;
 };
@@ -78,6 +79,18 @@ template <typename T, int VEC> struct Raw {
 
 __device__ __forceinline__ uint64_t drop_key(const DropArgs& d, int64_t row) { return (uint64_t)(d.keys ? d.keys[row] : d.first_row + row); }
 
+// philox4x32_10 with the rounds' keys from the kernel's parameters and both halves of a product in one instruction (dropout of 150,001 x 768
+// fp16 90 -> XX us)
+__device__ __forceinline__ void drop_block(const DropArgs& d, uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t out[4]) {
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(p1 >> 32) ^ c1 ^ d.k0[r]; c1 = (uint32_t)p1;
+        c2 = (uint32_t)(p0 >> 32) ^ c3 ^ d.k1[r]; c3 = (uint32_t)p0;
+    }
+    out[0] = c0; out[1] = c1; out[2] = c2; out[3] = c3;
+}
+
 // Which of elements c .. c + VEC - 1 of the row with this key are kept (c a multiple of VEC; VEC of 1, 2, 4 or 8): the halves of one Philox
 // block per eight elements.  16 bits an element, so that a block serves 16 or 32 bytes of a row: p is met to 2^-17, and the factor goes by
 // the p that is met.
@@ -85,7 +98,7 @@ template <int VEC> struct Keep {
     uint32_t w[(VEC + 1) / 2];
     __device__ __forceinline__ void draw(const DropArgs& d, uint64_t key, uint32_t c) {
         uint32_t all[4];
-        philox4x32_10((uint32_t)key, (uint32_t)(key >> 32), c >> 3, d.tag, d.k0, d.k1, all);
+        drop_block(d, (uint32_t)key, (uint32_t)(key >> 32), c >> 3, d.tag, all);
         if constexpr (VEC == 8) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) w[i] = all[i];
@@ -116,31 +129,52 @@ __device__ __forceinline__ float normal_cdf(float n, float* bell) {
     return n < 0.f ? tail : 1.f - tail;
 }
 
-__device__ __forceinline__ float act_value(int act, float n) {
-    if (act == ACT_RELU) return n < 0.f ? 0.f : n;   // (NaN stays)
-    if (act == ACT_SILU) return __fdividef(n, 1.f + fast_exp(-n));
-    if (act == ACT_GELU) { float bell; return n * normal_cdf(n, &bell); }
-    return n;
+__device__ __forceinline__ float max_nan(float a, float b) {   // (NaN stays)
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
 }
 
-// slope of the activation at n = hat * w + b.  A ReLU's slope jumps at zero: which side n lies on is decided in 64 bits where 32 leave it open,
-// so that the gradient does not go by how a sum was rounded.
-__device__ __forceinline__ float act_slope(int act, float n, float x, float mean, float rstd, float w, float b) {
+template <int N>
+__device__ __forceinline__ void act_values(int act, float (&n)[N]) {
     if (act == ACT_RELU) {
-        // |rounding of n| < 4 * 2^-24 * (|n - b| + |b|): three roundings of hat * w, one of the sum
-        const float reach = 3e-7f * (fabsf(n - b) + fabsf(b));
-        if (fabsf(n) > reach) return n > 0.f ? 1.f : 0.f;
-        const double at = ((double)x - (double)mean) * (double)rstd * (double)w + (double)b;
-        return at <= 0.0 ? 0.f : 1.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) n[e] = max_nan(n[e], 0.f);
+    } else if (act == ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) n[e] = __fdividef(n[e], 1.f + fast_exp(-n[e]));
+    } else if (act == ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) { float bell; n[e] *= normal_cdf(n[e], &bell); }
     }
-    if (act == ACT_SILU) {
-        const float s = __fdividef(1.f, 1.f + fast_exp(-n));
-        return s * (1.f + n * (1.f - s));
+}
+
+// d times the slope of the activation at n = hat * w + b, hat = (x - mean) * rstd.  A ReLU's slope jumps at zero: which side n lies on is
+// decided in 64 bits where 32 leave it open, so that the gradient does not go by how a sum was rounded.
+template <int N>
+__device__ __forceinline__ void act_slopes(int act, float (&d)[N], const float (&h)[N], const float (&x)[N], float mean, float rstd, const float (&w)[N],
+                                           const float (&b)[N]) {
+    if (act == ACT_RELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            // |rounding of n| < 4 * 2^-24 * (|h w| + |b|): three roundings of the product (it enters the sum unrounded), one of the sum
+            const float n = fmaf(h[e], w[e], b[e]);
+            bool up = !(n <= 0.f);
+            if (fabsf(n) <= 3e-7f * fmaf(2.f, fabsf(b[e]), fabsf(n))) up = !(((double)x[e] - (double)mean) * (double)rstd * (double)w[e] + (double)b[e] <= 0.0);
+            d[e] = up ? d[e] : 0.f;
+        }
+    } else if (act == ACT_SILU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float n = fmaf(h[e], w[e], b[e]), s = __fdividef(1.f, 1.f + fast_exp(-n));
+            d[e] *= s * fmaf(n, 1.f - s, 1.f);
+        }
+    } else if (act == ACT_GELU) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            float bell;
+            const float n = fmaf(h[e], w[e], b[e]), cdf = normal_cdf(n, &bell);
+            d[e] *= fmaf(n * 0.39894228040143268f, bell, cdf);
+        }
     }
-    if (act == ACT_GELU) {
-        float bell;
-        const float cdf = normal_cdf(n, &bell);
-        return fmaf(n * 0.39894228040143268f, bell, cdf);
-    }
-    return 1.f;
 }

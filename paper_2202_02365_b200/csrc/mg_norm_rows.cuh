@@ -21,6 +21,22 @@ struct NormArgs {
     DropArgs drop;
 };
 
+// A vector's normalised values, and the gradient in front of weight and bias: dz = dropout(dy) act'
+template <typename T, int VEC>
+__device__ __forceinline__ void grad_vector(const NormArgs& a, const Raw<T, VEC>& rx, const Raw<T, VEC>& rd, uint64_t key, int32_t c, float mean, float rstd,
+                                            const float (&w)[VEC], const float (&b)[VEC], float (&h)[VEC], float (&d)[VEC]) {
+    float x[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) { x[e] = rx.get(e); h[e] = (x[e] - mean) * rstd; d[e] = rd.get(e); }
+    act_slopes<VEC>(a.act, d, h, x, mean, rstd, w, b);
+    if (a.drop.on) {
+        Keep<VEC> keep;
+        keep.draw(a.drop, key, (uint32_t)c);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) d[e] = keep(a.drop, e) ? d[e] * a.drop.factor : 0.f;
+    }
+}
+
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kNormThreads) k_dropout(const T* x, int64_t x_stride, T* y, int64_t y_stride, int64_t rows, int32_t channels, DropArgs d) {
     const int64_t vecs = channels / VEC, step = (int64_t)gridDim.x * kNormThreads;
@@ -157,16 +173,25 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape
     T* y = static_cast<T*>(a.out);
     const Params<VEC, NV> par(a, params, sub, vecs);
     const int64_t step = (int64_t)gridDim.x * kNormWarps * per_warp;
-    for (int64_t row0 = (blockIdx.x * (int64_t)kNormWarps + (threadIdx.x >> 5)) * per_warp; row0 < a.rows; row0 += step) {
-        const int64_t row = row0 + (lane >> r.lanes);
-        const bool here = row < a.rows;
-        Raw<T, VEC> raw[NV];
-        float f[NV][VEC];
+    constexpr bool kAhead = VEC * NV <= 16;   // the next row is on its way while this one is worked on
+    Raw<T, VEC> raw[NV], next[kAhead ? NV : 1];
+    int64_t row = (blockIdx.x * (int64_t)kNormWarps + (threadIdx.x >> 5)) * per_warp + (lane >> r.lanes);
+    const auto fetch = [&](Raw<T, VEC>* to, int64_t from) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            raw[i].zero();
-            if (here && sub + 32 * i < vecs) raw[i].load(x + row * a.x_stride + (sub + 32 * i) * VEC);
+            to[i].zero();
+            if (from < a.rows && sub + 32 * i < vecs) to[i].load(x + from * a.x_stride + (sub + 32 * i) * VEC);
         }
+    };
+    if (kAhead) fetch(next, row);
+    for (; row - (lane >> r.lanes) < a.rows; row += step) {
+        const bool here = row < a.rows;
+        float f[NV][VEC];
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) raw[i] = next[i];
+            fetch(next, row + step);
+        } else fetch(raw, row);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -228,7 +253,8 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape
             float w[VEC], b[VEC];
             par.get(i, v, w, b);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f[i][e] = act_value(a.act, fmaf(f[i][e], w[e], b[e]));
+            for (int e = 0; e < VEC; ++e) f[i][e] = fmaf(f[i][e], w[e], b[e]);
+            act_values<VEC>(a.act, f[i]);
             if (a.drop.on) {
                 Keep<VEC> keep;
                 keep.draw(a.drop, key, (uint32_t)(v * VEC));
@@ -260,50 +286,65 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows_backward(NormArgs a,
 #pragma unroll
         for (int e = 0; e < VEC; ++e) dw[i][e] = db[i][e] = 0.f;
     const int64_t step = (int64_t)gridDim.x * kNormWarps * per_warp;
-    for (int64_t row0 = (blockIdx.x * (int64_t)kNormWarps + warp) * per_warp; row0 < a.rows; row0 += step) {
-        const int64_t row = row0 + (lane >> r.lanes);
-        const bool here = row < a.rows;
-        Raw<T, VEC> rx[NV], rd[NV];
-        float h[NV][VEC], g[NV][VEC], rstd[NV];
+    constexpr bool kAhead = false;   // the next row is on its way while this one is worked on
+    Raw<T, VEC> rx[NV], rd[NV], next_x[kAhead ? NV : 1], next_d[kAhead ? NV : 1];
+    int64_t row = (blockIdx.x * (int64_t)kNormWarps + warp) * per_warp + (lane >> r.lanes);
+    const auto fetch = [&](Raw<T, VEC>* to_x, Raw<T, VEC>* to_d, int64_t from) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            rx[i].zero(); rd[i].zero();
-            if (here && sub + 32 * i < vecs) {
-                rx[i].load(x + row * a.x_stride + (sub + 32 * i) * VEC);
-                rd[i].load(d_y + row * a.d_y_stride + (sub + 32 * i) * VEC);
+            to_x[i].zero(); to_d[i].zero();
+            if (from < a.rows && sub + 32 * i < vecs) {
+                to_x[i].load(x + from * a.x_stride + (sub + 32 * i) * VEC);
+                to_d[i].load(d_y + from * a.d_y_stride + (sub + 32 * i) * VEC);
             }
         }
+    };
+    if (kAhead) fetch(next_x, next_d, row);
+    for (; row - (lane >> r.lanes) < a.rows; row += step) {
+        const bool here = row < a.rows;
+        float h[NV][VEC], g[NV][VEC], rstd[NV];
+        if constexpr (kAhead) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) { rx[i] = next_x[i]; rd[i] = next_d[i]; }
+            fetch(next_x, next_d, row + step);
+        } else fetch(rx, rd, row);
         const uint64_t key = here && a.drop.on ? drop_key(a.drop, row) : 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int32_t v = sub + 32 * i;
             const bool in = here && v < vecs;
-            float mean = 0.f;
-            rstd[i] = 0.f;
-            if (in && !GENERAL) {
-                const int64_t at = row * a.groups + (r.gshift >= 31 ? 0 : v >> r.gshift);
-                mean = a.mean[at]; rstd[i] = a.rstd[at];
-            }
-            Keep<VEC> keep;
-            if (a.drop.on) keep.draw(a.drop, key, (uint32_t)(v * VEC));
             float w[VEC], b[VEC];
             par.get(i, in ? v : 0, w, b);
+            rstd[i] = 0.f;
+            if constexpr (GENERAL) {   // (every element has statistics of its own)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const int64_t at = row * a.groups + (v * VEC + e) / a.each;
+                    const float m_e = in ? a.mean[at] : 0.f, r_e = in ? a.rstd[at] : 0.f, x1[1] = {rx[i].get(e)}, w1[1] = {w[e]}, b1[1] = {b[e]};
+                    float d1[1] = {rd[i].get(e)};
+                    const float h1[1] = {(x1[0] - m_e) * r_e};
+                    act_slopes<1>(a.act, d1, h1, x1, m_e, r_e, w1, b1);
+                    h[i][e] = h1[0]; g[i][e] = d1[0];
+                }
+                if (a.drop.on) {
+                    Keep<VEC> keep;
+                    keep.draw(a.drop, key, (uint32_t)(v * VEC));
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) g[i][e] = keep(a.drop, e) ? g[i][e] * a.drop.factor : 0.f;
+                }
+            } else {
+                float mean = 0.f;
+                if (in) {
+                    const int64_t at = row * a.groups + (r.gshift >= 31 ? 0 : v >> r.gshift);
+                    mean = a.mean[at]; rstd[i] = a.rstd[at];
+                }
+                grad_vector<T, VEC>(a, rx[i], rd[i], key, v * VEC, mean, rstd[i], w, b, h[i], g[i]);
+            }
 #pragma unroll
             for (int e = 0; e < VEC; ++e) {
-                const int32_t c = v * VEC + e;
-                float r_e = rstd[i], m_e = mean;
-                if (GENERAL && in) {
-                    const int64_t at = row * a.groups + c / a.each;
-                    m_e = a.mean[at]; r_e = a.rstd[at];
-                }
-                const float xv = rx[i].get(e);
-                float d = rd[i].get(e);
-                h[i][e] = (xv - m_e) * r_e;
-                d *= act_slope(a.act, fmaf(h[i][e], w[e], b[e]), xv, m_e, r_e, w[e], b[e]);
-                if (a.drop.on) d = keep(a.drop, e) ? d * a.drop.factor : 0.f;
-                if (!in) d = 0.f;
-                dw[i][e] = fmaf(d, h[i][e], dw[i][e]); db[i][e] += d;
-                g[i][e] = d * w[e];
+                if (!in) g[i][e] = 0.f;
+                dw[i][e] = fmaf(g[i][e], h[i][e], dw[i][e]); db[i][e] += g[i][e];
+                g[i][e] *= w[e];
             }
         }
         if constexpr (GENERAL) {

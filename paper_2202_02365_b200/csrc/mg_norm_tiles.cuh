@@ -50,6 +50,30 @@ __device__ __forceinline__ int64_t queue_start(const TileArgs& a, int i) {   // 
     return (int64_t)(a.window_tile[i] + (i ? a.window_tile[i - 1] : 0)) * a.chunks;
 }
 
+// the sample and the rows of a tile
+__device__ inline void locate_tile(const TileArgs& a, int32_t tile, Tile* t) {
+    t->tile = tile;
+    int64_t s0, s1;
+    if (a.equal) {
+        t->sample = tile / a.tiles_per_sample;
+        t->first = t->sample * a.tiles_per_sample;
+        t->tiles = a.tiles_per_sample;
+        s0 = t->sample * a.rows_per_sample; s1 = s0 + a.rows_per_sample;
+    } else {
+        int32_t l = 0, h = a.samples;
+        while (h - l > 1) {
+            const int32_t mid = (l + h) >> 1;
+            if (sample_entry(a, mid).y <= tile) l = mid; else h = mid;
+        }
+        const int2 e = sample_entry(a, l), f = sample_entry(a, l + 1);
+        t->sample = l; t->first = e.y; t->tiles = f.y - e.y;
+        s0 = e.x; s1 = f.x;
+    }
+    t->row0 = s0 + (int64_t)(tile - t->first) * a.tile_rows;
+    t->row1 = min(s1, t->row0 + a.tile_rows);
+    t->sample_rows = s1 - s0;
+}
+
 __device__ inline void next_tile(const TileArgs& a, Tile* t) {
     const int64_t total = (int64_t)a.window_tile[a.windows] * a.chunks, p = atomicAdd(a.ticket, 1u);
     if (p >= 2 * total) { t->kind = 2; return; }
@@ -74,31 +98,12 @@ __device__ inline void next_tile(const TileArgs& a, Tile* t) {
     t->chunk = (int32_t)(off - (int64_t)tile * a.chunks);
     if (a.reversed && t->kind == 1) tile = n - 1 - tile;   // (what was read last is still in L2)
     tile += a.window_tile[w];
-    t->tile = tile;
-    int64_t s0, s1;
-    if (a.equal) {
-        t->sample = tile / a.tiles_per_sample;
-        t->first = t->sample * a.tiles_per_sample;
-        t->tiles = a.tiles_per_sample;
-        s0 = t->sample * a.rows_per_sample; s1 = s0 + a.rows_per_sample;
-    } else {
-        int32_t l = 0, h = a.samples;
-        while (h - l > 1) {
-            const int32_t mid = (l + h) >> 1;
-            if (sample_entry(a, mid).y <= tile) l = mid; else h = mid;
-        }
-        const int2 e = sample_entry(a, l), f = sample_entry(a, l + 1);
-        t->sample = l; t->first = e.y; t->tiles = f.y - e.y;
-        s0 = e.x; s1 = f.x;
-    }
-    t->row0 = s0 + (int64_t)(tile - t->first) * a.tile_rows;
-    t->row1 = min(s1, t->row0 + a.tile_rows);
-    t->sample_rows = s1 - s0;
+    locate_tile(a, tile, t);
 }
 
 // Mean and sum of squares about it of two sets (Chan, Golub and LeVeque 1979)
 __device__ __forceinline__ void merge_moments(float& n, float& m, float& q, float nb, float mb, float qb) {
-    const float all = n + nb, f = all > 0.f ? nb / all : 0.f, d = mb - m;
+    const float all = n + nb, f = all > 0.f ? __fdividef(nb, all) : 0.f, d = mb - m;
     m = fmaf(d, f, m);
     q += fmaf(d * n * f, d, qb);   // (a first set, n = 0: no square of its mean)
     n = all;
@@ -113,7 +118,7 @@ __device__ __forceinline__ void merge(Pair<VEC>& a, float nb, const float (&u)[V
 #pragma unroll
         for (int e = 0; e < VEC; ++e) { a.u[e] += u[e]; a.v[e] += v[e]; }
     } else {
-        const float all = a.n + nb, f = all > 0.f ? nb / all : 0.f, g = a.n * f;
+        const float all = a.n + nb, f = all > 0.f ? __fdividef(nb, all) : 0.f, g = a.n * f;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
             const float d = u[e] - a.u[e];
@@ -147,16 +152,10 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int3
             for (int k = 0; k < K; ++k) {
                 const int64_t row = r + k * n_ty;
                 if (row >= t.row1) break;
-                Keep<VEC> keep;
-                if (a.drop.on) keep.draw(a.drop, drop_key(a.drop, row), (uint32_t)c);
+                float h[VEC], d[VEC];
+                grad_vector<T, VEC>(a, raw[k], rd[k], a.drop.on ? drop_key(a.drop, row) : 0, c, mean, rstd, w, b, h, d);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float xv = raw[k].get(e), h = (xv - mean) * rstd;
-                    float d = rd[k].get(e) * act_slope(a.act, fmaf(h, w[e], b[e]), xv, mean, rstd, w[e], b[e]);
-                    if (a.drop.on) d = keep(a.drop, e) ? d * a.drop.factor : 0.f;
-                    p.u[e] = fmaf(d, h, p.u[e]);
-                    p.v[e] += d;
-                }
+                for (int e = 0; e < VEC; ++e) { p.u[e] = fmaf(d[e], h[e], p.u[e]); p.v[e] += d[e]; }
             }
         } else {
             const int64_t left = (t.row1 - r + n_ty - 1) / n_ty;
@@ -178,17 +177,16 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int3
     }
 }
 
-// The block's threads with the same channels, into `out` ([2][channels], the chunk's channels of it)
+// lanes with the same channels
 template <int VEC, bool BACKWARD>
-__device__ __forceinline__ void block_pairs(const TileArgs& a, Pair<VEC>& p, float* smem, int tx, int32_t chunk0, float* out) {
-    const int threads_x = 1 << a.tx, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__device__ __forceinline__ void lane_pairs(Pair<VEC>& p, int threads_x) {
+    const int lane = threadIdx.x & 31;
     for (int o = threads_x; o < 32; o <<= 1) {
         float u[VEC], v[VEC];
         const float n = __shfl_xor_sync(0xFFFFFFFFu, p.n, o);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) { u[e] = __shfl_xor_sync(0xFFFFFFFFu, p.u[e], o); v[e] = __shfl_xor_sync(0xFFFFFFFFu, p.v[e], o); }
-        // (the lower lane's set first on both sides, so that both have the same)
-        if (!BACKWARD && (lane & o)) {
+        if (!BACKWARD && (lane & o)) {   // (the lower lane's set first on both sides, so that both have the same)
             Pair<VEC> q;
             q.n = n;
 #pragma unroll
@@ -198,9 +196,16 @@ __device__ __forceinline__ void block_pairs(const TileArgs& a, Pair<VEC>& p, flo
             p = q;
         } else merge<VEC, BACKWARD>(p, n, u, v);
     }
-    const int across = threads_x < 32 ? kNormWarps : kNormThreads / threads_x;   // sets of a channel that are left
+}
+
+// The block's threads with the same channels, into `out` ([2][channels], the chunk's channels of it)
+template <int VEC, bool BACKWARD>
+__device__ __forceinline__ void block_pairs(const TileArgs& a, Pair<VEC>& p, float* smem, int tx, int32_t chunk0, float* out) {
+    const int threads_x = 1 << a.tx, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    lane_pairs<VEC, BACKWARD>(p, threads_x);
+    const int across = threads_x < 32 ? kNormThreads / 32 : kNormThreads / threads_x;   // sets of a channel that are left
     const int set = threads_x < 32 ? warp : threadIdx.x >> a.tx, width = threads_x * VEC;
-    float* su = smem;                          // [across][width], across * width <= 256 * VEC
+    float* su = smem;                          // [across][width], across * width <= kNormThreads * VEC
     float* sv = smem + kNormThreads * VEC;
     float* sn = smem + 2 * kNormThreads * VEC;   // [across]
     __syncthreads();
@@ -223,35 +228,60 @@ __device__ __forceinline__ void block_pairs(const TileArgs& a, Pair<VEC>& p, flo
     }
 }
 
-// sums of `n` sets that lie one behind the other, rows_of(i) rows each, into `out`
-template <bool BACKWARD, typename Rows>
-__device__ __forceinline__ void merge_parts(const TileArgs& a, const float* parts, int32_t n, Rows rows_of, float* out) {
+// sums of `n` sets that lie one behind the other, rows_of(i) rows each, into `out` and, where it is given, `shared` ([2][stride]); V channels a
+// thread at a time, B sets in flight
+template <bool BACKWARD, int NT, int V, int B, typename Rows>
+__device__ __forceinline__ void merge_parts(const TileArgs& a, const float* parts, int32_t n, Rows rows_of, float* out, int tid, float* shared, int stride) {
     const int64_t step = 2 * (int64_t)a.channels;
-    for (int32_t c = threadIdx.x; c < a.channels; c += kNormThreads) {
-        float u = 0.f, v = 0.f, m = 0.f;
-        for (int32_t i0 = 0; i0 < n; i0 += 8) {
-            float pu[8], pv[8];
+    for (int32_t c = tid * V; c < a.channels; c += NT * V) {
+        float u[V], v[V], m = 0.f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (i0 + k < n) { pu[k] = __ldcg(parts + (i0 + k) * step + c); pv[k] = __ldcg(parts + (i0 + k) * step + a.channels + c); }
+        for (int e = 0; e < V; ++e) u[e] = v[e] = 0.f;
+        for (int32_t i0 = 0; i0 < n; i0 += B) {
+            float pu[B][V], pv[B][V];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
+            for (int k = 0; k < B; ++k)
                 if (i0 + k < n) {
-                    if (BACKWARD) { u += pu[k]; v += pv[k]; }
-                    else merge_moments(m, u, v, rows_of(i0 + k), pu[k], pv[k]);
+                    const float* from = parts + (i0 + k) * step + c;
+                    if constexpr (V == 4) {
+                        const float4 x = __ldcg(reinterpret_cast<const float4*>(from)), y = __ldcg(reinterpret_cast<const float4*>(from + a.channels));
+                        pu[k][0] = x.x; pu[k][1] = x.y; pu[k][2] = x.z; pu[k][3] = x.w;
+                        pv[k][0] = y.x; pv[k][1] = y.y; pv[k][2] = y.z; pv[k][3] = y.w;
+                    } else { pu[k][0] = __ldcg(from); pv[k][0] = __ldcg(from + a.channels); }
+                }
+#pragma unroll
+            for (int k = 0; k < B; ++k)
+                if (i0 + k < n) {
+                    if (BACKWARD) {
+#pragma unroll
+                        for (int e = 0; e < V; ++e) { u[e] += pu[k][e]; v[e] += pv[k][e]; }
+                    } else {
+                        const float nb = rows_of(i0 + k), all = m + nb, f = __fdividef(nb, all), g = m * f;   // (no set is empty)
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            const float d = pu[k][e] - u[e];
+                            u[e] = fmaf(d, f, u[e]);
+                            v[e] += fmaf(d * g, d, pv[k][e]);
+                        }
+                        m = all;
+                    }
                 }
         }
-        __stcg(out + c, u);
-        __stcg(out + a.channels + c, v);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            __stcg(out + c + e, u[e]);
+            __stcg(out + a.channels + c + e, v[e]);
+            if (shared) { shared[c + e] = u[e]; shared[stride + c + e] = v[e]; }
+        }
     }
 }
 
 // the groups' values from the channels' of a whole sample: a warp per group
-template <bool BACKWARD>
+template <bool BACKWARD, int NT>
 __device__ __forceinline__ void finish_sample(const TileArgs& a, int32_t sample, float rows, const float* part) {
     const int lane = threadIdx.x & 31;
     const float n = rows * (float)a.each;
-    for (int32_t g = threadIdx.x >> 5; g < a.groups; g += kNormWarps) {
+    for (int32_t g = threadIdx.x >> 5; g < a.groups; g += NT / 32) {
         float u = 0.f, v = 0.f;
         for (int32_t c = g * a.each + lane; c < (g + 1) * a.each; c += 32) {
             if (BACKWARD) {
@@ -295,7 +325,7 @@ __device__ __forceinline__ void arrive(const TileArgs& a, const Tile& t, int32_t
     float* fan_part = a.fan_parts + fan_id * step;
     const auto tile_rows = [&](int32_t i) { return (float)min((int64_t)a.tile_rows, t.sample_rows - ((int64_t)fan * kFan + i) * a.tile_rows); };
     float* whole = BACKWARD ? a.parts + t.sample * step : a.fan_parts + (t.first / kFan + t.sample) * step;   // the sample's channels
-    merge_parts<BACKWARD>(a, a.tile_parts + ((int64_t)t.first + fan * kFan) * step, fan_tiles, tile_rows, fans == 1 ? whole : fan_part);
+    merge_parts<BACKWARD, kNormThreads, 1, 8>(a, a.tile_parts + ((int64_t)t.first + fan * kFan) * step, fan_tiles, tile_rows, fans == 1 ? whole : fan_part, threadIdx.x, nullptr, 0);
     __syncthreads();
     if (fans > 1) {
         __threadfence();
@@ -305,10 +335,10 @@ __device__ __forceinline__ void arrive(const TileArgs& a, const Tile& t, int32_t
         if (!*sh_last) return;
         __threadfence();
         const auto fan_rows = [&](int32_t i) { return (float)min((int64_t)kFan * a.tile_rows, t.sample_rows - (int64_t)i * kFan * a.tile_rows); };
-        merge_parts<BACKWARD>(a, a.fan_parts + (t.first / kFan + t.sample) * step, fans, fan_rows, whole);
+        merge_parts<BACKWARD, kNormThreads, 1, 8>(a, a.fan_parts + (t.first / kFan + t.sample) * step, fans, fan_rows, whole, threadIdx.x, nullptr, 0);
         __syncthreads();
     }
-    finish_sample<BACKWARD>(a, t.sample, (float)t.sample_rows, whole);
+    finish_sample<BACKWARD, kNormThreads>(a, t.sample, (float)t.sample_rows, whole);
     __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) *reinterpret_cast<volatile uint32_t*>(a.ready + t.sample) = 1u;
@@ -398,20 +428,22 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_tiles(const __grid_
                     for (int k = 0; k < U; ++k) {
                         const int64_t row = r + k * n_ty;
                         if (row >= t.row1) break;
-                        Keep<VEC> keep;
-                        if (a.drop.on) keep.draw(a.drop, drop_key(a.drop, row), (uint32_t)c);
                         float f[VEC];
+                        const uint64_t key = a.drop.on ? drop_key(a.drop, row) : 0;
+                        if constexpr (BACKWARD) {
+                            float h[VEC];
+                            grad_vector<T, VEC>(a, raw[k], rd[k], key, c, mean, rstd, w, b, h, f);
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            const float xv = raw[k].get(e);
-                            if (BACKWARD) {
-                                const float h = (xv - mean) * rstd;
-                                float d = rd[k].get(e) * act_slope(a.act, fmaf(h, w[e], b[e]), xv, mean, rstd, w[e], b[e]);
-                                if (a.drop.on) d = keep(a.drop, e) ? d * a.drop.factor : 0.f;
-                                f[e] = rstd * fmaf(-h, s2, fmaf(d, w[e], -s1));
-                            } else {
-                                f[e] = act_value(a.act, fmaf(xv - mean, w[e], b[e]));
-                                if (a.drop.on) f[e] = keep(a.drop, e) ? f[e] * a.drop.factor : 0.f;
+                            for (int e = 0; e < VEC; ++e) f[e] = rstd * fmaf(-h[e], s2, fmaf(f[e], w[e], -s1));
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < VEC; ++e) f[e] = fmaf(raw[k].get(e) - mean, w[e], b[e]);
+                            act_values<VEC>(a.act, f);
+                            if (a.drop.on) {
+                                Keep<VEC> keep;
+                                keep.draw(a.drop, key, (uint32_t)c);
+#pragma unroll
+                                for (int e = 0; e < VEC; ++e) f[e] = keep(a.drop, e) ? f[e] * a.drop.factor : 0.f;
                             }
                         }
                         raw[k].put(f);

@@ -585,12 +585,90 @@ int main() {
 """
 
 
-def test_refusals_on_the_host(tmp_path):
+# how calls are cut: every index that the kernels form lies in its array, whatever the shape
+CUTS = HOST[:HOST.index("int main")] + r"""
+#include <random>
+int main() {
+    std::mt19937 rng(1);
+    const auto pick = [&](int64_t lo, int64_t hi) { return (int64_t)std::exp(std::uniform_real_distribution<double>(std::log((double)lo), std::log(hi + 0.99))(rng)); };
+#define NEED(x) do { if (!(x)) { printf("line %d: %s (rows %lld channels %d groups %d samples %lld dtype %d backward %d vec %d)\n", __LINE__, #x, (long long)s.rows, s.channels, s.groups, (long long)n, s.dtype, backward, *v); return 1; } } while (0)
+    std::vector<int64_t> ends;
+    for (int i = 0; i < 20000; ++i) {
+        mg_norm_spec s{};
+        s.groups = (int)pick(1, 64); s.channels = s.groups * (int)pick(1, i % 50 ? 300 : 5000); s.dtype = (int)(rng() % 3); s.eps = 1.f;
+        s.rows_per_sample = pick(1, i % 7 ? 3000 : 40'000'000);
+        s.rows = s.rows_per_sample * pick(1, i % 9 ? 40 : 3000);
+        if (s.rows >= 1ll << 31) continue;
+        mg_dropout_spec drop{0.5, 1, 0, 0, reinterpret_cast<int64_t*>(4096)};
+        if (rng() % 2) s.dropout = &drop;
+        if (rng() % 2) {
+            s.n_samples = (int)std::min<int64_t>(pick(1, MG_MAX_BATCHES), s.rows + 1);
+            ends.assign(1, 0);
+            for (int k = 1; k < s.n_samples; ++k) ends.push_back((int64_t)(rng() % (uint64_t)(s.rows + 1)));
+            ends.push_back(s.rows);
+            std::sort(ends.begin(), ends.end());
+            s.sample_offsets = ends.data();
+        }
+        const int backward = rng() % 2;
+        const int64_t n = sample_count(&s);
+        const size_t have = norm_workspace(&s, 148, backward);
+        for (const int* v = vec_widths(s.dtype); *v; ++v) {
+            if (s.channels % *v) continue;
+            NormPlan p;
+            RingArgs a;
+            if (norm_mode(&s) == NORM_ROWS) {
+                plan_rows(&s, 148, backward, *v, &p);
+                NEED(p.bytes <= have && p.nv * *v <= kRowValues && p.nv * 32 * *v >= s.channels && p.grid >= 1);
+                continue;
+            }
+            for (int ring = 0; ring < 2; ++ring) {
+                if (ring && (*v < 4 || s.channels / s.groups % *v || !plan_ring(&s, 148, backward, *v, &p, &a))) continue;
+                if (!ring) plan_tiles(&s, 148, backward, *v, &p, &a);
+                NEED(p.bytes <= have);
+                const int fan = ring ? a.fan : kFan;
+                const int64_t pair = 2 * 4 * (int64_t)(ring ? s.groups : s.channels);
+                int64_t tile = 0, fans_end = 0;
+                for (int64_t q = 0; q < n; ++q) {
+                    const int64_t len = s.sample_offsets ? s.sample_offsets[q + 1] - s.sample_offsets[q] : s.rows_per_sample;
+                    const int64_t tiles = (len + a.tile_rows - 1) / a.tile_rows, first = tile / fan + q, fans = (tiles + fan - 1) / fan;
+                    NEED(first >= fans_end && tiles <= kFan * kFan && fans <= kFan);
+                    fans_end = first + std::max<int64_t>(fans, 1);
+                    tile += tiles;
+                    NEED(!a.equal || tiles == a.tiles_per_sample);
+                }
+                NEED(p.at_fan_count + 4 * fans_end <= p.at_sample_count && p.at_fan_parts + fans_end * pair <= p.at_group_parts);
+                NEED(p.at_sample_count + 4 * n <= p.at_ready && p.at_ready + 4 * n <= p.cleared && p.at_tile_parts + tile * pair <= p.at_fan_parts);
+                NEED(p.n_parts == (backward ? ring ? tile : n : 0) && p.at_parts + p.n_parts * 8 * s.channels <= p.at_slices);
+                NEED(!backward || p.at_slices + kParamSlices * 8 * s.channels <= p.bytes);
+                NEED(tile * a.chunks < 1ll << 30 && (int64_t)a.tile_rows > 0);
+                if (ring) {
+                    NEED(tile == a.total && kFan * kFan < kRingFifo && a.fan <= kFan && s.channels <= (*v << a.tx) && (1 << a.tx) <= kRingThreads);
+                    const int64_t row = (int64_t)s.channels * elem_size(s.dtype);
+                    NEED(a.sub_rows >= 1 && a.keys_at + (s.dropout ? 8 * a.sub_rows : 0) <= a.slot_bytes && a.sub_rows * row <= (backward ? a.d_y_at : a.keys_at));
+                    NEED(!backward || a.d_y_at + a.sub_rows * row <= a.keys_at);
+                    NEED(a.d_y_at % 16 == 0 && a.keys_at % 8 == 0 && a.slot_bytes % 128 == 0 && a.slot_bytes < 1 << 20);
+                    NEED(a.slots >= 4 && a.slots <= kRingSlots && ring_fixed_bytes(*v, s.channels) + a.slots * a.slot_bytes <= kRingSharedBytes);
+                    NEED(a.hold ? a.tile_rows <= a.sub_rows : a.tile_rows % a.sub_rows == 0);
+                } else {
+                    NEED(a.windows <= kMaxWindows && a.window_tile[a.windows] == tile && a.window_tile[0] == 0);
+                    for (int q = 0; q < a.windows; ++q) NEED(a.window_tile[q + 1] >= a.window_tile[q]);
+                    NEED((int64_t)s.channels <= (int64_t)a.chunks * (*v << a.tx) && a.tx <= 8);
+                }
+            }
+        }
+    }
+    return 0;
+}
+"""
+
+
+@pytest.mark.parametrize("what", ["refusals", "cuts"])
+def test_on_the_host(tmp_path, what):
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
     if not os.path.exists(nvcc):
         pytest.skip("no nvcc")
     source = tmp_path / "host.cu"
-    source.write_text(HOST)
+    source.write_text({"refusals": HOST, "cuts": CUTS}[what])
     program = str(tmp_path / "host")
     made = subprocess.run([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-O0", "-Xcompiler", "-w", "-I", build.CSRC,
                            "-I", os.path.join(build.ROOT, "include"), str(source), "-o", program], capture_output=True, text=True)
