@@ -66,7 +66,7 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
     MG_CUDA(ctx, on.err);
     const int mode = norm_mode(s);
     char* ws = static_cast<char*>(workspace);
-    RingArgs a;
+    TileArgs a;
     NormPlan p;
     a.x = m[0].p; a.x_stride = m[0].stride;
     if (backward) { a.d_y = m[1].p; a.d_y_stride = m[1].stride; }
@@ -82,19 +82,15 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
         MG_BY_TYPE(s->dtype, launch_rows<T>(l, a, st));
         ctx->launches++;
     } else if (mode == NORM_TILES) {
-        const int ring_vec = ring_vec_width(m, n_matrices, s);
-        if (!ring_vec || !plan_ring(s, ctx->n_sms, backward, ring_vec, &p, &a))
-            plan_tiles(s, ctx->n_sms, backward, vec_width(m, n_matrices, s->dtype, s->rows, a.each), &p, &a);
-        a.ticket = reinterpret_cast<uint32_t*>(ws);
+        plan_tiles(s, ctx->n_sms, backward, vec_width(m, n_matrices, s->dtype, s->rows, a.each), &p, &a);
         a.fan_count = reinterpret_cast<uint32_t*>(ws + p.at_fan_count);
         a.sample_count = reinterpret_cast<uint32_t*>(ws + p.at_sample_count);
-        a.ready = reinterpret_cast<uint32_t*>(ws + p.at_ready);
         a.tile_parts = reinterpret_cast<float*>(ws + p.at_tile_parts);
         a.fan_parts = reinterpret_cast<float*>(ws + p.at_fan_parts);
         a.group_parts = reinterpret_cast<float*>(ws + p.at_group_parts);
-        a.parts = backward && (params || p.mode == NORM_TILES) ? reinterpret_cast<float*>(ws + p.at_parts) : nullptr;
-        a.status = ctx->d_flags;
+        a.parts = reinterpret_cast<float*>(ws + p.at_parts);
         MG_CUDA(ctx, cudaMemsetAsync(ws, 0, p.cleared, st));
+        bool empty = false;
         if (!a.equal) {
             int2* table = reinterpret_cast<int2*>(ws + p.at_table);
             TableArgs t;
@@ -102,6 +98,7 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
             int32_t tile = 0, first = 0;
             for (int32_t i = 0; i <= a.samples; ++i) {
                 const int2 e = make_int2((int)s->sample_offsets[i], tile);
+                if (i < a.samples) empty = empty || s->sample_offsets[i + 1] == s->sample_offsets[i];
                 if (i < a.samples) tile += (int32_t)((s->sample_offsets[i + 1] - s->sample_offsets[i] + a.tile_rows - 1) / a.tile_rows);
                 if (a.samples <= kInlineSamples) { a.inl[i] = e; continue; }
                 t.at[t.n++] = e;
@@ -113,14 +110,20 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
             }
             if (a.samples > kInlineSamples) a.table = table;
         }
-        if (p.mode == NORM_RING) {
-            const RingLaunch l{p.vec, backward, p.grid};
-            MG_BY_TYPE(s->dtype, MG_CUDA(ctx, launch_ring<T>(l, a, st)));
-        } else {
-            const TileLaunch l{p.vec, backward, p.grid};
-            MG_BY_TYPE(s->dtype, launch_tiles<T>(l, a, st));
+        if (empty) {
+            k_norm_empty<<<std::min(a.samples, ctx->n_sms), 256, 0, st>>>(a, backward);
+            ctx->launches++;
         }
-        ctx->launches++;
+        const int windows = (int)p.window_tile.size() - 1;
+        for (int w = 0; windows > 0 && w <= windows; ++w) {   // the sums of window w and the results of the one before
+            a.sums_tile = p.window_tile[std::min(w, windows)];
+            a.sums_blocks = w < windows ? (p.window_tile[w + 1] - p.window_tile[w]) * a.chunks : 0;
+            a.result_tile = w ? p.window_tile[w - 1] : 0;
+            a.result_tiles = w ? p.window_tile[w] - p.window_tile[w - 1] : 0;
+            const TileLaunch l{p.vec, backward, a.sums_blocks + (int64_t)a.result_tiles * a.chunks};
+            MG_BY_TYPE(s->dtype, launch_tiles<T>(l, a, st));
+            ctx->launches++;
+        }
     }
     if (backward && params) {
         const int64_t columns = 2 * (int64_t)s->channels;

@@ -116,16 +116,18 @@ template <int VEC> struct Keep {
 
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2, ACT_GELU = 3 };   // MG_ACT_*
 
-// e^x to 2^-22 and |x| 2^-24 (the special function unit's power of two behind one product); 1 / x to 2^-22.  Where an activation uses them, either
-// enters times a factor below one: sums and statistics do without.
-__device__ __forceinline__ float fast_exp(float x) { return __expf(x); }
+// The special function unit's power of two and reciprocal, to 2^-22 (results below 2^-126 are zero).  Where an activation uses them, either enters times
+// a factor below one: sums and statistics do without.  (expf and a division take four times the instructions.)
+__device__ __forceinline__ float fast_exp2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float fast_rcp(float x) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float sigmoid(float n) { return fast_rcp(1.f + fast_exp2(-1.4426950408889634f * n)); }
 
-// (1 + erf(n / sqrt 2)) / 2 to 4 * 2^-24, by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (1.5e-7 off in erf); `bell` =
-// e^(-n^2 / 2), which the slope wants too.  A third of erff's instructions.
+// (1 + erf(n / sqrt 2)) / 2 to 4 * 2^-24, by Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26 (1.5e-7 off in erf, its
+// polynomial's coefficients halved here); `bell` = e^(-n^2 / 2), which the slope wants too.  A third of erff's instructions.
 __device__ __forceinline__ float normal_cdf(float n, float* bell) {
-    const float z = fabsf(n) * 0.70710678118654752f, t = __fdividef(1.f, fmaf(0.3275911f, z, 1.f));
-    *bell = fast_exp(-0.5f * n * n);
-    const float tail = 0.5f * *bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float t = fast_rcp(fmaf(0.3275911f * 0.70710678118654752f, fabsf(n), 1.f));
+    *bell = fast_exp2(n * n * -0.72134752044448170f);
+    const float tail = *bell * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 0.5307027145f, -0.7265760135f), 0.7107068705f), -0.142248368f), 0.127414796f);
     return n < 0.f ? tail : 1.f - tail;
 }
 
@@ -142,7 +144,7 @@ __device__ __forceinline__ void act_values(int act, float (&n)[N]) {
         for (int e = 0; e < N; ++e) n[e] = max_nan(n[e], 0.f);
     } else if (act == ACT_SILU) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) n[e] = __fdividef(n[e], 1.f + fast_exp(-n[e]));
+        for (int e = 0; e < N; ++e) n[e] *= sigmoid(n[e]);
     } else if (act == ACT_GELU) {
 #pragma unroll
         for (int e = 0; e < N; ++e) { float bell; n[e] *= normal_cdf(n[e], &bell); }
@@ -155,18 +157,24 @@ template <int N>
 __device__ __forceinline__ void act_slopes(int act, float (&d)[N], const float (&h)[N], const float (&x)[N], float mean, float rstd, const float (&w)[N],
                                            const float (&b)[N]) {
     if (act == ACT_RELU) {
+        float n[N];
+        bool near = false;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             // |rounding of n| < 4 * 2^-24 * (|h w| + |b|): three roundings of the product (it enters the sum unrounded), one of the sum
-            const float n = fmaf(h[e], w[e], b[e]);
-            bool up = !(n <= 0.f);
-            if (fabsf(n) <= 3e-7f * fmaf(2.f, fabsf(b[e]), fabsf(n))) up = !(((double)x[e] - (double)mean) * (double)rstd * (double)w[e] + (double)b[e] <= 0.0);
-            d[e] = up ? d[e] : 0.f;
+            n[e] = fmaf(h[e], w[e], b[e]);
+            near = near || fabsf(n[e]) <= 3e-7f * fmaf(2.f, fabsf(b[e]), fabsf(n[e]));
         }
+        if (near) {   // (hardly ever; the side is what is wanted of n)
+#pragma unroll
+            for (int e = 0; e < N; ++e) n[e] = (float)(((double)x[e] - (double)mean) * (double)rstd * (double)w[e] + (double)b[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) d[e] = n[e] <= 0.f ? 0.f : d[e];
     } else if (act == ACT_SILU) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float n = fmaf(h[e], w[e], b[e]), s = __fdividef(1.f, 1.f + fast_exp(-n));
+            const float n = fmaf(h[e], w[e], b[e]), s = sigmoid(n);
             d[e] *= s * fmaf(n, 1.f - s, 1.f);
         }
     } else if (act == ACT_GELU) {

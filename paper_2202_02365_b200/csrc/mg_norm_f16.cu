@@ -5,5 +5,4 @@ namespace mgnorm {
 template void launch_dropout<__half>(int, const void*, int64_t, void*, int64_t, int64_t, int32_t, const DropArgs&, int, cudaStream_t);
 template void launch_rows<__half>(const RowLaunch&, const NormArgs&, cudaStream_t);
 template void launch_tiles<__half>(const TileLaunch&, const TileArgs&, cudaStream_t);
-template cudaError_t launch_ring<__half>(const RingLaunch&, const RingArgs&, cudaStream_t);
 }

@@ -1,7 +1,7 @@
 // Launches of dropout's and group norm's kernels, by vector width.
 #pragma once
 
-#include "mg_norm_ring.cuh"
+#include "mg_norm_tiles.cuh"
 
 namespace mgnorm {
 
@@ -17,7 +17,8 @@ void launch_dropout(int vec, const void* x, int64_t x_stride, void* y, int64_t y
 
 template <typename T, int VEC, int NV>
 void launch_rows_of(const RowLaunch& l, const NormArgs& a, cudaStream_t st) {
-    const size_t params = Params<VEC, NV>::kHeld ? 0 : 2 * sizeof(float) * (size_t)a.channels, sums = 2 * sizeof(float) * (size_t)a.channels;
+    const size_t sums = 2 * sizeof(float) * (size_t)a.channels;
+    const size_t params = (l.backward ? Params<VEC, NV, true>::kHeld : Params<VEC, NV, false>::kHeld) ? 0 : sums;
     if (l.backward) {
         if (l.general) k_norm_rows_backward<T, VEC, NV, true><<<l.grid, kNormThreads, params + sums, st>>>(a, l.shape);
         else k_norm_rows_backward<T, VEC, NV, false><<<l.grid, kNormThreads, params + sums, st>>>(a, l.shape);
@@ -51,8 +52,8 @@ void launch_rows(const RowLaunch& l, const NormArgs& a, cudaStream_t st) {
 template <typename T, int VEC>
 void launch_tiles_of(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
     constexpr bool wide = sizeof(T) * VEC == 32;
-    if (l.backward) k_norm_tiles<T, VEC, true, wide ? 2 : 4, 2, 2><<<l.grid, kNormThreads, 0, st>>>(a);
-    else k_norm_tiles<T, VEC, false, wide ? 4 : 8, 4, 2><<<l.grid, kNormThreads, 0, st>>>(a);
+    if (l.backward) k_norm_tiles<T, VEC, true, wide ? 2 : 4, wide ? 1 : 2, 3><<<(unsigned)l.grid, kNormThreads, 0, st>>>(a);
+    else k_norm_tiles<T, VEC, false, wide ? 2 : 4, wide ? 2 : 4, 4><<<(unsigned)l.grid, kNormThreads, 0, st>>>(a);
 }
 
 template <typename T>
@@ -61,20 +62,6 @@ void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
     else if (l.vec == 4) launch_tiles_of<T, 4>(l, a, st);
     else if (sizeof(T) == 2 && l.vec == 2) launch_tiles_of<T, sizeof(T) == 2 ? 2 : 1>(l, a, st);
     else launch_tiles_of<T, 1>(l, a, st);
-}
-
-template <typename T, int VEC, bool BACKWARD>
-cudaError_t launch_ring_of(const RingLaunch& l, const RingArgs& a, cudaStream_t st) {
-    const int bytes = ring_fixed_bytes(VEC, a.channels) + a.slots * a.slot_bytes;
-    const cudaError_t e = cudaFuncSetAttribute(k_norm_ring<T, VEC, BACKWARD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == cudaSuccess) k_norm_ring<T, VEC, BACKWARD><<<l.grid, kRingBlock, bytes, st>>>(a);
-    return e;
-}
-
-template <typename T>
-cudaError_t launch_ring(const RingLaunch& l, const RingArgs& a, cudaStream_t st) {
-    if (l.vec == 8) return l.backward ? launch_ring_of<T, 8, true>(l, a, st) : launch_ring_of<T, 8, false>(l, a, st);
-    return l.backward ? launch_ring_of<T, 4, true>(l, a, st) : launch_ring_of<T, 4, false>(l, a, st);
 }
 
 }  // namespace mgnorm

@@ -4,9 +4,10 @@
 #include <math.h>
 
 #include <algorithm>
+#include <vector>
 
 #include "mg_internal.cuh"
-#include "mg_norm_ring.cuh"
+#include "mg_norm_tiles.cuh"
 
 namespace {
 
@@ -81,7 +82,7 @@ int64_t sample_count(const mg_norm_spec* s) { return s->sample_offsets ? s->n_sa
 
 // ---- how a call is cut ------------------------------------------------------------------
 
-enum { NORM_NOTHING = 0, NORM_ROWS = 1, NORM_TILES = 2, NORM_RING = 3 };
+enum { NORM_NOTHING = 0, NORM_ROWS = 1, NORM_TILES = 2 };
 
 struct NormPlan {
     int mode = NORM_NOTHING, vec = 1;
@@ -91,8 +92,9 @@ struct NormPlan {
     bool general = false;
     RowShape shape{0, 0};
     // workspace: bytes that are cleared first, then where the others start
-    size_t cleared = 0, at_fan_count = 0, at_sample_count = 0, at_ready = 0, at_table = 0, at_tile_parts = 0, at_fan_parts = 0, at_group_parts = 0, at_parts = 0, at_slices = 0, bytes = 0;
+    size_t cleared = 0, at_fan_count = 0, at_sample_count = 0, at_table = 0, at_tile_parts = 0, at_fan_parts = 0, at_group_parts = 0, at_parts = 0, at_slices = 0, bytes = 0;
     int64_t n_parts = 0;   // backward: what k_norm_params adds up
+    std::vector<int32_t> window_tile;   // tiles: where the windows start, and the end of the last
 };
 
 int ceil_log2(int64_t v) { int l = 0; while ((1ll << l) < v) ++l; return l; }
@@ -101,7 +103,7 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 constexpr int64_t kParamSlices = 64;   // of the parts that k_norm_params adds up in two steps
 constexpr int kRowsMaxChannels = 32 * kRowValues;
 constexpr int kRowBlocks = 8, kRowBlocksBackward = 4;   // blocks per SM
-constexpr int kTileBlocks = 2;
+constexpr int kTileBlocks = 4;
 
 // Rows that are samples by themselves, `vec` values to a vector.
 void plan_rows(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p) {
@@ -120,27 +122,8 @@ void plan_rows(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPla
     p->bytes = backward ? p->at_slices + sizeof(float) * 2 * (size_t)s->channels * kParamSlices : 0;
 }
 
-// tiles' and fans' sums of `columns` pairs, and `parts` of the weight's and bias's gradients
-void tile_workspace(const mg_norm_spec* s, bool backward, int64_t tiles, int64_t fans, int64_t columns, int64_t parts, NormPlan* p) {
-    const int64_t n = sample_count(s), pair = 2 * (int64_t)sizeof(float);
-    size_t at = 0;
-    const auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 15) / 16 * 16; return was; };
-    take(4);   // the ticket
-    p->at_fan_count = take(4 * (size_t)fans);
-    p->at_sample_count = take(4 * (size_t)n);
-    p->at_ready = take(4 * (size_t)n);
-    p->cleared = at;
-    p->at_table = take(s->sample_offsets && n > kInlineSamples ? sizeof(int2) * (size_t)(n + 1) : 0);
-    p->at_tile_parts = take((size_t)(tiles * columns * pair));
-    p->at_fan_parts = take((size_t)(fans * columns * pair));
-    p->at_group_parts = take(backward ? (size_t)(n * s->groups * pair) : 0);
-    p->n_parts = backward ? parts : 0;
-    p->at_parts = take((size_t)(p->n_parts * s->channels * pair));
-    p->at_slices = take(p->n_parts ? (size_t)(kParamSlices * s->channels * pair) : 0);
-    p->bytes = at;
-}
-
-constexpr int64_t kRingSlotBytes = 32 << 10, kTileBytes = 64 << 10, kWindowBytes = 16 << 20;
+constexpr int64_t kTileBytes = 192 << 10;
+inline int64_t window_bytes() { const char* e = getenv("MG_NORM_WINDOW_MB"); return (int64_t)(e ? atof(e) : 1e5) * (1 << 20); }
 
 // Samples of several rows.  a: the geometry's part of the arguments.
 void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p, TileArgs* a) {
@@ -153,82 +136,46 @@ void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPl
     a->tx = std::min(ceil_log2(kNormThreads), ceil_log2(vecs));
     a->chunks = (int32_t)((vecs + (1 << a->tx) - 1) >> a->tx);
     const int64_t n_ty = kNormThreads >> a->tx, row_bytes = std::min<int64_t>(s->channels, (int64_t)vec << a->tx) * elem;
-    // tiles of 64 KB, smaller ones where those would leave SMs idle, larger ones where a sample had more than kFan^2
-    const int64_t spread = (used * a->chunks + (int64_t)n_sms * kTileBlocks - 1) / ((int64_t)n_sms * kTileBlocks);
-    int64_t rows = std::min(std::max<int64_t>(kTileBytes / row_bytes, 1), std::max<int64_t>(spread, 1));
-    rows = std::max({round_up(rows, n_ty), round_up((longest + kFan * kFan - 1) / (kFan * kFan), n_ty), (int64_t)16});
+    // tiles of about 192 KB, so many of them that the blocks the SMs hold together take equal turns; smaller ones where there would not be a turn
+    // for each, larger ones where a sample had more than kFan^2
+    const int64_t held = (int64_t)n_sms * kTileBlocks, bytes = used * row_bytes * a->chunks, turns = std::max<int64_t>(1, (bytes + held * kTileBytes / 2) / (held * kTileBytes));
+    const int64_t spread = std::max<int64_t>(1, (used * a->chunks + held * turns - 1) / (held * turns));
+    const int64_t rows = std::max({round_up(spread, n_ty), round_up((longest + kFan * kFan - 1) / (kFan * kFan), n_ty), (int64_t)16});
     a->tile_rows = (int32_t)std::min<int64_t>(rows, 1 << 30);
     a->samples = (int32_t)n; a->equal = equal;
     a->rows_per_sample = s->rows_per_sample;
     a->tiles_per_sample = equal ? (int32_t)((s->rows_per_sample + a->tile_rows - 1) / a->tile_rows) : 0;
-    // windows: whole samples of at least 16 MB
-    const int64_t bytes_per_row = (int64_t)s->channels * elem * (backward ? 2 : 1);
-    const int64_t window = std::max(kWindowBytes, used * bytes_per_row / (kMaxWindows - 8));
-    int64_t tiles = 0, in_window = 0;
-    a->windows = 0;
-    a->window_tile[0] = 0;
-    const auto sample_tiles = [&](int64_t i) { return equal ? (int64_t)a->tiles_per_sample : (s->sample_offsets[i + 1] - s->sample_offsets[i] + a->tile_rows - 1) / a->tile_rows; };
+    // windows: whole samples
+    const int64_t bytes_per_row = (int64_t)s->channels * elem * (backward ? 2 : 1), window = window_bytes();
+    int64_t tiles = 0;
+    p->window_tile.assign(1, 0);
     if (equal) {
         const int64_t sample_bytes = std::max<int64_t>(1, s->rows_per_sample * bytes_per_row), per = std::max<int64_t>(1, (window + sample_bytes - 1) / sample_bytes);
-        for (int64_t i = 0; i < n; i += per) { tiles += std::min(per, n - i) * a->tiles_per_sample; a->window_tile[++a->windows] = (int32_t)tiles; }
+        for (int64_t i = 0; i < n; i += per) { tiles += std::min(per, n - i) * a->tiles_per_sample; p->window_tile.push_back((int32_t)tiles); }
     } else {
+        int64_t in_window = 0;
         for (int64_t i = 0; i < n; ++i) {
-            tiles += sample_tiles(i);
-            in_window += (s->sample_offsets[i + 1] - s->sample_offsets[i]) * bytes_per_row;
-            if (in_window >= window || i + 1 == n) { a->window_tile[++a->windows] = (int32_t)tiles; in_window = 0; }
+            const int64_t len = s->sample_offsets[i + 1] - s->sample_offsets[i];
+            tiles += (len + a->tile_rows - 1) / a->tile_rows;
+            in_window += len * bytes_per_row;
+            if ((in_window >= window || i + 1 == n) && tiles > p->window_tile.back()) { p->window_tile.push_back((int32_t)tiles); in_window = 0; }
         }
     }
-    a->reversed = longest * bytes_per_row > 48 << 20;   // (a sample that L2 does not hold)
-    p->grid = (int)std::max<int64_t>(1, std::min<int64_t>(2 * tiles * a->chunks, (int64_t)n_sms * kTileBlocks));
-    tile_workspace(s, backward, tiles, tiles / kFan + n + 1, s->channels, n, p);
-}
-
-// The same from a ring of slots in shared memory; false where the rows are too wide for it.
-bool plan_ring(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p, RingArgs* a) {
-    const int64_t n = sample_count(s), vecs = s->channels / vec, elem = elem_size(s->dtype), row_bytes = s->channels * elem;
-    if (vecs > kRingThreads || row_bytes % 16) return false;
-    p->mode = NORM_RING; p->vec = vec;
-    const bool equal = !s->sample_offsets, keys = s->dropout && s->dropout->row_keys;
-    const int64_t used = equal ? s->rows : s->sample_offsets[n];
-    int64_t longest = equal ? s->rows_per_sample : 0;
-    if (!equal) for (int64_t i = 0; i < n; ++i) longest = std::max(longest, s->sample_offsets[i + 1] - s->sample_offsets[i]);
-    a->tx = ceil_log2(vecs);
-    a->chunks = 1;
-    const int64_t n_ty = kRingThreads >> a->tx, per_row = row_bytes * (backward ? 2 : 1) + (keys ? 8 : 0);
-    // slots of up to 32 KB, rows in multiples of what the block's threads take at once
-    const int64_t room = kRingSharedBytes - ring_fixed_bytes(vec, s->channels);
-    int64_t sub = std::min(kRingSlotBytes, room / 4 - 256) / per_row;
-    if (sub < 1) return false;
-    if (sub > n_ty) sub = sub / n_ty * n_ty;
-    // tiles of a slot; smaller ones where those would leave SMs idle, down to 8 KB; of several slots where a sample had more than kFan^2
-    const int64_t most = (int64_t)kFan * kFan, least = std::max<int64_t>(1, (8 << 10) / per_row), spread = (used + n_sms - 1) / n_sms;
-    int64_t rows = std::min(sub, std::max(least, spread));
-    a->hold = longest <= most * rows;
-    if (!a->hold) {
-        const int64_t want = (longest + most - 1) / most;
-        rows = want <= sub ? want : round_up(want, sub);
-        a->hold = want <= sub;
-    }
-    a->sub_rows = (int32_t)std::min(sub, rows);
-    a->tile_rows = (int32_t)rows;
-    const int64_t sub_bytes = round_up(a->sub_rows * row_bytes, 16);
-    a->d_y_at = (int32_t)(backward ? sub_bytes : 0);
-    a->keys_at = (int32_t)(sub_bytes * (backward ? 2 : 1));
-    a->slot_bytes = (int32_t)round_up(a->keys_at + (keys ? 8 * a->sub_rows : 0), 128);
-    a->slots = (int32_t)std::min<int64_t>(kRingSlots, room / a->slot_bytes);
-    a->samples = (int32_t)n; a->equal = equal;
-    a->rows_per_sample = s->rows_per_sample;
-    a->tiles_per_sample = equal ? (int32_t)((s->rows_per_sample + rows - 1) / rows) : 0;
-    int64_t tiles = equal ? n * a->tiles_per_sample : 0;
-    if (!equal) for (int64_t i = 0; i < n; ++i) tiles += (s->sample_offsets[i + 1] - s->sample_offsets[i] + rows - 1) / rows;
-    a->total = (int32_t)tiles;
-    const int64_t longest_tiles = (longest + rows - 1) / rows;
-    a->fan = 4;   // two steps of about as many sets each: they are brought together one behind the other
-    while (a->fan < kFan && (int64_t)a->fan * a->fan < longest_tiles) ++a->fan;
-    a->patience = longest_tiles <= (int64_t)n_sms * a->slots * 7 / 8 ? 200 : 0;
-    p->grid = (int)std::max<int64_t>(1, std::min<int64_t>(tiles, n_sms));
-    tile_workspace(s, backward, tiles, tiles / a->fan + n + 1, s->groups, tiles, p);
-    return true;
+    a->reversed = 1;
+    const int64_t fans = tiles / kFan + n + 1, pair = 2 * (int64_t)sizeof(float) * s->channels;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 15) / 16 * 16; return was; };
+    p->at_fan_count = take(4 * (size_t)fans);
+    p->at_sample_count = take(4 * (size_t)n);
+    p->cleared = at;
+    p->at_table = take(!equal && n > kInlineSamples ? sizeof(int2) * (size_t)(n + 1) : 0);
+    p->at_tile_parts = take((size_t)(tiles * pair));
+    p->at_fan_parts = take((size_t)(fans * pair));
+    p->at_group_parts = take(backward ? 2 * sizeof(float) * (size_t)(n * s->groups) : 0);
+    p->n_parts = backward ? n : 0;
+    p->at_parts = take((size_t)(p->n_parts * pair));
+    p->at_slices = take(p->n_parts ? (size_t)(kParamSlices * pair) : 0);
+    p->bytes = at;
 }
 
 // the vector widths that there are kernels for: 32, 16, 8 (16-bit types: 16, 8, 4) and one element
@@ -254,8 +201,6 @@ size_t norm_workspace(const mg_norm_spec* s, int n_sms, bool backward) {
         if (mode == NORM_ROWS) plan_rows(s, n_sms, backward, *v, &p);
         else plan_tiles(s, n_sms, backward, *v, &p, &a);
         most = std::max(most, p.bytes);
-        RingArgs r;
-        if (mode == NORM_TILES && *v >= 4 && plan_ring(s, n_sms, backward, *v, &p, &r)) most = std::max(most, p.bytes);
     }
     return most;
 }
@@ -287,19 +232,6 @@ int rows_vec_width(const Matrix* m, int n, const mg_norm_spec* s) {
     const int32_t each = s->channels / s->groups;
     const int v = vec_width(m, n, s->dtype, s->rows, each), w = each / v;
     return (w & (w - 1)) == 0 ? v : vec_width(m, n, s->dtype, s->rows, s->channels);
-}
-
-// ... for the ring: its copies want 16-byte pieces, its stores whole vectors; 0 where they are neither
-int ring_vec_width(const Matrix* m, int n, const mg_norm_spec* s) {
-    const int64_t e = elem_size(s->dtype);
-    const int32_t each = s->channels / s->groups;
-    for (int i = 0; i + 1 < n; ++i)
-        if (reinterpret_cast<uintptr_t>(m[i].p) % 16 || (s->rows > 1 && m[i].stride * e % 16)) return 0;
-    if (s->channels * e % 16) return 0;
-    const Matrix& out = m[n - 1];
-    for (const int v : {8, 4})
-        if (each % v == 0 && reinterpret_cast<uintptr_t>(out.p) % (uintptr_t)(v * e) == 0 && (s->rows <= 1 || out.stride % v == 0)) return v;
-    return 0;
 }
 
 // every check of an entry point's arguments but the workspace's; `d`: the dropout as the kernels take it

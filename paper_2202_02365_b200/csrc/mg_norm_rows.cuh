@@ -86,15 +86,19 @@ __device__ __forceinline__ void group_sum(float (&s)[NV], const RowShape& r) {
         float t = s[0];
 #pragma unroll
         for (int i = 1; i < NV; ++i) t += s[i];
-        for (int o = 1; o < 1 << r.lanes; o <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+#pragma unroll
+        for (int o = 0; o < 5; ++o) if (o < r.lanes) t += __shfl_xor_sync(0xFFFFFFFFu, t, 1 << o);
 #pragma unroll
         for (int i = 0; i < NV; ++i) s[i] = t;
         return;
     }
-    const int width = 1 << min(r.gshift, r.lanes);
-    for (int o = 1; o < width; o <<= 1) {
+    const int steps = min(r.gshift, r.lanes);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], o);
+    for (int o = 0; o < 5; ++o) {
+        if (o < steps) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) s[i] += __shfl_xor_sync(0xFFFFFFFFu, s[i], 1 << o);
+        }
     }
     if (NV > 1 && r.gshift > 5) {   // (groups wider than a warp are of whole warps)
 #pragma unroll
@@ -111,13 +115,14 @@ __device__ __forceinline__ void group_sum(float (&s)[NV], const RowShape& r) {
 }
 
 __device__ __forceinline__ float row_sum(float t, int lanes) {
-    for (int o = 1; o < 1 << lanes; o <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+#pragma unroll
+    for (int o = 0; o < 5; ++o) if (o < lanes) t += __shfl_xor_sync(0xFFFFFFFFu, t, 1 << o);
     return t;
 }
 
 // Weight and bias of a lane's channels: held in registers where they are few, else read from shared memory again for every row.
-template <int VEC, int NV> struct Params {
-    static constexpr bool kHeld = VEC * NV <= 8;
+template <int VEC, int NV, bool BACKWARD> struct Params {
+    static constexpr bool kHeld = VEC * NV <= (BACKWARD ? 4 : 8);
     float w[kHeld ? NV : 1][VEC], b[kHeld ? NV : 1][VEC];
     const float* shared;
     int32_t channels;
@@ -171,7 +176,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape
     const float inv = 1.f / (float)a.each;
     const T* x = static_cast<const T*>(a.x);
     T* y = static_cast<T*>(a.out);
-    const Params<VEC, NV> par(a, params, sub, vecs);
+    const Params<VEC, NV, false> par(a, params, sub, vecs);
     const int64_t step = (int64_t)gridDim.x * kNormWarps * per_warp;
     constexpr bool kAhead = VEC * NV <= 16;   // the next row is on its way while this one is worked on
     Raw<T, VEC> raw[NV], next[kAhead ? NV : 1];
@@ -270,7 +275,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape
 // Gradient: dz = dropout(dy) act', then dx = rstd (dz w - mean(dz w) - hat mean(dz w hat)); every lane adds up dz hat and dz of its channels over
 // its rows, every block its lanes', and k_norm_params the blocks'.
 template <typename T, int VEC, int NV, bool GENERAL>
-__global__ void __launch_bounds__(kNormThreads) k_norm_rows_backward(NormArgs a, RowShape r) {
+__global__ void __launch_bounds__(kNormThreads, VEC * NV <= 8 ? 3 : 1) k_norm_rows_backward(NormArgs a, RowShape r) {
     extern __shared__ __align__(16) float params[];   // [2][channels], where they are not held; then the block's sums [2][channels]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane & ((1 << r.lanes) - 1), per_warp = 32 >> r.lanes;
     const int32_t vecs = a.channels / VEC;
@@ -278,16 +283,15 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows_backward(NormArgs a,
     const T* x = static_cast<const T*>(a.x);
     const T* d_y = static_cast<const T*>(a.d_y);
     T* d_x = static_cast<T*>(a.out);
-    const Params<VEC, NV> par(a, params, sub, vecs);
-    float* sums = params + (Params<VEC, NV>::kHeld ? 0 : 2 * a.channels);
+    const Params<VEC, NV, true> par(a, params, sub, vecs);
+    float* sums = params + (Params<VEC, NV, true>::kHeld ? 0 : 2 * a.channels);
     float dw[NV][VEC], db[NV][VEC];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) dw[i][e] = db[i][e] = 0.f;
     const int64_t step = (int64_t)gridDim.x * kNormWarps * per_warp;
-    constexpr bool kAhead = false;   // the next row is on its way while this one is worked on
-    Raw<T, VEC> rx[NV], rd[NV], next_x[kAhead ? NV : 1], next_d[kAhead ? NV : 1];
+    Raw<T, VEC> rx[NV], rd[NV];
     int64_t row = (blockIdx.x * (int64_t)kNormWarps + warp) * per_warp + (lane >> r.lanes);
     const auto fetch = [&](Raw<T, VEC>* to_x, Raw<T, VEC>* to_d, int64_t from) {
 #pragma unroll
@@ -299,15 +303,10 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows_backward(NormArgs a,
             }
         }
     };
-    if (kAhead) fetch(next_x, next_d, row);
     for (; row - (lane >> r.lanes) < a.rows; row += step) {
         const bool here = row < a.rows;
         float h[NV][VEC], g[NV][VEC], rstd[NV];
-        if constexpr (kAhead) {
-#pragma unroll
-            for (int i = 0; i < NV; ++i) { rx[i] = next_x[i]; rd[i] = next_d[i]; }
-            fetch(next_x, next_d, row + step);
-        } else fetch(rx, rd, row);
+        fetch(rx, rd, row);
         const uint64_t key = here && a.drop.on ? drop_key(a.drop, row) : 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {

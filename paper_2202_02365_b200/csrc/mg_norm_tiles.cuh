@@ -1,6 +1,6 @@
-// Group norm of samples of many rows: tiles of rows are dealt out to persistent blocks, first for the sums of a sample's channels, then, once
-// all of the sample's are there, for the result.  Both come from one queue, so one launch does it, and a sample that fits L2 is read from
-// memory once.
+// Group norm of samples of several rows, in two passes: tiles of rows are summed up by channel, the last block of a sample's brings its sums
+// together, and a launch later the tiles' results are computed.  No block waits for another.  A launch does the sums of one window of samples and
+// the results of the window before, so that both passes keep the memory busy together and the second finds its rows in L2.
 #pragma once
 
 #include "mg_norm_rows.cuh"
@@ -9,9 +9,6 @@ namespace mgnorm {
 
 constexpr int kFan = 32;             // tiles whose sums one block brings together; then as many of those
 constexpr int kInlineSamples = 64;   // samples whose place is handed over in the kernel's parameters
-constexpr int kMaxWindows = 72;
-constexpr int kTilePolls = 1 << 22;  // (a poll is an L2 round trip: far beyond any legitimate wait)
-constexpr uint32_t kRoleNorm = 30u;  // what a wait that ran out leaves in the context's status word
 
 struct TileArgs : NormArgs {
     // samples: equal ones, or a table of (first row, first tile), one entry more than samples
@@ -22,36 +19,25 @@ struct TileArgs : NormArgs {
     int2 inl[kInlineSamples + 1];
     // tiles: tile_rows rows, each in `chunks` runs of (256 or fewer) vectors
     int32_t tile_rows = 0, chunks = 0, tx = 0;   // tx: log2 of the threads along a row
-    // queue: the windows' first tiles; position p of the queue: sums of window 0, sums of window 1, results of window 0, sums of window 2, ...
-    int32_t windows = 0, reversed = 0;
-    int32_t window_tile[kMaxWindows + 1];
+    // this launch: sums of tiles from sums_tile on in the first sums_blocks blocks, results of those from result_tile on in the others
+    int32_t sums_tile = 0, sums_blocks = 0, result_tile = 0, result_tiles = 0, reversed = 0;
     // workspace
-    uint32_t* ticket = nullptr;      // cleared: the queue's next position ...
-    uint32_t* fan_count = nullptr;   // ... sums that have arrived, by kFan tiles of a sample ...
-    uint32_t* sample_count = nullptr;   // ... and by sample ...
-    uint32_t* ready = nullptr;       // ... 1: the sample's statistics (backward: group sums) are there
+    uint32_t* fan_count = nullptr;   // cleared: sums that have arrived, by kFan tiles of a sample ...
+    uint32_t* sample_count = nullptr;   // ... and by sample
     float* tile_parts = nullptr;     // [tiles][2][channels]
     float* fan_parts = nullptr;      // [tiles / kFan + samples][2][channels]
     float* group_parts = nullptr;    // backward: mean of dz w, mean of dz w hat: [samples][2][groups]
-    uint32_t* status = nullptr;
-    int32_t polls = kTilePolls;
 };
 
 struct Tile {
-    int32_t kind;          // 0 sums, 1 result, 2 nothing left
-    int32_t tile, chunk;   // its number among all
-    int32_t sample, first, tiles;   // the sample's first tile and how many it has
+    int32_t tile, sample, first, tiles;   // its number among all; the sample's first tile and how many it has
     int64_t row0, row1, sample_rows;
 };
 
 __device__ __forceinline__ int2 sample_entry(const TileArgs& a, int32_t s) { return a.table ? a.table[s] : a.inl[s]; }
 
-__device__ __forceinline__ int64_t queue_start(const TileArgs& a, int i) {   // of the sums of window i
-    return (int64_t)(a.window_tile[i] + (i ? a.window_tile[i - 1] : 0)) * a.chunks;
-}
-
 // the sample and the rows of a tile
-__device__ inline void locate_tile(const TileArgs& a, int32_t tile, Tile* t) {
+__device__ __forceinline__ void locate_tile(const TileArgs& a, int32_t tile, Tile* t) {
     t->tile = tile;
     int64_t s0, s1;
     if (a.equal) {
@@ -72,33 +58,6 @@ __device__ inline void locate_tile(const TileArgs& a, int32_t tile, Tile* t) {
     t->row0 = s0 + (int64_t)(tile - t->first) * a.tile_rows;
     t->row1 = min(s1, t->row0 + a.tile_rows);
     t->sample_rows = s1 - s0;
-}
-
-__device__ inline void next_tile(const TileArgs& a, Tile* t) {
-    const int64_t total = (int64_t)a.window_tile[a.windows] * a.chunks, p = atomicAdd(a.ticket, 1u);
-    if (p >= 2 * total) { t->kind = 2; return; }
-    int lo = 0, hi = a.windows;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (queue_start(a, mid) <= p) lo = mid; else hi = mid;
-    }
-    int64_t off = p - queue_start(a, lo);
-    int w = lo;
-    t->kind = 0;
-    const int64_t sums = (int64_t)(a.window_tile[lo + 1] - a.window_tile[lo]) * a.chunks;
-    if (off >= sums) {   // the results of the window before, and behind the last window's sums and those its own too
-        off -= sums;
-        t->kind = 1;
-        w = lo - 1;
-        const int64_t before = lo ? (int64_t)(a.window_tile[lo] - a.window_tile[lo - 1]) * a.chunks : 0;
-        if (lo == 0 || off >= before) { off -= before; w = lo; }
-    }
-    const int32_t n = a.window_tile[w + 1] - a.window_tile[w];
-    int32_t tile = (int32_t)(off / a.chunks);
-    t->chunk = (int32_t)(off - (int64_t)tile * a.chunks);
-    if (a.reversed && t->kind == 1) tile = n - 1 - tile;   // (what was read last is still in L2)
-    tile += a.window_tile[w];
-    locate_tile(a, tile, t);
 }
 
 // Mean and sum of squares about it of two sets (Chan, Golub and LeVeque 1979)
@@ -129,51 +88,60 @@ __device__ __forceinline__ void merge(Pair<VEC>& a, float nb, const float (&u)[V
     }
 }
 
-// Sums of a tile: every thread has one vector of the channels and every TY-th row, K rows in flight; then the block's threads are brought together.
+// Sums of a tile: every thread has one vector of the channels and every n_ty-th row, K rows in flight; then the block's threads are brought together.
 template <typename T, int VEC, bool BACKWARD, int K>
 __device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int32_t c, bool in, int ty, int n_ty, float mean, float rstd, const float (&w)[VEC],
                                           const float (&b)[VEC], Pair<VEC>& p) {
-    const T* x = static_cast<const T*>(a.x) + c;
-    const T* d_y = static_cast<const T*>(a.d_y) + c;
     p.n = 0.f;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) p.u[e] = p.v[e] = 0.f;
     if (!in) return;
-    for (int64_t r = t.row0 + ty; r < t.row1; r += (int64_t)K * n_ty) {
+    const int64_t x_step = (int64_t)n_ty * a.x_stride, d_step = (int64_t)n_ty * a.d_y_stride;
+    const T* x = static_cast<const T*>(a.x) + (t.row0 + ty) * a.x_stride + c;
+    const T* d_y = static_cast<const T*>(a.d_y) + (BACKWARD ? (t.row0 + ty) * a.d_y_stride + c : 0);
+    const int32_t rows = (int32_t)(t.row1 - t.row0);
+    for (int32_t r = ty; r < rows; r += K * n_ty) {
         Raw<T, VEC> raw[K], rd[BACKWARD ? K : 1];
 #pragma unroll
         for (int k = 0; k < K; ++k)
-            if (r + k * n_ty < t.row1) {
-                raw[k].load(x + (r + k * n_ty) * a.x_stride);
-                if (BACKWARD) rd[k].load(d_y + (r + k * n_ty) * a.d_y_stride);
+            if (r + k * n_ty < rows) {
+                raw[k].load(x + k * x_step);
+                if (BACKWARD) rd[k].load(d_y + k * d_step);
             }
         if constexpr (BACKWARD) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
-                const int64_t row = r + k * n_ty;
-                if (row >= t.row1) break;
+                if (r + k * n_ty >= rows) break;
                 float h[VEC], d[VEC];
-                grad_vector<T, VEC>(a, raw[k], rd[k], a.drop.on ? drop_key(a.drop, row) : 0, c, mean, rstd, w, b, h, d);
+                grad_vector<T, VEC>(a, raw[k], rd[k], a.drop.on ? drop_key(a.drop, t.row0 + r + k * n_ty) : 0, c, mean, rstd, w, b, h, d);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) { p.u[e] = fmaf(d[e], h[e], p.u[e]); p.v[e] += d[e]; }
             }
+            d_y += K * d_step;
         } else {
-            const int64_t left = (t.row1 - r + n_ty - 1) / n_ty;
-            const int n = left < K ? (int)left : K;
-            const float inv = 1.f / (float)n;
             float u[VEC], v[VEC];
+            if (r + (K - 1) * n_ty < rows) {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                float s = 0.f, q = 0.f;
+                for (int e = 0; e < VEC; ++e) {
+                    u[e] = raw[0].get(e); v[e] = 0.f;
 #pragma unroll
-                for (int k = 0; k < K; ++k) if (k < n) s += raw[k].get(e);
-                s *= inv;
+                    for (int k = 1; k < K; ++k) u[e] += raw[k].get(e);
+                    u[e] *= 1.f / K;
 #pragma unroll
-                for (int k = 0; k < K; ++k) if (k < n) { const float d = raw[k].get(e) - s; q = fmaf(d, d, q); }
-                u[e] = s; v[e] = q;
+                    for (int k = 0; k < K; ++k) { const float d = raw[k].get(e) - u[e]; v[e] = fmaf(d, d, v[e]); }
+                }
+                merge<VEC, false>(p, (float)K, u, v);
+            } else {
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    if (r + k * n_ty >= rows) break;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) { u[e] = raw[k].get(e); v[e] = 0.f; }
+                    merge<VEC, false>(p, 1.f, u, v);
+                }
             }
-            merge<VEC, false>(p, (float)n, u, v);
         }
+        x += K * x_step;
     }
 }
 
@@ -315,12 +283,14 @@ template <bool BACKWARD>
 __device__ __forceinline__ void arrive(const TileArgs& a, const Tile& t, int32_t* sh_last) {
     const int32_t in_sample = t.tile - t.first, fan = in_sample / kFan, fans = (t.tiles + kFan - 1) / kFan, fan_tiles = min(kFan, t.tiles - fan * kFan);
     const int64_t fan_id = t.first / kFan + t.sample + fan;   // (blocks of kFan tiles of all samples before lie below)
-    __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) *sh_last = atomicAdd(a.fan_count + fan_id, 1u) + 1u == (uint32_t)(fan_tiles * a.chunks);
+    if (threadIdx.x == 0) {   // (what the block's threads wrote before they met is announced with it)
+        __threadfence();
+        *sh_last = atomicAdd(a.fan_count + fan_id, 1u) + 1u == (uint32_t)(fan_tiles * a.chunks);
+        __threadfence();
+    }
     __syncthreads();
     if (!*sh_last) return;
-    __threadfence();
     const int64_t step = 2 * (int64_t)a.channels;
     float* fan_part = a.fan_parts + fan_id * step;
     const auto tile_rows = [&](int32_t i) { return (float)min((int64_t)a.tile_rows, t.sample_rows - ((int64_t)fan * kFan + i) * a.tile_rows); };
@@ -328,20 +298,18 @@ __device__ __forceinline__ void arrive(const TileArgs& a, const Tile& t, int32_t
     merge_parts<BACKWARD, kNormThreads, 1, 8>(a, a.tile_parts + ((int64_t)t.first + fan * kFan) * step, fan_tiles, tile_rows, fans == 1 ? whole : fan_part, threadIdx.x, nullptr, 0);
     __syncthreads();
     if (fans > 1) {
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) *sh_last = atomicAdd(a.sample_count + t.sample, 1u) + 1u == (uint32_t)fans;
+        if (threadIdx.x == 0) {
+            __threadfence();
+            *sh_last = atomicAdd(a.sample_count + t.sample, 1u) + 1u == (uint32_t)fans;
+            __threadfence();
+        }
         __syncthreads();
         if (!*sh_last) return;
-        __threadfence();
         const auto fan_rows = [&](int32_t i) { return (float)min((int64_t)kFan * a.tile_rows, t.sample_rows - (int64_t)i * kFan * a.tile_rows); };
         merge_parts<BACKWARD, kNormThreads, 1, 8>(a, a.fan_parts + (t.first / kFan + t.sample) * step, fans, fan_rows, whole, threadIdx.x, nullptr, 0);
         __syncthreads();
     }
     finish_sample<BACKWARD, kNormThreads>(a, t.sample, (float)t.sample_rows, whole);
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) *reinterpret_cast<volatile uint32_t*>(a.ready + t.sample) = 1u;
 }
 
 template <int VEC>
@@ -358,107 +326,95 @@ __device__ __forceinline__ void load_params(const float* p, int32_t c, float wit
     for (int e = 0; e < VEC; ++e) o[e] = p ? p[c + e] : without;
 }
 
-// A block that waits for a sample's sums waits for positions of the queue before its own, which running blocks have; one that is taken ahead of
-// its time is held by a block whose present one lies before it.  So every wait ends; it is bounded all the same.
 template <typename T, int VEC, bool BACKWARD, int K, int U, int MINB>
 __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_tiles(const __grid_constant__ TileArgs a) {
     __shared__ __align__(16) float smem[2 * kNormThreads * VEC + kNormWarps];
-    __shared__ Tile sh_tile[2];
     __shared__ int32_t sh_flag;
     const int tx = threadIdx.x & ((1 << a.tx) - 1), ty = threadIdx.x >> a.tx, n_ty = kNormThreads >> a.tx;
-    if (!a.equal) {   // samples without rows have no tiles
-        for (int32_t s = blockIdx.x; s < a.samples; s += gridDim.x) {
-            if (sample_entry(a, s).x != sample_entry(a, s + 1).x) continue;
-            if (!BACKWARD) for (int32_t g = threadIdx.x; g < a.groups; g += kNormThreads) { a.mean[(int64_t)s * a.groups + g] = 0.f; a.rstd[(int64_t)s * a.groups + g] = 0.f; }
-            else for (int32_t c = threadIdx.x; c < 2 * a.channels; c += kNormThreads) a.parts[2 * (int64_t)s * a.channels + c] = 0.f;
-        }
+    const bool sums = (int32_t)blockIdx.x < a.sums_blocks;
+    const int32_t item = (int32_t)blockIdx.x - (sums ? 0 : a.sums_blocks), tile = item / a.chunks, chunk = item - tile * a.chunks;
+    Tile t;
+    locate_tile(a, sums ? a.sums_tile + tile : a.result_tile + (a.reversed ? a.result_tiles - 1 - tile : tile), &t);
+    const int32_t chunk0 = chunk * (VEC << a.tx), c = chunk0 + tx * VEC;
+    const bool in = c < a.channels;
+    const int64_t stat = (int64_t)t.sample * a.groups + (in ? c / a.each : 0);
+    float w[VEC], b[VEC], mean = 0.f, rstd = 0.f;
+    if (BACKWARD || !sums) {
+        load_params<VEC>(in ? a.weight : nullptr, c, 1.f, w);
+        load_params<VEC>(in ? a.bias : nullptr, c, 0.f, b);
+        mean = a.mean[stat]; rstd = a.rstd[stat];
     }
-    if (threadIdx.x == 0) next_tile(a, &sh_tile[0]);
-    __syncthreads();
-    for (int at = 0;; at ^= 1) {
-        const Tile t = sh_tile[at];
-        if (t.kind == 2) break;
-        if (threadIdx.x == 0) next_tile(a, &sh_tile[at ^ 1]);
-        const int32_t chunk0 = t.chunk * (VEC << a.tx), c = chunk0 + tx * VEC;
-        const bool in = c < a.channels;
-        float w[VEC], b[VEC], mean = 0.f, rstd = 0.f;
-        if (BACKWARD || t.kind == 1) {
-            load_params<VEC>(in ? a.weight : nullptr, c, 1.f, w);
-            load_params<VEC>(in ? a.bias : nullptr, c, 0.f, b);
-        }
-        const int64_t stat = (int64_t)t.sample * a.groups + (in ? c / a.each : 0);
-        if (BACKWARD) { mean = a.mean[stat]; rstd = a.rstd[stat]; }
-        if (t.kind == 0) {
-            Pair<VEC> p;
-            tile_sums<T, VEC, BACKWARD, K>(a, t, c, in, ty, n_ty, mean, rstd, w, b, p);
-            block_pairs<VEC, BACKWARD>(a, p, smem, tx, chunk0, a.tile_parts + 2 * (int64_t)t.tile * a.channels);
-            arrive<BACKWARD>(a, t, &sh_flag);
-        } else {
-            if (threadIdx.x == 0) {
-                int polls = 0;
-                const volatile uint32_t* ready = a.ready + t.sample;
-                while (!*ready && ++polls < a.polls) {}
-                sh_flag = polls < a.polls;
-                if (!sh_flag) *reinterpret_cast<volatile uint32_t*>(a.status) = kRoleNorm;
-                __threadfence();
+    if (sums) {
+        Pair<VEC> p;
+        tile_sums<T, VEC, BACKWARD, K>(a, t, c, in, ty, n_ty, mean, rstd, w, b, p);
+        block_pairs<VEC, BACKWARD>(a, p, smem, tx, chunk0, a.tile_parts + 2 * (int64_t)t.tile * a.channels);
+        arrive<BACKWARD>(a, t, &sh_flag);
+        return;
+    }
+    if (!in) return;
+    float s1 = 0.f, s2 = 0.f;
+    if (BACKWARD) {
+        const int64_t at_group = (int64_t)t.sample * 2 * a.groups + c / a.each;
+        s1 = a.group_parts[at_group]; s2 = a.group_parts[at_group + a.groups];
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[e] *= rstd;
+    }
+    const int64_t x_step = (int64_t)n_ty * a.x_stride, d_step = (int64_t)n_ty * a.d_y_stride, out_step = (int64_t)n_ty * a.out_stride;
+    const T* x = static_cast<const T*>(a.x) + (t.row0 + ty) * a.x_stride + c;
+    const T* d_y = static_cast<const T*>(a.d_y) + (BACKWARD ? (t.row0 + ty) * a.d_y_stride + c : 0);
+    T* out = static_cast<T*>(a.out) + (t.row0 + ty) * a.out_stride + c;
+    const int32_t rows = (int32_t)(t.row1 - t.row0);
+    for (int32_t r = ty; r < rows; r += U * n_ty) {
+        Raw<T, VEC> raw[U], rd[BACKWARD ? U : 1];
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (r + k * n_ty < rows) {
+                raw[k].load(x + k * x_step);
+                if (BACKWARD) rd[k].load(d_y + k * d_step);
             }
-            __syncthreads();
-            if (in && sh_flag) {
-                const T* x = static_cast<const T*>(a.x) + c;
-                const T* d_y = static_cast<const T*>(a.d_y) + c;
-                T* out = static_cast<T*>(a.out) + c;
-                float s1 = 0.f, s2 = 0.f;
-                if (BACKWARD) {
-                    const int64_t at_group = (int64_t)t.sample * 2 * a.groups + c / a.each;
-                    s1 = __ldcg(a.group_parts + at_group); s2 = __ldcg(a.group_parts + at_group + a.groups);
-                } else {
-                    mean = __ldcg(a.mean + stat); rstd = __ldcg(a.rstd + stat);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) w[e] *= rstd;
-                }
-                for (int64_t r = t.row0 + ty; r < t.row1; r += (int64_t)U * n_ty) {
-                    Raw<T, VEC> raw[U], rd[BACKWARD ? U : 1];
+        for (int k = 0; k < U; ++k) {
+            if (r + k * n_ty >= rows) break;
+            const uint64_t key = a.drop.on ? drop_key(a.drop, t.row0 + r + k * n_ty) : 0;
+            float f[VEC];
+            if constexpr (BACKWARD) {
+                float h[VEC];
+                grad_vector<T, VEC>(a, raw[k], rd[k], key, c, mean, rstd, w, b, h, f);
 #pragma unroll
-                    for (int k = 0; k < U; ++k)
-                        if (r + k * n_ty < t.row1) {
-                            raw[k].load(x + (r + k * n_ty) * a.x_stride);
-                            if (BACKWARD) rd[k].load(d_y + (r + k * n_ty) * a.d_y_stride);
-                        }
+                for (int e = 0; e < VEC; ++e) f[e] = rstd * fmaf(-h[e], s2, fmaf(f[e], w[e], -s1));
+            } else {
 #pragma unroll
-                    for (int k = 0; k < U; ++k) {
-                        const int64_t row = r + k * n_ty;
-                        if (row >= t.row1) break;
-                        float f[VEC];
-                        const uint64_t key = a.drop.on ? drop_key(a.drop, row) : 0;
-                        if constexpr (BACKWARD) {
-                            float h[VEC];
-                            grad_vector<T, VEC>(a, raw[k], rd[k], key, c, mean, rstd, w, b, h, f);
+                for (int e = 0; e < VEC; ++e) f[e] = fmaf(raw[k].get(e) - mean, w[e], b[e]);
+                act_values<VEC>(a.act, f);
+                if (a.drop.on) {
+                    Keep<VEC> keep;
+                    keep.draw(a.drop, key, (uint32_t)c);
 #pragma unroll
-                            for (int e = 0; e < VEC; ++e) f[e] = rstd * fmaf(-h[e], s2, fmaf(f[e], w[e], -s1));
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < VEC; ++e) f[e] = fmaf(raw[k].get(e) - mean, w[e], b[e]);
-                            act_values<VEC>(a.act, f);
-                            if (a.drop.on) {
-                                Keep<VEC> keep;
-                                keep.draw(a.drop, key, (uint32_t)c);
-#pragma unroll
-                                for (int e = 0; e < VEC; ++e) f[e] = keep(a.drop, e) ? f[e] * a.drop.factor : 0.f;
-                            }
-                        }
-                        raw[k].put(f);
-                        raw[k].store(out + row * a.out_stride);
-                    }
+                    for (int e = 0; e < VEC; ++e) f[e] = keep(a.drop, e) ? f[e] * a.drop.factor : 0.f;
                 }
             }
+            raw[k].put(f);
+            raw[k].store(out + k * out_step);
         }
-        __syncthreads();
+        x += U * x_step; out += U * out_step;
+        if (BACKWARD) d_y += U * d_step;
+    }
+}
+
+// Samples without rows have no tiles: their statistics (backward: their parts of the weight's and bias's gradients) are zero.
+template <typename = void>
+__global__ void k_norm_empty(const __grid_constant__ TileArgs a, int backward) {
+    for (int32_t s = blockIdx.x; s < a.samples; s += gridDim.x) {
+        if (sample_entry(a, s).x != sample_entry(a, s + 1).x) continue;
+        if (!backward) for (int32_t g = threadIdx.x; g < a.groups; g += blockDim.x) { a.mean[(int64_t)s * a.groups + g] = 0.f; a.rstd[(int64_t)s * a.groups + g] = 0.f; }
+        else for (int32_t c = threadIdx.x; c < 2 * a.channels; c += blockDim.x) a.parts[2 * (int64_t)s * a.channels + c] = 0.f;
     }
 }
 
 // what a translation unit of its own per row type launches
 struct RowLaunch { int vec, nv; bool general, backward; int grid; RowShape shape; };
-struct TileLaunch { int vec; bool backward; int grid; };
+struct TileLaunch { int vec; bool backward; int64_t grid; };
 template <typename T> void launch_dropout(int vec, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t rows, int32_t channels, const DropArgs& d, int grid, cudaStream_t st);
 template <typename T> void launch_rows(const RowLaunch& l, const NormArgs& a, cudaStream_t st);
 template <typename T> void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st);

@@ -615,46 +615,32 @@ int main() {
         for (const int* v = vec_widths(s.dtype); *v; ++v) {
             if (s.channels % *v) continue;
             NormPlan p;
-            RingArgs a;
+            TileArgs a;
             if (norm_mode(&s) == NORM_ROWS) {
                 plan_rows(&s, 148, backward, *v, &p);
                 NEED(p.bytes <= have && p.nv * *v <= kRowValues && p.nv * 32 * *v >= s.channels && p.grid >= 1);
+                NEED(!backward || 8ull * s.channels * (p.n_parts + kParamSlices) <= p.bytes);
                 continue;
             }
-            for (int ring = 0; ring < 2; ++ring) {
-                if (ring && (*v < 4 || s.channels / s.groups % *v || !plan_ring(&s, 148, backward, *v, &p, &a))) continue;
-                if (!ring) plan_tiles(&s, 148, backward, *v, &p, &a);
-                NEED(p.bytes <= have);
-                const int fan = ring ? a.fan : kFan;
-                const int64_t pair = 2 * 4 * (int64_t)(ring ? s.groups : s.channels);
-                int64_t tile = 0, fans_end = 0;
-                for (int64_t q = 0; q < n; ++q) {
-                    const int64_t len = s.sample_offsets ? s.sample_offsets[q + 1] - s.sample_offsets[q] : s.rows_per_sample;
-                    const int64_t tiles = (len + a.tile_rows - 1) / a.tile_rows, first = tile / fan + q, fans = (tiles + fan - 1) / fan;
-                    NEED(first >= fans_end && tiles <= kFan * kFan && fans <= kFan);
-                    fans_end = first + std::max<int64_t>(fans, 1);
-                    tile += tiles;
-                    NEED(!a.equal || tiles == a.tiles_per_sample);
-                }
-                NEED(p.at_fan_count + 4 * fans_end <= p.at_sample_count && p.at_fan_parts + fans_end * pair <= p.at_group_parts);
-                NEED(p.at_sample_count + 4 * n <= p.at_ready && p.at_ready + 4 * n <= p.cleared && p.at_tile_parts + tile * pair <= p.at_fan_parts);
-                NEED(p.n_parts == (backward ? ring ? tile : n : 0) && p.at_parts + p.n_parts * 8 * s.channels <= p.at_slices);
-                NEED(!backward || p.at_slices + kParamSlices * 8 * s.channels <= p.bytes);
-                NEED(tile * a.chunks < 1ll << 30 && (int64_t)a.tile_rows > 0);
-                if (ring) {
-                    NEED(tile == a.total && kFan * kFan < kRingFifo && a.fan <= kFan && s.channels <= (*v << a.tx) && (1 << a.tx) <= kRingThreads);
-                    const int64_t row = (int64_t)s.channels * elem_size(s.dtype);
-                    NEED(a.sub_rows >= 1 && a.keys_at + (s.dropout ? 8 * a.sub_rows : 0) <= a.slot_bytes && a.sub_rows * row <= (backward ? a.d_y_at : a.keys_at));
-                    NEED(!backward || a.d_y_at + a.sub_rows * row <= a.keys_at);
-                    NEED(a.d_y_at % 16 == 0 && a.keys_at % 8 == 0 && a.slot_bytes % 128 == 0 && a.slot_bytes < 1 << 20);
-                    NEED(a.slots >= 4 && a.slots <= kRingSlots && ring_fixed_bytes(*v, s.channels) + a.slots * a.slot_bytes <= kRingSharedBytes);
-                    NEED(a.hold ? a.tile_rows <= a.sub_rows : a.tile_rows % a.sub_rows == 0);
-                } else {
-                    NEED(a.windows <= kMaxWindows && a.window_tile[a.windows] == tile && a.window_tile[0] == 0);
-                    for (int q = 0; q < a.windows; ++q) NEED(a.window_tile[q + 1] >= a.window_tile[q]);
-                    NEED((int64_t)s.channels <= (int64_t)a.chunks * (*v << a.tx) && a.tx <= 8);
-                }
+            plan_tiles(&s, 148, backward, *v, &p, &a);
+            NEED(p.bytes <= have);
+            const int64_t pair = 2 * 4 * (int64_t)s.channels;
+            int64_t tile = 0, fans_end = 0;
+            for (int64_t q = 0; q < n; ++q) {
+                const int64_t len = s.sample_offsets ? s.sample_offsets[q + 1] - s.sample_offsets[q] : s.rows_per_sample;
+                const int64_t tiles = (len + a.tile_rows - 1) / a.tile_rows, first = tile / kFan + q, fans = (tiles + kFan - 1) / kFan;
+                NEED(first >= fans_end && tiles <= kFan * kFan && fans <= kFan);
+                fans_end = first + std::max<int64_t>(fans, 1);
+                tile += tiles;
+                NEED(!a.equal || tiles == a.tiles_per_sample);
             }
+            NEED(p.at_fan_count + 4 * fans_end <= p.at_sample_count && p.at_fan_parts + fans_end * pair <= p.at_group_parts);
+            NEED(p.at_sample_count + 4 * n <= p.cleared && p.at_tile_parts + tile * pair <= p.at_fan_parts);
+            NEED(!backward || (p.n_parts == n && p.at_group_parts + 8 * n * s.groups <= p.at_parts && p.at_parts + n * pair <= p.at_slices && p.at_slices + kParamSlices * pair <= p.bytes));
+            NEED(tile * a.chunks < 1ll << 30 && (int64_t)a.tile_rows > 0);
+            NEED(p.window_tile.front() == 0 && p.window_tile.back() == tile);
+            for (size_t q = 0; q + 1 < p.window_tile.size(); ++q) NEED(p.window_tile[q + 1] > p.window_tile[q]);
+            NEED((int64_t)s.channels <= (int64_t)a.chunks * (*v << a.tx) && a.tx <= 8);
         }
     }
     return 0;
