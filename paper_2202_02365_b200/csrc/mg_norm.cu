@@ -88,7 +88,7 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
         a.tile_parts = reinterpret_cast<float*>(ws + p.at_tile_parts);
         a.fan_parts = reinterpret_cast<float*>(ws + p.at_fan_parts);
         a.group_parts = reinterpret_cast<float*>(ws + p.at_group_parts);
-        a.parts = reinterpret_cast<float*>(ws + p.at_parts);
+        a.parts = params ? reinterpret_cast<float*>(ws + p.at_parts) : nullptr;
         MG_CUDA(ctx, cudaMemsetAsync(ws, 0, p.cleared, st));
         bool empty = false;
         if (!a.equal) {
@@ -110,19 +110,14 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
             }
             if (a.samples > kInlineSamples) a.table = table;
         }
-        if (empty) {
-            k_norm_empty<<<std::min(a.samples, ctx->n_sms), 256, 0, st>>>(a, backward);
+        if (empty && !backward) {
+            k_norm_empty<<<std::min(a.samples, ctx->n_sms), 256, 0, st>>>(a);
             ctx->launches++;
         }
-        const int windows = (int)p.window_tile.size() - 1;
-        for (int w = 0; windows > 0 && w <= windows; ++w) {   // the sums of window w and the results of the one before
-            a.sums_tile = p.window_tile[std::min(w, windows)];
-            a.sums_blocks = w < windows ? (p.window_tile[w + 1] - p.window_tile[w]) * a.chunks : 0;
-            a.result_tile = w ? p.window_tile[w - 1] : 0;
-            a.result_tiles = w ? p.window_tile[w] - p.window_tile[w - 1] : 0;
-            const TileLaunch l{p.vec, backward, a.sums_blocks + (int64_t)a.result_tiles * a.chunks};
+        if (a.tiles > 0) {
+            const TileLaunch l{p.vec, p.sums_vec, backward};
             MG_BY_TYPE(s->dtype, launch_tiles<T>(l, a, st));
-            ctx->launches++;
+            ctx->launches += 2;
         }
     }
     if (backward && params) {

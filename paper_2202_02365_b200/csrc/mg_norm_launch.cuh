@@ -48,20 +48,33 @@ void launch_rows(const RowLaunch& l, const NormArgs& a, cudaStream_t st) {
     }
 }
 
-// K rows in flight for the sums, U for the results
+// K rows in flight per thread, MINB blocks to an SM
 template <typename T, int VEC>
-void launch_tiles_of(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
+void launch_sums(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
+    const unsigned grid = (unsigned)((int64_t)a.tiles * a.sums.chunks);
     constexpr bool wide = sizeof(T) * VEC == 32;
-    if (l.backward) k_norm_tiles<T, VEC, true, wide ? 2 : 4, wide ? 1 : 2, 3><<<(unsigned)l.grid, kNormThreads, 0, st>>>(a);
-    else k_norm_tiles<T, VEC, false, wide ? 2 : 4, wide ? 2 : 4, 4><<<(unsigned)l.grid, kNormThreads, 0, st>>>(a);
+    if (l.backward) k_norm_sums<T, VEC, true, wide ? 1 : VEC == 8 ? 2 : 4, 3><<<grid, kNormThreads, 0, st>>>(a);
+    else if constexpr (!wide) k_norm_sums<T, VEC, false, 4, 4><<<grid, kNormThreads, 0, st>>>(a);   // (nothing is gained by more than 16 bytes here)
+}
+template <typename T, int VEC>
+void launch_results(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
+    const unsigned grid = (unsigned)((int64_t)a.tiles * a.results.chunks);
+    constexpr bool wide = sizeof(T) * VEC == 32;
+    if (l.backward) k_norm_results<T, VEC, true, wide ? 1 : 2, 3><<<grid, kNormThreads, 0, st>>>(a);
+    else k_norm_results<T, VEC, false, wide ? 2 : 4, 4><<<grid, kNormThreads, 0, st>>>(a);
 }
 
 template <typename T>
 void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
-    if (l.vec == 8) launch_tiles_of<T, 8>(l, a, st);
-    else if (l.vec == 4) launch_tiles_of<T, 4>(l, a, st);
-    else if (sizeof(T) == 2 && l.vec == 2) launch_tiles_of<T, sizeof(T) == 2 ? 2 : 1>(l, a, st);
-    else launch_tiles_of<T, 1>(l, a, st);
+    constexpr int kTwo = sizeof(T) == 2 ? 2 : 1;
+    if (l.sums_vec == 8) launch_sums<T, 8>(l, a, st);
+    else if (l.sums_vec == 4) launch_sums<T, 4>(l, a, st);
+    else if (l.sums_vec == kTwo && kTwo == 2) launch_sums<T, kTwo>(l, a, st);
+    else launch_sums<T, 1>(l, a, st);
+    if (l.vec == 8) launch_results<T, 8>(l, a, st);
+    else if (l.vec == 4) launch_results<T, 4>(l, a, st);
+    else if (l.vec == kTwo && kTwo == 2) launch_results<T, kTwo>(l, a, st);
+    else launch_results<T, 1>(l, a, st);
 }
 
 }  // namespace mgnorm

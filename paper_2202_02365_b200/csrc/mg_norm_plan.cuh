@@ -4,7 +4,6 @@
 #include <math.h>
 
 #include <algorithm>
-#include <vector>
 
 #include "mg_internal.cuh"
 #include "mg_norm_tiles.cuh"
@@ -94,7 +93,7 @@ struct NormPlan {
     // workspace: bytes that are cleared first, then where the others start
     size_t cleared = 0, at_fan_count = 0, at_sample_count = 0, at_table = 0, at_tile_parts = 0, at_fan_parts = 0, at_group_parts = 0, at_parts = 0, at_slices = 0, bytes = 0;
     int64_t n_parts = 0;   // backward: what k_norm_params adds up
-    std::vector<int32_t> window_tile;   // tiles: where the windows start, and the end of the last
+    int sums_vec = 1;      // tiles: vectors of the sums
 };
 
 int ceil_log2(int64_t v) { int l = 0; while ((1ll << l) < v) ++l; return l; }
@@ -103,7 +102,7 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 constexpr int64_t kParamSlices = 64;   // of the parts that k_norm_params adds up in two steps
 constexpr int kRowsMaxChannels = 32 * kRowValues;
 constexpr int kRowBlocks = 8, kRowBlocksBackward = 4;   // blocks per SM
-constexpr int kTileBlocks = 4;
+constexpr int kTileBlocks = 4, kTileBlocksBackward = 3;
 
 // Rows that are samples by themselves, `vec` values to a vector.
 void plan_rows(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p) {
@@ -123,58 +122,52 @@ void plan_rows(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPla
 }
 
 constexpr int64_t kTileBytes = 192 << 10;
-inline int64_t window_bytes() { const char* e = getenv("MG_NORM_WINDOW_MB"); return (int64_t)(e ? atof(e) : 1e5) * (1 << 20); }
 
 // Samples of several rows.  a: the geometry's part of the arguments.
 void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p, TileArgs* a) {
     p->mode = NORM_TILES; p->vec = vec;
-    const int64_t n = sample_count(s), vecs = s->channels / vec, elem = elem_size(s->dtype);
+    const int64_t n = sample_count(s), elem = elem_size(s->dtype);
+    // (16 bytes a thread let more rows be on their way; with a dropout eight channels share a block of the generator)
+    p->sums_vec = backward && s->dropout ? vec : (int)std::min<int64_t>(vec, 16 / elem);
+    const auto shape = [&](int v) {
+        TileShape t;
+        const int64_t vecs = s->channels / v;
+        t.tx = std::min(ceil_log2(kNormThreads), ceil_log2(vecs));
+        t.chunks = (int32_t)((vecs + (1 << t.tx) - 1) >> t.tx);
+        return t;
+    };
+    a->sums = shape(p->sums_vec); a->results = shape(vec);
+    a->run = (int32_t)std::min<int64_t>(s->channels, (int64_t)p->sums_vec << a->sums.tx);
     const bool equal = !s->sample_offsets;
     const int64_t used = equal ? s->rows : s->sample_offsets[n];
     int64_t longest = equal ? s->rows_per_sample : 0;
     if (!equal) for (int64_t i = 0; i < n; ++i) longest = std::max(longest, s->sample_offsets[i + 1] - s->sample_offsets[i]);
-    a->tx = std::min(ceil_log2(kNormThreads), ceil_log2(vecs));
-    a->chunks = (int32_t)((vecs + (1 << a->tx) - 1) >> a->tx);
-    const int64_t n_ty = kNormThreads >> a->tx, row_bytes = std::min<int64_t>(s->channels, (int64_t)vec << a->tx) * elem;
     // tiles of about 192 KB, so many of them that the blocks the SMs hold together take equal turns; smaller ones where there would not be a turn
     // for each, larger ones where a sample had more than kFan^2
-    const int64_t held = (int64_t)n_sms * kTileBlocks, bytes = used * row_bytes * a->chunks, turns = std::max<int64_t>(1, (bytes + held * kTileBytes / 2) / (held * kTileBytes));
-    const int64_t spread = std::max<int64_t>(1, (used * a->chunks + held * turns - 1) / (held * turns));
+    const int64_t n_ty = kNormThreads >> a->results.tx, run_bytes = a->run * elem, chunks = a->sums.chunks;
+    const int64_t held = (int64_t)n_sms * (backward ? kTileBlocksBackward : kTileBlocks), bytes = used * run_bytes * chunks;
+    const int64_t turns = std::max<int64_t>(1, (bytes + held * kTileBytes / 2) / (held * kTileBytes)), spread = std::max<int64_t>(1, (used * chunks + held * turns - 1) / (held * turns));
     const int64_t rows = std::max({round_up(spread, n_ty), round_up((longest + kFan * kFan - 1) / (kFan * kFan), n_ty), (int64_t)16});
     a->tile_rows = (int32_t)std::min<int64_t>(rows, 1 << 30);
     a->samples = (int32_t)n; a->equal = equal;
     a->rows_per_sample = s->rows_per_sample;
     a->tiles_per_sample = equal ? (int32_t)((s->rows_per_sample + a->tile_rows - 1) / a->tile_rows) : 0;
-    // windows: whole samples
-    const int64_t bytes_per_row = (int64_t)s->channels * elem * (backward ? 2 : 1), window = window_bytes();
-    int64_t tiles = 0;
-    p->window_tile.assign(1, 0);
-    if (equal) {
-        const int64_t sample_bytes = std::max<int64_t>(1, s->rows_per_sample * bytes_per_row), per = std::max<int64_t>(1, (window + sample_bytes - 1) / sample_bytes);
-        for (int64_t i = 0; i < n; i += per) { tiles += std::min(per, n - i) * a->tiles_per_sample; p->window_tile.push_back((int32_t)tiles); }
-    } else {
-        int64_t in_window = 0;
-        for (int64_t i = 0; i < n; ++i) {
-            const int64_t len = s->sample_offsets[i + 1] - s->sample_offsets[i];
-            tiles += (len + a->tile_rows - 1) / a->tile_rows;
-            in_window += len * bytes_per_row;
-            if ((in_window >= window || i + 1 == n) && tiles > p->window_tile.back()) { p->window_tile.push_back((int32_t)tiles); in_window = 0; }
-        }
-    }
-    a->reversed = 1;
-    const int64_t fans = tiles / kFan + n + 1, pair = 2 * (int64_t)sizeof(float) * s->channels;
+    int64_t tiles = equal ? n * a->tiles_per_sample : 0;
+    if (!equal) for (int64_t i = 0; i < n; ++i) tiles += (s->sample_offsets[i + 1] - s->sample_offsets[i] + a->tile_rows - 1) / a->tile_rows;
+    a->tiles = (int32_t)tiles;
+    const int64_t fans = tiles / kFan + n + 1, pair = 2 * (int64_t)sizeof(float);
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 15) / 16 * 16; return was; };
     p->at_fan_count = take(4 * (size_t)fans);
     p->at_sample_count = take(4 * (size_t)n);
     p->cleared = at;
     p->at_table = take(!equal && n > kInlineSamples ? sizeof(int2) * (size_t)(n + 1) : 0);
-    p->at_tile_parts = take((size_t)(tiles * pair));
-    p->at_fan_parts = take((size_t)(fans * pair));
-    p->at_group_parts = take(backward ? 2 * sizeof(float) * (size_t)(n * s->groups) : 0);
-    p->n_parts = backward ? n : 0;
-    p->at_parts = take((size_t)(p->n_parts * pair));
-    p->at_slices = take(p->n_parts ? (size_t)(kParamSlices * pair) : 0);
+    p->at_tile_parts = take((size_t)(tiles * chunks * s->groups * pair));
+    p->at_fan_parts = take((size_t)(fans * s->groups * pair));
+    p->at_group_parts = take(backward ? (size_t)(n * s->groups * pair) : 0);
+    p->n_parts = backward ? tiles : 0;
+    p->at_parts = take((size_t)(p->n_parts * s->channels * pair));
+    p->at_slices = take(p->n_parts ? (size_t)(kParamSlices * s->channels * pair) : 0);
     p->bytes = at;
 }
 

@@ -1,6 +1,8 @@
-// Group norm of samples of several rows, in two passes: tiles of rows are summed up by channel, the last block of a sample's brings its sums
-// together, and a launch later the tiles' results are computed.  No block waits for another.  A launch does the sums of one window of samples and
-// the results of the window before, so that both passes keep the memory busy together and the second finds its rows in L2.
+// Group norm of samples of several rows, in two launches: tiles of rows are summed up, the last block of a sample's tiles brings its sums
+// together, and the second launch computes the results from the rows once more.  No block waits for another.  The second launch goes through
+// the tiles from the last to the first: what was read last is still in L2.
+// (One persistent launch with the rows kept in shared memory until their sample's sums were there, or read again as soon as they were, took
+// 1.4 to 3.9 times as long: every tile waits for round trips through L2 that nothing hides.)
 #pragma once
 
 #include "mg_norm_rows.cuh"
@@ -10,6 +12,9 @@ namespace mgnorm {
 constexpr int kFan = 32;             // tiles whose sums one block brings together; then as many of those
 constexpr int kInlineSamples = 64;   // samples whose place is handed over in the kernel's parameters
 
+// how a launch's blocks lie on a tile: 2^tx threads along a row, the channels in `chunks` runs of as many vectors
+struct TileShape { int32_t tx = 0, chunks = 0; };
+
 struct TileArgs : NormArgs {
     // samples: equal ones, or a table of (first row, first tile), one entry more than samples
     int32_t samples = 0, equal = 0;
@@ -17,16 +22,16 @@ struct TileArgs : NormArgs {
     int32_t tiles_per_sample = 0;
     const int2* table = nullptr;     // null: `inl`
     int2 inl[kInlineSamples + 1];
-    // tiles: tile_rows rows, each in `chunks` runs of (256 or fewer) vectors
-    int32_t tile_rows = 0, chunks = 0, tx = 0;   // tx: log2 of the threads along a row
-    // this launch: sums of tiles from sums_tile on in the first sums_blocks blocks, results of those from result_tile on in the others
-    int32_t sums_tile = 0, sums_blocks = 0, result_tile = 0, result_tiles = 0, reversed = 0;
+    int32_t tile_rows = 0, tiles = 0;
+    TileShape sums, results;
+    int32_t run = 0;                 // channels of a run, for the sums
     // workspace
-    uint32_t* fan_count = nullptr;   // cleared: sums that have arrived, by kFan tiles of a sample ...
+    uint32_t* fan_count = nullptr;      // cleared: sums that have arrived, by kFan tiles of a sample ...
     uint32_t* sample_count = nullptr;   // ... and by sample
-    float* tile_parts = nullptr;     // [tiles][2][channels]
-    float* fan_parts = nullptr;      // [tiles / kFan + samples][2][channels]
+    float* tile_parts = nullptr;     // [tiles][chunks][2][groups]: mean and squares about it, or (backward) sums of dz w hat and dz w
+    float* fan_parts = nullptr;      // [tiles / kFan + samples][2][groups]
     float* group_parts = nullptr;    // backward: mean of dz w, mean of dz w hat: [samples][2][groups]
+    // (parts: the tiles' sums by channel)
 };
 
 struct Tile {
@@ -90,8 +95,8 @@ __device__ __forceinline__ void merge(Pair<VEC>& a, float nb, const float (&u)[V
 
 // Sums of a tile: every thread has one vector of the channels and every n_ty-th row, K rows in flight; then the block's threads are brought together.
 template <typename T, int VEC, bool BACKWARD, int K>
-__device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int32_t c, bool in, int ty, int n_ty, float mean, float rstd, const float (&w)[VEC],
-                                          const float (&b)[VEC], Pair<VEC>& p) {
+__device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int32_t c, bool in, int ty, int n_ty, float mean, float rstd, const float* sw,
+                                          const float* sb, Pair<VEC>& p) {
     p.n = 0.f;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) p.u[e] = p.v[e] = 0.f;
@@ -112,7 +117,9 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int3
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 if (r + k * n_ty >= rows) break;
-                float h[VEC], d[VEC];
+                float h[VEC], d[VEC], w[VEC], b[VEC];
+                Params<VEC, 8, true>::read(sw, w);
+                Params<VEC, 8, true>::read(sb, b);
                 grad_vector<T, VEC>(a, raw[k], rd[k], a.drop.on ? drop_key(a.drop, t.row0 + r + k * n_ty) : 0, c, mean, rstd, w, b, h, d);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) { p.u[e] = fmaf(d[e], h[e], p.u[e]); p.v[e] += d[e]; }
@@ -166,150 +173,150 @@ __device__ __forceinline__ void lane_pairs(Pair<VEC>& p, int threads_x) {
     }
 }
 
-// The block's threads with the same channels, into `out` ([2][channels], the chunk's channels of it)
-template <int VEC, bool BACKWARD>
-__device__ __forceinline__ void block_pairs(const TileArgs& a, Pair<VEC>& p, float* smem, int tx, int32_t chunk0, float* out) {
-    const int threads_x = 1 << a.tx, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    lane_pairs<VEC, BACKWARD>(p, threads_x);
-    const int across = threads_x < 32 ? kNormThreads / 32 : kNormThreads / threads_x;   // sets of a channel that are left
-    const int set = threads_x < 32 ? warp : threadIdx.x >> a.tx, width = threads_x * VEC;
-    float* su = smem;                          // [across][width], across * width <= kNormThreads * VEC
-    float* sv = smem + kNormThreads * VEC;
-    float* sn = smem + 2 * kNormThreads * VEC;   // [across]
-    __syncthreads();
-    if (threads_x >= 32 || lane < threads_x) {
+template <int VEC> __device__ __forceinline__ void put_shared(float* s, const float (&v)[VEC]) {
+    if constexpr (VEC % 4 == 0) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) { su[set * width + tx * VEC + e] = p.u[e]; sv[set * width + tx * VEC + e] = p.v[e]; }
+        for (int e = 0; e < VEC; e += 4) *reinterpret_cast<float4*>(s + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s[e] = v[e];
+    }
+}
+
+// The block's threads with the same channels: su[i], sv[i] become channel i's of the run (su, sv: [256 * VEC], sn: [kNormWarps or the sets])
+template <int VEC, bool BACKWARD>
+__device__ __forceinline__ void block_pairs(Pair<VEC>& p, float* su, float* sv, float* sn, int log_x, int32_t channels) {
+    const int threads_x = 1 << log_x, tx = threadIdx.x & (threads_x - 1), lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    lane_pairs<VEC, BACKWARD>(p, threads_x);
+    const int across = threads_x < 32 ? kNormWarps : kNormThreads / threads_x;   // sets of a channel that are left
+    const int set = threads_x < 32 ? warp : threadIdx.x >> log_x, width = threads_x * VEC;
+    if (threads_x >= 32 || lane < threads_x) {
+        put_shared<VEC>(su + set * width + tx * VEC, p.u);
+        put_shared<VEC>(sv + set * width + tx * VEC, p.v);
         if (tx == 0) sn[set] = p.n;
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < width; i += kNormThreads) {
-        const int32_t c = chunk0 + i;
-        if (c >= a.channels) break;
+    for (int i = threadIdx.x; i < min(width, channels); i += kNormThreads) {   // (a thread reads and writes its channel's column alone)
         float u = su[i], v = sv[i], n = sn[0];
+        if (across == 1) break;
         for (int s = 1; s < across; ++s) {
             if (BACKWARD) { u += su[s * width + i]; v += sv[s * width + i]; }
             else merge_moments(n, u, v, sn[s], su[s * width + i], sv[s * width + i]);
         }
-        __stcg(out + c, u);
-        __stcg(out + a.channels + c, v);
+        su[i] = u; sv[i] = v;
     }
+    __syncthreads();
 }
 
-// sums of `n` sets that lie one behind the other, rows_of(i) rows each, into `out` and, where it is given, `shared` ([2][stride]); V channels a
-// thread at a time, B sets in flight
-template <bool BACKWARD, int NT, int V, int B, typename Rows>
-__device__ __forceinline__ void merge_parts(const TileArgs& a, const float* parts, int32_t n, Rows rows_of, float* out, int tid, float* shared, int stride) {
-    const int64_t step = 2 * (int64_t)a.channels;
-    for (int32_t c = tid * V; c < a.channels; c += NT * V) {
-        float u[V], v[V], m = 0.f;
-#pragma unroll
-        for (int e = 0; e < V; ++e) u[e] = v[e] = 0.f;
-        for (int32_t i0 = 0; i0 < n; i0 += B) {
-            float pu[B][V], pv[B][V];
-#pragma unroll
-            for (int k = 0; k < B; ++k)
-                if (i0 + k < n) {
-                    const float* from = parts + (i0 + k) * step + c;
-                    if constexpr (V == 4) {
-                        const float4 x = __ldcg(reinterpret_cast<const float4*>(from)), y = __ldcg(reinterpret_cast<const float4*>(from + a.channels));
-                        pu[k][0] = x.x; pu[k][1] = x.y; pu[k][2] = x.z; pu[k][3] = x.w;
-                        pv[k][0] = y.x; pv[k][1] = y.y; pv[k][2] = y.z; pv[k][3] = y.w;
-                    } else { pu[k][0] = __ldcg(from); pv[k][0] = __ldcg(from + a.channels); }
-                }
-#pragma unroll
-            for (int k = 0; k < B; ++k)
-                if (i0 + k < n) {
-                    if (BACKWARD) {
-#pragma unroll
-                        for (int e = 0; e < V; ++e) { u[e] += pu[k][e]; v[e] += pv[k][e]; }
-                    } else {
-                        const float nb = rows_of(i0 + k), all = m + nb, f = __fdividef(nb, all), g = m * f;   // (no set is empty)
-#pragma unroll
-                        for (int e = 0; e < V; ++e) {
-                            const float d = pu[k][e] - u[e];
-                            u[e] = fmaf(d, f, u[e]);
-                            v[e] += fmaf(d * g, d, pv[k][e]);
-                        }
-                        m = all;
-                    }
-                }
-        }
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-            __stcg(out + c + e, u[e]);
-            __stcg(out + a.channels + c + e, v[e]);
-            if (shared) { shared[c + e] = u[e]; shared[stride + c + e] = v[e]; }
-        }
-    }
+// threads that share a group, of one warp, where `threads` work on `groups`
+__device__ __forceinline__ int group_threads(int groups, int threads) {
+    int per = 1;
+    while (per < 32 && 2 * per * groups <= threads) per *= 2;
+    return per;
 }
 
-// the groups' values from the channels' of a whole sample: a warp per group
-template <bool BACKWARD, int NT>
-__device__ __forceinline__ void finish_sample(const TileArgs& a, int32_t sample, float rows, const float* part) {
-    const int lane = threadIdx.x & 31;
-    const float n = rows * (float)a.each;
-    for (int32_t g = threadIdx.x >> 5; g < a.groups; g += NT / 32) {
+// channels that a run [c0, c1) and a group have in common
+__device__ __forceinline__ int32_t shared_channels(const TileArgs& a, int32_t g, int32_t c0, int32_t c1) { return max(0, min(c1, (g + 1) * a.each) - max(c0, g * a.each)); }
+
+// a run's groups from its channels
+template <bool BACKWARD>
+__device__ __forceinline__ void run_groups(const TileArgs& a, const float* su, const float* sv, int32_t c0, int32_t c1, float rows, float* out) {
+    const int32_t g_lo = c0 / a.each, n_g = (c1 - 1) / a.each - g_lo + 1;
+    const int per = group_threads(n_g, kNormThreads), sub = threadIdx.x % per;
+    for (int32_t q = 0; q < n_g; q += kNormThreads / per) {   // (all threads of a warp go round together)
+        const int32_t g = g_lo + q + threadIdx.x / per, lo = max(c0, g * a.each), hi = q + (int)threadIdx.x / per < n_g ? min(c1, (g + 1) * a.each) : 0;
         float u = 0.f, v = 0.f;
-        for (int32_t c = g * a.each + lane; c < (g + 1) * a.each; c += 32) {
+        for (int32_t c = lo + sub; c < hi; c += per) {
             if (BACKWARD) {
                 const float w = a.weight ? a.weight[c] : 1.f;
-                u = fmaf(w, __ldcg(part + c), u); v = fmaf(w, __ldcg(part + a.channels + c), v);
-            } else u += __ldcg(part + c);
+                u = fmaf(w, su[c - c0], u); v = fmaf(w, sv[c - c0], v);
+            } else u += su[c - c0];
         }
-        u = row_sum(u, 5); v = row_sum(v, 5);
-        if (BACKWARD) {
-            if (lane == 0) {
-                __stcg(a.group_parts + ((int64_t)sample * 2) * a.groups + g, v / n);        // mean of dz w
-                __stcg(a.group_parts + ((int64_t)sample * 2 + 1) * a.groups + g, u / n);    // mean of dz w hat
-            }
-            continue;
+        for (int o = 1; o < per; o <<= 1) { u += __shfl_xor_sync(0xFFFFFFFFu, u, o); if (BACKWARD) v += __shfl_xor_sync(0xFFFFFFFFu, v, o); }
+        if (!BACKWARD) {
+            u /= (float)max(hi - lo, 1);
+            for (int32_t c = lo + sub; c < hi; c += per) { const float d = su[c - c0] - u; v += fmaf(d * rows, d, sv[c - c0]); }
+            for (int o = 1; o < per; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
         }
-        const float mean = u / (float)a.each;
-        for (int32_t c = g * a.each + lane; c < (g + 1) * a.each; c += 32) {
-            const float d = __ldcg(part + c) - mean;
-            v += fmaf(d * d, rows, __ldcg(part + a.channels + c));
-        }
-        v = row_sum(v, 5);
-        if (lane == 0) {
-            __stcg(a.mean + (int64_t)sample * a.groups + g, mean);
-            __stcg(a.rstd + (int64_t)sample * a.groups + g, rsqrtf(v / n + a.eps));
-        }
+        if (sub == 0 && lo < hi) { __stcg(out + g, u); __stcg(out + a.groups + g, v); }
     }
 }
 
-// A tile's sums are written: the last of kFan tiles brings theirs together, the last of those the sample's.
+// `n` sets of the groups' values that lie one behind the other, of values_of(i, g) values each (none: the set is not there), to `use(g, u, v)`
+template <bool BACKWARD, typename Values, typename Use>
+__device__ __forceinline__ void merge_sets(const TileArgs& a, const float* parts, int32_t n, Values values_of, Use use) {
+    const int64_t step = 2 * (int64_t)a.groups;
+    const int per = group_threads(a.groups, kNormThreads), sub = threadIdx.x % per;
+    constexpr int B = 4;   // sets on their way at a time
+    for (int32_t g0 = 0; g0 < a.groups; g0 += kNormThreads / per) {
+        const int32_t g = min(g0 + (int)threadIdx.x / per, a.groups - 1);
+        float m = 0.f, u = 0.f, v = 0.f;
+        for (int32_t i0 = sub; i0 < n; i0 += B * per) {
+            float pu[B], pv[B], pn[B];
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                const int32_t i = min(i0 + k * per, n - 1);
+                pn[k] = i0 + k * per < n ? values_of(i, g) : 0.f;
+                pu[k] = __ldcg(parts + i * step + g); pv[k] = __ldcg(parts + i * step + a.groups + g);
+            }
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                if (pn[k] == 0.f) continue;
+                if (BACKWARD) { u += pu[k]; v += pv[k]; }
+                else merge_moments(m, u, v, pn[k], pu[k], pv[k]);
+            }
+        }
+        for (int o = 1; o < per; o <<= 1) {
+            const float mb = __shfl_xor_sync(0xFFFFFFFFu, m, o), ub = __shfl_xor_sync(0xFFFFFFFFu, u, o), vb = __shfl_xor_sync(0xFFFFFFFFu, v, o);
+            if (BACKWARD) { u += ub; v += vb; }
+            else if (threadIdx.x & o) { float x = mb, y = ub, z = vb; merge_moments(x, y, z, m, u, v); m = x; u = y; v = z; }   // (the lower threads' set first)
+            else merge_moments(m, u, v, mb, ub, vb);
+        }
+        if (sub == 0 && g0 + (int)threadIdx.x / per < a.groups) use(g, u, v);
+    }
+}
+
+// A block's sums are written: the last of kFan tiles' brings theirs together, the last of those the sample's.
 template <bool BACKWARD>
 __device__ __forceinline__ void arrive(const TileArgs& a, const Tile& t, int32_t* sh_last) {
-    const int32_t in_sample = t.tile - t.first, fan = in_sample / kFan, fans = (t.tiles + kFan - 1) / kFan, fan_tiles = min(kFan, t.tiles - fan * kFan);
-    const int64_t fan_id = t.first / kFan + t.sample + fan;   // (blocks of kFan tiles of all samples before lie below)
-    __syncthreads();
-    if (threadIdx.x == 0) {   // (what the block's threads wrote before they met is announced with it)
-        __threadfence();
-        *sh_last = atomicAdd(a.fan_count + fan_id, 1u) + 1u == (uint32_t)(fan_tiles * a.chunks);
-        __threadfence();
-    }
-    __syncthreads();
-    if (!*sh_last) return;
-    const int64_t step = 2 * (int64_t)a.channels;
-    float* fan_part = a.fan_parts + fan_id * step;
-    const auto tile_rows = [&](int32_t i) { return (float)min((int64_t)a.tile_rows, t.sample_rows - ((int64_t)fan * kFan + i) * a.tile_rows); };
-    float* whole = BACKWARD ? a.parts + t.sample * step : a.fan_parts + (t.first / kFan + t.sample) * step;   // the sample's channels
-    merge_parts<BACKWARD, kNormThreads, 1, 8>(a, a.tile_parts + ((int64_t)t.first + fan * kFan) * step, fan_tiles, tile_rows, fans == 1 ? whole : fan_part, threadIdx.x, nullptr, 0);
-    __syncthreads();
-    if (fans > 1) {
-        if (threadIdx.x == 0) {
+    const int32_t fan = (t.tile - t.first) / kFan, fans = (t.tiles + kFan - 1) / kFan, fan_tiles = min(kFan, t.tiles - fan * kFan), chunks = a.sums.chunks;
+    const int64_t first_fan = t.first / kFan + t.sample;   // (those of all samples before lie below)
+    const int64_t step = 2 * (int64_t)a.groups;
+    const auto last = [&](uint32_t* counter, int32_t want) {
+        __syncthreads();
+        if (threadIdx.x == 0) {   // (what the block's threads wrote before they met is announced with it)
             __threadfence();
-            *sh_last = atomicAdd(a.sample_count + t.sample, 1u) + 1u == (uint32_t)fans;
+            *sh_last = atomicAdd(counter, 1u) + 1u == (uint32_t)want;
             __threadfence();
         }
         __syncthreads();
-        if (!*sh_last) return;
-        const auto fan_rows = [&](int32_t i) { return (float)min((int64_t)kFan * a.tile_rows, t.sample_rows - (int64_t)i * kFan * a.tile_rows); };
-        merge_parts<BACKWARD, kNormThreads, 1, 8>(a, a.fan_parts + (t.first / kFan + t.sample) * step, fans, fan_rows, whole, threadIdx.x, nullptr, 0);
-        __syncthreads();
-    }
-    finish_sample<BACKWARD, kNormThreads>(a, t.sample, (float)t.sample_rows, whole);
+        return *sh_last != 0;
+    };
+    const float values = (float)t.sample_rows * (float)a.each;
+    const auto finish = [&](int32_t g, float u, float v) {
+        if (BACKWARD) {
+            a.group_parts[t.sample * step + g] = v / values;               // mean of dz w
+            a.group_parts[t.sample * step + a.groups + g] = u / values;    // mean of dz w hat
+        } else {
+            a.mean[(int64_t)t.sample * a.groups + g] = u;
+            a.rstd[(int64_t)t.sample * a.groups + g] = rsqrtf(v / values + a.eps);
+        }
+    };
+    if (!last(a.fan_count + first_fan + fan, fan_tiles * chunks)) return;
+    float* fan_part = a.fan_parts + (first_fan + fan) * step;
+    const auto tile_values = [&](int32_t i, int32_t g) {
+        const int64_t rows = min((int64_t)a.tile_rows, t.sample_rows - ((int64_t)fan * kFan + i / chunks) * a.tile_rows);
+        const int32_t c0 = i % chunks * a.run;
+        return (float)rows * (float)(chunks == 1 ? a.each : shared_channels(a, g, c0, min(c0 + a.run, a.channels)));
+    };
+    const auto keep = [&](int32_t g, float u, float v) {
+        if (fans == 1) finish(g, u, v);
+        else { __stcg(fan_part + g, u); __stcg(fan_part + a.groups + g, v); }
+    };
+    merge_sets<BACKWARD>(a, a.tile_parts + ((int64_t)t.first + fan * kFan) * chunks * step, fan_tiles * chunks, tile_values, keep);
+    if (fans == 1 || !last(a.sample_count + t.sample, fans)) return;
+    const auto fan_values = [&](int32_t i, int32_t) { return (float)min((int64_t)kFan * a.tile_rows, t.sample_rows - (int64_t)i * kFan * a.tile_rows) * (float)a.each; };
+    merge_sets<BACKWARD>(a, a.fan_parts + first_fan * step, fans, fan_values, finish);
 }
 
 template <int VEC>
@@ -326,37 +333,58 @@ __device__ __forceinline__ void load_params(const float* p, int32_t c, float wit
     for (int e = 0; e < VEC; ++e) o[e] = p ? p[c + e] : without;
 }
 
-template <typename T, int VEC, bool BACKWARD, int K, int U, int MINB>
-__global__ void __launch_bounds__(kNormThreads, MINB) k_norm_tiles(const __grid_constant__ TileArgs a) {
-    __shared__ __align__(16) float smem[2 * kNormThreads * VEC + kNormWarps];
-    __shared__ int32_t sh_flag;
-    const int tx = threadIdx.x & ((1 << a.tx) - 1), ty = threadIdx.x >> a.tx, n_ty = kNormThreads >> a.tx;
-    const bool sums = (int32_t)blockIdx.x < a.sums_blocks;
-    const int32_t item = (int32_t)blockIdx.x - (sums ? 0 : a.sums_blocks), tile = item / a.chunks, chunk = item - tile * a.chunks;
+// weight and bias of a block's run of channels, for the gradient: in shared memory, so that more blocks fit an SM's registers
+template <int VEC>
+__device__ __forceinline__ void share_params(const TileArgs& a, float* sw, float* sb, int32_t c0, int32_t n) {
+    for (int i = threadIdx.x; i < n; i += kNormThreads) { sw[i] = a.weight ? a.weight[c0 + i] : 1.f; sb[i] = a.bias ? a.bias[c0 + i] : 0.f; }
+    __syncthreads();
+}
+
+template <typename T, int VEC, bool BACKWARD, int K, int MINB>
+__global__ void __launch_bounds__(kNormThreads, MINB) k_norm_sums(const __grid_constant__ TileArgs a) {
+    __shared__ __align__(16) float su[kNormThreads * VEC], sv[kNormThreads * VEC], sw[BACKWARD ? kNormThreads * VEC : 4], sb[BACKWARD ? kNormThreads * VEC : 4];
+    __shared__ float sn[kNormThreads];
+    __shared__ int32_t sh_last;
+    const int tx = threadIdx.x & ((1 << a.sums.tx) - 1), ty = threadIdx.x >> a.sums.tx, n_ty = kNormThreads >> a.sums.tx;
+    const int32_t tile = (int32_t)blockIdx.x / a.sums.chunks, chunk = (int32_t)blockIdx.x - tile * a.sums.chunks;
     Tile t;
-    locate_tile(a, sums ? a.sums_tile + tile : a.result_tile + (a.reversed ? a.result_tiles - 1 - tile : tile), &t);
-    const int32_t chunk0 = chunk * (VEC << a.tx), c = chunk0 + tx * VEC;
-    const bool in = c < a.channels;
-    const int64_t stat = (int64_t)t.sample * a.groups + (in ? c / a.each : 0);
-    float w[VEC], b[VEC], mean = 0.f, rstd = 0.f;
-    if (BACKWARD || !sums) {
-        load_params<VEC>(in ? a.weight : nullptr, c, 1.f, w);
-        load_params<VEC>(in ? a.bias : nullptr, c, 0.f, b);
-        mean = a.mean[stat]; rstd = a.rstd[stat];
-    }
-    if (sums) {
-        Pair<VEC> p;
-        tile_sums<T, VEC, BACKWARD, K>(a, t, c, in, ty, n_ty, mean, rstd, w, b, p);
-        block_pairs<VEC, BACKWARD>(a, p, smem, tx, chunk0, a.tile_parts + 2 * (int64_t)t.tile * a.channels);
-        arrive<BACKWARD>(a, t, &sh_flag);
-        return;
-    }
-    if (!in) return;
-    float s1 = 0.f, s2 = 0.f;
+    locate_tile(a, tile, &t);
+    const int32_t c0 = chunk * a.run, c1 = min(c0 + a.run, a.channels), c = c0 + tx * VEC;
+    const bool in = c < c1;
+    float mean = 0.f, rstd = 0.f;
     if (BACKWARD) {
-        const int64_t at_group = (int64_t)t.sample * 2 * a.groups + c / a.each;
-        s1 = a.group_parts[at_group]; s2 = a.group_parts[at_group + a.groups];
+        const int64_t stat = (int64_t)t.sample * a.groups + (in ? c / a.each : 0);
+        mean = a.mean[stat]; rstd = a.rstd[stat];
+        share_params<VEC>(a, sw, sb, c0, c1 - c0);
+    }
+    Pair<VEC> p;
+    tile_sums<T, VEC, BACKWARD, K>(a, t, c, in, ty, n_ty, mean, rstd, sw + tx * VEC, sb + tx * VEC, p);
+    block_pairs<VEC, BACKWARD>(p, su, sv, sn, a.sums.tx, c1 - c0);
+    if (BACKWARD && a.parts) {
+        float* to = a.parts + 2 * (int64_t)tile * a.channels + c0;
+        for (int i = threadIdx.x; i < c1 - c0; i += kNormThreads) { to[i] = su[i]; to[a.channels + i] = sv[i]; }
+    }
+    run_groups<BACKWARD>(a, su, sv, c0, c1, (float)(t.row1 - t.row0), a.tile_parts + 2 * ((int64_t)tile * a.sums.chunks + chunk) * a.groups);
+    arrive<BACKWARD>(a, t, &sh_last);
+}
+
+template <typename T, int VEC, bool BACKWARD, int U, int MINB>
+__global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __grid_constant__ TileArgs a) {
+    __shared__ __align__(16) float sw[BACKWARD ? kNormThreads * VEC : 4], sb[BACKWARD ? kNormThreads * VEC : 4];
+    const int tx = threadIdx.x & ((1 << a.results.tx) - 1), ty = threadIdx.x >> a.results.tx, n_ty = kNormThreads >> a.results.tx;
+    const int32_t from_last = (int32_t)blockIdx.x / a.results.chunks, c0 = ((int32_t)blockIdx.x - from_last * a.results.chunks) * (VEC << a.results.tx), c = c0 + tx * VEC;
+    Tile t;
+    locate_tile(a, a.tiles - 1 - from_last, &t);
+    if (BACKWARD) share_params<VEC>(a, sw, sb, c0, min(VEC << a.results.tx, a.channels - c0));
+    if (c >= a.channels) return;
+    const int32_t group = c / a.each;
+    const float mean = a.mean[(int64_t)t.sample * a.groups + group], rstd = a.rstd[(int64_t)t.sample * a.groups + group];
+    float s1 = 0.f, s2 = 0.f, w[VEC], b[VEC];
+    if (BACKWARD) {
+        s1 = a.group_parts[(int64_t)t.sample * 2 * a.groups + group]; s2 = a.group_parts[((int64_t)t.sample * 2 + 1) * a.groups + group];
     } else {
+        load_params<VEC>(a.weight, c, 1.f, w);
+        load_params<VEC>(a.bias, c, 0.f, b);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) w[e] *= rstd;
     }
@@ -380,6 +408,8 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_tiles(const __grid_
             float f[VEC];
             if constexpr (BACKWARD) {
                 float h[VEC];
+                Params<VEC, 8, true>::read(sw + tx * VEC, w);
+                Params<VEC, 8, true>::read(sb + tx * VEC, b);
                 grad_vector<T, VEC>(a, raw[k], rd[k], key, c, mean, rstd, w, b, h, f);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f[e] = rstd * fmaf(-h[e], s2, fmaf(f[e], w[e], -s1));
@@ -402,19 +432,18 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_tiles(const __grid_
     }
 }
 
-// Samples without rows have no tiles: their statistics (backward: their parts of the weight's and bias's gradients) are zero.
+// Samples without rows have no tiles: their statistics are zero.
 template <typename = void>
-__global__ void k_norm_empty(const __grid_constant__ TileArgs a, int backward) {
+__global__ void k_norm_empty(const __grid_constant__ TileArgs a) {
     for (int32_t s = blockIdx.x; s < a.samples; s += gridDim.x) {
         if (sample_entry(a, s).x != sample_entry(a, s + 1).x) continue;
-        if (!backward) for (int32_t g = threadIdx.x; g < a.groups; g += blockDim.x) { a.mean[(int64_t)s * a.groups + g] = 0.f; a.rstd[(int64_t)s * a.groups + g] = 0.f; }
-        else for (int32_t c = threadIdx.x; c < 2 * a.channels; c += blockDim.x) a.parts[2 * (int64_t)s * a.channels + c] = 0.f;
+        for (int32_t g = threadIdx.x; g < a.groups; g += blockDim.x) { a.mean[(int64_t)s * a.groups + g] = 0.f; a.rstd[(int64_t)s * a.groups + g] = 0.f; }
     }
 }
 
 // what a translation unit of its own per row type launches
 struct RowLaunch { int vec, nv; bool general, backward; int grid; RowShape shape; };
-struct TileLaunch { int vec; bool backward; int64_t grid; };
+struct TileLaunch { int vec, sums_vec; bool backward; };
 template <typename T> void launch_dropout(int vec, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t rows, int32_t channels, const DropArgs& d, int grid, cudaStream_t st);
 template <typename T> void launch_rows(const RowLaunch& l, const NormArgs& a, cudaStream_t st);
 template <typename T> void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st);

@@ -624,7 +624,7 @@ int main() {
             }
             plan_tiles(&s, 148, backward, *v, &p, &a);
             NEED(p.bytes <= have);
-            const int64_t pair = 2 * 4 * (int64_t)s.channels;
+            const int64_t pair = 2 * 4 * (int64_t)s.groups, channels = 2 * 4 * (int64_t)s.channels;
             int64_t tile = 0, fans_end = 0;
             for (int64_t q = 0; q < n; ++q) {
                 const int64_t len = s.sample_offsets ? s.sample_offsets[q + 1] - s.sample_offsets[q] : s.rows_per_sample;
@@ -634,13 +634,13 @@ int main() {
                 tile += tiles;
                 NEED(!a.equal || tiles == a.tiles_per_sample);
             }
+            NEED(tile == a.tiles && tile * std::max(a.sums.chunks, a.results.chunks) < 1ll << 31 && a.tile_rows > 0);
             NEED(p.at_fan_count + 4 * fans_end <= p.at_sample_count && p.at_fan_parts + fans_end * pair <= p.at_group_parts);
-            NEED(p.at_sample_count + 4 * n <= p.cleared && p.at_tile_parts + tile * pair <= p.at_fan_parts);
-            NEED(!backward || (p.n_parts == n && p.at_group_parts + 8 * n * s.groups <= p.at_parts && p.at_parts + n * pair <= p.at_slices && p.at_slices + kParamSlices * pair <= p.bytes));
-            NEED(tile * a.chunks < 1ll << 30 && (int64_t)a.tile_rows > 0);
-            NEED(p.window_tile.front() == 0 && p.window_tile.back() == tile);
-            for (size_t q = 0; q + 1 < p.window_tile.size(); ++q) NEED(p.window_tile[q + 1] > p.window_tile[q]);
-            NEED((int64_t)s.channels <= (int64_t)a.chunks * (*v << a.tx) && a.tx <= 8);
+            NEED(p.at_sample_count + 4 * n <= p.cleared && p.at_tile_parts + tile * a.sums.chunks * pair <= p.at_fan_parts);
+            NEED(!backward || (p.n_parts == tile && p.at_group_parts + n * pair <= p.at_parts && p.at_parts + tile * channels <= p.at_slices && p.at_slices + kParamSlices * channels <= p.bytes));
+            NEED((int64_t)s.channels <= (int64_t)a.sums.chunks * a.run && (int64_t)a.run * (a.sums.chunks - 1) < s.channels && a.run <= p.sums_vec * 256 && a.run <= (p.sums_vec << a.sums.tx));
+            NEED((int64_t)s.channels <= (int64_t)a.results.chunks * (*v << a.results.tx) && a.results.tx <= 8 && a.sums.tx <= 8);
+            NEED(s.channels % p.sums_vec == 0 && (a.sums.chunks == 1 || a.run % p.sums_vec == 0));
         }
     }
     return 0;
