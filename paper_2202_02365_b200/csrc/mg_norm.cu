@@ -5,31 +5,34 @@
 
 namespace {
 
-// Sums of `n` parts ([n][columns]) by column: 32 columns a block, 8 threads to a column; blockIdx.y: a slice of the parts.  In the last step the
+// Sums of `n` parts ([n][columns]) by column: 32 columns a block, 32 threads to a column; blockIdx.y: a slice of the parts.  In the last step the
 // columns are the weight's gradients, then the bias's.
-__global__ void __launch_bounds__(kNormThreads) k_norm_params(const float* parts, int64_t n, int64_t columns, float* out, float* d_weight, float* d_bias) {
-    __shared__ float part[kNormWarps][32];
+constexpr int kParamThreads = 1024, kParamParts = 1024;   // (more parts are added up in two steps)
+__global__ void __launch_bounds__(kParamThreads) k_norm_params(const float* parts, int64_t n, int64_t columns, float* out, float* d_weight, float* d_bias) {
+    constexpr int W = kParamThreads / 32, U = 8;
+    __shared__ float part[W][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + lane, lo = n * blockIdx.y / gridDim.y, hi = n * (blockIdx.y + 1) / gridDim.y;
+    const int64_t c0 = (int64_t)blockIdx.x * 32, c = c0 + lane, lo = n * blockIdx.y / gridDim.y, hi = n * (blockIdx.y + 1) / gridDim.y;
     float s = 0.f;
-    if (c < columns) {
-        int64_t i = lo + warp;
-        for (; i + 7 * kNormWarps < hi; i += 8 * kNormWarps) {
-            float v[8];
+    if (c < columns)
+        for (int64_t i = lo + warp; i < hi; i += U * W) {
+            float v[U];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = __ldcg(parts + (i + k * kNormWarps) * columns + c);
+            for (int k = 0; k < U; ++k) v[k] = i + k * W < hi ? __ldcg(parts + (i + k * W) * columns + c) : 0.f;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s += v[k];
+            for (int k = 0; k < U; ++k) s += v[k];
         }
-        for (; i < hi; i += kNormWarps) s += __ldcg(parts + i * columns + c);
-    }
     part[warp][lane] = s;
     __syncthreads();
-    if (warp || c >= columns) return;
-    for (int w = 1; w < kNormWarps; ++w) s += part[w][lane];
-    if (out) { out[blockIdx.y * columns + c] = s; return; }
-    float* to = c < columns / 2 ? d_weight : d_bias;
-    if (to) to[c < columns / 2 ? c : c - columns / 2] = s;
+    // warp w: column c0 + w
+    s = part[lane][warp];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    const int64_t to = c0 + warp;
+    if (lane || to >= columns) return;
+    if (out) { out[blockIdx.y * columns + to] = s; return; }
+    float* grad = to < columns / 2 ? d_weight : d_bias;
+    if (grad) grad[to < columns / 2 ? to : to - columns / 2] = s;
 }
 
 constexpr int kSamplesPerLaunch = 480;   // (in the kernel's parameters: a host array need not outlive the call, nor a captured graph)
@@ -125,13 +128,13 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
         const unsigned blocks = (unsigned)((columns + 31) / 32);
         const float* parts = a.parts;
         int64_t n = p.n_parts;
-        if (n > 512) {   // (one step reads them with 16 blocks for 256 channels)
+        if (n > kParamParts) {
             float* slices = reinterpret_cast<float*>(ws + p.at_slices);
-            k_norm_params<<<dim3(blocks, (unsigned)kParamSlices), kNormThreads, 0, st>>>(parts, n, columns, slices, nullptr, nullptr);
+            k_norm_params<<<dim3(blocks, (unsigned)kParamSlices), kParamThreads, 0, st>>>(parts, n, columns, slices, nullptr, nullptr);
             ctx->launches++;
             parts = slices; n = kParamSlices;
         }
-        k_norm_params<<<blocks, kNormThreads, 0, st>>>(parts, n, columns, nullptr, d_weight, d_bias);
+        k_norm_params<<<blocks, kParamThreads, 0, st>>>(parts, n, columns, nullptr, d_weight, d_bias);
         ctx->launches++;
     }
     MG_CUDA(ctx, cudaGetLastError());

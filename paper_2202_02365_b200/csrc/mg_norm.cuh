@@ -151,38 +151,48 @@ __device__ __forceinline__ void act_values(int act, float (&n)[N]) {
     }
 }
 
-// d times the slope of the activation at n = hat * w + b, hat = (x - mean) * rstd.  A ReLU's slope jumps at zero: which side n lies on is
-// decided in 64 bits where 32 leave it open, so that the gradient does not go by how a sum was rounded.
-template <int N>
-__device__ __forceinline__ void act_slopes(int act, float (&d)[N], const float (&h)[N], const float (&x)[N], float mean, float rstd, const float (&w)[N],
-                                           const float (&b)[N]) {
+// d times the slope of the activation at n, which is fmaf(hat-like factor, weight-like factor, b): exact(e) has element e's in 64 bits.  A ReLU's slope
+// jumps at zero: which side n lies on is decided in 64 bits where 32 leave it open, so that the gradient does not go by how a sum was rounded.
+template <int N, typename Exact>
+__device__ __forceinline__ void act_slopes(int act, float (&d)[N], const float (&n)[N], const float (&b)[N], Exact exact) {
     if (act == ACT_RELU) {
-        float n[N];
+        uint32_t up = 0;
         bool near = false;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            // |rounding of n| < 4 * 2^-24 * (|h w| + |b|): three roundings of the product (it enters the sum unrounded), one of the sum
-            n[e] = fmaf(h[e], w[e], b[e]);
+            // |rounding of n| < 4 * 2^-24 * (|n - b| + |b|): three roundings of the product (it enters the sum unrounded), one of the sum
             near = near || fabsf(n[e]) <= 3e-7f * fmaf(2.f, fabsf(b[e]), fabsf(n[e]));
+            up |= (uint32_t)!(n[e] <= 0.f) << e;
         }
-        if (near) {   // (hardly ever; the side is what is wanted of n)
-#pragma unroll
-            for (int e = 0; e < N; ++e) n[e] = (float)(((double)x[e] - (double)mean) * (double)rstd * (double)w[e] + (double)b[e]);
+        if (near) {   // (hardly ever)
+            up = 0;
+#pragma unroll 1
+            for (int e = 0; e < N; ++e) up |= (uint32_t)!(exact(e) <= 0.0) << e;
         }
 #pragma unroll
-        for (int e = 0; e < N; ++e) d[e] = n[e] <= 0.f ? 0.f : d[e];
+        for (int e = 0; e < N; ++e) d[e] = up >> e & 1u ? d[e] : 0.f;
     } else if (act == ACT_SILU) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const float n = fmaf(h[e], w[e], b[e]), s = sigmoid(n);
-            d[e] *= s * fmaf(n, 1.f - s, 1.f);
+            const float s = sigmoid(n[e]);
+            d[e] *= s * fmaf(n[e], 1.f - s, 1.f);
         }
     } else if (act == ACT_GELU) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             float bell;
-            const float n = fmaf(h[e], w[e], b[e]), cdf = normal_cdf(n, &bell);
-            d[e] *= fmaf(n * 0.39894228040143268f, bell, cdf);
+            const float cdf = normal_cdf(n[e], &bell);
+            d[e] *= fmaf(n[e] * 0.39894228040143268f, bell, cdf);
         }
     }
+}
+
+// dropout of a vector's values
+template <int VEC>
+__device__ __forceinline__ void drop_vector(const DropArgs& d, uint64_t key, int32_t c, float (&f)[VEC]) {
+    if (!d.on) return;
+    Keep<VEC> keep;
+    keep.draw(d, key, (uint32_t)c);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f[e] = keep(d, e) ? f[e] * d.factor : 0.f;
 }

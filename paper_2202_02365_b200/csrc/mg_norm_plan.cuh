@@ -101,7 +101,7 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 constexpr int64_t kParamSlices = 64;   // of the parts that k_norm_params adds up in two steps
 constexpr int kRowsMaxChannels = 32 * kRowValues;
-constexpr int kRowBlocks = 8, kRowBlocksBackward = 4;   // blocks per SM
+constexpr int kRowBlocks = 8;   // blocks per SM, forward
 constexpr int kTileBlocks = 4, kTileBlocksBackward = 3;
 
 // Rows that are samples by themselves, `vec` values to a vector.
@@ -115,13 +115,13 @@ void plan_rows(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPla
     p->general = s->groups > 1 && (each % vec || (width & (width - 1)));
     p->shape.gshift = s->groups == 1 ? 31 : ceil_log2(std::max<int64_t>(width, 1));
     const int64_t per_block = (int64_t)kNormWarps * (32 >> p->shape.lanes);
-    p->grid = (int)std::min<int64_t>((s->rows + per_block - 1) / per_block, (int64_t)n_sms * (backward ? kRowBlocksBackward : kRowBlocks));
+    p->grid = (int)std::min<int64_t>((s->rows + per_block - 1) / per_block, (int64_t)n_sms * (!backward ? kRowBlocks : p->nv * vec <= 8 ? 3 : p->nv * vec <= 16 ? 2 : 1));   // (backward: as many as an SM holds)
     p->n_parts = backward ? p->grid : 0;
     p->at_slices = sizeof(float) * 2 * (size_t)s->channels * (size_t)p->n_parts;
     p->bytes = backward ? p->at_slices + sizeof(float) * 2 * (size_t)s->channels * kParamSlices : 0;
 }
 
-constexpr int64_t kTileBytes = 192 << 10;
+constexpr int64_t kTileBytes = 384 << 10;
 
 // Samples of several rows.  a: the geometry's part of the arguments.
 void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p, TileArgs* a) {
@@ -142,18 +142,25 @@ void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPl
     const int64_t used = equal ? s->rows : s->sample_offsets[n];
     int64_t longest = equal ? s->rows_per_sample : 0;
     if (!equal) for (int64_t i = 0; i < n; ++i) longest = std::max(longest, s->sample_offsets[i + 1] - s->sample_offsets[i]);
-    // tiles of about 192 KB, so many of them that the blocks the SMs hold together take equal turns; smaller ones where there would not be a turn
+    // tiles of about 384 KB, so many of them that the blocks the SMs hold together take equal turns; smaller ones where there would not be a turn
     // for each, larger ones where a sample had more than kFan^2
     const int64_t n_ty = kNormThreads >> a->results.tx, run_bytes = a->run * elem, chunks = a->sums.chunks;
     const int64_t held = (int64_t)n_sms * (backward ? kTileBlocksBackward : kTileBlocks), bytes = used * run_bytes * chunks;
     const int64_t turns = std::max<int64_t>(1, (bytes + held * kTileBytes / 2) / (held * kTileBytes)), spread = std::max<int64_t>(1, (used * chunks + held * turns - 1) / (held * turns));
-    const int64_t rows = std::max({round_up(spread, n_ty), round_up((longest + kFan * kFan - 1) / (kFan * kFan), n_ty), (int64_t)16});
+    const auto count = [&](int64_t rows) {
+        if (equal) return n * ((s->rows_per_sample + rows - 1) / rows);
+        int64_t tiles = 0;
+        for (int64_t i = 0; i < n; ++i) tiles += (s->sample_offsets[i + 1] - s->sample_offsets[i] + rows - 1) / rows;
+        return tiles;
+    };
+    int64_t rows = std::max({round_up(spread, n_ty), round_up((longest + kFan * kFan - 1) / (kFan * kFan), n_ty), (int64_t)16});
+    int64_t tiles = count(rows);
+    // (a tile more than the blocks' turns costs a turn)
+    for (int tries = 0; tries < 8 && tiles * chunks > held * turns; ++tries) tiles = count(rows += round_up(std::max<int64_t>(rows / 32, 1), n_ty));
     a->tile_rows = (int32_t)std::min<int64_t>(rows, 1 << 30);
     a->samples = (int32_t)n; a->equal = equal;
     a->rows_per_sample = s->rows_per_sample;
     a->tiles_per_sample = equal ? (int32_t)((s->rows_per_sample + a->tile_rows - 1) / a->tile_rows) : 0;
-    int64_t tiles = equal ? n * a->tiles_per_sample : 0;
-    if (!equal) for (int64_t i = 0; i < n; ++i) tiles += (s->sample_offsets[i + 1] - s->sample_offsets[i] + a->tile_rows - 1) / a->tile_rows;
     a->tiles = (int32_t)tiles;
     const int64_t fans = tiles / kFan + n + 1, pair = 2 * (int64_t)sizeof(float);
     size_t at = 0;

@@ -25,16 +25,16 @@ struct NormArgs {
 template <typename T, int VEC>
 __device__ __forceinline__ void grad_vector(const NormArgs& a, const Raw<T, VEC>& rx, const Raw<T, VEC>& rd, uint64_t key, int32_t c, float mean, float rstd,
                                             const float (&w)[VEC], const float (&b)[VEC], float (&h)[VEC], float (&d)[VEC]) {
-    float x[VEC];
+    float n[VEC];
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) { x[e] = rx.get(e); h[e] = (x[e] - mean) * rstd; d[e] = rd.get(e); }
-    act_slopes<VEC>(a.act, d, h, x, mean, rstd, w, b);
-    if (a.drop.on) {
-        Keep<VEC> keep;
-        keep.draw(a.drop, key, (uint32_t)c);
+    for (int e = 0; e < VEC; ++e) { h[e] = (rx.get(e) - mean) * rstd; n[e] = fmaf(h[e], w[e], b[e]); d[e] = rd.get(e); }
+    act_slopes<VEC>(a.act, d, n, b, [&](int e) {
+        float x = 0.f, we = 0.f, be = 0.f;
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) d[e] = keep(a.drop, e) ? d[e] * a.drop.factor : 0.f;
-    }
+        for (int i = 0; i < VEC; ++i) if (i == e) { x = rx.get(i); we = w[i]; be = b[i]; }
+        return ((double)x - (double)mean) * (double)rstd * (double)we + (double)be;
+    });
+    drop_vector<VEC>(a.drop, key, c, d);
 }
 
 template <typename T, int VEC>
@@ -260,12 +260,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape
 #pragma unroll
             for (int e = 0; e < VEC; ++e) f[i][e] = fmaf(f[i][e], w[e], b[e]);
             act_values<VEC>(a.act, f[i]);
-            if (a.drop.on) {
-                Keep<VEC> keep;
-                keep.draw(a.drop, key, (uint32_t)(v * VEC));
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) f[i][e] = keep(a.drop, e) ? f[i][e] * a.drop.factor : 0.f;
-            }
+            drop_vector<VEC>(a.drop, key, v * VEC, f[i]);
             raw[i].put(f[i]);
             raw[i].store(y + row * a.out_stride + v * VEC);
         }
@@ -319,11 +314,12 @@ __global__ void __launch_bounds__(kNormThreads, VEC * NV <= 8 ? 3 : 1) k_norm_ro
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const int64_t at = row * a.groups + (v * VEC + e) / a.each;
-                    const float m_e = in ? a.mean[at] : 0.f, r_e = in ? a.rstd[at] : 0.f, x1[1] = {rx[i].get(e)}, w1[1] = {w[e]}, b1[1] = {b[e]};
+                    const float m_e = in ? a.mean[at] : 0.f, r_e = in ? a.rstd[at] : 0.f, x1 = rx[i].get(e), b1[1] = {b[e]};
                     float d1[1] = {rd[i].get(e)};
-                    const float h1[1] = {(x1[0] - m_e) * r_e};
-                    act_slopes<1>(a.act, d1, h1, x1, m_e, r_e, w1, b1);
-                    h[i][e] = h1[0]; g[i][e] = d1[0];
+                    h[i][e] = (x1 - m_e) * r_e;
+                    const float n1[1] = {fmaf(h[i][e], w[e], b[e])};
+                    act_slopes<1>(a.act, d1, n1, b1, [&](int) { return ((double)x1 - (double)m_e) * (double)r_e * (double)w[e] + (double)b[e]; });
+                    g[i][e] = d1[0];
                 }
                 if (a.drop.on) {
                     Keep<VEC> keep;

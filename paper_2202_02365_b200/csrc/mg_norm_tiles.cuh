@@ -93,9 +93,27 @@ __device__ __forceinline__ void merge(Pair<VEC>& a, float nb, const float (&u)[V
     }
 }
 
-// Sums of a tile: every thread has one vector of the channels and every n_ty-th row, K rows in flight; then the block's threads are brought together.
+// x - mean and dz = dropout(dy) act' of a vector, for the statistics of one sample: wr = weight rstd
+template <typename T, int VEC>
+__device__ __forceinline__ void centred_grad(const TileArgs& a, const Raw<T, VEC>& rx, const Raw<T, VEC>& rd, int64_t row, int32_t c, float mean, float rstd,
+                                             const float (&wr)[VEC], const float* sb, float (&xc)[VEC], float (&d)[VEC]) {
+    float n[VEC], b[VEC];
+    Params<VEC, 8, true>::read(sb, b);
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) { xc[e] = rx.get(e) - mean; n[e] = fmaf(xc[e], wr[e], b[e]); d[e] = rd.get(e); }
+    act_slopes<VEC>(a.act, d, n, b, [&](int e) {
+        float x = 0.f;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) if (i == e) x = rx.get(i);
+        return ((double)x - (double)mean) * (double)rstd * (double)(a.weight ? a.weight[c + e] : 1.f) + (double)(a.bias ? a.bias[c + e] : 0.f);
+    });
+    drop_vector<VEC>(a.drop, a.drop.on ? drop_key(a.drop, row) : 0, c, d);
+}
+
+// Sums of a tile: every thread has one vector of the channels and every n_ty-th row, K rows on their way; then the block's threads are brought
+// together.  Forward: the mean of K rows first, then the squares about it, then the two sets of moments as one.
 template <typename T, int VEC, bool BACKWARD, int K>
-__device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int32_t c, bool in, int ty, int n_ty, float mean, float rstd, const float* sw,
+__device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int32_t c, bool in, int ty, int n_ty, float mean, float rstd, const float* swr,
                                           const float* sb, Pair<VEC>& p) {
     p.n = 0.f;
 #pragma unroll
@@ -113,18 +131,18 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int3
                 raw[k].load(x + k * x_step);
                 if (BACKWARD) rd[k].load(d_y + k * d_step);
             }
+        x += K * x_step;
+        if (BACKWARD) d_y += K * d_step;
         if constexpr (BACKWARD) {
 #pragma unroll
             for (int k = 0; k < K; ++k) {
                 if (r + k * n_ty >= rows) break;
-                float h[VEC], d[VEC], w[VEC], b[VEC];
-                Params<VEC, 8, true>::read(sw, w);
-                Params<VEC, 8, true>::read(sb, b);
-                grad_vector<T, VEC>(a, raw[k], rd[k], a.drop.on ? drop_key(a.drop, t.row0 + r + k * n_ty) : 0, c, mean, rstd, w, b, h, d);
+                float xc[VEC], d[VEC], wr[VEC];
+                Params<VEC, 8, true>::read(swr, wr);
+                centred_grad<T, VEC>(a, raw[k], rd[k], t.row0 + r + k * n_ty, c, mean, rstd, wr, sb, xc, d);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) { p.u[e] = fmaf(d[e], h[e], p.u[e]); p.v[e] += d[e]; }
+                for (int e = 0; e < VEC; ++e) { p.u[e] = fmaf(d[e], xc[e], p.u[e]); p.v[e] += d[e]; }
             }
-            d_y += K * d_step;
         } else {
             float u[VEC], v[VEC];
             if (r + (K - 1) * n_ty < rows) {
@@ -148,7 +166,10 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int3
                 }
             }
         }
-        x += K * x_step;
+    }
+    if (BACKWARD) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) p.u[e] *= rstd;
     }
 }
 
@@ -333,10 +354,12 @@ __device__ __forceinline__ void load_params(const float* p, int32_t c, float wit
     for (int e = 0; e < VEC; ++e) o[e] = p ? p[c + e] : without;
 }
 
-// weight and bias of a block's run of channels, for the gradient: in shared memory, so that more blocks fit an SM's registers
-template <int VEC>
-__device__ __forceinline__ void share_params(const TileArgs& a, float* sw, float* sb, int32_t c0, int32_t n) {
-    for (int i = threadIdx.x; i < n; i += kNormThreads) { sw[i] = a.weight ? a.weight[c0 + i] : 1.f; sb[i] = a.bias ? a.bias[c0 + i] : 0.f; }
+// weight rstd and bias of a block's run of channels, for the gradient: in shared memory, so that more blocks fit an SM's registers
+__device__ __forceinline__ void share_params(const TileArgs& a, const Tile& t, float* swr, float* sb, int32_t c0, int32_t n) {
+    for (int i = threadIdx.x; i < n; i += kNormThreads) {
+        swr[i] = (a.weight ? a.weight[c0 + i] : 1.f) * a.rstd[(int64_t)t.sample * a.groups + (c0 + i) / a.each];
+        sb[i] = a.bias ? a.bias[c0 + i] : 0.f;
+    }
     __syncthreads();
 }
 
@@ -355,7 +378,7 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_sums(const __grid_c
     if (BACKWARD) {
         const int64_t stat = (int64_t)t.sample * a.groups + (in ? c / a.each : 0);
         mean = a.mean[stat]; rstd = a.rstd[stat];
-        share_params<VEC>(a, sw, sb, c0, c1 - c0);
+        share_params(a, t, sw, sb, c0, c1 - c0);
     }
     Pair<VEC> p;
     tile_sums<T, VEC, BACKWARD, K>(a, t, c, in, ty, n_ty, mean, rstd, sw + tx * VEC, sb + tx * VEC, p);
@@ -375,7 +398,10 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __gri
     const int32_t from_last = (int32_t)blockIdx.x / a.results.chunks, c0 = ((int32_t)blockIdx.x - from_last * a.results.chunks) * (VEC << a.results.tx), c = c0 + tx * VEC;
     Tile t;
     locate_tile(a, a.tiles - 1 - from_last, &t);
-    if (BACKWARD) share_params<VEC>(a, sw, sb, c0, min(VEC << a.results.tx, a.channels - c0));
+    const T* x = static_cast<const T*>(a.x) + (t.row0 + ty) * a.x_stride + c;
+    const T* d_y = static_cast<const T*>(a.d_y) + (BACKWARD ? (t.row0 + ty) * a.d_y_stride + c : 0);
+    const int32_t rows = (int32_t)(t.row1 - t.row0);
+    if (BACKWARD) share_params(a, t, sw, sb, c0, min(VEC << a.results.tx, a.channels - c0));
     if (c >= a.channels) return;
     const int32_t group = c / a.each;
     const float mean = a.mean[(int64_t)t.sample * a.groups + group], rstd = a.rstd[(int64_t)t.sample * a.groups + group];
@@ -389,10 +415,8 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __gri
         for (int e = 0; e < VEC; ++e) w[e] *= rstd;
     }
     const int64_t x_step = (int64_t)n_ty * a.x_stride, d_step = (int64_t)n_ty * a.d_y_stride, out_step = (int64_t)n_ty * a.out_stride;
-    const T* x = static_cast<const T*>(a.x) + (t.row0 + ty) * a.x_stride + c;
-    const T* d_y = static_cast<const T*>(a.d_y) + (BACKWARD ? (t.row0 + ty) * a.d_y_stride + c : 0);
     T* out = static_cast<T*>(a.out) + (t.row0 + ty) * a.out_stride + c;
-    const int32_t rows = (int32_t)(t.row1 - t.row0);
+    const float k1 = -s1 * rstd, k2 = -s2 * rstd * rstd;
     for (int32_t r = ty; r < rows; r += U * n_ty) {
         Raw<T, VEC> raw[U], rd[BACKWARD ? U : 1];
 #pragma unroll
@@ -404,25 +428,19 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __gri
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             if (r + k * n_ty >= rows) break;
-            const uint64_t key = a.drop.on ? drop_key(a.drop, t.row0 + r + k * n_ty) : 0;
+            const int64_t row = t.row0 + r + k * n_ty;
             float f[VEC];
-            if constexpr (BACKWARD) {
-                float h[VEC];
+            if constexpr (BACKWARD) {   // rstd (dz w - mean(dz w) - hat mean(dz w hat))
+                float xc[VEC];
                 Params<VEC, 8, true>::read(sw + tx * VEC, w);
-                Params<VEC, 8, true>::read(sb + tx * VEC, b);
-                grad_vector<T, VEC>(a, raw[k], rd[k], key, c, mean, rstd, w, b, h, f);
+                centred_grad<T, VEC>(a, raw[k], rd[k], row, c, mean, rstd, w, sb + tx * VEC, xc, f);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) f[e] = rstd * fmaf(-h[e], s2, fmaf(f[e], w[e], -s1));
+                for (int e = 0; e < VEC; ++e) f[e] = fmaf(f[e], w[e], fmaf(xc[e], k2, k1));
             } else {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f[e] = fmaf(raw[k].get(e) - mean, w[e], b[e]);
                 act_values<VEC>(a.act, f);
-                if (a.drop.on) {
-                    Keep<VEC> keep;
-                    keep.draw(a.drop, key, (uint32_t)c);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) f[e] = keep(a.drop, e) ? f[e] * a.drop.factor : 0.f;
-                }
+                drop_vector<VEC>(a.drop, a.drop.on ? drop_key(a.drop, row) : 0, c, f);
             }
             raw[k].put(f);
             raw[k].store(out + k * out_step);
