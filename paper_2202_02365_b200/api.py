@@ -82,6 +82,12 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         _lib = C.CDLL(path)
         _lib.mg_last_error.restype = C.c_char_p
         _lib.mg_kernel_launches.restype = C.c_int64
+        # (declared, numbers are converted on the way: half the time of wrapping each)
+        p, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+        _lib.mg_dropout.argtypes = [p, p, i64, p, i64, C.c_int, i64, i32, p, p]
+        _lib.mg_group_norm_workspace.argtypes = [p, p, C.c_int, p]
+        _lib.mg_group_norm.argtypes = [p, p, p, i64, p, i64, p, p, p, C.c_size_t, p]
+        _lib.mg_group_norm_backward.argtypes = [p, p, p, i64, p, i64, p, p, p, i64, p, p, p, C.c_size_t, p]
     return _lib
 
 
@@ -690,8 +696,8 @@ class Context:
         channels = x.shape[-1]
         rows = x.numel() // channels if channels else 0
         spec = drop._spec(rows, self.device)
-        self._check(self.lib.mg_dropout(self.handle, _ptr(x), C.c_int64(x_stride), _ptr(out), C.c_int64(out_stride), C.c_int(ROW_TYPES[x.dtype]),
-                                        C.c_int64(rows), C.c_int32(channels), C.byref(spec), _raw_stream(self.device)))
+        self._check(self.lib.mg_dropout(self.handle, x.data_ptr(), x_stride, out.data_ptr(), out_stride, ROW_TYPES[x.dtype], rows, channels, C.byref(spec),
+                                        torch._C._cuda_getCurrentRawStream(self.device.index)))
         return out
 
     def dropout_backward(self, d_y: torch.Tensor, drop: Dropout, out: torch.Tensor | None = None) -> torch.Tensor:
@@ -699,32 +705,34 @@ class Context:
         return self.dropout(d_y, drop, out)
 
     def _norm_spec(self, x, groups, weight, bias, sample_offsets, eps, activation, dropout):
-        channels = x.shape[-1]
+        """The library's description of the call, the number of samples and where the last ends (None: at the last row), and what must live until the
+        call is made."""
+        shape = x.shape
+        channels = shape[-1]
         rows = x.numel() // channels if channels else 0
         for p in (weight, bias):
             assert p is None or (p.device == self.device and p.dtype == torch.float32 and p.is_contiguous() and p.numel() == channels), \
                 "weight, bias: a contiguous float32 value per channel"
-        offsets = None
+        offsets = end = None
         if sample_offsets is not None:
-            assert x.dim() == 2, "sample_offsets cut the rows of a matrix"
+            assert len(shape) == 2, "sample_offsets cut the rows of a matrix"
             offsets = _host(sample_offsets, torch.int64)
             samples = offsets.numel() - 1
+            end = int(offsets[-1]) if samples >= 0 else 0
         else:
-            per = 1
-            for n in x.shape[1:-1]:
-                per *= n
-            samples = x.shape[0] if per else 0
+            samples = shape[0] if rows or len(shape) == 2 else 0
         drop = dropout._spec(rows, self.device) if dropout is not None else None
         spec = NormSpec(rows, channels, groups, ROW_TYPES[x.dtype], ACTIVATIONS[activation], eps, samples if offsets is not None else 0,
                         offsets.data_ptr() if offsets is not None else None, 1 if offsets is not None or not samples else rows // samples,
                         weight.data_ptr() if weight is not None else None, bias.data_ptr() if bias is not None else None,
                         C.addressof(drop) if drop is not None else None)
-        return spec, samples, rows if offsets is None else offsets, drop
+        return spec, samples, end, (offsets, drop)
 
     def _norm_workspace(self, spec, backward):
         need = C.c_size_t(0)
-        self._check(self.lib.mg_group_norm_workspace(self.handle, C.byref(spec), C.c_int(backward), C.byref(need)))
-        return torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None, need
+        self._check(self.lib.mg_group_norm_workspace(self.handle, C.byref(spec), backward, C.byref(need)))
+        n = need.value
+        return (torch.empty(n, dtype=torch.uint8, device=self.device) if n else None), n
 
     def group_norm(self, x: torch.Tensor, groups: int, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None, sample_offsets=None,
                    eps: float = 1e-5, activation: str = "none", dropout: Dropout | None = None, out: torch.Tensor | None = None):
@@ -733,36 +741,35 @@ class Context:
         other, mini-batches of a packed layer, say; or x is [samples, ..., channels].  activation: "none", "relu", "silu" or "gelu".  Rows
         behind the last sample stay as they are in `out`, and are zero in a new tensor."""
         x, x_stride = _matrix(x, self.device)
-        spec, samples, rows, drop = self._norm_spec(x, groups, weight, bias, sample_offsets, eps, activation, dropout)
+        spec, samples, end, held = self._norm_spec(x, groups, weight, bias, sample_offsets, eps, activation, dropout)
+        work, need = self._norm_workspace(spec, 0)
         new = out is None
         out, out_stride = _result(out, x)
-        mean = torch.empty((2, samples, groups), dtype=torch.float32, device=self.device)
-        mean, rstd = mean[0], mean[1]
-        work, need = self._norm_workspace(spec, 0)
-        self._check(self.lib.mg_group_norm(self.handle, C.byref(spec), _ptr(x), C.c_int64(x_stride), _ptr(out), C.c_int64(out_stride), _ptr(mean), _ptr(rstd),
-                                           _ptr(work), need, _raw_stream(self.device)))
-        if new and sample_offsets is not None and int(rows[-1]) < x.shape[0]:
-            out[int(rows[-1]):].zero_()
+        mean, rstd = torch.empty((2, samples, groups), dtype=torch.float32, device=self.device).unbind(0)
+        self._check(self.lib.mg_group_norm(self.handle, C.byref(spec), x.data_ptr(), x_stride, out.data_ptr(), out_stride, mean.data_ptr(), rstd.data_ptr(),
+                                           work.data_ptr() if need else None, need, torch._C._cuda_getCurrentRawStream(self.device.index)))
+        if new and end is not None and end < x.shape[0]:
+            out[end:].zero_()
         return out, mean, rstd
 
     def group_norm_backward(self, d_y: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, groups: int, weight: torch.Tensor | None = None,
                             bias: torch.Tensor | None = None, sample_offsets=None, activation: str = "none", dropout: Dropout | None = None,
                             out: torch.Tensor | None = None):
         """Gradients of group_norm from its output's: of x, and of weight and bias (as if they were ones and zeros where they are None).
-        x, mean, rstd and the rest as in the forward call; out may be d_y."""
+        x, mean, rstd and the rest as in the forward call; out may be d_y or x."""
         x, x_stride = _matrix(x, self.device)
         d_y, d_y_stride = _matrix(d_y, self.device, x)
-        spec, samples, rows, drop = self._norm_spec(x, groups, weight, bias, sample_offsets, 1.0, activation, dropout)
+        spec, samples, end, held = self._norm_spec(x, groups, weight, bias, sample_offsets, 1.0, activation, dropout)
         for s in (mean, rstd):
             assert s.device == self.device and s.dtype == torch.float32 and s.shape == (samples, groups), "mean, rstd: as group_norm gave them"
         mean, rstd = mean.contiguous(), rstd.contiguous()
+        work, need = self._norm_workspace(spec, 1)
         new = out is None
         out, out_stride = _result(out, x)
         d_weight, d_bias = torch.empty((2, x.shape[-1]), dtype=torch.float32, device=self.device).unbind(0)
-        work, need = self._norm_workspace(spec, 1)
-        self._check(self.lib.mg_group_norm_backward(self.handle, C.byref(spec), _ptr(x), C.c_int64(x_stride), _ptr(d_y), C.c_int64(d_y_stride), _ptr(mean),
-                                                    _ptr(rstd), _ptr(out), C.c_int64(out_stride), _ptr(d_weight), _ptr(d_bias), _ptr(work), need,
-                                                    _raw_stream(self.device)))
-        if new and sample_offsets is not None and int(rows[-1]) < x.shape[0]:
-            out[int(rows[-1]):].zero_()
+        self._check(self.lib.mg_group_norm_backward(self.handle, C.byref(spec), x.data_ptr(), x_stride, d_y.data_ptr(), d_y_stride, mean.data_ptr(),
+                                                    rstd.data_ptr(), out.data_ptr(), out_stride, d_weight.data_ptr(), d_bias.data_ptr(),
+                                                    work.data_ptr() if need else None, need, torch._C._cuda_getCurrentRawStream(self.device.index)))
+        if new and end is not None and end < x.shape[0]:
+            out[end:].zero_()
         return out, d_weight, d_bias

@@ -63,7 +63,8 @@ struct DeviceScope {   // work goes to the context's device; the caller's curren
 // both directions, arguments checked; `m`: the matrices, the output last
 int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices, bool backward, float* mean, float* rstd, float* d_weight, float* d_bias,
              const DropArgs& drop, void* workspace, size_t workspace_bytes, cudaStream_t st) {
-    if (workspace_bytes < norm_workspace(s, ctx->n_sms, backward) || (!workspace && norm_workspace(s, ctx->n_sms, backward)))
+    const size_t need = norm_workspace(s, ctx->n_sms, backward);
+    if (workspace_bytes < need || (!workspace && need))
         return mg_fail(ctx, MG_ERR_CAPACITY, "the workspace is smaller than mg_group_norm_workspace says");
     DeviceScope on(ctx->device);
     MG_CUDA(ctx, on.err);
@@ -92,7 +93,7 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
         a.fan_parts = reinterpret_cast<float*>(ws + p.at_fan_parts);
         a.group_parts = reinterpret_cast<float*>(ws + p.at_group_parts);
         a.parts = params ? reinterpret_cast<float*>(ws + p.at_parts) : nullptr;
-        MG_CUDA(ctx, cudaMemsetAsync(ws, 0, p.cleared, st));
+        if (p.cleared) MG_CUDA(ctx, cudaMemsetAsync(ws, 0, p.cleared, st));
         bool empty = false;
         if (!a.equal) {
             int2* table = reinterpret_cast<int2*>(ws + p.at_table);
@@ -113,14 +114,14 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
             }
             if (a.samples > kInlineSamples) a.table = table;
         }
-        if (empty && !backward) {
+        if (empty && !backward && !p.block_grid) {
             k_norm_empty<<<std::min(a.samples, ctx->n_sms), 256, 0, st>>>(a);
             ctx->launches++;
         }
-        if (a.tiles > 0) {
-            const TileLaunch l{p.vec, p.sums_vec, backward};
+        if (a.tiles > 0 || p.block_grid) {
+            const TileLaunch l{p.vec, p.sums_vec, backward, p.block_grid};
             MG_BY_TYPE(s->dtype, launch_tiles<T>(l, a, st));
-            ctx->launches += 2;
+            ctx->launches += p.block_grid ? 1 : 2;
         }
     }
     if (backward && params) {

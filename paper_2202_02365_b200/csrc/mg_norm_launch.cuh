@@ -64,9 +64,22 @@ void launch_results(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
     else k_norm_results<T, VEC, false, wide ? 2 : 4, 4><<<grid, kNormThreads, 0, st>>>(a);
 }
 
+template <typename T, int VEC>
+void launch_block(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
+    if (l.backward) k_norm_block<T, VEC, true><<<l.block_grid, kNormThreads, 0, st>>>(a);
+    else k_norm_block<T, VEC, false><<<l.block_grid, kNormThreads, 0, st>>>(a);
+}
+
 template <typename T>
 void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
     constexpr int kTwo = sizeof(T) == 2 ? 2 : 1;
+    if (l.block_grid) {
+        if (l.vec == 8) launch_block<T, 8>(l, a, st);
+        else if (l.vec == 4) launch_block<T, 4>(l, a, st);
+        else if (l.vec == kTwo && kTwo == 2) launch_block<T, kTwo>(l, a, st);
+        else launch_block<T, 1>(l, a, st);
+        return;
+    }
     if (l.sums_vec == 8) launch_sums<T, 8>(l, a, st);
     else if (l.sums_vec == 4) launch_sums<T, 4>(l, a, st);
     else if (l.sums_vec == kTwo && kTwo == 2) launch_sums<T, kTwo>(l, a, st);

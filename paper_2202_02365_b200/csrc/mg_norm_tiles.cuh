@@ -239,9 +239,9 @@ __device__ __forceinline__ int group_threads(int groups, int threads) {
 // channels that a run [c0, c1) and a group have in common
 __device__ __forceinline__ int32_t shared_channels(const TileArgs& a, int32_t g, int32_t c0, int32_t c1) { return max(0, min(c1, (g + 1) * a.each) - max(c0, g * a.each)); }
 
-// a run's groups from its channels
-template <bool BACKWARD>
-__device__ __forceinline__ void run_groups(const TileArgs& a, const float* su, const float* sv, int32_t c0, int32_t c1, float rows, float* out) {
+// a run's groups from its channels, to put(g, u, v): mean and squares about it, or sums of dz w hat and dz w
+template <bool BACKWARD, typename Put>
+__device__ __forceinline__ void run_groups(const TileArgs& a, const float* su, const float* sv, int32_t c0, int32_t c1, float rows, Put put) {
     const int32_t g_lo = c0 / a.each, n_g = (c1 - 1) / a.each - g_lo + 1;
     const int per = group_threads(n_g, kNormThreads), sub = threadIdx.x % per;
     for (int32_t q = 0; q < n_g; q += kNormThreads / per) {   // (all threads of a warp go round together)
@@ -259,7 +259,7 @@ __device__ __forceinline__ void run_groups(const TileArgs& a, const float* su, c
             for (int32_t c = lo + sub; c < hi; c += per) { const float d = su[c - c0] - u; v += fmaf(d * rows, d, sv[c - c0]); }
             for (int o = 1; o < per; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
         }
-        if (sub == 0 && lo < hi) { __stcg(out + g, u); __stcg(out + a.groups + g, v); }
+        if (sub == 0 && lo < hi) put(g, u, v);
     }
 }
 
@@ -387,35 +387,20 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_sums(const __grid_c
         float* to = a.parts + 2 * (int64_t)tile * a.channels + c0;
         for (int i = threadIdx.x; i < c1 - c0; i += kNormThreads) { to[i] = su[i]; to[a.channels + i] = sv[i]; }
     }
-    run_groups<BACKWARD>(a, su, sv, c0, c1, (float)(t.row1 - t.row0), a.tile_parts + 2 * ((int64_t)tile * a.sums.chunks + chunk) * a.groups);
+    float* part = a.tile_parts + 2 * ((int64_t)tile * a.sums.chunks + chunk) * a.groups;
+    run_groups<BACKWARD>(a, su, sv, c0, c1, (float)(t.row1 - t.row0), [&](int32_t g, float u, float v) { __stcg(part + g, u); __stcg(part + a.groups + g, v); });
     arrive<BACKWARD>(a, t, &sh_last);
 }
 
-template <typename T, int VEC, bool BACKWARD, int U, int MINB>
-__global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __grid_constant__ TileArgs a) {
-    __shared__ __align__(16) float sw[BACKWARD ? kNormThreads * VEC : 4], sb[BACKWARD ? kNormThreads * VEC : 4];
-    const int tx = threadIdx.x & ((1 << a.results.tx) - 1), ty = threadIdx.x >> a.results.tx, n_ty = kNormThreads >> a.results.tx;
-    const int32_t from_last = (int32_t)blockIdx.x / a.results.chunks, c0 = ((int32_t)blockIdx.x - from_last * a.results.chunks) * (VEC << a.results.tx), c = c0 + tx * VEC;
-    Tile t;
-    locate_tile(a, a.tiles - 1 - from_last, &t);
+// Results of a tile's rows: U rows on their way per thread.  Forward: w, b = weight rstd and bias; backward: from shared memory.
+template <typename T, int VEC, bool BACKWARD, int U>
+__device__ __forceinline__ void tile_results(const TileArgs& a, const Tile& t, int32_t c, int ty, int n_ty, float mean, float rstd, float s1, float s2,
+                                             float (&w)[VEC], float (&b)[VEC], const float* swr, const float* sb) {
+    const int64_t x_step = (int64_t)n_ty * a.x_stride, d_step = (int64_t)n_ty * a.d_y_stride, out_step = (int64_t)n_ty * a.out_stride;
     const T* x = static_cast<const T*>(a.x) + (t.row0 + ty) * a.x_stride + c;
     const T* d_y = static_cast<const T*>(a.d_y) + (BACKWARD ? (t.row0 + ty) * a.d_y_stride + c : 0);
-    const int32_t rows = (int32_t)(t.row1 - t.row0);
-    if (BACKWARD) share_params(a, t, sw, sb, c0, min(VEC << a.results.tx, a.channels - c0));
-    if (c >= a.channels) return;
-    const int32_t group = c / a.each;
-    const float mean = a.mean[(int64_t)t.sample * a.groups + group], rstd = a.rstd[(int64_t)t.sample * a.groups + group];
-    float s1 = 0.f, s2 = 0.f, w[VEC], b[VEC];
-    if (BACKWARD) {
-        s1 = a.group_parts[(int64_t)t.sample * 2 * a.groups + group]; s2 = a.group_parts[((int64_t)t.sample * 2 + 1) * a.groups + group];
-    } else {
-        load_params<VEC>(a.weight, c, 1.f, w);
-        load_params<VEC>(a.bias, c, 0.f, b);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) w[e] *= rstd;
-    }
-    const int64_t x_step = (int64_t)n_ty * a.x_stride, d_step = (int64_t)n_ty * a.d_y_stride, out_step = (int64_t)n_ty * a.out_stride;
     T* out = static_cast<T*>(a.out) + (t.row0 + ty) * a.out_stride + c;
+    const int32_t rows = (int32_t)(t.row1 - t.row0);
     const float k1 = -s1 * rstd, k2 = -s2 * rstd * rstd;
     for (int32_t r = ty; r < rows; r += U * n_ty) {
         Raw<T, VEC> raw[U], rd[BACKWARD ? U : 1];
@@ -432,8 +417,8 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __gri
             float f[VEC];
             if constexpr (BACKWARD) {   // rstd (dz w - mean(dz w) - hat mean(dz w hat))
                 float xc[VEC];
-                Params<VEC, 8, true>::read(sw + tx * VEC, w);
-                centred_grad<T, VEC>(a, raw[k], rd[k], row, c, mean, rstd, w, sb + tx * VEC, xc, f);
+                Params<VEC, 8, true>::read(swr, w);
+                centred_grad<T, VEC>(a, raw[k], rd[k], row, c, mean, rstd, w, sb, xc, f);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f[e] = fmaf(f[e], w[e], fmaf(xc[e], k2, k1));
             } else {
@@ -450,6 +435,85 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __gri
     }
 }
 
+template <typename T, int VEC, bool BACKWARD, int U, int MINB>
+__global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __grid_constant__ TileArgs a) {
+    __shared__ __align__(16) float sw[BACKWARD ? kNormThreads * VEC : 4], sb[BACKWARD ? kNormThreads * VEC : 4];
+    const int tx = threadIdx.x & ((1 << a.results.tx) - 1), ty = threadIdx.x >> a.results.tx, n_ty = kNormThreads >> a.results.tx;
+    const int32_t from_last = (int32_t)blockIdx.x / a.results.chunks, c0 = ((int32_t)blockIdx.x - from_last * a.results.chunks) * (VEC << a.results.tx), c = c0 + tx * VEC;
+    Tile t;
+    locate_tile(a, a.tiles - 1 - from_last, &t);
+    if (BACKWARD) share_params(a, t, sw, sb, c0, min(VEC << a.results.tx, a.channels - c0));
+    if (c >= a.channels) return;
+    const int32_t group = c / a.each;
+    const float mean = a.mean[(int64_t)t.sample * a.groups + group], rstd = a.rstd[(int64_t)t.sample * a.groups + group];
+    float s1 = 0.f, s2 = 0.f, w[VEC], b[VEC];
+    if (BACKWARD) {
+        s1 = a.group_parts[(int64_t)t.sample * 2 * a.groups + group]; s2 = a.group_parts[((int64_t)t.sample * 2 + 1) * a.groups + group];
+    } else {
+        load_params<VEC>(a.weight, c, 1.f, w);
+        load_params<VEC>(a.bias, c, 0.f, b);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) w[e] *= rstd;
+    }
+    tile_results<T, VEC, BACKWARD, U>(a, t, c, ty, n_ty, mean, rstd, s1, s2, w, b, sw + tx * VEC, sb + tx * VEC);
+}
+
+// Samples that a block goes through twice by itself (its second look finds them in L1 or L2): one launch, nothing handed from block to block.
+constexpr int kBlockChannels = 1024, kBlockGroups = 256;
+template <typename T, int VEC, bool BACKWARD>
+__global__ void __launch_bounds__(kNormThreads, 2) k_norm_block(const __grid_constant__ TileArgs a) {
+    __shared__ __align__(16) float su[kNormThreads * VEC], sv[kNormThreads * VEC], sw[BACKWARD ? kBlockChannels : 4], sb[BACKWARD ? kBlockChannels : 4], acc[BACKWARD ? 2 * kBlockChannels : 4];
+    __shared__ float sn[kNormThreads], g1[kBlockGroups], g2[kBlockGroups];
+    const int tx = threadIdx.x & ((1 << a.results.tx) - 1), ty = threadIdx.x >> a.results.tx, n_ty = kNormThreads >> a.results.tx;
+    const int32_t c = tx * VEC;
+    const bool in = c < a.channels;
+    const int32_t group = in ? c / a.each : 0;
+    for (int i = threadIdx.x; BACKWARD && i < 2 * a.channels; i += kNormThreads) acc[i] = 0.f;
+    for (int32_t s = blockIdx.x; s < a.samples; s += gridDim.x) {
+        Tile t;
+        t.sample = s;
+        t.row0 = a.equal ? s * a.rows_per_sample : sample_entry(a, s).x;
+        t.row1 = a.equal ? t.row0 + a.rows_per_sample : sample_entry(a, s + 1).x;
+        t.sample_rows = t.row1 - t.row0;
+        const int64_t stat = (int64_t)s * a.groups;
+        __syncthreads();   // (shared memory has been read)
+        if (t.sample_rows == 0) {
+            for (int32_t g = threadIdx.x; !BACKWARD && g < a.groups; g += kNormThreads) { a.mean[stat + g] = 0.f; a.rstd[stat + g] = 0.f; }
+            continue;
+        }
+        float mean = 0.f, rstd = 0.f, w[VEC], b[VEC];
+        if (BACKWARD) {
+            mean = a.mean[stat + group]; rstd = a.rstd[stat + group];
+            share_params(a, t, sw, sb, 0, a.channels);
+        }
+        Pair<VEC> p;
+        tile_sums<T, VEC, BACKWARD, sizeof(T) * VEC == 32 ? 2 : 4>(a, t, c, in, ty, n_ty, mean, rstd, sw + c, sb + c, p);
+        block_pairs<VEC, BACKWARD>(p, su, sv, sn, a.results.tx, a.channels);
+        for (int i = threadIdx.x; BACKWARD && i < a.channels; i += kNormThreads) { acc[i] += su[i]; acc[a.channels + i] += sv[i]; }
+        const float values = (float)t.sample_rows * (float)a.each;
+        run_groups<BACKWARD>(a, su, sv, 0, a.channels, (float)t.sample_rows, [&](int32_t g, float u, float v) {
+            if (BACKWARD) { g1[g] = v / values; g2[g] = u / values; }
+            else {
+                g1[g] = u; g2[g] = rsqrtf(v / values + a.eps);
+                a.mean[stat + g] = u; a.rstd[stat + g] = g2[g];
+            }
+        });
+        __syncthreads();
+        if (!in) continue;
+        if (!BACKWARD) {
+            mean = g1[group]; rstd = g2[group];
+            load_params<VEC>(a.weight, c, 1.f, w);
+            load_params<VEC>(a.bias, c, 0.f, b);
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) w[e] *= rstd;
+        }
+        tile_results<T, VEC, BACKWARD, sizeof(T) * VEC == 32 ? 2 : 4>(a, t, c, ty, n_ty, mean, rstd, g1[group], g2[group], w, b, sw + c, sb + c);
+    }
+    if (!BACKWARD || !a.parts) return;
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * a.channels; i += kNormThreads) a.parts[2 * (int64_t)blockIdx.x * a.channels + i] = acc[i];
+}
+
 // Samples without rows have no tiles: their statistics are zero.
 template <typename = void>
 __global__ void k_norm_empty(const __grid_constant__ TileArgs a) {
@@ -461,7 +525,7 @@ __global__ void k_norm_empty(const __grid_constant__ TileArgs a) {
 
 // what a translation unit of its own per row type launches
 struct RowLaunch { int vec, nv; bool general, backward; int grid; RowShape shape; };
-struct TileLaunch { int vec, sums_vec; bool backward; };
+struct TileLaunch { int vec, sums_vec; bool backward; int block_grid; };   // block_grid: of k_norm_block, or 0
 template <typename T> void launch_dropout(int vec, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t rows, int32_t channels, const DropArgs& d, int grid, cudaStream_t st);
 template <typename T> void launch_rows(const RowLaunch& l, const NormArgs& a, cudaStream_t st);
 template <typename T> void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st);

@@ -624,6 +624,12 @@ int main() {
             }
             plan_tiles(&s, 148, backward, *v, &p, &a);
             NEED(p.bytes <= have);
+            if (p.block_grid) {
+                NEED(s.channels <= kBlockChannels && s.groups <= kBlockGroups && s.channels <= (*v << a.results.tx) && a.results.tx <= 8 && p.block_grid <= n);
+                NEED(!backward || (p.n_parts == p.block_grid && p.at_parts + 8ull * p.n_parts * s.channels <= p.at_slices && p.at_slices + 8ull * kParamSlices * s.channels <= p.bytes));
+                NEED(s.n_samples <= kInlineSamples || p.at_table + 8ull * (s.n_samples + 1) <= p.at_parts);
+                continue;
+            }
             const int64_t pair = 2 * 4 * (int64_t)s.groups, channels = 2 * 4 * (int64_t)s.channels;
             int64_t tile = 0, fans_end = 0;
             for (int64_t q = 0; q < n; ++q) {
