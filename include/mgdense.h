@@ -374,7 +374,7 @@ int mg_layer_output(mg_ctx* ctx, const mg_model* m, mg_dense* d, int32_t layer, 
  *    Nothing in it needs clearing (every value read was written earlier in the same call), but
  *    two calls that overlap on the GPU — from two contexts or two host threads — race on it:
  *    run them one after the other.
- * Other errors as mg_forward. */
+ * Models with a norm or a dropout between their layers are refused (MG_ERR_STATE).  Other errors as mg_forward. */
 int mg_forward_noalloc(mg_ctx* ctx, const mg_model* m, mg_dense* d, float* out_dev);
 
 /* ---- link prediction: shared negatives, target union, DistMult ------------------------ */
@@ -564,6 +564,29 @@ int mg_group_norm(mg_ctx* ctx, const mg_norm_spec* spec, const void* x, int64_t 
 int mg_group_norm_backward(mg_ctx* ctx, const mg_norm_spec* spec, const void* x, int64_t x_stride, const void* d_y, int64_t d_y_stride,
                            const float* mean, const float* rstd, void* d_x, int64_t d_x_stride, float* d_weight, float* d_bias,
                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- between two layers of a model --------------------------------------------------------- */
+
+/* After every layer but the last, H^l = dropout(act(norm(Z^l))), Z^l = self . w_self + mean(neighbours) . w_nbr + bias.  By default there is no norm,
+ * no dropout, and act is a ReLU.
+ *
+ * norm = MG_NORM_ROWS: every node's row is a sample of mg_group_norm by itself; MG_NORM_BATCH: the rows of a mini-batch's layer share their
+ * statistics (in training and afterwards: there are no running ones); MG_NORM_NONE: back to the plain ReLU (the other arguments are not
+ * used).  `groups` must divide dims[1] .. dims[k-1].  weight[l], bias[l], l = 0 .. k-2: HOST [dims[l + 1]] (copied; a null array or entry stands for
+ * ones, zeros).  The statistics are of fp32 rows: a layer's output and the normalised one are both kept where mg_keep_layer_outputs asks
+ * for it, else the one takes the other's place.  mg_backward goes through the norm; mg_model_sgd_step and mg_model_adagrad_step step its weights
+ * and biases too.  A forward pass before the call can no longer be followed by mg_backward.  Errors: MG_ERR_ARG, MG_ERR_OOM. */
+#define MG_NORM_NONE 0
+#define MG_NORM_ROWS 1
+#define MG_NORM_BATCH 2
+int mg_model_set_norm(mg_model* m, int norm, int32_t groups, float eps, int activation, const float* const* weight, const float* const* bias);
+/* Dropout of every H^l, 1 <= l < k, from the next forward pass on: mg_dropout with the site l and the row keys (mini-batch << 32) + node id, so
+ * that the mask of a sample does not go by the order its nodes were found in.  p = 0: none (evaluation); a training loop gives every step a seed
+ * of its own.  mg_backward uses what its forward pass used.  Errors: MG_ERR_ARG. */
+int mg_model_set_dropout(mg_model* m, double p, uint64_t seed);
+/* DEVICE pointers to the gradients of the norm behind layer `layer` (1 .. k-1) that the last mg_backward left: [dims[layer]] each, owned by the model.
+ * Errors: MG_ERR_ARG, MG_ERR_STATE (no norm, no backward pass). */
+int mg_model_norm_grads(const mg_model* m, int32_t layer, const float** d_weight, const float** d_bias);
 
 /* ---- COMET: partition replacement for link prediction out of core (Section 5.1, Section 6) ----
  * Host-side planning only; no context, no device work.  Partition ids are the physical partitions of

@@ -10,7 +10,6 @@ import ctypes as C
 import importlib.util
 import os
 import warnings
-import weakref
 from dataclasses import dataclass
 
 import numpy as np
@@ -37,6 +36,7 @@ EXPORTS = [
     "mg_forward", "mg_set_layer_window", "mg_keep_layer_outputs", "mg_forward_host_async", "mg_wait_output", "mg_forward_noalloc", "mg_gather_h0", "mg_layer_output", "mg_lp_prepare", "mg_lp_view", "mg_lp_targets", "mg_lp_record_stream", "mg_lp_free",
     "mg_distmult_score", "mg_kernel_launches", "mg_profile", "mg_profile_read", "mg_comet_plan", "mg_comet_bias", "mg_comet_autotune", "mg_gat_model_create", "mg_gat_model_set_heads", "mg_gat_model_free", "mg_gat_forward", "mg_backward", "mg_backward_begin", "mg_backward_end", "mg_model_grads", "mg_model_sgd_step", "mg_model_adagrad_step", "mg_dense_packed_ids", "mg_apply_embedding_sgd",
     "mg_dropout", "mg_group_norm_workspace", "mg_group_norm", "mg_group_norm_backward",
+    "mg_model_set_norm", "mg_model_set_dropout", "mg_model_norm_grads",
 ]
 
 
@@ -189,10 +189,10 @@ def comet_autotune(n_nodes: int, dim: int, n_edges: int, bytes_per_edge: int, cp
 
 
 class _DeviceInts:
-    """A library-owned device buffer of n int32 values, exposed through the CUDA array interface."""
+    """A library-owned device buffer of n int32 (or other 4-byte) values, exposed through the CUDA array interface."""
 
-    def __init__(self, ptr: int, n: int):
-        self.__cuda_array_interface__ = {"shape": (n,), "typestr": "<i4", "data": (int(ptr), False), "version": 2}
+    def __init__(self, ptr: int, n: int, typestr: str = "<i4"):
+        self.__cuda_array_interface__ = {"shape": (n,), "typestr": typestr, "data": (int(ptr), False), "version": 2}
 
 
 def _from_dev(ptr, n: int, device) -> torch.Tensor:
@@ -250,11 +250,34 @@ class DenseView:
     repr_map: torch.Tensor
 
 
-class Dense:
-    def __init__(self, ctx: "Context"):
+class _Owned:
+    """A handle of the library's that belongs to a context.  The context knows the handles, not the objects: where both go in one garbage collection,
+    weak references are cleared before either is finalised, and whichever comes first frees the handle."""
+    _free = ""      # the library's call
+
+    def _own(self, ctx: "Context"):
         self.ctx = ctx
         self.handle = C.c_void_p(0)
-        ctx._children.add(self)
+        ctx._owned[id(self.handle)] = (self._free, self.handle)
+
+    def free(self):
+        if self.handle:
+            getattr(self.ctx.lib, self._free)(self.handle)
+            self.handle.value = None
+
+    def __del__(self):
+        try:
+            self.free()
+            self.ctx._owned.pop(id(self.handle), None)
+        except Exception:
+            pass
+
+
+class Dense(_Owned):
+    _free = "mg_dense_free"
+
+    def __init__(self, ctx: "Context"):
+        self._own(ctx)
 
     def counts(self):
         lib = self.ctx.lib
@@ -304,23 +327,12 @@ class Dense:
         ctx._check(copy(ctx.handle, self.handle, at, ref, _ptr(out), _ALIGN, _raw_stream(ctx.device)))
         return DenseView(*_pieces(out, room)[::2])
 
-    def free(self):
-        if self.handle:
-            self.ctx.lib.mg_dense_free(self.handle)
-            self.handle = C.c_void_p(0)
 
-    def __del__(self):
-        try:
-            self.free()
-        except Exception:
-            pass
+class Model(_Owned):
+    _free = "mg_model_free"
 
-
-class Model:
     def __init__(self, ctx: "Context", layers, precision: int = GEMM_TF32):
-        self.ctx = ctx
-        self.handle = C.c_void_p(0)
-        ctx._children.add(self)
+        self._own(ctx)
         k = len(layers)
         self.dims = [int(layers[0][0].shape[0])] + [int(l[0].shape[1]) for l in layers]
         keep = []
@@ -345,24 +357,44 @@ class Model:
         """"mean" (GraphSage's mean over the sampled neighbours, the default) or "sum"."""
         self.ctx._check(self.ctx.lib.mg_model_set_aggregator(self.handle, C.c_int({"mean": 0, "sum": 1}[aggregator])))
 
-    def free(self):
-        if self.handle:
-            self.ctx.lib.mg_model_free(self.handle)
-            self.handle = C.c_void_p(0)
+    def set_norm(self, over: str | None, groups: int = 1, weights=None, biases=None, eps: float = 1e-5, activation: str = "relu"):
+        """After every layer but the last: group norm over every node's row by itself (over="rows"), or over a mini-batch's rows ("batch"), with
+        an activation.  weights, biases: a host tensor per layer but the last, or None for ones and zeros.  over=None: the plain ReLU again."""
+        n = len(self.dims) - 2
+        keep, arrs = [], []
+        for given in (weights, biases):
+            ptrs = (C.c_void_p * max(n, 1))()
+            if given is not None:
+                assert len(given) == n, "a tensor for every layer but the last"
+                for i, p in enumerate(given):
+                    t = _host(p, torch.float32)
+                    assert t.numel() == self.dims[i + 1], "a value for every column of the layer"
+                    keep.append(t)
+                    ptrs[i] = t.data_ptr()
+            arrs.append(ptrs)
+        self.ctx._check(self.ctx.lib.mg_model_set_norm(self.handle, C.c_int({None: 0, "rows": 1, "batch": 2}[over]), C.c_int32(groups), C.c_float(eps),
+                                                       C.c_int(ACTIVATIONS[activation]), arrs[0], arrs[1]))
 
-    def __del__(self):
-        try:
-            self.free()
-        except Exception:
-            pass
+    def set_dropout(self, p: float, seed: int = 0):
+        """Dropout of every layer's output but the last's, from the next forward pass on; p = 0: none."""
+        self.ctx._check(self.ctx.lib.mg_model_set_dropout(self.handle, C.c_double(p), C.c_uint64(int(seed) & 0xFFFFFFFFFFFFFFFF)))
+
+    def norm_grads(self):
+        """(d_weight, d_bias) of the norm behind every layer but the last, as the last backward pass left them."""
+        out = []
+        for layer in range(1, len(self.dims) - 1):
+            p = [C.c_void_p(0), C.c_void_p(0)]
+            self.ctx._check(self.ctx.lib.mg_model_norm_grads(self.handle, C.c_int32(layer), C.byref(p[0]), C.byref(p[1])))
+            out.append(tuple(torch.as_tensor(_DeviceInts(q.value, self.dims[layer], "<f4"), device=self.ctx.device).clone() for q in p))
+        return out
 
 
-class GatModel:
+class GatModel(_Owned):
     """layers: list of (w [d_in, d_out], a_src [d_out], a_dst [d_out], bias [d_out]) host tensors."""
+    _free = "mg_gat_model_free"
 
     def __init__(self, ctx: "Context", layers, precision: int = GEMM_TF32, negative_slope: float = 0.2):
-        self.ctx = ctx
-        self.handle = C.c_void_p(0)
+        self._own(ctx)
         k = len(layers)
         self.dims = [int(layers[0][0].shape[0])] + [int(l[0].shape[1]) for l in layers]
         keep, arrs = [], []
@@ -381,23 +413,12 @@ class GatModel:
         """Attention heads per layer: equal column blocks of every layer's width, concatenated."""
         self.ctx._check(self.ctx.lib.mg_gat_model_set_heads(self.handle, C.c_int32(heads)))
 
-    def free(self):
-        if self.handle:
-            self.ctx.lib.mg_gat_model_free(self.handle)
-            self.handle = C.c_void_p(0)
 
-    def __del__(self):
-        try:
-            self.free()
-        except Exception:
-            pass
+class LpBatch(_Owned):
+    _free = "mg_lp_free"
 
-
-class LpBatch:
     def __init__(self, ctx: "Context"):
-        self.ctx = ctx
-        self.handle = C.c_void_p(0)
-        ctx._children.add(self)
+        self._own(ctx)
         self.n_edges = 0
         self.negs = 0
 
@@ -424,17 +445,6 @@ class LpBatch:
         self.ctx._check(self.ctx.lib.mg_lp_record_stream(self.ctx.handle, self.handle, _raw_stream(dev)))
         return arrays
 
-    def free(self):
-        if self.handle:
-            self.ctx.lib.mg_lp_free(self.handle)
-            self.handle = C.c_void_p(0)
-
-    def __del__(self):
-        try:
-            self.free()
-        except Exception:
-            pass
-
 
 class Context:
     """One device, one stream.  Mirrors the C calls one to one."""
@@ -446,7 +456,7 @@ class Context:
         self.device = torch.device("cuda", device)
         self.stream = stream
         self.handle = C.c_void_p(0)
-        self._children = weakref.WeakSet()
+        self._owned = {}      # handles that belong to the context, and what frees them
         sptr = C.c_void_p(stream.cuda_stream if stream is not None else 0)
         rc = self.lib.mg_create(C.byref(self.handle), C.c_int(device), sptr)
         if rc != MG_OK:
@@ -461,8 +471,10 @@ class Context:
 
     def close(self):
         if self.handle:
-            for child in list(self._children):
-                child.free()
+            for free, handle in list(self._owned.values()):
+                if handle:
+                    getattr(self.lib, free)(handle)
+                    handle.value = None
             self.lib.mg_destroy(self.handle)
             self.handle = C.c_void_p(0)
 

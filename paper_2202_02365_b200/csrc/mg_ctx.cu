@@ -366,6 +366,7 @@ extern "C" int mg_destroy(mg_ctx* c) {
     mg_reads_free(&c->array_reads);
     for (int i = 0; i < 2; ++i) { if (c->ev_hk_done[i]) cudaEventDestroy(c->ev_hk_done[i]); cudaFree(c->hk_buf[i]); }
     cudaFree(c->lp_ws); cudaFree(c->dm_images);
+    cudaFree(c->ws_z); cudaFree(c->ws_stats); cudaFree(c->ws_keys); cudaFree(c->ws_norm);
     for (auto& s : c->lp_spare) { cudaFree(s.block); if (s.idle) cudaEventDestroy(s.idle); mg_reads_free(&s.reads); }
     cudaStreamDestroy(c->prep_stream);
     cudaFree(c->bw_g); cudaFree(c->bw_x); cudaFree(c->bw_dx); cudaFree(c->bw_lists);

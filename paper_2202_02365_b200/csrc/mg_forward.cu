@@ -485,10 +485,206 @@ extern "C" int mg_model_free(mg_model* m) {
         cudaFree(m->w_cat[l]); cudaFree(m->w_cat_t[l]); cudaFree(m->w_pad_t[l]); cudaFree(m->bias[l]);
     }
     cudaFree(m->zeros); cudaFree(m->g_block); cudaFree(m->s_block);
+    cudaFree(m->norm_block); cudaFree(m->norm_g); cudaFree(m->norm_s);
     mg_reads_free(&m->g_reads);
     for (int l = 0; l < MG_MAX_HOPS; ++l) cudaFree(m->w_pad_h[l]);
     if (m->ctx && m->ctx->last_fwd_model == m) m->ctx->last_fwd_model = nullptr;
     delete m;
+    return MG_OK;
+}
+
+namespace {
+
+struct RowGeom {
+    int32_t B, k;
+    const int32_t* rowbase;   // [(k + 1)][B + 1]
+    const int32_t* cum;       // [B][k + 2]
+    const int32_t* node_off;  // [(k + 1)][B + 1]
+};
+
+// packed row of layer `layer` -> its mini-batch, its local row, its place in the hop-major node list
+__device__ __forceinline__ void locate_row(const RowGeom& g, int layer, int64_t row, int32_t* b_out, int32_t* local_out, int32_t* node_out) {
+    const int32_t* rb = g.rowbase + (int64_t)layer * (g.B + 1);
+    int lo = 0, hi = g.B;   // rb[lo] <= row < rb[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((int64_t)rb[mid] <= row) lo = mid; else hi = mid;
+    }
+    const int32_t local = (int32_t)(row - rb[lo]);
+    const int32_t* cum = g.cum + (int64_t)lo * (g.k + 2);
+    int j = 0;
+    while (j + 1 <= g.k && cum[j + 1] <= local) ++j;
+    *b_out = lo; *local_out = local;
+    *node_out = g.node_off[(int64_t)j * (g.B + 1) + lo] + (local - cum[j]);
+}
+
+struct RowKeyArgs {
+    RowGeom g;
+    const int32_t* nodes;
+    int32_t layer;
+    int64_t rows;
+    int64_t* keys;
+};
+
+// keys of a layer's rows for its dropout: the mini-batch above the node's id
+__global__ void __launch_bounds__(kThreads) k_row_keys(RowKeyArgs a) {
+    for (int64_t row = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; row < a.rows; row += (int64_t)gridDim.x * blockDim.x) {
+        int32_t b, local, node;
+        locate_row(a.g, a.layer, row, &b, &local, &node);
+        a.keys[row] = ((int64_t)b << 32) + a.nodes[node];
+    }
+}
+
+template <bool ADAGRAD>
+__global__ void __launch_bounds__(kThreads) k_norm_step(float* w, const float* g, float* state, int64_t n, float lr, float eps) {
+    for (int64_t i = blockIdx.x * (int64_t)blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
+        if (ADAGRAD) {
+            const float s = state[i] + g[i] * g[i];
+            state[i] = s;
+            w[i] -= lr * g[i] / (sqrtf(s) + eps);
+        } else w[i] -= lr * g[i];
+    }
+}
+
+}  // namespace
+
+// ---- between two layers ------------------------------------------------------------------
+// weight of layer l's norm (1 <= l < k) in a block of the model's; its bias stands dims[l] behind
+static int64_t norm_at(const mg_model* m, int l) {
+    int64_t at = 0;
+    for (int q = 1; q < l; ++q) at += 2 * m->dims[q];
+    return at;
+}
+
+static bool between_layers(const mg_model* m) { return m->k > 1 && (m->norm != MG_NORM_NONE || m->drop_p > 0.0); }
+
+struct BetweenPlan {   // where layer l's rows, statistics and keys start
+    int64_t z_at[MG_MAX_HOPS + 1] = {0}, stats_at[MG_MAX_HOPS + 1] = {0}, samples[MG_MAX_HOPS + 1] = {0}, keys_at[MG_MAX_HOPS + 1] = {0};
+    int64_t z = 0, stats = 0, keys = 0;
+};
+static BetweenPlan plan_between(const mg_model* m, const mg_dense* d) {
+    BetweenPlan p;
+    for (int l = 1; l < m->k; ++l) {
+        const int64_t rows = d->h_hdr.rows_total[l];
+        p.z_at[l] = p.z; p.z += (rows * m->dims[l] + 7) / 8 * 8;   // (32-byte aligned starts)
+        p.samples[l] = m->norm == MG_NORM_ROWS ? rows : d->n_batches;
+        p.stats_at[l] = p.stats; p.stats += 2 * p.samples[l] * m->norm_groups;
+        p.keys_at[l] = p.keys; p.keys += rows;
+    }
+    return p;
+}
+
+struct BetweenCall {   // layer l's norm and dropout as mg_group_norm takes them
+    mg_norm_spec norm;
+    mg_dropout_spec drop;
+    std::vector<int64_t> offsets;
+};
+static void between_call(const mg_ctx* ctx, const mg_model* m, const mg_dense* d, const BetweenPlan& p, int l, double drop_p, uint64_t seed, BetweenCall* c) {
+    c->drop = mg_dropout_spec{drop_p, seed, (uint32_t)l, 0, ctx->ws_keys + p.keys_at[l]};
+    memset(&c->norm, 0, sizeof(c->norm));
+    mg_norm_spec& s = c->norm;
+    s.rows = d->h_hdr.rows_total[l]; s.channels = m->dims[l]; s.groups = m->norm_groups; s.dtype = MG_DTYPE_F32;
+    s.activation = m->norm_act; s.eps = m->norm_eps; s.rows_per_sample = 1;
+    if (m->norm == MG_NORM_BATCH) {
+        const int32_t* rb = d->h_rowbase.data() + (size_t)l * (d->n_batches + 1);
+        c->offsets.assign(rb, rb + d->n_batches + 1);
+        s.n_samples = d->n_batches; s.sample_offsets = c->offsets.data();
+    }
+    s.weight = m->norm_block + norm_at(m, l); s.bias = s.weight + m->dims[l];
+    s.dropout = drop_p > 0.0 ? &c->drop : nullptr;
+}
+
+static int norm_scratch(mg_ctx* ctx, const mg_norm_spec* s, int backward) {
+    size_t bytes = 0;
+    if (int rc = mg_group_norm_workspace(ctx, s, backward, &bytes)) return rc;
+    if (ctx->ws_norm_bytes < bytes) return mg_ensure(ctx, &ctx->ws_norm, &ctx->ws_norm_bytes, bytes + bytes / 4);
+    return MG_OK;
+}
+
+// Z^l -> H^l behind layer l's kernels; without a norm, relu(Z^l) -> H^l in place
+static int between_forward(mg_ctx* ctx, const mg_model* m, const mg_dense* d, const BetweenPlan& p, int l, const float* z, float* h) {
+    BetweenCall c;
+    between_call(ctx, m, d, p, l, m->drop_p, m->drop_seed, &c);
+    ProfScope ps(ctx, PH_OTHER);
+    if (m->drop_p > 0.0 && c.norm.rows > 0) {
+        RowKeyArgs a{{d->n_batches, d->k, d->rowbase, d->cum, d->node_off}, d->nodes, l, c.norm.rows, ctx->ws_keys + p.keys_at[l]};
+        k_row_keys<<<mg_grid(ctx, 4), kThreads, 0, ctx->stream>>>(a);
+        ctx->launches++;
+    }
+    const int32_t width = m->dims[l];
+    if (m->norm == MG_NORM_NONE) return mg_dropout(ctx, z, width, h, width, MG_DTYPE_F32, c.norm.rows, width, &c.drop, ctx->stream);
+    if (int rc = norm_scratch(ctx, &c.norm, 0)) return rc;
+    float* mean = ctx->ws_stats + p.stats_at[l];
+    return mg_group_norm(ctx, &c.norm, z, width, h, width, mean, mean + p.samples[l] * m->norm_groups, ctx->ws_norm, ctx->ws_norm_bytes, ctx->stream);
+}
+
+// dH^l -> dZ^l in place, the norm's gradients into the model
+static int between_backward(mg_ctx* ctx, mg_model* m, const mg_dense* d, const BetweenPlan& p, int l, float* g) {
+    BetweenCall c;
+    between_call(ctx, m, d, p, l, ctx->fwd_drop_p, ctx->fwd_drop_seed, &c);
+    if (int rc = norm_scratch(ctx, &c.norm, 1)) return rc;
+    const int32_t width = m->dims[l];
+    const float* mean = ctx->ws_stats + p.stats_at[l];
+    float* d_weight = m->norm_g + norm_at(m, l);
+    return mg_group_norm_backward(ctx, &c.norm, ctx->ws_z + p.z_at[l], width, g, width, mean, mean + p.samples[l] * m->norm_groups, g, width, d_weight, d_weight + width,
+                                  ctx->ws_norm, ctx->ws_norm_bytes, ctx->stream);
+}
+
+extern "C" int mg_model_set_norm(mg_model* m, int norm, int32_t groups, float eps, int activation, const float* const* weight, const float* const* bias) {
+    if (!m) return MG_ERR_ARG;
+    mg_ctx* ctx = m->ctx;
+    if (norm != MG_NORM_NONE && norm != MG_NORM_ROWS && norm != MG_NORM_BATCH) return mg_fail(ctx, MG_ERR_ARG, "unknown norm");
+    if (norm != MG_NORM_NONE) {
+        if (!(eps > 0.f) || std::isinf(eps)) return mg_fail(ctx, MG_ERR_ARG, "eps must be positive and finite");
+        if (activation < MG_ACT_NONE || activation > MG_ACT_GELU) return mg_fail(ctx, MG_ERR_ARG, "unknown activation");
+        for (int l = 1; l < m->k; ++l)
+            if (groups < 1 || m->dims[l] % groups) return mg_fail(ctx, MG_ERR_ARG, "the groups must divide the widths of the layers");
+    }
+    MG_CUDA(ctx, cudaSetDevice(ctx->device));
+    if (ctx->last_fwd_model == m) ctx->last_fwd_model = nullptr;
+    MG_CUDA(ctx, cudaStreamSynchronize(ctx->stream));   // (the blocks below may be in use)
+    cudaFree(m->norm_s); m->norm_s = nullptr;
+    m->norm_g_valid = false;
+    m->norm = MG_NORM_NONE;
+    if (norm == MG_NORM_NONE || m->k == 1) return MG_OK;
+    const size_t elems = (size_t)norm_at(m, m->k);
+    if (!m->norm_block) {
+        if (mg_malloc(ctx, (void**)&m->norm_block, elems * sizeof(float)) != cudaSuccess || mg_malloc(ctx, (void**)&m->norm_g, elems * sizeof(float)) != cudaSuccess) {
+            cudaGetLastError();
+            cudaFree(m->norm_block); m->norm_block = nullptr;
+            return mg_fail(ctx, MG_ERR_OOM, "allocation of the norm's parameters failed");
+        }
+        m->norm_elems = elems;
+    }
+    std::vector<float> host(elems);
+    for (int l = 1; l < m->k; ++l) {
+        float* at = host.data() + norm_at(m, l);
+        for (int c = 0; c < m->dims[l]; ++c) {
+            at[c] = weight && weight[l - 1] ? weight[l - 1][c] : 1.f;
+            at[m->dims[l] + c] = bias && bias[l - 1] ? bias[l - 1][c] : 0.f;
+        }
+    }
+    MG_CUDA(ctx, cudaMemcpyAsync(m->norm_block, host.data(), elems * sizeof(float), cudaMemcpyHostToDevice, ctx->stream));
+    MG_CUDA(ctx, cudaStreamSynchronize(ctx->stream));
+    m->norm = norm; m->norm_groups = groups; m->norm_eps = eps; m->norm_act = activation;
+    return MG_OK;
+}
+
+extern "C" int mg_model_set_dropout(mg_model* m, double p, uint64_t seed) {
+    if (!m) return MG_ERR_ARG;
+    if (!(p >= 0.0 && p <= 1.0)) return mg_fail(m->ctx, MG_ERR_ARG, "the share to drop must be in [0, 1]");
+    m->drop_p = nearbyint(p * 65536.0) > 0.0 ? p : 0.0;
+    m->drop_seed = seed;
+    return MG_OK;
+}
+
+extern "C" int mg_model_norm_grads(const mg_model* m, int32_t layer, const float** d_weight, const float** d_bias) {
+    if (!m) return MG_ERR_ARG;
+    if (layer < 1 || layer >= m->k) return mg_fail(m->ctx, MG_ERR_ARG, "layer must be in [1, k)");
+    if (m->norm == MG_NORM_NONE) return mg_fail(m->ctx, MG_ERR_STATE, "the model has no norm");
+    if (!m->norm_g_valid) return mg_fail(m->ctx, MG_ERR_STATE, "mg_backward has not run");
+    if (d_weight) *d_weight = m->norm_g + norm_at(m, layer);
+    if (d_bias) *d_bias = m->norm_g + norm_at(m, layer) + m->dims[layer];
     return MG_OK;
 }
 
@@ -594,7 +790,8 @@ static int forward_pass(mg_ctx* ctx, const mg_model* m, mg_dense* d, float* out,
     const bool in_table = out_at < table_at + table_bytes && table_at < out_at + out_bytes;
     float* out2 = out_mode == OUT_DEVICE && any_fused && mg_layer_fused_supported(m->dims[k - 1], m->dims[k]) && out_at % 16 == 0 && !in_table ? out : nullptr;
     const int sub = ctx->layer_window_batches;
-    ctx->layers_kept = !(all_fused && sub > 0 && !ctx->keep_layers && k > 1);
+    const bool between = between_layers(m);
+    ctx->layers_kept = between || !(all_fused && sub > 0 && !ctx->keep_layers && k > 1);
     if (!ctx->layers_kept) {
         const int32_t* rb = d->h_rowbase.data();      // [(k+1)][B+1]
         size_t ring_off[MG_MAX_HOPS + 1] = {0}, ring_total = 0;
@@ -635,7 +832,7 @@ static int forward_pass(mg_ctx* ctx, const mg_model* m, mg_dense* d, float* out,
     // per-layer outputs H^1..H^k live in one workspace (kept for mg_layer_output).  A model may ask for fp16
     // intermediates (mg_model_set_intermediates): used when every layer runs in the fused kernel with fp16 weights
     // at hand, the widths allow 64-column output boxes, and nobody needs the fp32 layer outputs afterwards.
-    bool f16_inter = m->f16_intermediates && all_fused && !ctx->keep_layers && !m->sum_aggr && k > 1;
+    bool f16_inter = m->f16_intermediates && all_fused && !ctx->keep_layers && !m->sum_aggr && k > 1 && !between;
     for (int l = 1; l < k && f16_inter; ++l) f16_inter = m->dims[l] % 128 == 0 && m->w_pad_h[l] != nullptr;
     ctx->layers_kept = !f16_inter;
     size_t total = 0;           // bytes
@@ -675,7 +872,7 @@ static int forward_pass(mg_ctx* ctx, const mg_model* m, mg_dense* d, float* out,
         int64_t words = 0, bits = 0;
         const auto fused = [&](int l) { return ctx->keep_layers && m->precision == MG_GEMM_TF32 && mg_layer_fused_supported(m->dims[l - 1], m->dims[l]); };
         for (int l = 1; l <= k; ++l) {
-            ctx->positive_at[l] = l < k && fused(l) ? words : -1;
+            ctx->positive_at[l] = l < k && fused(l) && !between ? words : -1;   // (what lies between the layers looks at its own)
             if (ctx->positive_at[l] >= 0) words += mg_positive_words(d->h_hdr.rows_total[l], m->dims[l]);
         }
         bits = words;
@@ -698,18 +895,35 @@ static int forward_pass(mg_ctx* ctx, const mg_model* m, mg_dense* d, float* out,
         }
     }
 
+    // A norm behind the layers takes their outputs without a ReLU: kept beside the normalised ones for the backward pass, or in their place.
+    const bool norm = between && m->norm != MG_NORM_NONE;
+    BetweenPlan bp;
+    ctx->z_kept = false;
+    ctx->fwd_drop_p = m->drop_p; ctx->fwd_drop_seed = m->drop_seed;
+    if (between) {
+        bp = plan_between(m, d);
+        ctx->z_kept = norm && ctx->keep_layers;
+        if (ctx->z_kept && ctx->ws_z_elems < (size_t)bp.z && (rc = mg_ensure(ctx, &ctx->ws_z, &ctx->ws_z_elems, (size_t)(bp.z + bp.z / 4 + 8)))) return rc;
+        if (norm && ctx->ws_stats_elems < (size_t)bp.stats && (rc = mg_ensure(ctx, &ctx->ws_stats, &ctx->ws_stats_elems, (size_t)(bp.stats + bp.stats / 4)))) return rc;
+        if (m->drop_p > 0.0 && ctx->ws_keys_elems < (size_t)bp.keys && (rc = mg_ensure(ctx, &ctx->ws_keys, &ctx->ws_keys_elems, (size_t)(bp.keys + bp.keys / 4)))) return rc;
+    }
     const bool half = ctx->feat_dtype == MG_DTYPE_F16;
     for (int l = 1; l <= k; ++l) {
+        if (l > 1 && between) {   // what lies between layer l - 1 and this one
+            float* h = reinterpret_cast<float*>(ws_bytes + off[l - 1]);
+            if ((rc = between_forward(ctx, m, d, bp, l - 1, ctx->z_kept ? ctx->ws_z + bp.z_at[l - 1] : h, h))) return rc;
+        }
         const int d_in = m->dims[l - 1], d_out = m->dims[l];
         const int64_t M = d->h_hdr.rows_total[l];
-        float* h_out = l == k ? hk : reinterpret_cast<float*>(ws_bytes + off[l]);
+        float* h_out = l == k ? hk : ctx->z_kept ? ctx->ws_z + bp.z_at[l] : reinterpret_cast<float*>(ws_bytes + off[l]);
+        const bool relu = l < k && !norm;
         const float* h_prev = l > 1 ? reinterpret_cast<const float*>(ws_bytes + off[l - 1]) : nullptr;
         if (m->precision == MG_GEMM_TF32 && mg_layer_fused_supported(d_in, d_out)) {
             // gather + segment mean + both linear maps in one persistent tensor-core kernel
             {
                 ProfScope ps(ctx, l == 1 ? PH_AGG_L1 : PH_AGG_REST);
                 rc = mg_layer_fused(ctx, d, l, d_in, d_out, m->w_pad_t[l - 1], m->bias[l - 1], h_prev, h_out, l == k ? out2 : nullptr,
-                                    (l < k ? 1 : 0) | (m->sum_aggr ? 2 : 0), rows_inline ? nullptr : ctx->ws_meta + meta_at[l], 0, M, 0,
+                                    (relu ? 1 : 0) | (m->sum_aggr ? 2 : 0), rows_inline ? nullptr : ctx->ws_meta + meta_at[l], 0, M, 0,
                                     (l == 1 || f16_inter) ? m->w_pad_h[l - 1] : nullptr, f16_inter && l > 1, f16_inter && l < k,
                                     ctx->positive_at[l] >= 0 ? ctx->ws_saved + ctx->positive_at[l] : nullptr,
                                     ctx->agg_at[l] >= 0 ? reinterpret_cast<float*>(ctx->ws_saved + ctx->agg_at[l]) : nullptr);
@@ -742,7 +956,6 @@ static int forward_pass(mg_ctx* ctx, const mg_model* m, mg_dense* d, float* out,
             {
                 ProfScope ps(ctx, PH_GEMM);
                 const int64_t rows = r1 - r0;
-                const bool relu = l < k;
                 if (m->precision == MG_GEMM_FP32) {
                     dim3 grid((unsigned)((rows + 63) / 64), (unsigned)((d_out + 63) / 64));
                     if (relu) k_gemm_fp32<true><<<grid, 256, 0, st>>>(ctx->ws_x, m->w_cat[l - 1], m->bias[l - 1], h_out + r0 * d_out, rows, d_out, 2 * d_in);
@@ -858,29 +1071,6 @@ extern "C" int mg_layer_output(mg_ctx* ctx, const mg_model* m, mg_dense* d, int3
 // other sums are fp32.  Sums over rows meet by atomic adds, so low-order bits vary from run to run.
 // ---------------------------------------------------------------------------------------
 namespace {
-
-struct RowGeom {
-    int32_t B, k;
-    const int32_t* rowbase;   // [(k + 1)][B + 1]
-    const int32_t* cum;       // [B][k + 2]
-    const int32_t* node_off;  // [(k + 1)][B + 1]
-};
-
-// packed row of layer `layer` -> its mini-batch, its local row, its place in the hop-major node list
-__device__ __forceinline__ void locate_row(const RowGeom& g, int layer, int64_t row, int32_t* b_out, int32_t* local_out, int32_t* node_out) {
-    const int32_t* rb = g.rowbase + (int64_t)layer * (g.B + 1);
-    int lo = 0, hi = g.B;   // rb[lo] <= row < rb[hi]
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if ((int64_t)rb[mid] <= row) lo = mid; else hi = mid;
-    }
-    const int32_t local = (int32_t)(row - rb[lo]);
-    const int32_t* cum = g.cum + (int64_t)lo * (g.k + 2);
-    int j = 0;
-    while (j + 1 <= g.k && cum[j + 1] <= local) ++j;
-    *b_out = lo; *local_out = local;
-    *node_out = g.node_off[(int64_t)j * (g.B + 1) + lo] + (local - cum[j]);
-}
 
 // The gradient of the last layer's bias: db += column sums of g (below it, k_grad_gather sums the bias on its way).  A thread keeps
 // four columns and walks down the rows (16-byte accesses, two rows in flight, a block covers whole rows); column sums meet in shared
@@ -1129,6 +1319,7 @@ struct GatherArgs {
     const uint32_t* positive;  // which of them are above zero, mg_positive_words (RELU_BITS), else null
     float* g_in;               // [rows_in, d_in]
     float* db;                 // [d_in] bias gradient of layer - 1 (with a ReLU)
+    float scale;               // of the gradients, with a ReLU: a dropout's
 };
 
 // Bound by the latency of scattered 512-byte row reads.  A warp works on 128 columns of 16 consecutive source rows, or of one
@@ -1266,6 +1457,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_grad_gather(GatherArgs a) {
                         acc = make_float4(pos.x >> bit & 1u ? acc.x : 0.f, pos.y >> bit & 1u ? acc.y : 0.f, pos.z >> bit & 1u ? acc.z : 0.f,
                                           pos.w >> bit & 1u ? acc.w : 0.f);
                     }
+                    acc.x *= a.scale; acc.y *= a.scale; acc.z *= a.scale; acc.w *= a.scale;
                     bias.x += acc.x; bias.y += acc.y; bias.z += acc.z; bias.w += acc.w;
                 }
                 if (on) {
@@ -1322,6 +1514,8 @@ extern "C" int mg_backward_begin(mg_ctx* ctx, mg_model* m, mg_dense* d, const fl
     if (!ctx->last_hk || ctx->last_fwd_model != m || ctx->last_fwd_dense != d)
         return mg_fail(ctx, MG_ERR_STATE, "mg_backward follows mg_forward of the same model and sample");
     if (!ctx->layers_kept) return mg_fail(ctx, MG_ERR_STATE, "the forward pass did not keep its intermediate layers: call mg_keep_layer_outputs(ctx, 1) first");
+    const bool norm = m->k > 1 && m->norm != MG_NORM_NONE;
+    if (norm && !ctx->z_kept) return mg_fail(ctx, MG_ERR_STATE, "the forward pass did not keep the layers in front of the norm: call mg_keep_layer_outputs(ctx, 1) first");
     MG_CUDA(ctx, cudaSetDevice(ctx->device));
     const int k = d->k, B = d->n_batches;
     cudaStream_t st = ctx->stream;
@@ -1423,6 +1617,8 @@ extern "C" int mg_backward_begin(mg_ctx* ctx, mg_model* m, mg_dense* d, const fl
         return MG_OK;
     };
     bool turned = false;
+    const BetweenPlan bp = plan_between(m, d);
+    if (norm) MG_CUDA(ctx, cudaMemsetAsync(m->norm_g, 0, m->norm_elems * sizeof(float), st));   // (of layers without rows, too)
     for (int l = k; l >= 1; --l) {
         const int d_in = m->dims[l - 1], d_out = m->dims[l];
         const int64_t M = d->h_hdr.rows_total[l];
@@ -1481,16 +1677,27 @@ extern "C" int mg_backward_begin(mg_ctx* ctx, mg_model* m, mg_dense* d, const fl
         turned = true;
         // dX -> the gradient of the layer's input rows
         const bool bits = l > 1 && ctx->positive_at[l - 1] >= 0;
+        // (a row that a dropout without a norm has zeroed is zero, and the others' gradients grow like they did)
+        const double drop_p = l > 1 && !norm ? ctx->fwd_drop_p : 0.0;
+        const double dropped = nearbyint(drop_p * 65536.0);
         GatherArgs ga{geom, l, rows_in, ra.cnt + ra.in_at[l], ra.rev, ra.units + ra.unit_at[l], ra.n_units + l, ra.bad, ctx->bw_dx, d_in,
-                      l > 1 ? ctx->ws_h[0] + h_off[l - 1] : nullptr, bits ? ctx->ws_saved + ctx->positive_at[l - 1] : nullptr, g_in, l > 1 ? m->g_bias[l - 2] : nullptr};
+                      l > 1 ? ctx->ws_h[0] + h_off[l - 1] : nullptr, bits ? ctx->ws_saved + ctx->positive_at[l - 1] : nullptr, g_in, l > 1 ? m->g_bias[l - 2] : nullptr,
+                      dropped < 65536.0 ? (float)(65536.0 / (65536.0 - dropped)) : 0.f};
         // (groups of 16 rows, a warp per 128 columns; the units come on top, the loop takes what does not fit the grid)
         const int64_t warps = (rows_in + kGradRows - 1) / kGradRows * std::max(1, (d_in + 127) / 128);
-        const int ggrid = (int)std::max<int64_t>(1, std::min<int64_t>(mg_grid(ctx, l > 1 ? 4 : 8), (warps + kThreads / 32 - 1) / (kThreads / 32) + 16));
+        const int ggrid = (int)std::max<int64_t>(1, std::min<int64_t>(mg_grid(ctx, l > 1 && !norm ? 4 : 8), (warps + kThreads / 32 - 1) / (kThreads / 32) + 16));
         if (bits) k_grad_gather<RELU_BITS><<<ggrid, kThreads, 0, st>>>(ga);
-        else if (l > 1) k_grad_gather<RELU_ROWS><<<ggrid, kThreads, 0, st>>>(ga);
+        else if (l > 1 && !norm) k_grad_gather<RELU_ROWS><<<ggrid, kThreads, 0, st>>>(ga);
         else k_grad_gather<RELU_NONE><<<ggrid, kThreads, 0, st>>>(ga);
         ctx->launches++;
+        if (l > 1 && norm) {
+            if ((rc = between_backward(ctx, m, d, bp, l - 1, g_in))) return rc;
+            const int blocks = (int)std::min<int64_t>(ctx->n_sms, (rows_in + kThreads / (d_in / 4) - 1) / (kThreads / (d_in / 4)));
+            k_grad_bias<<<blocks, kThreads, 0, st>>>(g_in, m->g_bias[l - 2], rows_in, d_in);
+            ctx->launches++;
+        }
     }
+    if (norm) m->norm_g_valid = true;
     if (ids_dev) launch_packed_ids(ctx, d, ids_dev);
     if (!ctx->ev_backward) MG_CUDA(ctx, cudaEventCreateWithFlags(&ctx->ev_backward, cudaEventDisableTiming));
     MG_CUDA(ctx, cudaGetLastError());
@@ -1547,7 +1754,19 @@ extern "C" int mg_model_adagrad_step(mg_ctx* ctx, mg_model* m, float lr, float e
         }
         MG_CUDA(ctx, cudaMemsetAsync(m->s_block, 0, m->g_elems * sizeof(float), ctx->stream));
     }
+    if (m->norm_g_valid && !m->norm_s) {
+        if (mg_malloc(ctx, (void**)&m->norm_s, m->norm_elems * sizeof(float)) != cudaSuccess) {
+            cudaGetLastError();
+            m->norm_s = nullptr;
+            return mg_fail(ctx, MG_ERR_OOM, "optimizer state allocation failed");
+        }
+        MG_CUDA(ctx, cudaMemsetAsync(m->norm_s, 0, m->norm_elems * sizeof(float), ctx->stream));
+    }
     launch_weights<W_ADAGRAD>(ctx, m, lr, eps);
+    if (m->norm_g_valid) {
+        k_norm_step<true><<<mg_grid(ctx, 1), kThreads, 0, ctx->stream>>>(m->norm_block, m->norm_g, m->norm_s, (int64_t)m->norm_elems, lr, eps);
+        ctx->launches++;
+    }
     MG_CUDA(ctx, cudaGetLastError());
     MG_CUDA(ctx, cudaStreamSynchronize(ctx->stream));
     return MG_OK;
@@ -1558,6 +1777,10 @@ extern "C" int mg_model_sgd_step(mg_ctx* ctx, mg_model* m, float lr) {
     if (int rc = optimizer_checks(ctx, m)) return rc;
     MG_CUDA(ctx, cudaSetDevice(ctx->device));
     launch_weights<W_SGD>(ctx, m, lr, 0.f);
+    if (m->norm_g_valid) {
+        k_norm_step<false><<<mg_grid(ctx, 1), kThreads, 0, ctx->stream>>>(m->norm_block, m->norm_g, nullptr, (int64_t)m->norm_elems, lr, 0.f);
+        ctx->launches++;
+    }
     MG_CUDA(ctx, cudaGetLastError());
     MG_CUDA(ctx, cudaStreamSynchronize(ctx->stream));
     return MG_OK;
@@ -1683,6 +1906,7 @@ extern "C" int mg_forward_noalloc(mg_ctx* ctx, const mg_model* m, mg_dense* d, f
     int rc = forward_checks(ctx, m, d);
     if (rc) return rc;
     if (!out_dev) return mg_fail(ctx, MG_ERR_ARG, "null output");
+    if (between_layers(m)) return mg_fail(ctx, MG_ERR_STATE, "mg_forward_noalloc: the model has a norm or a dropout between its layers");
     if (ctx->device < 0 || ctx->device >= kNoAllocMaxDevices) return mg_fail(ctx, MG_ERR_ARG, "device ordinal above %d", kNoAllocMaxDevices - 1);
     MG_CUDA(ctx, cudaSetDevice(ctx->device));
     // once per device, with that device current: the array's name is only a host-side handle, the

@@ -180,6 +180,14 @@ struct mg_ctx {
     float* bw_g = nullptr; float* bw_x = nullptr; float* bw_dx = nullptr;   // mg_backward scratch
     size_t bw_g_elems = 0, bw_x_elems = 0, bw_dx_elems = 0;
     uint32_t* bw_lists = nullptr; size_t bw_lists_elems = 0;   // mg_backward: the turned-round entries of all layers whose dX is handed down
+    // between two layers (mg_model_set_norm, mg_model_set_dropout): what the last forward pass left for mg_backward.  The layers' outputs before their
+    // norm (where layers are kept), statistics, the rows' keys, scratch
+    float* ws_z = nullptr; size_t ws_z_elems = 0;
+    float* ws_stats = nullptr; size_t ws_stats_elems = 0;
+    int64_t* ws_keys = nullptr; size_t ws_keys_elems = 0;
+    char* ws_norm = nullptr; size_t ws_norm_bytes = 0;
+    bool z_kept = false;
+    double fwd_drop_p = 0.0; uint64_t fwd_drop_seed = 0;
     char* dm_images = nullptr; size_t dm_images_bytes = 0;   // TF32 operand images of the negatives (mg_distmult_score)
     // profiling
     bool prof_on = false;
@@ -291,6 +299,19 @@ struct mg_model {
     QueuedReads g_reads;                       // copies of the block that mg_backward_begin queued on a caller's stream
     float* s_block = nullptr;                  // Adagrad: accumulated squared gradients, laid out like them
     float* zeros = nullptr;
+    // between the layers: norm (MG_NORM_*), its parameters, their gradients and Adagrad's sums, three blocks laid out alike: layer after layer
+    // (1 .. k-1) weight, bias
+    int norm = MG_NORM_NONE;
+    int32_t norm_groups = 1;
+    float norm_eps = 0.f;
+    int norm_act = MG_ACT_RELU;
+    float* norm_block = nullptr;
+    float* norm_g = nullptr;
+    float* norm_s = nullptr;
+    size_t norm_elems = 0;
+    bool norm_g_valid = false;
+    double drop_p = 0.0;
+    uint64_t drop_seed = 0;
 };
 
 struct mg_lp_batch {
