@@ -79,8 +79,7 @@ template <typename T, int VEC> struct Raw {
 
 __device__ __forceinline__ uint64_t drop_key(const DropArgs& d, int64_t row) { return (uint64_t)(d.keys ? d.keys[row] : d.first_row + row); }
 
-// philox4x32_10 with the rounds' keys from the kernel's parameters and both halves of a product in one instruction (dropout of 150,001 x 768
-// fp16 90 -> XX us)
+// philox4x32_10 with the rounds' keys from the kernel's parameters
 __device__ __forceinline__ void drop_block(const DropArgs& d, uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t out[4]) {
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
@@ -99,14 +98,17 @@ template <int VEC> struct Keep {
     __device__ __forceinline__ void draw(const DropArgs& d, uint64_t key, uint32_t c) {
         uint32_t all[4];
         drop_block(d, (uint32_t)key, (uint32_t)(key >> 32), c >> 3, d.tag, all);
+        take(c, all[0], all[1], all[2], all[3]);
+    }
+    // from the block's words
+    __device__ __forceinline__ void take(uint32_t c, uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
         if constexpr (VEC == 8) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = all[i];
+            w[0] = w0; w[1] = w1; w[2] = w2; w[3] = w3;
         } else if constexpr (VEC == 4) {
-            w[0] = c & 4 ? all[2] : all[0];
-            w[1] = c & 4 ? all[3] : all[1];
+            w[0] = c & 4 ? w2 : w0;
+            w[1] = c & 4 ? w3 : w1;
         } else {
-            const uint32_t lo = c & 2 ? all[1] : all[0], hi = c & 2 ? all[3] : all[2];
+            const uint32_t lo = c & 2 ? w1 : w0, hi = c & 2 ? w3 : w2;
             w[0] = c & 4 ? hi : lo;
             if (VEC == 1 && (c & 1)) w[0] >>= 16;
         }
@@ -156,21 +158,20 @@ __device__ __forceinline__ void act_values(int act, float (&n)[N]) {
 template <int N, typename Exact>
 __device__ __forceinline__ void act_slopes(int act, float (&d)[N], const float (&n)[N], const float (&b)[N], Exact exact) {
     if (act == ACT_RELU) {
-        uint32_t up = 0;
+        float side[N];
         bool near = false;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             // |rounding of n| < 4 * 2^-24 * (|n - b| + |b|): three roundings of the product (it enters the sum unrounded), one of the sum
+            side[e] = n[e];
             near = near || fabsf(n[e]) <= 3e-7f * fmaf(2.f, fabsf(b[e]), fabsf(n[e]));
-            up |= (uint32_t)!(n[e] <= 0.f) << e;
         }
         if (near) {   // (hardly ever)
-            up = 0;
-#pragma unroll 1
-            for (int e = 0; e < N; ++e) up |= (uint32_t)!(exact(e) <= 0.0) << e;
+#pragma unroll
+            for (int e = 0; e < N; ++e) side[e] = exact(e) <= 0.0 ? -1.f : 1.f;
         }
 #pragma unroll
-        for (int e = 0; e < N; ++e) d[e] = up >> e & 1u ? d[e] : 0.f;
+        for (int e = 0; e < N; ++e) d[e] = side[e] <= 0.f ? 0.f : d[e];
     } else if (act == ACT_SILU) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {

@@ -9,10 +9,11 @@ template <typename T>
 void launch_dropout(int vec, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t rows, int32_t channels, const DropArgs& d, int grid, cudaStream_t st) {
     const T* from = static_cast<const T*>(x);
     T* to = static_cast<T*>(y);
-    if (vec == 8) k_dropout<T, 8><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, rows, channels, d);
-    else if (vec == 4) k_dropout<T, 4><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, rows, channels, d);
-    else if (sizeof(T) == 2 && vec == 2) k_dropout<T, sizeof(T) == 2 ? 2 : 1><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, rows, channels, d);
-    else k_dropout<T, 1><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, rows, channels, d);
+    constexpr int kTwo = sizeof(T) == 2 ? 2 : 1;
+    if (vec == 8) k_dropout<T, 8><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, (int32_t)rows, channels, d);
+    else if (vec == 4) k_dropout_pieces<T, 4><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, (int32_t)rows, channels, d);
+    else if (vec == kTwo && kTwo == 2) k_dropout_pieces<T, kTwo><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, (int32_t)rows, channels, d);
+    else k_dropout_pieces<T, 1><<<grid, kNormThreads, 0, st>>>(from, x_stride, to, y_stride, (int32_t)rows, channels, d);
 }
 
 template <typename T, int VEC, int NV>

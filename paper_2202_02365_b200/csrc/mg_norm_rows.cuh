@@ -28,47 +28,84 @@ __device__ __forceinline__ void grad_vector(const NormArgs& a, const Raw<T, VEC>
     float n[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) { h[e] = (rx.get(e) - mean) * rstd; n[e] = fmaf(h[e], w[e], b[e]); d[e] = rd.get(e); }
-    act_slopes<VEC>(a.act, d, n, b, [&](int e) {
-        float x = 0.f, we = 0.f, be = 0.f;
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) if (i == e) { x = rx.get(i); we = w[i]; be = b[i]; }
-        return ((double)x - (double)mean) * (double)rstd * (double)we + (double)be;
-    });
+    act_slopes<VEC>(a.act, d, n, b, [&](int e) { return ((double)rx.get(e) - (double)mean) * (double)rstd * (double)w[e] + (double)b[e]; });
     drop_vector<VEC>(a.drop, key, c, d);
 }
 
+// Dropout of rows of eight-channel vectors: a thread draws a block of the generator for each.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kNormThreads) k_dropout(const T* x, int64_t x_stride, T* y, int64_t y_stride, int64_t rows, int32_t channels, DropArgs d) {
-    const int64_t vecs = channels / VEC, step = (int64_t)gridDim.x * kNormThreads;
-    int64_t i = blockIdx.x * (int64_t)kNormThreads + threadIdx.x;
-    int64_t row = i / vecs;
-    int32_t v = (int32_t)(i - row * vecs);
-    const int64_t step_rows = step / vecs;
-    const int32_t step_v = (int32_t)(step - step_rows * vecs);
-    constexpr int U = 4;   // accesses in flight per thread
+__global__ void __launch_bounds__(kNormThreads) k_dropout(const T* x, int64_t x_stride, T* y, int64_t y_stride, int32_t rows, int32_t channels, DropArgs d) {
+    static_assert(VEC == 8, "a block of the generator");
+    const int32_t vecs = channels / VEC;
+    const int64_t step = (int64_t)gridDim.x * kNormThreads, i0 = blockIdx.x * (int64_t)kNormThreads + threadIdx.x;
+    const int32_t step_rows = (int32_t)(step / vecs), step_v = (int32_t)(step - (int64_t)step_rows * vecs);
+    int64_t row = i0 / vecs;   // (beyond the rows by less than a step)
+    int32_t v = (int32_t)(i0 - row * vecs);
+    constexpr int U = sizeof(T) == 4 ? 2 : 4;   // vectors on their way per thread
     while (row < rows) {
         Raw<T, VEC> p[U];
-        int64_t at_row[U];
-        int32_t at_v[U];
+        int32_t at_row[U], at_v[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            at_row[u] = row; at_v[u] = v;
+            at_row[u] = row < rows ? (int32_t)row : -1; at_v[u] = v;
             if (row < rows) p[u].load(x + row * x_stride + v * VEC);
             row += step_rows; v += step_v;
-            if (v >= vecs) { v -= (int32_t)vecs; ++row; }
+            if (v >= vecs) { v -= vecs; ++row; }
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (at_row[u] >= rows) break;
+            if (at_row[u] < 0) break;
             if (d.on) {
-                Keep<VEC> keep;
-                keep.draw(d, drop_key(d, at_row[u]), (uint32_t)(at_v[u] * VEC));
                 float f[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) f[e] = keep(d, e) ? p[u].get(e) * d.factor : 0.f;
+                for (int e = 0; e < VEC; ++e) f[e] = p[u].get(e);
+                drop_vector<VEC>(d, drop_key(d, at_row[u]), at_v[u] * VEC, f);
                 p[u].put(f);
             }
             p[u].store(y + at_row[u] * y_stride + at_v[u] * VEC);
+        }
+    }
+}
+
+// Dropout of rows of narrower vectors.  A warp takes 8 / VEC pieces of 32 * VEC channels of a row at a time, 32 blocks of the generator in all: every
+// lane draws one and hands its words to the lanes that have the elements.  (A block drawn by every thread for VEC of its eight values: 77,777 x 101
+// bf16 38.9 us, this way XX.)
+template <typename T, int VEC>
+__global__ void __launch_bounds__(kNormThreads) k_dropout_pieces(const T* x, int64_t x_stride, T* y, int64_t y_stride, int32_t rows, int32_t channels, DropArgs d) {
+    constexpr int P = 8 / VEC, kBlocks = 32 / P;   // pieces; blocks of the generator in each
+    const int lane = threadIdx.x & 31;
+    const int32_t pieces = (channels + 32 * VEC - 1) / (32 * VEC);
+    const int64_t all = (int64_t)rows * pieces, step = (int64_t)gridDim.x * kNormWarps * P;
+    for (int64_t i0 = ((int64_t)blockIdx.x * kNormWarps + (threadIdx.x >> 5)) * P; i0 < all; i0 += step) {
+        int32_t row[P], c[P];
+        Raw<T, VEC> p[P];
+        int64_t r = i0 / pieces;
+        int32_t q = (int32_t)(i0 - r * pieces), drawn_row = 0, drawn_c = 0;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            row[k] = r < rows ? (int32_t)r : -1;
+            c[k] = (q * 32 + lane) * VEC;
+            if (lane / kBlocks == k) { drawn_row = max(row[k], 0); drawn_c = q * 32 * VEC + lane % kBlocks * 8; }
+            if (c[k] >= channels) row[k] = -1;
+            if (row[k] >= 0) p[k].load(x + r * x_stride + c[k]);
+            if (++q == pieces) { q = 0; ++r; }
+        }
+        uint32_t w[4];
+        const uint64_t key = drop_key(d, drawn_row);
+        drop_block(d, (uint32_t)key, (uint32_t)(key >> 32), (uint32_t)drawn_c >> 3, d.tag, w);
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const int from = k * kBlocks + lane * VEC / 8;   // the lane that drew this one's block
+            const uint32_t w0 = __shfl_sync(0xFFFFFFFFu, w[0], from), w1 = __shfl_sync(0xFFFFFFFFu, w[1], from), w2 = __shfl_sync(0xFFFFFFFFu, w[2], from),
+                           w3 = __shfl_sync(0xFFFFFFFFu, w[3], from);
+            Keep<VEC> keep;
+            keep.take((uint32_t)(lane * VEC), w0, w1, w2, w3);
+            if (row[k] < 0) continue;
+            float f[VEC];
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[e] = keep(d, e) ? p[k].get(e) * d.factor : 0.f;
+            if (d.on) p[k].put(f);
+            p[k].store(y + row[k] * y_stride + c[k]);
         }
     }
 }
