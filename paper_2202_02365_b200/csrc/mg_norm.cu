@@ -157,7 +157,7 @@ extern "C" int mg_dropout(mg_ctx* ctx, const void* x, int64_t x_stride, void* y,
     // (vectors to a thread at a time; narrower ones in pieces of 32 lanes, 8 / vec of them to a warp)
     const int64_t per_block = vec == 8 ? 4 * kNormThreads : (int64_t)kNormWarps * (8 / vec), items = vec == 8 ? rows * (channels / vec) : rows * ((channels + 32 * vec - 1) / (32 * vec));
     const int64_t blocks = (items + per_block - 1) / per_block;
-    MG_BY_TYPE(dtype, launch_dropout<T>(vec, x, x_stride, y, y_stride, rows, channels, d, (int)std::min<int64_t>(blocks, mg_grid(ctx, 8)), (cudaStream_t)stream));
+    MG_BY_TYPE(dtype, launch_dropout<T>(vec, x, x_stride, y, y_stride, rows, channels, d, (int)std::min<int64_t>(blocks, mg_grid(ctx, vec == 8 ? 8 : 10)), (cudaStream_t)stream));
     ctx->launches++;
     MG_CUDA(ctx, cudaGetLastError());
     return MG_OK;

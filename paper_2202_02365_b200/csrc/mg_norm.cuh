@@ -98,17 +98,14 @@ template <int VEC> struct Keep {
     __device__ __forceinline__ void draw(const DropArgs& d, uint64_t key, uint32_t c) {
         uint32_t all[4];
         drop_block(d, (uint32_t)key, (uint32_t)(key >> 32), c >> 3, d.tag, all);
-        take(c, all[0], all[1], all[2], all[3]);
-    }
-    // from the block's words
-    __device__ __forceinline__ void take(uint32_t c, uint32_t w0, uint32_t w1, uint32_t w2, uint32_t w3) {
         if constexpr (VEC == 8) {
-            w[0] = w0; w[1] = w1; w[2] = w2; w[3] = w3;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = all[i];
         } else if constexpr (VEC == 4) {
-            w[0] = c & 4 ? w2 : w0;
-            w[1] = c & 4 ? w3 : w1;
+            w[0] = c & 4 ? all[2] : all[0];
+            w[1] = c & 4 ? all[3] : all[1];
         } else {
-            const uint32_t lo = c & 2 ? w1 : w0, hi = c & 2 ? w3 : w2;
+            const uint32_t lo = c & 2 ? all[1] : all[0], hi = c & 2 ? all[3] : all[2];
             w[0] = c & 4 ? hi : lo;
             if (VEC == 1 && (c & 1)) w[0] >>= 16;
         }

@@ -68,45 +68,67 @@ __global__ void __launch_bounds__(kNormThreads) k_dropout(const T* x, int64_t x_
 }
 
 // Dropout of rows of narrower vectors.  A warp takes 8 / VEC pieces of 32 * VEC channels of a row at a time, 32 blocks of the generator in all: every
-// lane draws one and hands its words to the lanes that have the elements.  (A block drawn by every thread for VEC of its eight values: 77,777 x 101
-// bf16 38.9 us, this way XX.)
+// lane draws one and leaves it in shared memory for the lanes that have the elements.
 template <typename T, int VEC>
-__global__ void __launch_bounds__(kNormThreads) k_dropout_pieces(const T* x, int64_t x_stride, T* y, int64_t y_stride, int32_t rows, int32_t channels, DropArgs d) {
-    constexpr int P = 8 / VEC, kBlocks = 32 / P;   // pieces; blocks of the generator in each
-    const int lane = threadIdx.x & 31;
-    const int32_t pieces = (channels + 32 * VEC - 1) / (32 * VEC);
-    const int64_t all = (int64_t)rows * pieces, step = (int64_t)gridDim.x * kNormWarps * P;
-    for (int64_t i0 = ((int64_t)blockIdx.x * kNormWarps + (threadIdx.x >> 5)) * P; i0 < all; i0 += step) {
-        int32_t row[P], c[P];
+__global__ void __launch_bounds__(kNormThreads, 5) k_dropout_pieces(const T* x, int64_t x_stride, T* y, int64_t y_stride, int32_t rows, int32_t channels, DropArgs d) {
+    constexpr int P = 8 / VEC, kBlocks = 32 / P, kWide = 32 * VEC;   // pieces; blocks of the generator in each; channels of one
+    __shared__ __align__(16) uint32_t words[kNormWarps][128];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t pieces = (channels + kWide - 1) / kWide;
+    const int64_t step = (int64_t)gridDim.x * kNormWarps * P, first = ((int64_t)blockIdx.x * kNormWarps + warp) * P;
+    const int32_t step_rows = (int32_t)(step / pieces), step_q = (int32_t)(step - (int64_t)step_rows * pieces);
+    int64_t row = first / pieces;   // (beyond the rows by less than a step)
+    int32_t q = (int32_t)(first - row * pieces);
+    const int64_t x_wrap = x_stride - (int64_t)pieces * kWide, y_wrap = y_stride - (int64_t)pieces * kWide;
+    while (row < rows) {
         Raw<T, VEC> p[P];
-        int64_t r = i0 / pieces;
-        int32_t q = (int32_t)(i0 - r * pieces), drawn_row = 0, drawn_c = 0;
+        uint32_t have = 0;
+        int32_t drawn_row = (int32_t)row, drawn_c = 0;
+        {
+            const T* px = x + row * x_stride + (q * 32 + lane) * VEC;
+            int32_t r = (int32_t)row, at = q;
+#pragma unroll
+            for (int k = 0; k < P; ++k) {
+                if (lane / kBlocks == k) { drawn_row = r; drawn_c = at * kWide + lane % kBlocks * 8; }
+                if (r < rows && (at * 32 + lane) * VEC < channels) { p[k].load(px); have |= 1u << k; }
+                px += kWide;
+                if (++at == pieces) { at = 0; ++r; px += x_wrap; }
+            }
+        }
+        if (d.on) {
+            uint32_t w[4];
+            const uint64_t key = drop_key(d, min(drawn_row, rows - 1));
+            drop_block(d, (uint32_t)key, (uint32_t)(key >> 32), (uint32_t)drawn_c >> 3, d.tag, w);
+            __syncwarp();
+            *reinterpret_cast<uint4*>(words[warp] + 4 * lane) = make_uint4(w[0], w[1], w[2], w[3]);
+            __syncwarp();
+        }
+        T* py = y + row * y_stride + (q * 32 + lane) * VEC;
+        int32_t at = q;
 #pragma unroll
         for (int k = 0; k < P; ++k) {
-            row[k] = r < rows ? (int32_t)r : -1;
-            c[k] = (q * 32 + lane) * VEC;
-            if (lane / kBlocks == k) { drawn_row = max(row[k], 0); drawn_c = q * 32 * VEC + lane % kBlocks * 8; }
-            if (c[k] >= channels) row[k] = -1;
-            if (row[k] >= 0) p[k].load(x + r * x_stride + c[k]);
-            if (++q == pieces) { q = 0; ++r; }
-        }
-        uint32_t w[4];
-        const uint64_t key = drop_key(d, drawn_row);
-        drop_block(d, (uint32_t)key, (uint32_t)(key >> 32), (uint32_t)drawn_c >> 3, d.tag, w);
+            if (have >> k & 1u) {
+                if (d.on) {
+                    const uint32_t* from = words[warp] + 4 * (k * kBlocks + lane * VEC / 8);
+                    Keep<VEC> keep;
+                    if constexpr (VEC == 1) keep.w[0] = reinterpret_cast<const uint16_t*>(from)[lane & 7];
+                    else if constexpr (VEC == 2) keep.w[0] = from[lane & 3];
+                    else {
+                        const uint2 v = *reinterpret_cast<const uint2*>(from + (lane & 1) * 2);
+                        keep.w[0] = v.x; keep.w[1] = v.y;
+                    }
+                    float f[VEC];
 #pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const int from = k * kBlocks + lane * VEC / 8;   // the lane that drew this one's block
-            const uint32_t w0 = __shfl_sync(0xFFFFFFFFu, w[0], from), w1 = __shfl_sync(0xFFFFFFFFu, w[1], from), w2 = __shfl_sync(0xFFFFFFFFu, w[2], from),
-                           w3 = __shfl_sync(0xFFFFFFFFu, w[3], from);
-            Keep<VEC> keep;
-            keep.take((uint32_t)(lane * VEC), w0, w1, w2, w3);
-            if (row[k] < 0) continue;
-            float f[VEC];
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] = keep(d, e) ? p[k].get(e) * d.factor : 0.f;
-            if (d.on) p[k].put(f);
-            p[k].store(y + row[k] * y_stride + c[k]);
+                    for (int e = 0; e < VEC; ++e) f[e] = keep(d, e) ? p[k].get(e) * d.factor : 0.f;
+                    p[k].put(f);
+                }
+                p[k].store(py);
+            }
+            py += kWide;
+            if (++at == pieces) { at = 0; py += y_wrap; }
         }
+        row += step_rows; q += step_q;
+        if (q >= pieces) { q -= pieces; ++row; }
     }
 }
 
