@@ -386,6 +386,7 @@ class Model(_Owned):
             p = [C.c_void_p(0), C.c_void_p(0)]
             self.ctx._check(self.ctx.lib.mg_model_norm_grads(self.handle, C.c_int32(layer), C.byref(p[0]), C.byref(p[1])))
             out.append(tuple(torch.as_tensor(_DeviceInts(q.value, self.dims[layer], "<f4"), device=self.ctx.device).clone() for q in p))
+        torch.cuda.current_stream(self.ctx.device).synchronize()   # (the next backward pass, on the context's stream, writes the model's)
         return out
 
 

@@ -185,7 +185,7 @@ extern "C" int mg_group_norm_backward(mg_ctx* ctx, const mg_norm_spec* spec, con
                                       void* workspace, size_t workspace_bytes, void* stream) {
     if (!ctx) return MG_ERR_ARG;
     DropArgs drop;
-    if (int rc = check_norm_call(ctx, spec, x, x_stride, d_y, d_y_stride, true, d_x, d_x_stride, mean, rstd, workspace, &drop)) return rc;
+    if (int rc = check_norm_call(ctx, spec, x, x_stride, d_y, d_y_stride, true, d_x, d_x_stride, mean, rstd, workspace, &drop, d_weight, d_bias)) return rc;
     const Matrix m[3] = {{"x", x, x_stride, false}, {"d_y", d_y, d_y_stride, false}, {"d_x", d_x, d_x_stride, true}};
     return run_norm(ctx, spec, m, 3, true, const_cast<float*>(mean), const_cast<float*>(rstd), d_weight, d_bias, drop, workspace, workspace_bytes, (cudaStream_t)stream);
 }

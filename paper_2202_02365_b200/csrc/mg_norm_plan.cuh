@@ -265,15 +265,16 @@ int check_dropout_call(mg_ctx* ctx, const void* x, int64_t x_stride, const void*
 }
 
 int check_norm_call(mg_ctx* ctx, const mg_norm_spec* s, const void* x, int64_t x_stride, const void* d_y, int64_t d_y_stride, bool backward,
-                    const void* out, int64_t out_stride, const float* mean, const float* rstd, const void* workspace, DropArgs* d) {
+                    const void* out, int64_t out_stride, const float* mean, const float* rstd, const void* workspace, DropArgs* d,
+                    const float* d_weight = nullptr, const float* d_bias = nullptr) {
     if (int rc = check_norm(ctx, s)) return rc;
     if (int rc = check_dropout(ctx, s->dropout, d)) return rc;
     const Matrix fwd[2] = {{"x", x, x_stride, false}, {"y", out, out_stride, true}};
     const Matrix bwd[3] = {{"x", x, x_stride, false}, {"d_y", d_y, d_y_stride, false}, {"d_x", out, out_stride, true}};
     if (int rc = check_matrices(ctx, backward ? bwd : fwd, backward ? 3 : 2, s->dtype, s->rows, s->channels)) return rc;
     if (sample_count(s) > 0 && (!mean || !rstd)) return mg_fail(ctx, MG_ERR_ARG, "null statistics");
-    for (const void* p : {(const void*)mean, (const void*)rstd, (const void*)s->weight, (const void*)s->bias})
-        if (reinterpret_cast<uintptr_t>(p) % 4) return mg_fail(ctx, MG_ERR_ARG, "statistics, weight and bias must be 4-byte aligned");
+    for (const void* p : {(const void*)mean, (const void*)rstd, (const void*)s->weight, (const void*)s->bias, (const void*)d_weight, (const void*)d_bias})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return mg_fail(ctx, MG_ERR_ARG, "statistics, weight, bias and their gradients must be 4-byte aligned");
     if (reinterpret_cast<uintptr_t>(workspace) % 16) return mg_fail(ctx, MG_ERR_ARG, "the workspace must be 16-byte aligned");
     return MG_OK;
 }

@@ -462,6 +462,64 @@ def test_captured_and_replayed(ctx, samples):
 
 
 @pytest.mark.gpu
+def test_rows_far_apart(ctx):
+    rows, stride = 10, 2 ** 28 - 8                                                  # the last ones start behind 2^31 elements
+    flat = torch.empty((rows - 1) * stride + 2 ** 20, dtype=torch.float16, device="cuda")
+    for channels in (96, 4096):
+        x = flat.as_strided((rows, channels), (stride, 1))
+        x.copy_(rows_of(rows, channels, torch.float16, 3))
+        for samples in ("rows", [rows], [4, 0, 6]):
+            check_norm(ctx, x, samples, 4, "silu", mg.Dropout(0.4, 6))
+        check_norm(ctx, x, [rows], 4, "gelu", out=flat.as_strided((rows, channels), (stride, 1), 4096 * 64))
+        keep = kept(range(rows), channels, 0.4, 6, 0)
+        y = ctx.dropout(x, mg.Dropout(0.4, 6))
+        check_dropout(y, x, keep, 0.4)
+        assert torch.equal(ctx.dropout(x, mg.Dropout(0.4, 6), out=x), y)
+
+
+@pytest.mark.gpu
+def test_more_than_two_to_the_31_elements(ctx):
+    rows, channels, groups, last, p = 4_300_000, 512, 4, 1000, 0.25
+    x = torch.empty((rows, channels), dtype=torch.float16, device="cuda").normal_(0.3, 1.0, generator=torch.Generator("cuda").manual_seed(7))
+    assert x.numel() > 2 ** 31
+    tail, first, h = x[rows - last:], rows - last, half_step(x.dtype)
+    keep = kept(range(first, rows), channels, p, 9, 1)
+    y = ctx.dropout(x, mg.Dropout(p, 9, 1))
+    check_dropout(y[first:], tail, keep, p)
+    del y
+    # rows by themselves: the last ones as in a call of their own
+    y, mean, rstd = ctx.group_norm(x, groups, activation="silu", dropout=mg.Dropout(p, 9, 1))
+    want = ctx.group_norm(tail, groups, activation="silu", dropout=mg.Dropout(p, 9, 1, first))
+    for a, b in zip((y, mean, rstd), want):
+        assert torch.equal(a[first:], b)
+    d_x, _, d_b = ctx.group_norm_backward(x, x, mean, rstd, groups, dropout=mg.Dropout(p, 9, 1), out=y)
+    assert torch.equal(d_x[first:], ctx.group_norm_backward(tail, tail, *want[1:], groups, dropout=mg.Dropout(p, 9, 1, first))[0])
+    del y, d_x
+    # one sample.  A thread merges at most 1050 rows (a sample has at most 1024 tiles, four threads share a channel's rows), then 256 threads, 32 tiles
+    # and 32 sets of those meet: chains of fewer than 2048 roundings.
+    chain = 2048
+    blocks = [(lo, min(lo + 100_000, rows)) for lo in range(0, rows, 100_000)]
+    n = rows * (channels // groups)
+    put = lambda t: t.repeat_interleave(channels // groups)  # noqa: E731
+    total = lambda f: sum(f(x[lo:hi].double()).view(hi - lo, groups, -1).sum((0, 2)) for lo, hi in blocks)  # noqa: E731
+    m = total(lambda t: t) / n
+    size, var = total(lambda t: t.abs()) / n, total(lambda t: (t - put(m)) ** 2) / n
+    y, mean, rstd = ctx.group_norm(x, groups, sample_offsets=[0, rows])
+    t_mean, w_rstd = chain * U * size, (var + 1e-5).rsqrt()
+    assert bool(((mean[0].double() - m).abs() <= t_mean).all())
+    assert bool(((rstd[0].double() - w_rstd).abs() <= w_rstd * (chain + 12) * U + 0.5 * w_rstd ** 3 * t_mean ** 2).all())
+    m, r = put(mean[0].double()), put(rstd[0].double())
+    hat = (tail.double() - m) * r
+    assert bool(((y[first:].double() - hat).abs() <= (6 * U + h * (1 + 6 * U)) * (hat.abs() + m.abs() * r) + smallest(x.dtype)).all())
+    s1, s2 = put(total(lambda t: t) / n), put(total(lambda t: t * (t - m) * r) / n)
+    a1, a2 = put(size), put(total(lambda t: (t * (t - m) * r).abs()) / n)
+    d_x = ctx.group_norm_backward(x, x, mean, rstd, groups, sample_offsets=[0, rows], out=y)[0]
+    want = r * (tail.double() - s1 - hat * s2)
+    t_x = r * (1 + h) * ((chain + 8) * U * (a1 + hat.abs() * a2) + 8 * U * (tail.double().abs() + a1 + hat.abs() * a2)) + h * want.abs() + smallest(x.dtype)
+    assert bool(((d_x[first:].double() - want).abs() <= t_x).all())
+
+
+@pytest.mark.gpu
 def test_refusals(ctx):
     x = torch.randn(12, 16, device="cuda")
     ones = torch.ones(16, device="cuda")
@@ -572,6 +630,8 @@ int main() {
     const int64_t back[3] = {0, 5, 4};
     EXPECT(MG_ERR_ARG, with([&](auto& s) { s.sample_offsets = back; s.n_samples = 2; }));
     EXPECT(MG_ERR_ARG, with([&](auto& s) { s.weight = reinterpret_cast<float*>(base + 2); }));
+    EXPECT(MG_ERR_ARG, check_norm_call(&context, &ok, base, 16, far, 16, true, far + 4096, 16, stats, stats, nullptr, &d, reinterpret_cast<float*>(base + 2)));
+    EXPECT(MG_ERR_ARG, check_norm_call(&context, &ok, base, 16, far, 16, true, far + 4096, 16, stats, stats, nullptr, &d, nullptr, reinterpret_cast<float*>(base + 1)));
     drop.p = 2.0;
     EXPECT(MG_ERR_ARG, with([&](auto& s) { s.dropout = &drop; }));
     EXPECT(MG_ERR_ARG, norm(ok, nullptr));

@@ -224,6 +224,42 @@ def test_the_plain_model_is_as_it_was():
     near(r.forward(), layers[-1][2].expand(220, 16), 1e-6)      # all of the first layer dropped: the last one's bias
 
 
+def test_gradients_of_the_norm_are_the_callers_own():
+    r = Run([16, 32, 8], [4, 3], [40])
+    r.set(how("rows", 4))
+    r.ctx.keep_layer_outputs(True)
+    r.forward()
+    d_out = r.d_out.cuda()
+    r.ctx.backward(r.model, r.dense, d_out)
+    want = [t.clone() for q in r.model.norm_grads() for t in q]
+    other = 3 * d_out
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):      # a stream that is behind
+        torch.cuda._sleep(100_000_000)
+        got = [t for q in r.model.norm_grads() for t in q]
+    r.ctx.backward(r.model, r.dense, other)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_mini_batches_without_targets():
+    for over in ("rows", "batch"):
+        r = Run([16, 32, 24, 8], [4, 3, 2], [5])
+        r.set(how(over, 4, p=0.3))
+        r.ctx.keep_layer_outputs(True)
+        for counts in ([0, 0], [0, 7, 0]):
+            ends = np.cumsum([0] + counts).tolist()
+            dense = r.ctx.sample_many(torch.arange(sum(counts), dtype=torch.int32, device="cuda"), ends, [4, 3, 2], list(range(1, len(counts) + 1)))
+            out = r.ctx.forward(r.model, dense, torch.zeros(max(1, sum(counts)), 8, device="cuda"))
+            assert bool(out.isfinite().all()) and bool(out.any()) == (sum(counts) > 0)
+            if sum(counts) == 0:
+                continue                              # (no forward pass that a backward pass could follow)
+            grads, g_h0, _ = r.ctx.backward(r.model, dense, torch.ones_like(out), want_h0_grad=True)
+            assert bool(g_h0.isfinite().all())
+            for t in [t for q in grads + r.model.norm_grads() for t in q]:
+                assert bool(t.isfinite().all()) and bool(t.any())
+
+
 def test_refusals():
     r = Run([16, 24, 8], [4, 3], [40])
     for call in (lambda: r.model.set_norm("rows", 5), lambda: r.model.set_norm("rows", 0), lambda: r.model.set_norm("batch", 2, eps=0.0), lambda: r.model.set_dropout(1.5),
