@@ -95,7 +95,7 @@ __device__ __forceinline__ void merge(Pair<VEC>& a, float nb, const float (&u)[V
 
 // x - mean and dz = dropout(dy) act' of a vector, for the statistics of one sample: wr = weight rstd
 template <typename T, int VEC>
-__device__ __forceinline__ void centred_grad(const TileArgs& a, const Raw<T, VEC>& rx, const Raw<T, VEC>& rd, int64_t row, int32_t c, float mean, float rstd,
+__device__ __forceinline__ void centred_grad(const TileArgs& a, const Raw<T, VEC>& rx, const Raw<T, VEC>& rd, uint64_t key, int32_t c, float mean, float rstd,
                                              const float (&wr)[VEC], const float* sb, float (&xc)[VEC], float (&d)[VEC]) {
     float n[VEC], b[VEC];
     Params<VEC, 8, true>::read(sb, b);
@@ -107,7 +107,7 @@ __device__ __forceinline__ void centred_grad(const TileArgs& a, const Raw<T, VEC
         for (int i = 0; i < VEC; ++i) if (i == e) x = rx.get(i);
         return ((double)x - (double)mean) * (double)rstd * (double)(a.weight ? a.weight[c + e] : 1.f) + (double)(a.bias ? a.bias[c + e] : 0.f);
     });
-    drop_vector<VEC>(a.drop, a.drop.on ? drop_key(a.drop, row) : 0, c, d);
+    drop_vector<VEC>(a.drop, key, c, d);
 }
 
 // Sums of a tile: every thread has one vector of the channels and every n_ty-th row, K rows on their way; then the block's threads are brought
@@ -125,11 +125,15 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int3
     const int32_t rows = (int32_t)(t.row1 - t.row0);
     for (int32_t r = ty; r < rows; r += K * n_ty) {
         Raw<T, VEC> raw[K], rd[BACKWARD ? K : 1];
+        uint64_t key[BACKWARD ? K : 1];
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (r + k * n_ty < rows) {
                 raw[k].load(x + k * x_step);
-                if (BACKWARD) rd[k].load(d_y + k * d_step);
+                if (BACKWARD) {
+                    rd[k].load(d_y + k * d_step);
+                    key[k] = a.drop.on ? drop_key(a.drop, t.row0 + r + k * n_ty) : 0;
+                }
             }
         x += K * x_step;
         if (BACKWARD) d_y += K * d_step;
@@ -139,7 +143,7 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int3
                 if (r + k * n_ty >= rows) break;
                 float xc[VEC], d[VEC], wr[VEC];
                 Params<VEC, 8, true>::read(swr, wr);
-                centred_grad<T, VEC>(a, raw[k], rd[k], t.row0 + r + k * n_ty, c, mean, rstd, wr, sb, xc, d);
+                centred_grad<T, VEC>(a, raw[k], rd[k], key[k], c, mean, rstd, wr, sb, xc, d);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) { p.u[e] = fmaf(d[e], xc[e], p.u[e]); p.v[e] += d[e]; }
             }
@@ -404,28 +408,29 @@ __device__ __forceinline__ void tile_results(const TileArgs& a, const Tile& t, i
     const float k1 = -s1 * rstd, k2 = -s2 * rstd * rstd;
     for (int32_t r = ty; r < rows; r += U * n_ty) {
         Raw<T, VEC> raw[U], rd[BACKWARD ? U : 1];
+        uint64_t key[U];   // (fetched with the row: behind its arrival it would be waited for once more)
 #pragma unroll
         for (int k = 0; k < U; ++k)
             if (r + k * n_ty < rows) {
                 raw[k].load(x + k * x_step);
                 if (BACKWARD) rd[k].load(d_y + k * d_step);
+                key[k] = a.drop.on ? drop_key(a.drop, t.row0 + r + k * n_ty) : 0;
             }
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             if (r + k * n_ty >= rows) break;
-            const int64_t row = t.row0 + r + k * n_ty;
             float f[VEC];
             if constexpr (BACKWARD) {   // rstd (dz w - mean(dz w) - hat mean(dz w hat))
                 float xc[VEC];
                 Params<VEC, 8, true>::read(swr, w);
-                centred_grad<T, VEC>(a, raw[k], rd[k], row, c, mean, rstd, w, sb, xc, f);
+                centred_grad<T, VEC>(a, raw[k], rd[k], key[k], c, mean, rstd, w, sb, xc, f);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f[e] = fmaf(f[e], w[e], fmaf(xc[e], k2, k1));
             } else {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f[e] = fmaf(raw[k].get(e) - mean, w[e], b[e]);
                 act_values<VEC>(a.act, f);
-                drop_vector<VEC>(a.drop, a.drop.on ? drop_key(a.drop, row) : 0, c, f);
+                drop_vector<VEC>(a.drop, key[k], c, f);
             }
             raw[k].put(f);
             raw[k].store(out + k * out_step);
