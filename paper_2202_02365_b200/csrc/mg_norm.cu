@@ -119,7 +119,7 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
             ctx->launches++;
         }
         if (a.tiles > 0 || p.block_grid) {
-            const TileLaunch l{p.vec, p.sums_vec, backward, p.block_grid};
+            const TileLaunch l{p.vec, p.sums_vec, backward, p.block_grid, p.cluster};
             MG_BY_TYPE(s->dtype, launch_tiles<T>(l, a, st));
             ctx->launches += p.block_grid ? 1 : 2;
         }

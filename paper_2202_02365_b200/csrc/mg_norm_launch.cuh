@@ -67,8 +67,21 @@ void launch_results(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
 
 template <typename T, int VEC>
 void launch_block(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
-    if (l.backward) k_norm_block<T, VEC, true><<<l.block_grid, kNormThreads, 0, st>>>(a);
-    else k_norm_block<T, VEC, false><<<l.block_grid, kNormThreads, 0, st>>>(a);
+    constexpr int K = sizeof(T) * VEC == 32 ? 2 : 4;
+    if (l.cluster == 1) {
+        if (l.backward) k_norm_block<T, VEC, true, false, K><<<l.block_grid, kNormThreads, 0, st>>>(a);
+        else k_norm_block<T, VEC, false, false, K><<<l.block_grid, kNormThreads, 0, st>>>(a);
+        return;
+    }
+    const auto kernel = l.backward ? k_norm_block<T, VEC, true, true, VEC == 8 ? 2 : 4> : k_norm_block<T, VEC, false, true, 4>;
+    if (l.cluster > 8) cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)l.cluster; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t how = {};
+    how.gridDim = dim3((unsigned)l.block_grid); how.blockDim = dim3(kNormThreads); how.stream = st;
+    how.attrs = &attr; how.numAttrs = 1;
+    cudaLaunchKernelEx(&how, kernel, a);   // (an error is found by cudaGetLastError)
 }
 
 template <typename T>

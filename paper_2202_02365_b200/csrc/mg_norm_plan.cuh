@@ -94,7 +94,7 @@ struct NormPlan {
     size_t cleared = 0, at_fan_count = 0, at_sample_count = 0, at_table = 0, at_tile_parts = 0, at_fan_parts = 0, at_group_parts = 0, at_parts = 0, at_slices = 0, bytes = 0;
     int64_t n_parts = 0;   // backward: what k_norm_params adds up
     int sums_vec = 1;      // tiles: vectors of the sums
-    int block_grid = 0;    // samples that a block deals with by itself: how many blocks
+    int block_grid = 0, cluster = 0;   // samples that a block or a cluster deals with by itself: how many blocks, and how many to a sample
 };
 
 int ceil_log2(int64_t v) { int l = 0; while ((1ll << l) < v) ++l; return l; }
@@ -122,10 +122,18 @@ void plan_rows(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPla
     p->bytes = backward ? p->at_slices + sizeof(float) * 2 * (size_t)s->channels * kParamSlices : 0;
 }
 
-// Samples of up to 64 KB go to one block each.  In a replayed graph, fp32 rows of 128 channels with a SiLU, against the two launches: one sample of 16 KB
-// 4.5 / 10.3 us (backward 7.4 / 14.4), of 64 KB 7.2 / 12.2 (13.3 / 15.2), of 128 KB 11.1 / 12.3 (20.5 / 15.1); 600 of 64 KB 23.5 / 28.3 (48 / 53),
-// 20,000 of 4 KB 237 / 300 (280 / 421).
+// Samples of up to 64 KB go to one block each, larger ones to a cluster of up to 16 with shares as large; one above 32 KB to as many blocks as two to
+// an SM leave it (clusters of 16: one to an SM, they are hard to place), with no less than 8 KB each.  In a replayed graph, fp32 rows of 128 channels
+// with a SiLU, against the two launches, forward / backward in us: one sample of 16 KB 4.4 / 7.0 against 12.1 / 15.5 (two blocks 6.7 / 9.3), of 64 KB
+// in 8 blocks 7.5 / 10.1 against 12.2 / 16.4 (one block 6.9 / 12.7), of 256 KB in 16 8.6 / 11.7 against 12.4 / 16.4, of 1 MB 11.1 / 18.3 against
+// 15.4 / 18.5, of 2 MB 14.4 / 25.8 against 16.4 / 19.7; 16 of 256 KB in 8 blocks each 10.1 / 17.0 (in 16: 16.7 / 22.2) against 16.4 / 19.1; 64 of 256 KB
+// in 4 12.8 / 23.2 (in 8: 19.4 / 32.6) against 19.9 / 30.5; 600 of 64 KB 24.6 / 49.5 against 30.7 / 59.5; 20,000 of 4 KB 235 / 290 against 300 / 421.
 constexpr int64_t kBlockBytes = 64 << 10;
+int blocks_of_sample(int64_t n, int64_t bytes, int n_sms) {
+    int c = 1;
+    while (bytes > 32 << 10 && c < kMaxCluster && bytes > (8 << 10) * c && n * c * 2 <= (c * 2 == kMaxCluster ? n_sms : 2 * n_sms)) c *= 2;
+    return bytes <= kBlockBytes * c ? c : 0;
+}
 constexpr int64_t kTileBytes = 384 << 10;
 
 // Samples of several rows.  a: the geometry's part of the arguments.
@@ -147,12 +155,11 @@ void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPl
     const int64_t used = equal ? s->rows : s->sample_offsets[n];
     int64_t longest = equal ? s->rows_per_sample : 0;
     if (!equal) for (int64_t i = 0; i < n; ++i) longest = std::max(longest, s->sample_offsets[i + 1] - s->sample_offsets[i]);
-    // samples that a block deals with by itself
     a->samples = (int32_t)n; a->equal = equal;
     a->rows_per_sample = s->rows_per_sample;
-    p->block_grid = 0;
-    if (a->results.chunks == 1 && s->channels <= kBlockChannels && s->groups <= kBlockGroups && longest * s->channels * elem <= kBlockBytes) {
-        p->block_grid = (int)std::min<int64_t>(n, (int64_t)n_sms * 4);
+    if (a->results.chunks == 1 && s->channels <= kBlockChannels && s->groups <= kBlockGroups) p->cluster = blocks_of_sample(n, longest * s->channels * elem, n_sms);
+    if (p->cluster) {
+        p->block_grid = (int)std::min<int64_t>(n, (int64_t)n_sms * 4 / p->cluster) * p->cluster;
         size_t at = 0;
         const auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 15) / 16 * 16; return was; };
         p->cleared = 0;

@@ -125,16 +125,15 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int3
     const int32_t rows = (int32_t)(t.row1 - t.row0);
     for (int32_t r = ty; r < rows; r += K * n_ty) {
         Raw<T, VEC> raw[K], rd[BACKWARD ? K : 1];
-        uint64_t key[BACKWARD ? K : 1];
+        uint64_t key = 0;
 #pragma unroll
         for (int k = 0; k < K; ++k)
             if (r + k * n_ty < rows) {
                 raw[k].load(x + k * x_step);
-                if (BACKWARD) {
-                    rd[k].load(d_y + k * d_step);
-                    key[k] = a.drop.on ? drop_key(a.drop, t.row0 + r + k * n_ty) : 0;
-                }
+                if (BACKWARD) rd[k].load(d_y + k * d_step);
             }
+        // (a single row's key with the row: behind its arrival it would be waited for once more.  More rows' are too many registers.)
+        if (BACKWARD && K == 1 && a.drop.on) key = drop_key(a.drop, t.row0 + r);
         x += K * x_step;
         if (BACKWARD) d_y += K * d_step;
         if constexpr (BACKWARD) {
@@ -143,7 +142,8 @@ __device__ __forceinline__ void tile_sums(const TileArgs& a, const Tile& t, int3
                 if (r + k * n_ty >= rows) break;
                 float xc[VEC], d[VEC], wr[VEC];
                 Params<VEC, 8, true>::read(swr, wr);
-                centred_grad<T, VEC>(a, raw[k], rd[k], key[k], c, mean, rstd, wr, sb, xc, d);
+                if (K > 1 && a.drop.on) key = drop_key(a.drop, t.row0 + r + k * n_ty);
+                centred_grad<T, VEC>(a, raw[k], rd[k], key, c, mean, rstd, wr, sb, xc, d);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) { p.u[e] = fmaf(d[e], xc[e], p.u[e]); p.v[e] += d[e]; }
             }
@@ -267,10 +267,9 @@ __device__ __forceinline__ void run_groups(const TileArgs& a, const float* su, c
     }
 }
 
-// `n` sets of the groups' values that lie one behind the other, of values_of(i, g) values each (none: the set is not there), to `use(g, u, v)`
-template <bool BACKWARD, typename Values, typename Use>
-__device__ __forceinline__ void merge_sets(const TileArgs& a, const float* parts, int32_t n, Values values_of, Use use) {
-    const int64_t step = 2 * (int64_t)a.groups;
+// `n` sets of the groups' values, fetch(i, g, u, v), of values_of(i, g) values each (none: the set is not there), to `use(g, u, v)`
+template <bool BACKWARD, typename Values, typename Fetch, typename Use>
+__device__ __forceinline__ void merge_sets(const TileArgs& a, int32_t n, Values values_of, Fetch fetch, Use use) {
     const int per = group_threads(a.groups, kNormThreads), sub = threadIdx.x % per;
     constexpr int B = 4;   // sets on their way at a time
     for (int32_t g0 = 0; g0 < a.groups; g0 += kNormThreads / per) {
@@ -282,7 +281,7 @@ __device__ __forceinline__ void merge_sets(const TileArgs& a, const float* parts
             for (int k = 0; k < B; ++k) {
                 const int32_t i = min(i0 + k * per, n - 1);
                 pn[k] = i0 + k * per < n ? values_of(i, g) : 0.f;
-                pu[k] = __ldcg(parts + i * step + g); pv[k] = __ldcg(parts + i * step + a.groups + g);
+                fetch(i, g, pu[k], pv[k]);
             }
 #pragma unroll
             for (int k = 0; k < B; ++k) {
@@ -338,10 +337,11 @@ __device__ __forceinline__ void arrive(const TileArgs& a, const Tile& t, int32_t
         if (fans == 1) finish(g, u, v);
         else { __stcg(fan_part + g, u); __stcg(fan_part + a.groups + g, v); }
     };
-    merge_sets<BACKWARD>(a, a.tile_parts + ((int64_t)t.first + fan * kFan) * chunks * step, fan_tiles * chunks, tile_values, keep);
+    const auto from = [&](const float* sets) { return [=](int32_t i, int32_t g, float& u, float& v) { u = __ldcg(sets + i * step + g); v = __ldcg(sets + i * step + step / 2 + g); }; };
+    merge_sets<BACKWARD>(a, fan_tiles * chunks, tile_values, from(a.tile_parts + ((int64_t)t.first + fan * kFan) * chunks * step), keep);
     if (fans == 1 || !last(a.sample_count + t.sample, fans)) return;
     const auto fan_values = [&](int32_t i, int32_t) { return (float)min((int64_t)kFan * a.tile_rows, t.sample_rows - (int64_t)i * kFan * a.tile_rows) * (float)a.each; };
-    merge_sets<BACKWARD>(a, a.fan_parts + first_fan * step, fans, fan_values, finish);
+    merge_sets<BACKWARD>(a, fans, fan_values, from(a.fan_parts + first_fan * step), finish);
 }
 
 template <int VEC>
@@ -408,29 +408,30 @@ __device__ __forceinline__ void tile_results(const TileArgs& a, const Tile& t, i
     const float k1 = -s1 * rstd, k2 = -s2 * rstd * rstd;
     for (int32_t r = ty; r < rows; r += U * n_ty) {
         Raw<T, VEC> raw[U], rd[BACKWARD ? U : 1];
-        uint64_t key[U];   // (fetched with the row: behind its arrival it would be waited for once more)
+        uint64_t key = 0;
 #pragma unroll
         for (int k = 0; k < U; ++k)
             if (r + k * n_ty < rows) {
                 raw[k].load(x + k * x_step);
                 if (BACKWARD) rd[k].load(d_y + k * d_step);
-                key[k] = a.drop.on ? drop_key(a.drop, t.row0 + r + k * n_ty) : 0;
             }
+        if (U == 1 && a.drop.on) key = drop_key(a.drop, t.row0 + r);   // (as for the sums)
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             if (r + k * n_ty >= rows) break;
             float f[VEC];
+            if (U > 1 && a.drop.on) key = drop_key(a.drop, t.row0 + r + k * n_ty);
             if constexpr (BACKWARD) {   // rstd (dz w - mean(dz w) - hat mean(dz w hat))
                 float xc[VEC];
                 Params<VEC, 8, true>::read(swr, w);
-                centred_grad<T, VEC>(a, raw[k], rd[k], key[k], c, mean, rstd, w, sb, xc, f);
+                centred_grad<T, VEC>(a, raw[k], rd[k], key, c, mean, rstd, w, sb, xc, f);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f[e] = fmaf(f[e], w[e], fmaf(xc[e], k2, k1));
             } else {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f[e] = fmaf(raw[k].get(e) - mean, w[e], b[e]);
                 act_values<VEC>(a.act, f);
-                drop_vector<VEC>(a.drop, key[k], c, f);
+                drop_vector<VEC>(a.drop, key, c, f);
             }
             raw[k].put(f);
             raw[k].store(out + k * out_step);
@@ -463,46 +464,77 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __gri
     tile_results<T, VEC, BACKWARD, U>(a, t, c, ty, n_ty, mean, rstd, s1, s2, w, b, sw + tx * VEC, sb + tx * VEC);
 }
 
-// Samples that a block goes through twice by itself (its second look finds them in L1 or L2): one launch, nothing handed from block to block.
-constexpr int kBlockChannels = 1024, kBlockGroups = 256;
-template <typename T, int VEC, bool BACKWARD>
+// Samples that a block, or a cluster of blocks, goes through twice by itself (its second look finds them in L1 or L2): one launch.  The blocks of a
+// cluster take equal shares of the rows and read each other's sums from shared memory.
+constexpr int kBlockChannels = 1024, kBlockGroups = 256, kMaxCluster = 16;
+
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ uint32_t cluster_size() { uint32_t r; asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+__device__ __forceinline__ float peer_value(const float* mine, uint32_t rank) {   // the same place in another block's shared memory
+    uint32_t at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(mine)), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+
+template <typename T, int VEC, bool BACKWARD, bool CLUSTER, int K>
 __global__ void __launch_bounds__(kNormThreads, 2) k_norm_block(const __grid_constant__ TileArgs a) {
     __shared__ __align__(16) float su[kNormThreads * VEC], sv[kNormThreads * VEC], sw[BACKWARD ? kBlockChannels : 4], sb[BACKWARD ? kBlockChannels : 4], acc[BACKWARD ? 2 * kBlockChannels : 4];
-    __shared__ float sn[kNormThreads], g1[kBlockGroups], g2[kBlockGroups];
+    __shared__ float sn[kNormThreads], g1[kBlockGroups], g2[kBlockGroups], part1[CLUSTER ? kBlockGroups : 1], part2[CLUSTER ? kBlockGroups : 1];
     const int tx = threadIdx.x & ((1 << a.results.tx) - 1), ty = threadIdx.x >> a.results.tx, n_ty = kNormThreads >> a.results.tx;
-    const int32_t c = tx * VEC;
+    const int32_t c = tx * VEC, size = CLUSTER ? (int32_t)cluster_size() : 1, rank = CLUSTER ? (int32_t)cluster_rank() : 0;
     const bool in = c < a.channels;
     const int32_t group = in ? c / a.each : 0;
+    bool read = false;   // the others' sums have been: they may write theirs anew, or end, when all have
     for (int i = threadIdx.x; BACKWARD && i < 2 * a.channels; i += kNormThreads) acc[i] = 0.f;
-    for (int32_t s = blockIdx.x; s < a.samples; s += gridDim.x) {
+    for (int32_t s = (int32_t)blockIdx.x / size; s < a.samples; s += (int32_t)gridDim.x / size) {
         Tile t;
         t.sample = s;
-        t.row0 = a.equal ? s * a.rows_per_sample : sample_entry(a, s).x;
-        t.row1 = a.equal ? t.row0 + a.rows_per_sample : sample_entry(a, s + 1).x;
-        t.sample_rows = t.row1 - t.row0;
+        const int64_t row0 = a.equal ? s * a.rows_per_sample : sample_entry(a, s).x;
+        t.sample_rows = a.equal ? a.rows_per_sample : sample_entry(a, s + 1).x - row0;
         const int64_t stat = (int64_t)s * a.groups;
-        __syncthreads();   // (shared memory has been read)
         if (t.sample_rows == 0) {
             for (int32_t g = threadIdx.x; !BACKWARD && g < a.groups; g += kNormThreads) { a.mean[stat + g] = 0.f; a.rstd[stat + g] = 0.f; }
             continue;
         }
+        const int64_t share = (t.sample_rows + size - 1) / size;
+        const auto start = [&](int32_t r) { return min(r * share, t.sample_rows); };
+        t.row0 = row0 + start(rank);
+        t.row1 = row0 + start(rank + 1);
         float mean = 0.f, rstd = 0.f, w[VEC], b[VEC];
+        __syncthreads();   // (shared memory has been read)
         if (BACKWARD) {
             mean = a.mean[stat + group]; rstd = a.rstd[stat + group];
             share_params(a, t, sw, sb, 0, a.channels);
         }
         Pair<VEC> p;
-        tile_sums<T, VEC, BACKWARD, sizeof(T) * VEC == 32 ? 2 : 4>(a, t, c, in, ty, n_ty, mean, rstd, sw + c, sb + c, p);
+        tile_sums<T, VEC, BACKWARD, K>(a, t, c, in, ty, n_ty, mean, rstd, sw + c, sb + c, p);
         block_pairs<VEC, BACKWARD>(p, su, sv, sn, a.results.tx, a.channels);
         for (int i = threadIdx.x; BACKWARD && i < a.channels; i += kNormThreads) { acc[i] += su[i]; acc[a.channels + i] += sv[i]; }
         const float values = (float)t.sample_rows * (float)a.each;
-        run_groups<BACKWARD>(a, su, sv, 0, a.channels, (float)t.sample_rows, [&](int32_t g, float u, float v) {
+        const auto finish = [&](int32_t g, float u, float v) {
             if (BACKWARD) { g1[g] = v / values; g2[g] = u / values; }
             else {
                 g1[g] = u; g2[g] = rsqrtf(v / values + a.eps);
-                a.mean[stat + g] = u; a.rstd[stat + g] = g2[g];
+                if (rank == 0) { a.mean[stat + g] = u; a.rstd[stat + g] = g2[g]; }
             }
+        };
+        if (CLUSTER && read) cluster_wait();
+        run_groups<BACKWARD>(a, su, sv, 0, a.channels, (float)(t.row1 - t.row0), [&](int32_t g, float u, float v) {
+            if (!CLUSTER) finish(g, u, v);
+            else { part1[g] = u; part2[g] = v; }
         });
+        if constexpr (CLUSTER) {
+            cluster_arrive();
+            cluster_wait();
+            merge_sets<BACKWARD>(a, size, [&](int32_t i, int32_t) { return (float)(start(i + 1) - start(i)) * (float)a.each; },
+                                 [&](int32_t i, int32_t g, float& u, float& v) { u = peer_value(part1 + g, i); v = peer_value(part2 + g, i); }, finish);
+            cluster_arrive();
+            read = true;
+        }
         __syncthreads();
         if (!in) continue;
         if (!BACKWARD) {
@@ -512,8 +544,9 @@ __global__ void __launch_bounds__(kNormThreads, 2) k_norm_block(const __grid_con
 #pragma unroll
             for (int e = 0; e < VEC; ++e) w[e] *= rstd;
         }
-        tile_results<T, VEC, BACKWARD, sizeof(T) * VEC == 32 ? 2 : 4>(a, t, c, ty, n_ty, mean, rstd, g1[group], g2[group], w, b, sw + c, sb + c);
+        tile_results<T, VEC, BACKWARD, K>(a, t, c, ty, n_ty, mean, rstd, g1[group], g2[group], w, b, sw + c, sb + c);
     }
+    if (CLUSTER && read) cluster_wait();
     if (!BACKWARD || !a.parts) return;
     __syncthreads();
     for (int i = threadIdx.x; i < 2 * a.channels; i += kNormThreads) a.parts[2 * (int64_t)blockIdx.x * a.channels + i] = acc[i];
@@ -530,7 +563,7 @@ __global__ void k_norm_empty(const __grid_constant__ TileArgs a) {
 
 // what a translation unit of its own per row type launches
 struct RowLaunch { int vec, nv; bool general, backward; int grid; RowShape shape; };
-struct TileLaunch { int vec, sums_vec; bool backward; int block_grid; };   // block_grid: of k_norm_block, or 0
+struct TileLaunch { int vec, sums_vec; bool backward; int block_grid, cluster; };   // block_grid: of k_norm_block, or 0
 template <typename T> void launch_dropout(int vec, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t rows, int32_t channels, const DropArgs& d, int grid, cudaStream_t st);
 template <typename T> void launch_rows(const RowLaunch& l, const NormArgs& a, cudaStream_t st);
 template <typename T> void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st);

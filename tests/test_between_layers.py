@@ -320,6 +320,18 @@ def test_large_samples(ctx, samples, channels, groups, dtype):
     check_norm(ctx, x, samples, groups, "silu", mg.Dropout(0.3, 9))
 
 
+# samples that several blocks share: from two to sixteen of them, shares without a row, many samples for each cluster, empty ones in between
+@pytest.mark.gpu
+@pytest.mark.parametrize("samples,channels,groups,dtype", [([100], 128, 8, "f32"), ([2000], 128, 8, "f32"), ([35], 1024, 32, "bf16"), ([17, 0, 16, 1], 1020, 5, "f32"), ([500] * 16, 128, 4, "f32"),
+                                                           ([700, 0, 300, 512] * 16, 256, 32, "f16"), ([137, 137, 137], 100, 4, "f32"), ([3, 250, 0, 249] * 35, 64, 2, "f32"), ([130] * 148, 128, 1, "f16")])
+def test_samples_of_several_blocks(ctx, samples, channels, groups, dtype):
+    x = rows_of(sum(samples) + 2, channels, TYPES[dtype], 3)
+    for kind, drop in (("silu", None), ("relu", mg.Dropout(0.4, 6))):
+        first = check_norm(ctx, x, samples, groups, kind, drop)
+        for a, b in zip(first, check_norm(ctx, x, samples, groups, kind, drop)):
+            assert torch.equal(a, b)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape,groups", [((4, 9, 48), 3), ((2, 33, 17, 64), 8), ((5, 1, 32), 2), ((300, 4, 16), 1), ((3, 2000, 96), 4), ((0, 5, 8), 2), ((4, 0, 8), 2)])
 def test_equal_samples(ctx, shape, groups):
@@ -685,7 +697,7 @@ int main() {
             plan_tiles(&s, 148, backward, *v, &p, &a);
             NEED(p.bytes <= have);
             if (p.block_grid) {
-                NEED(s.channels <= kBlockChannels && s.groups <= kBlockGroups && s.channels <= (*v << a.results.tx) && a.results.tx <= 8 && p.block_grid <= n);
+                NEED(s.channels <= kBlockChannels && s.groups <= kBlockGroups && s.channels <= (*v << a.results.tx) && a.results.tx <= 8 && p.block_grid <= n * p.cluster && p.block_grid % p.cluster == 0 && p.cluster <= kMaxCluster);
                 NEED(!backward || (p.n_parts == p.block_grid && p.at_parts + 8ull * p.n_parts * s.channels <= p.at_slices && p.at_slices + 8ull * kParamSlices * s.channels <= p.bytes));
                 NEED(s.n_samples <= kInlineSamples || p.at_table + 8ull * (s.n_samples + 1) <= p.at_parts);
                 continue;
