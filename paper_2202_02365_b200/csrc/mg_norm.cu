@@ -12,6 +12,7 @@ __global__ void __launch_bounds__(kParamThreads) k_norm_params(const float* part
     constexpr int W = kParamThreads / 32, U = 8;
     __shared__ float part[W][33];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    chain_wait();
     const int64_t c0 = (int64_t)blockIdx.x * 32, c = c0 + lane, lo = n * blockIdx.y / gridDim.y, hi = n * (blockIdx.y + 1) / gridDim.y;
     float s = 0.f;
     if (c < columns)
@@ -131,11 +132,11 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
         int64_t n = p.n_parts;
         if (n > kParamParts) {
             float* slices = reinterpret_cast<float*>(ws + p.at_slices);
-            k_norm_params<<<dim3(blocks, (unsigned)kParamSlices), kParamThreads, 0, st>>>(parts, n, columns, slices, nullptr, nullptr);
+            launch_chained(dim3(blocks, (unsigned)kParamSlices), kParamThreads, st, k_norm_params, parts, n, columns, slices, (float*)nullptr, (float*)nullptr);
             ctx->launches++;
             parts = slices; n = kParamSlices;
         }
-        k_norm_params<<<blocks, kParamThreads, 0, st>>>(parts, n, columns, nullptr, d_weight, d_bias);
+        launch_chained(dim3(blocks), kParamThreads, st, k_norm_params, parts, n, columns, (float*)nullptr, d_weight, d_bias);
         ctx->launches++;
     }
     MG_CUDA(ctx, cudaGetLastError());

@@ -61,8 +61,8 @@ template <typename T, int VEC>
 void launch_results(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
     const unsigned grid = (unsigned)((int64_t)a.tiles * a.results.chunks);
     constexpr bool wide = sizeof(T) * VEC == 32;
-    if (l.backward) k_norm_results<T, VEC, true, wide ? 1 : 2, 3><<<grid, kNormThreads, 0, st>>>(a);
-    else k_norm_results<T, VEC, false, wide ? 2 : 4, 4><<<grid, kNormThreads, 0, st>>>(a);
+    if (l.backward) launch_chained(dim3(grid), kNormThreads, st, k_norm_results<T, VEC, true, wide ? 1 : 2, 3>, a);
+    else launch_chained(dim3(grid), kNormThreads, st, k_norm_results<T, VEC, false, wide ? 2 : 4, 4>, a);
 }
 
 template <typename T, int VEC>

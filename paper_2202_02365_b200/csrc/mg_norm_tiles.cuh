@@ -367,6 +367,10 @@ __device__ __forceinline__ void share_params(const TileArgs& a, const Tile& t, f
     __syncthreads();
 }
 
+// A launch that may begin while the one before it ends: nothing of that one's is read, nor anything written, before chain_wait.
+__device__ __forceinline__ void chain_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }   // (the next one's blocks may come where there is room)
+__device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 template <typename T, int VEC, bool BACKWARD, int K, int MINB>
 __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_sums(const __grid_constant__ TileArgs a) {
     __shared__ __align__(16) float su[kNormThreads * VEC], sv[kNormThreads * VEC], sw[BACKWARD ? kNormThreads * VEC : 4], sb[BACKWARD ? kNormThreads * VEC : 4];
@@ -386,6 +390,7 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_sums(const __grid_c
     }
     Pair<VEC> p;
     tile_sums<T, VEC, BACKWARD, K>(a, t, c, in, ty, n_ty, mean, rstd, sw + tx * VEC, sb + tx * VEC, p);
+    chain_start();
     block_pairs<VEC, BACKWARD>(p, su, sv, sn, a.sums.tx, c1 - c0);
     if (BACKWARD && a.parts) {
         float* to = a.parts + 2 * (int64_t)tile * a.channels + c0;
@@ -449,6 +454,8 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __gri
     Tile t;
     locate_tile(a, a.tiles - 1 - from_last, &t);
     if (BACKWARD) share_params(a, t, sw, sb, c0, min(VEC << a.results.tx, a.channels - c0));
+    chain_start();
+    chain_wait();
     if (c >= a.channels) return;
     const int32_t group = c / a.each;
     const float mean = a.mean[(int64_t)t.sample * a.groups + group], rstd = a.rstd[(int64_t)t.sample * a.groups + group];
@@ -559,6 +566,18 @@ __global__ void k_norm_empty(const __grid_constant__ TileArgs a) {
         if (sample_entry(a, s).x != sample_entry(a, s + 1).x) continue;
         for (int32_t g = threadIdx.x; g < a.groups; g += blockDim.x) { a.mean[(int64_t)s * a.groups + g] = 0.f; a.rstd[(int64_t)s * a.groups + g] = 0.f; }
     }
+}
+
+// behind a launch of this file's in the same stream (an error is found by cudaGetLastError)
+template <typename... P, typename... A>
+void launch_chained(dim3 grid, int threads, cudaStream_t st, void (*kernel)(P...), A... args) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t how = {};
+    how.gridDim = grid; how.blockDim = dim3((unsigned)threads); how.stream = st;
+    how.attrs = &attr; how.numAttrs = 1;
+    cudaLaunchKernelEx(&how, kernel, args...);
 }
 
 // what a translation unit of its own per row type launches
