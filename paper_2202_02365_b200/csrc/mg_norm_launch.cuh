@@ -59,7 +59,7 @@ void launch_sums(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
 }
 template <typename T, int VEC>
 void launch_results(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
-    const unsigned grid = (unsigned)((int64_t)a.tiles * a.results.chunks);
+    const unsigned grid = (unsigned)((int64_t)a.tiles * a.parts_of_tile * a.results.chunks);
     constexpr bool wide = sizeof(T) * VEC == 32;
     if (l.backward) launch_chained(dim3(grid), kNormThreads, st, k_norm_results<T, VEC, true, wide ? 1 : 2, 3>, a);
     else launch_chained(dim3(grid), kNormThreads, st, k_norm_results<T, VEC, false, wide ? 2 : 4, 4>, a);

@@ -137,7 +137,11 @@ int blocks_of_sample(int64_t n, int64_t bytes, int n_sms) {
     while (bytes > 32 << 10 && c < kMaxCluster && bytes > (8 << 10) * c && n * c * 2 <= (c * 2 == kMaxCluster ? n_sms : 2 * n_sms)) c *= 2;
     return bytes <= kBlockBytes * c ? c : 0;
 }
-constexpr int64_t kTileBytes = 384 << 10;
+// Larger ones are cut into tiles, each summed up by one block, as many as the SMs hold together: one turn.  Where the samples' ends would leave that turn
+// uneven, more turns, of tiles of no less than 384 KB.  Results are computed by blocks of a few turns of loads, which make room for the next ones: 128 KB of
+// rows each, 512 KB where there is a gradient (its blocks prepare more).  In a replayed graph: 24 samples of 22,625 rows of 256 fp32 channels 292 us with
+// tiles of 384 KB for both, 270 so, backward 531 and 512; one sample of 2,000,003 rows of 128, backward, 981 and 844.
+constexpr int64_t kTileBytes = 384 << 10, kPartBytes = 128 << 10, kPartBytesBackward = 512 << 10;
 
 // Samples of several rows.  a: the geometry's part of the arguments.
 void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p, TileArgs* a) {
@@ -174,24 +178,35 @@ void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPl
         a->tiles = 0; a->tile_rows = 1 << 30; a->tiles_per_sample = 1;
         return;
     }
-    // tiles of about 384 KB, so many of them that the blocks the SMs hold together take equal turns; smaller ones where there would not be a turn
-    // for each, larger ones where a sample had more than kFan^2
-    const int64_t n_ty = kNormThreads >> a->results.tx, run_bytes = a->run * elem, chunks = a->sums.chunks;
-    const int64_t held = (int64_t)n_sms * (backward ? kTileBlocksBackward : kTileBlocks), bytes = used * run_bytes * chunks;
-    const int64_t turns = std::max<int64_t>(1, (bytes + held * kTileBytes / 2) / (held * kTileBytes)), spread = std::max<int64_t>(1, (used * chunks + held * turns - 1) / (held * turns));
+    const int64_t n_ty = kNormThreads >> a->results.tx, row_bytes = (int64_t)s->channels * elem, chunks = a->sums.chunks;
+    const int64_t held = (int64_t)n_sms * (backward ? kTileBlocksBackward : kTileBlocks), units = used * chunks;
     const auto count = [&](int64_t rows) {
         if (equal) return n * ((s->rows_per_sample + rows - 1) / rows);
         int64_t tiles = 0;
         for (int64_t i = 0; i < n; ++i) tiles += (s->sample_offsets[i + 1] - s->sample_offsets[i] + rows - 1) / rows;
         return tiles;
     };
-    int64_t rows = std::max({round_up(spread, n_ty), round_up((longest + kFan * kFan - 1) / (kFan * kFan), n_ty), (int64_t)16});
-    int64_t tiles = count(rows);
-    // (a tile more than the blocks' turns costs a turn)
-    for (int tries = 0; tries < 8 && tiles * chunks > held * turns; ++tries) tiles = count(rows += round_up(std::max<int64_t>(rows / 32, 1), n_ty));
+    const int64_t least = std::max({round_up((longest + kFan * kFan - 1) / (kFan * kFan), n_ty), (int64_t)16}), most_turns = std::max<int64_t>(1, used * row_bytes / (held * kTileBytes));
+    int64_t rows = least, tiles = 0;
+    double best = 0.0;
+    for (int64_t turns = n > kInlineSamples ? most_turns : 1; used > 0 && turns <= most_turns; turns = turns < 4 || turns == most_turns ? turns + 1 : most_turns) {
+        int64_t r = std::max(round_up(std::max<int64_t>(1, (units + held * turns - 1) / (held * turns)), n_ty), least), t = count(r);
+        // (a tile more than the blocks' turns costs a turn)
+        for (int tries = 0; tries < 4 && t * chunks > held * turns; ++tries) t = count(r += round_up(std::max<int64_t>(r / 32, 1), n_ty));
+        const double even = (double)units / ((double)((t * chunks + held - 1) / held * held) * (double)r);
+        if (even > best) { best = even; rows = r; tiles = t; }
+        if (best >= 0.9) break;
+    }
+    rows = std::min(rows, std::max(round_up(longest, n_ty), (int64_t)16));
     a->tile_rows = (int32_t)std::min<int64_t>(rows, 1 << 30);
     a->tiles_per_sample = equal ? (int32_t)((s->rows_per_sample + a->tile_rows - 1) / a->tile_rows) : 0;
     a->tiles = (int32_t)tiles;
+    // (no more than twice the blocks that have rows)
+    const int64_t run_bytes = std::min<int64_t>(s->channels, (int64_t)vec << a->results.tx) * elem, part = backward ? kPartBytesBackward : kPartBytes;
+    const int64_t part_of = (rows * run_bytes + part / 2) / part, useful = 2 * used * run_bytes / part / std::max<int64_t>(tiles, 1);
+    const int64_t parts = std::max<int64_t>(1, std::min(part_of, useful));
+    a->part_rows = (int32_t)round_up((a->tile_rows + parts - 1) / parts, n_ty);
+    a->parts_of_tile = (a->tile_rows + a->part_rows - 1) / a->part_rows;
     const int64_t fans = tiles / kFan + n + 1, pair = 2 * (int64_t)sizeof(float);
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 15) / 16 * 16; return was; };

@@ -23,6 +23,7 @@ struct TileArgs : NormArgs {
     const int2* table = nullptr;     // null: `inl`
     int2 inl[kInlineSamples + 1];
     int32_t tile_rows = 0, tiles = 0;
+    int32_t parts_of_tile = 1, part_rows = 0;   // results: a tile's rows by several blocks
     TileShape sums, results;
     int32_t run = 0;                 // channels of a run, for the sums
     // workspace
@@ -452,7 +453,10 @@ __global__ void __launch_bounds__(kNormThreads, MINB) k_norm_results(const __gri
     const int tx = threadIdx.x & ((1 << a.results.tx) - 1), ty = threadIdx.x >> a.results.tx, n_ty = kNormThreads >> a.results.tx;
     const int32_t from_last = (int32_t)blockIdx.x / a.results.chunks, c0 = ((int32_t)blockIdx.x - from_last * a.results.chunks) * (VEC << a.results.tx), c = c0 + tx * VEC;
     Tile t;
-    locate_tile(a, a.tiles - 1 - from_last, &t);
+    locate_tile(a, a.tiles - 1 - from_last / a.parts_of_tile, &t);
+    t.row0 += (int64_t)(a.parts_of_tile - 1 - from_last % a.parts_of_tile) * a.part_rows;
+    t.row1 = min(t.row1, t.row0 + a.part_rows);
+    if (t.row0 >= t.row1) return;   // (a sample's last tile has fewer rows)
     if (BACKWARD) share_params(a, t, sw, sb, c0, min(VEC << a.results.tx, a.channels - c0));
     chain_start();
     chain_wait();

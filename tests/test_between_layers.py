@@ -313,7 +313,7 @@ def test_samples_of_uneven_rows(ctx, dtype, samples, channels, groups, pad):
 
 # samples larger than one multiprocessor holds, than a cluster of them, and than all of them
 @pytest.mark.gpu
-@pytest.mark.parametrize("samples,channels,groups,dtype", [([900, 2500], 128, 8, "f32"), ([20_000, 300, 9_000], 256, 8, "f32"), ([50_001], 100, 4, "f16"), ([40_000] * 3, 192, 2, "bf16"),
+@pytest.mark.parametrize("samples,channels,groups,dtype", [([900, 2500], 128, 8, "f32"), ([20_000, 300, 9_000], 256, 8, "f32"), ([400_000, 5, 70_000], 128, 2, "f32"), ([90_000] * 3, 1024, 8, "f16"), ([50_001], 100, 4, "f16"), ([40_000] * 3, 192, 2, "bf16"),
                                                            ([70_000, 1], 101, 1, "f32"), ([30_000, 0, 2], 1030, 2, "f16"), ([150_000], 128, 4, "f32")])
 def test_large_samples(ctx, samples, channels, groups, dtype):
     x = rows_of(sum(samples), channels, TYPES[dtype], 3)
@@ -677,7 +677,8 @@ int main() {
             s.n_samples = (int)std::min<int64_t>(pick(1, MG_MAX_BATCHES), s.rows + 1);
             ends.assign(1, 0);
             for (int k = 1; k < s.n_samples; ++k) ends.push_back((int64_t)(rng() % (uint64_t)(s.rows + 1)));
-            ends.push_back(s.rows);
+            ends.push_back(rng() % 16 ? s.rows : 0);   // (all of them empty, now and then)
+            for (int64_t& e : ends) e = std::min(e, ends.back());
             std::sort(ends.begin(), ends.end());
             s.sample_offsets = ends.data();
         }
@@ -713,9 +714,10 @@ int main() {
                 NEED(!a.equal || tiles == a.tiles_per_sample);
             }
             NEED(tile == a.tiles && tile * std::max(a.sums.chunks, a.results.chunks) < 1ll << 31 && a.tile_rows > 0);
+            NEED(a.parts_of_tile >= 1 && (int64_t)a.parts_of_tile * a.part_rows >= a.tile_rows && (int64_t)(a.parts_of_tile - 1) * a.part_rows < a.tile_rows && tile * a.parts_of_tile * a.results.chunks < 1ll << 31);
             NEED(p.at_fan_count + 4 * fans_end <= p.at_sample_count && p.at_fan_parts + fans_end * pair <= p.at_group_parts);
             NEED(p.at_sample_count + 4 * n <= p.cleared && p.at_tile_parts + tile * a.sums.chunks * pair <= p.at_fan_parts);
-            NEED(!backward || (p.n_parts == tile && p.at_group_parts + n * pair <= p.at_parts && p.at_parts + tile * channels <= p.at_slices && p.at_slices + kParamSlices * channels <= p.bytes));
+            NEED(!backward || (tile == 0 && p.n_parts == 0) || (p.n_parts == tile && p.at_group_parts + n * pair <= p.at_parts && p.at_parts + tile * channels <= p.at_slices && p.at_slices + kParamSlices * channels <= p.bytes));
             NEED((int64_t)s.channels <= (int64_t)a.sums.chunks * a.run && (int64_t)a.run * (a.sums.chunks - 1) < s.channels && a.run <= p.sums_vec * 256 && a.run <= (p.sums_vec << a.sums.tx));
             NEED((int64_t)s.channels <= (int64_t)a.results.chunks * (*v << a.results.tx) && a.results.tx <= 8 && a.sums.tx <= 8);
             NEED(s.channels % p.sums_vec == 0 && (a.sums.chunks == 1 || a.run % p.sums_vec == 0));
