@@ -507,9 +507,9 @@ def test_more_than_two_to_the_31_elements(ctx):
     d_x, _, d_b = ctx.group_norm_backward(x, x, mean, rstd, groups, dropout=mg.Dropout(p, 9, 1), out=y)
     assert torch.equal(d_x[first:], ctx.group_norm_backward(tail, tail, *want[1:], groups, dropout=mg.Dropout(p, 9, 1, first))[0])
     del y, d_x
-    # one sample.  A thread merges at most 1050 rows (a sample has at most 1024 tiles, four threads share a channel's rows), then 256 threads, 32 tiles
-    # and 32 sets of those meet: chains of fewer than 2048 roundings.
-    chain = 2048
+    # one sample.  It has 592 tiles, or 444 where there is a gradient: at most 9,685 rows, four threads to a channel, so that a thread adds up at most
+    # 2,422; then 4 threads, 32 tiles and 14 sets of those meet: chains of fewer than 4096 roundings
+    chain = 4096
     blocks = [(lo, min(lo + 100_000, rows)) for lo in range(0, rows, 100_000)]
     n = rows * (channels // groups)
     put = lambda t: t.repeat_interleave(channels // groups)  # noqa: E731
