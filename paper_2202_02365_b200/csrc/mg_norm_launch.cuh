@@ -54,15 +54,15 @@ template <typename T, int VEC>
 void launch_sums(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
     const unsigned grid = (unsigned)((int64_t)a.tiles * a.sums.chunks);
     constexpr bool wide = sizeof(T) * VEC == 32;
-    if (l.backward) k_norm_sums<T, VEC, true, wide ? 1 : VEC == 8 ? 2 : 4, 3><<<grid, kNormThreads, 0, st>>>(a);
-    else if constexpr (!wide) k_norm_sums<T, VEC, false, 4, 4><<<grid, kNormThreads, 0, st>>>(a);   // (nothing is gained by more than 16 bytes here)
+    if (l.backward) k_norm_sums<T, VEC, true, wide ? 1 : VEC == 8 ? 2 : VEC == 1 ? 8 : 4, 3><<<grid, kNormThreads, 0, st>>>(a);
+    else if constexpr (!wide) k_norm_sums<T, VEC, false, VEC == 1 ? 16 : VEC == 2 ? 8 : 4, 4><<<grid, kNormThreads, 0, st>>>(a);   // (nothing is gained by more than 16 bytes here)
 }
 template <typename T, int VEC>
 void launch_results(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
     const unsigned grid = (unsigned)((int64_t)a.tiles * a.parts_of_tile * a.results.chunks);
     constexpr bool wide = sizeof(T) * VEC == 32;
-    if (l.backward) launch_chained(dim3(grid), kNormThreads, st, k_norm_results<T, VEC, true, wide ? 1 : 2, 3>, a);
-    else launch_chained(dim3(grid), kNormThreads, st, k_norm_results<T, VEC, false, wide ? 2 : 4, 4>, a);
+    if (l.backward) launch_chained(dim3(grid), kNormThreads, st, k_norm_results<T, VEC, true, wide ? 1 : VEC == 1 ? 8 : VEC == 2 ? 4 : 2, 3>, a);
+    else launch_chained(dim3(grid), kNormThreads, st, k_norm_results<T, VEC, false, wide ? 2 : VEC == 1 ? 16 : VEC == 2 ? 8 : 4, 4>, a);
 }
 
 template <typename T, int VEC>
