@@ -83,7 +83,7 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
     if (mode == NORM_ROWS) {
         plan_rows(s, ctx->n_sms, backward, rows_vec_width(m, n_matrices, s), &p);
         a.parts = params ? reinterpret_cast<float*>(ws) : nullptr;
-        const RowLaunch l{p.vec, p.nv, p.general, backward, p.grid, p.shape};
+        const RowLaunch l{p.vec, p.nv, p.cut, backward, p.grid, p.shape};
         MG_BY_TYPE(s->dtype, launch_rows<T>(l, a, st));
         ctx->launches++;
     } else if (mode == NORM_TILES) {

@@ -21,11 +21,11 @@ void launch_rows_of(const RowLaunch& l, const NormArgs& a, cudaStream_t st) {
     const size_t sums = 2 * sizeof(float) * (size_t)a.channels;
     const size_t params = (l.backward ? Params<VEC, NV, true>::kHeld : Params<VEC, NV, false>::kHeld) ? 0 : sums;
     if (l.backward) {
-        if (l.general) k_norm_rows_backward<T, VEC, NV, true><<<l.grid, kNormThreads, params + sums, st>>>(a, l.shape);
-        else k_norm_rows_backward<T, VEC, NV, false><<<l.grid, kNormThreads, params + sums, st>>>(a, l.shape);
+        const auto kernel = l.cut == ROW_EVEN ? k_norm_rows_backward<T, VEC, NV, ROW_EVEN> : l.cut == ROW_NARROW ? k_norm_rows_backward<T, VEC, NV, ROW_NARROW> : k_norm_rows_backward<T, VEC, NV, ROW_MASKS>;
+        kernel<<<l.grid, kNormThreads, params + sums, st>>>(a, l.shape);
     } else {
-        if (l.general) k_norm_rows<T, VEC, NV, true><<<l.grid, kNormThreads, params, st>>>(a, l.shape);
-        else k_norm_rows<T, VEC, NV, false><<<l.grid, kNormThreads, params, st>>>(a, l.shape);
+        const auto kernel = l.cut == ROW_EVEN ? k_norm_rows<T, VEC, NV, ROW_EVEN> : l.cut == ROW_NARROW ? k_norm_rows<T, VEC, NV, ROW_NARROW> : k_norm_rows<T, VEC, NV, ROW_MASKS>;
+        kernel<<<l.grid, kNormThreads, params, st>>>(a, l.shape);
     }
 }
 

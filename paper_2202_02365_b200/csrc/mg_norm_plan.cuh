@@ -88,8 +88,8 @@ struct NormPlan {
     int grid = 0;
     // rows
     int nv = 1;
-    bool general = false;
-    RowShape shape{0, 0};
+    int cut = ROW_EVEN;
+    RowShape shape{0, 0, 0};
     // workspace: bytes that are cleared first, then where the others start
     size_t cleared = 0, at_fan_count = 0, at_sample_count = 0, at_table = 0, at_tile_parts = 0, at_fan_parts = 0, at_group_parts = 0, at_parts = 0, at_slices = 0, bytes = 0;
     int64_t n_parts = 0;   // backward: what k_norm_params adds up
@@ -113,7 +113,11 @@ void plan_rows(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPla
     p->shape.lanes = std::min(5, ceil_log2(vecs));
     p->nv = 1 << ceil_log2((vecs + 31) / 32);
     const int64_t width = each / vec;
-    p->general = s->groups > 1 && (each % vec || (width & (width - 1)));
+    // Groups of other widths than a power of two, us forward / backward.  Narrow ones of whole vectors meet in shared memory: 100,000 fp32 rows of 768 in 32
+    // groups 115 / 276 (under masks 1,812 / 2,749), 200,000 of 192 in 16 67 / 124 (591 / 762).  Wide ones, where that takes a lane as many reads as a group
+    // has vectors, are few: under masks 200,000 of 602 in 2 take 831 / 2,480.
+    if (s->groups > 1 && (each % vec || (width & (width - 1)))) p->cut = each % vec == 0 && width < 2 * vec * s->groups ? ROW_NARROW : ROW_MASKS;
+    p->shape.width = p->cut == ROW_NARROW ? (int32_t)width : 0;
     p->shape.gshift = s->groups == 1 ? 31 : ceil_log2(std::max<int64_t>(width, 1));
     const int64_t per_block = (int64_t)kNormWarps * (32 >> p->shape.lanes);
     // forward: more blocks where each has sixteen turns all the same (543,000 rows of 256: 201 us in eight to an SM, 196 in sixteen; 60,000 of 128: 15.2 and
@@ -272,11 +276,11 @@ int vec_width(const Matrix* m, int n, int dtype, int64_t rows, int32_t of) {
     return 1;
 }
 
-// ... for rows that are samples by themselves: a group's vectors where they are a power of two in number, else the row's
+// ... for rows that are samples by themselves: a group's vectors where they are a power of two in number or as wide as fours, else the row's
 int rows_vec_width(const Matrix* m, int n, const mg_norm_spec* s) {
     const int32_t each = s->channels / s->groups;
     const int v = vec_width(m, n, s->dtype, s->rows, each), w = each / v;
-    return (w & (w - 1)) == 0 ? v : vec_width(m, n, s->dtype, s->rows, s->channels);
+    return (w & (w - 1)) == 0 || v >= 4 ? v : vec_width(m, n, s->dtype, s->rows, s->channels);
 }
 
 // every check of an entry point's arguments but the workspace's; `d`: the dropout as the kernels take it

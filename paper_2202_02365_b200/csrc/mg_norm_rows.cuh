@@ -143,10 +143,11 @@ __global__ void __launch_bounds__(kNormThreads, 5) k_dropout_pieces(const T* x, 
 // The bytes bound it, and half of the issue slots go to the row's sums, the generator and the activation: 768,000 fp32 rows of 256 with a ReLU and a
 // dropout 284 us, 5.5 TB/s; the gradient of 543,000 334 us, 5.0 TB/s.
 // A row's vectors lie on 2^lanes lanes (all 32 where it has more than 32 vectors, NV of them per lane then); a warp holds 32 >> lanes rows.
-// The groups are equal blocks of `1 << gshift` vectors (gshift 31: the whole row) or, GENERAL, of any width: then they are taken one after
-// the other under masks.
+// The groups are equal blocks of `1 << gshift` vectors (gshift 31: the whole row), or narrow ones of `width` whole vectors, summed up through shared
+// memory, or of any width, taken one after the other under masks.
+enum { ROW_EVEN = 0, ROW_NARROW = 1, ROW_MASKS = 2 };
 
-struct RowShape { int32_t lanes, gshift; };
+struct RowShape { int32_t lanes, gshift, width; };
 
 template <int NV>
 __device__ __forceinline__ void group_sum(float (&s)[NV], const RowShape& r) {
@@ -181,6 +182,43 @@ __device__ __forceinline__ void group_sum(float (&s)[NV], const RowShape& r) {
         }
     }
 }
+
+// Sums over groups.  Narrow ones: a lane's vectors' sums to shared memory, then its groups' from there, all lanes of a group in the same order.
+template <int NV, bool NARROW> struct Groups {
+    float* buf = nullptr;   // the row's
+    int32_t at[NARROW ? NV : 1], width = 0;   // the groups of a lane's vectors
+    __device__ __forceinline__ Groups(float (&all)[kNormWarps][NARROW ? 32 * NV : 1], const RowShape& r, int sub, int32_t vecs) {
+        if constexpr (NARROW) {
+            width = r.width;   // (above 0)
+            buf = all[threadIdx.x >> 5] + ((threadIdx.x & 31) - sub);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) at[i] = sub + 32 * i < vecs ? (sub + 32 * i) / width : 0;
+        }
+    }
+    __device__ __forceinline__ void sum(float (&s)[NV], const RowShape& r, int sub) const {
+        if constexpr (NARROW) {
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) buf[sub + 32 * i] = s[i];
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) s[i] = buf[at[i] * width];
+            for (int32_t j = 1; j < width; ++j) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) s[i] += buf[at[i] * width + j];
+            }
+        } else group_sum<NV>(s, r);
+    }
+    // a vector's group, and whether it is the group's first
+    __device__ __forceinline__ int32_t of(int i, int32_t v, const RowShape& r) const {
+        if constexpr (NARROW) return at[i];
+        else return r.gshift >= 31 ? 0 : v >> r.gshift;
+    }
+    __device__ __forceinline__ bool first(int i, int32_t v, const RowShape& r) const {
+        if constexpr (NARROW) return v == at[i] * width;
+        else return r.gshift >= 31 ? v == 0 : (v & ((1 << r.gshift) - 1)) == 0;
+    }
+};
 
 __device__ __forceinline__ float row_sum(float t, int lanes) {
 #pragma unroll
@@ -236,7 +274,7 @@ template <int VEC, int NV, bool BACKWARD> struct Params {
     }
 };
 
-template <typename T, int VEC, int NV, bool GENERAL>
+template <typename T, int VEC, int NV, int CUT>
 __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape r) {
     extern __shared__ __align__(16) float params[];   // [2][channels], where they are not held
     const int lane = threadIdx.x & 31, sub = lane & ((1 << r.lanes) - 1), per_warp = 32 >> r.lanes;
@@ -245,6 +283,8 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape
     const T* x = static_cast<const T*>(a.x);
     T* y = static_cast<T*>(a.out);
     const Params<VEC, NV, false> par(a, params, sub, vecs);
+    __shared__ float vector_sums[kNormWarps][CUT == ROW_NARROW ? 32 * NV : 1];
+    const Groups<NV, CUT == ROW_NARROW> groups(vector_sums, r, sub, vecs);
     const int64_t step = (int64_t)gridDim.x * kNormWarps * per_warp;
     constexpr bool kAhead = VEC * NV <= 16;   // the next row is on its way while this one is worked on
     Raw<T, VEC> raw[NV], next[kAhead ? NV : 1];
@@ -269,7 +309,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) f[i][e] = raw[i].get(e);
-        if constexpr (GENERAL) {   // f becomes the normalised value
+        if constexpr (CUT == ROW_MASKS) {   // f becomes the normalised value
             for (int32_t g = 0, lo = 0; g < a.groups; ++g, lo += a.each) {
                 float s = 0.f, q = 0.f;
 #pragma unroll
@@ -296,7 +336,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) s[i] += f[i][e];
             }
-            group_sum<NV>(s, r);
+            groups.sum(s, r, sub);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 s[i] *= inv; q[i] = 0.f;
@@ -305,13 +345,13 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape
                 for (int e = 0; e < VEC; ++e) { f[i][e] -= s[i]; q[i] = fmaf(f[i][e], f[i][e], q[i]); }
                 if (!in) q[i] = 0.f;
             }
-            group_sum<NV>(q, r);
+            groups.sum(q, r, sub);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
                 const float rstd = rsqrtf(q[i] * inv + a.eps);
                 const int32_t v = sub + 32 * i;
-                if (here && v < vecs && (r.gshift >= 31 ? v == 0 : (v & ((1 << r.gshift) - 1)) == 0)) {
-                    const int64_t at = row * a.groups + (r.gshift >= 31 ? 0 : v >> r.gshift);
+                if (here && v < vecs && groups.first(i, v, r)) {
+                    const int64_t at = row * a.groups + groups.of(i, v, r);
                     a.mean[at] = s[i]; a.rstd[at] = rstd;
                 }
 #pragma unroll
@@ -337,7 +377,7 @@ __global__ void __launch_bounds__(kNormThreads) k_norm_rows(NormArgs a, RowShape
 
 // Gradient: dz = dropout(dy) act', then dx = rstd (dz w - mean(dz w) - hat mean(dz w hat)); every lane adds up dz hat and dz of its channels over
 // its rows, every block its lanes', and k_norm_params the blocks'.
-template <typename T, int VEC, int NV, bool GENERAL>
+template <typename T, int VEC, int NV, int CUT>
 __global__ void __launch_bounds__(kNormThreads, VEC * NV <= 8 ? 3 : 1) k_norm_rows_backward(NormArgs a, RowShape r) {
     extern __shared__ __align__(16) float params[];   // [2][channels], where they are not held; then the block's sums [2][channels]
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane & ((1 << r.lanes) - 1), per_warp = 32 >> r.lanes;
@@ -347,6 +387,8 @@ __global__ void __launch_bounds__(kNormThreads, VEC * NV <= 8 ? 3 : 1) k_norm_ro
     const T* d_y = static_cast<const T*>(a.d_y);
     T* d_x = static_cast<T*>(a.out);
     const Params<VEC, NV, true> par(a, params, sub, vecs);
+    __shared__ float vector_sums[kNormWarps][CUT == ROW_NARROW ? 32 * NV : 1];
+    const Groups<NV, CUT == ROW_NARROW> groups(vector_sums, r, sub, vecs);
     float* sums = params + (Params<VEC, NV, true>::kHeld ? 0 : 2 * a.channels);
     float dw[NV][VEC], db[NV][VEC];
 #pragma unroll
@@ -378,7 +420,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC * NV <= 8 ? 3 : 1) k_norm_ro
             float w[VEC], b[VEC];
             par.get(i, in ? v : 0, w, b);
             rstd[i] = 0.f;
-            if constexpr (GENERAL) {   // (every element has statistics of its own)
+            if constexpr (CUT == ROW_MASKS) {   // (every element has statistics of its own)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const int64_t at = row * a.groups + (v * VEC + e) / a.each;
@@ -398,7 +440,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC * NV <= 8 ? 3 : 1) k_norm_ro
             } else {
                 float mean = 0.f;
                 if (in) {
-                    const int64_t at = row * a.groups + (r.gshift >= 31 ? 0 : v >> r.gshift);
+                    const int64_t at = row * a.groups + groups.of(i, v, r);
                     mean = a.mean[at]; rstd[i] = a.rstd[at];
                 }
                 grad_vector<T, VEC>(a, rx[i], rd[i], key, v * VEC, mean, rstd[i], w, b, h[i], g[i]);
@@ -410,7 +452,7 @@ __global__ void __launch_bounds__(kNormThreads, VEC * NV <= 8 ? 3 : 1) k_norm_ro
                 g[i][e] *= w[e];
             }
         }
-        if constexpr (GENERAL) {
+        if constexpr (CUT == ROW_MASKS) {
             for (int32_t q = 0, lo = 0; q < a.groups; ++q, lo += a.each) {
                 float s1 = 0.f, s2 = 0.f;
 #pragma unroll
@@ -434,8 +476,8 @@ __global__ void __launch_bounds__(kNormThreads, VEC * NV <= 8 ? 3 : 1) k_norm_ro
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) { s1[i] += g[i][e]; s2[i] = fmaf(g[i][e], h[i][e], s2[i]); }
             }
-            group_sum<NV>(s1, r);
-            group_sum<NV>(s2, r);
+            groups.sum(s1, r, sub);
+            groups.sum(s2, r, sub);
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll

@@ -595,7 +595,7 @@ void launch_chained(dim3 grid, int threads, cudaStream_t st, void (*kernel)(P...
 }
 
 // what a translation unit of its own per row type launches
-struct RowLaunch { int vec, nv; bool general, backward; int grid; RowShape shape; };
+struct RowLaunch { int vec, nv, cut; bool backward; int grid; RowShape shape; };
 struct TileLaunch { int vec, sums_vec; bool backward; int block_grid, cluster; };   // block_grid: of k_norm_block, or 0
 template <typename T> void launch_dropout(int vec, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t rows, int32_t channels, const DropArgs& d, int grid, cudaStream_t st);
 template <typename T> void launch_rows(const RowLaunch& l, const NormArgs& a, cudaStream_t st);

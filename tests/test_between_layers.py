@@ -287,7 +287,8 @@ def check_norm(ctx, x, samples, groups, kind, drop=None, affine=True, eps=1e-5, 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("rows,channels,groups,pad,shift", [(1, 8, 1, 0, 0), (3, 16, 2, 0, 0), (513, 128, 1, 0, 0), (100, 100, 4, 0, 0), (37, 101, 1, 3, 1), (65, 256, 8, 0, 0),
-                                                            (90, 602, 7, 0, 0), (11, 1024, 32, 8, 0), (9, 2048, 4, 0, 0), (4, 4100, 5, 0, 0), (70, 96, 3, 0, 0), (129, 64, 64, 0, 0)])
+                                                            (90, 602, 7, 0, 0), (11, 1024, 32, 8, 0), (9, 2048, 4, 0, 0), (4, 4100, 5, 0, 0), (70, 96, 3, 0, 0), (129, 64, 64, 0, 0), (133, 768, 32, 0, 0), (60, 192, 16, 0, 0),
+                                                            (19, 1020, 60, 1, 1), (17, 1023, 341, 0, 0), (140, 12, 4, 0, 0), (90, 360, 10, 0, 0)])
 def test_every_row_by_itself(ctx, dtype, rows, channels, groups, pad, shift):
     x = rows_of(rows, channels, TYPES[dtype], 3, pad, shift)
     for i, kind in enumerate(ACTS):
