@@ -552,7 +552,8 @@ typedef struct mg_norm_spec {
 } mg_norm_spec;
 
 /* Bytes of DEVICE memory (16-byte aligned) that the call wants beside its arguments; calls that may run at the same time each want
- * their own. */
+ * their own.  Sums by channel (backward: 8 bytes a channel) are kept by the blocks that work on a call, and by sample only where those are few or
+ * longer than 16 rows: a quarter of the matrix at most. */
 int mg_group_norm_workspace(mg_ctx* ctx, const mg_norm_spec* spec, int backward, size_t* bytes);
 /* mean, rstd: DEVICE [samples, groups], written.  Strides, streams and capture as mg_dropout; y may be x.  Sums are fp32, in an order that
  * does not change from run to run.  Errors: MG_ERR_ARG, MG_ERR_CAPACITY (workspace too small). */

@@ -64,7 +64,7 @@ struct DeviceScope {   // work goes to the context's device; the caller's curren
 // both directions, arguments checked; `m`: the matrices, the output last
 int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices, bool backward, float* mean, float* rstd, float* d_weight, float* d_bias,
              const DropArgs& drop, void* workspace, size_t workspace_bytes, cudaStream_t st) {
-    const size_t need = norm_workspace(s, ctx->n_sms, backward);
+    const size_t need = call_workspace(s, ctx->n_sms, backward);
     if (workspace_bytes < need || (!workspace && need))
         return mg_fail(ctx, MG_ERR_CAPACITY, "the workspace is smaller than mg_group_norm_workspace says");
     DeviceScope on(ctx->device);
@@ -87,7 +87,7 @@ int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices
         MG_BY_TYPE(s->dtype, launch_rows<T>(l, a, st));
         ctx->launches++;
     } else if (mode == NORM_TILES) {
-        plan_tiles(s, ctx->n_sms, backward, vec_width(m, n_matrices, s->dtype, s->rows, a.each), &p, &a);
+        plan_samples(s, ctx->n_sms, backward, vec_width(m, n_matrices, s->dtype, s->rows, a.each), &p, &a);
         a.fan_count = reinterpret_cast<uint32_t*>(ws + p.at_fan_count);
         a.sample_count = reinterpret_cast<uint32_t*>(ws + p.at_sample_count);
         a.tile_parts = reinterpret_cast<float*>(ws + p.at_tile_parts);
@@ -171,7 +171,7 @@ extern "C" int mg_group_norm_workspace(mg_ctx* ctx, const mg_norm_spec* spec, in
     if (!ctx) return MG_ERR_ARG;
     if (!bytes) return mg_fail(ctx, MG_ERR_ARG, "null argument");
     if (int rc = check_norm(ctx, spec)) return rc;
-    *bytes = norm_workspace(spec, ctx->n_sms, backward != 0);
+    *bytes = call_workspace(spec, ctx->n_sms, backward != 0);
     return MG_OK;
 }
 

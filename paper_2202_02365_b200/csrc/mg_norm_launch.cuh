@@ -84,9 +84,22 @@ void launch_block(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
     cudaLaunchKernelEx(&how, kernel, a);   // (an error is found by cudaGetLastError)
 }
 
+template <typename T, int VEC>
+void launch_wide(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
+    if (l.backward) k_norm_wide<T, VEC, true, VEC == 8 ? 1 : 2, kWideBlocks<VEC>><<<l.block_grid, kNormThreads, 0, st>>>(a);
+    else k_norm_wide<T, VEC, false, VEC == 8 ? 2 : 4, 4><<<l.block_grid, kNormThreads, 0, st>>>(a);
+}
+
 template <typename T>
 void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st) {
     constexpr int kTwo = sizeof(T) == 2 ? 2 : 1;
+    if (l.block_grid && !l.cluster) {
+        if (l.vec == 8) launch_wide<T, 8>(l, a, st);
+        else if (l.vec == 4) launch_wide<T, 4>(l, a, st);
+        else if (l.vec == kTwo && kTwo == 2) launch_wide<T, kTwo>(l, a, st);
+        else launch_wide<T, 1>(l, a, st);
+        return;
+    }
     if (l.block_grid) {
         if (l.vec == 8) launch_block<T, 8>(l, a, st);
         else if (l.vec == 4) launch_block<T, 4>(l, a, st);

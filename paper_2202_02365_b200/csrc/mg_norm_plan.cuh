@@ -147,28 +147,40 @@ int blocks_of_sample(int64_t n, int64_t bytes, int n_sms) {
 // tiles of 384 KB for both, 270 so, backward 531 and 512; one sample of 2,000,003 rows of 128, backward, 981 and 844.
 constexpr int64_t kTileBytes = 384 << 10, kPartBytes = 128 << 10, kPartBytesBackward = 512 << 10;
 
-// Samples of several rows.  a: the geometry's part of the arguments.
+TileShape tile_shape(const mg_norm_spec* s, int vec) {
+    TileShape t;
+    const int64_t vecs = s->channels / vec;
+    t.tx = std::min(ceil_log2(kNormThreads), ceil_log2(vecs));
+    t.chunks = (int32_t)((vecs + (1 << t.tx) - 1) >> t.tx);
+    return t;
+}
+
+int64_t longest_sample(const mg_norm_spec* s) {
+    if (!s->sample_offsets) return s->rows_per_sample;
+    int64_t longest = 0;
+    for (int32_t i = 0; i < s->n_samples; ++i) longest = std::max(longest, s->sample_offsets[i + 1] - s->sample_offsets[i]);
+    return longest;
+}
+
+// How many blocks k_norm_block gives a sample, 0 where it does not take the call.
+int sample_blocks(const mg_norm_spec* s, int n_sms, int vec, int64_t longest) {
+    if (tile_shape(s, vec).chunks > 1 || s->channels > kBlockChannels || s->groups > kBlockGroups) return 0;
+    return blocks_of_sample(sample_count(s), longest * s->channels * elem_size(s->dtype), n_sms);
+}
+
+// Samples of several rows, or of a row too wide for a warp.  a: the geometry's part of the arguments.
 void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p, TileArgs* a) {
     p->mode = NORM_TILES; p->vec = vec;
     const int64_t n = sample_count(s), elem = elem_size(s->dtype);
     // (16 bytes a thread let more rows be on their way; with a dropout eight channels share a block of the generator)
     p->sums_vec = backward && s->dropout ? vec : (int)std::min<int64_t>(vec, 16 / elem);
-    const auto shape = [&](int v) {
-        TileShape t;
-        const int64_t vecs = s->channels / v;
-        t.tx = std::min(ceil_log2(kNormThreads), ceil_log2(vecs));
-        t.chunks = (int32_t)((vecs + (1 << t.tx) - 1) >> t.tx);
-        return t;
-    };
-    a->sums = shape(p->sums_vec); a->results = shape(vec);
+    a->sums = tile_shape(s, p->sums_vec); a->results = tile_shape(s, vec);
     a->run = (int32_t)std::min<int64_t>(s->channels, (int64_t)p->sums_vec << a->sums.tx);
     const bool equal = !s->sample_offsets;
-    const int64_t used = equal ? s->rows : s->sample_offsets[n];
-    int64_t longest = equal ? s->rows_per_sample : 0;
-    if (!equal) for (int64_t i = 0; i < n; ++i) longest = std::max(longest, s->sample_offsets[i + 1] - s->sample_offsets[i]);
+    const int64_t used = equal ? s->rows : s->sample_offsets[n], longest = longest_sample(s);
     a->samples = (int32_t)n; a->equal = equal;
     a->rows_per_sample = s->rows_per_sample;
-    if (a->results.chunks == 1 && s->channels <= kBlockChannels && s->groups <= kBlockGroups) p->cluster = blocks_of_sample(n, longest * s->channels * elem, n_sms);
+    p->cluster = sample_blocks(s, n_sms, vec, longest);
     if (p->cluster) {
         p->block_grid = (int)std::min<int64_t>(n, (int64_t)n_sms * 4 / p->cluster) * p->cluster;
         size_t at = 0;
@@ -227,6 +239,36 @@ void plan_tiles(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPl
     p->bytes = at;
 }
 
+// Many short samples that k_norm_block does not take go to k_norm_wide.  Tiles, of which each sample has one at least, would keep sums by channel for
+// every one of them: 200,000 single rows of 2,048 fp32 channels asked for 3.8 GB beside their 1.6, of 4,096 in fp16 for 7.5 GB; here for 7 and 15 MB.  Both
+// sides, tiles / k_norm_wide, forward and backward, us: these two, in 32 groups, 4,399 / 1,940 and 9,127 / 4,997, 5,605 / 3,530 and 14,317 / 11,430; 50,000 fp16
+// rows of 4,095 in one 8,600 / 5,100 and 15,050 / 7,900; 20,000 samples of 8 fp32 rows of 602 in two 880 / 560 and 1,484 / 1,130; 3,000 of 16 fp16 rows of 2,048
+// 148 / 119 and 437 / 320.  Of 30 rows and more tiles are faster (3,000 of 30 of 602: 232 / 295 and 478 / 600), and their sums by channel a quarter of the
+// rows or less; 600 rows of 4,096 took 30 / 21 and 60 / 64, 1,200 of them 46 / 31 and 281 / 101.
+constexpr int64_t kShortRows = 16, kWideBytes = 128 << 20;
+constexpr int kShortSamples = 6, kWideLeastBlocks = 16;   // per SM; in all, whatever kWideBytes says
+bool short_samples(const mg_norm_spec* s, int n_sms) { return sample_count(s) > kShortSamples * (int64_t)n_sms && longest_sample(s) <= kShortRows; }
+
+void plan_wide(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p, TileArgs* a) {
+    p->mode = NORM_TILES; p->vec = p->sums_vec = vec;
+    const int64_t n = sample_count(s), pair = 2 * (int64_t)sizeof(float);
+    a->sums = a->results = tile_shape(s, vec);
+    a->run = (int32_t)std::min<int64_t>(s->channels, (int64_t)vec << a->results.tx);
+    a->samples = (int32_t)n; a->equal = !s->sample_offsets;
+    a->rows_per_sample = s->rows_per_sample;
+    a->tiles = 0; a->tile_rows = 1 << 30; a->tiles_per_sample = 1;
+    p->block_grid = (int)std::min<int64_t>(n, (int64_t)n_sms * (!backward ? 8 : vec == 8 ? kWideBlocks<8> : kWideBlocks<1>));
+    if (backward) p->block_grid = (int)std::min<int64_t>(p->block_grid, std::max<int64_t>(kWideBytes / (pair * s->channels), kWideLeastBlocks));
+    p->cluster = 0;
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 15) / 16 * 16; return was; };
+    p->at_table = take(!a->equal && n > kInlineSamples ? sizeof(int2) * (size_t)(n + 1) : 0);
+    p->at_group_parts = take(backward ? (size_t)(p->block_grid * s->groups * pair) : 0);
+    p->n_parts = backward ? p->block_grid : 0;   // (k_norm_params takes as many in one step)
+    p->at_parts = take((size_t)(p->n_parts * s->channels * pair));
+    p->bytes = at;
+}
+
 // the vector widths that there are kernels for: 32, 16, 8 (16-bit types: 16, 8, 4) and one element
 const int* vec_widths(int dtype) {
     static const int wide[] = {8, 4, 1, 0}, narrow[] = {8, 4, 2, 1, 0};
@@ -239,7 +281,7 @@ int norm_mode(const mg_norm_spec* s) {
     return NORM_TILES;
 }
 
-// whatever the matrices' alignment makes of it
+// what rows, or samples cut as plan_tiles has it, want: the most that the matrices' alignment makes of it
 size_t norm_workspace(const mg_norm_spec* s, int n_sms, bool backward) {
     const int mode = norm_mode(s);
     size_t most = 0;
@@ -249,6 +291,26 @@ size_t norm_workspace(const mg_norm_spec* s, int n_sms, bool backward) {
         TileArgs a;
         if (mode == NORM_ROWS) plan_rows(s, n_sms, backward, *v, &p);
         else plan_tiles(s, n_sms, backward, *v, &p, &a);
+        most = std::max(most, p.bytes);
+    }
+    return most;
+}
+
+// how a call of samples is cut, given its vectors
+void plan_samples(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPlan* p, TileArgs* a) {
+    if (short_samples(s, n_sms) && !sample_blocks(s, n_sms, vec, longest_sample(s))) plan_wide(s, n_sms, backward, vec, p, a);
+    else plan_tiles(s, n_sms, backward, vec, p, a);
+}
+
+// what a call wants, whatever the matrices' alignment makes of it
+size_t call_workspace(const mg_norm_spec* s, int n_sms, bool backward) {
+    if (norm_mode(s) != NORM_TILES || !short_samples(s, n_sms)) return norm_workspace(s, n_sms, backward);
+    size_t most = 0;
+    for (const int* v = vec_widths(s->dtype); *v; ++v) {
+        if (s->channels % *v) continue;
+        NormPlan p;
+        TileArgs a;
+        plan_samples(s, n_sms, backward, *v, &p, &a);
         most = std::max(most, p.bytes);
     }
     return most;

@@ -573,6 +573,102 @@ __global__ void __launch_bounds__(kNormThreads, 2) k_norm_block(const __grid_con
     for (int i = threadIdx.x; i < 2 * a.channels; i += kNormThreads) a.parts[2 * (int64_t)blockIdx.x * a.channels + i] = acc[i];
 }
 
+// Many short samples that k_norm_block does not take (more channels or groups than its shared memory has room for, or rows that alignment cuts into more
+// than one run of vectors): a block goes through a sample by itself, run after run of its channels, twice.  What groups and channels add up to lies in
+// memory, by block and not by sample: a group that a run's end cuts is added up in the sample's statistics (backward: in the block's own place), the
+// gradients of weight and bias in the block's part.
+template <int VEC> constexpr int kWideBlocks = VEC == 8 ? 2 : 3;   // per SM, backward: what registers leave room for
+
+template <typename T, int VEC, bool BACKWARD, int K, int MINB>
+__global__ void __launch_bounds__(kNormThreads, MINB) k_norm_wide(const __grid_constant__ TileArgs a) {
+    __shared__ __align__(16) float su[kNormThreads * VEC], sv[kNormThreads * VEC], sw[BACKWARD ? kNormThreads * VEC : 4], sb[BACKWARD ? kNormThreads * VEC : 4];
+    __shared__ float sn[kNormThreads];
+    const int tx = threadIdx.x & ((1 << a.results.tx) - 1), ty = threadIdx.x >> a.results.tx, n_ty = kNormThreads >> a.results.tx;
+    float* const sums = BACKWARD ? a.group_parts + 2 * (int64_t)blockIdx.x * a.groups : nullptr;
+    float* const part = BACKWARD && a.parts ? a.parts + 2 * (int64_t)blockIdx.x * a.channels : nullptr;
+    bool first = true;
+    for (int32_t s = (int32_t)blockIdx.x; s < a.samples; s += (int32_t)gridDim.x) {
+        Tile t;
+        t.sample = s;
+        t.row0 = a.equal ? s * a.rows_per_sample : sample_entry(a, s).x;
+        t.row1 = a.equal ? t.row0 + a.rows_per_sample : sample_entry(a, s + 1).x;
+        const int64_t stat = (int64_t)s * a.groups;
+        const float rows = (float)(t.row1 - t.row0), values = rows * (float)a.each;
+        if (t.row0 == t.row1) {
+            for (int32_t g = threadIdx.x; !BACKWARD && g < a.groups; g += kNormThreads) { a.mean[stat + g] = 0.f; a.rstd[stat + g] = 0.f; }
+            continue;
+        }
+        float* const u_at = BACKWARD ? sums : a.mean + stat;
+        float* const v_at = BACKWARD ? sums + a.groups : a.rstd + stat;
+        for (int32_t c0 = 0; c0 < a.channels; c0 += a.run) {
+            const int32_t c1 = min(c0 + a.run, a.channels), c = c0 + tx * VEC;
+            const bool in = c < c1;
+            float mean = 0.f, rstd = 0.f;
+            __syncthreads();   // (shared memory has been read)
+            if (BACKWARD) {
+                const int64_t at = stat + (in ? c / a.each : 0);
+                mean = a.mean[at]; rstd = a.rstd[at];
+                share_params(a, t, sw, sb, c0, c1 - c0);
+            }
+            Pair<VEC> p;
+            tile_sums<T, VEC, BACKWARD, K>(a, t, c, in, ty, n_ty, mean, rstd, sw + tx * VEC, sb + tx * VEC, p);
+            float pu[BACKWARD ? VEC : 1], pv[BACKWARD ? VEC : 1];   // (what the part has: on its way while the block's threads meet)
+            if (BACKWARD && part) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const int i = threadIdx.x + j * kNormThreads;
+                    pu[j] = pv[j] = 0.f;
+                    if (!first && i < c1 - c0) { pu[j] = part[c0 + i]; pv[j] = part[a.channels + c0 + i]; }
+                }
+            }
+            block_pairs<VEC, BACKWARD>(p, su, sv, sn, a.results.tx, c1 - c0);
+            if (BACKWARD && part) {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const int i = threadIdx.x + j * kNormThreads;
+                    if (i < c1 - c0) { part[c0 + i] = pu[j] + su[i]; part[a.channels + c0 + i] = pv[j] + sv[i]; }
+                }
+            }
+            run_groups<BACKWARD>(a, su, sv, c0, c1, rows, [&](int32_t g, float u, float v) {
+                const int32_t before = c0 - g * a.each;   // channels of the group in the runs before
+                if (before > 0) {
+                    float n = rows * (float)before, m = u_at[g], q = v_at[g];
+                    if (BACKWARD) { m += u; q += v; }
+                    else merge_moments(n, m, q, rows * (float)shared_channels(a, g, c0, c1), u, v);
+                    u = m; v = q;
+                }
+                u_at[g] = u; v_at[g] = v;
+            });
+        }
+        __syncthreads();
+        for (int32_t g = threadIdx.x; g < a.groups; g += kNormThreads) {
+            if (BACKWARD) { const float u = u_at[g]; u_at[g] = v_at[g] / values; v_at[g] = u / values; }   // mean of dz w, mean of dz w hat
+            else v_at[g] = rsqrtf(v_at[g] / values + a.eps);
+        }
+        __syncthreads();
+        for (int32_t c0 = 0; c0 < a.channels; c0 += a.run) {
+            const int32_t c = c0 + tx * VEC;
+            if (BACKWARD && a.run < a.channels) {   // (a single run's are still there)
+                __syncthreads();
+                share_params(a, t, sw, sb, c0, min(a.run, a.channels - c0));
+            }
+            if (c >= min(c0 + a.run, a.channels)) continue;
+            const int32_t group = c / a.each;
+            float w[VEC], b[VEC];
+            const float mean = a.mean[stat + group], rstd = a.rstd[stat + group];
+            if (!BACKWARD) {
+                load_params<VEC>(a.weight, c, 1.f, w);
+                load_params<VEC>(a.bias, c, 0.f, b);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) w[e] *= rstd;
+            }
+            tile_results<T, VEC, BACKWARD, K>(a, t, c, ty, n_ty, mean, rstd, BACKWARD ? u_at[group] : 0.f, BACKWARD ? v_at[group] : 0.f, w, b, sw + tx * VEC, sb + tx * VEC);
+        }
+        first = false;
+    }
+    for (int32_t i = threadIdx.x; part && first && i < 2 * a.channels; i += kNormThreads) part[i] = 0.f;   // (none of its samples has a row)
+}
+
 // Samples without rows have no tiles: their statistics are zero.
 template <typename = void>
 __global__ void k_norm_empty(const __grid_constant__ TileArgs a) {
@@ -596,7 +692,7 @@ void launch_chained(dim3 grid, int threads, cudaStream_t st, void (*kernel)(P...
 
 // what a translation unit of its own per row type launches
 struct RowLaunch { int vec, nv, cut; bool backward; int grid; RowShape shape; };
-struct TileLaunch { int vec, sums_vec; bool backward; int block_grid, cluster; };   // block_grid: of k_norm_block, or 0
+struct TileLaunch { int vec, sums_vec; bool backward; int block_grid, cluster; };   // block_grid: of k_norm_block, or (no blocks to a sample's cluster) of k_norm_wide, or 0
 template <typename T> void launch_dropout(int vec, const void* x, int64_t x_stride, void* y, int64_t y_stride, int64_t rows, int32_t channels, const DropArgs& d, int grid, cudaStream_t st);
 template <typename T> void launch_rows(const RowLaunch& l, const NormArgs& a, cudaStream_t st);
 template <typename T> void launch_tiles(const TileLaunch& l, const TileArgs& a, cudaStream_t st);
