@@ -303,7 +303,8 @@ int mg_model_set_aggregator(mg_model* m, int aggregator);
  * so this is an option, not the default (the paper stores 4-byte floats).  Takes effect when every layer runs in the
  * fused tensor-core kernel (MG_GEMM_TF32, widths <= 256), the intermediate widths are multiples of 128, the mean
  * aggregator is used, the weights suit fp16 (largest magnitude below 2^15, root mean square above 2^-10) and
- * mg_keep_layer_outputs is off; otherwise the call is accepted and fp32 is used.  Errors: MG_ERR_ARG. */
+ * mg_keep_layer_outputs is off, and the model has neither a norm nor a dropout between its layers; otherwise the call is accepted and fp32 is
+ * used.  Errors: MG_ERR_ARG. */
 int mg_model_set_intermediates(mg_model* m, int dtype);
 int mg_model_free(mg_model* m);
 
@@ -319,7 +320,8 @@ int mg_forward(mg_ctx* ctx, const mg_model* m, mg_dense* d, float* out, int out_
  * before the next starts, and H^1..H^{k-1} stay available for mg_layer_output.  mini_batches = w > 0: the
  * layers run over windows of w consecutive mini-batches through small reused buffers, so that a layer's
  * output is read back from L2 instead of DRAM; H^k is the same, the intermediate layers are not kept.
- * Only the fused tensor-core layers (MG_GEMM_TF32, widths <= 256) use windows. */
+ * Only the fused tensor-core layers (MG_GEMM_TF32, widths <= 256) use windows, and only where nothing lies between them: a model with a norm or a dropout
+ * (mg_model_set_norm, mg_model_set_dropout) runs every layer over all mini-batches, and needs the memory for it. */
 int mg_set_layer_window(mg_ctx* ctx, int32_t mini_batches);
 /* enable = 1 forces the whole-layer schedule whatever the window, so that mg_layer_output and mg_backward work.  With MG_GEMM_TF32 the forward
  * pass then also leaves, to save mg_backward work, a bit per intermediate output and, for the rows of later layers with more than three
@@ -552,8 +554,8 @@ typedef struct mg_norm_spec {
 } mg_norm_spec;
 
 /* Bytes of DEVICE memory (16-byte aligned) that the call wants beside its arguments; calls that may run at the same time each want
- * their own.  Sums by channel (backward: 8 bytes a channel) are kept by the blocks that work on a call, and by sample only where those are few or
- * longer than 16 rows: a quarter of the matrix at most. */
+ * their own.  Backward, sums by channel are kept, 8 bytes a channel, by the blocks that work on the call; and by sample where samples are longer than 16
+ * rows (a quarter of the matrix or less), or no more than six for each multiprocessor, or offsets cut long and short ones. */
 int mg_group_norm_workspace(mg_ctx* ctx, const mg_norm_spec* spec, int backward, size_t* bytes);
 /* mean, rstd: DEVICE [samples, groups], written.  Strides, streams and capture as mg_dropout; y may be x.  Sums are fp32, in an order that
  * does not change from run to run.  Errors: MG_ERR_ARG, MG_ERR_CAPACITY (workspace too small). */
@@ -576,14 +578,15 @@ int mg_group_norm_backward(mg_ctx* ctx, const mg_norm_spec* spec, const void* x,
  * used).  `groups` must divide dims[1] .. dims[k-1].  weight[l], bias[l], l = 0 .. k-2: HOST [dims[l + 1]] (copied; a null array or entry stands for
  * ones, zeros).  The statistics are of fp32 rows: a layer's output and the normalised one are both kept where mg_keep_layer_outputs asks
  * for it, else the one takes the other's place.  mg_backward goes through the norm; mg_model_sgd_step and mg_model_adagrad_step step its weights
- * and biases too.  A forward pass before the call can no longer be followed by mg_backward.  Errors: MG_ERR_ARG, MG_ERR_OOM. */
+ * and biases too.  A forward pass before the call can no longer be followed by mg_backward.  With a norm, windows of layers (mg_set_layer_window) and fp16
+ * intermediates (mg_model_set_intermediates) are not used, and mg_forward_noalloc refuses the model.  Errors: MG_ERR_ARG, MG_ERR_OOM. */
 #define MG_NORM_NONE 0
 #define MG_NORM_ROWS 1
 #define MG_NORM_BATCH 2
 int mg_model_set_norm(mg_model* m, int norm, int32_t groups, float eps, int activation, const float* const* weight, const float* const* bias);
 /* Dropout of every H^l, 1 <= l < k, from the next forward pass on: mg_dropout with the site l and the row keys (mini-batch << 32) + node id, so
  * that the mask of a sample does not go by the order its nodes were found in.  p = 0: none (evaluation); a training loop gives every step a seed
- * of its own.  mg_backward uses what its forward pass used.  Errors: MG_ERR_ARG. */
+ * of its own.  mg_backward uses what its forward pass used.  While p > 0, windows, fp16 intermediates and mg_forward_noalloc are as with a norm.  Errors: MG_ERR_ARG. */
 int mg_model_set_dropout(mg_model* m, double p, uint64_t seed);
 /* DEVICE pointers to the gradients of the norm behind layer `layer` (1 .. k-1) that the last mg_backward left: [dims[layer]] each, owned by the model.
  * Errors: MG_ERR_ARG, MG_ERR_STATE (no norm, no backward pass). */

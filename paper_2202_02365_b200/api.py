@@ -349,7 +349,8 @@ class Model(_Owned):
                                            C.c_int(precision), C.byref(self.handle)))
 
     def set_intermediates(self, dtype):
-        """torch.float16: keep H^1 .. H^{k-1} as fp16 inside forward (where the model allows it); torch.float32: default."""
+        """torch.float16: keep H^1 .. H^{k-1} as fp16 inside forward (where the model allows it: not with a norm or a dropout between the layers);
+        torch.float32: default."""
         code = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16}[dtype]
         self.ctx._check(self.ctx.lib.mg_model_set_intermediates(self.handle, C.c_int(code)))
 
@@ -359,7 +360,8 @@ class Model(_Owned):
 
     def set_norm(self, over: str | None, groups: int = 1, weights=None, biases=None, eps: float = 1e-5, activation: str = "relu"):
         """After every layer but the last: group norm over every node's row by itself (over="rows"), or over a mini-batch's rows ("batch"), with
-        an activation.  weights, biases: a host tensor per layer but the last, or None for ones and zeros.  over=None: the plain ReLU again."""
+        an activation.  weights, biases: a host tensor per layer but the last, or None for ones and zeros.  over=None: the plain ReLU again.  With a
+        norm, windows of layers (set_layer_window) and fp16 intermediates (set_intermediates) are not used, and forward_noalloc refuses the model."""
         n = len(self.dims) - 2
         keep, arrs = [], []
         for given in (weights, biases):
@@ -376,7 +378,8 @@ class Model(_Owned):
                                                        C.c_int(ACTIVATIONS[activation]), arrs[0], arrs[1]))
 
     def set_dropout(self, p: float, seed: int = 0):
-        """Dropout of every layer's output but the last's, from the next forward pass on; p = 0: none."""
+        """Dropout of every layer's output but the last's, from the next forward pass on; p = 0: none.  While p > 0, windows, fp16 intermediates and
+        forward_noalloc are as with a norm."""
         self.ctx._check(self.ctx.lib.mg_model_set_dropout(self.handle, C.c_double(p), C.c_uint64(int(seed) & 0xFFFFFFFFFFFFFFFF)))
 
     def norm_grads(self):
@@ -647,6 +650,8 @@ class Context:
         return out
 
     def set_layer_window(self, mini_batches: int):
+        """Layers over windows of so many mini-batches at a time, 0: over all of them; models with a norm or a dropout between their layers take
+        them all at once."""
         self._check(self.lib.mg_set_layer_window(self.handle, C.c_int32(mini_batches)))
 
     def keep_layer_outputs(self, on: bool = True):
@@ -703,7 +708,7 @@ class Context:
     # -- between two layers
     def dropout(self, x: torch.Tensor, drop: Dropout, out: torch.Tensor | None = None) -> torch.Tensor:
         """x [..., channels] with the elements that `drop` names zeroed and the others scaled up, queued on torch's current stream.  out:
-        where to (x itself, say), else a new tensor."""
+        where to (x itself, say), else a new tensor.  torch's autograd does not see the call: its gradient is dropout_backward."""
         x, x_stride = _matrix(x, self.device)
         out, out_stride = _result(out, x)
         channels = x.shape[-1]
@@ -752,7 +757,8 @@ class Context:
         """dropout(activation(norm(x) * weight + bias)), the mean and the reciprocal deviation [samples, groups].  x is [rows, channels]:
         every row is a sample by itself or, with sample_offsets (host; first rows and the end of the last), samples lie one behind the
         other, mini-batches of a packed layer, say; or x is [samples, ..., channels].  activation: "none", "relu", "silu" or "gelu".  Rows
-        behind the last sample stay as they are in `out`, and are zero in a new tensor."""
+        behind the last sample stay as they are in `out`, and are zero in a new tensor.  (Samples of a shape without rows, [4, 0, 8], are none: their
+        statistics are [0, groups].)  torch's autograd does not see the call: its gradients are group_norm_backward's."""
         x, x_stride = _matrix(x, self.device)
         spec, samples, end, held = self._norm_spec(x, groups, weight, bias, sample_offsets, eps, activation, dropout)
         work, need = self._norm_workspace(spec, 0)

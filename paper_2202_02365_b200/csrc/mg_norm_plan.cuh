@@ -114,8 +114,10 @@ void plan_rows(const mg_norm_spec* s, int n_sms, bool backward, int vec, NormPla
     p->nv = 1 << ceil_log2((vecs + 31) / 32);
     const int64_t width = each / vec;
     // Groups of other widths than a power of two, us forward / backward.  Narrow ones of whole vectors meet in shared memory: 100,000 fp32 rows of 768 in 32
-    // groups 115 / 276 (under masks 1,812 / 2,749), 200,000 of 192 in 16 67 / 124 (591 / 762).  Wide ones, where that takes a lane as many reads as a group
-    // has vectors, are few: under masks 200,000 of 602 in 2 take 831 / 2,480.
+    // groups 115 / 276 (under masks 1,812 / 2,749), 200,000 of 192 in 16 67 / 124 (591 / 762).  Under masks, one after the other: wide ones, where shared memory
+    // takes a lane as many reads as a group has vectors, and all that are not whole vectors, narrow or many as they may be.  That costs what the groups' number
+    // and the row's values multiply to: 200,000 fp32 rows of 602 in 2 545 / 2,104 with a ReLU, of 100 in 4 176 / 288, of 300 in 10 1,198 / 2,493, of 320 in 32
+    // 2,128 / 3,256 (their bytes 147 / 220, 24 / 37, 73 / 110, 78 / 117); backward also a division and two loads of statistics for every value.
     if (s->groups > 1 && (each % vec || (width & (width - 1)))) p->cut = each % vec == 0 && width < 2 * vec * s->groups ? ROW_NARROW : ROW_MASKS;
     p->shape.width = p->cut == ROW_NARROW ? (int32_t)width : 0;
     p->shape.gshift = s->groups == 1 ? 31 : ceil_log2(std::max<int64_t>(width, 1));
