@@ -2,8 +2,8 @@
 //
 // What fits: a block, or a cluster of blocks, sums a sample up and computes its results in one launch (k_norm_block; k_norm_wide for many short samples that it
 // does not take).  The rest: two launches.  Tiles of rows are summed up, the last block of a sample's tiles brings its sums together (no block waits for
-// another), and the second launch computes the results from the rows once more.  It reads them from memory: of 91 MB and more, 95 to 99 % come from DRAM
-// again, of 67 MB of fp16 maps two thirds, whether it begins with the tiles that were summed up last or with the first (the same time to half a percent).  Sums are
+// another), and the second launch computes the results from the rows once more.  It reads most of them from memory again: of 185 MB and more 93 to 100 % come
+// from DRAM, of 93 MB 75 to 98, of 67 MB of fp16 maps 37 to 65; to begin with the tiles that were summed up last takes the same time to half a percent.  Sums are
 // means and squares about them, merged pairwise by Chan, Golub and LeVeque's formulas: a mean that is k deviations from zero costs the variance the digits
 // of k, not of its square; for the gradient, plain sums of dz and dz hat.
 //
