@@ -40,7 +40,7 @@ extern "C" {
 
 #define MG_DTYPE_F32 0
 #define MG_DTYPE_F16 1
-#define MG_DTYPE_BF16 2 /* rows of mg_dropout and mg_group_norm; feature tables are fp32 or fp16 */
+#define MG_DTYPE_BF16 2 /* rows of mg_dropout and mg_group_norm, of rows by id, and logits; feature tables are fp32 or fp16 */
 
 #define MG_BACKING_HBM 0  /* the whole feature table lives in device memory */
 #define MG_BACKING_HOST 1 /* the table stays in (preferably pinned) host memory; only the
@@ -591,6 +591,92 @@ int mg_model_set_dropout(mg_model* m, double p, uint64_t seed);
 /* DEVICE pointers to the gradients of the norm behind layer `layer` (1 .. k-1) that the last mg_backward left: [dims[layer]] each, owned by the model.
  * Errors: MG_ERR_ARG, MG_ERR_STATE (no norm, no backward pass). */
 int mg_model_norm_grads(const mg_model* m, int32_t layer, const float** d_weight, const float** d_bias);
+
+/* ---- rows by id: learned rows, relation embeddings ------------------------------------------- */
+
+/* y[i] = scale * table[ids[i]], i = 0 .. n - 1, computed in fp32 and rounded once; zero where ids[i] is not in [0, n_rows): -1, say, where a batch is
+ * padded.  Rows are table_stride / y_stride elements apart, of table_dtype / y_dtype (MG_DTYPE_*); ids are int32 or (ids_are_i64) int64.  DEVICE
+ * pointers, aligned to their elements; y lies apart from the table, its rows do not overlap.  Rows of whole 16-byte pieces are fastest.  One kernel,
+ * queued on `stream` (a cudaStream_t of the context's device; NULL = the default stream), not waited for; it may be captured into a graph.
+ * Errors: MG_ERR_ARG (2^31 rows or ids or more among them). */
+int mg_embedding(mg_ctx* ctx, const void* table, int64_t table_stride, int table_dtype, int64_t n_rows, int32_t dim, const void* ids, int ids_are_i64,
+                 int64_t n, float scale, void* y, int64_t y_stride, int y_dtype, void* stream);
+
+/* The places of each id, by which the gradient of mg_embedding is summed up: order = the places 0 .. n - 1 by ascending id, equal ones by ascending place,
+ * those of ids outside [0, n_rows) behind all others; group_ids = the distinct ids in ascending order (of the type of ids); starts[g] .. starts[g + 1] =
+ * where the places of group_ids[g] lie in order; *n_groups = how many there are.  All DEVICE: order [n] int32, group_ids [min(n, n_rows)],
+ * starts [min(n, n_rows) + 1] int32, n_groups one int32; behind the last group, group_ids and starts stay as they were.  A program that looks the same
+ * ids up in several tables, or takes several gradients, keeps them.  Streams, capture and errors as mg_embedding; MG_ERR_CAPACITY: the workspace (DEVICE,
+ * 16-byte aligned, one for each call that may run at the same time) is smaller than mg_id_groups_workspace says.  Where a bounded wait on the device runs
+ * out (nothing that is known of makes it), *n_groups is -1: no group is to be used, and mg_embedding_backward writes none. */
+int mg_id_groups_workspace(mg_ctx* ctx, int64_t n, int64_t n_rows, size_t* bytes);
+int mg_id_groups(mg_ctx* ctx, const void* ids, int ids_are_i64, int64_t n, int64_t n_rows, int32_t* order, void* group_ids, int32_t* starts,
+                 int32_t* n_groups, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradient of mg_embedding: for every group g the sum of scale * d_y[i] over its places, in fp32 and in an order that does not change from run to run
+ * (no float is added atomically), rounded once to out_dtype, into
+ *   MG_ROWS_TABLE    row group_ids[g] of `out`, which has n_rows rows; every other row is set to zero
+ *   MG_ROWS_ADD      the same, added to what is there; other rows are neither read nor written
+ *   MG_ROWS_COMPACT  row g of `out`, which has min(n, n_rows) rows; those behind the last group stay as they were
+ * order .. n_groups as mg_id_groups left them for this n and n_rows (DEVICE; read by the kernels).  `out` lies apart from d_y, its rows do not overlap.
+ * Streams, capture, workspace and errors as mg_id_groups. */
+#define MG_ROWS_TABLE 0
+#define MG_ROWS_ADD 1
+#define MG_ROWS_COMPACT 2
+int mg_embedding_backward_workspace(mg_ctx* ctx, int64_t n, int64_t n_rows, int32_t dim, size_t* bytes);
+int mg_embedding_backward(mg_ctx* ctx, const void* d_y, int64_t d_y_stride, int d_y_dtype, int64_t n, int64_t n_rows, int32_t dim, float scale,
+                          const int32_t* order, const void* group_ids, int ids_are_i64, const int32_t* starts, const int32_t* n_groups, int into,
+                          void* out, int64_t out_stride, int out_dtype, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- losses of a layer's output: log probabilities, distillation ------------------------------ */
+
+/* Rows of logits: z = scale * x, x of `rows` x `classes` values, rows `stride` elements apart.  Everything is computed in fp32: m = the row's largest z,
+ * lse = m + log sum exp(z - m), log p_j = z_j - lse.  A logit of -infinity is a class that is not allowed.  A row that allows none has lse = -infinity, entropy 0
+ * and log probabilities of -infinity; one with a NaN or +infinity has NaN for all of them.  (So has one that scale carries beyond fp32.) */
+typedef struct mg_logits {
+    const void* x;           /* DEVICE, aligned to its elements */
+    int64_t stride, rows;
+    int32_t classes;         /* 1 .. 2^28 */
+    int32_t dtype;           /* MG_DTYPE_* */
+    float scale;             /* 1 / temperature: positive and finite */
+} mg_logits;
+
+#define MG_MAX_TOP 32
+
+/* Of every row: log_prob = log p of its label (labels: int32 or, labels_are_i64, int64; a label outside [0, classes), -100 say, is none: log_prob 0), the
+ * entropy -sum p log p, lse, and the `top` (0 .. MG_MAX_TOP, no more than there are classes) likeliest classes, the likeliest first, equal ones by ascending
+ * class, NaN before all: top_ids and top_log_probs [rows, top].  All DEVICE; labels, log_prob (which wants labels), entropy, lse, top_ids and top_log_probs are
+ * nullable.  One kernel; streams, capture and errors as mg_dropout. */
+int mg_log_probs(mg_ctx* ctx, const mg_logits* logits, const void* labels, int labels_are_i64, int32_t top, float* log_prob, float* entropy, float* lse,
+                 int32_t* top_ids, float* top_log_probs, void* stream);
+/* Gradient with respect to x of a scalar loss, from those with respect to log_prob (g), entropy (h) and lse (l), each nullable (zero):
+ *   d_x_j = scale (g [j = label] + p_j (l - g - h (log p_j + entropy))),  g of a row without a label 0,
+ * with the forward call's lse and (where h is given) entropy.  A row whose gradients are all zero, or that allows no class, gets zeros, whatever it holds.
+ * d_x is of the logits' type; it may be x with the same stride, or lie apart from it. */
+int mg_log_probs_backward(mg_ctx* ctx, const mg_logits* logits, const float* lse, const void* labels, int labels_are_i64, const float* d_log_prob,
+                          const float* entropy, const float* d_entropy, const float* d_lse, void* d_x, int64_t d_x_stride, void* stream);
+
+#define MG_MAX_TEACHER 1024
+
+/* A teacher's top logits: row r has up to `entries` pairs of a class and a logit; a class outside [0, classes), -1 say, is no pair.  q = softmax over the
+ * row's pairs of scale * value (the scale of the logits) or, with `lse`, exp(scale * value - lse[r]): probabilities of the whole of the teacher's
+ * classes, which need not sum up to one.  mg_log_probs's top_ids and top_log_probs are such pairs. */
+typedef struct mg_teacher {
+    const void* ids;         /* DEVICE [rows, entries], int32 or (ids_are_i64) int64, rows ids_stride elements apart */
+    const void* values;      /* DEVICE [rows, entries] of `dtype`, rows values_stride elements apart */
+    const float* lse;        /* DEVICE [rows], nullable */
+    int64_t ids_stride, values_stride;
+    int32_t ids_are_i64, dtype;
+    int32_t entries;         /* 1 .. MG_MAX_TEACHER */
+} mg_teacher;
+
+/* loss = sum over the row's pairs of q (log q - log p[class]), zero where there is none or q is zero; lse (nullable) as mg_log_probs's.  One kernel; streams,
+ * capture and errors as mg_dropout. */
+int mg_distill(mg_ctx* ctx, const mg_logits* logits, const mg_teacher* teacher, float* loss, float* lse, void* stream);
+/* Gradient with respect to x from the loss's: d_x_j = scale d_loss (p_j sum q - sum of the q of the pairs that name j), with the forward call's lse.  A row
+ * without pairs, with d_loss zero, or that allows no class gets zeros, whatever it holds.  d_x as mg_log_probs_backward's. */
+int mg_distill_backward(mg_ctx* ctx, const mg_logits* logits, const float* lse, const mg_teacher* teacher, const float* d_loss, void* d_x,
+                        int64_t d_x_stride, void* stream);
 
 /* ---- COMET: partition replacement for link prediction out of core (Section 5.1, Section 6) ----
  * Host-side planning only; no context, no device work.  Partition ids are the physical partitions of

@@ -25,7 +25,7 @@ DTYPE_F32, DTYPE_F16, DTYPE_BF16 = 0, 1, 2
 BACKING_HBM, BACKING_HOST = 0, 1
 GEMM_TF32, GEMM_FP32 = 0, 1
 CORRUPT_DST, CORRUPT_SRC, CORRUPT_BOTH = 1, 2, 3
-ROW_TYPES = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}      # of dropout and group_norm
+ROW_TYPES = {torch.float32: DTYPE_F32, torch.float16: DTYPE_F16, torch.bfloat16: DTYPE_BF16}      # of dropout, group_norm, rows by id and logits
 ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 
 # every symbol include/mgdense.h declares
@@ -37,6 +37,8 @@ EXPORTS = [
     "mg_distmult_score", "mg_kernel_launches", "mg_profile", "mg_profile_read", "mg_comet_plan", "mg_comet_bias", "mg_comet_autotune", "mg_gat_model_create", "mg_gat_model_set_heads", "mg_gat_model_free", "mg_gat_forward", "mg_backward", "mg_backward_begin", "mg_backward_end", "mg_model_grads", "mg_model_sgd_step", "mg_model_adagrad_step", "mg_dense_packed_ids", "mg_apply_embedding_sgd",
     "mg_dropout", "mg_group_norm_workspace", "mg_group_norm", "mg_group_norm_backward",
     "mg_model_set_norm", "mg_model_set_dropout", "mg_model_norm_grads",
+    "mg_embedding", "mg_id_groups_workspace", "mg_id_groups", "mg_embedding_backward_workspace", "mg_embedding_backward",
+    "mg_log_probs", "mg_log_probs_backward", "mg_distill", "mg_distill_backward",
 ]
 
 
@@ -67,6 +69,15 @@ class NormSpec(C.Structure):
                 ("weight", C.c_void_p), ("bias", C.c_void_p), ("dropout", C.c_void_p)]
 
 
+class LogitsSpec(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("stride", C.c_int64), ("rows", C.c_int64), ("classes", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
+
+
+class TeacherSpec(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("values", C.c_void_p), ("lse", C.c_void_p), ("ids_stride", C.c_int64), ("values_stride", C.c_int64),
+                ("ids_are_i64", C.c_int32), ("dtype", C.c_int32), ("entries", C.c_int32)]
+
+
 _lib = None
 _views = None           # the native part of the binding (csrc/mg_views.cpp), False where it was not built ...
 _export_copy = 0        # ... and the entry point it calls
@@ -88,6 +99,15 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         _lib.mg_group_norm_workspace.argtypes = [p, p, C.c_int, p]
         _lib.mg_group_norm.argtypes = [p, p, p, i64, p, i64, p, p, p, C.c_size_t, p]
         _lib.mg_group_norm_backward.argtypes = [p, p, p, i64, p, i64, p, p, p, i64, p, p, p, C.c_size_t, p]
+        _lib.mg_embedding.argtypes = [p, p, i64, C.c_int, i64, i32, p, C.c_int, i64, C.c_float, p, i64, C.c_int, p]
+        _lib.mg_id_groups_workspace.argtypes = [p, i64, i64, p]
+        _lib.mg_id_groups.argtypes = [p, p, C.c_int, i64, i64, p, p, p, p, p, C.c_size_t, p]
+        _lib.mg_embedding_backward_workspace.argtypes = [p, i64, i64, i32, p]
+        _lib.mg_embedding_backward.argtypes = [p, p, i64, C.c_int, i64, i64, i32, C.c_float, p, p, C.c_int, p, p, C.c_int, p, i64, C.c_int, p, C.c_size_t, p]
+        _lib.mg_log_probs.argtypes = [p, p, p, C.c_int, i32, p, p, p, p, p, p]
+        _lib.mg_log_probs_backward.argtypes = [p, p, p, p, C.c_int, p, p, p, p, p, i64, p]
+        _lib.mg_distill.argtypes = [p, p, p, p, p, p]
+        _lib.mg_distill_backward.argtypes = [p, p, p, p, p, p, i64, p]
     return _lib
 
 
@@ -237,6 +257,48 @@ def _result(out: torch.Tensor | None, like: torch.Tensor):
     assert out.device == like.device and out.shape == like.shape and out.dtype == like.dtype, "out: a tensor like the input"
     assert (out.shape[-1] <= 1 or out.stride(-1) == 1) and (out.dim() == 2 or out.is_contiguous()), "out: channels one behind the other"
     return out, out.stride(0) if out.dim() == 2 else out.shape[-1]
+
+
+ROWS_TABLE, ROWS_ADD, ROWS_COMPACT = 0, 1, 2
+
+
+@dataclass(frozen=True)
+class IdGroups:
+    """The places of each id (Context.id_groups): `order` has them by ascending id, `ids` the distinct ids, `starts` where each one's places lie in
+    order, `count` (one element, on the device) how many ids there are; `ids` and `starts` mean nothing behind it."""
+    order: torch.Tensor
+    ids: torch.Tensor
+    starts: torch.Tensor
+    count: torch.Tensor
+    n_rows: int
+
+
+@dataclass(frozen=True)
+class LogProbs:
+    """What Context.log_probs gives, a value (top_ids, top_log_probs: `top` of them) for each row of logits; None for what was not asked for."""
+    log_prob: torch.Tensor | None
+    entropy: torch.Tensor
+    lse: torch.Tensor
+    top_ids: torch.Tensor | None
+    top_log_probs: torch.Tensor | None
+
+
+def _ids(t: torch.Tensor, device: torch.device, what: str = "ids"):
+    """Whole numbers as the library takes them: contiguous, and whether they have 64 bits."""
+    assert t.device == device and t.dtype in (torch.int32, torch.int64), f"{what}: a CUDA tensor of int32 or int64, on the context's device"
+    return t.contiguous(), t.dtype == torch.int64
+
+
+def _by_row(t: torch.Tensor | None, shape, device: torch.device, what: str):
+    """A float32 value for every row, or None."""
+    if t is None:
+        return None
+    assert t.device == device and t.dtype == torch.float32 and t.shape == shape, f"{what}: a float32 value for each row, on the context's device"
+    return t.contiguous()
+
+
+def _at(t: torch.Tensor | None):
+    return t.data_ptr() if t is not None else None
 
 
 @dataclass
@@ -792,3 +854,165 @@ class Context:
         if new and end is not None and end < x.shape[0]:
             out[end:].zero_()
         return out, d_weight, d_bias
+
+    # -- rows by id
+    def embedding(self, table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0, dtype: torch.dtype | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+        """scale * table[ids], [*ids.shape, dim], zero where an id is no row of the table (-1, say, in a padded batch), queued on torch's current stream.
+        dtype: of the result, else the table's.  torch's autograd does not see the call: its gradients are embedding_backward's."""
+        assert table.dim() == 2, "a table [rows, dim]"
+        table, stride = _matrix(table, self.device)
+        ids, wide = _ids(ids, self.device)
+        rows, dim = table.shape
+        shape = (*ids.shape, dim)
+        if out is None:
+            out = torch.empty(shape, dtype=dtype or table.dtype, device=self.device)
+        assert out.device == self.device and out.shape == shape and out.dtype in ROW_TYPES and out.dtype == (dtype or out.dtype), "out: a CUDA tensor [*ids.shape, dim]"
+        assert (dim <= 1 or out.stride(-1) == 1) and (out.dim() == 2 or out.is_contiguous()), "out: a row's values one behind the other"
+        self._check(self.lib.mg_embedding(self.handle, table.data_ptr(), stride, ROW_TYPES[table.dtype], rows, dim, ids.data_ptr(), wide, ids.numel(), scale,
+                                          out.data_ptr(), out.stride(0) if out.dim() == 2 else dim, ROW_TYPES[out.dtype], torch._C._cuda_getCurrentRawStream(self.device.index)))
+        return out
+
+    def id_groups(self, ids: torch.Tensor, n_rows: int) -> IdGroups:
+        """The places of each id among `ids`, taken flat, for a table of n_rows rows: what the gradient of embedding is summed up by.  Keep them where the
+        same ids are looked up in several tables."""
+        ids, wide = _ids(ids, self.device)
+        n = ids.numel()
+        most = min(n, n_rows)
+        need = C.c_size_t(0)
+        self._check(self.lib.mg_id_groups_workspace(self.handle, n, n_rows, C.byref(need)))
+        work = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        block = torch.empty(n + most + 2, dtype=torch.int32, device=self.device)
+        order, starts, count = torch.split(block, [n, most + 1, 1])
+        distinct = torch.empty(most, dtype=ids.dtype, device=self.device)
+        self._check(self.lib.mg_id_groups(self.handle, ids.data_ptr(), wide, n, n_rows, order.data_ptr(), distinct.data_ptr(), starts.data_ptr(), count.data_ptr(),
+                                          work.data_ptr(), need.value, torch._C._cuda_getCurrentRawStream(self.device.index)))
+        return IdGroups(order, distinct, starts, count, n_rows)
+
+    def _group_sums(self, d_y, groups: IdGroups, scale, into, out):
+        n, dim = d_y.shape
+        need = C.c_size_t(0)
+        self._check(self.lib.mg_embedding_backward_workspace(self.handle, n, groups.n_rows, dim, C.byref(need)))
+        work = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
+        self._check(self.lib.mg_embedding_backward(self.handle, d_y.data_ptr(), d_y.stride(0), ROW_TYPES[d_y.dtype], n, groups.n_rows, dim, scale, groups.order.data_ptr(),
+                                                   groups.ids.data_ptr(), groups.ids.dtype == torch.int64, groups.starts.data_ptr(), groups.count.data_ptr(), into,
+                                                   out.data_ptr(), out.stride(0), ROW_TYPES[out.dtype], _at(work), need.value,
+                                                   torch._C._cuda_getCurrentRawStream(self.device.index)))
+
+    def _grouped(self, d_y, ids, n_rows):
+        """The gradient as a matrix of a row for each id, and the ids' groups."""
+        if not isinstance(ids, IdGroups):
+            assert d_y.shape[:-1] == ids.shape, "d_y: a row for each id"
+            ids = self.id_groups(ids, n_rows)
+        assert n_rows == ids.n_rows, "groups of ids belong to the number of rows they were made for"
+        assert d_y.dim() >= 1 and d_y.shape[:-1].numel() == ids.order.numel(), "d_y: a row for each id"
+        if d_y.dim() != 2:
+            d_y = d_y.reshape(ids.order.numel(), d_y.shape[-1])
+        return _matrix(d_y, self.device)[0], ids
+
+    def embedding_backward(self, d_y: torch.Tensor, ids: torch.Tensor | IdGroups, n_rows: int, scale: float = 1.0, dtype: torch.dtype | None = None,
+                           out: torch.Tensor | None = None, accumulate: bool = False) -> torch.Tensor:
+        """Gradient of embedding with respect to its table of n_rows rows, from its output's d_y [*ids.shape, dim]: sums in fp32, in an order that does not change
+        from run to run.  ids: those of the lookup, or their id_groups.  out: where to, else a new tensor (of `dtype`, else of d_y's type); accumulate: it is added
+        to what `out` holds, and rows without an id are not touched."""
+        d_y, groups = self._grouped(d_y, ids, n_rows)
+        assert out is not None or not accumulate, "accumulate wants out"
+        if out is None:
+            out = torch.empty((n_rows, d_y.shape[1]), dtype=dtype or d_y.dtype, device=self.device)
+        assert out.device == self.device and out.shape == (n_rows, d_y.shape[1]) and out.dtype in ROW_TYPES and out.dtype == (dtype or out.dtype), "out: a CUDA tensor [n_rows, dim]"
+        assert out.shape[1] <= 1 or out.stride(1) == 1, "out: a row's values one behind the other"
+        self._group_sums(d_y, groups, scale, ROWS_ADD if accumulate else ROWS_TABLE, out)
+        return out
+
+    def embedding_backward_rows(self, d_y: torch.Tensor, ids: torch.Tensor | IdGroups, n_rows: int, scale: float = 1.0, dtype: torch.dtype | None = None):
+        """The same gradient as the distinct ids, ascending, and a row for each.  The host waits for the number of ids (not for the sums), so the call cannot be
+        captured; the rows are the first of a block that has room for min(ids, n_rows)."""
+        d_y, groups = self._grouped(d_y, ids, n_rows)
+        count = torch.empty(1, dtype=torch.int32, pin_memory=True)
+        count.copy_(groups.count, non_blocking=True)
+        known = torch.cuda.Event()
+        known.record(torch.cuda.current_stream(self.device))
+        rows = torch.empty((groups.ids.numel(), d_y.shape[1]), dtype=dtype or d_y.dtype, device=self.device)
+        self._group_sums(d_y, groups, scale, ROWS_COMPACT, rows)
+        known.synchronize()
+        n = int(count)
+        if n < 0:
+            raise MgError(-7, "a bounded wait on the device ran out")
+        return groups.ids[:n], rows[:n]
+
+    # -- losses
+    def _logits(self, x: torch.Tensor, scale: float):
+        x, stride = _matrix(x, self.device)
+        return x, LogitsSpec(x.data_ptr(), stride, x.shape[:-1].numel(), x.shape[-1], ROW_TYPES[x.dtype], scale)
+
+    def _labels(self, labels, shape):
+        if labels is None:
+            return None, False
+        labels, wide = _ids(labels, self.device, "labels")
+        assert labels.shape == shape, "labels: one for each row"
+        return labels, wide
+
+    def log_probs(self, logits: torch.Tensor, labels: torch.Tensor | None = None, top: int = 0, scale: float = 1.0) -> LogProbs:
+        """Of every row of logits [..., classes], with z = scale * logits: the log probability of its label (0 where the label is none of the classes, -100 say), the
+        entropy, lse = log sum exp z, and the `top` likeliest classes with their log probabilities, equal ones by ascending class.  fp32, queued on torch's
+        current stream.  A logit of -infinity is a class that is not allowed.  The gradients are log_probs_backward's."""
+        x, spec = self._logits(logits, scale)
+        shape = x.shape[:-1]
+        labels, wide = self._labels(labels, shape)
+        block = torch.empty((2 if labels is None else 3, *shape), dtype=torch.float32, device=self.device).unbind(0)
+        ids = torch.empty((*shape, top), dtype=torch.int32, device=self.device) if top > 0 else None
+        best = torch.empty((*shape, top), dtype=torch.float32, device=self.device) if top > 0 else None
+        log_prob = block[2] if labels is not None else None
+        self._check(self.lib.mg_log_probs(self.handle, C.byref(spec), _at(labels), wide, top, _at(log_prob), block[0].data_ptr(), block[1].data_ptr(), _at(ids), _at(best),
+                                          torch._C._cuda_getCurrentRawStream(self.device.index)))
+        return LogProbs(log_prob, block[0], block[1], ids, best)
+
+    def log_probs_backward(self, logits: torch.Tensor, lse: torch.Tensor, labels: torch.Tensor | None = None, d_log_prob: torch.Tensor | None = None,
+                           entropy: torch.Tensor | None = None, d_entropy: torch.Tensor | None = None, d_lse: torch.Tensor | None = None, scale: float = 1.0,
+                           out: torch.Tensor | None = None) -> torch.Tensor:
+        """Gradient of a loss with respect to the logits from those with respect to log_prob, entropy and lse (a value for each row, or None); lse and (for
+        d_entropy) entropy as log_probs gave them.  out may be the logits."""
+        x, spec = self._logits(logits, scale)
+        shape = x.shape[:-1]
+        labels, wide = self._labels(labels, shape)
+        lse, g, h, l = (_by_row(t, shape, self.device, what) for t, what in ((lse, "lse"), (d_log_prob, "d_log_prob"), (d_entropy, "d_entropy"), (d_lse, "d_lse")))
+        entropy = _by_row(entropy, shape, self.device, "entropy")
+        out, stride = _result(out, x)
+        self._check(self.lib.mg_log_probs_backward(self.handle, C.byref(spec), _at(lse), _at(labels), wide, _at(g), _at(entropy), _at(h), _at(l), out.data_ptr(), stride,
+                                                   torch._C._cuda_getCurrentRawStream(self.device.index)))
+        return out
+
+    def _teacher(self, ids, values, lse, shape):
+        assert ids.device == self.device and ids.dtype in (torch.int32, torch.int64), "teacher_ids: a CUDA tensor of int32 or int64, on the context's device"
+        assert ids.shape[:-1] == shape and ids.shape == values.shape, "teacher_ids, teacher_logits: the same number of entries for each row"
+        values, v_stride = _matrix(values, self.device)
+        if ids.shape[-1] > 1 and ids.stride(-1) != 1 or ids.dim() > 2 and not ids.is_contiguous():
+            ids = ids.contiguous()
+        lse = _by_row(lse, shape, self.device, "teacher_lse")
+        spec = TeacherSpec(ids.data_ptr(), values.data_ptr(), _at(lse), ids.stride(0) if ids.dim() == 2 else ids.shape[-1], v_stride, ids.dtype == torch.int64,
+                           ROW_TYPES[values.dtype], ids.shape[-1])
+        return spec, (ids, values, lse)
+
+    def distill(self, logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, scale: float = 1.0, teacher_lse: torch.Tensor | None = None):
+        """(loss, lse) of every row of logits [..., classes] against a teacher's top logits: teacher_ids, teacher_logits [..., entries] (log_probs's top_ids and
+        top_log_probs, say; a class that is none, -1, is no entry).  q = softmax of scale * teacher_logits over the entries (with teacher_lse: exp(scale *
+        teacher_logits - teacher_lse), the teacher's probabilities as they are), loss = sum q (log q - log p), p = softmax of scale * logits.  A temperature T is a
+        scale of 1 / T.  fp32, queued on torch's current stream; the gradient is distill_backward's."""
+        x, spec = self._logits(logits, scale)
+        shape = x.shape[:-1]
+        teacher, held = self._teacher(teacher_ids, teacher_logits, teacher_lse, shape)
+        loss, lse = torch.empty((2, *shape), dtype=torch.float32, device=self.device).unbind(0)
+        self._check(self.lib.mg_distill(self.handle, C.byref(spec), C.byref(teacher), loss.data_ptr(), lse.data_ptr(), torch._C._cuda_getCurrentRawStream(self.device.index)))
+        return loss, lse
+
+    def distill_backward(self, d_loss: torch.Tensor, logits: torch.Tensor, lse: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor,
+                         scale: float = 1.0, teacher_lse: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+        """Gradient of distill's loss with respect to the logits, from the loss's (a value for each row); lse and the rest as in the forward call.  out may be
+        the logits."""
+        x, spec = self._logits(logits, scale)
+        shape = x.shape[:-1]
+        teacher, held = self._teacher(teacher_ids, teacher_logits, teacher_lse, shape)
+        lse, d_loss = _by_row(lse, shape, self.device, "lse"), _by_row(d_loss, shape, self.device, "d_loss")
+        out, stride = _result(out, x)
+        self._check(self.lib.mg_distill_backward(self.handle, C.byref(spec), _at(lse), C.byref(teacher), _at(d_loss), out.data_ptr(), stride,
+                                                 torch._C._cuda_getCurrentRawStream(self.device.index)))
+        return out

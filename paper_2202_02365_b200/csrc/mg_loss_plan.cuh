@@ -1,0 +1,83 @@
+// Host side of the losses: checks of arguments.  No CUDA calls.
+#pragma once
+
+#include <math.h>
+
+#include <algorithm>
+
+#include "mg_call.cuh"
+
+namespace {
+
+inline int check_floats(mg_ctx* ctx, std::initializer_list<const void*> all) {
+    for (const void* p : all)
+        if (reinterpret_cast<uintptr_t>(p) % 4) return mg_fail(ctx, MG_ERR_ARG, "values by row must be 4-byte aligned");
+    return MG_OK;
+}
+
+inline int check_logits(mg_ctx* ctx, const mg_logits* z) {
+    if (!z) return mg_fail(ctx, MG_ERR_ARG, "null argument");
+    if (!known_dtype(z->dtype)) return mg_fail(ctx, MG_ERR_ARG, "unknown dtype");
+    if (z->rows < 0 || z->rows >= 1ll << 31) return mg_fail(ctx, MG_ERR_ARG, "the number of rows must be in [0, 2^31)");
+    if (z->classes < 1 || z->classes > 1 << 28) return mg_fail(ctx, MG_ERR_ARG, "the number of classes must be in [1, 2^28]");
+    if (!(z->scale > 0.f) || isinf(z->scale)) return mg_fail(ctx, MG_ERR_ARG, "the scale must be positive and finite");
+    return check_matrix(ctx, "the logits", z->x, z->stride, z->dtype, z->rows, z->classes, false);
+}
+
+inline int check_labels(mg_ctx* ctx, const void* labels, int labels_are_i64) {
+    if (reinterpret_cast<uintptr_t>(labels) % (labels_are_i64 ? 8 : 4)) return mg_fail(ctx, MG_ERR_ARG, "the labels are not aligned to their elements");
+    return MG_OK;
+}
+
+inline int check_gradient(mg_ctx* ctx, const mg_logits* z, const float* lse, const void* d_x, int64_t d_x_stride) {
+    if (z->rows > 0 && !lse) return mg_fail(ctx, MG_ERR_ARG, "null lse");
+    if (int rc = check_matrix(ctx, "d_x", d_x, d_x_stride, z->dtype, z->rows, z->classes, true)) return rc;
+    return check_apart(ctx, "the logits", z->x, z->stride, d_x, d_x_stride, z->dtype, z->rows, z->classes);
+}
+
+inline int check_log_probs(mg_ctx* ctx, const mg_logits* z, const void* labels, int labels_are_i64, int32_t top, const float* log_prob, const float* entropy, const float* lse,
+                           const int32_t* top_ids, const float* top_log_probs) {
+    if (int rc = check_logits(ctx, z)) return rc;
+    if (int rc = check_labels(ctx, labels, labels_are_i64)) return rc;
+    if (z->rows > 0 && log_prob && !labels) return mg_fail(ctx, MG_ERR_ARG, "log probabilities of labels want labels");
+    if (top < 0 || top > MG_MAX_TOP || top > z->classes) return mg_fail(ctx, MG_ERR_ARG, "top must be in [0, %d], and no more than there are classes", MG_MAX_TOP);
+    return check_floats(ctx, {log_prob, entropy, lse, top_ids, top_log_probs});
+}
+
+inline int check_log_probs_backward(mg_ctx* ctx, const mg_logits* z, const float* lse, const void* labels, int labels_are_i64, const float* d_log_prob, const float* entropy,
+                                    const float* d_entropy, const float* d_lse, const void* d_x, int64_t d_x_stride) {
+    if (int rc = check_logits(ctx, z)) return rc;
+    if (int rc = check_labels(ctx, labels, labels_are_i64)) return rc;
+    if (z->rows > 0 && d_log_prob && !labels) return mg_fail(ctx, MG_ERR_ARG, "log probabilities of labels want labels");
+    if (z->rows > 0 && d_entropy && !entropy) return mg_fail(ctx, MG_ERR_ARG, "the entropy's gradient wants the entropy");
+    if (int rc = check_floats(ctx, {lse, d_log_prob, entropy, d_entropy, d_lse})) return rc;
+    return check_gradient(ctx, z, lse, d_x, d_x_stride);
+}
+
+inline int check_teacher(mg_ctx* ctx, const mg_logits* z, const mg_teacher* t) {
+    if (!t) return mg_fail(ctx, MG_ERR_ARG, "null argument");
+    if (!known_dtype(t->dtype)) return mg_fail(ctx, MG_ERR_ARG, "unknown dtype");
+    if (t->entries < 1 || t->entries > MG_MAX_TEACHER) return mg_fail(ctx, MG_ERR_ARG, "the teacher's entries must be in [1, %d]", MG_MAX_TEACHER);
+    if (int rc = check_matrix(ctx, "the teacher's values", t->values, t->values_stride, t->dtype, z->rows, t->entries, false)) return rc;
+    if (z->rows > 0 && !t->ids) return mg_fail(ctx, MG_ERR_ARG, "null classes of the teacher's");
+    if (reinterpret_cast<uintptr_t>(t->ids) % (t->ids_are_i64 ? 8 : 4)) return mg_fail(ctx, MG_ERR_ARG, "the teacher's classes are not aligned to their elements");
+    if (z->rows > 1 && (t->ids_stride < 0 || t->ids_stride > 1ll << 28)) return mg_fail(ctx, MG_ERR_ARG, "the rows of the teacher's classes must be 0 to 2^28 elements apart");
+    return check_floats(ctx, {t->lse});
+}
+
+inline int check_distill(mg_ctx* ctx, const mg_logits* z, const mg_teacher* t, const float* loss, const float* lse) {
+    if (int rc = check_logits(ctx, z)) return rc;
+    if (int rc = check_teacher(ctx, z, t)) return rc;
+    if (z->rows > 0 && !loss) return mg_fail(ctx, MG_ERR_ARG, "null loss");
+    return check_floats(ctx, {loss, lse});
+}
+
+inline int check_distill_backward(mg_ctx* ctx, const mg_logits* z, const float* lse, const mg_teacher* t, const float* d_loss, const void* d_x, int64_t d_x_stride) {
+    if (int rc = check_logits(ctx, z)) return rc;
+    if (int rc = check_teacher(ctx, z, t)) return rc;
+    if (z->rows > 0 && !d_loss) return mg_fail(ctx, MG_ERR_ARG, "null gradient of the loss");
+    if (int rc = check_floats(ctx, {lse, d_loss})) return rc;
+    return check_gradient(ctx, z, lse, d_x, d_x_stride);
+}
+
+}  // namespace

@@ -42,25 +42,6 @@ __global__ void k_norm_table(const __grid_constant__ TableArgs a, int2* out) {
     for (int i = threadIdx.x; i < a.n; i += blockDim.x) out[i] = a.at[i];
 }
 
-struct DeviceScope {   // work goes to the context's device; the caller's current one stays
-    int before = -1;
-    cudaError_t err;
-    explicit DeviceScope(int device) {
-        err = cudaGetDevice(&before);
-        if (err == cudaSuccess && before != device) err = cudaSetDevice(device);
-        else if (err == cudaSuccess) before = -1;
-    }
-    ~DeviceScope() { if (before >= 0) cudaSetDevice(before); }
-};
-
-// `by_type<T>(...)` for the rows' type
-#define MG_BY_TYPE(dtype, call)                              \
-    do {                                                     \
-        if ((dtype) == MG_DTYPE_F32) { using T = float; call; }          \
-        else if ((dtype) == MG_DTYPE_F16) { using T = __half; call; }    \
-        else { using T = __nv_bfloat16; call; }              \
-    } while (0)
-
 // both directions, arguments checked; `m`: the matrices, the output last
 int run_norm(mg_ctx* ctx, const mg_norm_spec* s, const Matrix* m, int n_matrices, bool backward, float* mean, float* rstd, float* d_weight, float* d_bias,
              const DropArgs& drop, void* workspace, size_t workspace_bytes, cudaStream_t st) {
