@@ -1,230 +1,101 @@
 // Losses of a layer's output: log probabilities with entropy and top alternatives, distillation from a teacher's top logits, and their gradients.
+#include "mg_loss_grad.cuh"
 #include "mg_loss_plan.cuh"
-#include "mg_norm.cuh"
 
 namespace {
 
-constexpr int kLossThreads = 256;
-constexpr float kNegInf = -__builtin_huge_valf();
-
-template <typename T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
-template <typename T> __device__ __forceinline__ T from_float(float v);
-template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
-template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
-template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-
-__device__ __forceinline__ int64_t id_at(const void* ids, int is_i64, int64_t i) {
-    return is_i64 ? static_cast<const int64_t*>(ids)[i] : (int64_t)static_cast<const int32_t*>(ids)[i];
-}
-
-// Floats as whole numbers of the same order, between 0 and 2^32 - 1: equal values (both zeros among them) are equal, NaN is above all.
-constexpr uint32_t kNanOrder = 0xFFFFFFFEu;
-__device__ __forceinline__ uint32_t order_of(float v) {
-    if (v != v) return kNanOrder;
-    const uint32_t b = __float_as_uint(v + 0.f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float value_of(uint32_t o) {
-    return o == kNanOrder ? __uint_as_float(0x7FFFFFFFu) : __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
-}
-
-template <typename F>
-__device__ float block_reduce(float v, F f) {
-    __shared__ float part[kLossThreads / 32];
-    for (int o = 16; o; o >>= 1) v = f(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = v;
-    __syncthreads();
-    v = part[0];
-    for (int w = 1; w < kLossThreads / 32; ++w) v = f(v, part[w]);
-    return v;
-}
-__device__ __forceinline__ float block_sum(float v) { return block_reduce(v, [](float a, float b) { return a + b; }); }
-__device__ __forceinline__ float block_max(float v) { return block_reduce(v, [](float a, float b) { return fmaxf(a, b); }); }
-__device__ uint64_t block_max_key(uint64_t v) {
-    __shared__ uint64_t part[kLossThreads / 32];
-    for (int o = 16; o; o >>= 1) v = max(v, (uint64_t)__shfl_xor_sync(0xFFFFFFFFu, (unsigned long long)v, o));
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) part[threadIdx.x / 32] = v;
-    __syncthreads();
-    v = part[0];
-    for (int w = 1; w < kLossThreads / 32; ++w) v = max(v, part[w]);
-    return v;
-}
-
-// m = the largest logit (0 where none is allowed), sum of exp(scale (x - m)), and of it times scale (x - m)
-struct RowStats { float m, sum, weighted; bool none; };
-
-template <typename T>
-__device__ RowStats row_stats(const T* x, int32_t classes, float scale) {
-    float m = kNegInf;
-    for (int32_t c = threadIdx.x; c < classes; c += kLossThreads) m = fmaxf(m, to_float(x[c]));
-    m = block_max(m);
-    float bad = 0.f;
-    RowStats s{m, 0.f, 0.f, false};
-    if (m == kNegInf) s.m = 0.f;
-    for (int32_t c = threadIdx.x; c < classes; c += kLossThreads) {
-        const float d = scale * (to_float(x[c]) - s.m), e = expf(d);
-        s.sum += e;
-        if (e > 0.f) s.weighted += e * d;
-        if (d != d) bad = 1.f;
-    }
-    s.sum = block_sum(s.sum);
-    s.weighted = block_sum(s.weighted);
-    s.none = m == kNegInf && block_sum(bad) == 0.f;
-    return s;
-}
-
-struct ScoreArgs {
-    const void* labels; int labels_are_i64;
-    int32_t top;
-    float *log_prob, *entropy, *lse; int32_t* top_ids; float* top_log_probs;
-};
-
-template <typename T>
-__global__ void __launch_bounds__(kLossThreads) k_log_probs(const T* all, int64_t stride, int64_t rows, int32_t classes, float scale, ScoreArgs a) {
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T* x = all + r * stride;
-        const RowStats s = row_stats(x, classes, scale);
-        const float log_sum = logf(s.sum);   // (-infinity where no class is allowed)
-        const auto log_p = [&](float v) { return s.none ? kNegInf : scale * (v - s.m) - log_sum; };
-        if (threadIdx.x == 0) {
-            if (a.lse) a.lse[r] = fmaf(scale, s.m, log_sum);
-            if (a.entropy) a.entropy[r] = s.none ? 0.f : log_sum - s.weighted / s.sum;
-            if (a.log_prob) {
-                const int64_t label = id_at(a.labels, a.labels_are_i64, r);
-                a.log_prob[r] = label >= 0 && label < classes ? log_p(to_float(x[label])) : 0.f;
-            }
-        }
-        uint64_t last = ~0ull;
-        for (int k = 0; k < a.top; ++k) {
-            uint64_t best = 0;
-            for (int32_t c = threadIdx.x; c < classes; c += kLossThreads) {
-                const uint64_t key = (uint64_t)order_of(to_float(x[c])) << 32 | (uint32_t)~c;
-                if (key < last && key > best) best = key;
-            }
-            last = block_max_key(best);
-            if (threadIdx.x == 0) {
-                if (a.top_ids) a.top_ids[r * a.top + k] = (int32_t) ~(uint32_t)last;
-                if (a.top_log_probs) a.top_log_probs[r * a.top + k] = log_p(value_of((uint32_t)(last >> 32)));
-            }
-        }
-        __syncthreads();
-    }
-}
-
-struct ScoreGradArgs {
-    const float* lse;
-    const void* labels; int labels_are_i64;
-    const float *d_log_prob, *entropy, *d_entropy, *d_lse;
-};
-
-template <typename T>
-__global__ void __launch_bounds__(kLossThreads) k_log_probs_backward(const T* all, int64_t stride, int64_t rows, int32_t classes, float scale, ScoreGradArgs a, T* d_all, int64_t d_stride) {
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T* x = all + r * stride;
-        T* d = d_all + r * d_stride;
-        const float lse = a.lse[r];
-        int64_t label = a.d_log_prob ? id_at(a.labels, a.labels_are_i64, r) : -1;
-        if (label >= classes) label = -1;
-        const float g = label >= 0 ? a.d_log_prob[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f, l = a.d_lse ? a.d_lse[r] : 0.f;
-        const float entropy = h != 0.f ? a.entropy[r] : 0.f;
-        const bool zero = (g == 0.f && h == 0.f && l == 0.f) || lse == kNegInf;
-        for (int32_t c = threadIdx.x; c < classes; c += kLossThreads) {
-            float v = 0.f;
-            if (!zero) {
-                const float log_p = fmaf(scale, to_float(x[c]), -lse), p = expf(log_p);
-                v = p == 0.f ? 0.f : p * (l - g - (h != 0.f ? h * (log_p + entropy) : 0.f));
-                if (c == label) v += g;
-            }
-            d[c] = from_float<T>(scale * v);
-        }
-    }
-}
-
-struct TeacherArgs {
-    const void *ids, *values; const float* lse;
-    int64_t ids_stride, values_stride;
-    int ids_are_i64, dtype;
-    int32_t entries;
-};
-
-// the teacher's classes of a row (-1: no pair) and their probabilities, and the sum of these
-__device__ float teacher_row(const TeacherArgs& t, int64_t r, int32_t classes, float scale, int32_t* ids, float* q, float* log_q) {
-    float m = kNegInf;
-    for (int k = threadIdx.x; k < t.entries; k += kLossThreads) {
-        const int64_t id = id_at(t.ids, t.ids_are_i64, r * t.ids_stride + k);
-        ids[k] = id >= 0 && id < classes ? (int32_t)id : -1;
-        const int64_t at = r * t.values_stride + k;
-        float v = kNegInf;
-        if (ids[k] >= 0) v = scale * (t.dtype == MG_DTYPE_F32 ? static_cast<const float*>(t.values)[at] : t.dtype == MG_DTYPE_F16 ? to_float(static_cast<const __half*>(t.values)[at]) : to_float(static_cast<const __nv_bfloat16*>(t.values)[at]));
-        log_q[k] = v;
-        m = fmaxf(m, v);
-        if (v != v) m = v;
-    }
-    float sum = 0.f, shift;
-    if (t.lse) shift = t.lse[r];
-    else {
-        m = block_max(m);
-        if (m == kNegInf) m = 0.f;
-        for (int k = threadIdx.x; k < t.entries; k += kLossThreads) sum += expf(log_q[k] - m);
-        sum = block_sum(sum);
-        shift = sum == 0.f ? 0.f : m + logf(sum);
-    }
-    sum = 0.f;
-    for (int k = threadIdx.x; k < t.entries; k += kLossThreads) {
-        if (ids[k] >= 0) log_q[k] -= shift;
-        q[k] = ids[k] >= 0 ? expf(log_q[k]) : 0.f;
-        sum += q[k];
-    }
-    return block_sum(sum);
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kLossThreads) k_distill(const T* all, int64_t stride, int64_t rows, int32_t classes, float scale, TeacherArgs t, float* loss, float* lse) {
-    __shared__ int32_t ids[MG_MAX_TEACHER];
-    __shared__ float q[MG_MAX_TEACHER], log_q[MG_MAX_TEACHER];
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T* x = all + r * stride;
-        const RowStats s = row_stats(x, classes, scale);
-        const float log_sum = logf(s.sum);
-        teacher_row(t, r, classes, scale, ids, q, log_q);
-        float v = 0.f;
-        for (int k = threadIdx.x; k < t.entries; k += kLossThreads)
-            if (ids[k] >= 0 && q[k] != 0.f) v += q[k] * (log_q[k] - (s.none ? kNegInf : scale * (to_float(x[ids[k]]) - s.m) - log_sum));
-        v = block_sum(v);
-        if (threadIdx.x == 0) {
-            loss[r] = v;
-            if (lse) lse[r] = fmaf(scale, s.m, log_sum);
-        }
-        __syncthreads();
-    }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(kLossThreads) k_distill_backward(const T* all, int64_t stride, int64_t rows, int32_t classes, float scale, const float* all_lse, TeacherArgs t, const float* d_loss, T* d_all, int64_t d_stride) {
-    __shared__ int32_t ids[MG_MAX_TEACHER];
-    __shared__ float q[MG_MAX_TEACHER], log_q[MG_MAX_TEACHER];
-    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-        const T* x = all + r * stride;
-        T* d = d_all + r * d_stride;
-        const float lse = all_lse[r], g = d_loss[r], mass = teacher_row(t, r, classes, scale, ids, q, log_q);
-        const bool zero = g == 0.f || mass == 0.f || lse == kNegInf;
-        __syncthreads();
-        for (int32_t c = threadIdx.x; c < classes; c += kLossThreads) {
-            float v = 0.f;
-            if (!zero) {
-                v = mass * expf(fmaf(scale, to_float(x[c]), -lse));
-                for (int k = 0; k < t.entries; ++k)
-                    if (ids[k] == c) v -= q[k];
-            }
-            d[c] = from_float<T>(scale * g * v);
-        }
-        __syncthreads();
-    }
-}
+using namespace mgloss;
 
 TeacherArgs teacher_args(const mg_teacher* t) { return {t->ids, t->values, t->lse, t->ids_stride, t->values_stride, t->ids_are_i64, t->dtype, t->entries}; }
+
+int pow2_up(int64_t v) { int p = 1; while (p < v) p *= 2; return p; }
+
+// rows that begin and end with a 16-byte vector each
+bool whole_vectors(const void* p, int64_t stride, int64_t rows, int32_t classes, int dtype) {
+    const int64_t vec = 16 / elem_size(dtype);
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && classes % vec == 0 && (rows <= 1 || stride % vec == 0);
+}
+// two matrices whose rows begin equally far from one
+bool same_phase(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t rows, int dtype) {
+    const int64_t vec = 16 / elem_size(dtype);
+    return (reinterpret_cast<uintptr_t>(a) - reinterpret_cast<uintptr_t>(b)) % 16 == 0 && (rows <= 1 || (a_stride - b_stride) % vec == 0);
+}
+
+constexpr int kHeldValues = 32;   // of a narrow row, to a lane
+
+// lanes to a narrow row, and values to a lane (8, 16 or 32)
+struct RowShapeOf { int lanes, values; };
+RowShapeOf row_shape(int32_t classes, int dtype, bool edges) {
+    const int vec = 16 / elem_size(dtype), least = edges && vec == 8 ? 16 : 8;   // (an edge to a lane)
+    const int64_t vecs = std::max<int64_t>(1, classes / vec);
+    for (int values : {8, 16})
+        for (int lanes = least; lanes <= 32; lanes *= 2)
+            if (vecs * vec <= (int64_t)lanes * values && (values == 16 || lanes == least)) return {lanes, values};
+    return {32, kHeldValues};
+}
+bool narrow(int32_t classes) { return classes <= 32 * kHeldValues; }
+
+template <typename T, bool EDGES>
+void launch_rows_of(const ScoreArgs& a, const TeacherArgs* t, float* loss, const RowShapeOf& s, int grid, cudaStream_t st) {
+    constexpr int VEC = 16 / sizeof(T);
+    if (t) {
+        if (s.values == 8) k_distill_rows<T, 8 / VEC, EDGES><<<grid, mgloss::kRowThreads, 0, st>>>(a, *t, loss, s.lanes);
+        else if (s.values == 16) k_distill_rows<T, 16 / VEC, EDGES><<<grid, mgloss::kRowThreads, 0, st>>>(a, *t, loss, s.lanes);
+        else k_distill_rows<T, 32 / VEC, EDGES><<<grid, mgloss::kRowThreads, 0, st>>>(a, *t, loss, s.lanes);
+    } else {
+        if (s.values == 8) k_scores_rows<T, 8 / VEC, EDGES><<<grid, mgloss::kRowThreads, 0, st>>>(a, s.lanes);
+        else if (s.values == 16) k_scores_rows<T, 16 / VEC, EDGES><<<grid, mgloss::kRowThreads, 0, st>>>(a, s.lanes);
+        else k_scores_rows<T, 32 / VEC, EDGES><<<grid, mgloss::kRowThreads, 0, st>>>(a, s.lanes);
+    }
+}
+
+template <typename K, typename... A>
+void launch_cluster(K kernel, int64_t blocks, int parts, cudaStream_t st, A... args) {
+    if (parts > 8) cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)parts; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t how = {};
+    how.gridDim = dim3((unsigned)blocks); how.blockDim = dim3(kWideThreads); how.stream = st;
+    how.attrs = &attr; how.numAttrs = parts > 1 ? 1 : 0;
+    cudaLaunchKernelEx(&how, kernel, args...);   // (an error is found by cudaGetLastError)
+}
+
+// how many blocks share a wide row: as many as there is room for on the GPU, a segment of registers to each at least
+int wide_parts(int64_t rows, int32_t classes, int dtype, int n_sms) {
+    const int64_t segment = (int64_t)kWideThreads * kWideVecs * 16 / elem_size(dtype) / 2;
+    int parts = 1;
+    while (parts < 16 && rows * parts * 2 <= 4 * n_sms && classes / (parts * 2) >= segment / 2) parts *= 2;
+    return parts;
+}
+
+// both forward directions; `t`: distillation
+int run_forward(mg_ctx* ctx, const mg_logits* z, const ScoreArgs& a, const TeacherArgs* t, float* loss, cudaStream_t st) {
+    DeviceScope on(ctx->device);
+    MG_CUDA(ctx, on.err);
+    const bool edges = !whole_vectors(z->x, z->stride, z->rows, z->classes, z->dtype);
+    if (narrow(z->classes)) {
+        const RowShapeOf s = row_shape(z->classes, z->dtype, edges);
+        const int groups = mgloss::kRowThreads / s.lanes;
+        const int grid = (int)std::min<int64_t>((z->rows + groups - 1) / groups, mg_grid(ctx, 64));
+        MG_BY_TYPE(z->dtype, (edges ? launch_rows_of<T, true>(a, t, loss, s, grid, st) : launch_rows_of<T, false>(a, t, loss, s, grid, st)));
+    } else {
+        const int parts = wide_parts(z->rows, z->classes, z->dtype, ctx->n_sms);
+        const int64_t blocks = z->rows * parts;
+        if (t) MG_BY_TYPE(z->dtype, (edges ? launch_cluster(k_distill_wide<T, true>, blocks, parts, st, a, *t, loss, parts) : launch_cluster(k_distill_wide<T, false>, blocks, parts, st, a, *t, loss, parts)));
+        else MG_BY_TYPE(z->dtype, (edges ? launch_cluster(k_scores_wide<T, true>, blocks, parts, st, a, parts) : launch_cluster(k_scores_wide<T, false>, blocks, parts, st, a, parts)));
+    }
+    ctx->launches++;
+    MG_CUDA(ctx, cudaGetLastError());
+    return MG_OK;
+}
+
+// pieces of a row's gradient: about four to each block that the GPU holds
+int grad_chunks(int64_t rows, int32_t classes, int dtype, int n_sms) {
+    const int64_t vecs = classes / (16 / elem_size(dtype)), least = (int64_t)kGradThreads * kGradBatch;
+    const int64_t most = std::max<int64_t>(1, vecs / least), want = (32ll * n_sms + rows - 1) / rows;
+    return (int)std::min({most, std::max<int64_t>(want, vecs / (4 * least)), (int64_t)((1ll << 31) - 1) / rows});
+}
 
 }  // namespace
 
@@ -233,14 +104,8 @@ extern "C" int mg_log_probs(mg_ctx* ctx, const mg_logits* z, const void* labels,
     if (!ctx) return MG_ERR_ARG;
     if (int rc = check_log_probs(ctx, z, labels, labels_are_i64, top, log_prob, entropy, lse, top_ids, top_log_probs)) return rc;
     if (z->rows == 0) return MG_OK;
-    DeviceScope on(ctx->device);
-    MG_CUDA(ctx, on.err);
-    const ScoreArgs a{labels, labels_are_i64, top, log_prob, entropy, lse, top_ids, top_log_probs};
-    const int grid = (int)std::min<int64_t>(z->rows, mg_grid(ctx, 8));
-    MG_BY_TYPE(z->dtype, (k_log_probs<T><<<grid, kLossThreads, 0, (cudaStream_t)stream>>>(static_cast<const T*>(z->x), z->stride, z->rows, z->classes, z->scale, a)));
-    ctx->launches++;
-    MG_CUDA(ctx, cudaGetLastError());
-    return MG_OK;
+    const ScoreArgs a{z->x, z->stride, z->rows, z->classes, z->scale, z->scale * kLog2e, labels, labels_are_i64, top_ids || top_log_probs ? top : 0, log_prob, entropy, lse, top_ids, top_log_probs};
+    return run_forward(ctx, z, a, nullptr, nullptr, (cudaStream_t)stream);
 }
 
 extern "C" int mg_log_probs_backward(mg_ctx* ctx, const mg_logits* z, const float* lse, const void* labels, int labels_are_i64, const float* d_log_prob,
@@ -250,9 +115,13 @@ extern "C" int mg_log_probs_backward(mg_ctx* ctx, const mg_logits* z, const floa
     if (z->rows == 0) return MG_OK;
     DeviceScope on(ctx->device);
     MG_CUDA(ctx, on.err);
-    const ScoreGradArgs a{lse, labels, labels_are_i64, d_log_prob, entropy, d_entropy, d_lse};
-    const int grid = (int)std::min<int64_t>(z->rows, mg_grid(ctx, 8));
-    MG_BY_TYPE(z->dtype, (k_log_probs_backward<T><<<grid, kLossThreads, 0, (cudaStream_t)stream>>>(static_cast<const T*>(z->x), z->stride, z->rows, z->classes, z->scale, a, static_cast<T*>(d_x), d_x_stride)));
+    const GradArgs a{z->x, z->stride, z->rows, z->classes, z->scale, d_x, d_x_stride, lse, labels, labels_are_i64, d_log_prob, entropy, d_entropy, d_lse, {}, nullptr};
+    const bool same = same_phase(z->x, z->stride, d_x, d_x_stride, z->rows, z->dtype);
+    const int vec = 16 / elem_size(z->dtype), lanes = std::min(kGradThreads, std::max(8, pow2_up((z->classes / vec + kGradBatch - 1) / kGradBatch)));
+    const int chunks = lanes == kGradThreads ? grad_chunks(z->rows, z->classes, z->dtype, ctx->n_sms) : 1, groups = kGradThreads / lanes;
+    const int grid = (int)std::min<int64_t>((z->rows * chunks + groups - 1) / groups, (1ll << 31) - 1);
+    const cudaStream_t st = (cudaStream_t)stream;
+    MG_BY_TYPE(z->dtype, (same ? k_scores_grad<T, true><<<grid, kGradThreads, 0, st>>>(a, lanes, chunks) : k_scores_grad<T, false><<<grid, kGradThreads, 0, st>>>(a, lanes, chunks)));
     ctx->launches++;
     MG_CUDA(ctx, cudaGetLastError());
     return MG_OK;
@@ -262,13 +131,9 @@ extern "C" int mg_distill(mg_ctx* ctx, const mg_logits* z, const mg_teacher* tea
     if (!ctx) return MG_ERR_ARG;
     if (int rc = check_distill(ctx, z, teacher, loss, lse)) return rc;
     if (z->rows == 0) return MG_OK;
-    DeviceScope on(ctx->device);
-    MG_CUDA(ctx, on.err);
-    const int grid = (int)std::min<int64_t>(z->rows, mg_grid(ctx, 8));
-    MG_BY_TYPE(z->dtype, (k_distill<T><<<grid, kLossThreads, 0, (cudaStream_t)stream>>>(static_cast<const T*>(z->x), z->stride, z->rows, z->classes, z->scale, teacher_args(teacher), loss, lse)));
-    ctx->launches++;
-    MG_CUDA(ctx, cudaGetLastError());
-    return MG_OK;
+    const ScoreArgs a{z->x, z->stride, z->rows, z->classes, z->scale, z->scale * kLog2e, nullptr, 0, 0, nullptr, nullptr, lse, nullptr, nullptr};
+    const TeacherArgs t = teacher_args(teacher);
+    return run_forward(ctx, z, a, &t, loss, (cudaStream_t)stream);
 }
 
 extern "C" int mg_distill_backward(mg_ctx* ctx, const mg_logits* z, const float* lse, const mg_teacher* teacher, const float* d_loss, void* d_x,
@@ -278,8 +143,19 @@ extern "C" int mg_distill_backward(mg_ctx* ctx, const mg_logits* z, const float*
     if (z->rows == 0) return MG_OK;
     DeviceScope on(ctx->device);
     MG_CUDA(ctx, on.err);
-    const int grid = (int)std::min<int64_t>(z->rows, mg_grid(ctx, 8));
-    MG_BY_TYPE(z->dtype, (k_distill_backward<T><<<grid, kLossThreads, 0, (cudaStream_t)stream>>>(static_cast<const T*>(z->x), z->stride, z->rows, z->classes, z->scale, lse, teacher_args(teacher), d_loss, static_cast<T*>(d_x), d_x_stride)));
+    const GradArgs a{z->x, z->stride, z->rows, z->classes, z->scale, d_x, d_x_stride, lse, nullptr, 0, nullptr, nullptr, nullptr, nullptr, teacher_args(teacher), d_loss};
+    const bool same = same_phase(z->x, z->stride, d_x, d_x_stride, z->rows, z->dtype);
+    const cudaStream_t st = (cudaStream_t)stream;
+    const int vec = 16 / elem_size(z->dtype);
+    const int lanes = std::max({8, pow2_up((z->classes / vec + kGradBatch - 1) / kGradBatch), pow2_up((teacher->entries + kTeacherRoom - 1) / kTeacherRoom)});
+    if (lanes <= 32) {
+        const int groups = kGradThreads / lanes;
+        const int grid = (int)std::min<int64_t>((z->rows + groups - 1) / groups, mg_grid(ctx, 64));
+        MG_BY_TYPE(z->dtype, (same ? k_distill_grad_rows<T, true><<<grid, kGradThreads, 0, st>>>(a, lanes) : k_distill_grad_rows<T, false><<<grid, kGradThreads, 0, st>>>(a, lanes)));
+    } else {
+        const int chunks = grad_chunks(z->rows, z->classes, z->dtype, ctx->n_sms);
+        MG_BY_TYPE(z->dtype, (same ? k_distill_grad<T, true><<<(unsigned)(z->rows * chunks), kGradThreads, 0, st>>>(a, chunks) : k_distill_grad<T, false><<<(unsigned)(z->rows * chunks), kGradThreads, 0, st>>>(a, chunks)));
+    }
     ctx->launches++;
     MG_CUDA(ctx, cudaGetLastError());
     return MG_OK;
