@@ -604,14 +604,15 @@ int mg_embedding(mg_ctx* ctx, const void* table, int64_t table_stride, int table
 
 /* The places of each id, by which the gradient of mg_embedding is summed up: order = the places 0 .. n - 1 by ascending id, equal ones by ascending place,
  * those of ids outside [0, n_rows) behind all others; group_ids = the distinct ids in ascending order (of the type of ids); starts[g] .. starts[g + 1] =
- * where the places of group_ids[g] lie in order; *n_groups = how many there are.  All DEVICE: order [n] int32, group_ids [min(n, n_rows)],
- * starts [min(n, n_rows) + 1] int32, n_groups one int32; behind the last group, group_ids and starts stay as they were.  A program that looks the same
- * ids up in several tables, or takes several gradients, keeps them.  Streams, capture and errors as mg_embedding; MG_ERR_CAPACITY: the workspace (DEVICE,
- * 16-byte aligned, one for each call that may run at the same time) is smaller than mg_id_groups_workspace says.  Where a bounded wait on the device runs
- * out (nothing that is known of makes it), *n_groups is -1: no group is to be used, and mg_embedding_backward writes none. */
+ * where the places of group_ids[g] lie in order; group_of[i] = the group of order[i], -1 for an id that is no row; *n_groups = how many there are.  All DEVICE:
+ * order and group_of [n] int32, group_ids [min(n, n_rows)], starts [min(n, n_rows) + 1] int32, n_groups one int32; behind the last group, group_ids and
+ * starts stay as they were.  A program that looks the same ids up in several tables, or takes several gradients, keeps them.  Streams, capture and errors
+ * as mg_embedding; MG_ERR_CAPACITY: the workspace (DEVICE, 16-byte aligned, one for each call that may run at the same time) is smaller than
+ * mg_id_groups_workspace says.  Where a bounded wait on the device runs out (nothing that is known of makes it), *n_groups is -1: no group is to be used, and
+ * mg_embedding_backward writes none. */
 int mg_id_groups_workspace(mg_ctx* ctx, int64_t n, int64_t n_rows, size_t* bytes);
-int mg_id_groups(mg_ctx* ctx, const void* ids, int ids_are_i64, int64_t n, int64_t n_rows, int32_t* order, void* group_ids, int32_t* starts,
-                 int32_t* n_groups, void* workspace, size_t workspace_bytes, void* stream);
+int mg_id_groups(mg_ctx* ctx, const void* ids, int ids_are_i64, int64_t n, int64_t n_rows, int32_t* order, int32_t* group_of, void* group_ids,
+                 int32_t* starts, int32_t* n_groups, void* workspace, size_t workspace_bytes, void* stream);
 
 /* Gradient of mg_embedding: for every group g the sum of scale * d_y[i] over its places, in fp32 and in an order that does not change from run to run
  * (no float is added atomically), rounded once to out_dtype, into
@@ -625,8 +626,8 @@ int mg_id_groups(mg_ctx* ctx, const void* ids, int ids_are_i64, int64_t n, int64
 #define MG_ROWS_COMPACT 2
 int mg_embedding_backward_workspace(mg_ctx* ctx, int64_t n, int64_t n_rows, int32_t dim, size_t* bytes);
 int mg_embedding_backward(mg_ctx* ctx, const void* d_y, int64_t d_y_stride, int d_y_dtype, int64_t n, int64_t n_rows, int32_t dim, float scale,
-                          const int32_t* order, const void* group_ids, int ids_are_i64, const int32_t* starts, const int32_t* n_groups, int into,
-                          void* out, int64_t out_stride, int out_dtype, void* workspace, size_t workspace_bytes, void* stream);
+                          const int32_t* order, const int32_t* group_of, const void* group_ids, int ids_are_i64, const int32_t* starts,
+                          const int32_t* n_groups, int into, void* out, int64_t out_stride, int out_dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- losses of a layer's output: log probabilities, distillation ------------------------------ */
 

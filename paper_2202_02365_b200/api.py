@@ -101,9 +101,9 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
         _lib.mg_group_norm_backward.argtypes = [p, p, p, i64, p, i64, p, p, p, i64, p, p, p, C.c_size_t, p]
         _lib.mg_embedding.argtypes = [p, p, i64, C.c_int, i64, i32, p, C.c_int, i64, C.c_float, p, i64, C.c_int, p]
         _lib.mg_id_groups_workspace.argtypes = [p, i64, i64, p]
-        _lib.mg_id_groups.argtypes = [p, p, C.c_int, i64, i64, p, p, p, p, p, C.c_size_t, p]
+        _lib.mg_id_groups.argtypes = [p, p, C.c_int, i64, i64, p, p, p, p, p, p, C.c_size_t, p]
         _lib.mg_embedding_backward_workspace.argtypes = [p, i64, i64, i32, p]
-        _lib.mg_embedding_backward.argtypes = [p, p, i64, C.c_int, i64, i64, i32, C.c_float, p, p, C.c_int, p, p, C.c_int, p, i64, C.c_int, p, C.c_size_t, p]
+        _lib.mg_embedding_backward.argtypes = [p, p, i64, C.c_int, i64, i64, i32, C.c_float, p, p, p, C.c_int, p, p, C.c_int, p, i64, C.c_int, p, C.c_size_t, p]
         _lib.mg_log_probs.argtypes = [p, p, p, C.c_int, i32, p, p, p, p, p, p]
         _lib.mg_log_probs_backward.argtypes = [p, p, p, p, C.c_int, p, p, p, p, p, i64, p]
         _lib.mg_distill.argtypes = [p, p, p, p, p, p]
@@ -264,9 +264,10 @@ ROWS_TABLE, ROWS_ADD, ROWS_COMPACT = 0, 1, 2
 
 @dataclass(frozen=True)
 class IdGroups:
-    """The places of each id (Context.id_groups): `order` has them by ascending id, `ids` the distinct ids, `starts` where each one's places lie in
-    order, `count` (one element, on the device) how many ids there are; `ids` and `starts` mean nothing behind it."""
+    """The places of each id (Context.id_groups): `order` has them by ascending id, `group_of` which of the distinct `ids` each is of (-1: of none), `starts`
+    where each one's places lie in order, `count` (one element, on the device) how many ids there are; `ids` and `starts` mean nothing behind it."""
     order: torch.Tensor
+    group_of: torch.Tensor
     ids: torch.Tensor
     starts: torch.Tensor
     count: torch.Tensor
@@ -881,19 +882,19 @@ class Context:
         need = C.c_size_t(0)
         self._check(self.lib.mg_id_groups_workspace(self.handle, n, n_rows, C.byref(need)))
         work = torch.empty(need.value, dtype=torch.uint8, device=self.device)
-        block = torch.empty(n + most + 2, dtype=torch.int32, device=self.device)
-        order, starts, count = torch.split(block, [n, most + 1, 1])
+        block = torch.empty(2 * n + most + 2, dtype=torch.int32, device=self.device)
+        order, group_of, starts, count = torch.split(block, [n, n, most + 1, 1])
         distinct = torch.empty(most, dtype=ids.dtype, device=self.device)
-        self._check(self.lib.mg_id_groups(self.handle, ids.data_ptr(), wide, n, n_rows, order.data_ptr(), distinct.data_ptr(), starts.data_ptr(), count.data_ptr(),
+        self._check(self.lib.mg_id_groups(self.handle, ids.data_ptr(), wide, n, n_rows, order.data_ptr(), group_of.data_ptr(), distinct.data_ptr(), starts.data_ptr(), count.data_ptr(),
                                           work.data_ptr(), need.value, torch._C._cuda_getCurrentRawStream(self.device.index)))
-        return IdGroups(order, distinct, starts, count, n_rows)
+        return IdGroups(order, group_of, distinct, starts, count, n_rows)
 
     def _group_sums(self, d_y, groups: IdGroups, scale, into, out):
         n, dim = d_y.shape
         need = C.c_size_t(0)
         self._check(self.lib.mg_embedding_backward_workspace(self.handle, n, groups.n_rows, dim, C.byref(need)))
         work = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
-        self._check(self.lib.mg_embedding_backward(self.handle, d_y.data_ptr(), d_y.stride(0), ROW_TYPES[d_y.dtype], n, groups.n_rows, dim, scale, groups.order.data_ptr(),
+        self._check(self.lib.mg_embedding_backward(self.handle, d_y.data_ptr(), d_y.stride(0), ROW_TYPES[d_y.dtype], n, groups.n_rows, dim, scale, groups.order.data_ptr(), groups.group_of.data_ptr(),
                                                    groups.ids.data_ptr(), groups.ids.dtype == torch.int64, groups.starts.data_ptr(), groups.count.data_ptr(), into,
                                                    out.data_ptr(), out.stride(0), ROW_TYPES[out.dtype], _at(work), need.value,
                                                    torch._C._cuda_getCurrentRawStream(self.device.index)))

@@ -9,7 +9,7 @@
 
 namespace {
 
-constexpr int kSortBits = 8, kSortBins = 1 << kSortBits, kSortThreads = 256, kSortPer = 16, kSortTile = kSortThreads * kSortPer;
+constexpr int kPlanBits = 8, kPlanBins = 1 << kPlanBits, kPlanThreads = 256;   // of the sort
 
 inline size_t rows_align(size_t bytes) { return (bytes + 15) / 16 * 16; }
 
@@ -44,64 +44,88 @@ inline int check_lookup(mg_ctx* ctx, const void* table, int64_t table_stride, in
 // ---- groups of equal ids -----------------------------------------------------------------
 
 struct GroupPlan {
-    int passes = 0;          // of eight bits each
+    int passes = 0, bits = 0;   // of so many bits each
+    int per = 16;               // ids to a thread: fewer where tiles would be few
     int64_t tiles = 0;
-    size_t at_keys[2] = {0, 0}, at_order = 0, at_hist = 0, at_heads = 0, bytes = 0;
+    size_t cleared = 0, at_states = 0, at_chain = 0, at_keys[2] = {0, 0}, at_order = 0, bytes = 0;
 };
+constexpr size_t kSortSharedBytes = 4 * (4 * kPlanBins + 8);
 
 // keys are 0 .. n_rows; n_rows stands for an id that is no row
-inline GroupPlan plan_groups(int64_t n, int64_t n_rows) {
+inline GroupPlan plan_groups(int64_t n, int64_t n_rows, int n_sms = 148) {
     GroupPlan p;
     int bits = 1;
     while (bits < 31 && n_rows >> bits) ++bits;
-    p.passes = (bits + kSortBits - 1) / kSortBits;
-    p.tiles = (n + kSortTile - 1) / kSortTile;
+    p.passes = (bits + kPlanBits - 1) / kPlanBits;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    while (p.per > 4 && n < (int64_t)n_sms * kPlanThreads * p.per / 2) p.per /= 2;
+    p.tiles = (n + kPlanThreads * p.per - 1) / (kPlanThreads * p.per);
     size_t at = 0;
     const auto take = [&](size_t bytes) { const size_t was = at; at += rows_align(bytes); return was; };
+    take(kSortSharedBytes);
+    p.at_states = take(8 * (size_t)(p.passes * p.tiles) * kPlanBins);
+    p.at_chain = take(8 * (size_t)std::max<int64_t>(p.tiles, 1));
+    p.cleared = at;
     p.at_keys[0] = take(4 * (size_t)n);
     p.at_keys[1] = take(4 * (size_t)n);
     p.at_order = take(4 * (size_t)n);
-    p.at_hist = take(4 * (size_t)p.tiles * kSortBins);
-    p.at_heads = take(4 * (size_t)p.tiles);
     p.bytes = at;
     return p;
 }
 
-inline int check_groups(mg_ctx* ctx, const void* ids, int ids_are_i64, int64_t n, int64_t n_rows, const void* order, const void* group_ids, const void* starts,
-                        const void* n_groups, const void* workspace, size_t workspace_bytes) {
+inline int check_groups(mg_ctx* ctx, const void* ids, int ids_are_i64, int64_t n, int64_t n_rows, const void* order, const void* group_of, const void* group_ids,
+                        const void* starts, const void* n_groups, const void* workspace, size_t workspace_bytes) {
     if (int rc = check_ids(ctx, ids, ids_are_i64, n, n_rows)) return rc;
-    if ((n > 0 && !order) || (n > 0 && n_rows > 0 && !group_ids) || !starts || !n_groups) return mg_fail(ctx, MG_ERR_ARG, "null argument");
+    if ((n > 0 && (!order || !group_of)) || (n > 0 && n_rows > 0 && !group_ids) || !starts || !n_groups) return mg_fail(ctx, MG_ERR_ARG, "null argument");
     if (reinterpret_cast<uintptr_t>(group_ids) % (ids_are_i64 ? 8 : 4)) return mg_fail(ctx, MG_ERR_ARG, "the groups' ids are not aligned to their elements");
-    for (const void* p : {order, starts, n_groups})
-        if (reinterpret_cast<uintptr_t>(p) % 4) return mg_fail(ctx, MG_ERR_ARG, "order, starts and n_groups must be 4-byte aligned");
+    for (const void* p : {order, group_of, starts, n_groups})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return mg_fail(ctx, MG_ERR_ARG, "order, group_of, starts and n_groups must be 4-byte aligned");
     if (reinterpret_cast<uintptr_t>(workspace) % 16) return mg_fail(ctx, MG_ERR_ARG, "the workspace must be 16-byte aligned");
-    const size_t need = plan_groups(n, n_rows).bytes;
+    const size_t need = plan_groups(n, n_rows, ctx->n_sms).bytes;
     if (workspace_bytes < need || (!workspace && need)) return mg_fail(ctx, MG_ERR_CAPACITY, "the workspace is smaller than mg_id_groups_workspace says");
     return MG_OK;
 }
 
 // ---- sums by group -----------------------------------------------------------------------
 
-inline size_t sums_workspace(int64_t, int64_t, int32_t) { return 0; }
+struct SumPlan {
+    int32_t chunk = 1, chunks = 0, pitch = 0;
+    size_t at_begun = 0, bytes = 0;
+};
+
+// Places to a chunk: 1,536 threads of every multiprocessor are to have one, of 32 places at least (16 more of a row's values, or 8 lanes, make half as many chunks), and no
+// id is to leave more than 4,096 shares.
+inline SumPlan plan_sums(int64_t n, int64_t n_rows, int32_t dim, int n_sms = 148) {
+    SumPlan p;
+    p.pitch = (dim + 7) / 8 * 8;
+    if (n == 0 || n_rows == 0) return p;
+    const int64_t lanes = dim >= 128 ? (dim + 127) / 128 * 32 : dim > 64 ? 32 : dim > 32 ? 16 : dim > 16 ? 8 : 4;
+    p.chunk = (int32_t)std::max<int64_t>({n * lanes / ((int64_t)n_sms * 1536), n / 4096, 32});
+    p.chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
+    p.at_begun = rows_align(8 * (size_t)p.chunks * p.pitch);
+    p.bytes = p.at_begun + rows_align(4 * (size_t)p.chunks);
+    return p;
+}
+inline size_t sums_workspace(int64_t n, int64_t n_rows, int32_t dim, int n_sms = 148) { return plan_sums(n, n_rows, dim, n_sms).bytes; }
 
 inline int check_sums(mg_ctx* ctx, const void* d_y, int64_t d_y_stride, int d_y_dtype, int64_t n, int64_t n_rows, int32_t dim, float scale, const void* order,
-                      const void* group_ids, int ids_are_i64, const void* starts, const void* n_groups, int into, const void* out, int64_t out_stride, int out_dtype,
+                      const void* group_of, const void* group_ids, int ids_are_i64, const void* starts, const void* n_groups, int into, const void* out, int64_t out_stride, int out_dtype,
                       const void* workspace, size_t workspace_bytes) {
     if (!known_dtype(d_y_dtype) || !known_dtype(out_dtype)) return mg_fail(ctx, MG_ERR_ARG, "unknown dtype");
     if (dim < 1 || dim > 1 << 24) return mg_fail(ctx, MG_ERR_ARG, "the width of a row must be in [1, 2^24]");
     if (!isfinite(scale)) return mg_fail(ctx, MG_ERR_ARG, "the scale must be finite");
     if (into != MG_ROWS_TABLE && into != MG_ROWS_ADD && into != MG_ROWS_COMPACT) return mg_fail(ctx, MG_ERR_ARG, "unknown place for the sums");
     if (n < 0 || n >= (1ll << 31) - 1 || n_rows < 0 || n_rows >= (1ll << 31) - 1) return mg_fail(ctx, MG_ERR_ARG, "the numbers of ids and of rows must be in [0, 2^31 - 2]");
-    if ((n > 0 && !order) || (n > 0 && n_rows > 0 && !group_ids) || !starts || !n_groups) return mg_fail(ctx, MG_ERR_ARG, "null argument");
+    if ((n > 0 && (!order || !group_of)) || (n > 0 && n_rows > 0 && !group_ids) || !starts || !n_groups) return mg_fail(ctx, MG_ERR_ARG, "null argument");
     if (reinterpret_cast<uintptr_t>(group_ids) % (ids_are_i64 ? 8 : 4)) return mg_fail(ctx, MG_ERR_ARG, "the groups' ids are not aligned to their elements");
-    for (const void* p : {order, starts, n_groups})
-        if (reinterpret_cast<uintptr_t>(p) % 4) return mg_fail(ctx, MG_ERR_ARG, "order, starts and n_groups must be 4-byte aligned");
+    for (const void* p : {order, group_of, starts, n_groups})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return mg_fail(ctx, MG_ERR_ARG, "order, group_of, starts and n_groups must be 4-byte aligned");
     const int64_t out_rows = into == MG_ROWS_COMPACT ? std::min(n, n_rows) : n_rows;
     if (int rc = check_matrix(ctx, "d_y", d_y, d_y_stride, d_y_dtype, n, dim, false)) return rc;
     if (int rc = check_matrix(ctx, "the output", out, out_stride, out_dtype, out_rows, dim, true)) return rc;
     if (!lie_apart(d_y, d_y_stride, d_y_dtype, n, out, out_stride, out_dtype, out_rows, dim)) return mg_fail(ctx, MG_ERR_ARG, "the output overlaps d_y");
     if (reinterpret_cast<uintptr_t>(workspace) % 16) return mg_fail(ctx, MG_ERR_ARG, "the workspace must be 16-byte aligned");
-    const size_t need = sums_workspace(n, n_rows, dim);
+    const size_t need = sums_workspace(n, n_rows, dim, ctx->n_sms);
     if (workspace_bytes < need || (!workspace && need)) return mg_fail(ctx, MG_ERR_CAPACITY, "the workspace is smaller than mg_embedding_backward_workspace says");
     return MG_OK;
 }

@@ -1,0 +1,225 @@
+// The gradient of looked-up rows: sums over the places of each id, in an order that goes by the places alone.
+//
+// The sorted places are cut into chunks.  A part of a warp goes along a chunk's places, adds up rows and writes a sum where the id changes; an id that begins in the chunk and
+// ends no more than a chunk's length on is followed to its end, so that most ids are summed up in one go.  Of an id with more places than a chunk has, every chunk leaves
+// its share in the workspace, and a second kernel adds the shares up.  No float is added atomically.
+#pragma once
+
+#include "mg_norm.cuh"
+#include "mg_rows_sort.cuh"
+
+namespace mgrows {
+
+constexpr int kSumThreads = 256, kJoinThreads = 512;
+
+struct SumArgs {
+    const void* d_y; int64_t d_y_stride, n, n_rows;
+    int32_t dim; float scale;
+    const int32_t *order, *group_of, *starts, *n_groups; const void* group_ids; int ids_are_i64;
+    int into;
+    void* out; int64_t out_stride;
+    int32_t chunk, chunks;        // places to a chunk
+    float* shares; int32_t pitch; // [chunks][2][pitch]: of the id that the chunk begins within, of the one that goes on behind it
+    int32_t* begun;               // [chunks]: the group that begins in the chunk and has shares, -1
+};
+
+// how many groups there are, and places that belong to one
+__device__ __forceinline__ bool group_extent(const SumArgs& a, int32_t* groups, int64_t* places) {
+    *groups = *a.n_groups;
+    if (*groups <= 0 || *groups > min(a.n, a.n_rows)) return false;
+    *places = min((int64_t)a.starts[*groups], a.n);
+    return true;
+}
+
+template <typename O, int VEC>
+__device__ __forceinline__ void write_sum(const SumArgs& a, int64_t row, int32_t c, float (&s)[VEC]) {
+    O* to = static_cast<O*>(a.out) + row * a.out_stride + c;
+    Raw<O, VEC> raw;
+    if (a.into == MG_ROWS_ADD) {
+        raw.load(to);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s[e] = fmaf(s[e], a.scale, raw.get(e));
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) s[e] *= a.scale;
+    }
+    raw.put(s);
+    raw.store(to);
+}
+
+// `lanes` lanes to a chunk, NV vectors of its rows to a lane, U rows on their way; blockIdx.y: which of the rows' columns
+template <typename T, typename O, int VEC, int NV, int U>
+__global__ void __launch_bounds__(kSumThreads) k_chunk_sums(const __grid_constant__ SumArgs a, int lanes) {
+    chain_wait();
+    chain_start();
+    const int sub = (int)threadIdx.x & (lanes - 1);
+    const int32_t chunk = (int32_t)((blockIdx.x * (int64_t)kSumThreads + threadIdx.x) / lanes);
+    const int32_t c0 = ((int32_t)blockIdx.y * NV * lanes + sub) * VEC, step = lanes * VEC;
+    int32_t groups;
+    int64_t places, lo = 0, hi = 0;
+    int32_t before = -1, behind = -1;   // groups with shares: that go on from the chunk before, that go on behind this one
+    if (group_extent(a, &groups, &places) && chunk < a.chunks) {
+        lo = (int64_t)chunk * a.chunk;
+        hi = min(lo + a.chunk, places);
+        if (lo < hi) {
+            const auto group_at = [&](int64_t i) { return min(max(a.group_of[i], 0), groups - 1); };
+            const int32_t first = group_at(lo), came = lo > 0 ? group_at(lo - 1) : -1, last = group_at(hi - 1);
+            const int64_t end = a.starts[first + 1], last_end = a.starts[last + 1];
+            const bool long_first = end - a.starts[first] > a.chunk, long_last = last_end - a.starts[last] > a.chunk;
+            if (came == first) {
+                if (long_first) before = first;
+                else lo = end;            // whom it began with has it
+            }
+            if (long_last) { if (last_end > hi && last != before) behind = last; }
+            else if (last != before && lo < hi) hi = min(last_end, places);
+        }
+    }
+    if (sub == 0 && blockIdx.y == 0 && chunk < a.chunks) a.begun[chunk] = behind;
+    float acc[NV][VEC];
+#pragma unroll
+    for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) acc[v][e] = 0.f;
+    int32_t cur = -1;
+    int64_t cur_row = -1;
+    const auto flush = [&]() {
+        if (cur < 0) return;
+        const bool share = cur == before || cur == behind;
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            const int32_t c = c0 + v * step;
+            if (c < a.dim) {
+                if (share) {
+                    float* to = a.shares + ((int64_t)chunk * 2 + (cur == behind)) * a.pitch + c;
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) to[e] = acc[v][e];
+                } else if (cur_row >= 0) write_sum<O, VEC>(a, cur_row, c, acc[v]);
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) acc[v][e] = 0.f;
+        }
+    };
+    const uint32_t peers = lanes == 32 ? 0xFFFFFFFFu : (1u << lanes) - 1u << ((int)(threadIdx.x & 31) & ~(lanes - 1));
+    // a place and its group for each lane, asked for while those before are dealt with; then the rows, U at a time
+    int32_t next_place = -1, next_group = -1;
+    if (lo + sub < hi) { next_place = a.order[lo + sub]; next_group = a.group_of[lo + sub]; }
+    for (int64_t p = lo; p < hi; p += lanes) {
+        int32_t place = next_place;
+        const int32_t group = next_group;
+        int64_t row = group < 0 || group >= groups ? -1 : a.into == MG_ROWS_COMPACT ? group : id_at(a.group_ids, a.ids_are_i64, group);
+        if (row >= a.n_rows) row = -1;
+        if (place >= a.n) place = -1;
+        next_place = next_group = -1;
+        if (p + lanes + sub < hi) { next_place = a.order[p + lanes + sub]; next_group = a.group_of[p + lanes + sub]; }
+        const int count = (int)min((int64_t)lanes, hi - p);
+        for (int i0 = 0; i0 < count; i0 += U) {
+            Raw<T, VEC> raw[U][NV];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int32_t at = __shfl_sync(peers, place, (i0 + u) & (lanes - 1), lanes);
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    if (i0 + u < count && at >= 0 && c0 + v * step < a.dim) raw[u][v].load(static_cast<const T*>(a.d_y) + at * a.d_y_stride + c0 + v * step);
+                    else raw[u][v].zero();
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int32_t g = __shfl_sync(peers, group, (i0 + u) & (lanes - 1), lanes);
+                const int32_t r = __shfl_sync(peers, (int32_t)row, (i0 + u) & (lanes - 1), lanes);
+                if (i0 + u < count) {
+                    if (g != cur) { flush(); cur = g; cur_row = r; }
+#pragma unroll
+                    for (int v = 0; v < NV; ++v)
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) acc[v][e] += raw[u][v].get(e);
+                }
+            }
+        }
+    }
+    flush();
+}
+
+// The shares of the id that begins in a chunk and goes on behind it: 32 lanes of four columns, 16 warps that each take a stretch of the chunks.
+template <typename O>
+__global__ void __launch_bounds__(kJoinThreads) k_join_shares(const __grid_constant__ SumArgs a) {
+    constexpr int W = kJoinThreads / 32;
+    __shared__ float4 part[W][32];
+    chain_wait();
+    chain_start();
+    const int32_t chunk = (int32_t)blockIdx.x, g = a.begun[chunk];
+    if (g < 0) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int32_t c = ((int32_t)blockIdx.y * 32 + lane) * 4;
+    const int64_t end = min((int64_t)a.starts[g + 1], a.n);
+    const int32_t last = min((int32_t)((end - 1) / a.chunk), a.chunks - 1), shares = last - chunk + 1;
+    const int32_t lo = (int32_t)((int64_t)shares * warp / W), hi = (int32_t)((int64_t)shares * (warp + 1) / W);
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c < a.dim) {
+        constexpr int U = 4;
+        for (int32_t i0 = lo; i0 < hi; i0 += U) {
+            float4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)   // (the first chunk's is the share of an id that begins there)
+                v[u] = i0 + u < hi ? *reinterpret_cast<const float4*>(a.shares + ((int64_t)(chunk + i0 + u) * 2 + (i0 + u == 0)) * a.pitch + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int u = 0; u < U; ++u) { s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w; }
+        }
+    }
+    part[warp][lane] = s;
+    __syncthreads();
+    if (warp || c >= a.dim) return;
+    for (int w = 1; w < W; ++w) { const float4 o = part[w][lane]; s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w; }
+    const int64_t row = a.into == MG_ROWS_COMPACT ? g : id_at(a.group_ids, a.ids_are_i64, g);
+    if (row < 0 || row >= a.n_rows) return;
+    const float all[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < a.dim) {
+            float one[1] = {all[e]};
+            write_sum<O, 1>(a, row, c + e, one);
+        }
+}
+
+// Zeros into the rows of the table that no id names: a block finds the named ones among its rows, marks them in shared memory and writes the others.
+constexpr int kMostZeroRows = 2048;
+template <typename O, int VEC>
+__global__ void __launch_bounds__(kSumThreads) k_zero_others(const __grid_constant__ SumArgs a, int zero_rows) {
+    __shared__ uint32_t named[kMostZeroRows / 32];
+    __shared__ int64_t sh_first;
+    chain_wait();
+    chain_start();
+    const int64_t r0 = (int64_t)blockIdx.x * zero_rows, r1 = min(r0 + zero_rows, a.n_rows);
+    const int64_t groups = max((int64_t)0, min((int64_t)*a.n_groups, min(a.n, a.n_rows)));
+    if (threadIdx.x < kMostZeroRows / 32) named[threadIdx.x] = 0;
+    if (threadIdx.x < 32) {
+        // the first group whose id is r0 or more, 32 probes at a time
+        int64_t lo = 0, hi = groups;
+        while (lo < hi) {
+            const int64_t step = (hi - lo + 31) / 32, at = lo + step * threadIdx.x;
+            const uint32_t below = __ballot_sync(0xFFFFFFFFu, at < hi && id_at(a.group_ids, a.ids_are_i64, at) < r0);
+            const int k = __popc(below);   // the probes up to it lie below
+            hi = min(hi, k < 32 ? lo + step * k : hi);
+            lo = k ? lo + step * (k - 1) + 1 : lo;
+            if (k == 0) hi = lo;
+        }
+        if (threadIdx.x == 0) sh_first = lo;
+    }
+    __syncthreads();
+    for (int64_t g = sh_first + threadIdx.x; g < min(groups, sh_first + zero_rows); g += kSumThreads) {
+        const int64_t id = id_at(a.group_ids, a.ids_are_i64, g);
+        if (id >= r0 && id < r1) atomicOr(&named[(id - r0) >> 5], 1u << ((id - r0) & 31));
+    }
+    __syncthreads();
+    Raw<O, VEC> zero;
+    zero.zero();
+    const int vecs = a.dim / VEC, lanes = min(kSumThreads, max(1, 1 << (31 - __clz(max(vecs, 1)))));
+    const int sub = (int)threadIdx.x & (lanes - 1);
+    for (int64_t r = r0 + threadIdx.x / lanes; r < r1; r += kSumThreads / lanes) {
+        if (named[(r - r0) >> 5] >> ((r - r0) & 31) & 1) continue;
+        O* to = static_cast<O*>(a.out) + r * a.out_stride;
+        for (int v = sub; v < vecs; v += lanes) zero.store(to + v * VEC);
+    }
+}
+
+}  // namespace mgrows

@@ -139,6 +139,8 @@ def check_groups(groups, ids, n_rows):
     assert count == len(distinct) and torch.equal(groups.ids[:count].long(), distinct) and groups.ids.dtype == ids.dtype
     ends = torch.cat([torch.zeros(1, dtype=torch.int64, device="cuda"), sizes.cumsum(0)])
     assert torch.equal(groups.starts[:count + 1].long(), ends)
+    of = torch.repeat_interleave(torch.arange(count, device="cuda"), sizes)
+    assert torch.equal(groups.group_of[:len(of)].long(), of) and (groups.group_of[len(of):] == -1).all()
     key = torch.where(valid, flat, n_rows)
     assert torch.equal(groups.order.long(), torch.argsort(key, stable=True))
 
@@ -376,15 +378,16 @@ int main() {
     EXPECT(MG_ERR_ARG, lookup([](L& a) { a.ts = (1ll << 28) + 1; }));
     for (const float s : {(float)NAN, (float)INFINITY}) EXPECT(MG_ERR_ARG, lookup([&](L& a) { a.scale = s; }));
 
-    struct G { const void* ids; int wide; int64_t n, rows; const void *order, *gids, *starts, *count, *ws; size_t bytes; };
-    const G good{ids, 0, 1000, 500, base, far, far + 8000, far + 16000, more, 1 << 30};
-    const auto groups = [&](auto change) { G a = good; change(a); return check_groups(&context, a.ids, a.wide, a.n, a.rows, a.order, a.gids, a.starts, a.count, a.ws, a.bytes); };
+    struct G { const void* ids; int wide; int64_t n, rows; const void *order, *of, *gids, *starts, *count, *ws; size_t bytes; };
+    const G good{ids, 0, 1000, 500, base, base + 8000, far, far + 8000, far + 16000, more, 1 << 30};
+    const auto groups = [&](auto change) { G a = good; change(a); return check_groups(&context, a.ids, a.wide, a.n, a.rows, a.order, a.of, a.gids, a.starts, a.count, a.ws, a.bytes); };
     EXPECT(MG_OK, groups([](G&) {}));
     EXPECT(MG_OK, groups([](G& a) { a.bytes = plan_groups(a.n, a.rows).bytes; }));
     EXPECT(MG_ERR_CAPACITY, groups([](G& a) { a.bytes = plan_groups(a.n, a.rows).bytes - 1; }));
     EXPECT(MG_ERR_CAPACITY, groups([](G& a) { a.ws = nullptr; }));
     EXPECT(MG_ERR_ARG, groups([&](G& a) { a.ws = more + 8; }));
     EXPECT(MG_ERR_ARG, groups([](G& a) { a.order = nullptr; }));
+    EXPECT(MG_ERR_ARG, groups([](G& a) { a.of = nullptr; }));
     EXPECT(MG_ERR_ARG, groups([](G& a) { a.gids = nullptr; }));
     EXPECT(MG_ERR_ARG, groups([](G& a) { a.starts = nullptr; }));
     EXPECT(MG_ERR_ARG, groups([](G& a) { a.count = nullptr; }));
@@ -394,9 +397,9 @@ int main() {
     EXPECT(MG_ERR_ARG, groups([&](G& a) { a.rows = huge; }));
     EXPECT(MG_ERR_ARG, groups([](G& a) { a.ids = nullptr; }));
 
-    struct S { const void* d; int64_t ds; int dd; int64_t n, rows; int32_t dim; float scale; const void *order, *gids; int wide; const void *starts, *count; int into; const void* out; int64_t os; int od; const void* ws; size_t bytes; };
-    const S fine{base, 16, MG_DTYPE_F32, 1000, 500, 16, 1.f, ids, ids + 4000, 0, ids + 8000, ids + 16000, MG_ROWS_TABLE, far, 16, MG_DTYPE_F32, more, 1 << 30};
-    const auto sums = [&](auto change) { S a = fine; change(a); return check_sums(&context, a.d, a.ds, a.dd, a.n, a.rows, a.dim, a.scale, a.order, a.gids, a.wide, a.starts, a.count, a.into, a.out, a.os, a.od, a.ws, a.bytes); };
+    struct S { const void* d; int64_t ds; int dd; int64_t n, rows; int32_t dim; float scale; const void *order, *of, *gids; int wide; const void *starts, *count; int into; const void* out; int64_t os; int od; const void* ws; size_t bytes; };
+    const S fine{base, 16, MG_DTYPE_F32, 1000, 500, 16, 1.f, ids, ids + 20000, ids + 4000, 0, ids + 8000, ids + 16000, MG_ROWS_TABLE, far, 16, MG_DTYPE_F32, more, 1 << 30};
+    const auto sums = [&](auto change) { S a = fine; change(a); return check_sums(&context, a.d, a.ds, a.dd, a.n, a.rows, a.dim, a.scale, a.order, a.of, a.gids, a.wide, a.starts, a.count, a.into, a.out, a.os, a.od, a.ws, a.bytes); };
     EXPECT(MG_OK, sums([](S&) {}));
     EXPECT(MG_OK, sums([](S& a) { a.into = MG_ROWS_COMPACT; }));
     EXPECT(MG_OK, sums([](S& a) { a.bytes = sums_workspace(a.n, a.rows, a.dim); }));
