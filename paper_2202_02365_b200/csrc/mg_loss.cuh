@@ -58,16 +58,28 @@ template <int VEC> struct Cut {
     __device__ __forceinline__ int32_t edge(int32_t e) const { return e < head ? e : e + vecs * VEC; }
 };
 
-// over the lanes of one row: a power of two of them, side by side
-template <typename F>
-__device__ __forceinline__ float over_lanes(float v, int lanes, F f) {
-    for (int o = lanes >> 1; o; o >>= 1) v = f(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+// A row covered by 16-byte vectors of memory: the first and the last may reach beyond it.  Vector v has the classes from v VEC - lead on.
+template <int VEC> struct Cover {
+    int32_t lead, vecs;
+    __device__ __forceinline__ Cover(const void* row, int elem, int32_t classes, bool whole) {
+        lead = whole ? 0 : (int32_t)((uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u) / (uint32_t)elem);
+        vecs = (lead + classes + VEC - 1) / VEC;
+    }
+};
+
+// over the LANES lanes of one row, side by side
+template <int LANES, typename F>
+__device__ __forceinline__ float over_lanes(float v, F f) {
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) v = f(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
     return v;
 }
-__device__ __forceinline__ float lanes_sum(float v, int lanes) { return over_lanes(v, lanes, [](float a, float b) { return a + b; }); }
-__device__ __forceinline__ float lanes_max(float v, int lanes) { return over_lanes(v, lanes, [](float a, float b) { return fmaxf(a, b); }); }
-__device__ __forceinline__ uint64_t lanes_max(uint64_t v, int lanes) {
-    for (int o = lanes >> 1; o; o >>= 1) v = max(v, (uint64_t)__shfl_xor_sync(0xFFFFFFFFu, (unsigned long long)v, o));
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v) { return over_lanes<LANES>(v, [](float a, float b) { return a + b; }); }
+template <int LANES> __device__ __forceinline__ float lanes_max(float v) { return over_lanes<LANES>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int LANES>
+__device__ __forceinline__ uint64_t lanes_max(uint64_t v) {
+#pragma unroll
+    for (int o = LANES / 2; o; o >>= 1) v = max(v, (uint64_t)__shfl_xor_sync(0xFFFFFFFFu, (unsigned long long)v, o));
     return v;
 }
 

@@ -1,0 +1,20 @@
+// Launches of the losses' gradients.
+#include "mg_loss_grad.cuh"
+#include "mg_loss_launch.cuh"
+
+namespace mgloss {
+
+void launch_scores_grad(const GradLaunch& l, const GradArgs& a, cudaStream_t st) {
+    const auto go = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kGradThreads, 0, st>>>(a, l.lanes, l.chunks); };
+    MG_LOSS_BY_TYPE(l.dtype, (l.whole ? go(k_scores_grad<T, true, true>) : l.same ? go(k_scores_grad<T, true, false>) : go(k_scores_grad<T, false, false>)));
+}
+
+void launch_distill_grad(const GradLaunch& l, const GradArgs& a, cudaStream_t st) {
+    const auto rows = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kGradThreads, 0, st>>>(a); };
+    const auto block = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kGradThreads, 0, st>>>(a, l.chunks); };
+    if (l.lanes == 8) MG_LOSS_BY_TYPE(l.dtype, (l.whole ? rows(k_distill_grad_rows<T, 8, true, true>) : l.same ? rows(k_distill_grad_rows<T, 8, true, false>) : rows(k_distill_grad_rows<T, 8, false, false>)));
+    else if (l.lanes == 32) MG_LOSS_BY_TYPE(l.dtype, (l.whole ? rows(k_distill_grad_rows<T, 32, true, true>) : l.same ? rows(k_distill_grad_rows<T, 32, true, false>) : rows(k_distill_grad_rows<T, 32, false, false>)));
+    else MG_LOSS_BY_TYPE(l.dtype, (l.whole ? block(k_distill_grad<T, true, true>) : l.same ? block(k_distill_grad<T, true, false>) : block(k_distill_grad<T, false, false>)));
+}
+
+}  // namespace mgloss

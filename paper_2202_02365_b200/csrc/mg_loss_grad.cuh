@@ -8,18 +8,18 @@ namespace mgloss {
 
 constexpr int kGradThreads = 256, kGradBatch = 4;   // vectors of a thread that are on their way at once
 
-// what a row's gradient is made of: p (base + slope log p), and `more` at the label
-struct RowGrad { float scale, minus_lse, base, slope, more; int32_t label; };
+// What a row's gradient is made of: p (base + slope log p).
+struct RowGrad { float scale, minus_lse, base, slope; };
 
-// the gradients of the classes c .. c + N - 1, in place of their logits
-template <bool LABELS, int N>
-__device__ __forceinline__ void grads(const RowGrad& g, float (&v)[N], int32_t c) {
+// the gradients of neighbouring classes, in place of their logits
+template <int N>
+__device__ __forceinline__ void grads(const RowGrad& g, float (&v)[N]) {
     if constexpr (N == 1) {
         const float log_p = fmaf(v[0], g.scale, g.minus_lse);
-        v[0] = fast_exp2(log_p * kLog2e) * (LABELS ? fmaf(fmaxf(log_p, kLeast), g.slope, g.base) : g.base);
+        v[0] = fast_exp2(log_p * kLog2e) * fmaf(fmaxf(log_p, kLeast), g.slope, g.base);
     } else {
         const Pair scale = pair(g.scale, g.scale), lse = pair(g.minus_lse, g.minus_lse), base = pair(g.base, g.base), slope = pair(g.slope, g.slope), log2e = pair(kLog2e, kLog2e);
-        const bool sloped = LABELS && g.slope != 0.f;
+        const bool sloped = g.slope != 0.f;
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
             const Pair log_p = fma2(pair(v[i], v[i + 1]), scale, lse), y = mul2(log_p, log2e);
@@ -34,67 +34,77 @@ __device__ __forceinline__ void grads(const RowGrad& g, float (&v)[N], int32_t c
             split(d, &v[i], &v[i + 1]);
         }
     }
-    if (LABELS && (uint32_t)(g.label - c) < (uint32_t)N) {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (c + i == g.label) v[i] += g.more;
-    }
 }
 
-// Vectors [lo, hi) of a row cut where the gradient's vectors begin, and with `edges` the elements before and behind all vectors; by `lanes` threads.  SAME: the logits' vectors
-// begin there too; else they are read element by element.
-template <bool LABELS, bool SAME, typename T>
-__device__ __forceinline__ void stream_row(const RowGrad& g, bool zero, const T* x, T* d, const Cut<16 / sizeof(T)>& cut, int32_t lo, int32_t hi, bool edges, int sub, int lanes) {
+// one class's gradient, and `more`
+template <typename T>
+__device__ __forceinline__ void write_one(const RowGrad& g, float x, float more, T* to) {
+    float f[1] = {x};
+    grads(g, f);
+    f[0] += more;
+    Raw<T, 1> one;
+    one.put(f);
+    one.store(to);
+}
+
+// Vectors [lo, hi) of what covers the gradient's row, by `lanes` threads.  WHOLE: rows of both begin and end with a vector; SAME: the logits' vectors begin where the
+// gradient's do, else they are read element by element (a row of 50,257 fp32 logits 8 bytes off: as fast, the elements come from the first-level cache).
+template <bool SAME, bool WHOLE, typename T>
+__device__ __forceinline__ void stream_row(const RowGrad& g, bool zero, const T* x, T* d, int32_t classes, int32_t lead, int32_t lo, int32_t hi, int sub, int lanes) {
     constexpr int VEC = 16 / sizeof(T);
     for (int32_t v0 = lo + sub; v0 < hi; v0 += kGradBatch * lanes) {
         Raw<T, VEC> raw[kGradBatch];
         T one[SAME ? 1 : kGradBatch * VEC];
         if (!zero) {
 #pragma unroll
-            for (int j = 0; j < kGradBatch; ++j)
-                if (v0 + j * lanes < hi) {
-                    const T* at = x + cut.head + (v0 + j * lanes) * VEC;
-                    if constexpr (SAME) raw[j].load(at);
+            for (int j = 0; j < kGradBatch; ++j) {
+                const int32_t c = (v0 + j * lanes) * VEC - lead;
+                if (v0 + j * lanes < hi && (WHOLE || (c >= 0 && c + VEC <= classes))) {
+                    if constexpr (SAME) raw[j].load(x + c);
                     else
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) one[j * VEC + e] = at[e];
+                        for (int e = 0; e < VEC; ++e) one[j * VEC + e] = x[c + e];
                 }
+            }
         }
 #pragma unroll
-        for (int j = 0; j < kGradBatch; ++j)
-            if (v0 + j * lanes < hi) {
-                const int32_t c = cut.head + (v0 + j * lanes) * VEC;
-                float f[VEC];
+        for (int j = 0; j < kGradBatch; ++j) {
+            if (v0 + j * lanes >= hi) continue;
+            const int32_t c = (v0 + j * lanes) * VEC - lead;
+            const bool full = WHOLE || (c >= 0 && c + VEC <= classes);
+            float f[VEC];
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    if constexpr (SAME) f[e] = raw[j].get(e);
-                    else f[e] = to_float(one[j * VEC + e]);
-                }
-                if (zero) {
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) f[e] = 0.f;
-                } else grads<LABELS>(g, f, c);
-                raw[j].put(f);
-                raw[j].store(d + c);
+            for (int e = 0; e < VEC; ++e) {
+                if constexpr (SAME) f[e] = raw[j].get(e);
+                else f[e] = to_float(one[j * VEC + e]);
             }
+            if (!full && !zero)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (c + e >= 0 && c + e < classes) f[e] = to_float(x[c + e]);
+            if (zero) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) f[e] = 0.f;
+            } else grads(g, f);
+            raw[j].put(f);
+            if (full) raw[j].store(d + c);
+            else
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (c + e >= 0 && c + e < classes) {
+                        Raw<T, 1> one_out;
+                        const float v[1] = {f[e]};
+                        one_out.put(v);
+                        one_out.store(d + c + e);
+                    }
+        }
     }
-    if (edges)
-        for (int e = sub; e < cut.edges; e += lanes) {
-            const int32_t c = cut.edge(e);
-            float f[1] = {0.f};
-            if (!zero) {
-                f[0] = to_float(x[c]);
-                grads<LABELS>(g, f, c);
-            }
-            Raw<T, 1> one;
-            one.put(f);
-            one.store(d + c);
-        }
 }
 
-// `lanes` threads to a row, or to one of its `chunks` pieces
-template <typename T, bool SAME>
+// `lanes` threads to a row, or to one of its `chunks` pieces.  The label's gradient is written over what its vector got, by the thread that had the vector.
+template <typename T, bool SAME, bool WHOLE>
 __global__ void __launch_bounds__(kGradThreads) k_scores_grad(const __grid_constant__ GradArgs a, int lanes, int chunks) {
+    constexpr int VEC = 16 / sizeof(T);
     const int group = (int)threadIdx.x / lanes, sub = (int)threadIdx.x & (lanes - 1), groups = kGradThreads / lanes;
     const int64_t items = a.rows * chunks;
     for (int64_t i = (int64_t)blockIdx.x * groups + group; i < items; i += (int64_t)gridDim.x * groups) {
@@ -102,15 +112,20 @@ __global__ void __launch_bounds__(kGradThreads) k_scores_grad(const __grid_const
         const int32_t chunk = (int32_t)(i - r * chunks);
         const T* x = static_cast<const T*>(a.x) + r * a.stride;
         T* d = static_cast<T*>(a.d) + r * a.d_stride;
-        const Cut<16 / sizeof(T)> cut(d, sizeof(T), a.classes);
+        const Cover<VEC> cover(d, sizeof(T), a.classes, WHOLE);
+        int32_t lo = 0, hi = cover.vecs;
+        if (chunks > 1) { lo = (int32_t)((int64_t)cover.vecs * chunk / chunks); hi = (int32_t)((int64_t)cover.vecs * (chunk + 1) / chunks); }
         const float lse = a.lse[r];
-        RowGrad g;
-        g.label = a.d_log_prob ? class_at(a.labels, a.labels_are_i64, r, a.classes) : -1;
-        const float of_label = g.label >= 0 ? a.d_log_prob[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f, l = a.d_lse ? a.d_lse[r] : 0.f;
+        const int32_t label = a.d_log_prob ? class_at(a.labels, a.labels_are_i64, r, a.classes) : -1;
+        const float of_label = label >= 0 ? a.d_log_prob[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f, l = a.d_lse ? a.d_lse[r] : 0.f;
         const float entropy = h != 0.f ? a.entropy[r] : 0.f;
         const bool zero = (of_label == 0.f && h == 0.f && l == 0.f) || lse == kNegInf;
-        g.scale = a.scale; g.minus_lse = -lse; g.base = a.scale * (l - of_label - h * entropy); g.slope = -a.scale * h; g.more = a.scale * of_label;
-        stream_row<true, SAME>(g, zero, x, d, cut, (int32_t)((int64_t)cut.vecs * chunk / chunks), (int32_t)((int64_t)cut.vecs * (chunk + 1) / chunks), chunk == 0, sub, lanes);
+        const RowGrad g{a.scale, -lse, a.scale * (l - of_label - h * entropy), -a.scale * h};
+        const int32_t at = (label + cover.lead) / VEC;
+        const bool mine = label >= 0 && !zero && at >= lo && at < hi && ((at - lo) & (lanes - 1)) == sub;
+        const float x_label = mine ? to_float(x[label]) : 0.f;
+        stream_row<SAME, WHOLE>(g, zero, x, d, a.classes, cover.lead, lo, hi, sub, lanes);
+        if (mine) write_one(g, x_label, a.scale * of_label, d + label);
     }
 }
 
@@ -131,109 +146,106 @@ __device__ __forceinline__ bool first_of_class(const int32_t* c, const float* q,
 
 constexpr int kTeacherRoom = 8;   // pairs that a row of the narrow kernel may have, for each of its lanes
 
-template <typename T, bool SAME>
-__global__ void __launch_bounds__(kGradThreads) k_distill_grad_rows(const __grid_constant__ GradArgs a, int lanes) {
+template <typename T, int LANES, bool SAME, bool WHOLE>
+__global__ void __launch_bounds__(kGradThreads) k_distill_grad_rows(const __grid_constant__ GradArgs a) {
+    constexpr int GROUPS = kGradThreads / LANES;
     __shared__ int32_t all_c[kGradThreads * kTeacherRoom];
-    __shared__ float all_q[kGradThreads * kTeacherRoom], all_d[kGradThreads * kTeacherRoom];
+    __shared__ float all_q[kGradThreads * kTeacherRoom], all_x[kGradThreads * kTeacherRoom];
     const TeacherArgs& t = a.teacher;
-    const int group = (int)threadIdx.x / lanes, sub = (int)threadIdx.x & (lanes - 1), groups = kGradThreads / lanes;
-    int32_t* c = all_c + group * lanes * kTeacherRoom;
-    float *q = all_q + group * lanes * kTeacherRoom, *own = all_d + group * lanes * kTeacherRoom;
-    for (int64_t r0 = (int64_t)blockIdx.x * groups; r0 < a.rows; r0 += (int64_t)gridDim.x * groups) {
+    const int group = (int)threadIdx.x / LANES, sub = (int)threadIdx.x % LANES;
+    int32_t* c = all_c + group * LANES * kTeacherRoom;
+    float *q = all_q + group * LANES * kTeacherRoom, *at_class = all_x + group * LANES * kTeacherRoom;
+    for (int64_t r0 = (int64_t)blockIdx.x * GROUPS; r0 < a.rows; r0 += (int64_t)gridDim.x * GROUPS) {
         const int64_t r = r0 + group;
         const bool on = r < a.rows;
         const T* x = static_cast<const T*>(a.x) + (on ? r : 0) * a.stride;
         T* d = static_cast<T*>(a.d) + (on ? r : 0) * a.d_stride;
         const float lse = on ? a.lse[r] : 0.f, d_loss = on ? a.d_loss[r] : 0.f;
-        float shift, sum, mass = 0.f;
-        teacher_sums(t, r, on, a.classes, a.scale, sub, lanes, &shift, &sum);
-        const float part = sum == 0.f ? 0.f : 1.f / sum;
-        for (int k = sub; on && k < t.entries; k += lanes) {
+        // the pairs' classes, values (times the scale) and logits
+        float m = kNegInf, shift, sum = 1.f, mass = 0.f;
+        for (int k = sub; on && k < t.entries; k += LANES) {
             c[k] = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, a.classes);
-            q[k] = c[k] >= 0 ? fast_exp2((a.scale * float_at(t.values, t.dtype, r * t.values_stride + k) - shift) * kLog2e) * part : 0.f;
+            if (c[k] < 0) continue;
+            q[k] = a.scale * float_at(t.values, t.dtype, r * t.values_stride + k);
+            at_class[k] = to_float(x[c[k]]);
+            m = fmaxf(m, q[k]);
+        }
+        if (t.lse) shift = on ? t.lse[r] : 0.f;
+        else {
+            shift = centre(lanes_max<LANES>(m));
+            sum = 0.f;
+            for (int k = sub; on && k < t.entries; k += LANES)
+                if (c[k] >= 0) sum += fast_exp2((q[k] - shift) * kLog2e);
+            sum = lanes_sum<LANES>(sum);
+        }
+        const float part = sum == 0.f ? 0.f : 1.f / sum;
+        for (int k = sub; on && k < t.entries; k += LANES) {
+            q[k] = c[k] >= 0 ? fast_exp2((q[k] - shift) * kLog2e) * part : 0.f;
             mass += q[k];
         }
-        mass = lanes_sum(mass, lanes);
+        mass = lanes_sum<LANES>(mass);
         const bool zero = d_loss == 0.f || mass == 0.f || lse == kNegInf;
-        RowGrad g;
-        g.scale = a.scale; g.minus_lse = -lse; g.base = a.scale * d_loss * mass; g.slope = g.more = 0.f; g.label = -1;
+        const RowGrad g{a.scale, -lse, a.scale * d_loss * mass, 0.f};
         __syncwarp();
-        uint32_t first = 0;   // which of the lane's pairs are the first of their class
-        for (int k = sub, i = 0; on && !zero && k < t.entries; k += lanes, ++i) {
+        const Cover<16 / sizeof(T)> cover(d, sizeof(T), a.classes, WHOLE);
+        if (on) stream_row<SAME, WHOLE>(g, zero, x, d, a.classes, cover.lead, 0, cover.vecs, sub, LANES);
+        __syncwarp();
+        for (int k = sub; on && !zero && k < t.entries; k += LANES) {
             float of_class;
-            if (first_of_class(c, q, k, t.entries, &of_class)) {
-                float f[1] = {to_float(x[c[k]])};
-                grads<false>(g, f, 0);
-                own[k] = f[0] - a.scale * d_loss * of_class;
-                first |= 1u << i;
-            }
+            if (first_of_class(c, q, k, t.entries, &of_class)) write_one(g, at_class[k], -a.scale * d_loss * of_class, d + c[k]);
         }
-        __syncwarp();
-        const Cut<16 / sizeof(T)> cut(d, sizeof(T), a.classes);
-        if (on) stream_row<false, SAME>(g, zero, x, d, cut, 0, cut.vecs, true, sub, lanes);
-        __syncwarp();
-        for (int k = sub; first; k += lanes, first >>= 1)
-            if (first & 1) {
-                Raw<T, 1> one;
-                const float f[1] = {own[k]};
-                one.put(f);
-                one.store(d + c[k]);
-            }
         __syncwarp();
     }
 }
 
 // a block to a row, or to one of its `chunks` pieces
-template <typename T, bool SAME>
+template <typename T, bool SAME, bool WHOLE>
 __global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_constant__ GradArgs a, int chunks) {
-    __shared__ int32_t c[MG_MAX_TEACHER];
-    __shared__ float q[MG_MAX_TEACHER], warps[kWideWarps];
     constexpr int VEC = 16 / sizeof(T);
+    __shared__ int32_t c[MG_MAX_TEACHER];
+    __shared__ float q[MG_MAX_TEACHER], scratch[8], sh_mass;
     const TeacherArgs& t = a.teacher;
     const int64_t r = blockIdx.x / (unsigned)chunks;
     const int32_t chunk = (int32_t)(blockIdx.x - (unsigned)r * (unsigned)chunks);
     const T* x = static_cast<const T*>(a.x) + r * a.stride;
     T* d = static_cast<T*>(a.d) + r * a.d_stride;
     const float lse = a.lse[r], d_loss = a.d_loss[r];
+    const Cover<VEC> cover(d, sizeof(T), a.classes, WHOLE);
+    const int32_t lo = (int32_t)((int64_t)cover.vecs * chunk / chunks), hi = (int32_t)((int64_t)cover.vecs * (chunk + 1) / chunks);
+    const int warps = (min(t.entries, 256) + 31) / 32;
     TeacherRow row;
-    row.load(t, r, a.classes, a.scale, warps);
-    float mass = 0.f;
+    float at_class[kTeacherEach];
+    if ((int)threadIdx.x < warps * 32) {
+        row.load(t, r, a.classes, a.scale);
 #pragma unroll
-    for (int i = 0; i < kTeacherEach; ++i) {
-        const int k = threadIdx.x + i * kWideThreads;
-        if (k < t.entries) { c[k] = row.c[i]; q[k] = row.q[i]; }
-        mass += row.q[i];
-    }
-    mass = block_sum(mass, warps);   // (and c and q are there for all)
-    const bool zero = d_loss == 0.f || mass == 0.f || lse == kNegInf;
-    RowGrad g;
-    g.scale = a.scale; g.minus_lse = -lse; g.base = a.scale * d_loss * mass; g.slope = g.more = 0.f; g.label = -1;
-    const Cut<VEC> cut(d, sizeof(T), a.classes);
-    const int32_t lo = (int32_t)((int64_t)cut.vecs * chunk / chunks), hi = (int32_t)((int64_t)cut.vecs * (chunk + 1) / chunks);
-    float own[kTeacherEach];
-#pragma unroll
-    for (int i = 0; i < kTeacherEach; ++i) {
-        const int k = threadIdx.x + i * kWideThreads;
-        const int32_t at = row.c[i] - cut.head;
-        const bool here = row.c[i] >= 0 && !zero && (at >= 0 && at < cut.vecs * VEC ? at >= lo * VEC && at < hi * VEC : chunk == 0);
-        float of_class;
-        if (here && first_of_class(c, q, k, t.entries, &of_class)) {
-            float f[1] = {to_float(x[row.c[i]])};
-            grads<false>(g, f, 0);
-            own[i] = f[0] - a.scale * d_loss * of_class;
-        } else row.c[i] = -1;
-    }
-    __syncthreads();
-    stream_row<false, SAME>(g, zero, x, d, cut, lo, hi, chunk == 0, (int)threadIdx.x, kGradThreads);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kTeacherEach; ++i)
-        if (row.c[i] >= 0) {
-            Raw<T, 1> one;
-            const float f[1] = {own[i]};
-            one.put(f);
-            one.store(d + row.c[i]);
+        for (int i = 0; i < kTeacherEach; ++i) {
+            const int32_t at = row.c[i] >= 0 ? (row.c[i] + cover.lead) / VEC : -1;
+            at_class[i] = at >= lo && at < hi ? to_float(x[row.c[i]]) : 0.f;
         }
+        float log_shift;
+        const float mass = row.probabilities(t, r, warps, scratch, &log_shift);
+#pragma unroll
+        for (int i = 0; i < kTeacherEach; ++i) {
+            const int k = threadIdx.x + i * 256;
+            if (k < t.entries) { c[k] = row.c[i]; q[k] = row.v[i]; }
+        }
+        if (threadIdx.x == 0) sh_mass = mass;
+    }
+    __syncthreads();
+    const float mass = sh_mass;
+    const bool zero = d_loss == 0.f || mass == 0.f || lse == kNegInf;
+    const RowGrad g{a.scale, -lse, a.scale * d_loss * mass, 0.f};
+    stream_row<SAME, WHOLE>(g, zero, x, d, a.classes, cover.lead, lo, hi, (int)threadIdx.x, kGradThreads);
+    __syncthreads();
+    if (zero || (int)threadIdx.x >= warps * 32) return;
+#pragma unroll
+    for (int i = 0; i < kTeacherEach; ++i) {
+        const int k = threadIdx.x + i * 256;
+        if (k >= t.entries) break;
+        const int32_t at = row.c[i] >= 0 ? (row.c[i] + cover.lead) / VEC : -1;
+        float of_class;
+        if (at >= lo && at < hi && first_of_class(c, q, k, t.entries, &of_class)) write_one(g, at_class[i], -a.scale * d_loss * of_class, d + row.c[i]);
+    }
 }
 
 }  // namespace mgloss

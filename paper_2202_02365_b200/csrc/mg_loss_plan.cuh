@@ -1,4 +1,4 @@
-// Host side of the losses: checks of arguments.  No CUDA calls.
+// Host side of the losses: checks of arguments, and how a call is cut into work.  No CUDA calls.
 #pragma once
 
 #include <math.h>
@@ -78,6 +78,71 @@ inline int check_distill_backward(mg_ctx* ctx, const mg_logits* z, const float* 
     if (z->rows > 0 && !d_loss) return mg_fail(ctx, MG_ERR_ARG, "null gradient of the loss");
     if (int rc = check_floats(ctx, {lse, d_loss})) return rc;
     return check_gradient(ctx, z, lse, d_x, d_x_stride);
+}
+
+// ---- how a call is cut ------------------------------------------------------------------
+
+// rows that begin and end with a 16-byte vector each
+inline bool whole_vectors(const void* p, int64_t stride, int64_t rows, int32_t classes, int dtype) {
+    const int64_t vec = 16 / elem_size(dtype);
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && classes % vec == 0 && (rows <= 1 || stride % vec == 0);
+}
+// two matrices whose rows begin equally far from one
+inline bool same_phase(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t rows, int dtype) {
+    const int64_t vec = 16 / elem_size(dtype);
+    return (reinterpret_cast<uintptr_t>(a) - reinterpret_cast<uintptr_t>(b)) % 16 == 0 && (rows <= 1 || (a_stride - b_stride) % vec == 0);
+}
+
+constexpr int kPlanRowThreads = 256, kPlanHeld = 32;   // of the narrow kernels; values of a row to a lane
+constexpr int kPlanWideThreads = 256, kPlanWideMost = 1024, kPlanWideVecs = 8;
+
+struct ForwardPlan { int nv = 0, lanes = 0, parts = 1, threads = 0; int64_t blocks = 0; };
+
+// Rows that 32 lanes hold in registers are narrow (however they lie to the vectors): 8 lanes to a row where these hold it and are as many as best classes are asked for.
+// Wide rows: a block goes along one, or a cluster of up to 16 blocks where rows are fewer than the GPU holds blocks (four to a multiprocessor), a quarter of a segment of
+// registers to each at least; where all of these leave room, blocks of 1,024 threads.
+inline ForwardPlan plan_forward(const mg_logits* z, int32_t top, int n_sms) {
+    ForwardPlan p;
+    const int64_t vec = 16 / elem_size(z->dtype), covered = (z->classes + vec - 1 + vec - 1) / vec, held = kPlanHeld / vec;
+    if (covered <= 32 * held) {
+        p.lanes = covered <= 8 * held && top <= 8 ? 8 : 32;
+        p.nv = (int)((covered + p.lanes - 1) / p.lanes);
+        p.threads = kPlanRowThreads;
+        const int64_t groups = kPlanRowThreads / p.lanes;
+        p.blocks = std::min<int64_t>((z->rows + groups - 1) / groups, (int64_t)n_sms * 64);
+        return p;
+    }
+    const int64_t segment = (int64_t)kPlanWideThreads * kPlanWideVecs * vec;
+    while (p.parts < 16 && z->rows * p.parts * 2 <= 4ll * n_sms && z->classes / (p.parts * 2) >= segment / 4) p.parts *= 2;
+    p.threads = z->rows * p.parts <= n_sms && z->classes / p.parts > 2 * segment ? kPlanWideMost : kPlanWideThreads;
+    p.blocks = z->rows * p.parts;
+    return p;
+}
+
+constexpr int kPlanGradThreads = 256, kPlanGradBatch = 4, kPlanTeacherRoom = 8;
+
+struct GradPlan { int lanes = 0, chunks = 1; int64_t blocks = 0; };
+
+// Gradients: threads to a row, so that each has up to eight vectors; a block goes along rows that are longer, or along a piece of one.  Of a teacher's pairs the narrow
+// kernel takes eight for each lane.
+inline GradPlan plan_grad(const mg_logits* z, int32_t entries, int n_sms) {
+    GradPlan p;
+    const int64_t vec = 16 / elem_size(z->dtype), covered = (z->classes + 2 * (vec - 1)) / vec;
+    p.lanes = 4;
+    while (p.lanes < kPlanGradThreads && covered > 8 * p.lanes) p.lanes *= 2;
+    if (entries) p.lanes = p.lanes <= 8 && entries <= 8 * kPlanTeacherRoom ? 8 : p.lanes <= 32 && entries <= 32 * kPlanTeacherRoom ? 32 : kPlanGradThreads;
+    if (p.lanes == kPlanGradThreads) {
+        // pieces of four batches, or as few as give every multiprocessor 32 blocks
+        const int64_t batch = (int64_t)kPlanGradThreads * kPlanGradBatch, most = std::max<int64_t>(1, covered / batch), want = (32ll * n_sms + z->rows - 1) / std::max<int64_t>(z->rows, 1);
+        p.chunks = (int)std::min({most, std::max(want, covered / (4 * batch)), ((int64_t)(1ll << 31) - 1) / std::max<int64_t>(z->rows, 1)});
+        p.chunks = std::max(p.chunks, 1);
+        p.blocks = z->rows * p.chunks;
+    } else {
+        const int64_t groups = kPlanGradThreads / p.lanes;
+        p.blocks = (z->rows + groups - 1) / groups;
+        if (entries) p.blocks = std::min<int64_t>(p.blocks, (int64_t)n_sms * 64);
+    }
+    return p;
 }
 
 }  // namespace

@@ -1,0 +1,26 @@
+// Launches of the log probabilities' kernels.
+#include "mg_loss_launch.cuh"
+#include "mg_loss_rows.cuh"
+#include "mg_loss_wide.cuh"
+
+namespace mgloss {
+
+template <typename T, int NV, int LANES>
+static void launch_rows(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t st) {
+    if (l.whole) k_scores_rows<T, NV, LANES, true><<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a);
+    else k_scores_rows<T, NV, LANES, false><<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a);
+}
+
+template <typename T, int THREADS>
+static void launch_wide(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t st) {
+    if (l.whole) launch_cluster(k_scores_wide<T, THREADS, false>, l, st, a, l.parts);
+    else launch_cluster(k_scores_wide<T, THREADS, true>, l, st, a, l.parts);
+}
+
+void launch_scores(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t st) {
+    if (!l.lanes) MG_LOSS_BY_TYPE(l.dtype, (l.threads == kWideThreads ? launch_wide<T, kWideThreads>(l, a, st) : launch_wide<T, kWideMostThreads>(l, a, st)));
+    else if (l.lanes == 8) MG_LOSS_BY_TYPE(l.dtype, MG_LOSS_BY_VECTORS(l.nv, (launch_rows<T, NV, 8>(l, a, st))));
+    else MG_LOSS_BY_TYPE(l.dtype, MG_LOSS_BY_VECTORS(l.nv, (launch_rows<T, NV, 32>(l, a, st))));
+}
+
+}  // namespace mgloss

@@ -7,8 +7,9 @@
 
 namespace mgloss {
 
-constexpr int kWideThreads = 256, kWideWarps = kWideThreads / 32, kWideVecs = 8;
-constexpr int kWideRoom = 1024, kWideTrim = 256;   // candidates for the best classes: room, and how many of them are cut down to the best again
+constexpr int kWideThreads = 256, kWideMostThreads = 1024, kWideVecs = 8;   // (four segments of 32 KB on their way to an SM)
+constexpr int kWideRoom = 1024, kWideTrim = 256;   // vectors that may hold one of the best classes: room, and how many of them are cut down to the best again ...
+constexpr int kWideLook = 8;                       // ... which is looked at behind every so many segments
 
 // packed values of one type: two halves to a word, or a float
 template <typename T> struct Word {
@@ -87,56 +88,121 @@ __device__ __forceinline__ RowSums joined(RowSums a, RowSums b, float scale2) {
     return r;
 }
 
-struct WideShared {
-    float max[kWideWarps], sum[kWideWarps], weighted[kWideWarps], least[kWideWarps];
-    float part[3];                 // of a block: what others of its cluster read
-    int n;                         // candidates so far; more than there is room for: the best are found one by one
-    uint64_t room[kWideRoom];
-    uint64_t best[MG_MAX_TOP];
-    uint64_t warp_best[kWideWarps];
+template <int THREADS> struct WideShared {
+    static constexpr int WARPS = THREADS / 32;
+    float max[WARPS], sum[WARPS], weighted[WARPS], scratch[WARPS];
+    float all[3];                  // of the block: what others of its cluster read
+    int n, n_best;                 // vectors, classes that may be among the best; more than there is room for: the best are found one by one
+    float first[32];               // the largest values of the first segment's threads, a few of each warp
+    uint64_t vecs[kWideRoom];      // a vector's largest value and its number
+    uint64_t room[kWideRoom];      // a class and its value
+    uint64_t best[MG_MAX_TOP], warp_best[WARPS];
 };
 
-// the `top` best of the block's candidates to sh->best, the best first (every thread; behind a barrier, and before one)
-__device__ __forceinline__ void rank_candidates(WideShared* sh, int n, int32_t top) {
-    for (int i = threadIdx.x; i < n; i += kWideThreads) {
-        const uint64_t key = sh->room[i];
+// the `top` best of the keys to `best`, the best first (every thread; behind a barrier, and before one)
+template <int THREADS>
+__device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int32_t top, uint64_t* best) {
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        const uint64_t key = keys[i];
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += sh->room[j] > key;
-        if (rank < top) sh->best[rank] = key;
+        for (int j = 0; j < n; ++j) rank += keys[j] > key;
+        if (rank < top) best[rank] = key;
     }
 }
 
-// A row's part `part` of `parts`: its classes are vectors [lo, hi) of the cut, the first part's the edges too.
-template <typename T, bool WEIGHTED, bool EDGES>
-__device__ RowSums go_along(const T* x, int32_t classes, float scale2, int part, int parts, int32_t top, WideShared* sh) {
-    constexpr int VEC = 16 / sizeof(T), WORDS = 4;
+// A value that no more than a few of the row's lie above, and `top` do not lie below: the top-th largest of the few largest that each warp's threads have found in their
+// first vectors.  (full: warps all of whose threads have one.)
+template <int THREADS>
+__device__ __forceinline__ float first_bound(float own, int full, int32_t top, WideShared<THREADS>* sh) {
+    if (full <= 0) return kNegInf;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, use = min(full, 32), each = min(32 / use, (top + use - 1) / use + 1);
+    if (each * use < top) return kNegInf;
+    if (warp < use) {
+        float left = own;
+        for (int k = 0; k < each; ++k) {
+            const float most = value_of(__reduce_max_sync(0xFFFFFFFFu, order_of(left)));
+            const uint32_t holders = __ballot_sync(0xFFFFFFFFu, left == most);
+            if (lane == __ffs(holders) - 1) left = kNegInf;
+            if (lane == 0) sh->first[warp * each + k] = most;
+        }
+    }
+    __syncthreads();
+    const float v = lane < each * use ? sh->first[lane] : kNegInf;
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < 32; ++j) {
+        const float o = __shfl_sync(0xFFFFFFFFu, v, j);
+        rank += o > v || (o == v && j < lane);
+    }
+    return __shfl_sync(0xFFFFFFFFu, v, __ffs(__ballot_sync(0xFFFFFFFFu, rank == top - 1)) - 1);
+}
+
+// A row's part `part` of `parts`: its classes are vectors [lo, hi) of the cut, the first part's the edges too.  `meanwhile` is called when the first loads are on their way.
+// On return thread 0 .. all have the part's sums, and sh->best the part's best classes (zero where it has fewer).
+template <typename T, int THREADS, bool WEIGHTED, bool EDGES, typename F>
+__device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float scale2, int part, int parts, int32_t top, WideShared<THREADS>* sh, F meanwhile) {
+    constexpr int VEC = 16 / sizeof(T), WORDS = 4, WARPS = THREADS / 32;
     const Cut<VEC> cut(x, sizeof(T), classes);
     const int32_t lo = (int32_t)((int64_t)cut.vecs * part / parts), hi = (int32_t)((int64_t)cut.vecs * (part + 1) / parts);
     // segments of about equal length, eight vectors to a thread at most
-    const int32_t segments = max(1, (hi - lo + kWideThreads * kWideVecs - 1) / (kWideThreads * kWideVecs)), each = max(1, (hi - lo + segments - 1) / segments);
+    const int32_t segments = max(1, (hi - lo + THREADS * kWideVecs - 1) / (THREADS * kWideVecs)), each = max(1, (hi - lo + segments - 1) / segments);
+    const bool has_edge = EDGES && part == 0 && (int)threadIdx.x < cut.edges;
     Running<WEIGHTED> run;
     float least = kNegInf;      // what lies below is not among the best
-    bool known = false;
     for (int32_t s = 0; s < segments; ++s) {
         const int32_t from = lo + s * each, to = min(from + each, hi);
         Raw<T, VEC> raw[kWideVecs];
 #pragma unroll
         for (int j = 0; j < kWideVecs; ++j) {
-            const int32_t v = from + j * kWideThreads + (int32_t)threadIdx.x;
+            const int32_t v = from + j * THREADS + (int32_t)threadIdx.x;
             if (v < to) raw[j].load(x + cut.head + v * VEC);
             else
 #pragma unroll
                 for (int w = 0; w < WORDS; ++w) raw[j].w[w] = Word<T>::least();
         }
         float edge = kNegInf;
-        const bool has_edge = EDGES && s == 0 && part == 0 && (int)threadIdx.x < cut.edges;
-        if (has_edge) edge = to_float(x[cut.edge(threadIdx.x)]);
-        uint32_t most = Word<T>::least();
+        if (s == 0) {
+            if (has_edge) edge = to_float(x[cut.edge(threadIdx.x)]);
+            meanwhile();
+        }
+        uint32_t most[kWideVecs], all = Word<T>::least();
 #pragma unroll
-        for (int j = 0; j < kWideVecs; ++j)
+        for (int j = 0; j < kWideVecs; ++j) {
+            most[j] = Word<T>::max(Word<T>::max(raw[j].w[0], raw[j].w[1]), Word<T>::max(raw[j].w[2], raw[j].w[3]));
+            all = Word<T>::max(all, most[j]);
+        }
+        const float own = fmaxf(Word<T>::largest(all), edge);
+        if (top) {
+            if (s == 0) {
+                if (threadIdx.x == 0) { sh->n = 0; sh->n_best = 0; }
+                least = first_bound<THREADS>(own, min((to - from) / 32, WARPS), top, sh);
+                __syncthreads();
+            }
+            if (own >= least) {
 #pragma unroll
-            for (int w = 0; w < WORDS; ++w) most = Word<T>::max(most, raw[j].w[w]);
-        const float own = fmaxf(Word<T>::largest(most), edge);
+                for (int j = 0; j < kWideVecs; ++j) {
+                    const int32_t v = from + j * THREADS + (int32_t)threadIdx.x;
+                    const float m = Word<T>::largest(most[j]);
+                    if (m >= least && v < to) {
+                        const int at = atomicAdd(&sh->n, 1);
+                        if (at < kWideRoom) sh->vecs[at] = key_of(m, v);
+                    }
+                }
+            }
+            if (s % kWideLook == kWideLook - 1 && s + 1 < segments) {
+                // (a vector that holds one of the best is among the `top` whose largest values are)
+                __syncthreads();
+                const int n = sh->n;
+                if (n > kWideTrim && n <= kWideRoom) {
+                    rank_keys<THREADS>(sh->vecs, n, top, sh->best);
+                    __syncthreads();
+                    if ((int)threadIdx.x < top) sh->vecs[threadIdx.x] = sh->best[threadIdx.x];
+                    if (threadIdx.x == 0) sh->n = top;
+                    least = fmaxf(least, value_of((uint32_t)(sh->best[top - 1] >> 32)));
+                }
+                __syncthreads();
+            }
+        }
         run.raise(own, scale2);
 #pragma unroll
         for (int j = 0; j < kWideVecs; ++j)
@@ -147,82 +213,68 @@ __device__ RowSums go_along(const T* x, int32_t classes, float scale2, int part,
                 else Word<T>::floats(raw[j].w[w], &a, &b);
                 run.add(a, b, scale2);
             }
-        if (EDGES) run.add(edge, kNegInf, scale2);
-        if (top) {
-            if (!known) {
-                // The warps' ceil(top / warps)-th largest of their threads' largest: the least of these is no larger than the row's top-th largest value.
-                // (Warps all of whose threads have a vector; none, and all values are candidates.)
-                const int full = min((to - from) / 32, kWideWarps), each_warp = (top + full - 1) / max(full, 1);
-                float left = own, of_warp = kNegInf;
-                for (int k = 0; k < each_warp; ++k) {
-                    of_warp = value_of(__reduce_max_sync(0xFFFFFFFFu, order_of(left)));
-                    const uint32_t holders = __ballot_sync(0xFFFFFFFFu, left == of_warp);
-                    if ((int)(threadIdx.x & 31) == __ffs(holders) - 1) left = kNegInf;
-                }
-                if ((threadIdx.x & 31) == 0) sh->least[threadIdx.x / 32] = of_warp;
-                if (threadIdx.x == 0) sh->n = 0;
-                __syncthreads();
-                least = full ? sh->least[0] : kNegInf;
-#pragma unroll
-                for (int w = 1; w < kWideWarps; ++w)
-                    if (w < full) least = fminf(least, sh->least[w]);
-                known = true;
-            }
-            if (own >= least) {
-#pragma unroll
-                for (int j = 0; j < kWideVecs; ++j)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const float v = raw[j].get(e);
-                        const int32_t at = from + j * kWideThreads + (int32_t)threadIdx.x;
-                        if (v >= least && at < to) {
-                            const int i = atomicAdd(&sh->n, 1);
-                            if (i < kWideRoom) sh->room[i] = key_of(v, cut.head + at * VEC + e);
-                        }
-                    }
-                if (has_edge && edge >= least) {
-                    const int i = atomicAdd(&sh->n, 1);
-                    if (i < kWideRoom) sh->room[i] = key_of(edge, cut.edge(threadIdx.x));
-                }
-            }
-            if (s + 1 < segments) {
-                __syncthreads();
-                const int n = sh->n;
-                if (n > kWideTrim && n <= kWideRoom) {
-                    rank_candidates(sh, n, top);
-                    __syncthreads();
-                    if ((int)threadIdx.x < top) sh->room[threadIdx.x] = sh->best[threadIdx.x];
-                    if (threadIdx.x == 0) sh->n = top;
-                    least = value_of((uint32_t)(sh->best[top - 1] >> 32));
-                }
-                __syncthreads();
-            }
-        }
+        if (EDGES && s == 0) run.add(edge, kNegInf, scale2);
     }
     // over the block, in an order that does not change
     RowSums r = run.both();
+#pragma unroll
     for (int o = 16; o; o >>= 1) {
         const RowSums other{__shfl_xor_sync(0xFFFFFFFFu, r.max, o), __shfl_xor_sync(0xFFFFFFFFu, r.sum, o), WEIGHTED ? __shfl_xor_sync(0xFFFFFFFFu, r.weighted, o) : 0.f};
         r = joined<WEIGHTED>(r, other, scale2);
     }
-    if ((threadIdx.x & 31) == 0) { sh->max[threadIdx.x / 32] = r.max; sh->sum[threadIdx.x / 32] = r.sum; sh->weighted[threadIdx.x / 32] = r.weighted; }
+    if ((threadIdx.x & 31) == 0) { sh->max[threadIdx.x / 32] = r.max; sh->sum[threadIdx.x / 32] = r.sum; if (WEIGHTED) sh->weighted[threadIdx.x / 32] = r.weighted; }
     __syncthreads();
-    r = {sh->max[0], sh->sum[0], sh->weighted[0]};
+    if (threadIdx.x < 32) {
+        const int w = threadIdx.x;
+        r = {kNegInf, 0.f, 0.f};
+        if (w < WARPS) r = {sh->max[w], sh->sum[w], WEIGHTED ? sh->weighted[w] : 0.f};
 #pragma unroll
-    for (int w = 1; w < kWideWarps; ++w) r = joined<WEIGHTED>(r, {sh->max[w], sh->sum[w], sh->weighted[w]}, scale2);
+        for (int o = WARPS / 2; o; o >>= 1) {
+            const RowSums other{__shfl_xor_sync(0xFFFFFFFFu, r.max, o), __shfl_xor_sync(0xFFFFFFFFu, r.sum, o), WEIGHTED ? __shfl_xor_sync(0xFFFFFFFFu, r.weighted, o) : 0.f};
+            r = joined<WEIGHTED>(r, other, scale2);
+        }
+        if (w == 0) { sh->all[0] = r.max; sh->all[1] = r.sum; sh->all[2] = r.weighted; }
+    }
+    if (top) {
+        // the classes of the vectors that are left
+        const int n = sh->n;
+        if (n <= kWideRoom) {
+            for (int i = threadIdx.x; i < n; i += THREADS) {
+                const int32_t c = cut.head + class_of(sh->vecs[i]) * VEC;
+                Raw<T, VEC> raw;
+                raw.load(x + c);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e)
+                    if (raw.get(e) >= least) {
+                        const int at = atomicAdd(&sh->n_best, 1);
+                        if (at < kWideRoom) sh->room[at] = key_of(raw.get(e), c + e);
+                    }
+            }
+            if (has_edge) {
+                const int32_t c = cut.edge(threadIdx.x);
+                const float v = to_float(x[c]);
+                if (v >= least) {
+                    const int at = atomicAdd(&sh->n_best, 1);
+                    if (at < kWideRoom) sh->room[at] = key_of(v, c);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    r = {sh->all[0], sh->all[1], sh->all[2]};
     return r;
 }
 
 // The best of the part one by one, each a pass over it: where candidates overflow (more equal values than there is room for, values that rise along the row, NaN).
-template <typename T>
-__device__ __noinline__ void best_one_by_one(const T* x, int32_t classes, int part, int parts, int32_t top, WideShared* sh) {
-    constexpr int VEC = 16 / sizeof(T);
+template <typename T, int THREADS>
+__device__ __noinline__ void best_one_by_one(const T* x, int32_t classes, int part, int parts, int32_t top, WideShared<THREADS>* sh) {
+    constexpr int VEC = 16 / sizeof(T), WARPS = THREADS / 32;
     const Cut<VEC> cut(x, sizeof(T), classes);
     const int32_t lo = (int32_t)((int64_t)cut.vecs * part / parts), hi = (int32_t)((int64_t)cut.vecs * (part + 1) / parts);
     uint64_t last = ~0ull;
     for (int k = 0; k < top; ++k) {
         uint64_t best = 0;
-        for (int32_t c = cut.head + lo * VEC + (int32_t)threadIdx.x; c < cut.head + hi * VEC; c += kWideThreads) {
+        for (int32_t c = cut.head + lo * VEC + (int32_t)threadIdx.x; c < cut.head + hi * VEC; c += THREADS) {
             const uint64_t key = key_of(to_float(x[c]), c);
             if (key < last && key > best) best = key;
         }
@@ -231,148 +283,173 @@ __device__ __noinline__ void best_one_by_one(const T* x, int32_t classes, int pa
             const uint64_t key = key_of(to_float(x[c]), c);
             if (key < last && key > best) best = key;
         }
-        best = lanes_max(best, 32);
+        best = lanes_max<32>(best);
         __syncthreads();
         if ((threadIdx.x & 31) == 0) sh->warp_best[threadIdx.x / 32] = best;
         __syncthreads();
         last = sh->warp_best[0];
-        for (int w = 1; w < kWideWarps; ++w) last = max(last, sh->warp_best[w]);
+        for (int w = 1; w < WARPS; ++w) last = max(last, sh->warp_best[w]);
         if (threadIdx.x == 0) sh->best[k] = last;   // (zero where the part has fewer classes)
         if (last == 0) last = 1;
     }
-    __syncthreads();
 }
 
 // the parts' sums, in rank 0's hands
-template <bool WEIGHTED>
-__device__ __forceinline__ RowSums over_cluster(RowSums r, int parts, float scale2, WideShared* sh) {
+template <bool WEIGHTED, int THREADS>
+__device__ __forceinline__ RowSums over_cluster(RowSums r, int parts, float scale2, WideShared<THREADS>* sh) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
-    if (threadIdx.x == 0) { sh->part[0] = r.max; sh->part[1] = r.sum; sh->part[2] = r.weighted; }
     cluster.sync();
     if (cluster.block_rank() == 0)
         for (int p = 1; p < parts; ++p) {
-            const float* from = cluster.map_shared_rank(sh->part, p);
+            const float* from = cluster.map_shared_rank(sh->all, p);
             r = joined<WEIGHTED>(r, {from[0], from[1], from[2]}, scale2);
         }
     return r;
 }
 
-template <typename T, bool EDGES>
-__global__ void __launch_bounds__(kWideThreads, 4) k_scores_wide(const __grid_constant__ ScoreArgs a, int parts) {
+template <typename T, int THREADS, bool EDGES>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_wide(const __grid_constant__ ScoreArgs a, int parts) {
     namespace cg = cooperative_groups;
-    __shared__ WideShared sh;
-    const int64_t r = blockIdx.x / parts;
-    const int part = (int)(blockIdx.x - (unsigned)(r * parts));
+    __shared__ WideShared<THREADS> sh;
+    const int64_t r = blockIdx.x / (unsigned)parts;
+    const int part = (int)(blockIdx.x - (unsigned)r * (unsigned)parts);
     const T* x = static_cast<const T*>(a.x) + r * a.stride;
-    const int32_t label = threadIdx.x == 0 && part == 0 && a.log_prob ? class_at(a.labels, a.labels_are_i64, r, a.classes) : -1;
-    const float at_label = label >= 0 ? to_float(x[label]) : 0.f;
-    RowSums s = go_along<T, true, EDGES>(x, a.classes, a.scale2, part, parts, a.top, &sh);
+    int32_t label = -1;
+    float at_label = 0.f;
+    RowSums s = go_along<T, THREADS, true, EDGES>(x, a.classes, a.scale2, part, parts, a.top, &sh, [&] {
+        if (threadIdx.x == 0 && part == 0 && a.log_prob) {
+            label = class_at(a.labels, a.labels_are_i64, r, a.classes);
+            if (label >= 0) at_label = to_float(x[label]);
+        }
+    });
     if (a.top) {
-        // (behind go_along's last barrier)
-        const int n = sh.n;
-        if (n > kWideRoom || n < a.top || !(s.sum < __builtin_huge_valf()) || !(s.max > kNegInf)) best_one_by_one(x, a.classes, part, parts, a.top, &sh);
-        else rank_candidates(&sh, n, a.top);
+        const int n = sh.n_best;
+        if (sh.n > kWideRoom || n > kWideRoom || n < a.top || !(s.sum < __builtin_huge_valf()) || !(s.max > kNegInf)) best_one_by_one<T, THREADS>(x, a.classes, part, parts, a.top, &sh);
+        else rank_keys<THREADS>(sh.room, n, a.top, sh.best);
         __syncthreads();
     }
     if (parts > 1) s = over_cluster<true>(s, parts, a.scale2, &sh);
     if (part == 0) {
-        const RowResult res(s, a.scale);
-        if (threadIdx.x == 0) {
-            if (a.lse) a.lse[r] = res.lse;
-            if (a.entropy) a.entropy[r] = res.entropy;
-            if (a.log_prob) a.log_prob[r] = label >= 0 ? res.log_p(at_label) : 0.f;
-        }
         if (a.top && parts > 1) {
             cg::cluster_group cluster = cg::this_cluster();
             const int n = parts * a.top;      // (MG_MAX_TOP from each of 16 blocks: there is room)
-            for (int i = threadIdx.x; i < n; i += kWideThreads) sh.room[i] = cluster.map_shared_rank(sh.best, i / a.top)[i % a.top];
+            for (int i = threadIdx.x; i < n; i += THREADS) sh.room[i] = cluster.map_shared_rank(sh.best, i / a.top)[i % a.top];
             __syncthreads();
-            rank_candidates(&sh, n, a.top);
+            rank_keys<THREADS>(sh.room, n, a.top, sh.best);
             __syncthreads();
         }
-        if ((int)threadIdx.x < a.top) {
-            const uint64_t key = sh.best[threadIdx.x];
-            if (a.top_ids) a.top_ids[r * a.top + threadIdx.x] = class_of(key);
-            if (a.top_log_probs) a.top_log_probs[r * a.top + threadIdx.x] = res.log_p(value_of((uint32_t)(key >> 32)));
+        if (threadIdx.x < 32) {
+            const RowResult res(s, a.scale);
+            if (threadIdx.x == 0) {
+                if (a.lse) a.lse[r] = res.lse;
+                if (a.entropy) a.entropy[r] = res.entropy;
+                if (a.log_prob) a.log_prob[r] = label >= 0 ? res.log_p(at_label) : 0.f;
+            }
+            if ((int)threadIdx.x < a.top) {
+                const uint64_t key = sh.best[threadIdx.x];
+                if (a.top_ids) a.top_ids[r * a.top + threadIdx.x] = class_of(key);
+                if (a.top_log_probs) a.top_log_probs[r * a.top + threadIdx.x] = res.log_p(value_of((uint32_t)(key >> 32)));
+            }
         }
     }
     if (parts > 1) cg::this_cluster().sync();   // (nobody leaves while its memory is read)
 }
 
-__device__ __forceinline__ float block_sum(float v, float* warps) {
-    v = lanes_sum(v, 32);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) warps[threadIdx.x / 32] = v;
-    __syncthreads();
-    v = warps[0];
-    for (int w = 1; w < kWideWarps; ++w) v += warps[w];
-    return v;
+// A row's pairs of a teacher's, four or fewer to each of 256 threads: class, scaled value.
+constexpr int kTeacherEach = MG_MAX_TEACHER / 256;
+
+// Sum and largest of a value over the first `warps` warps of a block, in their hands; barrier 1 is theirs.
+__device__ __forceinline__ void some_warps_meet(int warps) {
+    if (warps > 1) asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
+    else __syncwarp();
 }
-__device__ __forceinline__ float block_max(float v, float* warps) {
-    v = lanes_max(v, 32);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) warps[threadIdx.x / 32] = v;
-    __syncthreads();
-    v = warps[0];
-    for (int w = 1; w < kWideWarps; ++w) v = fmaxf(v, warps[w]);
+template <typename F>
+__device__ __forceinline__ float over_warps(float v, int warps, float* scratch, F f) {
+    v = over_lanes<32>(v, f);
+    if (warps == 1) return v;
+    some_warps_meet(warps);
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x / 32] = v;
+    some_warps_meet(warps);
+    v = scratch[0];
+    for (int w = 1; w < warps; ++w) v = f(v, scratch[w]);
     return v;
 }
 
-// A block's view of a teacher's row: four entries to a thread at most (class -1: none).
-constexpr int kTeacherEach = MG_MAX_TEACHER / kWideThreads;
+// The teacher's probabilities of a row's pairs: the warps that have a pair each work them out; `c`, `q` and `log_q` [entries] get classes (-1: none), probabilities, logarithms.
+// (256 threads at most.)  Returns their sum.
 struct TeacherRow {
     int32_t c[kTeacherEach];
-    float q[kTeacherEach], log_q[kTeacherEach];
-    __device__ __forceinline__ void load(const TeacherArgs& t, int64_t r, int32_t classes, float scale, float* warps) {
-        float m = kNegInf;
+    float v[kTeacherEach];
+    __device__ __forceinline__ void load(const TeacherArgs& t, int64_t r, int32_t classes, float scale) {
 #pragma unroll
         for (int i = 0; i < kTeacherEach; ++i) {
-            const int k = threadIdx.x + i * kWideThreads;
-            c[i] = k < t.entries ? class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, classes) : -1;
-            log_q[i] = c[i] >= 0 ? scale * float_at(t.values, t.dtype, r * t.values_stride + k) : kNegInf;
-            m = fmaxf(m, log_q[i]);
+            const int k = threadIdx.x + i * 256;
+            c[i] = -1; v[i] = kNegInf;
+            if (k < t.entries) {
+                c[i] = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, classes);
+                if (c[i] >= 0) v[i] = scale * float_at(t.values, t.dtype, r * t.values_stride + k);
+            }
         }
-        float sum = 1.f, shift;
+    }
+    // q in the place of v; log q = v - log_shift
+    __device__ __forceinline__ float probabilities(const TeacherArgs& t, int64_t r, int warps, float* scratch, float* log_shift) {
+        float shift, sum = 1.f;
         if (t.lse) shift = t.lse[r];
         else {
-            m = block_max(m, warps);
-            shift = m == kNegInf ? 0.f : m;
+            float m = kNegInf;
+#pragma unroll
+            for (int i = 0; i < kTeacherEach; ++i) m = fmaxf(m, v[i]);
+            m = over_warps(m, warps, scratch, [](float a, float b) { return fmaxf(a, b); });
+            shift = centre(m);
             sum = 0.f;
 #pragma unroll
             for (int i = 0; i < kTeacherEach; ++i)
-                if (c[i] >= 0) sum += fast_exp2((log_q[i] - shift) * kLog2e);
-            sum = block_sum(sum, warps);
+                if (c[i] >= 0) sum += fast_exp2((v[i] - shift) * kLog2e);
+            sum = over_warps(sum, warps, scratch, [](float a, float b) { return a + b; });
         }
-        const float log_sum = logf(sum), part = sum == 0.f ? 0.f : 1.f / sum;
+        const float part = sum == 0.f ? 0.f : 1.f / sum;
+        *log_shift = shift + (sum == 0.f ? 0.f : logf(sum));
+        float mass = 0.f;
 #pragma unroll
         for (int i = 0; i < kTeacherEach; ++i) {
-            const float d = log_q[i] - shift;
-            q[i] = c[i] >= 0 ? fast_exp2(d * kLog2e) * part : 0.f;
-            log_q[i] = d - log_sum;
+            v[i] = c[i] >= 0 ? fast_exp2((v[i] - shift) * kLog2e) * part : 0.f;
+            mass += v[i];
         }
+        return over_warps(mass, warps, scratch, [](float a, float b) { return a + b; });
     }
 };
 
-template <typename T, bool EDGES>
-__global__ void __launch_bounds__(kWideThreads, 4) k_distill_wide(const __grid_constant__ ScoreArgs a, const __grid_constant__ TeacherArgs t, float* loss, int parts) {
-    __shared__ WideShared sh;
+template <typename T, int THREADS, bool EDGES>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_wide(const __grid_constant__ ScoreArgs a, const __grid_constant__ TeacherArgs t, float* loss, int parts) {
     namespace cg = cooperative_groups;
-    const int64_t r = blockIdx.x / parts;
-    const int part = (int)(blockIdx.x - (unsigned)(r * parts));
+    __shared__ WideShared<THREADS> sh;
+    __shared__ float at_class[MG_MAX_TEACHER];   // the student's logits, fetched while the first segment is on its way
+    const int64_t r = blockIdx.x / (unsigned)parts;
+    const int part = (int)(blockIdx.x - (unsigned)r * (unsigned)parts);
     const T* x = static_cast<const T*>(a.x) + r * a.stride;
-    RowSums s = go_along<T, false, EDGES>(x, a.classes, a.scale2, part, parts, 0, &sh);
+    const int warps = min(256 / 32, (t.entries + 31) / 32);
+    const bool teaches = part == 0 && (int)threadIdx.x < warps * 32;
+    RowSums s = go_along<T, THREADS, false, EDGES>(x, a.classes, a.scale2, part, parts, 0, &sh, [&] {
+        if (teaches)
+            for (int k = threadIdx.x; k < t.entries; k += 256) {
+                const int32_t c = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, a.classes);
+                at_class[k] = c >= 0 ? to_float(x[c]) : 0.f;
+            }
+    });
     if (parts > 1) s = over_cluster<false>(s, parts, a.scale2, &sh);
-    if (part == 0) {
+    if (teaches) {
         const RowResult res(s, a.scale);
         TeacherRow row;
-        __syncthreads();
-        row.load(t, r, a.classes, a.scale, sh.max);
-        float v = 0.f;
+        row.load(t, r, a.classes, a.scale);
+        float raw[kTeacherEach], log_shift, v = 0.f;
+#pragma unroll
+        for (int i = 0; i < kTeacherEach; ++i) raw[i] = row.v[i];
+        row.probabilities(t, r, warps, sh.scratch, &log_shift);
 #pragma unroll
         for (int i = 0; i < kTeacherEach; ++i)
-            if (row.q[i] != 0.f) v = fmaf(row.q[i], row.log_q[i] - res.log_p(to_float(x[row.c[i]])), v);
-        v = block_sum(v, sh.max);
+            if (row.v[i] != 0.f) v = fmaf(row.v[i], (raw[i] - log_shift) - res.log_p(at_class[threadIdx.x + i * 256]), v);
+        v = over_warps(v, warps, sh.scratch, [](float a, float b) { return a + b; });
         if (threadIdx.x == 0) {
             loss[r] = v;
             if (a.lse) a.lse[r] = res.lse;
