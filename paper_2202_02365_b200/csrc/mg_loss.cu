@@ -24,9 +24,10 @@ int run_forward(mg_ctx* ctx, const mg_logits* z, const ScoreArgs& a, const mg_te
 int run_backward(mg_ctx* ctx, const mg_logits* z, const GradArgs& a, bool distill, cudaStream_t st) {
     DeviceScope on(ctx->device);
     MG_CUDA(ctx, on.err);
-    const GradPlan p = plan_grad(z, distill ? a.teacher.entries : 0, ctx->n_sms);
+    GradPlan p = plan_grad(z, distill ? a.teacher.entries : 0, ctx->n_sms);
+    if (!distill && (p.flat_rows = flat_rows(z, a.d, a.d_stride, ctx->n_sms))) p.blocks = (z->rows + p.flat_rows - 1) / p.flat_rows;
     const bool same = same_phase(z->x, z->stride, a.d, a.d_stride, z->rows, z->dtype);
-    const GradLaunch l{z->dtype, same, same && whole_vectors(z->x, z->stride, z->rows, z->classes, z->dtype) && whole_vectors(a.d, a.d_stride, z->rows, z->classes, z->dtype), p.lanes, p.chunks, p.blocks};
+    const GradLaunch l{z->dtype, same, same && whole_vectors(z->x, z->stride, z->rows, z->classes, z->dtype) && whole_vectors(a.d, a.d_stride, z->rows, z->classes, z->dtype), p.lanes, p.chunks, p.blocks, p.flat_rows};
     if (distill) launch_distill_grad(l, a, st);
     else launch_scores_grad(l, a, st);
     ctx->launches++;

@@ -5,6 +5,12 @@
 namespace mgloss {
 
 void launch_scores_grad(const GradLaunch& l, const GradArgs& a, cudaStream_t st) {
+    if (l.flat_rows) {
+        const uint32_t reciprocal = (uint32_t)((1ull << 32) / (uint64_t)a.classes + 1);   // (values to a block times classes are below 2^32)
+        const auto flat = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kGradThreads, 0, st>>>(a, l.flat_rows, reciprocal); };
+        MG_LOSS_BY_TYPE(l.dtype, (l.whole ? flat(k_scores_grad_flat<T, false>) : flat(k_scores_grad_flat<T, true>)));
+        return;
+    }
     const auto go = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kGradThreads, 0, st>>>(a, l.lanes, l.chunks); };
     MG_LOSS_BY_TYPE(l.dtype, (l.whole ? go(k_scores_grad<T, true, true>) : l.same ? go(k_scores_grad<T, true, false>) : go(k_scores_grad<T, false, false>)));
 }

@@ -21,6 +21,7 @@ struct GradLaunch {
     bool same, whole;      // logits' and gradient's vectors begin alike; rows begin and end with one
     int lanes, chunks;     // threads to a row (256: a block), pieces of it
     int64_t blocks;
+    int flat_rows;         // rows to a block that takes them as one run, 0: not so
 };
 void launch_scores_grad(const GradLaunch& l, const GradArgs& a, cudaStream_t st);
 void launch_distill_grad(const GradLaunch& l, const GradArgs& a, cudaStream_t st);

@@ -121,7 +121,17 @@ inline ForwardPlan plan_forward(const mg_logits* z, int32_t top, int n_sms) {
 
 constexpr int kPlanGradThreads = 256, kPlanGradBatch = 4, kPlanTeacherRoom = 8;
 
-struct GradPlan { int lanes = 0, chunks = 1; int64_t blocks = 0; };
+struct GradPlan { int lanes = 0, chunks = 1; int64_t blocks = 0; int flat_rows = 0; };
+
+// Rows that lie one behind the other from a vector's beginning on, in both matrices: a block takes as many as have 2,048 vectors (8 at least, a multiple of 8, so that every block begins
+// with one; 256 at most), fewer where two blocks to a multiprocessor would not come about.  Rows of up to 2,048 values of two bytes: beyond, they are taken one by one.
+inline int flat_rows(const mg_logits* z, const void* d, int64_t d_stride, int n_sms) {
+    const int64_t vec = 16 / elem_size(z->dtype);
+    if (z->classes < vec || z->classes > 256 * vec || (z->rows > 1 && (z->stride != z->classes || d_stride != z->classes))) return 0;
+    if (reinterpret_cast<uintptr_t>(z->x) % 16 || reinterpret_cast<uintptr_t>(d) % 16) return 0;
+    const int64_t full = 2048 * vec / z->classes / 8 * 8, few = (z->rows + 2 * n_sms - 1) / (2 * n_sms);
+    return (int)std::max<int64_t>(8, std::min<int64_t>({full, (few + 7) / 8 * 8, 256}));
+}
 
 // Gradients: threads to a row, so that each has up to eight vectors; a block goes along rows that are longer, or along a piece of one.  Of a teacher's pairs the narrow
 // kernel takes eight for each lane.

@@ -45,7 +45,7 @@ template <typename T> struct Word {
 // One thread's part of a row's sums, as it goes along: whenever its largest value grows, what it has is scaled down.
 template <bool WEIGHTED> struct Running {
     float max = kNegInf;
-    Pair sum = {0}, weighted = {0};
+    Pair sum = {0}, weighted = {0}, minus_max = {0};
     __device__ __forceinline__ void raise(float m, float scale2) {
         if (!(m > max)) return;
         if (max != kNegInf) {
@@ -56,10 +56,10 @@ template <bool WEIGHTED> struct Running {
             sum = mul2(ff, sum);
         }
         max = m;
+        minus_max = pair(-m, -m);
     }
-    __device__ __forceinline__ void add(float a, float b, float scale2) {
-        const float m = -centre(max);
-        const Pair y = mul2(add2(pair(a, b), pair(m, m)), pair(scale2, scale2));
+    __device__ __forceinline__ void add(float a, float b, Pair scale2) {
+        const Pair y = mul2(add2(pair(a, b), minus_max), scale2);
         float y0, y1;
         split(y, &y0, &y1);
         const Pair e = pair(fast_exp2(y0), fast_exp2(y1));
@@ -141,36 +141,37 @@ __device__ __forceinline__ float first_bound(float own, int full, int32_t top, W
 // On return thread 0 .. all have the part's sums, and sh->best the part's best classes (zero where it has fewer).
 template <typename T, int THREADS, bool WEIGHTED, bool EDGES, typename F>
 __device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float scale2, int part, int parts, int32_t top, WideShared<THREADS>* sh, F meanwhile) {
-    constexpr int VEC = 16 / sizeof(T), WORDS = 4, WARPS = THREADS / 32;
+    constexpr int VEC = 16 / sizeof(T), WARPS = THREADS / 32;
     const Cut<VEC> cut(x, sizeof(T), classes);
     const int32_t lo = (int32_t)((int64_t)cut.vecs * part / parts), hi = (int32_t)((int64_t)cut.vecs * (part + 1) / parts);
-    // segments of about equal length, eight vectors to a thread at most
-    const int32_t segments = max(1, (hi - lo + THREADS * kWideVecs - 1) / (THREADS * kWideVecs)), each = max(1, (hi - lo + segments - 1) / segments);
+    // segments of about as many rounds of a vector to each thread, eight at most: the last round of all alone is not a whole one
+    const int32_t rounds = max(1, (hi - lo + THREADS - 1) / THREADS), segments = (rounds + kWideVecs - 1) / kWideVecs, each = (rounds + segments - 1) / segments;
     const bool has_edge = EDGES && part == 0 && (int)threadIdx.x < cut.edges;
+    const Pair scales = pair(scale2, scale2);
     Running<WEIGHTED> run;
     float least = kNegInf;      // what lies below is not among the best
     for (int32_t s = 0; s < segments; ++s) {
-        const int32_t from = lo + s * each, to = min(from + each, hi);
-        Raw<T, VEC> raw[kWideVecs];
+        const int32_t from = lo + s * each * THREADS, to = min(from + each * THREADS, hi), full = (to - from) / THREADS, some = (to - from + THREADS - 1) / THREADS;
+        const uint4* at = reinterpret_cast<const uint4*>(x + cut.head) + from + threadIdx.x;
+        uint4 raw[kWideVecs];
 #pragma unroll
         for (int j = 0; j < kWideVecs; ++j) {
-            const int32_t v = from + j * THREADS + (int32_t)threadIdx.x;
-            if (v < to) raw[j].load(x + cut.head + v * VEC);
-            else
-#pragma unroll
-                for (int w = 0; w < WORDS; ++w) raw[j].w[w] = Word<T>::least();
+            if (j < full) raw[j] = __ldg(at + j * THREADS);
+            else if (j < some) {
+                raw[j] = make_uint4(Word<T>::least(), Word<T>::least(), Word<T>::least(), Word<T>::least());
+                if (from + j * THREADS + (int32_t)threadIdx.x < to) raw[j] = __ldg(at + j * THREADS);
+            }
         }
         float edge = kNegInf;
         if (s == 0) {
             if (has_edge) edge = to_float(x[cut.edge(threadIdx.x)]);
             meanwhile();
         }
-        uint32_t most[kWideVecs], all = Word<T>::least();
+        const auto largest_of = [](const uint4& w) { return Word<T>::max(Word<T>::max(w.x, w.y), Word<T>::max(w.z, w.w)); };
+        uint32_t all = Word<T>::least();
 #pragma unroll
-        for (int j = 0; j < kWideVecs; ++j) {
-            most[j] = Word<T>::max(Word<T>::max(raw[j].w[0], raw[j].w[1]), Word<T>::max(raw[j].w[2], raw[j].w[3]));
-            all = Word<T>::max(all, most[j]);
-        }
+        for (int j = 0; j < kWideVecs; ++j)
+            if (j < some) all = Word<T>::max(all, largest_of(raw[j]));
         const float own = fmaxf(Word<T>::largest(all), edge);
         if (top) {
             if (s == 0) {
@@ -180,14 +181,15 @@ __device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float s
             }
             if (own >= least) {
 #pragma unroll
-                for (int j = 0; j < kWideVecs; ++j) {
-                    const int32_t v = from + j * THREADS + (int32_t)threadIdx.x;
-                    const float m = Word<T>::largest(most[j]);
-                    if (m >= least && v < to) {
-                        const int at = atomicAdd(&sh->n, 1);
-                        if (at < kWideRoom) sh->vecs[at] = key_of(m, v);
+                for (int j = 0; j < kWideVecs; ++j)
+                    if (j < some) {
+                        const int32_t v = from + j * THREADS + (int32_t)threadIdx.x;
+                        const float m = Word<T>::largest(largest_of(raw[j]));
+                        if (m >= least && v < to) {
+                            const int i = atomicAdd(&sh->n, 1);
+                            if (i < kWideRoom) sh->vecs[i] = key_of(m, v);
+                        }
                     }
-                }
             }
             if (s % kWideLook == kWideLook - 1 && s + 1 < segments) {
                 // (a vector that holds one of the best is among the `top` whose largest values are)
@@ -206,14 +208,17 @@ __device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float s
         run.raise(own, scale2);
 #pragma unroll
         for (int j = 0; j < kWideVecs; ++j)
+            if (j < some) {
+                const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
 #pragma unroll
-            for (int w = 0; w < WORDS; w += 3 - Word<T>::N) {
-                float a, b;
-                if constexpr (sizeof(T) == 4) { a = __uint_as_float(raw[j].w[w]); b = __uint_as_float(raw[j].w[w + 1]); }
-                else Word<T>::floats(raw[j].w[w], &a, &b);
-                run.add(a, b, scale2);
+                for (int k = 0; k < 4; k += 3 - Word<T>::N) {
+                    float a, b;
+                    if constexpr (sizeof(T) == 4) { a = __uint_as_float(w[k]); b = __uint_as_float(w[k + 1]); }
+                    else Word<T>::floats(w[k], &a, &b);
+                    run.add(a, b, scales);
+                }
             }
-        if (EDGES && s == 0) run.add(edge, kNegInf, scale2);
+        if (EDGES && s == 0) run.add(edge, kNegInf, scales);
     }
     // over the block, in an order that does not change
     RowSums r = run.both();
