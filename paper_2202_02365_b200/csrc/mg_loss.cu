@@ -13,7 +13,7 @@ int run_forward(mg_ctx* ctx, const mg_logits* z, const ScoreArgs& a, const mg_te
     DeviceScope on(ctx->device);
     MG_CUDA(ctx, on.err);
     const ForwardPlan p = plan_forward(z, a.top, ctx->n_sms);
-    const ForwardLaunch l{z->dtype, whole_vectors(z->x, z->stride, z->rows, z->classes, z->dtype), p.nv, p.lanes, p.parts, p.threads, p.blocks};
+    const ForwardLaunch l{z->dtype, whole_vectors(z->x, z->stride, z->rows, z->classes, z->dtype), p.nv, p.lanes, p.parts_log2, p.threads, p.blocks};
     if (teacher) launch_distill(l, a, teacher_args(teacher), loss, st);
     else launch_scores(l, a, st);
     ctx->launches++;
@@ -27,7 +27,7 @@ int run_backward(mg_ctx* ctx, const mg_logits* z, const GradArgs& a, bool distil
     GradPlan p = plan_grad(z, distill ? a.teacher.entries : 0, ctx->n_sms);
     if (!distill && (p.flat_rows = flat_rows(z, a.d, a.d_stride, ctx->n_sms))) p.blocks = (z->rows + p.flat_rows - 1) / p.flat_rows;
     const bool same = same_phase(z->x, z->stride, a.d, a.d_stride, z->rows, z->dtype);
-    const GradLaunch l{z->dtype, same, same && whole_vectors(z->x, z->stride, z->rows, z->classes, z->dtype) && whole_vectors(a.d, a.d_stride, z->rows, z->classes, z->dtype), p.lanes, p.chunks, p.blocks, p.flat_rows};
+    const GradLaunch l{z->dtype, same, same && whole_vectors(z->x, z->stride, z->rows, z->classes, z->dtype) && whole_vectors(a.d, a.d_stride, z->rows, z->classes, z->dtype), p.lanes, p.chunks, p.piece, p.blocks, p.flat_rows};
     if (distill) launch_distill_grad(l, a, st);
     else launch_scores_grad(l, a, st);
     ctx->launches++;

@@ -67,6 +67,13 @@ template <int VEC> struct Cover {
     }
 };
 
+// the largest of a warp's values (not a NaN where there is a number), in one instruction of sm_100a
+__device__ __forceinline__ float warp_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
 // over the LANES lanes of one row, side by side
 template <int LANES, typename F>
 __device__ __forceinline__ float over_lanes(float v, F f) {
@@ -75,7 +82,11 @@ __device__ __forceinline__ float over_lanes(float v, F f) {
     return v;
 }
 template <int LANES> __device__ __forceinline__ float lanes_sum(float v) { return over_lanes<LANES>(v, [](float a, float b) { return a + b; }); }
-template <int LANES> __device__ __forceinline__ float lanes_max(float v) { return over_lanes<LANES>(v, [](float a, float b) { return fmaxf(a, b); }); }
+template <int LANES>
+__device__ __forceinline__ float lanes_max(float v) {
+    if constexpr (LANES == 32) return warp_max(v);
+    else return over_lanes<LANES>(v, [](float a, float b) { return fmaxf(a, b); });
+}
 template <int LANES>
 __device__ __forceinline__ uint64_t lanes_max(uint64_t v) {
 #pragma unroll

@@ -11,13 +11,15 @@ void launch_scores_grad(const GradLaunch& l, const GradArgs& a, cudaStream_t st)
         MG_LOSS_BY_TYPE(l.dtype, (l.whole ? flat(k_scores_grad_flat<T, false>) : flat(k_scores_grad_flat<T, true>)));
         return;
     }
-    const auto go = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kGradThreads, 0, st>>>(a, l.lanes, l.chunks); };
+    int lanes_log2 = 0;
+    while (1 << lanes_log2 < l.lanes) ++lanes_log2;
+    const auto go = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kGradThreads, 0, st>>>(a, lanes_log2, l.chunks, l.piece); };
     MG_LOSS_BY_TYPE(l.dtype, (l.whole ? go(k_scores_grad<T, true, true>) : l.same ? go(k_scores_grad<T, true, false>) : go(k_scores_grad<T, false, false>)));
 }
 
 void launch_distill_grad(const GradLaunch& l, const GradArgs& a, cudaStream_t st) {
     const auto rows = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kGradThreads, 0, st>>>(a); };
-    const auto block = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kGradThreads, 0, st>>>(a, l.chunks); };
+    const auto block = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kGradThreads, 0, st>>>(a, l.chunks, l.piece); };
     if (l.lanes == 8) MG_LOSS_BY_TYPE(l.dtype, (l.whole ? rows(k_distill_grad_rows<T, 8, true, true>) : l.same ? rows(k_distill_grad_rows<T, 8, true, false>) : rows(k_distill_grad_rows<T, 8, false, false>)));
     else if (l.lanes == 32) MG_LOSS_BY_TYPE(l.dtype, (l.whole ? rows(k_distill_grad_rows<T, 32, true, true>) : l.same ? rows(k_distill_grad_rows<T, 32, true, false>) : rows(k_distill_grad_rows<T, 32, false, false>)));
     else MG_LOSS_BY_TYPE(l.dtype, (l.whole ? block(k_distill_grad<T, true, true>) : l.same ? block(k_distill_grad<T, true, false>) : block(k_distill_grad<T, false, false>)));

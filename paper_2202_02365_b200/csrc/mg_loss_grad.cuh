@@ -103,18 +103,17 @@ __device__ __forceinline__ void stream_row(const RowGrad& g, bool zero, const T*
 
 // `lanes` threads to a row, or to one of its `chunks` pieces.  The label's gradient is written over what its vector got, by the thread that had the vector.
 template <typename T, bool SAME, bool WHOLE>
-__global__ void __launch_bounds__(kGradThreads) k_scores_grad(const __grid_constant__ GradArgs a, int lanes, int chunks) {
+__global__ void __launch_bounds__(kGradThreads) k_scores_grad(const __grid_constant__ GradArgs a, int lanes_log2, int chunks, int32_t piece) {
     constexpr int VEC = 16 / sizeof(T);
-    const int group = (int)threadIdx.x / lanes, sub = (int)threadIdx.x & (lanes - 1), groups = kGradThreads / lanes;
-    const int64_t items = a.rows * chunks;
-    for (int64_t i = (int64_t)blockIdx.x * groups + group; i < items; i += (int64_t)gridDim.x * groups) {
-        const int64_t r = chunks == 1 ? i : i / chunks;
-        const int32_t chunk = (int32_t)(i - r * chunks);
+    const int lanes = 1 << lanes_log2, group = (int)threadIdx.x >> lanes_log2, sub = (int)threadIdx.x & (lanes - 1), groups = kGradThreads >> lanes_log2;
+    const int64_t r = chunks == 1 ? (int64_t)blockIdx.x * groups + group : blockIdx.x / (unsigned)chunks;
+    if (r < a.rows) {
+        const int32_t chunk = chunks == 1 ? 0 : (int32_t)(blockIdx.x - (unsigned)r * (unsigned)chunks);
         const T* x = static_cast<const T*>(a.x) + r * a.stride;
         T* d = static_cast<T*>(a.d) + r * a.d_stride;
         const Cover<VEC> cover(d, sizeof(T), a.classes, WHOLE);
         int32_t lo = 0, hi = cover.vecs;
-        if (chunks > 1) { lo = (int32_t)((int64_t)cover.vecs * chunk / chunks); hi = (int32_t)((int64_t)cover.vecs * (chunk + 1) / chunks); }
+        if (chunks > 1) { lo = min(chunk * piece, cover.vecs); hi = min(lo + piece, cover.vecs); }
         const float lse = a.lse[r];
         const int32_t label = a.d_log_prob ? class_at(a.labels, a.labels_are_i64, r, a.classes) : -1;
         const float of_label = label >= 0 ? a.d_log_prob[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f, l = a.d_lse ? a.d_lse[r] : 0.f;
@@ -284,7 +283,7 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad_rows(const __grid
 
 // a block to a row, or to one of its `chunks` pieces
 template <typename T, bool SAME, bool WHOLE>
-__global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_constant__ GradArgs a, int chunks) {
+__global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_constant__ GradArgs a, int chunks, int32_t piece) {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ int32_t c[MG_MAX_TEACHER];
     __shared__ float q[MG_MAX_TEACHER], scratch[8], sh_mass;
@@ -295,7 +294,7 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_cons
     T* d = static_cast<T*>(a.d) + r * a.d_stride;
     const float lse = a.lse[r], d_loss = a.d_loss[r];
     const Cover<VEC> cover(d, sizeof(T), a.classes, WHOLE);
-    const int32_t lo = (int32_t)((int64_t)cover.vecs * chunk / chunks), hi = (int32_t)((int64_t)cover.vecs * (chunk + 1) / chunks);
+    const int32_t lo = min(chunk * piece, cover.vecs), hi = min(lo + piece, cover.vecs);
     const int warps = (min(t.entries, 256) + 31) / 32;
     TeacherRow row;
     float at_class[kTeacherEach];

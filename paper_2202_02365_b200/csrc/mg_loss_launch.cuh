@@ -10,7 +10,7 @@ struct ForwardLaunch {
     int dtype;
     bool whole;            // rows begin and end with a vector
     int nv, lanes;         // narrow rows: vectors to a lane, lanes to a row; wide ones: 0
-    int parts, threads;    // wide rows: blocks to a row, threads to a block
+    int parts_log2, threads;   // wide rows: blocks to a row, threads to a block
     int64_t blocks;
 };
 void launch_scores(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t st);
@@ -19,7 +19,8 @@ void launch_distill(const ForwardLaunch& l, const ScoreArgs& a, const TeacherArg
 struct GradLaunch {
     int dtype;
     bool same, whole;      // logits' and gradient's vectors begin alike; rows begin and end with one
-    int lanes, chunks;     // threads to a row (256: a block), pieces of it
+    int lanes, chunks;     // threads to a row (256: a block), pieces of it ...
+    int32_t piece;         // ... of so many vectors
     int64_t blocks;
     int flat_rows;         // rows to a block that takes them as one run, 0: not so
 };
@@ -27,14 +28,17 @@ void launch_scores_grad(const GradLaunch& l, const GradArgs& a, cudaStream_t st)
 void launch_distill_grad(const GradLaunch& l, const GradArgs& a, cudaStream_t st);
 
 template <typename K, typename... A>
-void launch_cluster(K kernel, const ForwardLaunch& l, cudaStream_t st, const A&... args) {
-    if (l.parts > 8) cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+void launch_cluster(K kernel, int ring_bytes, const ForwardLaunch& l, cudaStream_t st, const A&... args) {
+    const int parts = 1 << l.parts_log2;
+    if (parts > 8) cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (ring_bytes > 32 << 10) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes);   // (beside the static, beyond 48 KB)
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = (unsigned)l.parts; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    attr.val.clusterDim.x = (unsigned)parts; attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t how = {};
     how.gridDim = dim3((unsigned)l.blocks); how.blockDim = dim3((unsigned)l.threads); how.stream = st;
-    how.attrs = &attr; how.numAttrs = l.parts > 1 ? 1 : 0;
+    how.dynamicSmemBytes = (size_t)ring_bytes;
+    how.attrs = &attr; how.numAttrs = parts > 1 ? 1 : 0;
     cudaLaunchKernelEx(&how, kernel, args...);   // (an error is found by cudaGetLastError)
 }
 

@@ -96,7 +96,7 @@ inline bool same_phase(const void* a, int64_t a_stride, const void* b, int64_t b
 constexpr int kPlanRowThreads = 256, kPlanHeld = 32;   // of the narrow kernels; values of a row to a lane
 constexpr int kPlanWideThreads = 256, kPlanWideMost = 1024, kPlanWideVecs = 8;
 
-struct ForwardPlan { int nv = 0, lanes = 0, parts = 1, threads = 0; int64_t blocks = 0; };
+struct ForwardPlan { int nv = 0, lanes = 0, parts = 1, parts_log2 = 0, threads = 0; int64_t blocks = 0; };
 
 // Rows that 32 lanes hold in registers are narrow (however they lie to the vectors): 8 lanes to a row where these hold it and are as many as best classes are asked for.
 // Wide rows: a block goes along one, or a cluster of up to 16 blocks where rows are fewer than the GPU holds blocks (four to a multiprocessor), a quarter of a segment of
@@ -113,7 +113,7 @@ inline ForwardPlan plan_forward(const mg_logits* z, int32_t top, int n_sms) {
         return p;
     }
     const int64_t segment = (int64_t)kPlanWideThreads * kPlanWideVecs * vec;
-    while (p.parts < 16 && z->rows * p.parts * 2 <= 4ll * n_sms && z->classes / (p.parts * 2) >= segment / 4) p.parts *= 2;
+    while (p.parts < 16 && z->rows * p.parts * 2 <= 4ll * n_sms && z->classes / (p.parts * 2) >= segment / 4) { p.parts *= 2; ++p.parts_log2; }
     p.threads = z->rows * p.parts <= n_sms && z->classes / p.parts > 2 * segment ? kPlanWideMost : kPlanWideThreads;
     p.blocks = z->rows * p.parts;
     return p;
@@ -121,7 +121,7 @@ inline ForwardPlan plan_forward(const mg_logits* z, int32_t top, int n_sms) {
 
 constexpr int kPlanGradThreads = 256, kPlanGradBatch = 4, kPlanTeacherRoom = 8;
 
-struct GradPlan { int lanes = 0, chunks = 1; int64_t blocks = 0; int flat_rows = 0; };
+struct GradPlan { int lanes = 0, chunks = 1; int32_t piece = 0; int64_t blocks = 0; int flat_rows = 0; };
 
 // Rows that lie one behind the other from a vector's beginning on, in both matrices: a block takes as many as have 2,048 vectors (8 at least, a multiple of 8, so that every block begins
 // with one; 256 at most), fewer where two blocks to a multiprocessor would not come about.  Rows of up to 2,048 values of two bytes: beyond, they are taken one by one.
@@ -146,6 +146,7 @@ inline GradPlan plan_grad(const mg_logits* z, int32_t entries, int n_sms) {
         const int64_t batch = (int64_t)kPlanGradThreads * kPlanGradBatch, most = std::max<int64_t>(1, covered / batch), want = (32ll * n_sms + z->rows - 1) / std::max<int64_t>(z->rows, 1);
         p.chunks = (int)std::min({most, std::max(want, covered / (4 * batch)), ((int64_t)(1ll << 31) - 1) / std::max<int64_t>(z->rows, 1)});
         p.chunks = std::max(p.chunks, 1);
+        p.piece = (int32_t)((covered + p.chunks - 1) / p.chunks);
         p.blocks = z->rows * p.chunks;
     } else {
         const int64_t groups = kPlanGradThreads / p.lanes;

@@ -13,8 +13,8 @@ static void launch_rows(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t
 
 template <typename T, int THREADS>
 static void launch_wide(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t st) {
-    if (l.whole) launch_cluster(k_scores_wide<T, THREADS, false>, l, st, a, l.parts);
-    else launch_cluster(k_scores_wide<T, THREADS, true>, l, st, a, l.parts);
+    if (l.whole) launch_cluster(k_scores_wide<T, THREADS, false>, kWideAhead * THREADS * 16, l, st, a, l.parts_log2);
+    else launch_cluster(k_scores_wide<T, THREADS, true>, kWideAhead * THREADS * 16, l, st, a, l.parts_log2);
 }
 
 void launch_scores(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t st) {

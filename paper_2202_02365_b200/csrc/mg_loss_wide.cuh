@@ -1,4 +1,5 @@
-// Wide rows of logits, forward: blocks that go along a row in segments of registers, one or a cluster of them to a row.
+// Wide rows of logits, forward: a block or a cluster of them goes along a row, whose vectors every thread has brought to places of its own in shared memory some rounds ahead:
+// no registers wait for them, and no thread for another's.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -7,9 +8,16 @@
 
 namespace mgloss {
 
-constexpr int kWideThreads = 256, kWideMostThreads = 1024, kWideVecs = 8;   // (four segments of 32 KB on their way to an SM)
-constexpr int kWideRoom = 1024, kWideTrim = 256;   // vectors that may hold one of the best classes: room, and how many of them are cut down to the best again ...
-constexpr int kWideLook = 8;                       // ... which is looked at behind every so many segments
+constexpr int kWideThreads = 256, kWideMostThreads = 1024;
+constexpr int kWideAhead = 6;                      // vectors of a thread that are on their way (24 KB of a block; with five or six blocks to an SM more than the memory's latency asks for)
+constexpr int kWideRoom = 512, kWideTrim = 128;    // vectors that may hold one of the best classes: room, and how many of them are cut down to the best again ...
+constexpr int kWideLook = 32;                      // ... which is looked at behind every so many rounds
+
+__device__ __forceinline__ void copy_ahead(void* shared, const void* global) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global) : "memory");
+}
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 // packed values of one type: two halves to a word, or a float
 template <typename T> struct Word {
@@ -42,12 +50,14 @@ template <typename T> struct Word {
     }
 };
 
-// One thread's part of a row's sums, as it goes along: whenever its largest value grows, what it has is scaled down.
+// One thread's part of a row's sums, as it goes along, about a value that none of its own lies far above: where one comes that is more than 2^8 times as likely, what it has
+// is scaled down.  (About the largest value itself, almost every vector early in a row would scale one lane's sums down.)
+constexpr float kFarAbove = 8.f;
 template <bool WEIGHTED> struct Running {
     float max = kNegInf;
     Pair sum = {0}, weighted = {0}, minus_max = {0};
     __device__ __forceinline__ void raise(float m, float scale2) {
-        if (!(m > max)) return;
+        if (!((m - max) * scale2 > kFarAbove)) return;   // (a first number is infinitely far above)
         if (max != kNegInf) {
             const float by = (max - m) * scale2, f = fast_exp2(by);
             const Pair ff = pair(f, f);
@@ -74,28 +84,25 @@ template <bool WEIGHTED> struct Running {
     }
 };
 
-// sums about different largest values brought together about the larger
-template <bool WEIGHTED>
-__device__ __forceinline__ RowSums joined(RowSums a, RowSums b, float scale2) {
-    const float m = fmaxf(a.max, b.max), by_a = (a.max - m) * scale2, by_b = (b.max - m) * scale2;
+// Sums about different values brought together about the largest of these: over the lanes of a warp, or over the first COUNT of them.
+template <bool WEIGHTED, int COUNT>
+__device__ __forceinline__ RowSums over_warp(RowSums a, float scale2) {
+    const float m = warp_max(a.max), by = (a.max - m) * scale2;
     // (a part without a class has no sum; one with a NaN alone keeps it)
-    const float fa = a.max == kNegInf ? 1.f : fast_exp2(by_a), fb = b.max == kNegInf ? 1.f : fast_exp2(by_b);
-    RowSums r{m, fmaf(a.sum, fa, b.sum * fb), 0.f};
-    if (WEIGHTED) {
-        const float wa = fa == 0.f || a.max == kNegInf ? 0.f : fa * fmaf(a.sum, by_a, a.weighted), wb = fb == 0.f || b.max == kNegInf ? 0.f : fb * fmaf(b.sum, by_b, b.weighted);
-        r.weighted = wa + wb;
-    }
-    return r;
+    const float f = a.max == kNegInf ? 1.f : fast_exp2(by);
+    if (WEIGHTED) a.weighted = f == 0.f || a.max == kNegInf ? 0.f : f * fmaf(a.sum, by, a.weighted);   // sum 2^(y + by) (y + by)
+    return {m, lanes_sum<COUNT>(a.sum * f), WEIGHTED ? lanes_sum<COUNT>(a.weighted) : 0.f};
 }
 
-template <int THREADS> struct WideShared {
+// (ROOM: without best classes, none)
+template <int THREADS, int ROOM> struct WideShared {
     static constexpr int WARPS = THREADS / 32;
     float max[WARPS], sum[WARPS], weighted[WARPS], scratch[WARPS];
     float all[3];                  // of the block: what others of its cluster read
     int n, n_best;                 // vectors, classes that may be among the best; more than there is room for: the best are found one by one
-    float first[32];               // the largest values of the first segment's threads, a few of each warp
-    uint64_t vecs[kWideRoom];      // a vector's largest value and its number
-    uint64_t room[kWideRoom];      // a class and its value
+    float first[32], bound;        // the largest values of the threads' first vectors, a few of each warp; what lies below is not among the best
+    uint64_t vecs[ROOM];           // a vector's largest value and its number
+    uint64_t room[ROOM];           // a class and its value
     uint64_t best[MG_MAX_TOP], warp_best[WARPS];
 };
 
@@ -112,132 +119,121 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int32_t t
 
 // A value that no more than a few of the row's lie above, and `top` do not lie below: the top-th largest of the few largest that each warp's threads have found in their
 // first vectors.  (full: warps all of whose threads have one.)
-template <int THREADS>
-__device__ __forceinline__ float first_bound(float own, int full, int32_t top, WideShared<THREADS>* sh) {
-    if (full <= 0) return kNegInf;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, use = min(full, 32), each = min(32 / use, (top + use - 1) / use + 1);
-    if (each * use < top) return kNegInf;
+template <int THREADS, int ROOM>
+__device__ __forceinline__ float first_bound(float own, int full, int32_t top, WideShared<THREADS, ROOM>* sh) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, use = max(min(full, 32), 1), each = min(32 / use, (top + use - 1) / use + 1);
+    if (full <= 0 || each * use < top) { __syncthreads(); return kNegInf; }
     if (warp < use) {
         float left = own;
         for (int k = 0; k < each; ++k) {
-            const float most = value_of(__reduce_max_sync(0xFFFFFFFFu, order_of(left)));
+            const float most = warp_max(left);
             const uint32_t holders = __ballot_sync(0xFFFFFFFFu, left == most);
             if (lane == __ffs(holders) - 1) left = kNegInf;
             if (lane == 0) sh->first[warp * each + k] = most;
         }
     }
     __syncthreads();
-    const float v = lane < each * use ? sh->first[lane] : kNegInf;
-    int rank = 0;
-#pragma unroll 8
-    for (int j = 0; j < 32; ++j) {
-        const float o = __shfl_sync(0xFFFFFFFFu, v, j);
-        rank += o > v || (o == v && j < lane);
+    if (warp == 0) {
+        float v = lane < each * use ? sh->first[lane] : kNegInf;
+        // sorted over the warp, the largest first (a bitonic network)
+#pragma unroll
+        for (int size = 2; size <= 32; size *= 2)
+#pragma unroll
+            for (int o = size / 2; o; o >>= 1) {
+                const float other = __shfl_xor_sync(0xFFFFFFFFu, v, o);
+                v = ((lane & o) == 0) == ((lane & size) == 0) ? fmaxf(v, other) : fminf(v, other);
+            }
+        if (lane == top - 1) sh->bound = v;
     }
-    return __shfl_sync(0xFFFFFFFFu, v, __ffs(__ballot_sync(0xFFFFFFFFu, rank == top - 1)) - 1);
+    __syncthreads();
+    return sh->bound;
 }
 
-// A row's part `part` of `parts`: its classes are vectors [lo, hi) of the cut, the first part's the edges too.  `meanwhile` is called when the first loads are on their way.
+// the largest value of a vector, of each half of its words
+template <typename T>
+__device__ __forceinline__ uint32_t largest_of(const uint4& w) { return Word<T>::max(Word<T>::max(w.x, w.y), Word<T>::max(w.z, w.w)); }
+
+// A row's part `part` of 2^parts_log2: its classes are vectors [lo, hi) of the cut, the first part's the edges too.  `meanwhile` is called when the first vectors are on their way.
 // On return thread 0 .. all have the part's sums, and sh->best the part's best classes (zero where it has fewer).
-template <typename T, int THREADS, bool WEIGHTED, bool EDGES, typename F>
-__device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float scale2, int part, int parts, int32_t top, WideShared<THREADS>* sh, F meanwhile) {
+template <typename T, int THREADS, int ROOM, bool WEIGHTED, bool EDGES, typename F>
+__device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float scale2, int part, int parts_log2, int32_t top, WideShared<THREADS, ROOM>* sh, uint4* ring, F meanwhile) {
     constexpr int VEC = 16 / sizeof(T), WARPS = THREADS / 32;
     const Cut<VEC> cut(x, sizeof(T), classes);
-    const int32_t lo = (int32_t)((int64_t)cut.vecs * part / parts), hi = (int32_t)((int64_t)cut.vecs * (part + 1) / parts);
-    // segments of about as many rounds of a vector to each thread, eight at most: the last round of all alone is not a whole one
-    const int32_t rounds = max(1, (hi - lo + THREADS - 1) / THREADS), segments = (rounds + kWideVecs - 1) / kWideVecs, each = (rounds + segments - 1) / segments;
+    const int32_t lo = (int32_t)((int64_t)cut.vecs * part >> parts_log2), hi = (int32_t)((int64_t)cut.vecs * (part + 1) >> parts_log2);
+    const int32_t count = hi - lo, rounds = (count + THREADS - 1) / THREADS;
+    const uint4* from = reinterpret_cast<const uint4*>(x + cut.head) + lo + (int32_t)threadIdx.x;
+    uint4* own_ring = ring + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < kWideAhead; ++i) {
+        if (i * THREADS + (int32_t)threadIdx.x < count) copy_ahead(own_ring + i * THREADS, from + i * THREADS);
+        copies_end();
+    }
     const bool has_edge = EDGES && part == 0 && (int)threadIdx.x < cut.edges;
     const Pair scales = pair(scale2, scale2);
     Running<WEIGHTED> run;
     float least = kNegInf;      // what lies below is not among the best
-    for (int32_t s = 0; s < segments; ++s) {
-        const int32_t from = lo + s * each * THREADS, to = min(from + each * THREADS, hi), full = (to - from) / THREADS, some = (to - from + THREADS - 1) / THREADS;
-        const uint4* at = reinterpret_cast<const uint4*>(x + cut.head) + from + threadIdx.x;
-        uint4 raw[kWideVecs];
-#pragma unroll
-        for (int j = 0; j < kWideVecs; ++j) {
-            if (j < full) raw[j] = __ldg(at + j * THREADS);
-            else if (j < some) {
-                raw[j] = make_uint4(Word<T>::least(), Word<T>::least(), Word<T>::least(), Word<T>::least());
-                if (from + j * THREADS + (int32_t)threadIdx.x < to) raw[j] = __ldg(at + j * THREADS);
-            }
-        }
-        float edge = kNegInf;
-        if (s == 0) {
-            if (has_edge) edge = to_float(x[cut.edge(threadIdx.x)]);
-            meanwhile();
-        }
-        const auto largest_of = [](const uint4& w) { return Word<T>::max(Word<T>::max(w.x, w.y), Word<T>::max(w.z, w.w)); };
+    float edge = kNegInf;
+    if (has_edge) edge = to_float(x[cut.edge(threadIdx.x)]);
+    meanwhile();
+    if (top) {
         uint32_t all = Word<T>::least();
+        copies_wait<0>();
 #pragma unroll
-        for (int j = 0; j < kWideVecs; ++j)
-            if (j < some) all = Word<T>::max(all, largest_of(raw[j]));
-        const float own = fmaxf(Word<T>::largest(all), edge);
-        if (top) {
-            if (s == 0) {
-                if (threadIdx.x == 0) { sh->n = 0; sh->n_best = 0; }
-                least = first_bound<THREADS>(own, min((to - from) / 32, WARPS), top, sh);
-                __syncthreads();
+        for (int i = 0; i < kWideAhead; ++i)
+            if (i * THREADS + (int32_t)threadIdx.x < count) all = Word<T>::max(all, largest_of<T>(own_ring[i * THREADS]));
+        if (threadIdx.x == 0) { sh->n = 0; sh->n_best = 0; }
+        least = first_bound<THREADS>(fmaxf(Word<T>::largest(all), edge), min(count / 32, WARPS), top, sh);
+    }
+    if (EDGES) {
+        run.raise(edge, scale2);
+        run.add(edge, kNegInf, scales);
+    }
+    uint4* slot = own_ring;
+    for (int32_t i = 0, v = threadIdx.x; i < rounds; ++i, v += THREADS) {
+        copies_wait<kWideAhead - 1>();
+        if (v < count) {
+            const uint4 raw = *slot;
+            const float m = Word<T>::largest(largest_of<T>(raw));
+            if (top && m >= least) {
+                const int at = atomicAdd(&sh->n, 1);
+                if (at < kWideRoom) sh->vecs[at] = key_of(m, lo + v);
             }
-            if (own >= least) {
+            run.raise(m, scale2);
+            const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-                for (int j = 0; j < kWideVecs; ++j)
-                    if (j < some) {
-                        const int32_t v = from + j * THREADS + (int32_t)threadIdx.x;
-                        const float m = Word<T>::largest(largest_of(raw[j]));
-                        if (m >= least && v < to) {
-                            const int i = atomicAdd(&sh->n, 1);
-                            if (i < kWideRoom) sh->vecs[i] = key_of(m, v);
-                        }
-                    }
+            for (int k = 0; k < 4; k += 3 - Word<T>::N) {
+                float a, b;
+                if constexpr (sizeof(T) == 4) { a = __uint_as_float(w[k]); b = __uint_as_float(w[k + 1]); }
+                else Word<T>::floats(w[k], &a, &b);
+                run.add(a, b, scales);
             }
-            if (s % kWideLook == kWideLook - 1 && s + 1 < segments) {
-                // (a vector that holds one of the best is among the `top` whose largest values are)
-                __syncthreads();
-                const int n = sh->n;
-                if (n > kWideTrim && n <= kWideRoom) {
-                    rank_keys<THREADS>(sh->vecs, n, top, sh->best);
-                    __syncthreads();
-                    if ((int)threadIdx.x < top) sh->vecs[threadIdx.x] = sh->best[threadIdx.x];
-                    if (threadIdx.x == 0) sh->n = top;
-                    least = fmaxf(least, value_of((uint32_t)(sh->best[top - 1] >> 32)));
-                }
-                __syncthreads();
-            }
+            if (v + kWideAhead * THREADS < count) copy_ahead(slot, from + (i + kWideAhead) * THREADS);
         }
-        run.raise(own, scale2);
-#pragma unroll
-        for (int j = 0; j < kWideVecs; ++j)
-            if (j < some) {
-                const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
-#pragma unroll
-                for (int k = 0; k < 4; k += 3 - Word<T>::N) {
-                    float a, b;
-                    if constexpr (sizeof(T) == 4) { a = __uint_as_float(w[k]); b = __uint_as_float(w[k + 1]); }
-                    else Word<T>::floats(w[k], &a, &b);
-                    run.add(a, b, scales);
-                }
+        copies_end();
+        slot = slot == own_ring + (kWideAhead - 1) * THREADS ? own_ring : slot + THREADS;
+        if (top && i % kWideLook == kWideLook - 1 && i + 1 < rounds) {
+            // (a vector that holds one of the best is among the `top` whose largest values are)
+            __syncthreads();
+            const int n = sh->n;
+            if (n > kWideTrim && n <= kWideRoom) {
+                rank_keys<THREADS>(sh->vecs, n, top, sh->best);
+                __syncthreads();
+                if ((int)threadIdx.x < top) sh->vecs[threadIdx.x] = sh->best[threadIdx.x];
+                if (threadIdx.x == 0) sh->n = top;
+                least = fmaxf(least, value_of((uint32_t)(sh->best[top - 1] >> 32)));
             }
-        if (EDGES && s == 0) run.add(edge, kNegInf, scales);
+            __syncthreads();
+        }
     }
     // over the block, in an order that does not change
-    RowSums r = run.both();
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const RowSums other{__shfl_xor_sync(0xFFFFFFFFu, r.max, o), __shfl_xor_sync(0xFFFFFFFFu, r.sum, o), WEIGHTED ? __shfl_xor_sync(0xFFFFFFFFu, r.weighted, o) : 0.f};
-        r = joined<WEIGHTED>(r, other, scale2);
-    }
+    RowSums r = over_warp<WEIGHTED, 32>(run.both(), scale2);
     if ((threadIdx.x & 31) == 0) { sh->max[threadIdx.x / 32] = r.max; sh->sum[threadIdx.x / 32] = r.sum; if (WEIGHTED) sh->weighted[threadIdx.x / 32] = r.weighted; }
     __syncthreads();
     if (threadIdx.x < 32) {
         const int w = threadIdx.x;
         r = {kNegInf, 0.f, 0.f};
         if (w < WARPS) r = {sh->max[w], sh->sum[w], WEIGHTED ? sh->weighted[w] : 0.f};
-#pragma unroll
-        for (int o = WARPS / 2; o; o >>= 1) {
-            const RowSums other{__shfl_xor_sync(0xFFFFFFFFu, r.max, o), __shfl_xor_sync(0xFFFFFFFFu, r.sum, o), WEIGHTED ? __shfl_xor_sync(0xFFFFFFFFu, r.weighted, o) : 0.f};
-            r = joined<WEIGHTED>(r, other, scale2);
-        }
+        r = over_warp<WEIGHTED, WARPS>(r, scale2);
         if (w == 0) { sh->all[0] = r.max; sh->all[1] = r.sum; sh->all[2] = r.weighted; }
     }
     if (top) {
@@ -272,10 +268,10 @@ __device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float s
 
 // The best of the part one by one, each a pass over it: where candidates overflow (more equal values than there is room for, values that rise along the row, NaN).
 template <typename T, int THREADS>
-__device__ __noinline__ void best_one_by_one(const T* x, int32_t classes, int part, int parts, int32_t top, WideShared<THREADS>* sh) {
+__device__ __noinline__ void best_one_by_one(const T* x, int32_t classes, int part, int parts_log2, int32_t top, WideShared<THREADS, kWideRoom>* sh) {
     constexpr int VEC = 16 / sizeof(T), WARPS = THREADS / 32;
     const Cut<VEC> cut(x, sizeof(T), classes);
-    const int32_t lo = (int32_t)((int64_t)cut.vecs * part / parts), hi = (int32_t)((int64_t)cut.vecs * (part + 1) / parts);
+    const int32_t lo = (int32_t)((int64_t)cut.vecs * part >> parts_log2), hi = (int32_t)((int64_t)cut.vecs * (part + 1) >> parts_log2);
     uint64_t last = ~0ull;
     for (int k = 0; k < top; ++k) {
         uint64_t best = 0;
@@ -300,29 +296,42 @@ __device__ __noinline__ void best_one_by_one(const T* x, int32_t classes, int pa
 }
 
 // the parts' sums, in rank 0's hands
-template <bool WEIGHTED, int THREADS>
-__device__ __forceinline__ RowSums over_cluster(RowSums r, int parts, float scale2, WideShared<THREADS>* sh) {
+template <bool WEIGHTED, int THREADS, int ROOM>
+__device__ __forceinline__ RowSums over_cluster(RowSums r, int parts, float scale2, WideShared<THREADS, ROOM>* sh) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
-    if (cluster.block_rank() == 0)
-        for (int p = 1; p < parts; ++p) {
+    if (cluster.block_rank() == 0) {
+        const int p = threadIdx.x & 31;
+        r = {kNegInf, 0.f, 0.f};
+        if (p < parts) {
             const float* from = cluster.map_shared_rank(sh->all, p);
-            r = joined<WEIGHTED>(r, {from[0], from[1], from[2]}, scale2);
+            r = {from[0], from[1], from[2]};
         }
+        r = over_warp<WEIGHTED, 16>(r, scale2);
+        r = {r.max, __shfl_sync(0xFFFFFFFFu, r.sum, 0), __shfl_sync(0xFFFFFFFFu, r.weighted, 0)};
+    }
     return r;
 }
 
+#ifndef MG_SB
+#define MG_SB 6
+#endif
+#ifndef MG_DB
+#define MG_DB 6
+#endif
 template <typename T, int THREADS, bool EDGES>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_wide(const __grid_constant__ ScoreArgs a, int parts) {
+__global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? MG_SB : 1) k_scores_wide(const __grid_constant__ ScoreArgs a, int parts_log2) {
     namespace cg = cooperative_groups;
-    __shared__ WideShared<THREADS> sh;
-    const int64_t r = blockIdx.x / (unsigned)parts;
-    const int part = (int)(blockIdx.x - (unsigned)r * (unsigned)parts);
+    __shared__ WideShared<THREADS, kWideRoom> sh;
+    extern __shared__ __align__(16) uint4 ring[];   // kWideAhead vectors of each thread
+    const int parts = 1 << parts_log2;
+    const int64_t r = blockIdx.x >> parts_log2;
+    const int part = (int)(blockIdx.x & (unsigned)(parts - 1));
     const T* x = static_cast<const T*>(a.x) + r * a.stride;
     int32_t label = -1;
     float at_label = 0.f;
-    RowSums s = go_along<T, THREADS, true, EDGES>(x, a.classes, a.scale2, part, parts, a.top, &sh, [&] {
+    RowSums s = go_along<T, THREADS, kWideRoom, true, EDGES>(x, a.classes, a.scale2, part, parts_log2, a.top, &sh, ring, [&] {
         if (threadIdx.x == 0 && part == 0 && a.log_prob) {
             label = class_at(a.labels, a.labels_are_i64, r, a.classes);
             if (label >= 0) at_label = to_float(x[label]);
@@ -330,7 +339,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_scores_wide(const _
     });
     if (a.top) {
         const int n = sh.n_best;
-        if (sh.n > kWideRoom || n > kWideRoom || n < a.top || !(s.sum < __builtin_huge_valf()) || !(s.max > kNegInf)) best_one_by_one<T, THREADS>(x, a.classes, part, parts, a.top, &sh);
+        if (sh.n > kWideRoom || n > kWideRoom || n < a.top || !(s.sum < __builtin_huge_valf()) || !(s.max > kNegInf)) best_one_by_one<T, THREADS>(x, a.classes, part, parts_log2, a.top, &sh);
         else rank_keys<THREADS>(sh.room, n, a.top, sh.best);
         __syncthreads();
     }
@@ -426,16 +435,18 @@ struct TeacherRow {
 };
 
 template <typename T, int THREADS, bool EDGES>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) k_distill_wide(const __grid_constant__ ScoreArgs a, const __grid_constant__ TeacherArgs t, float* loss, int parts) {
+__global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? MG_DB : 1) k_distill_wide(const __grid_constant__ ScoreArgs a, const __grid_constant__ TeacherArgs t, float* loss, int parts_log2) {
     namespace cg = cooperative_groups;
-    __shared__ WideShared<THREADS> sh;
+    __shared__ WideShared<THREADS, 1> sh;
+    extern __shared__ __align__(16) uint4 ring[];   // kWideAhead vectors of each thread
     __shared__ float at_class[MG_MAX_TEACHER];   // the student's logits, fetched while the first segment is on its way
-    const int64_t r = blockIdx.x / (unsigned)parts;
-    const int part = (int)(blockIdx.x - (unsigned)r * (unsigned)parts);
+    const int parts = 1 << parts_log2;
+    const int64_t r = blockIdx.x >> parts_log2;
+    const int part = (int)(blockIdx.x & (unsigned)(parts - 1));
     const T* x = static_cast<const T*>(a.x) + r * a.stride;
     const int warps = min(256 / 32, (t.entries + 31) / 32);
     const bool teaches = part == 0 && (int)threadIdx.x < warps * 32;
-    RowSums s = go_along<T, THREADS, false, EDGES>(x, a.classes, a.scale2, part, parts, 0, &sh, [&] {
+    RowSums s = go_along<T, THREADS, 1, false, EDGES>(x, a.classes, a.scale2, part, parts_log2, 0, &sh, ring, [&] {
         if (teaches)
             for (int k = threadIdx.x; k < t.entries; k += 256) {
                 const int32_t c = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, a.classes);
