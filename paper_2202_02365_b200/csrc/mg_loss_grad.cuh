@@ -286,7 +286,7 @@ template <typename T, bool SAME, bool WHOLE>
 __global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_constant__ GradArgs a, int chunks, int32_t piece) {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ int32_t c[MG_MAX_TEACHER];
-    __shared__ float q[MG_MAX_TEACHER], scratch[8], sh_mass;
+    __shared__ float q[MG_MAX_TEACHER], at_class[MG_MAX_TEACHER], scratch[kTeacherThreads / 32], sh_mass;
     const TeacherArgs& t = a.teacher;
     const int64_t r = blockIdx.x / (unsigned)chunks;
     const int32_t chunk = (int32_t)(blockIdx.x - (unsigned)r * (unsigned)chunks);
@@ -295,23 +295,11 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_cons
     const float lse = a.lse[r], d_loss = a.d_loss[r];
     const Cover<VEC> cover(d, sizeof(T), a.classes, WHOLE);
     const int32_t lo = min(chunk * piece, cover.vecs), hi = min(lo + piece, cover.vecs);
-    const int warps = (min(t.entries, 256) + 31) / 32;
-    TeacherRow row;
-    float at_class[kTeacherEach];
+    const int warps = teacher_warps(t);
+    const auto here = [&](int32_t of) { return of >= 0 && (of + cover.lead) / VEC >= lo && (of + cover.lead) / VEC < hi; };
     if ((int)threadIdx.x < warps * 32) {
-        row.load(t, r, a.classes, a.scale);
-#pragma unroll
-        for (int i = 0; i < kTeacherEach; ++i) {
-            const int32_t at = row.c[i] >= 0 ? (row.c[i] + cover.lead) / VEC : -1;
-            at_class[i] = at >= lo && at < hi ? to_float(x[row.c[i]]) : 0.f;
-        }
-        float log_shift;
-        const float mass = row.probabilities(t, r, warps, scratch, &log_shift);
-#pragma unroll
-        for (int i = 0; i < kTeacherEach; ++i) {
-            const int k = threadIdx.x + i * 256;
-            if (k < t.entries) { c[k] = row.c[i]; q[k] = row.v[i]; }
-        }
+        const float mass = teacher_row(t, r, x, a.classes, a.scale, warps, scratch, q, at_class, c, here);
+        for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) q[k] = fast_exp2(q[k] * kLog2e);
         if (threadIdx.x == 0) sh_mass = mass;
     }
     __syncthreads();
@@ -321,13 +309,9 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_cons
     stream_row<SAME, WHOLE>(g, zero, x, d, a.classes, cover.lead, lo, hi, (int)threadIdx.x, kGradThreads);
     __syncthreads();
     if (zero || (int)threadIdx.x >= warps * 32) return;
-#pragma unroll
-    for (int i = 0; i < kTeacherEach; ++i) {
-        const int k = threadIdx.x + i * 256;
-        if (k >= t.entries) break;
-        const int32_t at = row.c[i] >= 0 ? (row.c[i] + cover.lead) / VEC : -1;
+    for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
         float of_class;
-        if (at >= lo && at < hi && first_of_class(c, q, k, t.entries, &of_class)) write_one(g, at_class[i], -a.scale * d_loss * of_class, d + row.c[i]);
+        if (here(c[k]) && first_of_class(c, q, k, t.entries, &of_class)) write_one(g, at_class[k], -a.scale * d_loss * of_class, d + c[k]);
     }
 }
 

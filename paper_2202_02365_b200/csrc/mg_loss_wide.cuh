@@ -10,11 +10,14 @@ namespace mgloss {
 
 constexpr int kWideThreads = 256, kWideMostThreads = 1024;
 constexpr int kWideAhead = 6;                      // vectors of a thread that are on their way (24 KB of a block; with five or six blocks to an SM more than the memory's latency asks for)
-constexpr int kWideRoom = 512, kWideTrim = 128;    // vectors that may hold one of the best classes: room, and how many of them are cut down to the best again ...
-constexpr int kWideLook = 32;                      // ... which is looked at behind every so many rounds
+constexpr int kWideRoom = 512, kWideTrim = 128;    // pairs of vectors, and classes, that may be among the best: room; how many classes are cut down to the best again
 
-__device__ __forceinline__ void copy_ahead(void* shared, const void* global) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(global) : "memory");
+// (places in shared memory by their 32-bit addresses)
+__device__ __forceinline__ void copy_ahead(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ uint4 copied(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
@@ -99,21 +102,28 @@ template <int THREADS, int ROOM> struct WideShared {
     static constexpr int WARPS = THREADS / 32;
     float max[WARPS], sum[WARPS], weighted[WARPS], scratch[WARPS];
     float all[3];                  // of the block: what others of its cluster read
-    int n, n_best;                 // vectors, classes that may be among the best; more than there is room for: the best are found one by one
+    int n, n_best;                 // pairs of vectors, classes that may be among the best; more than there is room for: the best are found one by one
     float first[32], bound;        // the largest values of the threads' first vectors, a few of each warp; what lies below is not among the best
-    uint64_t vecs[ROOM];           // a vector's largest value and its number
+    int32_t pairs[ROOM];
     uint64_t room[ROOM];           // a class and its value
     uint64_t best[MG_MAX_TOP], warp_best[WARPS];
 };
 
-// the `top` best of the keys to `best`, the best first (every thread; behind a barrier, and before one)
+// The `top` best of the keys to `best`, the best first (every thread; behind a barrier, and before one): each key's rank is counted, by up to eight neighbouring threads.
 template <int THREADS>
 __device__ __forceinline__ void rank_keys(const uint64_t* keys, int n, int32_t top, uint64_t* best) {
-    for (int i = threadIdx.x; i < n; i += THREADS) {
-        const uint64_t key = keys[i];
+    int share = 1;
+    while (share < 8 && n * share * 2 <= THREADS) share *= 2;
+    const int sub = (int)threadIdx.x & (share - 1);
+    for (int i0 = 0; i0 < n; i0 += THREADS / share) {
+        const int i = i0 + (int)threadIdx.x / share;
+        const uint64_t key = i < n ? keys[i] : ~0ull;
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += keys[j] > key;
-        if (rank < top) best[rank] = key;
+        if (i < n)
+#pragma unroll 4
+            for (int j = sub; j < n; j += share) rank += keys[j] > key;
+        for (int o = 1; o < share; o *= 2) rank += __shfl_xor_sync(0xFFFFFFFFu, rank, o);
+        if (i < n && sub == 0 && rank < top) best[rank] = key;
     }
 }
 
@@ -161,13 +171,15 @@ __device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float s
     const Cut<VEC> cut(x, sizeof(T), classes);
     const int32_t lo = (int32_t)((int64_t)cut.vecs * part >> parts_log2), hi = (int32_t)((int64_t)cut.vecs * (part + 1) >> parts_log2);
     const int32_t count = hi - lo, rounds = (count + THREADS - 1) / THREADS;
-    const uint4* from = reinterpret_cast<const uint4*>(x + cut.head) + lo + (int32_t)threadIdx.x;
-    uint4* own_ring = ring + threadIdx.x;
+    const char* from = reinterpret_cast<const char*>(x + cut.head) + ((int64_t)lo + (int32_t)threadIdx.x) * 16;
+    constexpr uint32_t kStep = THREADS * 16, kRing = kWideAhead * kStep;
+    const uint32_t first = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16, last = first + kRing;
 #pragma unroll
     for (int i = 0; i < kWideAhead; ++i) {
-        if (i * THREADS + (int32_t)threadIdx.x < count) copy_ahead(own_ring + i * THREADS, from + i * THREADS);
+        if (i * THREADS + (int32_t)threadIdx.x < count) copy_ahead(first + i * kStep, from + i * kStep);
         copies_end();
     }
+    from += kRing;
     const bool has_edge = EDGES && part == 0 && (int)threadIdx.x < cut.edges;
     const Pair scales = pair(scale2, scale2);
     Running<WEIGHTED> run;
@@ -180,7 +192,7 @@ __device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float s
         copies_wait<0>();
 #pragma unroll
         for (int i = 0; i < kWideAhead; ++i)
-            if (i * THREADS + (int32_t)threadIdx.x < count) all = Word<T>::max(all, largest_of<T>(own_ring[i * THREADS]));
+            if (i * THREADS + (int32_t)threadIdx.x < count) all = Word<T>::max(all, largest_of<T>(copied(first + i * kStep)));
         if (threadIdx.x == 0) { sh->n = 0; sh->n_best = 0; }
         least = first_bound<THREADS>(fmaxf(Word<T>::largest(all), edge), min(count / 32, WARPS), top, sh);
     }
@@ -188,42 +200,95 @@ __device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float s
         run.raise(edge, scale2);
         run.add(edge, kNegInf, scales);
     }
-    uint4* slot = own_ring;
-    for (int32_t i = 0, v = threadIdx.x; i < rounds; ++i, v += THREADS) {
-        copies_wait<kWideAhead - 1>();
-        if (v < count) {
-            const uint4 raw = *slot;
-            const float m = Word<T>::largest(largest_of<T>(raw));
-            if (top && m >= least) {
-                const int at = atomicAdd(&sh->n, 1);
-                if (at < kWideRoom) sh->vecs[at] = key_of(m, lo + v);
-            }
-            run.raise(m, scale2);
-            const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+    const auto add = [&](const uint4& raw) {
+        const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-            for (int k = 0; k < 4; k += 3 - Word<T>::N) {
-                float a, b;
-                if constexpr (sizeof(T) == 4) { a = __uint_as_float(w[k]); b = __uint_as_float(w[k + 1]); }
-                else Word<T>::floats(w[k], &a, &b);
-                run.add(a, b, scales);
+        for (int k = 0; k < 4; k += 3 - Word<T>::N) {
+            float a, b;
+            if constexpr (sizeof(T) == 4) { a = __uint_as_float(w[k]); b = __uint_as_float(w[k + 1]); }
+            else Word<T>::floats(w[k], &a, &b);
+            run.add(a, b, scales);
+        }
+    };
+    // Which of the last 32 pairs of the thread's vectors may hold one of the best: their classes are collected behind these, by whichever threads.
+    uint32_t flags = 0;
+    const auto collect = [&](int32_t pair0) {
+        for (; flags; flags &= flags - 1) {
+            const int at = atomicAdd(&sh->n, 1);
+            if (at < ROOM) sh->pairs[at] = (pair0 + __ffs(flags) - 1) * (2 * THREADS) + (int32_t)threadIdx.x;
+        }
+        __syncthreads();
+        const int n = sh->n;
+        if (n > ROOM) { if (threadIdx.x == 0) sh->n_best = ROOM + 1; }
+        else
+            for (int e = threadIdx.x; e < 2 * n; e += THREADS) {
+                const int32_t v = sh->pairs[e >> 1] + (e & 1) * THREADS;
+                if (v >= count) continue;
+                const int32_t c = cut.head + (lo + v) * VEC;
+                Raw<T, VEC> raw;
+                raw.load(x + c);
+                uint32_t some = 0;
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) some |= (raw.get(k) >= least ? 1u : 0u) << k;
+                for (; some; some &= some - 1) {
+                    const int at = atomicAdd(&sh->n_best, 1);
+                    if (at < ROOM) sh->room[at] = key_of(to_float(x[c + __ffs(some) - 1]), c + __ffs(some) - 1);
+                }
             }
-            if (v + kWideAhead * THREADS < count) copy_ahead(slot, from + (i + kWideAhead) * THREADS);
+        __syncthreads();
+    };
+    uint32_t slot = first;
+    int32_t i = 0;
+    // two rounds at a time, as long as every thread has a vector in both
+    for (const int32_t whole = count / THREADS; i + 2 <= whole; i += 2) {
+        copies_wait<kWideAhead - 2>();
+        const uint4 one = copied(slot), two = copied(slot + kStep);
+        const float m = Word<T>::largest(Word<T>::max(largest_of<T>(one), largest_of<T>(two)));
+        if (top && m >= least) flags |= 1u << (i / 2 % 32);
+        run.raise(m, scale2);
+        add(one);
+        add(two);
+        if (i + kWideAhead + 2 <= whole) {
+            copy_ahead(slot, from);
+            copy_ahead(slot + kStep, from + kStep);
+        } else {
+            const int32_t v = (i + kWideAhead) * THREADS + (int32_t)threadIdx.x;
+            if (v < count) copy_ahead(slot, from);
+            if (v + THREADS < count) copy_ahead(slot + kStep, from + kStep);
         }
         copies_end();
-        slot = slot == own_ring + (kWideAhead - 1) * THREADS ? own_ring : slot + THREADS;
-        if (top && i % kWideLook == kWideLook - 1 && i + 1 < rounds) {
-            // (a vector that holds one of the best is among the `top` whose largest values are)
-            __syncthreads();
-            const int n = sh->n;
-            if (n > kWideTrim && n <= kWideRoom) {
-                rank_keys<THREADS>(sh->vecs, n, top, sh->best);
+        copies_end();   // (a group for each round, as at the beginning and the end)
+        from += 2 * kStep;
+        slot += 2 * kStep;
+        if (slot == last) slot = first;
+        if (top && i % 64 == 62 && i + 2 < rounds) {
+            collect(i / 2 - 31);
+            const int n = sh->n_best;
+            if (n > kWideTrim && n <= ROOM) {
+                rank_keys<THREADS>(sh->room, n, top, sh->best);
                 __syncthreads();
-                if ((int)threadIdx.x < top) sh->vecs[threadIdx.x] = sh->best[threadIdx.x];
-                if (threadIdx.x == 0) sh->n = top;
+                if ((int)threadIdx.x < top) sh->room[threadIdx.x] = sh->best[threadIdx.x];
                 least = fmaxf(least, value_of((uint32_t)(sh->best[top - 1] >> 32)));
             }
             __syncthreads();
+            if (threadIdx.x == 0) { sh->n = 0; if (n > kWideTrim && n <= ROOM) sh->n_best = top; }
+            __syncthreads();
         }
+    }
+    for (int32_t v = i * THREADS + (int32_t)threadIdx.x; i < rounds; ++i, v += THREADS) {
+        copies_wait<kWideAhead - 1>();
+        if (v < count) {
+            const uint4 one = copied(slot);
+            const float m = Word<T>::largest(largest_of<T>(one));
+            if (top && m >= least) flags |= 1u << (i / 2 % 32);
+            run.raise(m, scale2);
+            add(one);
+            if (v + kWideAhead * THREADS < count) copy_ahead(slot, from);
+        }
+        copies_end();
+        from += kStep;
+        slot += kStep;
+        if (slot == last) slot = first;
     }
     // over the block, in an order that does not change
     RowSums r = over_warp<WEIGHTED, 32>(run.both(), scale2);
@@ -237,29 +302,11 @@ __device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float s
         if (w == 0) { sh->all[0] = r.max; sh->all[1] = r.sum; sh->all[2] = r.weighted; }
     }
     if (top) {
-        // the classes of the vectors that are left
-        const int n = sh->n;
-        if (n <= kWideRoom) {
-            for (int i = threadIdx.x; i < n; i += THREADS) {
-                const int32_t c = cut.head + class_of(sh->vecs[i]) * VEC;
-                Raw<T, VEC> raw;
-                raw.load(x + c);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (raw.get(e) >= least) {
-                        const int at = atomicAdd(&sh->n_best, 1);
-                        if (at < kWideRoom) sh->room[at] = key_of(raw.get(e), c + e);
-                    }
-            }
-            if (has_edge) {
-                const int32_t c = cut.edge(threadIdx.x);
-                const float v = to_float(x[c]);
-                if (v >= least) {
-                    const int at = atomicAdd(&sh->n_best, 1);
-                    if (at < kWideRoom) sh->room[at] = key_of(v, c);
-                }
-            }
+        if (has_edge && edge >= least) {
+            const int at = atomicAdd(&sh->n_best, 1);
+            if (at < ROOM) sh->room[at] = key_of(edge, cut.edge(threadIdx.x));
         }
+        collect((rounds - 1) / 64 * 32);
     }
     __syncthreads();
     r = {sh->all[0], sh->all[1], sh->all[2]};
@@ -314,14 +361,9 @@ __device__ __forceinline__ RowSums over_cluster(RowSums r, int parts, float scal
     return r;
 }
 
-#ifndef MG_SB
-#define MG_SB 6
-#endif
-#ifndef MG_DB
-#define MG_DB 6
-#endif
+constexpr int kWideBlocks = 6;   // to an SM
 template <typename T, int THREADS, bool EDGES>
-__global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? MG_SB : 1) k_scores_wide(const __grid_constant__ ScoreArgs a, int parts_log2) {
+__global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? kWideBlocks : 1) k_scores_wide(const __grid_constant__ ScoreArgs a, int parts_log2) {
     namespace cg = cooperative_groups;
     __shared__ WideShared<THREADS, kWideRoom> sh;
     extern __shared__ __align__(16) uint4 ring[];   // kWideAhead vectors of each thread
@@ -339,7 +381,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? MG_SB : 1) 
     });
     if (a.top) {
         const int n = sh.n_best;
-        if (sh.n > kWideRoom || n > kWideRoom || n < a.top || !(s.sum < __builtin_huge_valf()) || !(s.max > kNegInf)) best_one_by_one<T, THREADS>(x, a.classes, part, parts_log2, a.top, &sh);
+        if (n > kWideRoom || n < a.top || !(s.sum < __builtin_huge_valf()) || !(s.max > kNegInf)) best_one_by_one<T, THREADS>(x, a.classes, part, parts_log2, a.top, &sh);
         else rank_keys<THREADS>(sh.room, n, a.top, sh.best);
         __syncthreads();
     }
@@ -370,10 +412,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? MG_SB : 1) 
     if (parts > 1) cg::this_cluster().sync();   // (nobody leaves while its memory is read)
 }
 
-// A row's pairs of a teacher's, four or fewer to each of 256 threads: class, scaled value.
-constexpr int kTeacherEach = MG_MAX_TEACHER / 256;
-
-// Sum and largest of a value over the first `warps` warps of a block, in their hands; barrier 1 is theirs.
+// Over the first `warps` warps of a block, in their hands; barrier 1 is theirs.
 __device__ __forceinline__ void some_warps_meet(int warps) {
     if (warps > 1) asm volatile("bar.sync 1, %0;" ::"r"(warps * 32) : "memory");
     else __syncwarp();
@@ -390,81 +429,63 @@ __device__ __forceinline__ float over_warps(float v, int warps, float* scratch, 
     return v;
 }
 
-// The teacher's probabilities of a row's pairs: the warps that have a pair each work them out; `c`, `q` and `log_q` [entries] get classes (-1: none), probabilities, logarithms.
-// (256 threads at most.)  Returns their sum.
-struct TeacherRow {
-    int32_t c[kTeacherEach];
-    float v[kTeacherEach];
-    __device__ __forceinline__ void load(const TeacherArgs& t, int64_t r, int32_t classes, float scale) {
-#pragma unroll
-        for (int i = 0; i < kTeacherEach; ++i) {
-            const int k = threadIdx.x + i * 256;
-            c[i] = -1; v[i] = kNegInf;
-            if (k < t.entries) {
-                c[i] = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, classes);
-                if (c[i] >= 0) v[i] = scale * float_at(t.values, t.dtype, r * t.values_stride + k);
-            }
-        }
+// The warps that deal with a teacher's pairs: a pair to a thread, up to 256 threads; more pairs go round.
+constexpr int kTeacherThreads = 256;
+__device__ __forceinline__ int teacher_warps(const TeacherArgs& t) { return (min(t.entries, kTeacherThreads) + 31) / 32; }
+
+// The teacher's probabilities of a row's pairs, as logarithms (-infinity: none, or not a pair), in shared memory, by these warps; at_class: the logits of their classes, where `wanted(class)`.
+// Each thread deals with the same pairs throughout.  Returns the probabilities' sum.
+template <typename T, typename F>
+__device__ __forceinline__ float teacher_row(const TeacherArgs& t, int64_t r, const T* x, int32_t classes, float scale, int warps, float* scratch, float* log_q, float* at_class, int32_t* c, F wanted) {
+    float m = kNegInf;
+    for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
+        const int32_t of = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, classes);
+        const float v = of >= 0 ? scale * float_at(t.values, t.dtype, r * t.values_stride + k) : kNegInf;
+        at_class[k] = of >= 0 && wanted(of) ? to_float(x[of]) : 0.f;
+        log_q[k] = v;
+        if (c) c[k] = of;
+        m = fmaxf(m, v);
     }
-    // q in the place of v; log q = v - log_shift
-    __device__ __forceinline__ float probabilities(const TeacherArgs& t, int64_t r, int warps, float* scratch, float* log_shift) {
-        float shift, sum = 1.f;
-        if (t.lse) shift = t.lse[r];
-        else {
-            float m = kNegInf;
-#pragma unroll
-            for (int i = 0; i < kTeacherEach; ++i) m = fmaxf(m, v[i]);
-            m = over_warps(m, warps, scratch, [](float a, float b) { return fmaxf(a, b); });
-            shift = centre(m);
-            sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < kTeacherEach; ++i)
-                if (c[i] >= 0) sum += fast_exp2((v[i] - shift) * kLog2e);
-            sum = over_warps(sum, warps, scratch, [](float a, float b) { return a + b; });
-        }
-        const float part = sum == 0.f ? 0.f : 1.f / sum;
-        *log_shift = shift + (sum == 0.f ? 0.f : logf(sum));
-        float mass = 0.f;
-#pragma unroll
-        for (int i = 0; i < kTeacherEach; ++i) {
-            v[i] = c[i] >= 0 ? fast_exp2((v[i] - shift) * kLog2e) * part : 0.f;
-            mass += v[i];
-        }
-        return over_warps(mass, warps, scratch, [](float a, float b) { return a + b; });
+    float shift, sum = 0.f;
+    if (t.lse) shift = t.lse[r];
+    else {
+        shift = centre(over_warps(m, warps, scratch, [](float a, float b) { return fmaxf(a, b); }));
+        for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) sum += fast_exp2((log_q[k] - shift) * kLog2e);   // (0 of -infinity)
+        sum = over_warps(sum, warps, scratch, [](float a, float b) { return a + b; });
+        if (sum != 0.f) shift += logf(sum);
     }
-};
+    float mass = 0.f;
+    for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
+        log_q[k] -= shift;
+        mass += fast_exp2(log_q[k] * kLog2e);
+    }
+    return over_warps(mass, warps, scratch, [](float a, float b) { return a + b; });
+}
 
 template <typename T, int THREADS, bool EDGES>
-__global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? MG_DB : 1) k_distill_wide(const __grid_constant__ ScoreArgs a, const __grid_constant__ TeacherArgs t, float* loss, int parts_log2) {
+__global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? kWideBlocks : 1) k_distill_wide(const __grid_constant__ ScoreArgs a, const __grid_constant__ TeacherArgs t, float* loss, int parts_log2) {
     namespace cg = cooperative_groups;
     __shared__ WideShared<THREADS, 1> sh;
     extern __shared__ __align__(16) uint4 ring[];   // kWideAhead vectors of each thread
-    __shared__ float at_class[MG_MAX_TEACHER];   // the student's logits, fetched while the first segment is on its way
+    __shared__ float log_q[MG_MAX_TEACHER], at_class[MG_MAX_TEACHER];
     const int parts = 1 << parts_log2;
     const int64_t r = blockIdx.x >> parts_log2;
     const int part = (int)(blockIdx.x & (unsigned)(parts - 1));
     const T* x = static_cast<const T*>(a.x) + r * a.stride;
-    const int warps = min(256 / 32, (t.entries + 31) / 32);
+    const int warps = teacher_warps(t);
     const bool teaches = part == 0 && (int)threadIdx.x < warps * 32;
+    // (the teacher's side while the row's first vectors are on their way)
     RowSums s = go_along<T, THREADS, 1, false, EDGES>(x, a.classes, a.scale2, part, parts_log2, 0, &sh, ring, [&] {
-        if (teaches)
-            for (int k = threadIdx.x; k < t.entries; k += 256) {
-                const int32_t c = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, a.classes);
-                at_class[k] = c >= 0 ? to_float(x[c]) : 0.f;
-            }
+        if (teaches) teacher_row(t, r, x, a.classes, a.scale, warps, sh.scratch, log_q, at_class, nullptr, [](int32_t) { return true; });
     });
     if (parts > 1) s = over_cluster<false>(s, parts, a.scale2, &sh);
     if (teaches) {
         const RowResult res(s, a.scale);
-        TeacherRow row;
-        row.load(t, r, a.classes, a.scale);
-        float raw[kTeacherEach], log_shift, v = 0.f;
-#pragma unroll
-        for (int i = 0; i < kTeacherEach; ++i) raw[i] = row.v[i];
-        row.probabilities(t, r, warps, sh.scratch, &log_shift);
-#pragma unroll
-        for (int i = 0; i < kTeacherEach; ++i)
-            if (row.v[i] != 0.f) v = fmaf(row.v[i], (raw[i] - log_shift) - res.log_p(at_class[threadIdx.x + i * 256]), v);
+        float v = 0.f;
+        for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
+            const float q = fast_exp2(log_q[k] * kLog2e);
+            if (q != 0.f) v = fmaf(q, log_q[k] - res.log_p(at_class[k]), v);
+        }
         v = over_warps(v, warps, sh.scratch, [](float a, float b) { return a + b; });
         if (threadIdx.x == 0) {
             loss[r] = v;
