@@ -104,8 +104,8 @@ void launch_sums(const SumArgs& a, int vec, cudaStream_t st) {
     const int lanes = std::min(32, std::max(4, pow2_up((a.dim + (vec > 1 ? vec : 4) - 1) / (vec > 1 ? vec : 4))));
     const int columns = lanes * (vec > 1 ? vec : 4);
     const dim3 grid((unsigned)(((int64_t)a.chunks * lanes + kSumThreads - 1) / kSumThreads), (unsigned)((a.dim + columns - 1) / columns));
-    if (vec > 1) mgnorm::launch_chained(grid, kSumThreads, st, k_chunk_sums<T, O, WIDE, 1, 8>, a, lanes);
-    else mgnorm::launch_chained(grid, kSumThreads, st, k_chunk_sums<T, O, 1, 4, 4>, a, lanes);
+    if (vec > 1) mgnorm::launch_chained(grid, kSumThreads, st, k_chunk_sums<T, O, WIDE, 1, 4>, a, lanes);
+    else mgnorm::launch_chained(grid, kSumThreads, st, k_chunk_sums<T, O, 1, 4, 2>, a, lanes);
 }
 
 }  // namespace
@@ -186,7 +186,7 @@ extern "C" int mg_embedding_backward(mg_ctx* ctx, const void* d_y, int64_t d_y_s
     if (p.chunks > 0) {
         const int vec = row_vec(d_y, d_y_stride, d_y_dtype, n, out, out_stride, out_dtype, n_rows, dim);
         MG_BY_TYPE(d_y_dtype, using From = T; MG_BY_TYPE(out_dtype, (launch_sums<From, T>(a, vec, st))));
-        MG_BY_TYPE(out_dtype, mgnorm::launch_chained(dim3((unsigned)p.chunks, (unsigned)((dim + 127) / 128)), kJoinThreads, st, k_join_shares<T>, a));
+        MG_BY_TYPE(out_dtype, mgnorm::launch_chained(dim3((unsigned)std::min(p.chunks, mg_grid(ctx, 1)), (unsigned)((dim + 127) / 128)), kJoinThreads, st, k_join_shares<T>, a));
         ctx->launches += 2;
     }
     MG_CUDA(ctx, cudaGetLastError());

@@ -93,14 +93,14 @@ struct SumPlan {
     size_t at_begun = 0, bytes = 0;
 };
 
-// Places to a chunk: 1,536 threads of every multiprocessor are to have one, of 32 places at least (16 more of a row's values, or 8 lanes, make half as many chunks), and no
-// id is to leave more than 4,096 shares.
+// Places to a chunk: two times the 768 threads that a multiprocessor holds are to have one, of 32 places at least, and no id is to leave more than 8,192 shares.
 inline SumPlan plan_sums(int64_t n, int64_t n_rows, int32_t dim, int n_sms = 148) {
     SumPlan p;
     p.pitch = (dim + 7) / 8 * 8;
     if (n == 0 || n_rows == 0) return p;
     const int64_t lanes = dim >= 128 ? (dim + 127) / 128 * 32 : dim > 64 ? 32 : dim > 32 ? 16 : dim > 16 ? 8 : 4;
-    p.chunk = (int32_t)std::max<int64_t>({n * lanes / ((int64_t)n_sms * 1536), n / 4096, 32});
+    const int64_t threads = (int64_t)n_sms * 1536;
+    p.chunk = (int32_t)std::max<int64_t>({(n * lanes + threads - 1) / threads, n / 8192, 32});
     p.chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
     p.at_begun = rows_align(8 * (size_t)p.chunks * p.pitch);
     p.bytes = p.at_begun + rows_align(4 * (size_t)p.chunks);

@@ -26,19 +26,37 @@ struct SortShared {
     uint32_t failed;                        // a bounded wait ran out
 };
 
-// (digits of equal ids in one warp are added once: all the same id would wait for one another)
+// Which lanes of the warp have the same digit (`ok`: that have one), by a vote for each of its bits: a match instruction takes some 70 cycles of an SM, where this takes six.
+__device__ __forceinline__ uint32_t same_digit(uint32_t digit, int bits, bool ok) {
+    uint32_t peers = __ballot_sync(0xFFFFFFFFu, ok);
+#pragma unroll
+    for (int b = 0; b < kSortBits; ++b)
+        if (b < bits) {
+            const uint32_t votes = __ballot_sync(0xFFFFFFFFu, digit >> b & 1);
+            peers &= digit >> b & 1 ? votes : ~votes;
+        }
+    return peers;
+}
+
+// (a warp whose digits are all the same adds them once: many of one id would wait for one another)
 __global__ void __launch_bounds__(kSortThreads) k_sort_hist(const void* ids, int ids_are_i64, int64_t n, uint32_t none, int passes, int bits, SortShared* s) {
     __shared__ uint32_t sh[kMaxPasses][kSortBins];
     for (int p = 0; p < kMaxPasses; ++p) sh[p][threadIdx.x] = 0;
     __syncthreads();
     const int lane = threadIdx.x & 31;
-    for (int64_t j = (int64_t)blockIdx.x * kSortThreads; j < n; j += (int64_t)gridDim.x * kSortThreads) {
-        const int64_t i = j + threadIdx.x;
-        const uint32_t key = i < n ? sort_key(ids, ids_are_i64, i, none) : 0u;
-        for (int p = 0; p < passes; ++p) {
-            const uint32_t digit = i < n ? key >> p * bits & ((1u << bits) - 1u) : kSortBins;
-            const uint32_t peers = __match_any_sync(0xFFFFFFFFu, digit);
-            if (i < n && lane == __ffs(peers) - 1) atomicAdd(&sh[p][digit], (uint32_t)__popc(peers));
+    constexpr int U = 4;
+    for (int64_t j = (int64_t)blockIdx.x * kSortThreads * U; j < n; j += (int64_t)gridDim.x * kSortThreads * U) {
+        uint32_t key[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) key[u] = j + u * kSortThreads + threadIdx.x < n ? sort_key(ids, ids_are_i64, j + u * kSortThreads + threadIdx.x, none) : 0u;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const bool ok = j + u * kSortThreads + threadIdx.x < n;
+            for (int p = 0; p < passes; ++p) {
+                const uint32_t digit = key[u] >> p * bits & ((1u << bits) - 1u), of_first = __shfl_sync(0xFFFFFFFFu, digit, 0);
+                if (__all_sync(0xFFFFFFFFu, ok && digit == of_first)) { if (lane == 0) atomicAdd(&sh[p][digit], 32u); }
+                else if (ok) atomicAdd(&sh[p][digit], 1u);
+            }
         }
     }
     __syncthreads();
@@ -86,8 +104,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_pass(const void* ids, int
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
         const bool ok = (warp * PER + k) * 32 + lane < tile_n;
-        const uint32_t digit = ok ? key[k] >> shift & mask : kSortBins;
-        const uint32_t peers = __match_any_sync(0xFFFFFFFFu, digit);
+        const uint32_t digit = key[k] >> shift & mask, peers = same_digit(digit, bits, ok);
         const int leader = __ffs(peers) - 1;
         uint32_t old = 0;
         if (ok && lane == leader) { old = counts[warp][digit]; counts[warp][digit] = old + __popc(peers); }

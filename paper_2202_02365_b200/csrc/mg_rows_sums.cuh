@@ -10,7 +10,7 @@
 
 namespace mgrows {
 
-constexpr int kSumThreads = 256, kJoinThreads = 512;
+constexpr int kSumThreads = 256, kJoinThreads = 1024;
 
 struct SumArgs {
     const void* d_y; int64_t d_y_stride, n, n_rows;
@@ -22,14 +22,6 @@ struct SumArgs {
     float* shares; int32_t pitch; // [chunks][2][pitch]: of the id that the chunk begins within, of the one that goes on behind it
     int32_t* begun;               // [chunks]: the group that begins in the chunk and has shares, -1
 };
-
-// how many groups there are, and places that belong to one
-__device__ __forceinline__ bool group_extent(const SumArgs& a, int32_t* groups, int64_t* places) {
-    *groups = *a.n_groups;
-    if (*groups <= 0 || *groups > min(a.n, a.n_rows)) return false;
-    *places = min((int64_t)a.starts[*groups], a.n);
-    return true;
-}
 
 template <typename O, int VEC>
 __device__ __forceinline__ void write_sum(const SumArgs& a, int64_t row, int32_t c, float (&s)[VEC]) {
@@ -47,138 +39,170 @@ __device__ __forceinline__ void write_sum(const SumArgs& a, int64_t row, int32_t
     raw.store(to);
 }
 
-// `lanes` lanes to a chunk, NV vectors of its rows to a lane, U rows on their way; blockIdx.y: which of the rows' columns
+// `lanes` lanes to a chunk, NV vectors of its rows to a lane, U rows on their way while U others are added up; blockIdx.y: which of the rows' columns.
+// What a chunk has to know of its neighbours is asked for beside its first places, and of its first and last ids beside its first rows.
 template <typename T, typename O, int VEC, int NV, int U>
-__global__ void __launch_bounds__(kSumThreads) k_chunk_sums(const __grid_constant__ SumArgs a, int lanes) {
+__global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_constant__ SumArgs a, int lanes) {
     chain_wait();
     chain_start();
     const int sub = (int)threadIdx.x & (lanes - 1);
     const int32_t chunk = (int32_t)((blockIdx.x * (int64_t)kSumThreads + threadIdx.x) / lanes);
     const int32_t c0 = ((int32_t)blockIdx.y * NV * lanes + sub) * VEC, step = lanes * VEC;
-    int32_t groups;
-    int64_t places, lo = 0, hi = 0;
-    int32_t before = -1, behind = -1;   // groups with shares: that go on from the chunk before, that go on behind this one
-    if (group_extent(a, &groups, &places) && chunk < a.chunks) {
-        lo = (int64_t)chunk * a.chunk;
-        hi = min(lo + a.chunk, places);
-        if (lo < hi) {
-            const auto group_at = [&](int64_t i) { return min(max(a.group_of[i], 0), groups - 1); };
-            const int32_t first = group_at(lo), came = lo > 0 ? group_at(lo - 1) : -1, last = group_at(hi - 1);
-            const int64_t end = a.starts[first + 1], last_end = a.starts[last + 1];
-            const bool long_first = end - a.starts[first] > a.chunk, long_last = last_end - a.starts[last] > a.chunk;
-            if (came == first) {
-                if (long_first) before = first;
-                else lo = end;            // whom it began with has it
-            }
-            if (long_last) { if (last_end > hi && last != before) behind = last; }
-            else if (last != before && lo < hi) hi = min(last_end, places);
-        }
+    const uint32_t peers = lanes == 32 ? 0xFFFFFFFFu : ((1u << lanes) - 1u) << ((int)(threadIdx.x & 31) & ~(lanes - 1));
+    if (chunk >= a.chunks) return;
+    const int64_t lo = (int64_t)chunk * a.chunk, hi = min(lo + a.chunk, a.n);
+    const int32_t groups = *a.n_groups;
+    const bool some = groups > 0 && groups <= min(a.n, a.n_rows);
+    const auto group_at = [&](int64_t i) { return min(max(a.group_of[i], -1), groups - 1); };
+    int32_t place = -1, group = -1, next_place = -1, next_group = -1;   // of the lane, in this batch of `lanes` places and the next
+    int32_t first = -1, came = -1, last = -1;                            // groups: of the first place, of the one before, of the last
+    if (some) {
+        if (lo + sub < hi) { place = a.order[lo + sub]; group = group_at(lo + sub); }
+        first = group_at(lo); last = group_at(hi - 1);
+        if (lo > 0) came = group_at(lo - 1);
     }
-    if (sub == 0 && blockIdx.y == 0 && chunk < a.chunks) a.begun[chunk] = behind;
+    const auto load = [&](Raw<T, VEC> (&raw)[U][NV], int32_t of, int at) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t i = __shfl_sync(peers, of, (at + u) & (lanes - 1), lanes);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                if (i >= 0 && i < a.n && c0 + v * step < a.dim) raw[u][v].load(static_cast<const T*>(a.d_y) + i * a.d_y_stride + c0 + v * step);
+                else raw[u][v].zero();
+            }
+        }
+    };
+    Raw<T, VEC> one[U][NV], two[U][NV];
+    load(one, place, 0);
+    // an id that began before the chunk and is no longer than one is left to whom it began with; one that begins here, to its end; longer ones leave a share
+    int32_t before = -1, behind = -1, skip = -1;
+    int64_t end = hi;
+    if (first >= 0 && came == first) {
+        if (a.starts[first + 1] - a.starts[first] > a.chunk) before = first;
+        else skip = first;
+    }
+    if (last >= 0 && last != before && last != skip) {
+        const int64_t until = min((int64_t)a.starts[last + 1], a.n);
+        if (until - a.starts[last] > a.chunk) { if (until > hi) behind = last; }
+        else end = max(until, hi);
+    }
+    if (!some) end = lo;
+    if (sub == 0 && blockIdx.y == 0) a.begun[chunk] = behind;
     float acc[NV][VEC];
 #pragma unroll
     for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) acc[v][e] = 0.f;
-    int32_t cur = -1;
-    int64_t cur_row = -1;
+    int32_t cur = -1, cur_row = -1;
     const auto flush = [&]() {
-        if (cur < 0) return;
-        const bool share = cur == before || cur == behind;
+        if (cur >= 0 && cur != skip) {
+            const bool share = cur == before || cur == behind;
 #pragma unroll
-        for (int v = 0; v < NV; ++v) {
-            const int32_t c = c0 + v * step;
-            if (c < a.dim) {
+            for (int v = 0; v < NV; ++v) {
+                const int32_t c = c0 + v * step;
+                if (c >= a.dim) continue;
                 if (share) {
                     float* to = a.shares + ((int64_t)chunk * 2 + (cur == behind)) * a.pitch + c;
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) to[e] = acc[v][e];
                 } else if (cur_row >= 0) write_sum<O, VEC>(a, cur_row, c, acc[v]);
             }
+        }
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
 #pragma unroll
             for (int e = 0; e < VEC; ++e) acc[v][e] = 0.f;
+    };
+    const auto row_of = [&](int32_t g) -> int32_t {
+        const int64_t row = g < 0 ? -1 : a.into == MG_ROWS_COMPACT ? g : id_at(a.group_ids, a.ids_are_i64, g);
+        return row < a.n_rows ? (int32_t)row : -1;
+    };
+    int32_t row = row_of(group);
+    const auto ask = [&](int64_t p) {   // for a batch's places
+        next_place = next_group = -1;
+        if (p + sub < end) { next_place = a.order[p + sub]; next_group = group_at(p + sub); }
+    };
+    ask(lo + lanes);
+    const auto add = [&](const Raw<T, VEC> (&raw)[U][NV], int64_t p, int at) {   // the places p + at ..
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t g = __shfl_sync(peers, group, (at + u) & (lanes - 1), lanes), r = __shfl_sync(peers, row, (at + u) & (lanes - 1), lanes);
+            if (p + at + u < end) {
+                if (g != cur) { flush(); cur = g; cur_row = r; }
+#pragma unroll
+                for (int v = 0; v < NV; ++v)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) acc[v][e] += raw[u][v].get(e);
+            }
         }
     };
-    const uint32_t peers = lanes == 32 ? 0xFFFFFFFFu : (1u << lanes) - 1u << ((int)(threadIdx.x & 31) & ~(lanes - 1));
-    // a place and its group for each lane, asked for while those before are dealt with; then the rows, U at a time
-    int32_t next_place = -1, next_group = -1;
-    if (lo + sub < hi) { next_place = a.order[lo + sub]; next_group = a.group_of[lo + sub]; }
-    for (int64_t p = lo; p < hi; p += lanes) {
-        int32_t place = next_place;
-        const int32_t group = next_group;
-        int64_t row = group < 0 || group >= groups ? -1 : a.into == MG_ROWS_COMPACT ? group : id_at(a.group_ids, a.ids_are_i64, group);
-        if (row >= a.n_rows) row = -1;
-        if (place >= a.n) place = -1;
-        next_place = next_group = -1;
-        if (p + lanes + sub < hi) { next_place = a.order[p + lanes + sub]; next_group = a.group_of[p + lanes + sub]; }
-        const int count = (int)min((int64_t)lanes, hi - p);
-        for (int i0 = 0; i0 < count; i0 += U) {
-            Raw<T, VEC> raw[U][NV];
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int32_t at = __shfl_sync(peers, place, (i0 + u) & (lanes - 1), lanes);
-#pragma unroll
-                for (int v = 0; v < NV; ++v) {
-                    if (i0 + u < count && at >= 0 && c0 + v * step < a.dim) raw[u][v].load(static_cast<const T*>(a.d_y) + at * a.d_y_stride + c0 + v * step);
-                    else raw[u][v].zero();
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int32_t g = __shfl_sync(peers, group, (i0 + u) & (lanes - 1), lanes);
-                const int32_t r = __shfl_sync(peers, (int32_t)row, (i0 + u) & (lanes - 1), lanes);
-                if (i0 + u < count) {
-                    if (g != cur) { flush(); cur = g; cur_row = r; }
-#pragma unroll
-                    for (int v = 0; v < NV; ++v)
-#pragma unroll
-                        for (int e = 0; e < VEC; ++e) acc[v][e] += raw[u][v].get(e);
-                }
-            }
+    // (a batch is a multiple of 2 U places, or these are all of it)
+    for (int64_t p = lo; p < end; p += lanes) {
+        const int32_t after = next_place;   // places of the batch behind this one
+        for (int at = 0; at < lanes; at += 2 * U) {
+            if (lanes >= 2 * U) load(two, place, at + U);
+            add(one, p, at);
+            const bool more = at + 2 * U < lanes;
+            load(one, more ? place : after, more ? at + 2 * U : 0);
+            if (lanes >= 2 * U) add(two, p, at + U);
         }
+        place = next_place; group = next_group;
+        row = row_of(group);
+        ask(p + 2 * lanes);
     }
     flush();
 }
 
-// The shares of the id that begins in a chunk and goes on behind it: 32 lanes of four columns, 16 warps that each take a stretch of the chunks.
+// The shares of the ids that begin in a chunk and go on behind it: a block looks at every gridDim.x-th chunk; 32 lanes of four columns, 32 warps that each take a stretch of the
+// chunks that an id spans.
 template <typename O>
 __global__ void __launch_bounds__(kJoinThreads) k_join_shares(const __grid_constant__ SumArgs a) {
     constexpr int W = kJoinThreads / 32;
     __shared__ float4 part[W][32];
+    __shared__ int32_t found[kJoinThreads], n_found;
     chain_wait();
     chain_start();
-    const int32_t chunk = (int32_t)blockIdx.x, g = a.begun[chunk];
-    if (g < 0) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t c = ((int32_t)blockIdx.y * 32 + lane) * 4;
-    const int64_t end = min((int64_t)a.starts[g + 1], a.n);
-    const int32_t last = min((int32_t)((end - 1) / a.chunk), a.chunks - 1), shares = last - chunk + 1;
-    const int32_t lo = (int32_t)((int64_t)shares * warp / W), hi = (int32_t)((int64_t)shares * (warp + 1) / W);
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (c < a.dim) {
-        constexpr int U = 4;
-        for (int32_t i0 = lo; i0 < hi; i0 += U) {
-            float4 v[U];
+    for (int32_t c0 = (int32_t)blockIdx.x; c0 < a.chunks; c0 += (int32_t)gridDim.x * kJoinThreads) {
+        if (threadIdx.x == 0) n_found = 0;
+        __syncthreads();
+        const int64_t mine = c0 + (int64_t)threadIdx.x * gridDim.x;
+        if (mine < a.chunks && a.begun[mine] >= 0) found[atomicAdd(&n_found, 1)] = (int32_t)mine;   // (their order does not matter: each id's sum is its own)
+        __syncthreads();
+        for (int f = 0; f < n_found; ++f) {
+            const int32_t chunk = found[f], g = a.begun[chunk];
+            const int64_t end = min((int64_t)a.starts[g + 1], a.n);
+            const int32_t last = min((int32_t)((end - 1) / a.chunk), a.chunks - 1), shares = last - chunk + 1;
+            const int32_t lo = (int32_t)((int64_t)shares * warp / W), hi = (int32_t)((int64_t)shares * (warp + 1) / W);
+            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (c < a.dim) {
+                constexpr int U = 4;
+                for (int32_t i0 = lo; i0 < hi; i0 += U) {
+                    float4 v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u)   // (the first chunk's is the share of an id that begins there)
-                v[u] = i0 + u < hi ? *reinterpret_cast<const float4*>(a.shares + ((int64_t)(chunk + i0 + u) * 2 + (i0 + u == 0)) * a.pitch + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int u = 0; u < U; ++u)   // (the first chunk's is the share of an id that begins there)
+                        v[u] = i0 + u < hi ? *reinterpret_cast<const float4*>(a.shares + ((int64_t)(chunk + i0 + u) * 2 + (i0 + u == 0)) * a.pitch + c) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-            for (int u = 0; u < U; ++u) { s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w; }
+                    for (int u = 0; u < U; ++u) { s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w; }
+                }
+            }
+            part[warp][lane] = s;
+            __syncthreads();
+            const int64_t row = a.into == MG_ROWS_COMPACT ? g : id_at(a.group_ids, a.ids_are_i64, g);
+            if (warp == 0 && c < a.dim && row >= 0 && row < a.n_rows) {
+                for (int w = 1; w < W; ++w) { const float4 o = part[w][lane]; s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w; }
+                const float all[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < a.dim) {
+                        float one[1] = {all[e]};
+                        write_sum<O, 1>(a, row, c + e, one);
+                    }
+            }
+            __syncthreads();
         }
     }
-    part[warp][lane] = s;
-    __syncthreads();
-    if (warp || c >= a.dim) return;
-    for (int w = 1; w < W; ++w) { const float4 o = part[w][lane]; s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w; }
-    const int64_t row = a.into == MG_ROWS_COMPACT ? g : id_at(a.group_ids, a.ids_are_i64, g);
-    if (row < 0 || row >= a.n_rows) return;
-    const float all[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (c + e < a.dim) {
-            float one[1] = {all[e]};
-            write_sum<O, 1>(a, row, c + e, one);
-        }
 }
 
 // Zeros into the rows of the table that no id names: a block finds the named ones among its rows, marks them in shared memory and writes the others.
