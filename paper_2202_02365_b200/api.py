@@ -881,12 +881,12 @@ class Context:
         most = min(n, n_rows)
         need = C.c_size_t(0)
         self._check(self.lib.mg_id_groups_workspace(self.handle, n, n_rows, C.byref(need)))
-        work = torch.empty(need.value, dtype=torch.uint8, device=self.device)
+        work = torch.empty(need.value, dtype=torch.uint8, device=self.device) if need.value else None
         block = torch.empty(2 * n + most + 2, dtype=torch.int32, device=self.device)
         order, group_of, starts, count = torch.split(block, [n, n, most + 1, 1])
         distinct = torch.empty(most, dtype=ids.dtype, device=self.device)
         self._check(self.lib.mg_id_groups(self.handle, ids.data_ptr(), wide, n, n_rows, order.data_ptr(), group_of.data_ptr(), distinct.data_ptr(), starts.data_ptr(), count.data_ptr(),
-                                          work.data_ptr(), need.value, torch._C._cuda_getCurrentRawStream(self.device.index)))
+                                          _at(work), need.value, torch._C._cuda_getCurrentRawStream(self.device.index)))
         return IdGroups(order, group_of, distinct, starts, count, n_rows)
 
     def _group_sums(self, d_y, groups: IdGroups, scale, into, out):

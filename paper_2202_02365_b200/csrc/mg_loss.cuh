@@ -94,6 +94,20 @@ __device__ __forceinline__ uint64_t lanes_max(uint64_t v) {
     return v;
 }
 
+// sorted over the LANES lanes of one row, the largest first (a bitonic network)
+template <int LANES>
+__device__ __forceinline__ float lanes_sorted(float v) {
+    const int lane = threadIdx.x & (LANES - 1);
+#pragma unroll
+    for (int size = 2; size <= LANES; size *= 2)
+#pragma unroll
+        for (int o = size / 2; o; o >>= 1) {
+            const float other = __shfl_xor_sync(0xFFFFFFFFu, v, o);
+            v = ((lane & o) == 0) == ((lane & size) == 0) ? fmaxf(v, other) : fminf(v, other);
+        }
+    return v;
+}
+
 // Sums over a row, of powers of two: y = (x - max) scale log2(e), sum = sum 2^y, weighted = sum 2^y y; max: the largest x, in the place of which 0 is taken where no
 // class is allowed.  (The difference first: x scale - max scale in one instruction goes beyond fp32 where a mask writes the type's lowest value over a row.)
 struct RowSums { float max, sum, weighted; };

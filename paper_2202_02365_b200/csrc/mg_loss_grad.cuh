@@ -11,23 +11,34 @@ constexpr int kGradThreads = 256, kGradBatch = 4;   // vectors of a thread that 
 // What a row's gradient is made of: p (base + slope log p).
 struct RowGrad { float scale, minus_lse, base, slope; };
 
+// The exponentials of two logarithms of probabilities.  Of fp32 rows by expf: the special function unit's power of two is as many units of 2^-24 off as the logarithm has (three times
+// the plain form's error over a gradient), which the rounding to two bytes covers.  2,048 rows of 50,257 take as long.
+template <bool EXACT>
+__device__ __forceinline__ Pair exp_of(Pair log_p) {
+    float a, b;
+    if (EXACT) {
+        split(log_p, &a, &b);
+        return pair(expf(a), expf(b));
+    }
+    split(mul2(log_p, pair(kLog2e, kLog2e)), &a, &b);
+    return pair(fast_exp2(a), fast_exp2(b));
+}
+
 // the gradients of neighbouring classes, in place of their logits
-template <int N>
+template <bool EXACT, int N>
 __device__ __forceinline__ void grads(const RowGrad& g, float (&v)[N]) {
     if constexpr (N == 1) {
         const float log_p = fmaf(v[0], g.scale, g.minus_lse);
-        v[0] = fast_exp2(log_p * kLog2e) * fmaf(fmaxf(log_p, kLeast), g.slope, g.base);
+        v[0] = expf(log_p) * fmaf(fmaxf(log_p, kLeast), g.slope, g.base);
     } else {
-        const Pair scale = pair(g.scale, g.scale), lse = pair(g.minus_lse, g.minus_lse), base = pair(g.base, g.base), slope = pair(g.slope, g.slope), log2e = pair(kLog2e, kLog2e);
+        const Pair scale = pair(g.scale, g.scale), lse = pair(g.minus_lse, g.minus_lse), base = pair(g.base, g.base), slope = pair(g.slope, g.slope);
         const bool sloped = g.slope != 0.f;
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
-            const Pair log_p = fma2(pair(v[i], v[i + 1]), scale, lse), y = mul2(log_p, log2e);
-            float a, b;
-            split(y, &a, &b);
-            const Pair p = pair(fast_exp2(a), fast_exp2(b));
+            const Pair log_p = fma2(pair(v[i], v[i + 1]), scale, lse), p = exp_of<EXACT>(log_p);
             Pair d;
             if (sloped) {
+                float a, b;
                 split(log_p, &a, &b);
                 d = mul2(p, fma2(pair(fmaxf(a, kLeast), fmaxf(b, kLeast)), slope, base));
             } else d = mul2(p, base);
@@ -40,7 +51,7 @@ __device__ __forceinline__ void grads(const RowGrad& g, float (&v)[N]) {
 template <typename T>
 __device__ __forceinline__ void write_one(const RowGrad& g, float x, float more, T* to) {
     float f[1] = {x};
-    grads(g, f);
+    grads<true>(g, f);
     f[0] += more;
     Raw<T, 1> one;
     one.put(f);
@@ -85,7 +96,7 @@ __device__ __forceinline__ void stream_row(const RowGrad& g, bool zero, const T*
             if (zero) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f[e] = 0.f;
-            } else grads(g, f);
+            } else grads<sizeof(T) == 4>(g, f);
             raw[j].put(f);
             if (full) raw[j].store(d + c);
             else
@@ -159,7 +170,7 @@ __global__ void __launch_bounds__(kGradThreads) k_scores_grad_flat(const __grid_
     }
     __syncthreads();
     const bool sloped = a.d_entropy != nullptr;
-    const Pair scale = pair(a.scale, a.scale), log2e = pair(kLog2e, kLog2e);
+    const Pair scale = pair(a.scale, a.scale);
     const int32_t values = rows * a.classes, vecs = values / VEC;
     for (int32_t v0 = threadIdx.x; v0 < vecs; v0 += kGradBatch * kGradThreads) {
         uint4 raw[kGradBatch];
@@ -182,15 +193,14 @@ __global__ void __launch_bounds__(kGradThreads) k_scores_grad_flat(const __grid_
                 const bool first = !CROSS || e < left, second = !CROSS || e + 1 < left;
                 const Pair lse = CROSS ? pair(first ? p.minus_lse : q.minus_lse, second ? p.minus_lse : q.minus_lse) : pair(p.minus_lse, p.minus_lse);
                 Pair factor = CROSS ? pair(first ? p.base : q.base, second ? p.base : q.base) : pair(p.base, p.base);
-                const Pair log_p = fma2(pair(one.get(e), one.get(e + 1)), scale, lse), y = mul2(log_p, log2e);
+                const Pair log_p = fma2(pair(one.get(e), one.get(e + 1)), scale, lse), p_both = exp_of<sizeof(T) == 4>(log_p);
                 float s, t;
                 if (sloped) {
                     split(log_p, &s, &t);
                     const Pair slope = CROSS ? pair(first ? p.slope : q.slope, second ? p.slope : q.slope) : pair(p.slope, p.slope);
                     factor = fma2(pair(fmaxf(s, kLeast), fmaxf(t, kLeast)), slope, factor);
                 }
-                split(y, &s, &t);
-                split(mul2(pair(fast_exp2(s), fast_exp2(t)), factor), &f[e], &f[e + 1]);
+                split(mul2(p_both, factor), &f[e], &f[e + 1]);
             }
             if (p.zero | q.zero) {
 #pragma unroll
@@ -258,12 +268,12 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad_rows(const __grid
             shift = centre(lanes_max<LANES>(m));
             sum = 0.f;
             for (int k = sub; on && k < t.entries; k += LANES)
-                if (c[k] >= 0) sum += fast_exp2((q[k] - shift) * kLog2e);
+                if (c[k] >= 0) sum += expf(q[k] - shift);
             sum = lanes_sum<LANES>(sum);
         }
         const float part = sum == 0.f ? 0.f : 1.f / sum;
         for (int k = sub; on && k < t.entries; k += LANES) {
-            q[k] = c[k] >= 0 ? fast_exp2((q[k] - shift) * kLog2e) * part : 0.f;
+            q[k] = c[k] >= 0 ? expf(q[k] - shift) * part : 0.f;
             mass += q[k];
         }
         mass = lanes_sum<LANES>(mass);
@@ -298,9 +308,9 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_cons
     const int warps = teacher_warps(t);
     const auto here = [&](int32_t of) { return of >= 0 && (of + cover.lead) / VEC >= lo && (of + cover.lead) / VEC < hi; };
     if ((int)threadIdx.x < warps * 32) {
-        const float mass = teacher_row(t, r, x, a.classes, a.scale, warps, scratch, q, at_class, c, here);
-        for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) q[k] = fast_exp2(q[k] * kLog2e);
-        if (threadIdx.x == 0) sh_mass = mass;
+        const TeacherRow teacher = teacher_row(t, r, x, a.classes, a.scale, warps, scratch, q, at_class, c, here);
+        for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) q[k] = expf(q[k]) * teacher.part;
+        if (threadIdx.x == 0) sh_mass = teacher.mass;
     }
     __syncthreads();
     const float mass = sh_mass;

@@ -92,12 +92,7 @@ __device__ __forceinline__ void best_of(const HeldRow<T, NV, LANES, WHOLE>& row,
     const uint32_t peers = (LANES == 32 ? 0xFFFFFFFFu : (1u << LANES % 32) - 1u) << (lane & ~(LANES - 1));
     bool slow = top > LANES;
     if (!slow) {
-        float left = own, least = kNegInf;
-        for (int k = 0; k < top; ++k) {
-            least = lanes_max<LANES>(left);
-            const uint32_t holders = __ballot_sync(0xFFFFFFFFu, left == least) & peers;
-            if (lane == __ffs(holders) - 1) left = kNegInf;
-        }
+        const float least = __shfl_sync(0xFFFFFFFFu, lanes_sorted<LANES>(own), top - 1, LANES);
         slow = !(least > kNegInf) || !(r.log_sum < __builtin_huge_valf());
         uint32_t mine = 0;   // which of the lane's values are candidates
 #pragma unroll
@@ -171,7 +166,7 @@ __device__ __forceinline__ void teacher_sums(const TeacherArgs& t, int64_t r, bo
     m = lanes_max<LANES>(m);
     if (m == kNegInf) m = 0.f;
     for (int k = sub; on && k < t.entries; k += LANES)
-        if (class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, classes) >= 0) s += fast_exp2((scale * float_at(t.values, t.dtype, r * t.values_stride + k) - m) * kLog2e);
+        if (class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, classes) >= 0) s += expf(scale * float_at(t.values, t.dtype, r * t.values_stride + k) - m);
     *shift = m; *sum = lanes_sum<LANES>(s);
 }
 
@@ -194,7 +189,7 @@ __global__ void __launch_bounds__(kRowThreads, row_blocks(NV * 16 / sizeof(T))) 
         for (int k = sub; on && k < t.entries; k += LANES) {
             const int32_t c = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, a.classes);
             if (c < 0) continue;
-            const float d = a.scale * float_at(t.values, t.dtype, r * t.values_stride + k) - shift, q = fast_exp2(d * kLog2e) * part;
+            const float d = a.scale * float_at(t.values, t.dtype, r * t.values_stride + k) - shift, q = expf(d) * part;
             if (q != 0.f) v = fmaf(q, (d - log_sum) - res.log_p(to_float(x[c])), v);
         }
         v = lanes_sum<LANES>(v);

@@ -144,15 +144,7 @@ __device__ __forceinline__ float first_bound(float own, int full, int32_t top, W
     }
     __syncthreads();
     if (warp == 0) {
-        float v = lane < each * use ? sh->first[lane] : kNegInf;
-        // sorted over the warp, the largest first (a bitonic network)
-#pragma unroll
-        for (int size = 2; size <= 32; size *= 2)
-#pragma unroll
-            for (int o = size / 2; o; o >>= 1) {
-                const float other = __shfl_xor_sync(0xFFFFFFFFu, v, o);
-                v = ((lane & o) == 0) == ((lane & size) == 0) ? fmaxf(v, other) : fminf(v, other);
-            }
+        const float v = lanes_sorted<32>(lane < each * use ? sh->first[lane] : kNegInf);
         if (lane == top - 1) sh->bound = v;
     }
     __syncthreads();
@@ -433,33 +425,29 @@ __device__ __forceinline__ float over_warps(float v, int warps, float* scratch, 
 constexpr int kTeacherThreads = 256;
 __device__ __forceinline__ int teacher_warps(const TeacherArgs& t) { return (min(t.entries, kTeacherThreads) + 31) / 32; }
 
-// The teacher's probabilities of a row's pairs, as logarithms (-infinity: none, or not a pair), in shared memory, by these warps; at_class: the logits of their classes, where `wanted(class)`.
-// Each thread deals with the same pairs throughout.  Returns the probabilities' sum.
+// A teacher's row, by these warps: `above` [entries] in shared memory gets the values less `shift` (-infinity: not a pair), at_class the logits of their classes, where
+// `wanted(class)`.  Each thread deals with the same pairs throughout.  A pair's probability is exp(above) part, its logarithm above - log_sum.
+struct TeacherRow { float part, log_sum, mass; };   // mass: the probabilities' sum
 template <typename T, typename F>
-__device__ __forceinline__ float teacher_row(const TeacherArgs& t, int64_t r, const T* x, int32_t classes, float scale, int warps, float* scratch, float* log_q, float* at_class, int32_t* c, F wanted) {
+__device__ __forceinline__ TeacherRow teacher_row(const TeacherArgs& t, int64_t r, const T* x, int32_t classes, float scale, int warps, float* scratch, float* above, float* at_class, int32_t* c, F wanted) {
     float m = kNegInf;
     for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
         const int32_t of = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, classes);
         const float v = of >= 0 ? scale * float_at(t.values, t.dtype, r * t.values_stride + k) : kNegInf;
         at_class[k] = of >= 0 && wanted(of) ? to_float(x[of]) : 0.f;
-        log_q[k] = v;
+        above[k] = v;
         if (c) c[k] = of;
         m = fmaxf(m, v);
     }
-    float shift, sum = 0.f;
-    if (t.lse) shift = t.lse[r];
-    else {
-        shift = centre(over_warps(m, warps, scratch, [](float a, float b) { return fmaxf(a, b); }));
-        for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) sum += fast_exp2((log_q[k] - shift) * kLog2e);   // (0 of -infinity)
-        sum = over_warps(sum, warps, scratch, [](float a, float b) { return a + b; });
-        if (sum != 0.f) shift += logf(sum);
-    }
-    float mass = 0.f;
+    const float shift = t.lse ? t.lse[r] : centre(over_warps(m, warps, scratch, [](float a, float b) { return fmaxf(a, b); }));
+    float sum = 0.f;
     for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
-        log_q[k] -= shift;
-        mass += fast_exp2(log_q[k] * kLog2e);
+        above[k] -= shift;
+        sum += expf(above[k]);   // (0 of -infinity)
     }
-    return over_warps(mass, warps, scratch, [](float a, float b) { return a + b; });
+    sum = over_warps(sum, warps, scratch, [](float a, float b) { return a + b; });
+    if (t.lse) return {1.f, 0.f, sum};
+    return {sum == 0.f ? 0.f : 1.f / sum, logf(sum), sum == 0.f ? 0.f : sum * (1.f / sum)};
 }
 
 template <typename T, int THREADS, bool EDGES>
@@ -467,24 +455,24 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? kWideBlocks
     namespace cg = cooperative_groups;
     __shared__ WideShared<THREADS, 1> sh;
     extern __shared__ __align__(16) uint4 ring[];   // kWideAhead vectors of each thread
-    __shared__ float log_q[MG_MAX_TEACHER], at_class[MG_MAX_TEACHER];
+    __shared__ float above[MG_MAX_TEACHER], at_class[MG_MAX_TEACHER];
     const int parts = 1 << parts_log2;
     const int64_t r = blockIdx.x >> parts_log2;
     const int part = (int)(blockIdx.x & (unsigned)(parts - 1));
     const T* x = static_cast<const T*>(a.x) + r * a.stride;
     const int warps = teacher_warps(t);
     const bool teaches = part == 0 && (int)threadIdx.x < warps * 32;
-    // (the teacher's side while the row's first vectors are on their way)
+    TeacherRow teacher{0.f, 0.f, 0.f};   // (while the row's first vectors are on their way)
     RowSums s = go_along<T, THREADS, 1, false, EDGES>(x, a.classes, a.scale2, part, parts_log2, 0, &sh, ring, [&] {
-        if (teaches) teacher_row(t, r, x, a.classes, a.scale, warps, sh.scratch, log_q, at_class, nullptr, [](int32_t) { return true; });
+        if (teaches) teacher = teacher_row(t, r, x, a.classes, a.scale, warps, sh.scratch, above, at_class, nullptr, [](int32_t) { return true; });
     });
     if (parts > 1) s = over_cluster<false>(s, parts, a.scale2, &sh);
     if (teaches) {
         const RowResult res(s, a.scale);
         float v = 0.f;
         for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
-            const float q = fast_exp2(log_q[k] * kLog2e);
-            if (q != 0.f) v = fmaf(q, log_q[k] - res.log_p(at_class[k]), v);
+            const float q = expf(above[k]) * teacher.part;
+            if (q != 0.f) v = fmaf(q, (above[k] - teacher.log_sum) - res.log_p(at_class[k]), v);
         }
         v = over_warps(v, warps, sh.scratch, [](float a, float b) { return a + b; });
         if (threadIdx.x == 0) {

@@ -62,22 +62,19 @@ void launch_sort(mg_ctx* ctx, const GroupPlan& p, const void* ids, int ids_are_i
     SortShared* s = reinterpret_cast<SortShared*>(ws);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(ws + p.at_keys[0]), reinterpret_cast<uint32_t*>(ws + p.at_keys[1])};
     int32_t* spare = reinterpret_cast<int32_t*>(ws + p.at_order);
-    const unsigned tiles = (unsigned)std::max<int64_t>(p.tiles, 1);
+    const unsigned tiles = (unsigned)p.tiles;
     int at = 0;
-    if (n > 0) {
-        k_sort_hist<<<(unsigned)std::min<int64_t>((n + kSortThreads - 1) / kSortThreads, mg_grid(ctx, 4)), kSortThreads, 0, st>>>(ids, ids_are_i64, n, none, p.passes, p.bits, s);
-        // (the last pass ends in the caller's array)
-        int32_t* by[2] = {p.passes % 2 ? spare : order, p.passes % 2 ? order : spare};
-        for (int pass = 0; pass < p.passes; ++pass, at ^= 1) {
-            uint64_t* states = reinterpret_cast<uint64_t*>(ws + p.at_states) + (size_t)pass * p.tiles * kSortBins;
-            mgnorm::launch_chained(dim3(tiles), kSortThreads, st, pass ? k_sort_pass<PER, false> : k_sort_pass<PER, true>, ids, ids_are_i64, (const uint32_t*)keys[at], (const int32_t*)by[at], n, none, pass,
-                                   p.bits, s, states, keys[at ^ 1], by[at ^ 1], kSortPolls);
-        }
-        ctx->launches += 1 + p.passes;
+    k_sort_hist<<<(unsigned)std::min<int64_t>((n + kSortThreads - 1) / kSortThreads, mg_grid(ctx, 4)), kSortThreads, 0, st>>>(ids, ids_are_i64, n, none, p.passes, p.bits, s);
+    // (the last pass ends in the caller's array)
+    int32_t* by[2] = {p.passes % 2 ? spare : order, p.passes % 2 ? order : spare};
+    for (int pass = 0; pass < p.passes; ++pass, at ^= 1) {
+        uint64_t* states = reinterpret_cast<uint64_t*>(ws + p.at_states) + (size_t)pass * p.tiles * kSortBins;
+        mgnorm::launch_chained(dim3(tiles), kSortThreads, st, pass ? k_sort_pass<PER, false> : k_sort_pass<PER, true>, ids, ids_are_i64, (const uint32_t*)keys[at], (const int32_t*)by[at], n, none, pass,
+                               p.bits, s, states, keys[at ^ 1], by[at ^ 1], kSortPolls);
     }
     mgnorm::launch_chained(dim3(tiles), kSortThreads, st, k_sort_groups<PER>, (const uint32_t*)keys[at], n, none, s, reinterpret_cast<uint64_t*>(ws + p.at_chain), ids_are_i64, group_ids, starts, group_of,
                            n_groups, kSortPolls);
-    ctx->launches++;
+    ctx->launches += 2 + p.passes;
 }
 
 int pow2_up(int64_t v) { int p = 1; while (p < v) p *= 2; return p; }
@@ -146,6 +143,12 @@ extern "C" int mg_id_groups(mg_ctx* ctx, const void* ids, int ids_are_i64, int64
     MG_CUDA(ctx, on.err);
     const cudaStream_t st = (cudaStream_t)stream;
     const GroupPlan p = plan_groups(n, n_rows, ctx->n_sms);
+    if (!p.passes) {
+        k_sort_small<<<1, kSmallThreads, 0, st>>>(ids, ids_are_i64, (int32_t)n, (uint32_t)n_rows, order, group_of, group_ids, starts, n_groups);
+        ctx->launches++;
+        MG_CUDA(ctx, cudaGetLastError());
+        return MG_OK;
+    }
     char* ws = static_cast<char*>(workspace);
     MG_CUDA(ctx, cudaMemsetAsync(ws, 0, p.cleared, st));
     (p.per == 4 ? launch_sort<4> : p.per == 8 ? launch_sort<8> : launch_sort<16>)(ctx, p, ids, ids_are_i64, n, n_rows, order, group_of, group_ids, starts, n_groups, ws, st);
@@ -177,8 +180,9 @@ extern "C" int mg_embedding_backward(mg_ctx* ctx, const void* d_y, int64_t d_y_s
                     reinterpret_cast<float*>(ws), p.pitch, reinterpret_cast<int32_t*>(ws + p.at_begun)};
     if (into == MG_ROWS_TABLE && n_rows > 0) {
         const int vec = row_vec(out, out_stride, out_dtype, n_rows, out, out_stride, out_dtype, n_rows, dim);
-        // (rows to a block: 128 KB of them)
-        const int rows = (int)std::min<int64_t>(std::max<int64_t>((128 << 10) / ((int64_t)dim * elem_size(out_dtype)), 32) / 32 * 32, kMostZeroRows);
+        // (rows to a block: 128 KB of them, fewer where blocks would be fewer than four to a multiprocessor, 32 at least)
+        const int64_t much = (128 << 10) / ((int64_t)dim * elem_size(out_dtype)), few = (n_rows + mg_grid(ctx, 4) - 1) / mg_grid(ctx, 4);
+        const int rows = (int)std::min<int64_t>(std::max<int64_t>(std::min(much, few), 32) / 32 * 32, kMostZeroRows);
         const dim3 grid((unsigned)((n_rows + rows - 1) / rows));
         MG_BY_TYPE(out_dtype, (vec > 1 ? mgnorm::launch_chained(grid, kSumThreads, st, k_zero_others<T, 16 / (int)sizeof(T)>, a, rows) : mgnorm::launch_chained(grid, kSumThreads, st, k_zero_others<T, 1>, a, rows)));
         ctx->launches++;

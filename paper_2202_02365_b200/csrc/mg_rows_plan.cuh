@@ -9,7 +9,7 @@
 
 namespace {
 
-constexpr int kPlanBits = 8, kPlanBins = 1 << kPlanBits, kPlanThreads = 256;   // of the sort
+constexpr int kPlanBits = 8, kPlanBins = 1 << kPlanBits, kPlanThreads = 256, kPlanSmall = 4096;   // of the sort; ids that one block sorts
 
 inline size_t rows_align(size_t bytes) { return (bytes + 15) / 16 * 16; }
 
@@ -54,6 +54,7 @@ constexpr size_t kSortSharedBytes = 4 * (4 * kPlanBins + 8);
 // keys are 0 .. n_rows; n_rows stands for an id that is no row
 inline GroupPlan plan_groups(int64_t n, int64_t n_rows, int n_sms = 148) {
     GroupPlan p;
+    if (n <= kPlanSmall) return p;   // (one block, no workspace)
     int bits = 1;
     while (bits < 31 && n_rows >> bits) ++bits;
     p.passes = (bits + kPlanBits - 1) / kPlanBits;
@@ -93,14 +94,15 @@ struct SumPlan {
     size_t at_begun = 0, bytes = 0;
 };
 
-// Places to a chunk: two times the 768 threads that a multiprocessor holds are to have one, of 32 places at least, and no id is to leave more than 8,192 shares.
+// Places to a chunk: two times the 768 threads that a multiprocessor holds are to have one, of 16 places at least, and no id is to leave more than 8,192 shares.  (Threads as for
+// accesses of 16 bytes, of two-byte types where rows are wide.)
 inline SumPlan plan_sums(int64_t n, int64_t n_rows, int32_t dim, int n_sms = 148) {
     SumPlan p;
     p.pitch = (dim + 7) / 8 * 8;
     if (n == 0 || n_rows == 0) return p;
-    const int64_t lanes = dim >= 128 ? (dim + 127) / 128 * 32 : dim > 64 ? 32 : dim > 32 ? 16 : dim > 16 ? 8 : 4;
+    const int64_t lanes = dim >= 256 ? (dim + 255) / 256 * 32 : dim > 64 ? 32 : dim > 32 ? 16 : dim > 16 ? 8 : 4;
     const int64_t threads = (int64_t)n_sms * 1536;
-    p.chunk = (int32_t)std::max<int64_t>({(n * lanes + threads - 1) / threads, n / 8192, 32});
+    p.chunk = (int32_t)std::max<int64_t>({(n * lanes + threads - 1) / threads, n / 8192, 16});
     p.chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
     p.at_begun = rows_align(8 * (size_t)p.chunks * p.pitch);
     p.bytes = p.at_begun + rows_align(4 * (size_t)p.chunks);

@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_cons
     int32_t place = -1, group = -1, next_place = -1, next_group = -1;   // of the lane, in this batch of `lanes` places and the next
     int32_t first = -1, came = -1, last = -1;                            // groups: of the first place, of the one before, of the last
     if (some) {
-        if (lo + sub < hi) { place = a.order[lo + sub]; group = group_at(lo + sub); }
+        if (lo + sub < a.n) { place = a.order[lo + sub]; group = group_at(lo + sub); }
         first = group_at(lo); last = group_at(hi - 1);
         if (lo > 0) came = group_at(lo - 1);
     }
@@ -153,52 +153,69 @@ __global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_cons
     flush();
 }
 
-// The shares of the ids that begin in a chunk and go on behind it: a block looks at every gridDim.x-th chunk; 32 lanes of four columns, 32 warps that each take a stretch of the
-// chunks that an id spans.
+// The shares of the ids that begin in a chunk and go on behind it: a block looks at every gridDim.x-th chunk; 32 lanes of four columns.  Up to 32 shares are added up by a warp, more
+// by 32 warps that each take a stretch of the chunks that the id spans.
+constexpr int kWarpShares = 32;
+struct Spanned { int32_t chunk, shares, row; };   // the chunk that the id begins in
+__device__ __forceinline__ Spanned spanned(const SumArgs& a, int32_t chunk) {
+    const int32_t g = a.begun[chunk];
+    const int64_t end = min((int64_t)a.starts[g + 1], a.n), row = a.into == MG_ROWS_COMPACT ? g : id_at(a.group_ids, a.ids_are_i64, g);
+    return {chunk, min((int32_t)((end - 1) / a.chunk), a.chunks - 1) - chunk + 1, row < a.n_rows ? (int32_t)row : -1};
+}
+__device__ __forceinline__ float4 add_shares(const SumArgs& a, int32_t chunk, int32_t lo, int32_t hi, int32_t c) {
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c >= a.dim) return s;
+    constexpr int U = 8;
+    for (int32_t i0 = lo; i0 < hi; i0 += U) {
+        float4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)   // (the first chunk's is the share of an id that begins there)
+            v[u] = i0 + u < hi ? *reinterpret_cast<const float4*>(a.shares + ((int64_t)(chunk + i0 + u) * 2 + (i0 + u == 0)) * a.pitch + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int u = 0; u < U; ++u) { s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w; }
+    }
+    return s;
+}
+template <typename O>
+__device__ __forceinline__ void write_joined(const SumArgs& a, int64_t row, int32_t c, const float4& s) {
+    if (row < 0) return;
+    const float all[4] = {s.x, s.y, s.z, s.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < a.dim) {
+            float one[1] = {all[e]};
+            write_sum<O, 1>(a, row, c + e, one);
+        }
+}
 template <typename O>
 __global__ void __launch_bounds__(kJoinThreads) k_join_shares(const __grid_constant__ SumArgs a) {
     constexpr int W = kJoinThreads / 32;
     __shared__ float4 part[W][32];
-    __shared__ int32_t found[kJoinThreads], n_found;
+    __shared__ Spanned few[kJoinThreads], many[kJoinThreads];   // (their order does not matter: each id's sum is its own)
+    __shared__ int32_t n_few, n_many;
     chain_wait();
     chain_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t c = ((int32_t)blockIdx.y * 32 + lane) * 4;
     for (int32_t c0 = (int32_t)blockIdx.x; c0 < a.chunks; c0 += (int32_t)gridDim.x * kJoinThreads) {
-        if (threadIdx.x == 0) n_found = 0;
+        if (threadIdx.x == 0) n_few = n_many = 0;
         __syncthreads();
         const int64_t mine = c0 + (int64_t)threadIdx.x * gridDim.x;
-        if (mine < a.chunks && a.begun[mine] >= 0) found[atomicAdd(&n_found, 1)] = (int32_t)mine;   // (their order does not matter: each id's sum is its own)
+        if (mine < a.chunks && a.begun[mine] >= 0) {
+            const Spanned s = spanned(a, (int32_t)mine);
+            if (s.shares <= kWarpShares) few[atomicAdd(&n_few, 1)] = s;
+            else many[atomicAdd(&n_many, 1)] = s;
+        }
         __syncthreads();
-        for (int f = 0; f < n_found; ++f) {
-            const int32_t chunk = found[f], g = a.begun[chunk];
-            const int64_t end = min((int64_t)a.starts[g + 1], a.n);
-            const int32_t last = min((int32_t)((end - 1) / a.chunk), a.chunks - 1), shares = last - chunk + 1;
-            const int32_t lo = (int32_t)((int64_t)shares * warp / W), hi = (int32_t)((int64_t)shares * (warp + 1) / W);
-            float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (c < a.dim) {
-                constexpr int U = 4;
-                for (int32_t i0 = lo; i0 < hi; i0 += U) {
-                    float4 v[U];
-#pragma unroll
-                    for (int u = 0; u < U; ++u)   // (the first chunk's is the share of an id that begins there)
-                        v[u] = i0 + u < hi ? *reinterpret_cast<const float4*>(a.shares + ((int64_t)(chunk + i0 + u) * 2 + (i0 + u == 0)) * a.pitch + c) : make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int u = 0; u < U; ++u) { s.x += v[u].x; s.y += v[u].y; s.z += v[u].z; s.w += v[u].w; }
-                }
-            }
-            part[warp][lane] = s;
+        for (int f = warp; f < n_few; f += W) write_joined<O>(a, few[f].row, c, add_shares(a, few[f].chunk, 0, few[f].shares, c));
+        for (int f = 0; f < n_many; ++f) {
+            const Spanned s = many[f];
+            part[warp][lane] = add_shares(a, s.chunk, (int32_t)((int64_t)s.shares * warp / W), (int32_t)((int64_t)s.shares * (warp + 1) / W), c);
             __syncthreads();
-            const int64_t row = a.into == MG_ROWS_COMPACT ? g : id_at(a.group_ids, a.ids_are_i64, g);
-            if (warp == 0 && c < a.dim && row >= 0 && row < a.n_rows) {
-                for (int w = 1; w < W; ++w) { const float4 o = part[w][lane]; s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w; }
-                const float all[4] = {s.x, s.y, s.z, s.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (c + e < a.dim) {
-                        float one[1] = {all[e]};
-                        write_sum<O, 1>(a, row, c + e, one);
-                    }
+            if (warp == 0) {
+                float4 t = part[0][lane];
+                for (int w = 1; w < W; ++w) { const float4 o = part[w][lane]; t.x += o.x; t.y += o.y; t.z += o.z; t.w += o.w; }
+                write_joined<O>(a, s.row, c, t);
             }
             __syncthreads();
         }

@@ -379,7 +379,8 @@ int main() {
     for (const float s : {(float)NAN, (float)INFINITY}) EXPECT(MG_ERR_ARG, lookup([&](L& a) { a.scale = s; }));
 
     struct G { const void* ids; int wide; int64_t n, rows; const void *order, *of, *gids, *starts, *count, *ws; size_t bytes; };
-    const G good{ids, 0, 1000, 500, base, base + 8000, far, far + 8000, far + 16000, more, 1 << 30};
+    const G good{ids, 0, 10000, 500, base, base + 80000, far, far + 8000, far + 16000, more, 1 << 30};
+    if (plan_groups(4096, 500).bytes || !plan_groups(4097, 500).bytes) { printf("small\n"); ++bad; }
     const auto groups = [&](auto change) { G a = good; change(a); return check_groups(&context, a.ids, a.wide, a.n, a.rows, a.order, a.of, a.gids, a.starts, a.count, a.ws, a.bytes); };
     EXPECT(MG_OK, groups([](G&) {}));
     EXPECT(MG_OK, groups([](G& a) { a.bytes = plan_groups(a.n, a.rows).bytes; }));
