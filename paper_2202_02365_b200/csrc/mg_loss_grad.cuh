@@ -145,38 +145,38 @@ __global__ void __launch_bounds__(kGradThreads) k_scores_grad(const __grid_const
 struct FlatRow { float minus_lse, base, slope; int32_t zero; };
 constexpr int kFlatRows = 256;   // a block's, at most
 template <typename T, bool CROSS>
-__global__ void __launch_bounds__(kGradThreads) k_scores_grad_flat(const __grid_constant__ GradArgs a, int rows_each, uint32_t reciprocal) {
+__global__ void __launch_bounds__(kGradThreads, 4) k_scores_grad_flat(const __grid_constant__ GradArgs a, int rows_each, uint32_t reciprocal) {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ FlatRow params[kFlatRows + 1];
     const int64_t r0 = (int64_t)blockIdx.x * rows_each;
     const int rows = (int)min((int64_t)rows_each, a.rows - r0);
     const T* x = static_cast<const T*>(a.x) + r0 * a.classes;
     T* d = static_cast<T*>(a.d) + r0 * a.classes;
+    const int32_t values = rows * a.classes, vecs = values / VEC;
+    uint4 raw[kGradBatch];   // on their way while the rows' values are worked out
+#pragma unroll
+    for (int j = 0; j < kGradBatch; ++j)
+        if ((int)threadIdx.x + j * kGradThreads < vecs) raw[j] = reinterpret_cast<const uint4*>(x)[threadIdx.x + j * kGradThreads];
     int32_t label = -1;
     float x_label = 0.f, more = 0.f;
     RowGrad own{a.scale, 0.f, 0.f, 0.f};
     if ((int)threadIdx.x < rows) {
         const int64_t r = r0 + threadIdx.x;
-        const float lse = a.lse[r];
+        const float lse = a.lse[r], of_label = a.d_log_prob ? a.d_log_prob[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f, l = a.d_lse ? a.d_lse[r] : 0.f;
+        const float entropy = a.d_entropy ? a.entropy[r] : 0.f;
         if (a.d_log_prob) label = class_at(a.labels, a.labels_are_i64, r, a.classes);
-        const float g = label >= 0 ? a.d_log_prob[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f, l = a.d_lse ? a.d_lse[r] : 0.f;
-        const float entropy = h != 0.f ? a.entropy[r] : 0.f;
+        if (label >= 0) x_label = to_float(x[(int64_t)threadIdx.x * a.classes + label]);
+        const float g = label >= 0 ? of_label : 0.f;
         const bool zero = (g == 0.f && h == 0.f && l == 0.f) || lse == kNegInf;
-        own.minus_lse = -lse; own.base = a.scale * (l - g - h * entropy); own.slope = -a.scale * h;
+        own.minus_lse = -lse; own.base = a.scale * (l - g - (h != 0.f ? h * entropy : 0.f)); own.slope = -a.scale * h;
         more = a.scale * g;
         if (zero) label = -1;
-        if (label >= 0) x_label = to_float(x[(int64_t)threadIdx.x * a.classes + label]);
         params[threadIdx.x] = {own.minus_lse, own.base, own.slope, zero};
     }
     __syncthreads();
     const bool sloped = a.d_entropy != nullptr;
     const Pair scale = pair(a.scale, a.scale);
-    const int32_t values = rows * a.classes, vecs = values / VEC;
     for (int32_t v0 = threadIdx.x; v0 < vecs; v0 += kGradBatch * kGradThreads) {
-        uint4 raw[kGradBatch];
-#pragma unroll
-        for (int j = 0; j < kGradBatch; ++j)
-            if (v0 + j * kGradThreads < vecs) raw[j] = reinterpret_cast<const uint4*>(x)[v0 + j * kGradThreads];
 #pragma unroll
         for (int j = 0; j < kGradBatch; ++j) {
             const int32_t v = v0 + j * kGradThreads;
@@ -187,6 +187,7 @@ __global__ void __launch_bounds__(kGradThreads) k_scores_grad_flat(const __grid_
             if (CROSS && left < VEC) q = params[row + 1];   // (there is one: the block's values end behind the vector)
             Raw<T, VEC> one;
             one.w[0] = raw[j].x; one.w[1] = raw[j].y; one.w[2] = raw[j].z; one.w[3] = raw[j].w;
+            if (v + kGradBatch * kGradThreads < vecs) raw[j] = reinterpret_cast<const uint4*>(x)[v + kGradBatch * kGradThreads];
             float f[VEC];
 #pragma unroll
             for (int e = 0; e < VEC; e += 2) {

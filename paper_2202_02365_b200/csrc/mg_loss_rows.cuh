@@ -128,7 +128,7 @@ __device__ __forceinline__ void best_of(const HeldRow<T, NV, LANES, WHOLE>& row,
 }
 
 // (blocks to an SM: what the values to a lane leave registers for)
-constexpr int row_blocks(int values) { return values <= 8 ? 5 : values <= 16 ? 4 : 3; }
+constexpr int row_blocks(int values) { return values <= 8 ? 5 : values <= 24 ? 4 : 3; }
 
 template <typename T, int NV, int LANES, bool WHOLE>
 __global__ void __launch_bounds__(kRowThreads, row_blocks(NV * 16 / sizeof(T))) k_scores_rows(const __grid_constant__ ScoreArgs a) {
