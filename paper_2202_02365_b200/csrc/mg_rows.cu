@@ -151,7 +151,7 @@ extern "C" int mg_id_groups(mg_ctx* ctx, const void* ids, int ids_are_i64, int64
     }
     char* ws = static_cast<char*>(workspace);
     MG_CUDA(ctx, cudaMemsetAsync(ws, 0, p.cleared, st));
-    (p.per == 4 ? launch_sort<4> : p.per == 8 ? launch_sort<8> : launch_sort<16>)(ctx, p, ids, ids_are_i64, n, n_rows, order, group_of, group_ids, starts, n_groups, ws, st);
+    (p.per == 4 ? launch_sort<4> : launch_sort<8>)(ctx, p, ids, ids_are_i64, n, n_rows, order, group_of, group_ids, starts, n_groups, ws, st);
     MG_CUDA(ctx, cudaGetLastError());
     return MG_OK;
 }

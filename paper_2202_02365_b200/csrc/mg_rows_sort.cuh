@@ -67,8 +67,8 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_hist(const void* ids, int
 // One digit's pass: a tile's keys are ranked by digit, warp by warp and 32 at a time, laid out digit by digit in shared memory and written from there.  Where a digit's
 // keys of this tile begin is the digit's first place, and what the tiles before it have of the digit: a word per tile and digit says the tile's own number, or that
 // of all tiles up to it.  Tiles come from a counter, so those before are in running blocks and every wait ends; it is bounded all the same.
+// (One word at a time: four at once, of which the later ones are mostly not there yet, took 38 us in the place of 35 for all the kernels of 150,001 ids, sixteen 57.)
 constexpr uint64_t kOwn = 1ull << 32, kTotal = 2ull << 32;
-constexpr int kLookAhead = 4;
 
 template <int PER, bool FIRST>
 __global__ void __launch_bounds__(kSortThreads) k_sort_pass(const void* ids, int ids_are_i64, const uint32_t* keys, const int32_t* places, int64_t n, uint32_t none, int pass, int bits,
@@ -127,21 +127,17 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_pass(const void* ids, int
     uint32_t in_tile = inc - own, before = 0;
     int64_t first = (int64_t)(all_inc - all);
     for (int w = 0; w < warp; ++w) { in_tile += warp_tot[w]; first += warp_all[w]; }
-    int64_t back = tile - 1;
-    for (int polls = 0; back >= 0 && polls < max_polls; ++polls) {
-        uint64_t v[kLookAhead];
-#pragma unroll
-        for (int k = 0; k < kLookAhead; ++k) v[k] = back >= k ? state[(back - k) * kSortBins] : uint64_t(kTotal);
-        bool told = true;
-        const int64_t from = back;
-#pragma unroll
-        for (int k = 0; k < kLookAhead; ++k) {
-            told = told && v[k] >> 32 != 0;
-            if (told) { before += (uint32_t)v[k]; back = v[k] & kTotal ? -1 : from - k - 1; told = back >= 0; }
-        }
-        if (back != from) polls = 0;
+    bool known = tile == 0;
+    int polls = 0;
+    for (int64_t back = tile - 1; !known && polls < max_polls;) {
+        const uint64_t told = state[back * kSortBins];
+        if (!(told >> 32)) { ++polls; continue; }
+        before += (uint32_t)told;
+        known = (told & kTotal) != 0;   // (tile 0 says so)
+        --back;
+        polls = 0;
     }
-    if (back >= 0) atomicExch(&s->failed, 1u);
+    if (!known) atomicExch(&s->failed, 1u);
     if (tile > 0) state[tile * kSortBins] = kTotal | (uint64_t)(before + own);
     first += before;
     tile_base[threadIdx.x] = in_tile;
