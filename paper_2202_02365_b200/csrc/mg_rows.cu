@@ -96,11 +96,12 @@ void launch_lookup(const LookupArgs& a, int vec, unsigned grid, cudaStream_t st)
 }
 
 template <typename T, typename O>
-void launch_sums(const SumArgs& a, int vec, cudaStream_t st) {
+void launch_sums(SumArgs a, int vec, int64_t zero_blocks, cudaStream_t st) {
     constexpr int WIDE = sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4;
     const int lanes = std::min(32, std::max(4, pow2_up((a.dim + (vec > 1 ? vec : 4) - 1) / (vec > 1 ? vec : 4))));
     const int columns = lanes * (vec > 1 ? vec : 4);
-    const dim3 grid((unsigned)(((int64_t)a.chunks * lanes + kSumThreads - 1) / kSumThreads), (unsigned)((a.dim + columns - 1) / columns));
+    a.chunk_blocks = (int32_t)(((int64_t)a.chunks * lanes + kSumThreads - 1) / kSumThreads);
+    const dim3 grid((unsigned)(a.chunk_blocks + zero_blocks), (unsigned)((a.dim + columns - 1) / columns));
     if (vec > 1) mgnorm::launch_chained(grid, kSumThreads, st, k_chunk_sums<T, O, WIDE, 1, 4>, a, lanes);
     else mgnorm::launch_chained(grid, kSumThreads, st, k_chunk_sums<T, O, 1, 4, 2>, a, lanes);
 }
@@ -176,20 +177,21 @@ extern "C" int mg_embedding_backward(mg_ctx* ctx, const void* d_y, int64_t d_y_s
     const cudaStream_t st = (cudaStream_t)stream;
     const SumPlan p = plan_sums(n, n_rows, dim, ctx->n_sms);
     char* ws = static_cast<char*>(workspace);
+    // (rows to a block that writes zeros: 128 KB of them, fewer where blocks would be fewer than four to a multiprocessor, 32 at least)
+    const int64_t much = (128 << 10) / ((int64_t)dim * elem_size(out_dtype)), few = (n_rows + mg_grid(ctx, 4) - 1) / mg_grid(ctx, 4);
+    const int zero_rows = (int)std::min<int64_t>(std::max<int64_t>(std::min(much, few), 32) / 32 * 32, kMostZeroRows);
     const SumArgs a{d_y, d_y_stride, n, n_rows, dim, scale, order, group_of, starts, n_groups, group_ids, ids_are_i64, into, out, out_stride, p.chunk, p.chunks,
-                    reinterpret_cast<float*>(ws), p.pitch, reinterpret_cast<int32_t*>(ws + p.at_begun)};
-    if (into == MG_ROWS_TABLE && n_rows > 0) {
-        const int vec = row_vec(out, out_stride, out_dtype, n_rows, out, out_stride, out_dtype, n_rows, dim);
-        // (rows to a block: 128 KB of them, fewer where blocks would be fewer than four to a multiprocessor, 32 at least)
-        const int64_t much = (128 << 10) / ((int64_t)dim * elem_size(out_dtype)), few = (n_rows + mg_grid(ctx, 4) - 1) / mg_grid(ctx, 4);
-        const int rows = (int)std::min<int64_t>(std::max<int64_t>(std::min(much, few), 32) / 32 * 32, kMostZeroRows);
-        const dim3 grid((unsigned)((n_rows + rows - 1) / rows));
-        MG_BY_TYPE(out_dtype, (vec > 1 ? mgnorm::launch_chained(grid, kSumThreads, st, k_zero_others<T, 16 / (int)sizeof(T)>, a, rows) : mgnorm::launch_chained(grid, kSumThreads, st, k_zero_others<T, 1>, a, rows)));
+                    reinterpret_cast<float*>(ws), p.pitch, reinterpret_cast<int32_t*>(ws + p.at_begun), 0, zero_rows,
+                    row_vec(out, out_stride, out_dtype, n_rows, out, out_stride, out_dtype, n_rows, dim) == 16 / elem_size(out_dtype)};
+    int64_t zero_blocks = into == MG_ROWS_TABLE ? (n_rows + zero_rows - 1) / zero_rows : 0;
+    if (zero_blocks && (!p.chunks || n_rows * dim * elem_size(out_dtype) > 32ll << 20)) {
+        MG_BY_TYPE(out_dtype, mgnorm::launch_chained(dim3((unsigned)zero_blocks), kSumThreads, st, k_zero_others<T>, a));
         ctx->launches++;
+        zero_blocks = 0;
     }
     if (p.chunks > 0) {
         const int vec = row_vec(d_y, d_y_stride, d_y_dtype, n, out, out_stride, out_dtype, n_rows, dim);
-        MG_BY_TYPE(d_y_dtype, using From = T; MG_BY_TYPE(out_dtype, (launch_sums<From, T>(a, vec, st))));
+        MG_BY_TYPE(d_y_dtype, using From = T; MG_BY_TYPE(out_dtype, (launch_sums<From, T>(a, vec, zero_blocks, st))));
         MG_BY_TYPE(out_dtype, mgnorm::launch_chained(dim3((unsigned)std::min(p.chunks, mg_grid(ctx, 1)), (unsigned)((dim + 127) / 128)), kJoinThreads, st, k_join_shares<T>, a));
         ctx->launches += 2;
     }

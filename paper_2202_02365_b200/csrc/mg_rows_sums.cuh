@@ -21,6 +21,8 @@ struct SumArgs {
     int32_t chunk, chunks;        // places to a chunk
     float* shares; int32_t pitch; // [chunks][2][pitch]: of the id that the chunk begins within, of the one that goes on behind it
     int32_t* begun;               // [chunks]: the group that begins in the chunk and has shares, -1
+    int32_t chunk_blocks, zero_rows;   // blocks of the sums; rows to a block of those that write zeros
+    bool zero_wide;               // ... 16 bytes at a time
 };
 
 template <typename O, int VEC>
@@ -39,12 +41,68 @@ __device__ __forceinline__ void write_sum(const SumArgs& a, int64_t row, int32_t
     raw.store(to);
 }
 
+// Zeros into the rows of the table that no id names: a block finds the named ones among its rows, marks them in shared memory and writes the others.  Tables of up to 32 MB by blocks
+// behind those of the sums, in one launch (14,824 rows of 100: 49 us, by a kernel of its own 53); larger ones by the kernel of its own, of which an SM holds more blocks
+// (300,007 bf16 rows of 768: 199 us, with the sums 217).
+constexpr int kMostZeroRows = 2048;
+template <typename O>
+__device__ __forceinline__ void zero_others(const SumArgs& a, int64_t block) {
+    __shared__ uint32_t named[kMostZeroRows / 32];
+    __shared__ int64_t sh_first;
+    const int64_t r0 = block * a.zero_rows, r1 = min(r0 + a.zero_rows, a.n_rows);
+    const int64_t groups = max((int64_t)0, min((int64_t)*a.n_groups, min(a.n, a.n_rows)));
+    if (threadIdx.x < kMostZeroRows / 32) named[threadIdx.x] = 0;
+    if (threadIdx.x < 32) {
+        // the first group whose id is r0 or more, 32 probes at a time
+        int64_t lo = 0, hi = groups;
+        while (lo < hi) {
+            const int64_t step = (hi - lo + 31) / 32, at = lo + step * threadIdx.x;
+            const uint32_t below = __ballot_sync(0xFFFFFFFFu, at < hi && id_at(a.group_ids, a.ids_are_i64, at) < r0);
+            const int k = __popc(below);   // the probes up to it lie below
+            hi = min(hi, k < 32 ? lo + step * k : hi);
+            lo = k ? lo + step * (k - 1) + 1 : lo;
+            if (k == 0) hi = lo;
+        }
+        if (threadIdx.x == 0) sh_first = lo;
+    }
+    __syncthreads();
+    for (int64_t g = sh_first + threadIdx.x; g < min(groups, sh_first + a.zero_rows); g += kSumThreads) {
+        const int64_t id = id_at(a.group_ids, a.ids_are_i64, g);
+        if (id >= r0 && id < r1) atomicOr(&named[(id - r0) >> 5], 1u << ((id - r0) & 31));
+    }
+    __syncthreads();
+    const auto write = [&](auto zero, int width) {
+        zero.zero();
+        const int vecs = a.dim / width, lanes = min(kSumThreads, 1 << (31 - __clz(vecs)));
+        const int sub = (int)threadIdx.x & (lanes - 1);
+        for (int64_t r = r0 + threadIdx.x / lanes; r < r1; r += kSumThreads / lanes) {
+            if (named[(r - r0) >> 5] >> ((r - r0) & 31) & 1) continue;
+            O* to = static_cast<O*>(a.out) + r * a.out_stride;
+            for (int v = sub; v < vecs; v += lanes) zero.store(to + v * width);
+        }
+    };
+    constexpr int VEC = 16 / sizeof(O);
+    if (a.zero_wide) write(Raw<O, VEC>(), VEC);
+    else write(Raw<O, 1>(), 1);
+}
+
+template <typename O>
+__global__ void __launch_bounds__(kSumThreads) k_zero_others(const __grid_constant__ SumArgs a) {
+    chain_wait();
+    chain_start();
+    zero_others<O>(a, blockIdx.x);
+}
+
 // `lanes` lanes to a chunk, NV vectors of its rows to a lane, U rows on their way while U others are added up; blockIdx.y: which of the rows' columns.
 // What a chunk has to know of its neighbours is asked for beside its first places, and of its first and last ids beside its first rows.
 template <typename T, typename O, int VEC, int NV, int U>
 __global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_constant__ SumArgs a, int lanes) {
     chain_wait();
     chain_start();
+    if ((int32_t)blockIdx.x >= a.chunk_blocks) {
+        if (blockIdx.y == 0) zero_others<O>(a, (int64_t)blockIdx.x - a.chunk_blocks);
+        return;
+    }
     const int sub = (int)threadIdx.x & (lanes - 1);
     const int32_t chunk = (int32_t)((blockIdx.x * (int64_t)kSumThreads + threadIdx.x) / lanes);
     const int32_t c0 = ((int32_t)blockIdx.y * NV * lanes + sub) * VEC, step = lanes * VEC;
@@ -219,47 +277,6 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_shares(const __grid_const
             }
             __syncthreads();
         }
-    }
-}
-
-// Zeros into the rows of the table that no id names: a block finds the named ones among its rows, marks them in shared memory and writes the others.
-constexpr int kMostZeroRows = 2048;
-template <typename O, int VEC>
-__global__ void __launch_bounds__(kSumThreads) k_zero_others(const __grid_constant__ SumArgs a, int zero_rows) {
-    __shared__ uint32_t named[kMostZeroRows / 32];
-    __shared__ int64_t sh_first;
-    chain_wait();
-    chain_start();
-    const int64_t r0 = (int64_t)blockIdx.x * zero_rows, r1 = min(r0 + zero_rows, a.n_rows);
-    const int64_t groups = max((int64_t)0, min((int64_t)*a.n_groups, min(a.n, a.n_rows)));
-    if (threadIdx.x < kMostZeroRows / 32) named[threadIdx.x] = 0;
-    if (threadIdx.x < 32) {
-        // the first group whose id is r0 or more, 32 probes at a time
-        int64_t lo = 0, hi = groups;
-        while (lo < hi) {
-            const int64_t step = (hi - lo + 31) / 32, at = lo + step * threadIdx.x;
-            const uint32_t below = __ballot_sync(0xFFFFFFFFu, at < hi && id_at(a.group_ids, a.ids_are_i64, at) < r0);
-            const int k = __popc(below);   // the probes up to it lie below
-            hi = min(hi, k < 32 ? lo + step * k : hi);
-            lo = k ? lo + step * (k - 1) + 1 : lo;
-            if (k == 0) hi = lo;
-        }
-        if (threadIdx.x == 0) sh_first = lo;
-    }
-    __syncthreads();
-    for (int64_t g = sh_first + threadIdx.x; g < min(groups, sh_first + zero_rows); g += kSumThreads) {
-        const int64_t id = id_at(a.group_ids, a.ids_are_i64, g);
-        if (id >= r0 && id < r1) atomicOr(&named[(id - r0) >> 5], 1u << ((id - r0) & 31));
-    }
-    __syncthreads();
-    Raw<O, VEC> zero;
-    zero.zero();
-    const int vecs = a.dim / VEC, lanes = min(kSumThreads, max(1, 1 << (31 - __clz(max(vecs, 1)))));
-    const int sub = (int)threadIdx.x & (lanes - 1);
-    for (int64_t r = r0 + threadIdx.x / lanes; r < r1; r += kSumThreads / lanes) {
-        if (named[(r - r0) >> 5] >> ((r - r0) & 31) & 1) continue;
-        O* to = static_cast<O*>(a.out) + r * a.out_stride;
-        for (int v = sub; v < vecs; v += lanes) zero.store(to + v * VEC);
     }
 }
 
