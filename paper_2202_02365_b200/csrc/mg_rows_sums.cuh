@@ -119,13 +119,15 @@ __global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_cons
         first = group_at(lo); last = group_at(hi - 1);
         if (lo > 0) came = group_at(lo - 1);
     }
+    const uint32_t from_stride = (uint32_t)(a.d_y_stride * (int64_t)sizeof(T));   // (below 2^31)
     const auto load = [&](Raw<T, VEC> (&raw)[U][NV], int32_t of, int at) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int32_t i = __shfl_sync(peers, of, (at + u) & (lanes - 1), lanes);
+            const T* const row = reinterpret_cast<const T*>(static_cast<const char*>(a.d_y) + (uint64_t)(uint32_t)i * from_stride) + c0;
 #pragma unroll
             for (int v = 0; v < NV; ++v) {
-                if (i >= 0 && i < a.n && c0 + v * step < a.dim) raw[u][v].load(static_cast<const T*>(a.d_y) + i * a.d_y_stride + c0 + v * step);
+                if ((uint32_t)i < (uint32_t)a.n && c0 + v * step < a.dim) raw[u][v].load(row + v * step);
                 else raw[u][v].zero();
             }
         }
@@ -181,12 +183,16 @@ __global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_cons
         if (p + sub < end) { next_place = a.order[p + sub]; next_group = group_at(p + sub); }
     };
     ask(lo + lanes);
-    const auto add = [&](const Raw<T, VEC> (&raw)[U][NV], int64_t p, int at) {   // the places p + at ..
+    const auto add = [&](const Raw<T, VEC> (&raw)[U][NV], int left, int at) {   // the batch's places at .., as far as they are among its first `left`
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int32_t g = __shfl_sync(peers, group, (at + u) & (lanes - 1), lanes), r = __shfl_sync(peers, row, (at + u) & (lanes - 1), lanes);
-            if (p + at + u < end) {
-                if (g != cur) { flush(); cur = g; cur_row = r; }
+            const int32_t g = __shfl_sync(peers, group, (at + u) & (lanes - 1), lanes);
+            if (at + u < left) {
+                if (g != cur) {
+                    flush();
+                    cur = g;
+                    cur_row = __shfl_sync(peers, row, (at + u) & (lanes - 1), lanes);
+                }
 #pragma unroll
                 for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -197,12 +203,13 @@ __global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_cons
     // (a batch is a multiple of 2 U places, or these are all of it)
     for (int64_t p = lo; p < end; p += lanes) {
         const int32_t after = next_place;   // places of the batch behind this one
+        const int left = (int)min(end - p, (int64_t)lanes);
         for (int at = 0; at < lanes; at += 2 * U) {
             if (lanes >= 2 * U) load(two, place, at + U);
-            add(one, p, at);
+            add(one, left, at);
             const bool more = at + 2 * U < lanes;
             load(one, more ? place : after, more ? at + 2 * U : 0);
-            if (lanes >= 2 * U) add(two, p, at + U);
+            if (lanes >= 2 * U) add(two, left, at + U);
         }
         place = next_place; group = next_group;
         row = row_of(group);
