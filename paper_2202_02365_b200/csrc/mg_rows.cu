@@ -162,7 +162,7 @@ extern "C" int mg_embedding_backward_workspace(mg_ctx* ctx, int64_t n, int64_t n
     if (!bytes) return mg_fail(ctx, MG_ERR_ARG, "null argument");
     static const int32_t some = 0;
     if (int rc = check_ids(ctx, &some, 0, n, n_rows)) return rc;
-    if (dim < 1 || dim > 1 << 24) return mg_fail(ctx, MG_ERR_ARG, "the width of a row must be in [1, 2^24]");
+    if (dim < 1 || dim > 1 << 22) return mg_fail(ctx, MG_ERR_ARG, "the width of a row must be in [1, 2^22]");
     *bytes = sums_workspace(n, n_rows, dim, ctx->n_sms);
     return MG_OK;
 }

@@ -32,7 +32,7 @@ inline int check_ids(mg_ctx* ctx, const void* ids, int ids_are_i64, int64_t n, i
 inline int check_lookup(mg_ctx* ctx, const void* table, int64_t table_stride, int table_dtype, int64_t n_rows, int32_t dim, const void* ids, int ids_are_i64,
                         int64_t n, float scale, const void* y, int64_t y_stride, int y_dtype) {
     if (!known_dtype(table_dtype) || !known_dtype(y_dtype)) return mg_fail(ctx, MG_ERR_ARG, "unknown dtype");
-    if (dim < 1 || dim > 1 << 24) return mg_fail(ctx, MG_ERR_ARG, "the width of a row must be in [1, 2^24]");
+    if (dim < 1 || dim > 1 << 22) return mg_fail(ctx, MG_ERR_ARG, "the width of a row must be in [1, 2^22]");
     if (!isfinite(scale)) return mg_fail(ctx, MG_ERR_ARG, "the scale must be finite");
     if (int rc = check_ids(ctx, ids, ids_are_i64, n, n_rows)) return rc;
     if (int rc = check_matrix(ctx, "the table", table, table_stride, table_dtype, n_rows, dim, false)) return rc;
@@ -115,7 +115,7 @@ inline int check_sums(mg_ctx* ctx, const void* d_y, int64_t d_y_stride, int d_y_
                       const void* group_of, const void* group_ids, int ids_are_i64, const void* starts, const void* n_groups, int into, const void* out, int64_t out_stride, int out_dtype,
                       const void* workspace, size_t workspace_bytes) {
     if (!known_dtype(d_y_dtype) || !known_dtype(out_dtype)) return mg_fail(ctx, MG_ERR_ARG, "unknown dtype");
-    if (dim < 1 || dim > 1 << 24) return mg_fail(ctx, MG_ERR_ARG, "the width of a row must be in [1, 2^24]");
+    if (dim < 1 || dim > 1 << 22) return mg_fail(ctx, MG_ERR_ARG, "the width of a row must be in [1, 2^22]");
     if (!isfinite(scale)) return mg_fail(ctx, MG_ERR_ARG, "the scale must be finite");
     if (into != MG_ROWS_TABLE && into != MG_ROWS_ADD && into != MG_ROWS_COMPACT) return mg_fail(ctx, MG_ERR_ARG, "unknown place for the sums");
     if (n < 0 || n >= (1ll << 31) - 1 || n_rows < 0 || n_rows >= (1ll << 31) - 1) return mg_fail(ctx, MG_ERR_ARG, "the numbers of ids and of rows must be in [0, 2^31 - 2]");

@@ -369,6 +369,46 @@ def test_distill(ctx, dtype, rows, classes, entries):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("classes", [7, 8, 63, 153, 172, 1023, 1024, 1026, 1500, 2048, 2049, 6144, 6151, 16_400, 70_003, 140_001])
+def test_best_classes_wherever_they_lie(ctx, classes):
+    """The best at the rows' ends, at the borders of what a thread, a round and a row's part hold, and rising or falling along the row."""
+    for dtype in (torch.float32, torch.bfloat16):
+        for rows in (1, 40):
+            x = logits_of(rows, classes, dtype, classes, 1, 1, spread=0.5)
+            g = torch.Generator(device="cuda").manual_seed(classes)
+            at = torch.cat([torch.tensor([0, classes - 1, classes // 2], device="cuda"), torch.randint(0, classes, (9,), generator=g, device="cuda")]).unique()
+            x[:, at] = (10 + torch.randperm(len(at), generator=g, device="cuda")).to(dtype)
+            if rows > 1:
+                x[1] = (torch.arange(classes, device="cuda") / classes).to(dtype)      # rising: many equal ones in two bytes
+                x[2] = -(torch.arange(classes, device="cuda") / classes).to(dtype)
+                x[3, :classes // 3] = 9.0
+            check_scores(ctx, x, some_labels(rows, classes, 1), min(32, classes), 0.8)
+            check_scores(ctx, x, some_labels(rows, classes, 2), min(7, classes), 1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,classes", [(1, 8), (7, 153), (300, 153), (3000, 172), (50, 1024), (33, 2047), (257, 4), (900, 12), (5, 2048)])
+def test_runs_of_rows_with_and_without_gradients(ctx, rows, classes):
+    """Rows that lie one behind the other: every third without a label, some without any gradient, some that allow nothing, as the first and the last of all."""
+    for dtype in (torch.float32, torch.float16):
+        x = logits_of(rows, classes, dtype, rows)
+        x = x.contiguous()
+        labels = torch.randint(0, classes, (rows,), device="cuda")
+        labels[::3] = -100
+        x[rows // 2] = -INF
+        r = ctx.log_probs(x, labels)
+        g, h, l = torch.randn(3, rows, device="cuda")
+        h[1::4] = l[1::4] = 0.0
+        for how in (dict(d_log_prob=g), dict(d_log_prob=g, entropy=r.entropy, d_entropy=h, d_lse=l)):
+            want, off = scores_backward(x, r.lse, labels, how["d_log_prob"], how.get("entropy"), how.get("d_entropy"), how.get("d_lse"), 1.0, dtype)
+            got = ctx.log_probs_backward(x, r.lse, labels, **how)
+            near(got, want, off)
+            assert not got[rows // 2].any()
+            inplace = x.clone()
+            assert torch.equal(ctx.log_probs_backward(inplace, r.lse, labels, out=inplace, **how), got)
+
+
+@pytest.mark.gpu
 def test_shapes_and_nothing(ctx):
     x = logits_of(24, 50, torch.float32, 1).view(2, 3, 4, 50)
     labels = torch.randint(0, 50, (2, 3, 4), device="cuda")
