@@ -524,6 +524,7 @@ class Context:
         self.stream = stream
         self.handle = C.c_void_p(0)
         self._owned = {}      # handles that belong to the context, and what frees them
+        self._counted = None  # where a number of ids comes to the host
         sptr = C.c_void_p(stream.cuda_stream if stream is not None else 0)
         rc = self.lib.mg_create(C.byref(self.handle), C.c_int(device), sptr)
         if rc != MG_OK:
@@ -928,9 +929,10 @@ class Context:
         """The same gradient as the distinct ids, ascending, and a row for each.  The host waits for the number of ids (not for the sums), so the call cannot be
         captured; the rows are the first of a block that has room for min(ids, n_rows)."""
         d_y, groups = self._grouped(d_y, ids, n_rows)
-        count = torch.empty(1, dtype=torch.int32, pin_memory=True)
+        if self._counted is None:      # (one call at a time uses them: it waits for the copy itself)
+            self._counted = torch.empty(1, dtype=torch.int32, pin_memory=True), torch.cuda.Event()
+        count, known = self._counted
         count.copy_(groups.count, non_blocking=True)
-        known = torch.cuda.Event()
         known.record(torch.cuda.current_stream(self.device))
         rows = torch.empty((groups.ids.numel(), d_y.shape[1]), dtype=dtype or d_y.dtype, device=self.device)
         self._group_sums(d_y, groups, scale, ROWS_COMPACT, rows)

@@ -18,7 +18,8 @@ static void launch_wide(const ForwardLaunch& l, const ScoreArgs& a, const Teache
 }
 
 void launch_distill(const ForwardLaunch& l, const ScoreArgs& a, const TeacherArgs& t, float* loss, cudaStream_t st) {
-    if (!l.lanes) MG_LOSS_BY_TYPE(l.dtype, (l.threads == kWideThreads ? launch_wide<T, kWideThreads>(l, a, t, loss, st) : launch_wide<T, kWideMostThreads>(l, a, t, loss, st)));
+    if (!l.lanes) MG_LOSS_BY_TYPE(l.dtype, (l.threads == kWideThreads ? launch_wide<T, kWideThreads>(l, a, t, loss, st) : l.threads == kWideLeastThreads ? launch_wide<T, kWideLeastThreads>(l, a, t, loss, st) : launch_wide<T, kWideMostThreads>(l, a, t, loss, st)));
+    else if (l.lanes == 16) MG_LOSS_BY_TYPE(l.dtype, MG_LOSS_BY_VECTORS(l.nv, (launch_rows<T, NV, 16>(l, a, t, loss, st))));
     else if (l.lanes == 8) MG_LOSS_BY_TYPE(l.dtype, MG_LOSS_BY_VECTORS(l.nv, (launch_rows<T, NV, 8>(l, a, t, loss, st))));
     else MG_LOSS_BY_TYPE(l.dtype, MG_LOSS_BY_VECTORS(l.nv, (launch_rows<T, NV, 32>(l, a, t, loss, st))));
 }

@@ -306,10 +306,10 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_cons
     const float lse = a.lse[r], d_loss = a.d_loss[r];
     const Cover<VEC> cover(d, sizeof(T), a.classes, WHOLE);
     const int32_t lo = min(chunk * piece, cover.vecs), hi = min(lo + piece, cover.vecs);
-    const int warps = teacher_warps(t);
+    const int warps = teacher_warps<kTeacherThreads>(t);
     const auto here = [&](int32_t of) { return of >= 0 && (of + cover.lead) / VEC >= lo && (of + cover.lead) / VEC < hi; };
     if ((int)threadIdx.x < warps * 32) {
-        const TeacherRow teacher = teacher_row(t, r, x, a.classes, a.scale, warps, scratch, q, at_class, c, here);
+        const TeacherRow teacher = teacher_row<kTeacherThreads>(t, r, x, a.classes, a.scale, warps, scratch, q, at_class, c, here);
         for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) q[k] = expf(q[k]) * teacher.part;
         if (threadIdx.x == 0) sh_mass = teacher.mass;
     }

@@ -1,4 +1,4 @@
-// Narrow rows of logits, forward: 8 or 32 lanes to a row, which they hold in registers.
+// Narrow rows of logits, forward: 8, 16 or 32 lanes to a row, which they hold in registers.
 #pragma once
 
 #include "mg_loss.cuh"

@@ -18,7 +18,8 @@ static void launch_wide(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t
 }
 
 void launch_scores(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t st) {
-    if (!l.lanes) MG_LOSS_BY_TYPE(l.dtype, (l.threads == kWideThreads ? launch_wide<T, kWideThreads>(l, a, st) : launch_wide<T, kWideMostThreads>(l, a, st)));
+    if (!l.lanes) MG_LOSS_BY_TYPE(l.dtype, (l.threads == kWideThreads ? launch_wide<T, kWideThreads>(l, a, st) : l.threads == kWideLeastThreads ? launch_wide<T, kWideLeastThreads>(l, a, st) : launch_wide<T, kWideMostThreads>(l, a, st)));
+    else if (l.lanes == 16) MG_LOSS_BY_TYPE(l.dtype, MG_LOSS_BY_VECTORS(l.nv, (launch_rows<T, NV, 16>(l, a, st))));
     else if (l.lanes == 8) MG_LOSS_BY_TYPE(l.dtype, MG_LOSS_BY_VECTORS(l.nv, (launch_rows<T, NV, 8>(l, a, st))));
     else MG_LOSS_BY_TYPE(l.dtype, MG_LOSS_BY_VECTORS(l.nv, (launch_rows<T, NV, 32>(l, a, st))));
 }

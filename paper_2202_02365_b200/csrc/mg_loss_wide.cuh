@@ -8,9 +8,9 @@
 
 namespace mgloss {
 
-constexpr int kWideThreads = 256, kWideMostThreads = 1024;
+constexpr int kWideThreads = 256, kWideLeastThreads = 64, kWideMostThreads = 1024;
 constexpr int kWideAhead = 6;                      // vectors of a thread that are on their way (24 KB of a block; with five or six blocks to an SM more than the memory's latency asks for)
-constexpr int kWideRoom = 512, kWideTrim = 128;    // pairs of vectors, and classes, that may be among the best: room; how many classes are cut down to the best again
+constexpr int kWideRoom = 512, kWideTrim = 64;     // pairs of vectors, and classes, that may be among the best: room; how many classes are cut down to the best again
 
 // (places in shared memory by their 32-bit addresses)
 __device__ __forceinline__ void copy_ahead(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
@@ -21,6 +21,9 @@ __device__ __forceinline__ uint4 copied(uint32_t at) {
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+// blocks to an SM: 48 warps of the usual ones (their rings are 148 KB), 32 of the small
+constexpr int wide_blocks(int threads) { return threads == kWideThreads ? 6 : threads == kWideLeastThreads ? 16 : 1; }
 
 // packed values of one type: two halves to a word, or a float
 template <typename T> struct Word {
@@ -253,8 +256,9 @@ __device__ __forceinline__ RowSums go_along(const T* x, int32_t classes, float s
         from += 2 * kStep;
         slot += 2 * kStep;
         if (slot == last) slot = first;
-        if (top && i % 64 == 62 && i + 2 < rounds) {
-            collect(i / 2 - 31);
+        // long rows: behind 16, 32 and every 64 rounds, so that the bound keeps up with the row
+        if (top && rounds > 32 && (i == 14 || i == 30 || i % 64 == 62) && i + 2 < rounds) {
+            collect(i / 64 * 32);
             const int n = sh->n_best;
             if (n > kWideTrim && n <= ROOM) {
                 rank_keys<THREADS>(sh->room, n, top, sh->best);
@@ -353,9 +357,8 @@ __device__ __forceinline__ RowSums over_cluster(RowSums r, int parts, float scal
     return r;
 }
 
-constexpr int kWideBlocks = 6;   // to an SM
 template <typename T, int THREADS, bool EDGES>
-__global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? kWideBlocks : 1) k_scores_wide(const __grid_constant__ ScoreArgs a, int parts_log2) {
+__global__ void __launch_bounds__(THREADS, wide_blocks(THREADS)) k_scores_wide(const __grid_constant__ ScoreArgs a, int parts_log2) {
     namespace cg = cooperative_groups;
     __shared__ WideShared<THREADS, kWideRoom> sh;
     extern __shared__ __align__(16) uint4 ring[];   // kWideAhead vectors of each thread
@@ -421,17 +424,17 @@ __device__ __forceinline__ float over_warps(float v, int warps, float* scratch, 
     return v;
 }
 
-// The warps that deal with a teacher's pairs: a pair to a thread, up to 256 threads; more pairs go round.
+// The warps that deal with a teacher's pairs: a pair to a thread, up to 256 threads (or as many as a block has); more pairs go round.
 constexpr int kTeacherThreads = 256;
-__device__ __forceinline__ int teacher_warps(const TeacherArgs& t) { return (min(t.entries, kTeacherThreads) + 31) / 32; }
+template <int THREADS> __device__ __forceinline__ int teacher_warps(const TeacherArgs& t) { return (min(t.entries, THREADS) + 31) / 32; }
 
 // A teacher's row, by these warps: `above` [entries] in shared memory gets the values less `shift` (-infinity: not a pair), at_class the logits of their classes, where
 // `wanted(class)`.  Each thread deals with the same pairs throughout.  A pair's probability is exp(above) part, its logarithm above - log_sum.
 struct TeacherRow { float part, log_sum, mass; };   // mass: the probabilities' sum
-template <typename T, typename F>
+template <int THREADS, typename T, typename F>
 __device__ __forceinline__ TeacherRow teacher_row(const TeacherArgs& t, int64_t r, const T* x, int32_t classes, float scale, int warps, float* scratch, float* above, float* at_class, int32_t* c, F wanted) {
     float m = kNegInf;
-    for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
+    for (int k = threadIdx.x; k < t.entries; k += THREADS) {
         const int32_t of = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, classes);
         const float v = of >= 0 ? scale * float_at(t.values, t.dtype, r * t.values_stride + k) : kNegInf;
         at_class[k] = of >= 0 && wanted(of) ? to_float(x[of]) : 0.f;
@@ -441,7 +444,7 @@ __device__ __forceinline__ TeacherRow teacher_row(const TeacherArgs& t, int64_t 
     }
     const float shift = t.lse ? t.lse[r] : centre(over_warps(m, warps, scratch, [](float a, float b) { return fmaxf(a, b); }));
     float sum = 0.f;
-    for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
+    for (int k = threadIdx.x; k < t.entries; k += THREADS) {
         above[k] -= shift;
         sum += expf(above[k]);   // (0 of -infinity)
     }
@@ -451,7 +454,7 @@ __device__ __forceinline__ TeacherRow teacher_row(const TeacherArgs& t, int64_t 
 }
 
 template <typename T, int THREADS, bool EDGES>
-__global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? kWideBlocks : 1) k_distill_wide(const __grid_constant__ ScoreArgs a, const __grid_constant__ TeacherArgs t, float* loss, int parts_log2) {
+__global__ void __launch_bounds__(THREADS, wide_blocks(THREADS)) k_distill_wide(const __grid_constant__ ScoreArgs a, const __grid_constant__ TeacherArgs t, float* loss, int parts_log2) {
     namespace cg = cooperative_groups;
     __shared__ WideShared<THREADS, 1> sh;
     extern __shared__ __align__(16) uint4 ring[];   // kWideAhead vectors of each thread
@@ -460,17 +463,18 @@ __global__ void __launch_bounds__(THREADS, THREADS == kWideThreads ? kWideBlocks
     const int64_t r = blockIdx.x >> parts_log2;
     const int part = (int)(blockIdx.x & (unsigned)(parts - 1));
     const T* x = static_cast<const T*>(a.x) + r * a.stride;
-    const int warps = teacher_warps(t);
+    constexpr int TEACHERS = THREADS < kTeacherThreads ? THREADS : kTeacherThreads;
+    const int warps = teacher_warps<TEACHERS>(t);
     const bool teaches = part == 0 && (int)threadIdx.x < warps * 32;
     TeacherRow teacher{0.f, 0.f, 0.f};   // (while the row's first vectors are on their way)
     RowSums s = go_along<T, THREADS, 1, false, EDGES>(x, a.classes, a.scale2, part, parts_log2, 0, &sh, ring, [&] {
-        if (teaches) teacher = teacher_row(t, r, x, a.classes, a.scale, warps, sh.scratch, above, at_class, nullptr, [](int32_t) { return true; });
+        if (teaches) teacher = teacher_row<TEACHERS>(t, r, x, a.classes, a.scale, warps, sh.scratch, above, at_class, nullptr, [](int32_t) { return true; });
     });
     if (parts > 1) s = over_cluster<false>(s, parts, a.scale2, &sh);
     if (teaches) {
         const RowResult res(s, a.scale);
         float v = 0.f;
-        for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
+        for (int k = threadIdx.x; k < t.entries; k += TEACHERS) {
             const float q = expf(above[k]) * teacher.part;
             if (q != 0.f) v = fmaf(q, (above[k] - teacher.log_sum) - res.log_p(at_class[k]), v);
         }
