@@ -145,7 +145,7 @@ extern "C" int mg_id_groups(mg_ctx* ctx, const void* ids, int ids_are_i64, int64
     const cudaStream_t st = (cudaStream_t)stream;
     const GroupPlan p = plan_groups(n, n_rows, ctx->n_sms);
     if (!p.passes) {
-        k_sort_small<<<1, kSmallThreads, 0, st>>>(ids, ids_are_i64, (int32_t)n, (uint32_t)n_rows, order, group_of, group_ids, starts, n_groups);
+        k_sort_small<<<1, kSmallIds, 0, st>>>(ids, ids_are_i64, (int32_t)n, (uint32_t)n_rows, order, group_of, group_ids, starts, n_groups);
         ctx->launches++;
         MG_CUDA(ctx, cudaGetLastError());
         return MG_OK;

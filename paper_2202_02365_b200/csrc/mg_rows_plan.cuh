@@ -9,7 +9,7 @@
 
 namespace {
 
-constexpr int kPlanBits = 8, kPlanBins = 1 << kPlanBits, kPlanThreads = 256, kPlanSmall = 4096;   // of the sort; ids that one block sorts
+constexpr int kPlanBits = 8, kPlanBins = 1 << kPlanBits, kPlanThreads = 256, kPlanSmall = 1024;   // of the sort; ids that one block sorts
 
 inline size_t rows_align(size_t bytes) { return (bytes + 15) / 16 * 16; }
 

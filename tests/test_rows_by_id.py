@@ -211,7 +211,7 @@ def test_gradient_of_many_places(ctx, n, n_rows, dim, kind):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("n", [15, 16, 17, 33, 4095, 4096, 4097, 12_345])
+@pytest.mark.parametrize("n", [15, 16, 17, 33, 1023, 1024, 1025, 4097, 12_345])
 def test_ids_that_begin_and_end_anywhere(ctx, n):
     """Runs of equal ids of every length around a chunk's, from every place on; ids that are none among them."""
     g = torch.Generator(device="cuda").manual_seed(n)
@@ -397,7 +397,7 @@ int main() {
 
     struct G { const void* ids; int wide; int64_t n, rows; const void *order, *of, *gids, *starts, *count, *ws; size_t bytes; };
     const G good{ids, 0, 10000, 500, base, base + 80000, far, far + 8000, far + 16000, more, 1 << 30};
-    if (plan_groups(4096, 500).bytes || !plan_groups(4097, 500).bytes) { printf("small\n"); ++bad; }
+    if (plan_groups(1024, 500).bytes || !plan_groups(1025, 500).bytes) { printf("small\n"); ++bad; }
     const auto groups = [&](auto change) { G a = good; change(a); return check_groups(&context, a.ids, a.wide, a.n, a.rows, a.order, a.of, a.gids, a.starts, a.count, a.ws, a.bytes); };
     EXPECT(MG_OK, groups([](G&) {}));
     EXPECT(MG_OK, groups([](G& a) { a.bytes = plan_groups(a.n, a.rows).bytes; }));
