@@ -94,13 +94,15 @@ inline bool same_phase(const void* a, int64_t a_stride, const void* b, int64_t b
 }
 
 constexpr int kPlanRowThreads = 256, kPlanHeld = 32;   // of the narrow kernels; values of a row to a lane
-constexpr int kPlanWideThreads = 256, kPlanWideLeast = 64, kPlanWideMost = 1024, kPlanWideVecs = 8;
+constexpr int kPlanWideThreads = 128, kPlanWideLeast = 64, kPlanWideMost = 1024;
 
 struct ForwardPlan { int nv = 0, lanes = 0, parts = 1, parts_log2 = 0, threads = 0; int64_t blocks = 0; };
 
 // Rows that 32 lanes hold in registers are narrow (however they lie to the vectors): 8, 16 or 32 lanes to a row, as few as hold it and are as many as best classes are asked for.
-// Wide rows: a block of 256 threads goes along one, or of 64 where these have 32 rounds or fewer (20,000 fp32 rows of 2,000 with five best: PLACE); a cluster of up to 16 blocks where rows are
-// fewer than the GPU holds blocks (four to a multiprocessor), a quarter of 2,048 vectors to each at least; where all of these leave room, blocks of 1,024 threads.
+// Wide rows: a block of 128 threads goes along one, or of 64 where these have 16 rounds or fewer.  Both sides, 64 / 128 threads, us: 20,000 fp32 rows of 2,000 with five best 66 / 87, 30,000
+// bf16 rows of 5,000 with ten 122 / 150, 10,000 fp32 rows of 8,000 89 / 75, 5,000 of 16,000 91 / 67; by 256 threads 137, -, -, 73, and 4,096 bf16 rows of 50,257 without best classes 81
+// for 74.  A cluster of up to 16 blocks where rows are fewer than the GPU holds blocks (eight to a multiprocessor), 512 vectors to each at least; where all of these leave room, of
+// 1,024 threads each.
 inline ForwardPlan plan_forward(const mg_logits* z, int32_t top, int n_sms) {
     ForwardPlan p;
     const int64_t vec = 16 / elem_size(z->dtype), covered = (z->classes + vec - 1 + vec - 1) / vec, held = kPlanHeld / vec;
@@ -113,9 +115,8 @@ inline ForwardPlan plan_forward(const mg_logits* z, int32_t top, int n_sms) {
         p.blocks = std::min<int64_t>((z->rows + groups - 1) / groups, (int64_t)n_sms * 64);
         return p;
     }
-    const int64_t segment = (int64_t)kPlanWideThreads * kPlanWideVecs * vec;
-    while (p.parts < 16 && z->rows * p.parts * 2 <= 4ll * n_sms && z->classes / (p.parts * 2) >= segment / 4) { p.parts *= 2; ++p.parts_log2; }
-    p.threads = z->rows * p.parts <= n_sms && z->classes / p.parts > 2 * segment ? kPlanWideMost : p.parts == 1 && z->classes <= 32 * kPlanWideLeast * vec && z->rows > 4 * n_sms ? kPlanWideLeast : kPlanWideThreads;
+    while (p.parts < 16 && z->rows * p.parts * 2 <= 8ll * n_sms && z->classes / (p.parts * 2) >= 512 * vec) { p.parts *= 2; ++p.parts_log2; }
+    p.threads = z->rows * p.parts <= n_sms && z->classes / p.parts > 4096 * vec ? kPlanWideMost : p.parts == 1 && z->classes <= 16 * kPlanWideLeast * vec ? kPlanWideLeast : kPlanWideThreads;
     p.blocks = z->rows * p.parts;
     return p;
 }

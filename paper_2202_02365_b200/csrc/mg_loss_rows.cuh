@@ -1,4 +1,5 @@
-// Narrow rows of logits, forward: 8, 16 or 32 lanes to a row, which they hold in registers.
+// Narrow rows of logits, forward: 8, 16 or 32 lanes to a row, which they hold in registers.  128,000 fp32 rows of 172: 26 us without best classes (96 MB, 3.7 TB/s; 350 instructions for a
+// warp's four rows), 35 with one, 43 with five (900 instructions), 76 with ten; bound by instructions.
 #pragma once
 
 #include "mg_loss.cuh"

@@ -1,5 +1,8 @@
 // Wide rows of logits, forward: a block or a cluster of them goes along a row, whose vectors every thread has brought to places of its own in shared memory some rounds ahead:
-// no registers wait for them, and no thread for another's.
+// no registers wait for them, and no thread for another's.  8,192 bf16 rows of 32,000 against a teacher's 64 pairs: 91 us (5.8 TB/s), more where one follows the other at a lower clock;
+// 4,096 of 50,257 with twenty best 113, without 74.  Bound by instructions: five to seven a value (two for the conversion and the largest, one exponential at 16 a cycle and SM, sums in pairs)
+// and 300 to 1,000 a warp and row.  Measured and taken back: vectors in registers, eight of them to a thread in segments (119; 143 with twenty best), the same by blocks that stay and ask for
+// the next row's vectors early (141 - 230).
 #pragma once
 
 #include <cooperative_groups.h>
@@ -8,8 +11,8 @@
 
 namespace mgloss {
 
-constexpr int kWideThreads = 256, kWideLeastThreads = 64, kWideMostThreads = 1024;
-constexpr int kWideAhead = 6;                      // vectors of a thread that are on their way (24 KB of a block; with five or six blocks to an SM more than the memory's latency asks for)
+constexpr int kWideThreads = 128, kWideLeastThreads = 64, kWideMostThreads = 1024;
+constexpr int kWideAhead = 6;                      // vectors of a thread that are on their way (12 KB of a block of 128; with ten blocks to an SM more than the memory's latency asks for)
 constexpr int kWideRoom = 512, kWideTrim = 64;     // pairs of vectors, and classes, that may be among the best: room; how many classes are cut down to the best again
 
 // (places in shared memory by their 32-bit addresses)
@@ -22,8 +25,8 @@ __device__ __forceinline__ uint4 copied(uint32_t at) {
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// blocks to an SM: 48 warps of the usual ones (their rings are 148 KB), 32 of the small
-constexpr int wide_blocks(int threads) { return threads == kWideThreads ? 6 : threads == kWideLeastThreads ? 16 : 1; }
+// blocks to an SM: 40 warps of the usual ones, 32 of the small
+constexpr int wide_blocks(int threads) { return threads == kWideThreads ? 10 : threads == kWideLeastThreads ? 16 : 1; }
 
 // packed values of one type: two halves to a word, or a float
 template <typename T> struct Word {
@@ -424,7 +427,7 @@ __device__ __forceinline__ float over_warps(float v, int warps, float* scratch, 
     return v;
 }
 
-// The warps that deal with a teacher's pairs: a pair to a thread, up to 256 threads (or as many as a block has); more pairs go round.
+// The warps that deal with a teacher's pairs: a pair to a thread, up to 256 threads, or as many as a block has; more pairs go round.
 constexpr int kTeacherThreads = 256;
 template <int THREADS> __device__ __forceinline__ int teacher_warps(const TeacherArgs& t) { return (min(t.entries, THREADS) + 31) / 32; }
 
