@@ -12,7 +12,7 @@ TeacherArgs teacher_args(const mg_teacher* t) { return {t->ids, t->values, t->ls
 int run_forward(mg_ctx* ctx, const mg_logits* z, const ScoreArgs& a, const mg_teacher* teacher, float* loss, cudaStream_t st) {
     DeviceScope on(ctx->device);
     MG_CUDA(ctx, on.err);
-    const ForwardPlan p = plan_forward(z, a.top, ctx->n_sms);
+    const ForwardPlan p = plan_forward(z, a.top, !teacher, ctx->n_sms);
     const ForwardLaunch l{z->dtype, whole_vectors(z->x, z->stride, z->rows, z->classes, z->dtype), p.nv, p.lanes, p.parts_log2, p.threads, p.blocks};
     if (teacher) launch_distill(l, a, teacher_args(teacher), loss, st);
     else launch_scores(l, a, st);

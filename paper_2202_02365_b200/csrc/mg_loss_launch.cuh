@@ -9,7 +9,7 @@ namespace mgloss {
 struct ForwardLaunch {
     int dtype;
     bool whole;            // rows begin and end with a vector
-    int nv, lanes;         // narrow rows: vectors to a lane, lanes to a row; wide ones: 0
+    int nv, lanes;         // narrow rows: vectors to a lane, lanes to a row (1: a thread each); wide ones: 0
     int parts_log2, threads;   // wide rows: blocks to a row, threads to a block
     int64_t blocks;
 };

@@ -387,6 +387,22 @@ def test_best_classes_wherever_they_lie(ctx, classes):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("classes", [1, 2, 5, 8, 9, 16, 20, 31, 32, 33])
+def test_many_rows_of_few_classes(ctx, classes):
+    for dtype in (torch.float32, torch.float16):
+        for pad, masked in ((0, 0.0), (3, 0.4)):
+            x = logits_of(40_001, classes, dtype, classes, pad, 1 if pad else 0, masked=masked)
+            x[5] = -INF
+            x[6], x[7] = 1.0, -0.0
+            x[7, ::2] = 0.0
+            check_scores(ctx, x, some_labels(40_001, classes, 1), classes if classes < 33 else 32, 0.5)
+            check_scores(ctx, x, some_labels(40_001, classes, 2, torch.int32), 1, 1.0)
+            x[8, 0], x[9, classes // 2] = float("nan"), INF
+            r = ctx.log_probs(x, top=classes if classes < 33 else 32)
+            assert r.lse[8].isnan() and r.lse[9].isnan() and torch.equal(r.top_ids.long(), top_of(x, r.top_ids.shape[1]))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("rows,classes", [(1, 8), (7, 153), (300, 153), (3000, 172), (50, 1024), (33, 2047), (257, 4), (900, 12), (5, 2048)])
 def test_runs_of_rows_with_and_without_gradients(ctx, rows, classes):
     """Rows that lie one behind the other: every third without a label, some without any gradient, some that allow nothing, as the first and the last of all."""
