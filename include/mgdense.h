@@ -598,7 +598,7 @@ int mg_model_norm_grads(const mg_model* m, int32_t layer, const float** d_weight
  * padded.  Rows are table_stride / y_stride elements apart, of table_dtype / y_dtype (MG_DTYPE_*); ids are int32 or (ids_are_i64) int64.  DEVICE
  * pointers, aligned to their elements; y lies apart from the table, its rows do not overlap.  Rows of whole 16-byte pieces are fastest.  One kernel,
  * queued on `stream` (a cudaStream_t of the context's device; NULL = the default stream), not waited for; it may be captured into a graph.
- * Errors: MG_ERR_ARG (2^31 rows or ids or more among them). */
+ * Errors: MG_ERR_ARG (2^31 rows or ids or more, rows of more than 2^22 values among them). */
 int mg_embedding(mg_ctx* ctx, const void* table, int64_t table_stride, int table_dtype, int64_t n_rows, int32_t dim, const void* ids, int ids_are_i64,
                  int64_t n, float scale, void* y, int64_t y_stride, int y_dtype, void* stream);
 

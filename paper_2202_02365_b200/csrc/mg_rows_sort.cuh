@@ -1,5 +1,5 @@
 // The places of equal ids brought together: a radix sort of the ids by their places, eight bits at a time, each digit one kernel whose tiles look back at those
-// before them.  All kernels for 543,000 ids of two million rows (three digits): 55 us, for 50,000 of 14,824 22; bound by launches and the waits for the tiles before.
+// before them.  All kernels for 543,000 ids of two million rows (three digits): 52 us, for 50,000 of 14,824 22; bound by launches and the waits for the tiles before.
 #pragma once
 
 #include "mg_norm_tiles.cuh"
