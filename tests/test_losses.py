@@ -387,6 +387,37 @@ def test_best_classes_wherever_they_lie(ctx, classes):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("classes", [1100, 2500, 6151, 16_400, 70_003, 300_007])
+def test_many_equal_values_and_few_classes_that_are_allowed(ctx, classes):
+    """Rows of which many more classes are as good as the last of the best than there is room for, or fewer allowed than are asked for."""
+    for dtype in (torch.float32, torch.float16):
+        for rows in (1, 30):
+            g = torch.Generator(device="cuda").manual_seed(classes + rows)
+            x = torch.full((rows, classes + 3), float("nan"), dtype=dtype, device="cuda")[:, 1:1 + classes]
+            some = lambda n: torch.randint(0, classes, (n,), generator=g, device="cuda")
+            for r in range(rows):
+                x[r] = (-INF, torch.finfo(dtype).min, 0.0, -1e4)[r % 4]
+                x[r, some((0, 1, 5, 20, 90, 600)[r // 4 % 6])] = torch.randn(1, generator=g, device="cuda").item()
+                if r % 3 == 1:
+                    x[r, some(9)] = torch.randn(9, generator=g, device="cuda").to(dtype)
+            if rows > 1:
+                x[24] = (torch.arange(classes, device="cuda") // 7 / classes).to(dtype)      # rising by sevens
+                x[25, some(900)] = float("nan")
+                x[26, some(40)], x[27, some(40)] = float("nan"), INF
+                x[28] = -INF
+                x[28, [0, classes - 1]] = 1.0
+                x[29, classes // 2:] = -INF
+            for top in (32, 5):
+                r = ctx.log_probs(x, top=top)
+                best = top_of(x, top)
+                assert torch.equal(r.top_ids.long(), best)
+                fine = slice(0, 25)
+                (_, _), (_, _), (lse, lse_off), (log_p, log_p_off) = scores(x[fine], some_labels(len(x[fine]), classes, 1), 1.0)
+                near(r.lse[fine], lse, lse_off)
+                near(r.top_log_probs[fine], log_p.gather(-1, best[fine]), log_p_off.gather(-1, best[fine]))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("classes", [1, 2, 5, 8, 9, 16, 20, 31, 32, 33])
 def test_many_rows_of_few_classes(ctx, classes):
     for dtype in (torch.float32, torch.float16):
