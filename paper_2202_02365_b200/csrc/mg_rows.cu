@@ -82,31 +82,37 @@ void launch_sort(mg_ctx* ctx, const GroupPlan& p, const void* ids, int ids_are_i
 
 int pow2_up(int64_t v) { int p = 1; while (p < v) p *= 2; return p; }
 
-// elements to an access of 16 bytes (8 where types of two and four bytes meet), or one
+// Elements to an access: as many as make 16 bytes (8 where types of two and four bytes meet), or half or a quarter of that, as the rows' width and where they begin allow.
+// (500,000 bf16 rows of 100 of a million by 8 bytes 51 us, one element at a time 112; their gradient 194 and 331.)
 int row_vec(const void* a, int64_t a_stride, int a_dtype, int64_t a_rows, const void* b, int64_t b_stride, int b_dtype, int64_t b_rows, int32_t dim) {
-    const int vec = a_dtype != MG_DTYPE_F32 && b_dtype != MG_DTYPE_F32 ? 8 : 4;
+    int vec = a_dtype != MG_DTYPE_F32 && b_dtype != MG_DTYPE_F32 ? 8 : 4;
     const auto fits = [&](const void* p, int64_t stride, int dtype, int64_t rows) {
         return reinterpret_cast<uintptr_t>(p) % (uintptr_t)(vec * elem_size(dtype)) == 0 && (rows <= 1 || stride % vec == 0);
     };
-    return dim % vec == 0 && fits(a, a_stride, a_dtype, a_rows) && fits(b, b_stride, b_dtype, b_rows) ? vec : 1;
+    while (vec > 1 && !(dim % vec == 0 && fits(a, a_stride, a_dtype, a_rows) && fits(b, b_stride, b_dtype, b_rows))) vec /= 2;
+    return vec;
 }
 
 template <typename T, typename O>
 void launch_lookup(const LookupArgs& a, int vec, unsigned grid, cudaStream_t st) {
-    constexpr int WIDE = sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4;
-    if (vec > 1) k_embedding<T, O, WIDE, 4><<<grid, kRowThreads, 0, st>>>(a);
+    if constexpr (sizeof(T) == 2 && sizeof(O) == 2)
+        if (vec == 8) { k_embedding<T, O, 8, 4><<<grid, kRowThreads, 0, st>>>(a); return; }
+    if (vec == 4) k_embedding<T, O, 4, 4><<<grid, kRowThreads, 0, st>>>(a);
+    else if (vec == 2) k_embedding<T, O, 2, 8><<<grid, kRowThreads, 0, st>>>(a);
     else k_embedding<T, O, 1, 8><<<grid, kRowThreads, 0, st>>>(a);
 }
 
 template <typename T, typename O>
 void launch_sums(SumArgs a, int vec, int64_t zero_blocks, cudaStream_t st) {
-    constexpr int WIDE = sizeof(T) == 2 && sizeof(O) == 2 ? 8 : 4;
-    const int lanes = std::min(32, std::max(4, pow2_up((a.dim + (vec > 1 ? vec : 4) - 1) / (vec > 1 ? vec : 4))));
-    const int columns = lanes * (vec > 1 ? vec : 4);
+    const int each = std::max(vec, 4), lanes = std::min(32, std::max(4, pow2_up((a.dim + each - 1) / each))), columns = lanes * each;   // (columns to a lane)
     a.chunk_blocks = (int32_t)(((int64_t)a.chunks * lanes + kSumThreads - 1) / kSumThreads);
     const dim3 grid((unsigned)(a.chunk_blocks + zero_blocks), (unsigned)((a.dim + columns - 1) / columns));
-    if (vec > 1) mgnorm::launch_chained(grid, kSumThreads, st, k_chunk_sums<T, O, WIDE, 1, 4>, a, lanes);
-    else mgnorm::launch_chained(grid, kSumThreads, st, k_chunk_sums<T, O, 1, 4, 2>, a, lanes);
+    const auto go = [&](auto kernel) { mgnorm::launch_chained(grid, kSumThreads, st, kernel, a, lanes); };
+    if constexpr (sizeof(T) == 2 && sizeof(O) == 2)
+        if (vec == 8) { go(k_chunk_sums<T, O, 8, 1, 4>); return; }
+    if (vec == 4) go(k_chunk_sums<T, O, 4, 1, 4>);
+    else if (vec == 2) go(k_chunk_sums<T, O, 2, 2, 4>);
+    else go(k_chunk_sums<T, O, 1, 4, 2>);
 }
 
 }  // namespace
@@ -185,7 +191,7 @@ extern "C" int mg_embedding_backward(mg_ctx* ctx, const void* d_y, int64_t d_y_s
     const int zero_rows = (int)std::min<int64_t>(std::max<int64_t>(std::min(much, few), 32) / 32 * 32, kMostZeroRows);
     const SumArgs a{d_y, d_y_stride, n, n_rows, dim, scale, order, group_of, starts, n_groups, group_ids, ids_are_i64, into, out, out_stride, p.chunk, p.chunks,
                     reinterpret_cast<float*>(ws), p.pitch, reinterpret_cast<int32_t*>(ws + p.at_begun), 0, zero_rows,
-                    row_vec(out, out_stride, out_dtype, n_rows, out, out_stride, out_dtype, n_rows, dim) == 16 / elem_size(out_dtype)};
+                    row_vec(out, out_stride, out_dtype, n_rows, out, out_stride, out_dtype, n_rows, dim)};
     int64_t zero_blocks = into == MG_ROWS_TABLE ? (n_rows + zero_rows - 1) / zero_rows : 0;
     if (zero_blocks && (!p.chunks || n_rows * dim * elem_size(out_dtype) > 32ll << 20)) {
         MG_BY_TYPE(out_dtype, mgnorm::launch_chained(dim3((unsigned)zero_blocks), kSumThreads, st, k_zero_others<T>, a));

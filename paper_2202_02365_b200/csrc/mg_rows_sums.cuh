@@ -23,7 +23,7 @@ struct SumArgs {
     float* shares; int32_t pitch; // [chunks][2][pitch]: of the id that the chunk begins within, of the one that goes on behind it
     int32_t* begun;               // [chunks]: the group that begins in the chunk and has shares, -1
     int32_t chunk_blocks, zero_rows;   // blocks of the sums; rows to a block of those that write zeros
-    bool zero_wide;               // ... 16 bytes at a time
+    int32_t zero_vec;             // ... elements at a time
 };
 
 template <typename O, int VEC>
@@ -83,7 +83,8 @@ __device__ __forceinline__ void zero_others(const SumArgs& a, int64_t block) {
         }
     };
     constexpr int VEC = 16 / sizeof(O);
-    if (a.zero_wide) write(Raw<O, VEC>(), VEC);
+    if (a.zero_vec == VEC) write(Raw<O, VEC>(), VEC);
+    else if (a.zero_vec == VEC / 2) write(Raw<O, VEC / 2>(), VEC / 2);
     else write(Raw<O, 1>(), 1);
 }
 

@@ -114,6 +114,27 @@ def test_lookup(ctx, dtype, n, n_rows, dim):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dim,pad,shift", [(2, 0, 0), (6, 0, 2), (36, 0, 0), (36, 4, 4), (36, 2, 2), (50, 0, 0), (100, 0, 0), (100, 2, 6), (602, 6, 0), (300, 0, 4), (8, 0, 1), (128, 4, 0), (2052, 0, 0)])
+def test_widths_and_beginnings_between_vectors(ctx, dim, pad, shift):
+    """Rows of 4, 8 and 16 bytes' multiples that begin at others, of each pair of types, both ways."""
+    ids = ids_of(700, 90, 1, "padded")
+    for dtype in TYPES.values():
+        table, d_y = matrix(90, dim, dtype, 2, pad, shift), matrix(700, dim, dtype, 3, pad, shift)
+        for to in TYPES.values():
+            check_lookup(ctx.embedding(table, ids, 1.7, dtype=to), table, ids, 1.7)
+            out = matrix(700, dim, to, 4, pad, shift)
+            ctx.embedding(table, ids, 1.7, out=out)
+            check_lookup(out, table, ids, 1.7)
+            want, size, count = summed_up(d_y, ids, 90, 1.7)
+            check_sums(ctx.embedding_backward(d_y, ids, 90, 1.7, dtype=to), want, size, count)
+            out = matrix(90, dim, to, 5, pad, shift)
+            around = out.as_strided((90, out.stride(0)), out.stride(), out.storage_offset())[:, dim:]
+            ctx.embedding_backward(d_y, ids, 90, 1.7, out=out)
+            check_sums(out, want, size, count)
+            assert around[:-1].isnan().all()
+
+
+@pytest.mark.gpu
 def test_lookup_of_nothing_and_of_shapes(ctx):
     table = matrix(9, 12, torch.float32, 1)
     assert ctx.embedding(table, torch.empty(0, dtype=torch.int64, device="cuda")).shape == (0, 12)
