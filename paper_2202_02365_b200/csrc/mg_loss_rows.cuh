@@ -6,7 +6,7 @@
 
 namespace mgloss {
 
-constexpr int kRowThreads = 256, kRowWarps = kRowThreads / 32;
+constexpr int kRowThreads = 256;   // (as the host side has them)
 constexpr int kRowRoom = 8;        // candidates for the best classes that shared memory has room for, for each lane of a row
 
 // A row's values in the registers of its lanes, NV vectors to each; -infinity where the row has no more.  WHOLE: rows begin and end with a vector.
