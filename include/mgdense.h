@@ -661,7 +661,8 @@ int mg_log_probs_backward(mg_ctx* ctx, const mg_logits* logits, const float* lse
 
 /* A teacher's top logits: row r has up to `entries` pairs of a class and a logit; a class outside [0, classes), -1 say, is no pair.  q = softmax over the
  * row's pairs of scale * value (the scale of the logits) or, with `lse`, exp(scale * value - lse[r]): probabilities of the whole of the teacher's
- * classes, which need not sum up to one.  mg_log_probs's top_ids and top_log_probs are such pairs. */
+ * classes, which need not sum up to one.  A value of -infinity has q = 0, and what is no pair no part in anything, whatever lse[r] is: -infinity for a row
+ * that allowed the teacher no class, NaN for padding.  mg_log_probs's top_ids and top_log_probs are such pairs. */
 typedef struct mg_teacher {
     const void* ids;         /* DEVICE [rows, entries], int32 or (ids_are_i64) int64, rows ids_stride elements apart */
     const void* values;      /* DEVICE [rows, entries] of `dtype`, rows values_stride elements apart */

@@ -141,6 +141,10 @@ struct TeacherArgs {
     int32_t entries;
 };
 
+// A teacher's value less what its probabilities are taken about.  -infinity is a probability of zero whatever that is: the lse of a row that allows the teacher no class is -infinity, that
+// of a row that is padding may be anything.
+__device__ __forceinline__ float above_shift(float v, float shift) { return v > kNegInf ? v - shift : v; }
+
 struct GradArgs {
     const void* x; int64_t stride, rows; int32_t classes; float scale;
     void* d; int64_t d_stride;

@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad_rows(const __grid
         }
         const float part = sum == 0.f ? 0.f : 1.f / sum;
         for (int k = sub; on && k < t.entries; k += LANES) {
-            q[k] = c[k] >= 0 ? expf(q[k] - shift) * part : 0.f;
+            q[k] = c[k] >= 0 ? expf(above_shift(q[k], shift)) * part : 0.f;
             mass += q[k];
         }
         mass = lanes_sum<LANES>(mass);

@@ -258,7 +258,7 @@ __global__ void __launch_bounds__(kRowThreads, row_blocks(NV * 16 / sizeof(T))) 
         for (int k = sub; on && k < t.entries; k += LANES) {
             const int32_t c = class_at(t.ids, t.ids_are_i64, r * t.ids_stride + k, a.classes);
             if (c < 0) continue;
-            const float d = a.scale * float_at(t.values, t.dtype, r * t.values_stride + k) - shift, q = expf(d) * part;
+            const float d = above_shift(a.scale * float_at(t.values, t.dtype, r * t.values_stride + k), shift), q = expf(d) * part;
             if (q != 0.f) v = fmaf(q, (d - log_sum) - res.log_p(to_float(x[c])), v);
         }
         v = lanes_sum<LANES>(v);

@@ -523,8 +523,8 @@ __device__ __forceinline__ TeacherRow teacher_row(const TeacherArgs& t, int64_t 
     const float shift = t.lse ? t.lse[r] : centre(over_warps(m, warps, scratch, [](float a, float b) { return fmaxf(a, b); }));
     float sum = 0.f;
     for (int k = threadIdx.x; k < t.entries; k += THREADS) {
-        above[k] -= shift;
-        sum += expf(above[k]);   // (0 of -infinity)
+        above[k] = above_shift(above[k], shift);   // (what is no pair stays -infinity)
+        sum += expf(above[k]);                     // (0 of -infinity)
     }
     sum = over_warps(sum, warps, scratch, [](float a, float b) { return a + b; });
     if (t.lse) return {1.f, 0.f, sum};
