@@ -8,6 +8,9 @@ namespace mgloss {
 
 constexpr int kGradThreads = 256, kGradBatch = 4;   // vectors of a thread that are on their way at once
 
+// In the place of smaller logarithms, whose probabilities are zero in fp32 (e^-104): times any gradient of the entropy, up to 1e36, it stays a number.
+constexpr float kLeastLog = -200.f;
+
 // What a row's gradient is made of: p (base + slope log p).
 struct RowGrad { float scale, minus_lse, base, slope; };
 
@@ -29,7 +32,7 @@ template <bool EXACT, int N>
 __device__ __forceinline__ void grads(const RowGrad& g, float (&v)[N]) {
     if constexpr (N == 1) {
         const float log_p = fmaf(v[0], g.scale, g.minus_lse);
-        v[0] = expf(log_p) * fmaf(fmaxf(log_p, kLeast), g.slope, g.base);
+        v[0] = expf(log_p) * fmaf(fmaxf(log_p, kLeastLog), g.slope, g.base);
     } else {
         const Pair scale = pair(g.scale, g.scale), lse = pair(g.minus_lse, g.minus_lse), base = pair(g.base, g.base), slope = pair(g.slope, g.slope);
         const bool sloped = g.slope != 0.f;
@@ -40,7 +43,7 @@ __device__ __forceinline__ void grads(const RowGrad& g, float (&v)[N]) {
             if (sloped) {
                 float a, b;
                 split(log_p, &a, &b);
-                d = mul2(p, fma2(pair(fmaxf(a, kLeast), fmaxf(b, kLeast)), slope, base));
+                d = mul2(p, fma2(pair(fmaxf(a, kLeastLog), fmaxf(b, kLeastLog)), slope, base));
             } else d = mul2(p, base);
             split(d, &v[i], &v[i + 1]);
         }
@@ -201,7 +204,7 @@ __global__ void __launch_bounds__(kGradThreads, 4) k_scores_grad_flat(const __gr
                 if (sloped) {
                     split(log_p, &s, &t);
                     const Pair slope = CROSS ? pair(first ? p.slope : q.slope, second ? p.slope : q.slope) : pair(p.slope, p.slope);
-                    factor = fma2(pair(fmaxf(s, kLeast), fmaxf(t, kLeast)), slope, factor);
+                    factor = fma2(pair(fmaxf(s, kLeastLog), fmaxf(t, kLeastLog)), slope, factor);
                 }
                 split(mul2(p_both, factor), &f[e], &f[e + 1]);
             }

@@ -1,8 +1,9 @@
-"""Rows of a teacher's that hold no pair or allow no class, with a normaliser of their own that is no number, in every kernel of the distillation."""
+"""Rows of a teacher's that hold no pair or allow no class, with a normaliser of their own that is no number, in every kernel of the distillation; gradients
+of classes that are masked."""
 import pytest
 import torch
 
-from test_scores_and_distillation import INF, TYPES, ctx, distill, distill_backward, logits_of, near  # noqa: F401
+from test_scores_and_distillation import INF, TYPES, ctx, distill, distill_backward, logits_of, near, scores_backward, some_labels  # noqa: F401
 
 NAN = float("nan")
 
@@ -61,3 +62,19 @@ def test_a_teachers_rows_without_pairs_whatever_their_normaliser(ctx, classes, d
         assert (loss[:2] == 0).all() and loss[2].isfinite()
         d = ctx.distill_backward(d_loss[:3], x[:3], lse, best.top_ids, best.top_log_probs, teacher_lse=torch.where(best.lse == -INF, best.lse, 0.0))
         assert not d[:2].any() and d[2].isfinite().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,classes,pad", [(300, 5, 0), (300, 172, 0), (33, 172, 3), (9, 1000, 1), (5, 4099, 0), (3, 50_257, 0)])
+def test_masked_classes_under_a_large_gradient_of_the_entropy(ctx, rows, classes, pad):
+    """A loss that is scaled up, or summed up far: what is not allowed still gets zero, not zero times infinity."""
+    x = logits_of(rows, classes, torch.float32, classes, pad, masked=0.3)
+    x[1:, 1] = -1e30
+    labels = some_labels(rows, classes, 3)
+    r = ctx.log_probs(x, labels)
+    for size in (1e9, 1e30):
+        h = torch.linspace(-1.0, 1.0, rows, device="cuda") * size
+        want, off = scores_backward(x, r.lse, labels, None, r.entropy, h, None, 1.0, torch.float32)
+        got = ctx.log_probs_backward(x, r.lse, labels, entropy=r.entropy, d_entropy=h)
+        near(got, want, off)
+        assert not got[x == -INF].any()
