@@ -631,15 +631,21 @@ int mg_embedding_backward(mg_ctx* ctx, const void* d_y, int64_t d_y_stride, int 
 
 /* ---- losses of a layer's output: log probabilities, distillation ------------------------------ */
 
-/* Rows of logits: z = scale * x, x of `rows` x `classes` values, rows `stride` elements apart.  Everything is computed in fp32: m = the row's largest z,
- * lse = m + log sum exp(z - m), log p_j = z_j - lse.  A logit of -infinity is a class that is not allowed.  A row that allows none has lse = -infinity, entropy 0
- * and log probabilities of -infinity; one with a NaN or +infinity has NaN for all of them.  (So has one that scale carries beyond fp32.) */
+/* Rows of logits: z = scale * x, x of `rows` x `classes` values, rows `stride` elements apart.  Everything is computed in fp32: m = the row's largest x, or
+ * a value that it lies little above, s = sum exp(scale (x - m)), lse = scale m + log s, log p_j = scale (x_j - m) - log s.  A logit of -infinity is a class
+ * that is not allowed.  A row that allows none has lse = -infinity, entropy 0 and log probabilities of -infinity; one with a NaN or +infinity has NaN for all
+ * of them.  (Where scale m is beyond fp32, lse is infinite, and the rest what it should be; a scale above 2e38 makes all of it NaN.)
+ * row_sums: mg_log_probs and mg_distill leave m and log s of each row there, and the gradients, given them, take log p by them, as above.  Without, they take it
+ * as scale x_j - lse, from the lse that they are given: its rounding makes p off by a share of itself of up to 2^-24 |lse|, which is little as long as the
+ * logits are; where |lse| nears 2^24, as in a row that a mask of -1e9 or of the type's lowest value covers all over, log s is lost from it, and every masked
+ * class has p = 1. */
 typedef struct mg_logits {
     const void* x;           /* DEVICE, aligned to its elements */
     int64_t stride, rows;
     int32_t classes;         /* 1 .. 2^28 */
     int32_t dtype;           /* MG_DTYPE_* */
     float scale;             /* 1 / temperature: positive and finite */
+    float* row_sums;         /* DEVICE [rows][2], 8-byte aligned, nullable: of the same x and scale in both directions */
 } mg_logits;
 
 #define MG_MAX_TOP 32
@@ -652,7 +658,8 @@ int mg_log_probs(mg_ctx* ctx, const mg_logits* logits, const void* labels, int l
                  int32_t* top_ids, float* top_log_probs, void* stream);
 /* Gradient with respect to x of a scalar loss, from those with respect to log_prob (g), entropy (h) and lse (l), each nullable (zero):
  *   d_x_j = scale (g [j = label] + p_j (l - g - h (log p_j + entropy))),  g of a row without a label 0,
- * with the forward call's lse and (where h is given) entropy.  A row whose gradients are all zero, or that allows no class, gets zeros, whatever it holds.
+ * with the forward call's lse or row_sums (lse is not read then, and may be NULL) and (where h is given) entropy.  A row whose gradients are all zero, or that
+ * allows no class, gets zeros, whatever it holds.
  * d_x is of the logits' type; it may be x with the same stride, or lie apart from it. */
 int mg_log_probs_backward(mg_ctx* ctx, const mg_logits* logits, const float* lse, const void* labels, int labels_are_i64, const float* d_log_prob,
                           const float* entropy, const float* d_entropy, const float* d_lse, void* d_x, int64_t d_x_stride, void* stream);
@@ -675,7 +682,7 @@ typedef struct mg_teacher {
 /* loss = sum over the row's pairs of q (log q - log p[class]), zero where there is none or q is zero; lse (nullable) as mg_log_probs's.  One kernel; streams,
  * capture and errors as mg_dropout. */
 int mg_distill(mg_ctx* ctx, const mg_logits* logits, const mg_teacher* teacher, float* loss, float* lse, void* stream);
-/* Gradient with respect to x from the loss's: d_x_j = scale d_loss (p_j sum q - sum of the q of the pairs that name j), with the forward call's lse.  A row
+/* Gradient with respect to x from the loss's: d_x_j = scale d_loss (p_j sum q - sum of the q of the pairs that name j), with the forward call's lse or row_sums.  A row
  * without pairs, with d_loss zero, or that allows no class gets zeros, whatever it holds.  d_x as mg_log_probs_backward's. */
 int mg_distill_backward(mg_ctx* ctx, const mg_logits* logits, const float* lse, const mg_teacher* teacher, const float* d_loss, void* d_x,
                         int64_t d_x_stride, void* stream);

@@ -70,7 +70,8 @@ class NormSpec(C.Structure):
 
 
 class LogitsSpec(C.Structure):
-    _fields_ = [("x", C.c_void_p), ("stride", C.c_int64), ("rows", C.c_int64), ("classes", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float)]
+    _fields_ = [("x", C.c_void_p), ("stride", C.c_int64), ("rows", C.c_int64), ("classes", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
+                ("row_sums", C.c_void_p)]
 
 
 class TeacherSpec(C.Structure):
@@ -943,9 +944,14 @@ class Context:
         return groups.ids[:n], rows[:n]
 
     # -- losses
-    def _logits(self, x: torch.Tensor, scale: float):
+    def _logits(self, x: torch.Tensor, scale: float, row_sums: torch.Tensor | None):
         x, stride = _matrix(x, self.device)
-        return x, LogitsSpec(x.data_ptr(), stride, x.shape[:-1].numel(), x.shape[-1], ROW_TYPES[x.dtype], scale)
+        spec = LogitsSpec(x.data_ptr(), stride, x.shape[:-1].numel(), x.shape[-1], ROW_TYPES[x.dtype], scale)
+        if row_sums is not None:
+            assert row_sums.device == self.device and row_sums.dtype == torch.float32, "row_sums: a float32 tensor on the context's device"
+            assert row_sums.shape == (*x.shape[:-1], 2) and row_sums.is_contiguous(), "row_sums: two values for each row, one behind the other"
+            spec.row_sums = row_sums.data_ptr()
+        return x, spec
 
     def _labels(self, labels, shape):
         if labels is None:
@@ -954,11 +960,12 @@ class Context:
         assert labels.shape == shape, "labels: one for each row"
         return labels, wide
 
-    def log_probs(self, logits: torch.Tensor, labels: torch.Tensor | None = None, top: int = 0, scale: float = 1.0) -> LogProbs:
+    def log_probs(self, logits: torch.Tensor, labels: torch.Tensor | None = None, top: int = 0, scale: float = 1.0, row_sums: torch.Tensor | None = None) -> LogProbs:
         """Of every row of logits [..., classes], with z = scale * logits: the log probability of its label (0 where the label is none of the classes, -100 say), the
         entropy, lse = log sum exp z, and the `top` likeliest classes with their log probabilities, equal ones by ascending class.  fp32, queued on torch's
-        current stream.  A logit of -infinity is a class that is not allowed.  The gradients are log_probs_backward's."""
-        x, spec = self._logits(logits, scale)
+        current stream.  A logit of -infinity is a class that is not allowed.  The gradients are log_probs_backward's; row_sums, a contiguous float32 tensor [..., 2], is
+        filled for them."""
+        x, spec = self._logits(logits, scale, row_sums)
         shape = x.shape[:-1]
         labels, wide = self._labels(labels, shape)
         block = torch.empty((2 if labels is None else 3, *shape), dtype=torch.float32, device=self.device).unbind(0)
@@ -969,12 +976,14 @@ class Context:
                                           torch._C._cuda_getCurrentRawStream(self.device.index)))
         return LogProbs(log_prob, block[0], block[1], ids, best)
 
-    def log_probs_backward(self, logits: torch.Tensor, lse: torch.Tensor, labels: torch.Tensor | None = None, d_log_prob: torch.Tensor | None = None,
+    def log_probs_backward(self, logits: torch.Tensor, lse: torch.Tensor | None, labels: torch.Tensor | None = None, d_log_prob: torch.Tensor | None = None,
                            entropy: torch.Tensor | None = None, d_entropy: torch.Tensor | None = None, d_lse: torch.Tensor | None = None, scale: float = 1.0,
-                           out: torch.Tensor | None = None) -> torch.Tensor:
+                           out: torch.Tensor | None = None, row_sums: torch.Tensor | None = None) -> torch.Tensor:
         """Gradient of a loss with respect to the logits from those with respect to log_prob, entropy and lse (a value for each row, or None); lse and (for
-        d_entropy) entropy as log_probs gave them.  out may be the logits."""
-        x, spec = self._logits(logits, scale)
+        d_entropy) entropy as log_probs gave them.  out may be the logits.  Probabilities by lse are off by a share of themselves of up to 2^-24 |lse|, and wrong where a
+        mask of -1e9, say, or of the type's lowest value covers a row all over; by row_sums, as log_probs or distill filled them for these logits and this scale, they
+        are as exact as the forward call's (lse may then be None)."""
+        x, spec = self._logits(logits, scale, row_sums)
         shape = x.shape[:-1]
         labels, wide = self._labels(labels, shape)
         lse, g, h, l = (_by_row(t, shape, self.device, what) for t, what in ((lse, "lse"), (d_log_prob, "d_log_prob"), (d_entropy, "d_entropy"), (d_lse, "d_lse")))
@@ -995,23 +1004,25 @@ class Context:
                            ROW_TYPES[values.dtype], ids.shape[-1])
         return spec, (ids, values, lse)
 
-    def distill(self, logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, scale: float = 1.0, teacher_lse: torch.Tensor | None = None):
+    def distill(self, logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor, scale: float = 1.0, teacher_lse: torch.Tensor | None = None,
+                row_sums: torch.Tensor | None = None):
         """(loss, lse) of every row of logits [..., classes] against a teacher's top logits: teacher_ids, teacher_logits [..., entries] (log_probs's top_ids and
         top_log_probs, say; a class that is none, -1, is no entry).  q = softmax of scale * teacher_logits over the entries (with teacher_lse: exp(scale *
         teacher_logits - teacher_lse), the teacher's probabilities as they are), loss = sum q (log q - log p), p = softmax of scale * logits.  A temperature T is a
-        scale of 1 / T.  fp32, queued on torch's current stream; the gradient is distill_backward's."""
-        x, spec = self._logits(logits, scale)
+        scale of 1 / T.  fp32, queued on torch's current stream; the gradient is distill_backward's, for which row_sums is filled as by log_probs."""
+        x, spec = self._logits(logits, scale, row_sums)
         shape = x.shape[:-1]
         teacher, held = self._teacher(teacher_ids, teacher_logits, teacher_lse, shape)
         loss, lse = torch.empty((2, *shape), dtype=torch.float32, device=self.device).unbind(0)
         self._check(self.lib.mg_distill(self.handle, C.byref(spec), C.byref(teacher), loss.data_ptr(), lse.data_ptr(), torch._C._cuda_getCurrentRawStream(self.device.index)))
         return loss, lse
 
-    def distill_backward(self, d_loss: torch.Tensor, logits: torch.Tensor, lse: torch.Tensor, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor,
-                         scale: float = 1.0, teacher_lse: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
-        """Gradient of distill's loss with respect to the logits, from the loss's (a value for each row); lse and the rest as in the forward call.  out may be
-        the logits."""
-        x, spec = self._logits(logits, scale)
+    def distill_backward(self, d_loss: torch.Tensor, logits: torch.Tensor, lse: torch.Tensor | None, teacher_ids: torch.Tensor, teacher_logits: torch.Tensor,
+                         scale: float = 1.0, teacher_lse: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                         row_sums: torch.Tensor | None = None) -> torch.Tensor:
+        """Gradient of distill's loss with respect to the logits, from the loss's (a value for each row); lse, row_sums (see log_probs_backward) and the rest as in the
+        forward call.  out may be the logits."""
+        x, spec = self._logits(logits, scale, row_sums)
         shape = x.shape[:-1]
         teacher, held = self._teacher(teacher_ids, teacher_logits, teacher_lse, shape)
         lse, d_loss = _by_row(lse, shape, self.device, "lse"), _by_row(d_loss, shape, self.device, "d_loss")

@@ -6,6 +6,8 @@ namespace {
 
 using namespace mgloss;
 
+float2* row_sums_of(const mg_logits* z) { return reinterpret_cast<float2*>(z->row_sums); }
+
 TeacherArgs teacher_args(const mg_teacher* t) { return {t->ids, t->values, t->lse, t->ids_stride, t->values_stride, t->ids_are_i64, t->dtype, t->entries}; }
 
 // forward passes of both operators; `t`: distillation
@@ -42,7 +44,7 @@ extern "C" int mg_log_probs(mg_ctx* ctx, const mg_logits* z, const void* labels,
     if (!ctx) return MG_ERR_ARG;
     if (int rc = check_log_probs(ctx, z, labels, labels_are_i64, top, log_prob, entropy, lse, top_ids, top_log_probs)) return rc;
     if (z->rows == 0) return MG_OK;
-    const ScoreArgs a{z->x, z->stride, z->rows, z->classes, z->scale, z->scale * kLog2e, labels, labels_are_i64, top_ids || top_log_probs ? top : 0, log_prob, entropy, lse, top_ids, top_log_probs};
+    const ScoreArgs a{z->x, z->stride, z->rows, z->classes, z->scale, z->scale * kLog2e, labels, labels_are_i64, top_ids || top_log_probs ? top : 0, log_prob, entropy, lse, top_ids, top_log_probs, row_sums_of(z)};
     return run_forward(ctx, z, a, nullptr, nullptr, (cudaStream_t)stream);
 }
 
@@ -51,7 +53,7 @@ extern "C" int mg_log_probs_backward(mg_ctx* ctx, const mg_logits* z, const floa
     if (!ctx) return MG_ERR_ARG;
     if (int rc = check_log_probs_backward(ctx, z, lse, labels, labels_are_i64, d_log_prob, entropy, d_entropy, d_lse, d_x, d_x_stride)) return rc;
     if (z->rows == 0) return MG_OK;
-    const GradArgs a{z->x, z->stride, z->rows, z->classes, z->scale, d_x, d_x_stride, lse, labels, labels_are_i64, d_log_prob, entropy, d_entropy, d_lse, {}, nullptr};
+    const GradArgs a{z->x, z->stride, z->rows, z->classes, z->scale, d_x, d_x_stride, lse, labels, labels_are_i64, d_log_prob, entropy, d_entropy, d_lse, {}, nullptr, row_sums_of(z)};
     return run_backward(ctx, z, a, false, (cudaStream_t)stream);
 }
 
@@ -59,7 +61,7 @@ extern "C" int mg_distill(mg_ctx* ctx, const mg_logits* z, const mg_teacher* tea
     if (!ctx) return MG_ERR_ARG;
     if (int rc = check_distill(ctx, z, teacher, loss, lse)) return rc;
     if (z->rows == 0) return MG_OK;
-    const ScoreArgs a{z->x, z->stride, z->rows, z->classes, z->scale, z->scale * kLog2e, nullptr, 0, 0, nullptr, nullptr, lse, nullptr, nullptr};
+    const ScoreArgs a{z->x, z->stride, z->rows, z->classes, z->scale, z->scale * kLog2e, nullptr, 0, 0, nullptr, nullptr, lse, nullptr, nullptr, row_sums_of(z)};
     return run_forward(ctx, z, a, teacher, loss, (cudaStream_t)stream);
 }
 
@@ -68,6 +70,6 @@ extern "C" int mg_distill_backward(mg_ctx* ctx, const mg_logits* z, const float*
     if (!ctx) return MG_ERR_ARG;
     if (int rc = check_distill_backward(ctx, z, lse, teacher, d_loss, d_x, d_x_stride)) return rc;
     if (z->rows == 0) return MG_OK;
-    const GradArgs a{z->x, z->stride, z->rows, z->classes, z->scale, d_x, d_x_stride, lse, nullptr, 0, nullptr, nullptr, nullptr, nullptr, teacher_args(teacher), d_loss};
+    const GradArgs a{z->x, z->stride, z->rows, z->classes, z->scale, d_x, d_x_stride, lse, nullptr, 0, nullptr, nullptr, nullptr, nullptr, teacher_args(teacher), d_loss, row_sums_of(z)};
     return run_backward(ctx, z, a, true, (cudaStream_t)stream);
 }

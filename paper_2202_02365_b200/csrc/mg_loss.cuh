@@ -125,6 +125,7 @@ struct RowResult {
         lse = fmaf(scale, max, log_sum);
     }
     __device__ __forceinline__ float log_p(float x) const { return none ? kNegInf : scale * (x - max) - log_sum; }
+    __device__ __forceinline__ float2 sums() const { return make_float2(max, log_sum); }   // (no class is allowed: log_sum is -infinity)
 };
 
 struct ScoreArgs {
@@ -132,6 +133,7 @@ struct ScoreArgs {
     const void* labels; int labels_are_i64;
     int32_t top;
     float *log_prob, *entropy, *lse; int32_t* top_ids; float* top_log_probs;
+    float2* row_sums;
 };
 
 struct TeacherArgs {
@@ -153,6 +155,7 @@ struct GradArgs {
     const float *d_log_prob, *entropy, *d_entropy, *d_lse;
     TeacherArgs teacher;                      // distillation
     const float* d_loss;
+    const float2* row_sums;                   // in the place of lse, where there are
 };
 
 }  // namespace mgloss

@@ -7,8 +7,8 @@ namespace mgloss {
 
 template <typename T, int NV, int LANES>
 static void launch_rows(const ForwardLaunch& l, const ScoreArgs& a, const TeacherArgs& t, float* loss, cudaStream_t st) {
-    if (l.whole) k_distill_rows<T, NV, LANES, true><<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a, t, loss);
-    else k_distill_rows<T, NV, LANES, false><<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a, t, loss);
+    const auto go = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a, t, loss); };
+    a.row_sums ? go(k_distill_rows<T, NV, LANES, false, true>) : l.whole ? go(k_distill_rows<T, NV, LANES, true, false>) : go(k_distill_rows<T, NV, LANES, false, false>);
 }
 
 template <typename T, int THREADS>

@@ -11,8 +11,24 @@ constexpr int kGradThreads = 256, kGradBatch = 4;   // vectors of a thread that 
 // In the place of smaller logarithms, whose probabilities are zero in fp32 (e^-104): times any gradient of the entropy, up to 1e36, it stays a number.
 constexpr float kLeastLog = -200.f;
 
-// What a row's gradient is made of: p (base + slope log p).
-struct RowGrad { float scale, minus_lse, base, slope; };
+// What a row's gradient is made of: p (base + slope log p), log p = scale (x - about) + minus_lse (ABOUT), or without `about`: kernels of their own, since the difference and its register cost those
+// that do without up to 7 %.
+struct RowGrad { float scale, about, minus_lse, base, slope; };
+
+// What the forward call has left of a row: what its sum of exponentials was taken about and the sum's logarithm, or one number for both, of which a large one has lost the second.
+// (As they are loaded: an operation on them here holds the loads behind them up; 777,777 fp16 rows of 153 107 us, 111.)
+struct RowLog {
+    float about, lse;
+    __device__ __forceinline__ bool none() const { return lse == kNegInf; }   // no class is allowed
+};
+template <bool ABOUT>
+__device__ __forceinline__ RowLog row_log(const GradArgs& a, int64_t r) {
+    if (ABOUT) {
+        const float2 s = a.row_sums[r];
+        return {s.x, s.y};
+    }
+    return {0.f, a.lse[r]};
+}
 
 // The exponentials of two logarithms of probabilities.  Of fp32 rows by expf: the special function unit's power of two is as many units of 2^-24 off as the logarithm has (three times
 // the plain form's error over a gradient), which the rounding to two bytes covers.  2,048 rows of 50,257 take as long.
@@ -28,17 +44,19 @@ __device__ __forceinline__ Pair exp_of(Pair log_p) {
 }
 
 // the gradients of neighbouring classes, in place of their logits
-template <bool EXACT, int N>
+template <bool EXACT, bool ABOUT, int N>
 __device__ __forceinline__ void grads(const RowGrad& g, float (&v)[N]) {
     if constexpr (N == 1) {
-        const float log_p = fmaf(v[0], g.scale, g.minus_lse);
+        const float log_p = fmaf(ABOUT ? v[0] - g.about : v[0], g.scale, g.minus_lse);
         v[0] = expf(log_p) * fmaf(fmaxf(log_p, kLeastLog), g.slope, g.base);
     } else {
-        const Pair scale = pair(g.scale, g.scale), lse = pair(g.minus_lse, g.minus_lse), base = pair(g.base, g.base), slope = pair(g.slope, g.slope);
+        const Pair scale = pair(g.scale, g.scale), about = pair(-g.about, -g.about), lse = pair(g.minus_lse, g.minus_lse), base = pair(g.base, g.base), slope = pair(g.slope, g.slope);
         const bool sloped = g.slope != 0.f;
 #pragma unroll
         for (int i = 0; i < N; i += 2) {
-            const Pair log_p = fma2(pair(v[i], v[i + 1]), scale, lse), p = exp_of<EXACT>(log_p);
+            Pair x = pair(v[i], v[i + 1]);
+            if (ABOUT) x = add2(x, about);
+            const Pair log_p = fma2(x, scale, lse), p = exp_of<EXACT>(log_p);
             Pair d;
             if (sloped) {
                 float a, b;
@@ -51,10 +69,10 @@ __device__ __forceinline__ void grads(const RowGrad& g, float (&v)[N]) {
 }
 
 // one class's gradient, and `more`
-template <typename T>
+template <bool ABOUT, typename T>
 __device__ __forceinline__ void write_one(const RowGrad& g, float x, float more, T* to) {
     float f[1] = {x};
-    grads<true>(g, f);
+    grads<true, ABOUT>(g, f);
     f[0] += more;
     Raw<T, 1> one;
     one.put(f);
@@ -64,7 +82,7 @@ __device__ __forceinline__ void write_one(const RowGrad& g, float x, float more,
 // Vectors [lo, hi) of what covers the gradient's row, by `lanes` threads.  WHOLE: rows of both begin and end with a vector; SAME: the logits' vectors begin where the
 // gradient's do, else they are read element by element (2,048 fp32 rows of 50,257: 135 us, with logits that begin elsewhere 140; 4,096 bf16 ones 154 and 195).
 // Bound by the bytes: 824 MB in 139 us, 92 % of the copy's rate, with a teacher's pairs.
-template <bool SAME, bool WHOLE, typename T>
+template <bool ABOUT, bool SAME, bool WHOLE, typename T>
 __device__ __forceinline__ void stream_row(const RowGrad& g, bool zero, const T* x, T* d, int32_t classes, int32_t lead, int32_t lo, int32_t hi, int sub, int lanes) {
     constexpr int VEC = 16 / sizeof(T);
     for (int32_t v0 = lo + sub; v0 < hi; v0 += kGradBatch * lanes) {
@@ -100,7 +118,7 @@ __device__ __forceinline__ void stream_row(const RowGrad& g, bool zero, const T*
             if (zero) {
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) f[e] = 0.f;
-            } else grads<sizeof(T) == 4>(g, f);
+            } else grads<sizeof(T) == 4, ABOUT>(g, f);
             raw[j].put(f);
             if (full) raw[j].store(d + c);
             else
@@ -117,7 +135,7 @@ __device__ __forceinline__ void stream_row(const RowGrad& g, bool zero, const T*
 }
 
 // `lanes` threads to a row, or to one of its `chunks` pieces.  The label's gradient is written over what its vector got, by the thread that had the vector.
-template <typename T, bool SAME, bool WHOLE>
+template <typename T, bool ABOUT, bool SAME, bool WHOLE>
 __global__ void __launch_bounds__(kGradThreads) k_scores_grad(const __grid_constant__ GradArgs a, int lanes_log2, int chunks, int32_t piece) {
     constexpr int VEC = 16 / sizeof(T);
     const int lanes = 1 << lanes_log2, group = (int)threadIdx.x >> lanes_log2, sub = (int)threadIdx.x & (lanes - 1), groups = kGradThreads >> lanes_log2;
@@ -129,17 +147,17 @@ __global__ void __launch_bounds__(kGradThreads) k_scores_grad(const __grid_const
         const Cover<VEC> cover(d, sizeof(T), a.classes, WHOLE);
         int32_t lo = 0, hi = cover.vecs;
         if (chunks > 1) { lo = min(chunk * piece, cover.vecs); hi = min(lo + piece, cover.vecs); }
-        const float lse = a.lse[r];
+        const RowLog of = row_log<ABOUT>(a, r);
         const int32_t label = a.d_log_prob ? class_at(a.labels, a.labels_are_i64, r, a.classes) : -1;
         const float of_label = label >= 0 ? a.d_log_prob[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f, l = a.d_lse ? a.d_lse[r] : 0.f;
         const float entropy = h != 0.f ? a.entropy[r] : 0.f;
-        const bool zero = (of_label == 0.f && h == 0.f && l == 0.f) || lse == kNegInf;
-        const RowGrad g{a.scale, -lse, a.scale * (l - of_label - h * entropy), -a.scale * h};
+        const bool zero = (of_label == 0.f && h == 0.f && l == 0.f) || of.none();
+        const RowGrad g{a.scale, of.about, -of.lse, a.scale * (l - of_label - h * entropy), -a.scale * h};
         const int32_t at = (label + cover.lead) / VEC;
         const bool mine = label >= 0 && !zero && at >= lo && at < hi && ((at - lo) & (lanes - 1)) == sub;
         const float x_label = mine ? to_float(x[label]) : 0.f;
-        stream_row<SAME, WHOLE>(g, zero, x, d, a.classes, cover.lead, lo, hi, sub, lanes);
-        if (mine) write_one(g, x_label, a.scale * of_label, d + label);
+        stream_row<ABOUT, SAME, WHOLE>(g, zero, x, d, a.classes, cover.lead, lo, hi, sub, lanes);
+        if (mine) write_one<ABOUT>(g, x_label, a.scale * of_label, d + label);
     }
 }
 
@@ -149,10 +167,11 @@ __global__ void __launch_bounds__(kGradThreads) k_scores_grad(const __grid_const
 // bounds it are the latencies at a block's beginning and end; vectors are asked for before the rows' values.
 struct FlatRow { float minus_lse, base, slope; int32_t zero; };
 constexpr int kFlatRows = 256;   // a block's, at most
-template <typename T, bool CROSS>
+template <typename T, bool CROSS, bool ABOUT>
 __global__ void __launch_bounds__(kGradThreads, 4) k_scores_grad_flat(const __grid_constant__ GradArgs a, int rows_each, uint32_t reciprocal) {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ FlatRow params[kFlatRows + 1];
+    __shared__ float minus_about[ABOUT ? kFlatRows + 1 : 1];
     const int64_t r0 = (int64_t)blockIdx.x * rows_each;
     const int rows = (int)min((int64_t)rows_each, a.rows - r0);
     const T* x = static_cast<const T*>(a.x) + r0 * a.classes;
@@ -164,19 +183,21 @@ __global__ void __launch_bounds__(kGradThreads, 4) k_scores_grad_flat(const __gr
         if ((int)threadIdx.x + j * kGradThreads < vecs) raw[j] = reinterpret_cast<const uint4*>(x)[threadIdx.x + j * kGradThreads];
     int32_t label = -1;
     float x_label = 0.f, more = 0.f;
-    RowGrad own{a.scale, 0.f, 0.f, 0.f};
+    RowGrad own{a.scale, 0.f, 0.f, 0.f, 0.f};
     if ((int)threadIdx.x < rows) {
         const int64_t r = r0 + threadIdx.x;
-        const float lse = a.lse[r], of_label = a.d_log_prob ? a.d_log_prob[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f, l = a.d_lse ? a.d_lse[r] : 0.f;
+        const RowLog of = row_log<ABOUT>(a, r);
+        const float of_label = a.d_log_prob ? a.d_log_prob[r] : 0.f, h = a.d_entropy ? a.d_entropy[r] : 0.f, l = a.d_lse ? a.d_lse[r] : 0.f;
         const float entropy = a.d_entropy ? a.entropy[r] : 0.f;
         if (a.d_log_prob) label = class_at(a.labels, a.labels_are_i64, r, a.classes);
         if (label >= 0) x_label = to_float(x[(int64_t)threadIdx.x * a.classes + label]);
         const float g = label >= 0 ? of_label : 0.f;
-        const bool zero = (g == 0.f && h == 0.f && l == 0.f) || lse == kNegInf;
-        own.minus_lse = -lse; own.base = a.scale * (l - g - (h != 0.f ? h * entropy : 0.f)); own.slope = -a.scale * h;
+        const bool zero = (g == 0.f && h == 0.f && l == 0.f) || of.none();
+        own.about = of.about; own.minus_lse = -of.lse; own.base = a.scale * (l - g - (h != 0.f ? h * entropy : 0.f)); own.slope = -a.scale * h;
         more = a.scale * g;
         if (zero) label = -1;
         params[threadIdx.x] = {own.minus_lse, own.base, own.slope, zero};
+        if (ABOUT) minus_about[threadIdx.x] = -own.about;
     }
     __syncthreads();
     const bool sloped = a.d_entropy != nullptr;
@@ -190,6 +211,11 @@ __global__ void __launch_bounds__(kGradThreads, 4) k_scores_grad_flat(const __gr
             const FlatRow p = params[row];
             FlatRow q = p;
             if (CROSS && left < VEC) q = params[row + 1];   // (there is one: the block's values end behind the vector)
+            float p_about = 0.f, q_about = 0.f;
+            if (ABOUT) {
+                p_about = q_about = minus_about[row];
+                if (CROSS && left < VEC) q_about = minus_about[row + 1];
+            }
             Raw<T, VEC> one;
             one.w[0] = raw[j].x; one.w[1] = raw[j].y; one.w[2] = raw[j].z; one.w[3] = raw[j].w;
             if (v + kGradBatch * kGradThreads < vecs) raw[j] = reinterpret_cast<const uint4*>(x)[v + kGradBatch * kGradThreads];
@@ -199,7 +225,9 @@ __global__ void __launch_bounds__(kGradThreads, 4) k_scores_grad_flat(const __gr
                 const bool first = !CROSS || e < left, second = !CROSS || e + 1 < left;
                 const Pair lse = CROSS ? pair(first ? p.minus_lse : q.minus_lse, second ? p.minus_lse : q.minus_lse) : pair(p.minus_lse, p.minus_lse);
                 Pair factor = CROSS ? pair(first ? p.base : q.base, second ? p.base : q.base) : pair(p.base, p.base);
-                const Pair log_p = fma2(pair(one.get(e), one.get(e + 1)), scale, lse), p_both = exp_of<sizeof(T) == 4>(log_p);
+                Pair x_both = pair(one.get(e), one.get(e + 1));
+                if (ABOUT) x_both = add2(x_both, CROSS ? pair(first ? p_about : q_about, second ? p_about : q_about) : pair(p_about, p_about));
+                const Pair log_p = fma2(x_both, scale, lse), p_both = exp_of<sizeof(T) == 4>(log_p);
                 float s, t;
                 if (sloped) {
                     split(log_p, &s, &t);
@@ -222,10 +250,10 @@ __global__ void __launch_bounds__(kGradThreads, 4) k_scores_grad_flat(const __gr
         const int32_t at = vecs * VEC + (int32_t)threadIdx.x;
         const FlatRow p = params[rows - 1];   // (less than a vector, and a row has one at least)
         if (p.zero) { Raw<T, 1> none; none.zero(); none.store(d + at); }
-        else write_one({a.scale, p.minus_lse, p.base, p.slope}, to_float(x[at]), 0.f, d + at);
+        else write_one<ABOUT>({a.scale, ABOUT ? -minus_about[rows - 1] : 0.f, p.minus_lse, p.base, p.slope}, to_float(x[at]), 0.f, d + at);
     }
     __syncthreads();
-    if (label >= 0) write_one(own, x_label, more, d + (int64_t)threadIdx.x * a.classes + label);
+    if (label >= 0) write_one<ABOUT>(own, x_label, more, d + (int64_t)threadIdx.x * a.classes + label);
 }
 
 // Where a teacher's pairs name a class, its gradient is made apart: from the logit, which is read before anything is written (the gradient may take the logits' place),
@@ -245,7 +273,7 @@ __device__ __forceinline__ bool first_of_class(const int32_t* c, const float* q,
 
 constexpr int kTeacherRoom = 8;   // pairs that a row of the narrow kernel may have, for each of its lanes
 
-template <typename T, int LANES, bool SAME, bool WHOLE>
+template <typename T, int LANES, bool ABOUT, bool SAME, bool WHOLE>
 __global__ void __launch_bounds__(kGradThreads) k_distill_grad_rows(const __grid_constant__ GradArgs a) {
     constexpr int GROUPS = kGradThreads / LANES;
     __shared__ int32_t all_c[kGradThreads * kTeacherRoom];
@@ -259,7 +287,8 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad_rows(const __grid
         const bool on = r < a.rows;
         const T* x = static_cast<const T*>(a.x) + (on ? r : 0) * a.stride;
         T* d = static_cast<T*>(a.d) + (on ? r : 0) * a.d_stride;
-        const float lse = on ? a.lse[r] : 0.f, d_loss = on ? a.d_loss[r] : 0.f;
+        const RowLog of = row_log<ABOUT>(a, on ? r : 0);
+        const float d_loss = on ? a.d_loss[r] : 0.f;
         // the pairs' classes, values (times the scale) and logits
         float m = kNegInf, shift, sum = 1.f, mass = 0.f;
         for (int k = sub; on && k < t.entries; k += LANES) {
@@ -283,22 +312,22 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad_rows(const __grid
             mass += q[k];
         }
         mass = lanes_sum<LANES>(mass);
-        const bool zero = d_loss == 0.f || mass == 0.f || lse == kNegInf;
-        const RowGrad g{a.scale, -lse, a.scale * d_loss * mass, 0.f};
+        const bool zero = d_loss == 0.f || mass == 0.f || of.none();
+        const RowGrad g{a.scale, of.about, -of.lse, a.scale * d_loss * mass, 0.f};
         __syncwarp();
         const Cover<16 / sizeof(T)> cover(d, sizeof(T), a.classes, WHOLE);
-        if (on) stream_row<SAME, WHOLE>(g, zero, x, d, a.classes, cover.lead, 0, cover.vecs, sub, LANES);
+        if (on) stream_row<ABOUT, SAME, WHOLE>(g, zero, x, d, a.classes, cover.lead, 0, cover.vecs, sub, LANES);
         __syncwarp();
         for (int k = sub; on && !zero && k < t.entries; k += LANES) {
             float of_class;
-            if (first_of_class(c, q, k, t.entries, &of_class)) write_one(g, at_class[k], -a.scale * d_loss * of_class, d + c[k]);
+            if (first_of_class(c, q, k, t.entries, &of_class)) write_one<ABOUT>(g, at_class[k], -a.scale * d_loss * of_class, d + c[k]);
         }
         __syncwarp();
     }
 }
 
 // a block to a row, or to one of its `chunks` pieces
-template <typename T, bool SAME, bool WHOLE>
+template <typename T, bool ABOUT, bool SAME, bool WHOLE>
 __global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_constant__ GradArgs a, int chunks, int32_t piece) {
     constexpr int VEC = 16 / sizeof(T);
     __shared__ int32_t c[MG_MAX_TEACHER];
@@ -308,7 +337,8 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_cons
     const int32_t chunk = (int32_t)(blockIdx.x - (unsigned)r * (unsigned)chunks);
     const T* x = static_cast<const T*>(a.x) + r * a.stride;
     T* d = static_cast<T*>(a.d) + r * a.d_stride;
-    const float lse = a.lse[r], d_loss = a.d_loss[r];
+    const RowLog of = row_log<ABOUT>(a, r);
+    const float d_loss = a.d_loss[r];
     const Cover<VEC> cover(d, sizeof(T), a.classes, WHOLE);
     const int32_t lo = min(chunk * piece, cover.vecs), hi = min(lo + piece, cover.vecs);
     const int warps = teacher_warps<kTeacherThreads>(t);
@@ -320,14 +350,14 @@ __global__ void __launch_bounds__(kGradThreads) k_distill_grad(const __grid_cons
     }
     __syncthreads();
     const float mass = sh_mass;
-    const bool zero = d_loss == 0.f || mass == 0.f || lse == kNegInf;
-    const RowGrad g{a.scale, -lse, a.scale * d_loss * mass, 0.f};
-    stream_row<SAME, WHOLE>(g, zero, x, d, a.classes, cover.lead, lo, hi, (int)threadIdx.x, kGradThreads);
+    const bool zero = d_loss == 0.f || mass == 0.f || of.none();
+    const RowGrad g{a.scale, of.about, -of.lse, a.scale * d_loss * mass, 0.f};
+    stream_row<ABOUT, SAME, WHOLE>(g, zero, x, d, a.classes, cover.lead, lo, hi, (int)threadIdx.x, kGradThreads);
     __syncthreads();
     if (zero || (int)threadIdx.x >= warps * 32) return;
     for (int k = threadIdx.x; k < t.entries; k += kTeacherThreads) {
         float of_class;
-        if (here(c[k]) && first_of_class(c, q, k, t.entries, &of_class)) write_one(g, at_class[k], -a.scale * d_loss * of_class, d + c[k]);
+        if (here(c[k]) && first_of_class(c, q, k, t.entries, &of_class)) write_one<ABOUT>(g, at_class[k], -a.scale * d_loss * of_class, d + c[k]);
     }
 }
 

@@ -21,6 +21,7 @@ inline int check_logits(mg_ctx* ctx, const mg_logits* z) {
     if (z->rows < 0 || z->rows >= 1ll << 31) return mg_fail(ctx, MG_ERR_ARG, "the number of rows must be in [0, 2^31)");
     if (z->classes < 1 || z->classes > 1 << 28) return mg_fail(ctx, MG_ERR_ARG, "the number of classes must be in [1, 2^28]");
     if (!(z->scale > 0.f) || isinf(z->scale)) return mg_fail(ctx, MG_ERR_ARG, "the scale must be positive and finite");
+    if (reinterpret_cast<uintptr_t>(z->row_sums) % 8) return mg_fail(ctx, MG_ERR_ARG, "row_sums must be 8-byte aligned");
     return check_matrix(ctx, "the logits", z->x, z->stride, z->dtype, z->rows, z->classes, false);
 }
 
@@ -30,7 +31,7 @@ inline int check_labels(mg_ctx* ctx, const void* labels, int labels_are_i64) {
 }
 
 inline int check_gradient(mg_ctx* ctx, const mg_logits* z, const float* lse, const void* d_x, int64_t d_x_stride) {
-    if (z->rows > 0 && !lse) return mg_fail(ctx, MG_ERR_ARG, "null lse");
+    if (z->rows > 0 && !lse && !z->row_sums) return mg_fail(ctx, MG_ERR_ARG, "null lse");
     if (int rc = check_matrix(ctx, "d_x", d_x, d_x_stride, z->dtype, z->rows, z->classes, true)) return rc;
     return check_apart(ctx, "the logits", z->x, z->stride, d_x, d_x_stride, z->dtype, z->rows, z->classes);
 }

@@ -141,10 +141,11 @@ __device__ __forceinline__ void best_of(const HeldRow<T, NV, LANES, WHOLE>& row,
     best_one_by_one<T, LANES>(x, classes, sub, slow && on, r.max, r.log_sum, r.scale, r.none, top, ids, log_probs);
 }
 
+// (KEEP: the row's sums are asked for.  A question to each row instead costs those that they are not asked of up to 3 %, by the few instructions and where the compiler then puts the others.)
 // (blocks to an SM: what the values to a lane leave registers for)
 constexpr int row_blocks(int values) { return values <= 8 ? 5 : values <= 24 ? 4 : 3; }
 
-template <typename T, int NV, int LANES, bool WHOLE>
+template <typename T, int NV, int LANES, bool WHOLE, bool KEEP>
 __global__ void __launch_bounds__(kRowThreads, row_blocks(NV * 16 / sizeof(T))) k_scores_rows(const __grid_constant__ ScoreArgs a) {
     constexpr int GROUPS = kRowThreads / LANES;
     __shared__ uint64_t room[kRowThreads * kRowRoom];
@@ -163,6 +164,7 @@ __global__ void __launch_bounds__(kRowThreads, row_blocks(NV * 16 / sizeof(T))) 
             if (a.lse) a.lse[r] = res.lse;
             if (a.entropy) a.entropy[r] = res.entropy;
             if (a.log_prob) a.log_prob[r] = label >= 0 ? res.log_p(at_label) : 0.f;
+            if (KEEP) a.row_sums[r] = res.sums();
         }
         if (a.top)
             best_of(row, x, a.classes, own, sub, on, res, a.top, a.top_ids ? a.top_ids + r * a.top : nullptr, a.top_log_probs ? a.top_log_probs + r * a.top : nullptr,
@@ -172,7 +174,7 @@ __global__ void __launch_bounds__(kRowThreads, row_blocks(NV * 16 / sizeof(T))) 
 
 // Rows of up to 32 classes where there are many: a thread to a row.  The best of its values by going over them once for each, as whole numbers of the same order (zero: taken).
 // Few classes leave lanes idle and cost as many steps across them as many do.  800,000 fp32 rows of 5 with the best one 22 us (by eight lanes 103), of 20 with five 60 us (173).
-template <typename T, int MOST, bool WHOLE>
+template <typename T, int MOST, bool WHOLE, bool KEEP>
 __global__ void __launch_bounds__(kRowThreads) k_scores_tiny(const __grid_constant__ ScoreArgs a) {
     constexpr int VEC = 16 / sizeof(T);
     const int64_t r = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
@@ -207,6 +209,7 @@ __global__ void __launch_bounds__(kRowThreads) k_scores_tiny(const __grid_consta
         const int32_t label = class_at(a.labels, a.labels_are_i64, r, a.classes);
         a.log_prob[r] = label >= 0 ? res.log_p(to_float(x[label])) : 0.f;
     }
+    if (KEEP) a.row_sums[r] = res.sums();
     if (!a.top) return;
     uint32_t order[MOST];
 #pragma unroll
@@ -239,7 +242,7 @@ __device__ __forceinline__ void teacher_sums(const TeacherArgs& t, int64_t r, bo
     *shift = m; *sum = lanes_sum<LANES>(s);
 }
 
-template <typename T, int NV, int LANES, bool WHOLE>
+template <typename T, int NV, int LANES, bool WHOLE, bool KEEP>
 __global__ void __launch_bounds__(kRowThreads, row_blocks(NV * 16 / sizeof(T))) k_distill_rows(const __grid_constant__ ScoreArgs a, const __grid_constant__ TeacherArgs t, float* loss) {
     constexpr int GROUPS = kRowThreads / LANES;
     const int group = (int)threadIdx.x / LANES, sub = (int)threadIdx.x % LANES;
@@ -265,6 +268,7 @@ __global__ void __launch_bounds__(kRowThreads, row_blocks(NV * 16 / sizeof(T))) 
         if (on && sub == 0) {
             loss[r] = v;
             if (a.lse) a.lse[r] = res.lse;
+            if (KEEP) a.row_sums[r] = res.sums();
         }
     }
 }

@@ -7,8 +7,8 @@ namespace mgloss {
 
 template <typename T, int NV, int LANES>
 static void launch_rows(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t st) {
-    if (l.whole) k_scores_rows<T, NV, LANES, true><<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a);
-    else k_scores_rows<T, NV, LANES, false><<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a);
+    const auto go = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a); };
+    a.row_sums ? go(k_scores_rows<T, NV, LANES, false, true>) : l.whole ? go(k_scores_rows<T, NV, LANES, true, false>) : go(k_scores_rows<T, NV, LANES, false, false>);
 }
 
 template <typename T, int THREADS>
@@ -19,8 +19,8 @@ static void launch_wide(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t
 
 template <typename T, int MOST>
 static void launch_tiny(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t st) {
-    if (l.whole) k_scores_tiny<T, MOST, true><<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a);
-    else k_scores_tiny<T, MOST, false><<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a);
+    const auto go = [&](auto kernel) { kernel<<<(unsigned)l.blocks, kRowThreads, 0, st>>>(a); };
+    a.row_sums ? go(k_scores_tiny<T, MOST, false, true>) : l.whole ? go(k_scores_tiny<T, MOST, true, false>) : go(k_scores_tiny<T, MOST, false, false>);
 }
 
 void launch_scores(const ForwardLaunch& l, const ScoreArgs& a, cudaStream_t st) {

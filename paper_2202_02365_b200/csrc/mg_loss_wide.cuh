@@ -474,6 +474,7 @@ __global__ void __launch_bounds__(THREADS, wide_blocks(THREADS)) k_scores_wide(c
                 if (a.lse) a.lse[r] = res.lse;
                 if (a.entropy) a.entropy[r] = res.entropy;
                 if (a.log_prob) a.log_prob[r] = label >= 0 ? res.log_p(at_label) : 0.f;
+                if (a.row_sums) a.row_sums[r] = res.sums();
             }
             if ((int)threadIdx.x < a.top) {
                 const uint64_t key = sh.best[threadIdx.x];
@@ -560,6 +561,7 @@ __global__ void __launch_bounds__(THREADS, wide_blocks(THREADS)) k_distill_wide(
         if (threadIdx.x == 0) {
             loss[r] = v;
             if (a.lse) a.lse[r] = res.lse;
+            if (a.row_sums) a.row_sums[r] = res.sums();
         }
     }
     if (parts > 1) cg::this_cluster().sync();

@@ -1,9 +1,11 @@
 """Rows of a teacher's that hold no pair or allow no class, with a normaliser of their own that is no number, in every kernel of the distillation; gradients
-of classes that are masked."""
+of classes that are masked, and of rows far from zero or masked all over by a finite value."""
 import pytest
 import torch
 
-from test_scores_and_distillation import INF, TYPES, ctx, distill, distill_backward, logits_of, near, scores_backward, some_labels  # noqa: F401
+import paper_2202_02365_b200 as mg
+from test_scores_and_distillation import INF, TYPES, ctx, distill, distill_backward, logits_of, near, rows_of, scores_backward, some_labels, some_teacher  # noqa: F401
+from test_scores_and_distillation import U
 
 NAN = float("nan")
 
@@ -78,3 +80,100 @@ def test_masked_classes_under_a_large_gradient_of_the_entropy(ctx, rows, classes
         got = ctx.log_probs_backward(x, r.lse, labels, entropy=r.entropy, d_entropy=h)
         near(got, want, off)
         assert not got[x == -INF].any()
+
+
+SHIFTS = {torch.float32: (0.0, 40.0, -300.0, 1e4, -1e6, 3e7, -1e9, 1e30), torch.float16: (0.0, 200.0, -3e4, 6e4), torch.bfloat16: (0.0, 100.0, 3e4, -1e30)}
+
+
+def far_rows(classes, dtype, seed, pad, shift):
+    """Rows about values far from zero, masked all over by a finite value, all over but for some classes, and without a class."""
+    shifts = SHIFTS[dtype]
+    x = logits_of(2 * len(shifts) + 10, classes, dtype, seed, pad, shift, masked=0.3)
+    lowest = torch.finfo(dtype).min
+    for i, by in enumerate(shifts):
+        x[2 * i:2 * i + 2] = (x[2 * i:2 * i + 2].double() + by).to(dtype)
+    last = x[2 * len(shifts):]
+    last[0] = lowest
+    last[1] = max(-1e9, lowest)
+    last[2:4] = torch.where(last[2:4] == -INF, -INF, lowest)      # some are not allowed, the others masked
+    last[4, classes // 2:] = lowest
+    last[5, 1:] = lowest
+    last[6] = -INF
+    last[7] = lowest / 2
+    last[8] = torch.where(last[8] == -INF, lowest, torch.full_like(last[8], lowest / 2))
+    return x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("classes", [1, 5, 20, 153, 172, 1000, 2500, 6151, 50_257, 300_007])
+def test_gradients_by_the_rows_sums(ctx, classes, dtype):
+    """Probabilities as exact as the forward call's, where lse is rounded to less than its sum's logarithm.  Beside the roundings that scores_backward and distill_backward count: the
+    sum's relative error, its logarithm, and two roundings of x - m."""
+    dtype = TYPES[dtype]
+    for pad, shift, scale in ((0, 0, 1.0), (3, 1, 0.6), (0, 0, 2.5)):
+        x = far_rows(classes, dtype, classes, pad, shift)
+        rows = len(x)
+        if scale > 1:      # (times the scale no value is beyond fp32)
+            x.clamp_(min=torch.finfo(dtype).min / 4).masked_fill_(x <= torch.finfo(dtype).min / 4, torch.finfo(dtype).min / 4)
+        labels = some_labels(rows, classes, 3)
+        scale32 = torch.tensor(scale, dtype=torch.float32).double().item()
+        most = x.double().max(1, keepdim=True).values
+        about = x.double() - torch.where(most == -INF, 0.0, most)      # the same gradient, from numbers of an ordinary size
+        _, _, s, p, far, sum_off = rows_of(about, scale32)
+        log_s = torch.log(s)
+        p_off = U * p * (sum_off + 4 * log_s.abs() + 4 * far)
+        row_sums = torch.full((rows, 2), float("nan"), device="cuda")
+        r = ctx.log_probs(x, labels, scale=scale, row_sums=row_sums)
+        lse = scale32 * row_sums[:, 0].double() + row_sums[:, 1].double()
+        assert torch.equal(lse == -INF, r.lse == -INF) and ((lse - r.lse.double()).abs() <= 2 * U * (scale32 * row_sums[:, 0].double().abs() + lse.abs()))[lse.isfinite()].all()
+        g, h, l = torch.randn(3, rows, device="cuda", generator=torch.Generator(device="cuda").manual_seed(classes))
+        for how in (dict(d_log_prob=g), dict(d_log_prob=g, entropy=r.entropy, d_entropy=h, d_lse=l), dict(d_lse=l)):
+            want, off = scores_backward(about, log_s[:, 0], labels, how.get("d_log_prob"), how.get("entropy"), how.get("d_entropy"), how.get("d_lse"), scale32, dtype)
+            sizes = [how[k].double().abs()[:, None] if k in how else 0.0 for k in ("d_log_prob", "d_entropy", "d_lse")]
+            inner = torch.where(p > 0, torch.log(p).abs(), 0.0) + r.entropy.double().abs()[:, None]
+            off = off + scale32 * p_off * (sizes[0] + sizes[1] * (inner + 1) + sizes[2])
+            got = ctx.log_probs_backward(x, None, labels, scale=scale, row_sums=row_sums, **how)
+            near(got, want, off)
+            near(ctx.log_probs_backward(x, r.lse, labels, scale=scale, row_sums=row_sums, out=logits_of(rows, classes, dtype, 1, 5, 0), **how), want, off)      # (by another kernel)
+            near(ctx.log_probs_backward(x.clone(), None, labels, scale=scale, row_sums=row_sums, **how), want, off)      # (rows one behind the other)
+        ids, values = some_teacher(rows, classes, 20, 5)
+        sums = torch.empty(rows, 2, device="cuda")
+        ctx.distill(x, ids, values, scale=scale, row_sums=sums)
+        want, off = distill_backward(about, log_s[:, 0], ids, values, None, l, scale32, dtype)
+        off = off + scale32 * l.double().abs()[:, None] * 1.001 * p_off
+        for by in (sums, row_sums):
+            got = ctx.distill_backward(l, x, None, ids, values, scale=scale, row_sums=by)
+            near(got, want, off)
+        inplace = torch.empty_strided(x.shape, x.stride(), dtype=dtype, device="cuda").copy_(x)
+        assert torch.equal(ctx.distill_backward(l, inplace, None, ids, values, scale=scale, row_sums=row_sums, out=inplace), got)
+        inplace = torch.empty_strided(x.shape, x.stride(), dtype=dtype, device="cuda").copy_(x)
+        assert torch.equal(ctx.log_probs_backward(inplace, None, labels, scale=scale, row_sums=row_sums, out=inplace, d_lse=l), ctx.log_probs_backward(x, None, labels, scale=scale, row_sums=row_sums, d_lse=l))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,classes", [(4, 20), (4, 172), (4, 6151), (4, 250_000)])
+def test_a_row_that_is_masked_all_over_by_a_finite_value(ctx, rows, classes):
+    for value in (-1e9, torch.finfo(torch.float32).min):
+        x = torch.full((rows, classes), value, device="cuda")
+        row_sums = torch.empty(rows, 2, device="cuda")
+        ctx.log_probs(x, row_sums=row_sums)
+        d = ctx.log_probs_backward(x, None, d_lse=torch.ones(rows, device="cuda"), row_sums=row_sums)
+        assert ((d * classes - 1).abs() <= 1e-4).all()      # (n sums of one: below 2^-24 (n / 256 + 128) by the chains, 6e-5)
+
+
+@pytest.mark.gpu
+def test_refusals_of_row_sums(ctx):
+    x, labels, g = torch.randn(3, 8, 16, device="cuda")[0], torch.zeros(8, dtype=torch.int64, device="cuda"), torch.ones(8, device="cuda")
+    good = torch.empty(8, 2, device="cuda")
+    for bad in (good[:7], good.double(), good.cpu(), torch.empty(2, 8, device="cuda").t(), good[:, :1], good.view(16)):
+        for call in (lambda: ctx.log_probs(x, row_sums=bad), lambda: ctx.log_probs_backward(x, g, labels, g, row_sums=bad)):
+            with pytest.raises(AssertionError):
+                call()
+    with pytest.raises(mg.MgError) as e:
+        ctx.log_probs(x, row_sums=torch.empty(17, device="cuda")[1:].view(8, 2))
+    assert e.value.code == -1
+    with pytest.raises(mg.MgError):
+        ctx.log_probs_backward(x, None, labels, g)
+    ctx.log_probs(x, labels, row_sums=good)
+    assert good.isfinite().all()
