@@ -103,7 +103,7 @@ inline SumPlan plan_sums(int64_t n, int64_t n_rows, int32_t dim, int n_sms = 148
     if (n == 0 || n_rows == 0) return p;
     const int64_t lanes = dim >= 256 ? (dim + 255) / 256 * 32 : dim > 64 ? 32 : dim > 32 ? 16 : dim > 16 ? 8 : 4;
     const int64_t threads = (int64_t)n_sms * 1536;
-    p.chunk = (int32_t)std::max<int64_t>({(n * lanes + threads - 1) / threads, n / 8192, 16});
+    p.chunk = (int32_t)std::min<int64_t>(std::max<int64_t>({(n * lanes + threads - 1) / threads, (n + 8191) / 8192, 16}), std::max<int64_t>(n, 16));   // (no more than there are: n lanes / threads may pass 32 bits)
     p.chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
     p.at_begun = rows_align(8 * (size_t)p.chunks * p.pitch);
     p.bytes = p.at_begun + rows_align(4 * (size_t)p.chunks);
