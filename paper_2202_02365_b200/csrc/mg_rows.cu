@@ -107,12 +107,12 @@ void launch_sums(SumArgs a, int vec, int64_t zero_blocks, cudaStream_t st) {
     const int each = std::max(vec, 4), lanes = std::min(32, std::max(4, pow2_up((a.dim + each - 1) / each))), columns = lanes * each;   // (columns to a lane)
     a.chunk_blocks = (int32_t)(((int64_t)a.chunks * lanes + kSumThreads - 1) / kSumThreads);
     const dim3 grid((unsigned)(a.chunk_blocks + zero_blocks), (unsigned)((a.dim + columns - 1) / columns));
-    const auto go = [&](auto kernel) { mgnorm::launch_chained(grid, kSumThreads, st, kernel, a, lanes); };
+    const auto go = [&](auto kernel, auto of_long) { mgnorm::launch_chained(grid, kSumThreads, st, a.chunk > kSumChain ? of_long : kernel, a, lanes); };
     if constexpr (sizeof(T) == 2 && sizeof(O) == 2)
-        if (vec == 8) { go(k_chunk_sums<T, O, 8, 1, 4>); return; }
-    if (vec == 4) go(k_chunk_sums<T, O, 4, 1, 4>);
-    else if (vec == 2) go(k_chunk_sums<T, O, 2, 2, 4>);
-    else go(k_chunk_sums<T, O, 1, 4, 2>);
+        if (vec == 8) { go(k_chunk_sums<T, O, 8, 1, 4, false>, k_chunk_sums<T, O, 8, 1, 4, true>); return; }
+    if (vec == 4) go(k_chunk_sums<T, O, 4, 1, 4, false>, k_chunk_sums<T, O, 4, 1, 4, true>);
+    else if (vec == 2) go(k_chunk_sums<T, O, 2, 2, 4, false>, k_chunk_sums<T, O, 2, 2, 4, true>);
+    else go(k_chunk_sums<T, O, 1, 4, 2, false>, k_chunk_sums<T, O, 1, 4, 2, true>);
 }
 
 }  // namespace

@@ -12,6 +12,9 @@
 namespace mgrows {
 
 constexpr int kSumThreads = 256, kJoinThreads = 1024;
+// Places whose rows are added up in fp32 one behind the other; the sums of so many each are added up in 64 bits.  With 256 shares to a warp and 32 warps, no value goes through more than
+// 480 additions in fp32, however many places an id has.  (A multiple of every number of lanes.)
+constexpr int kSumChain = 192;
 
 struct SumArgs {
     const void* d_y; int64_t d_y_stride, n, n_rows;
@@ -97,7 +100,9 @@ __global__ void __launch_bounds__(kSumThreads) k_zero_others(const __grid_consta
 
 // `lanes` lanes to a chunk, NV vectors of its rows to a lane, U rows on their way while U others are added up; blockIdx.y: which of the rows' columns.
 // What a chunk has to know of its neighbours is asked for beside its first places, and of its first and last ids beside its first rows.
-template <typename T, typename O, int VEC, int NV, int U>
+// LONG: chunks of more than kSumChain places, which few calls have (more than some 1.4 million ids, or of 1.4 GB in fp32): a million bf16 rows of 1,024 434 us, without 419, and the others
+// would lose as much.
+template <typename T, typename O, int VEC, int NV, int U, bool LONG>
 __global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_constant__ SumArgs a, int lanes) {
     chain_wait();
     chain_start();
@@ -155,8 +160,28 @@ __global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_cons
     for (int v = 0; v < NV; ++v)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) acc[v][e] = 0.f;
+    __shared__ double put_away[LONG ? NV * VEC : 1][LONG ? kSumThreads : 1];   // the sum of an id's places up to the last kSumChain
+    bool has_put = false;
+    const auto put = [&]() {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                double& to = put_away[v * VEC + e][threadIdx.x];
+                to = (has_put ? to : 0.) + (double)acc[v][e];
+                acc[v][e] = 0.f;
+            }
+        has_put = true;
+    };
     int32_t cur = -1, cur_row = -1;
     const auto flush = [&]() {
+        if (LONG && has_put) {
+#pragma unroll
+            for (int v = 0; v < NV; ++v)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) acc[v][e] = (float)(put_away[v * VEC + e][threadIdx.x] + (double)acc[v][e]);
+            has_put = false;
+        }
         if (cur >= 0 && cur != skip) {
             const bool share = cur == before || cur == behind;
 #pragma unroll
@@ -213,6 +238,7 @@ __global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_cons
             load(one, more ? place : after, more ? at + 2 * U : 0);
             if (lanes >= 2 * U) add(two, left, at + U);
         }
+        if (LONG && ((uint32_t)(p - lo) + (uint32_t)lanes) % kSumChain == 0) put();
         place = next_place; group = next_group;
         row = row_of(group);
         ask(p + 2 * lanes);
@@ -229,6 +255,7 @@ __device__ __forceinline__ Spanned spanned(const SumArgs& a, int32_t chunk) {
     const int64_t end = min((int64_t)a.starts[g + 1], a.n), row = a.into == MG_ROWS_COMPACT ? g : id_at(a.group_ids, a.ids_are_i64, g);
     return {chunk, min((int32_t)((end - 1) / a.chunk), a.chunks - 1) - chunk + 1, row < a.n_rows ? (int32_t)row : -1};
 }
+// (of 8,192 shares, the most that there are, a warp has 256)
 __device__ __forceinline__ float4 add_shares(const SumArgs& a, int32_t chunk, int32_t lo, int32_t hi, int32_t c) {
     float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
     if (c >= a.dim) return s;

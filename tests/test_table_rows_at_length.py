@@ -4,8 +4,10 @@ import shutil
 import subprocess
 
 import pytest
+import torch
 
 from paper_2202_02365_b200 import build
+from test_table_rows import check_sums, ctx  # noqa: F401
 
 # ---- how a call is cut, on the host ---------------------------------------------------------------------------------
 PLANS = r"""
@@ -49,3 +51,26 @@ def run_on_the_host(tmp_path, program):
 
 def test_every_place_is_in_one_of_few_chunks(tmp_path):
     run_on_the_host(tmp_path, PLANS)
+
+
+# ---- on the GPU -----------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,dim,stretches", [(100_000, 65_536, 1), (100_000, 65_536, 50), (40_000, 262_144, 2), (9000, 1 << 20, 3), (30_000_000, 16, 1), (3_000_001, 36, 2), (30_000_000, 16, 9000),
+                                             (200_000, 3000, 3)])
+def test_sums_of_many_places_stay_within_their_bound(ctx, n, dim, stretches):
+    """One row over and over, of values whose fp32 sums are rounded the same way each time: a chain of some thousand additions is off by more than 512 roundings can be."""
+    values = torch.tensor([1 + 0.9 * 2.0 ** -13, 0.1, 0.7, -0.1, 1 + 0.9 * 2.0 ** -14, 3.0], device="cuda")
+    row = values[torch.arange(dim, device="cuda") % 6]
+    n_rows = stretches + 3
+    one_by_one = (torch.arange(n, device="cuda", dtype=torch.int32) % stretches) + 1      # (its places lie apart)
+    ids = torch.where(torch.arange(n, device="cuda") % 1000 == 7, -1, one_by_one)
+    ids[-1] = n_rows - 1                                                                  # an id of one place
+    count = torch.bincount(ids[ids >= 0].long(), minlength=n_rows)
+    for dtype in (torch.float32, torch.bfloat16):
+        d_y = row.to(dtype).expand(n, dim)
+        want = count[:, None].double() * d_y[0].double()
+        got = ctx.embedding_backward(d_y, ids, n_rows, dtype=torch.float32)
+        check_sums(got, want, want.abs(), count)
+        assert not got[count == 0].any()
+        distinct, rows = ctx.embedding_backward_rows(d_y, ids, n_rows, dtype=torch.float32)
+        assert torch.equal(rows, got[distinct.long()])
