@@ -6,7 +6,6 @@ namespace {
 
 using namespace mgrows;
 
-static_assert(kJoinThreads == kPlanJoinThreads, "a thread to a chunk");
 constexpr int kRowThreads = 256;
 
 // 543,000 fp32 rows of 128 out of two million: 90 us for 502 MB, 86 % of the copy's rate; the memory bounds it.  (A warp to a row: 157.)
@@ -202,7 +201,7 @@ extern "C" int mg_embedding_backward(mg_ctx* ctx, const void* d_y, int64_t d_y_s
     if (p.chunks > 0) {
         const int vec = row_vec(d_y, d_y_stride, d_y_dtype, n, out, out_stride, out_dtype, n_rows, dim);
         MG_BY_TYPE(d_y_dtype, using From = T; MG_BY_TYPE(out_dtype, (launch_sums<From, T>(a, vec, zero_blocks, st))));
-        MG_BY_TYPE(out_dtype, mgnorm::launch_chained(dim3((unsigned)p.join_blocks, (unsigned)((dim + 127) / 128)), kJoinThreads, st, k_join_shares<T>, a));
+        MG_BY_TYPE(out_dtype, mgnorm::launch_chained(dim3((unsigned)std::min(p.chunks, mg_grid(ctx, 1)), (unsigned)((dim + 127) / 128)), kJoinThreads, st, k_join_shares<T>, a));
         ctx->launches += 2;
     }
     MG_CUDA(ctx, cudaGetLastError());

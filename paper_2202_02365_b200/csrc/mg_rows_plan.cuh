@@ -10,7 +10,6 @@
 namespace {
 
 constexpr int kPlanBits = 8, kPlanBins = 1 << kPlanBits, kPlanThreads = 256, kPlanSmall = 1024;   // of the sort; ids that one block sorts
-constexpr int kPlanJoinThreads = 1024;   // of the sums' second kernel
 
 inline size_t rows_align(size_t bytes) { return (bytes + 15) / 16 * 16; }
 
@@ -93,7 +92,6 @@ inline int check_groups(mg_ctx* ctx, const void* ids, int ids_are_i64, int64_t n
 
 struct SumPlan {
     int32_t chunk = 1, chunks = 0, pitch = 0;
-    int32_t join_blocks = 0;   // of the kernel that adds shares up: a thread looks at one chunk
     size_t at_begun = 0, bytes = 0;
 };
 
@@ -107,7 +105,6 @@ inline SumPlan plan_sums(int64_t n, int64_t n_rows, int32_t dim, int n_sms = 148
     const int64_t threads = (int64_t)n_sms * 1536;
     p.chunk = (int32_t)std::min<int64_t>(std::max<int64_t>({(n * lanes + threads - 1) / threads, (n + 8191) / 8192, 16}), std::max<int64_t>(n, 16));   // (no more than there are: n lanes / threads may pass 32 bits)
     p.chunks = (int32_t)((n + p.chunk - 1) / p.chunk);
-    p.join_blocks = std::max(std::min(p.chunks, n_sms), (p.chunks + kPlanJoinThreads - 1) / kPlanJoinThreads);
     p.at_begun = rows_align(8 * (size_t)p.chunks * p.pitch);
     p.bytes = p.at_begun + rows_align(4 * (size_t)p.chunks);
     return p;

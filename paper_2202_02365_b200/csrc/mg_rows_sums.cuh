@@ -246,8 +246,7 @@ __global__ void __launch_bounds__(kSumThreads, 3) k_chunk_sums(const __grid_cons
     flush();
 }
 
-// The shares of the ids that begin in a chunk and go on behind it: a block looks at every gridDim.x-th chunk, a thread at one (there are as many
-// threads as chunks); 32 lanes of four columns.  Up to 32 shares are added up by a warp, more
+// The shares of the ids that begin in a chunk and go on behind it: a block looks at every gridDim.x-th chunk; 32 lanes of four columns.  Up to 32 shares are added up by a warp, more
 // by 32 warps that each take a stretch of the chunks that the id spans.
 constexpr int kWarpShares = 32;
 struct Spanned { int32_t chunk, shares, row; };   // the chunk that the id begins in
@@ -292,26 +291,28 @@ __global__ void __launch_bounds__(kJoinThreads) k_join_shares(const __grid_const
     chain_start();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t c = ((int32_t)blockIdx.y * 32 + lane) * 4;
-    if (threadIdx.x == 0) n_few = n_many = 0;
-    __syncthreads();
-    const int64_t mine = blockIdx.x + (int64_t)threadIdx.x * gridDim.x;
-    if (mine < a.chunks && a.begun[mine] >= 0) {
-        const Spanned s = spanned(a, (int32_t)mine);
-        if (s.shares <= kWarpShares) few[atomicAdd(&n_few, 1)] = s;
-        else many[atomicAdd(&n_many, 1)] = s;
-    }
-    __syncthreads();
-    for (int f = warp; f < n_few; f += W) write_joined<O>(a, few[f].row, c, add_shares(a, few[f].chunk, 0, few[f].shares, c));
-    for (int f = 0; f < n_many; ++f) {
-        const Spanned s = many[f];
-        part[warp][lane] = add_shares(a, s.chunk, (int32_t)((int64_t)s.shares * warp / W), (int32_t)((int64_t)s.shares * (warp + 1) / W), c);
+    for (int32_t c0 = (int32_t)blockIdx.x; c0 < a.chunks; c0 += (int32_t)gridDim.x * kJoinThreads) {
+        if (threadIdx.x == 0) n_few = n_many = 0;
         __syncthreads();
-        if (warp == 0) {
-            float4 t = part[0][lane];
-            for (int w = 1; w < W; ++w) { const float4 o = part[w][lane]; t.x += o.x; t.y += o.y; t.z += o.z; t.w += o.w; }
-            write_joined<O>(a, s.row, c, t);
+        const int64_t mine = c0 + (int64_t)threadIdx.x * gridDim.x;
+        if (mine < a.chunks && a.begun[mine] >= 0) {
+            const Spanned s = spanned(a, (int32_t)mine);
+            if (s.shares <= kWarpShares) few[atomicAdd(&n_few, 1)] = s;
+            else many[atomicAdd(&n_many, 1)] = s;
         }
         __syncthreads();
+        for (int f = warp; f < n_few; f += W) write_joined<O>(a, few[f].row, c, add_shares(a, few[f].chunk, 0, few[f].shares, c));
+        for (int f = 0; f < n_many; ++f) {
+            const Spanned s = many[f];
+            part[warp][lane] = add_shares(a, s.chunk, (int32_t)((int64_t)s.shares * warp / W), (int32_t)((int64_t)s.shares * (warp + 1) / W), c);
+            __syncthreads();
+            if (warp == 0) {
+                float4 t = part[0][lane];
+                for (int w = 1; w < W; ++w) { const float4 o = part[w][lane]; t.x += o.x; t.y += o.y; t.z += o.z; t.w += o.w; }
+                write_joined<O>(a, s.row, c, t);
+            }
+            __syncthreads();
+        }
     }
 }
 

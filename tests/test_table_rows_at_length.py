@@ -53,10 +53,6 @@ def test_every_place_is_in_one_of_few_chunks(tmp_path):
     run_on_the_host(tmp_path, PLANS)
 
 
-def test_every_chunks_shares_are_looked_for_by_a_thread_of_their_own(tmp_path):
-    run_on_the_host(tmp_path, PLANS.replace("p.chunks <= 8192 &&", "p.chunks <= 8192 && p.join_blocks >= 1 && (int64_t)p.join_blocks * kPlanJoinThreads >= p.chunks &&").replace("{8, 148}", "{1, 2, 7, 8, 148}"))
-
-
 # ---- on the GPU -----------------------------------------------------------------------------------------------------
 @pytest.mark.gpu
 @pytest.mark.parametrize("n,dim,stretches", [(100_000, 65_536, 1), (100_000, 65_536, 50), (40_000, 262_144, 2), (9000, 1 << 20, 3), (30_000_000, 16, 1), (3_000_001, 36, 2), (30_000_000, 16, 9000),
