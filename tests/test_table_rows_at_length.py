@@ -36,11 +36,11 @@ int main() {
 """
 
 
-def run_on_the_host(tmp_path, program):
+def run_program(tmp_path, program):
     nvcc = shutil.which("nvcc") or "/usr/local/cuda/bin/nvcc"
     if not os.path.exists(nvcc):
         pytest.skip("no nvcc")
-    source, out = tmp_path / "host.cu", str(tmp_path / "host")
+    source, out = tmp_path / "program.cu", str(tmp_path / "program")
     source.write_text(program)
     made = subprocess.run([nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-std=c++17", "-O0", "-Xcompiler", "-w", "-I", build.CSRC,
                            "-I", os.path.join(build.ROOT, "include"), str(source), "-o", out], capture_output=True, text=True)
@@ -50,7 +50,7 @@ def run_on_the_host(tmp_path, program):
 
 
 def test_every_place_is_in_one_of_few_chunks(tmp_path):
-    run_on_the_host(tmp_path, PLANS)
+    run_program(tmp_path, PLANS)
 
 
 # ---- on the GPU -----------------------------------------------------------------------------------------------------
@@ -74,3 +74,73 @@ def test_sums_of_many_places_stay_within_their_bound(ctx, n, dim, stretches):
         assert not got[count == 0].any()
         distinct, rows = ctx.embedding_backward_rows(d_y, ids, n_rows, dtype=torch.float32)
         assert torch.equal(rows, got[distinct.long()])
+
+
+# ---- kernels by themselves: what no call of the library makes happen ------------------------------------------------
+KERNELS = r"""
+#include <cstdarg>
+#include <cstdio>
+#include <vector>
+#include "mgdense.h"
+#include "mg_rows_sums.cuh"
+using namespace mgrows;
+
+static int bad = 0;
+#define EXPECT(is, what) do { if (!(is)) { printf("line %d: %s\n", __LINE__, what); ++bad; } } while (0)
+template <typename T> static T* device(const std::vector<T>& v) {
+    T* p = nullptr;
+    cudaMalloc(&p, v.size() * sizeof(T));
+    cudaMemcpy(p, v.data(), v.size() * sizeof(T), cudaMemcpyHostToDevice);
+    return p;
+}
+template <typename T> static std::vector<T> host(const T* p, size_t n) {
+    std::vector<T> v(n);
+    cudaMemcpy(v.data(), p, n * sizeof(T), cudaMemcpyDeviceToHost);
+    return v;
+}
+
+// 5,000 chunks by one block, in several rounds: ids of two to forty shares, each of which begins in the chunk that the one before ends in.
+static void join() {
+    const int chunk = 16, chunks = 5000, dim = 128, spans[] = {2, 3, 40, 2, 5, 33, 2, 2};
+    std::vector<float> shares((size_t)chunks * 2 * dim), want;
+    std::vector<int32_t> begun(chunks, -1), starts;
+    for (size_t i = 0; i < shares.size(); ++i) shares[i] = (float)(i / dim % 13 + 1);
+    int first = 0;
+    for (int g = 0;; ++g) {
+        const int span = spans[g % 8];
+        starts.push_back(first * chunk + 8);
+        if (first + span > chunks) break;
+        begun[first] = g;
+        float sum = 0.f;
+        for (int i = 0; i < span; ++i) sum += shares[((size_t)(first + i) * 2 + (i == 0)) * dim];
+        want.push_back(sum);
+        first += span - 1;
+    }
+    const int groups = (int)want.size();
+    SumArgs a = {};
+    a.n = (int64_t)chunks * chunk; a.n_rows = a.n; a.dim = dim; a.scale = 1.f; a.into = MG_ROWS_COMPACT; a.out_stride = dim; a.chunk = chunk; a.chunks = chunks; a.pitch = dim;
+    a.starts = device(starts); a.shares = device(shares); a.begun = device(begun);
+    float* out = device(std::vector<float>((size_t)groups * dim, -1.f));
+    a.out = out;
+    for (int t = 0; t < 20; ++t) {
+        cudaMemset(out, 0xFF, sizeof(float) * groups * dim);
+        k_join_shares<float><<<1, kJoinThreads>>>(a);
+        const std::vector<float> got = host(out, (size_t)groups * dim);
+        int wrong = 0;
+        for (int g = 0; g < groups; ++g)
+            for (int c = 0; c < dim; ++c) wrong += got[(size_t)g * dim + c] != want[g];
+        EXPECT(wrong == 0, "shares");
+    }
+}
+
+int main() {
+    join();
+    EXPECT(cudaDeviceSynchronize() == cudaSuccess, cudaGetErrorString(cudaGetLastError()));
+    return bad ? 1 : 0;
+}
+"""
+
+
+@pytest.mark.gpu
+def test_kernels_by_themselves(tmp_path):
+    run_program(tmp_path, KERNELS)
