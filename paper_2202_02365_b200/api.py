@@ -266,7 +266,7 @@ ROWS_TABLE, ROWS_ADD, ROWS_COMPACT = 0, 1, 2
 @dataclass(frozen=True)
 class IdGroups:
     """The places of each id (Context.id_groups): `order` has them by ascending id, `group_of` which of the distinct `ids` each is of (-1: of none), `starts`
-    where each one's places lie in order, `count` (one element, on the device) how many ids there are; `ids` and `starts` mean nothing behind it."""
+    where each one's places lie in order, `count` (one element, on the device) how many ids there are, -1 if a wait on the device ran out; `ids` and `starts` mean nothing behind it."""
     order: torch.Tensor
     group_of: torch.Tensor
     ids: torch.Tensor
@@ -916,7 +916,8 @@ class Context:
                            out: torch.Tensor | None = None, accumulate: bool = False) -> torch.Tensor:
         """Gradient of embedding with respect to its table of n_rows rows, from its output's d_y [*ids.shape, dim]: sums in fp32, in an order that does not change
         from run to run.  ids: those of the lookup, or their id_groups.  out: where to, else a new tensor (of `dtype`, else of d_y's type); accumulate: it is added
-        to what `out` holds, and rows without an id are not touched."""
+        to what `out` holds, and rows without an id are not touched.  Should a bounded wait of id_groups run out on the device (nothing that is known of makes it), its count
+        is -1 and there are no sums: a table of zeros, nothing added; who must know reads the count (embedding_backward_rows does, and raises)."""
         d_y, groups = self._grouped(d_y, ids, n_rows)
         assert out is not None or not accumulate, "accumulate wants out"
         if out is None:

@@ -165,6 +165,12 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_groups(const uint32_t* ke
     constexpr int TILE = kSortThreads * PER;
     __shared__ uint32_t warp_tot[kSortWarps], sh_tile, sh_before;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const auto say = [&](int32_t count) {   // -1 where a wait has run out, here or in the sort, or does so later
+        volatile int32_t* to = n_groups;
+        *to = count;
+        __threadfence();
+        if (*reinterpret_cast<volatile uint32_t*>(&s->failed)) *to = -1;
+    };
     chain_wait();
     chain_start();
     if (threadIdx.x == 0) sh_tile = atomicAdd(&s->ticket[kMaxPasses], 1u);
@@ -190,7 +196,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_groups(const uint32_t* ke
         bool gave_up = false;
         const uint32_t before = chain_tiles(states, (int32_t)tile, 1ull << 34, 0u, total, max_polls, &gave_up);
         if (lane == 0) sh_before = before;
-        if (gave_up && lane == 0) {
+        if (__any_sync(0xFFFFFFFFu, gave_up) && lane == 0) {   // (each lane waits for a tile of its own)
             atomicExch(&s->failed, 1u);
             __threadfence();
             *reinterpret_cast<volatile int32_t*>(n_groups) = -1;
@@ -215,13 +221,10 @@ __global__ void __launch_bounds__(kSortThreads) k_sort_groups(const uint32_t* ke
         }
         if (i + 1 == n || keys[i + 1] == none) {   // the last place of the last group
             if ((int64_t)to <= room) starts[to] = (int32_t)i + 1;
-            volatile int32_t* count = n_groups;
-            *count = (int32_t)to;
-            __threadfence();
-            if (*reinterpret_cast<volatile uint32_t*>(&s->failed)) *count = -1;
+            say((int32_t)to);
         }
     }
-    if (tile == 0 && threadIdx.x == 0 && keys[0] == none) { starts[0] = 0; *n_groups = 0; }
+    if (tile == 0 && threadIdx.x == 0 && keys[0] == none) { starts[0] = 0; say(0); }
 }
 
 // All of it in one block: few ids, whose sort by several kernels is launches and waits.  An id with its place below it to a thread, sorted by a bitonic network: steps within a

@@ -77,7 +77,7 @@ def test_sums_of_many_places_stay_within_their_bound(ctx, n, dim, stretches):
 
 
 # ---- kernels by themselves: what no call of the library makes happen ------------------------------------------------
-KERNELS = r"""
+COMMON = r"""
 #include <cstdarg>
 #include <cstdio>
 #include <vector>
@@ -99,6 +99,8 @@ template <typename T> static std::vector<T> host(const T* p, size_t n) {
     return v;
 }
 
+"""
+JOIN = COMMON + r"""
 // 5,000 chunks by one block, in several rounds: ids of two to forty shares, each of which begins in the chunk that the one before ends in.
 static void join() {
     const int chunk = 16, chunks = 5000, dim = 128, spans[] = {2, 3, 40, 2, 5, 33, 2, 2};
@@ -141,6 +143,41 @@ int main() {
 """
 
 
+GROUPS = COMMON + r"""
+// Groups of 3,000 sorted keys below 100 (`some`) or that are none: what is said of their number.
+static int32_t groups(bool some, bool failed, int first_tile, int tiles, const std::vector<uint64_t>& told, int polls) {
+    const int n = 3000, none = 100;
+    std::vector<uint32_t> keys(n, none);
+    if (some) for (int i = 0; i < n; ++i) keys[i] = i * none / n;
+    SortShared shared = {};
+    shared.failed = failed;
+    shared.ticket[kMaxPasses] = first_tile;
+    int32_t *ids = device(std::vector<int32_t>(none)), *starts = device(std::vector<int32_t>(none + 1)), *of = device(std::vector<int32_t>(n)), *count = device(std::vector<int32_t>(1, 12345));
+    k_sort_groups<4><<<tiles, kSortThreads>>>(device(keys), n, none, device(std::vector<SortShared>(1, shared)), device(told), 0, ids, starts, of, count, polls);
+    return host(count, 1)[0];
+}
+
+int main() {
+    const std::vector<uint64_t> nothing(3, 0);
+    EXPECT(groups(true, false, 0, 3, nothing, 1 << 20) == 100, "all is well");
+    EXPECT(groups(false, false, 0, 3, nothing, 1 << 20) == 0, "no group");
+    EXPECT(groups(true, true, 0, 3, nothing, 1 << 20) == -1, "the sort has failed");
+    EXPECT(groups(false, true, 0, 3, nothing, 1 << 20) == -1, "the sort has failed, no key of a row came out of it");
+    // the third tile by itself: the second has said how many it has, the first never says anything, which the second lane waits for
+    EXPECT(groups(true, false, 2, 1, {0, kChainTag | kChainOwn | 34, 0}, 8) == -1, "a wait has run out");
+    EXPECT(groups(true, false, 2, 1, {0, 0, 0}, 8) == -1, "a wait has run out");
+    EXPECT(cudaDeviceSynchronize() == cudaSuccess, cudaGetErrorString(cudaGetLastError()));
+    return bad ? 1 : 0;
+}
+"""
+
+
 @pytest.mark.gpu
-def test_kernels_by_themselves(tmp_path):
-    run_program(tmp_path, KERNELS)
+def test_shares_in_several_rounds(tmp_path):
+    run_program(tmp_path, JOIN)
+
+
+@pytest.mark.gpu
+def test_a_wait_that_has_run_out_is_told(tmp_path):
+    """On the device: waits of a few polls for a word that nobody writes."""
+    run_program(tmp_path, GROUPS)
