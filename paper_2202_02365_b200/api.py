@@ -906,6 +906,8 @@ class Context:
         if not isinstance(ids, IdGroups):
             assert d_y.shape[:-1] == ids.shape, "d_y: a row for each id"
             ids = self.id_groups(ids, n_rows)
+        else:
+            assert ids.order.device == ids.group_of.device == ids.ids.device == ids.starts.device == ids.count.device == self.device, "groups of ids, on the context's device"
         assert n_rows == ids.n_rows, "groups of ids belong to the number of rows they were made for"
         assert d_y.dim() >= 1 and d_y.shape[:-1].numel() == ids.order.numel(), "d_y: a row for each id"
         if d_y.dim() != 2:

@@ -1,11 +1,14 @@
 """Gradients of looked-up rows where ids are many: how the sorted places are cut, and how exact the sums stay."""
+import dataclasses
 import os
 import shutil
 import subprocess
+import types
 
 import pytest
 import torch
 
+import paper_2202_02365_b200 as mg
 from paper_2202_02365_b200 import build
 from test_table_rows import check_sums, ctx  # noqa: F401
 
@@ -51,6 +54,19 @@ def run_program(tmp_path, program):
 
 def test_every_place_is_in_one_of_few_chunks(tmp_path):
     run_program(tmp_path, PLANS)
+
+
+def test_groups_of_another_device_are_refused():
+    """Their addresses are read by kernels: before any call of the library."""
+    here, there = torch.device("meta"), torch.device("cpu")
+    ctx = types.SimpleNamespace(device=here)
+    d_y = torch.empty(5, 4, device=here)
+    some = lambda n, device: torch.empty(n, dtype=torch.int32, device=device)
+    good = mg.IdGroups(some(5, here), some(5, here), some(3, here), some(4, here), some(1, here), 3)
+    assert mg.Context._grouped(ctx, d_y, good, 3)[1] is good
+    for field in ("order", "group_of", "ids", "starts", "count"):
+        with pytest.raises(AssertionError):
+            mg.Context._grouped(ctx, d_y, dataclasses.replace(good, **{field: getattr(good, field).new_empty(getattr(good, field).shape, device=there)}), 3)
 
 
 # ---- on the GPU -----------------------------------------------------------------------------------------------------
