@@ -115,6 +115,7 @@ inline ForwardPlan plan_forward(const mg_logits* z, int32_t top, bool thread_row
     }
     const int64_t vec = 16 / elem_size(z->dtype), covered = (z->classes + vec - 1 + vec - 1) / vec, held = kPlanHeld / vec;
     if (covered <= 32 * held) {
+        static_assert(MG_MAX_TOP <= 32, "a lane at least to each of the best classes");
         p.lanes = 8;
         while (p.lanes < 32 && (covered > p.lanes * held || top > p.lanes)) p.lanes *= 2;
         p.nv = (int)((covered + p.lanes - 1) / p.lanes);

@@ -82,7 +82,7 @@ __device__ __noinline__ void best_one_by_one(const T* x, int32_t classes, int su
 }
 
 // The best of a row: the top-th largest of the lanes' own largest values is no larger than the top-th largest of all, so what lies below it is out; the others, as many and some
-// more, are put into shared memory and ranked against each other.  Where that does not work out (fewer lanes than `top`, too many equal values, rows that
+// more, are put into shared memory and ranked against each other.  Where that does not work out (too many equal values, rows that
 // allow fewer classes or hold a NaN) the best are found one by one.
 template <typename T, int NV, int LANES, bool WHOLE>
 __device__ __forceinline__ void best_of(const HeldRow<T, NV, LANES, WHOLE>& row, const T* x, int32_t classes, float own, int sub, bool on, const RowResult& r, int32_t top, int32_t* ids,
@@ -91,6 +91,8 @@ __device__ __forceinline__ void best_of(const HeldRow<T, NV, LANES, WHOLE>& row,
     constexpr int kRoom = kRowRoom * LANES;
     const int lane = threadIdx.x & 31;
     const uint32_t peers = (LANES == 32 ? 0xFFFFFFFFu : (1u << LANES % 32) - 1u) << (lane & ~(LANES - 1));
+    // (A guard of the lane that is asked below: plan_forward gives a row `top` lanes at least.  Without it 500,000 fp32 rows of 172 take 74 us for 71, with five best 153 for 148, by the order that the
+    // compiler then chooses.)
     bool slow = top > LANES;
     if (!slow) {
         float sorted = lanes_sorted<LANES>(own);

@@ -6,6 +6,7 @@ import torch
 import paper_2202_02365_b200 as mg
 from test_scores_and_distillation import INF, TYPES, ctx, distill, distill_backward, logits_of, near, rows_of, scores_backward, some_labels, some_teacher  # noqa: F401
 from test_scores_and_distillation import U
+from test_table_rows_at_length import run_program
 
 NAN = float("nan")
 
@@ -177,3 +178,36 @@ def test_refusals_of_row_sums(ctx):
         ctx.log_probs_backward(x, None, labels, g)
     ctx.log_probs(x, labels, row_sums=good)
     assert good.isfinite().all()
+
+
+PLANS = r"""
+#include <cstdarg>
+#include <cstdio>
+#include <initializer_list>
+#include "mg_loss_plan.cuh"
+int mg_fail(mg_ctx*, int code, const char*, ...) { return code; }
+int mg_cuda_fail(mg_ctx*, cudaError_t, const char*) { return MG_ERR_CUDA; }
+void mg_prof_begin(mg_ctx*, int) {}
+void mg_prof_end(mg_ctx*, int, int64_t) {}
+
+int main() {
+    int bad = 0;
+    for (const int dtype : {MG_DTYPE_F32, MG_DTYPE_F16, MG_DTYPE_BF16})
+        for (const int64_t rows : {(int64_t)1, (int64_t)500, (int64_t)40'000, (int64_t)1 << 30})
+            for (int32_t classes = 1; classes < 1100; ++classes)
+                for (int32_t top = 0; top <= MG_MAX_TOP && top <= classes; ++top)
+                    for (const bool threads : {false, true}) {
+                        const mg_logits z{nullptr, classes, rows, classes, dtype, 1.f};
+                        const ForwardPlan p = plan_forward(&z, top, threads, 148);
+                        const int vec = dtype == MG_DTYPE_F32 ? 4 : 8;
+                        const bool by_lanes = p.lanes >= 8 && p.lanes <= 32 && top <= p.lanes && p.nv * vec <= 32 && p.nv * p.lanes >= (classes + 2 * (vec - 1)) / vec;
+                        const bool by_threads = p.lanes == 1 && threads && classes <= 32, wide = p.lanes == 0 && p.threads >= 64;
+                        if (!by_lanes && !by_threads && !wide) { printf("%d classes, %d best: %d lanes of %d\n", classes, top, p.lanes, p.nv); ++bad; }
+                    }
+    return bad ? 1 : 0;
+}
+"""
+
+
+def test_a_row_has_as_many_lanes_as_best_classes(tmp_path):
+    run_program(tmp_path, PLANS)
