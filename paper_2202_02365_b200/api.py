@@ -949,12 +949,14 @@ class Context:
     # -- losses
     def _logits(self, x: torch.Tensor, scale: float, row_sums: torch.Tensor | None):
         x, stride = _matrix(x, self.device)
-        spec = LogitsSpec(x.data_ptr(), stride, x.shape[:-1].numel(), x.shape[-1], ROW_TYPES[x.dtype], scale)
+        of = x.shape
+        shape = of[:-1]
+        spec = LogitsSpec(x.data_ptr(), stride, shape.numel(), of[-1], ROW_TYPES[x.dtype], scale)
         if row_sums is not None:
             assert row_sums.device == self.device and row_sums.dtype == torch.float32, "row_sums: a float32 tensor on the context's device"
-            assert row_sums.shape == (*x.shape[:-1], 2) and row_sums.is_contiguous(), "row_sums: two values for each row, one behind the other"
+            assert row_sums.shape == (*shape, 2) and row_sums.is_contiguous(), "row_sums: two values for each row, one behind the other"
             spec.row_sums = row_sums.data_ptr()
-        return x, spec
+        return x, shape, spec
 
     def _labels(self, labels, shape):
         if labels is None:
@@ -968,8 +970,7 @@ class Context:
         entropy, lse = log sum exp z, and the `top` likeliest classes with their log probabilities, equal ones by ascending class.  fp32, queued on torch's
         current stream.  A logit of -infinity is a class that is not allowed.  The gradients are log_probs_backward's; row_sums, a contiguous float32 tensor [..., 2], is
         filled for them."""
-        x, spec = self._logits(logits, scale, row_sums)
-        shape = x.shape[:-1]
+        x, shape, spec = self._logits(logits, scale, row_sums)
         labels, wide = self._labels(labels, shape)
         block = torch.empty((2 if labels is None else 3, *shape), dtype=torch.float32, device=self.device).unbind(0)
         ids = torch.empty((*shape, top), dtype=torch.int32, device=self.device) if top > 0 else None
@@ -986,8 +987,7 @@ class Context:
         d_entropy) entropy as log_probs gave them.  out may be the logits.  Probabilities by lse are off by a share of themselves of up to 2^-24 |lse|, and wrong where a
         mask of -1e9, say, or of the type's lowest value covers a row all over; by row_sums, as log_probs or distill filled them for these logits and this scale, they
         are as exact as the forward call's (lse may then be None)."""
-        x, spec = self._logits(logits, scale, row_sums)
-        shape = x.shape[:-1]
+        x, shape, spec = self._logits(logits, scale, row_sums)
         labels, wide = self._labels(labels, shape)
         lse, g, h, l = (_by_row(t, shape, self.device, what) for t, what in ((lse, "lse"), (d_log_prob, "d_log_prob"), (d_entropy, "d_entropy"), (d_lse, "d_lse")))
         entropy = _by_row(entropy, shape, self.device, "entropy")
@@ -1013,8 +1013,7 @@ class Context:
         top_log_probs, say; a class that is none, -1, is no entry).  q = softmax of scale * teacher_logits over the entries (with teacher_lse: exp(scale *
         teacher_logits - teacher_lse), the teacher's probabilities as they are), loss = sum q (log q - log p), p = softmax of scale * logits.  A temperature T is a
         scale of 1 / T.  fp32, queued on torch's current stream; the gradient is distill_backward's, for which row_sums is filled as by log_probs."""
-        x, spec = self._logits(logits, scale, row_sums)
-        shape = x.shape[:-1]
+        x, shape, spec = self._logits(logits, scale, row_sums)
         teacher, held = self._teacher(teacher_ids, teacher_logits, teacher_lse, shape)
         loss, lse = torch.empty((2, *shape), dtype=torch.float32, device=self.device).unbind(0)
         self._check(self.lib.mg_distill(self.handle, C.byref(spec), C.byref(teacher), loss.data_ptr(), lse.data_ptr(), torch._C._cuda_getCurrentRawStream(self.device.index)))
@@ -1025,8 +1024,7 @@ class Context:
                          row_sums: torch.Tensor | None = None) -> torch.Tensor:
         """Gradient of distill's loss with respect to the logits, from the loss's (a value for each row); lse, row_sums (see log_probs_backward) and the rest as in the
         forward call.  out may be the logits."""
-        x, spec = self._logits(logits, scale, row_sums)
-        shape = x.shape[:-1]
+        x, shape, spec = self._logits(logits, scale, row_sums)
         teacher, held = self._teacher(teacher_ids, teacher_logits, teacher_lse, shape)
         lse, d_loss = _by_row(lse, shape, self.device, "lse"), _by_row(d_loss, shape, self.device, "d_loss")
         out, stride = _result(out, x)
