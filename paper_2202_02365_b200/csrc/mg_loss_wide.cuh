@@ -1,6 +1,6 @@
 // Wide rows of logits, forward: a block or a cluster of them goes along a row, whose vectors every thread has brought to places of its own in shared memory some rounds ahead:
 // no registers wait for them, and no thread for another's.  8,192 bf16 rows of 32,000 against a teacher's 64 pairs: 91 us (5.8 TB/s), more where one follows the other at a lower clock;
-// 4,096 of 50,257 with twenty best 113, without 74.  Bound by instructions: five to seven a value (two for the conversion and the largest, one exponential at 16 a cycle and SM, sums in pairs)
+// 4,096 of 50,257 with twenty best 109 to 119 (by box and clock), without 72 to 74.  Bound by instructions: five to seven a value (two for the conversion and the largest, one exponential at 16 a cycle and SM, sums in pairs)
 // and 300 to 1,000 a warp and row.  Measured and taken back: vectors in registers, eight of them to a thread in segments (119; 143 with twenty best), the same by blocks that stay and ask for
 // the next row's vectors early (141 - 230).
 #pragma once

@@ -2,7 +2,7 @@
 //
 // The sorted places are cut into chunks.  A part of a warp goes along a chunk's places, adds up rows and writes a sum where the id changes; an id that begins in the chunk and
 // ends no more than a chunk's length on is followed to its end, so that most ids are summed up in one go.  Of an id with more places than a chunk has, every chunk leaves
-// its share in the workspace, and a second kernel adds the shares up.  No float is added atomically.  543,000 fp32 rows of 128 into 433,750: 94 us for 504 MB, 5.4 TB/s, the shares 5; bound by
+// its share in the workspace, and a second kernel adds the shares up.  No float is added atomically.  543,000 fp32 rows of 128 into 433,750: 100 us for 504 MB, 5.0 TB/s, the shares 7; bound by
 // the latency of rows that lie anywhere, with 24 warps to an SM that have four to eight rows each on their way.
 #pragma once
 
